@@ -423,6 +423,59 @@ int dmx_step_static(int K, int64_t P, const int64_t* seg_offsets, int S, int gra
                     float* momentum, float lr, float beta, float* prev_agg, float* out_state,
                     void* cuda_stream);
 
+/*
+ * dmx_adamw_* — AdamW over n tensors in one launch, moments in fp32 or in 8-bit block codes.
+ * Per element, with s the optional gradient factor:
+ *   g = s*grad       m' = b1 m + (1-b1) g       v' = b2 v + (1-b2) g^2
+ *   p' = p (1 - lr*wd) - lr/(1-b1^t) * m' / (sqrt(v') / sqrt(1-b2^t) + eps)       (wd = 0 where decay[i] is 0)
+ * Arithmetic is fp32; parameters of type DMX_BF16 are rounded once when written.
+ *
+ * State. Tensor i owns ceil(sizes[i]/256) consecutive blocks of DMX_ADAMW_BLOCK elements, the first one at
+ * dmx_adamw_first_block(h, i), dmx_adamw_blocks(h) in all; element j of the tensor is element first*256 + j of
+ * the state arrays, which hold blocks*256 entries each (zero them before the first step; entries past a
+ * tensor's end stay zero):
+ *   state_bits 32   m, v fp32; m_scale, v_scale NULL
+ *   state_bits 8    m int8 codes c with first moment m_scale[block] * sgn(c) * (c/127)^2, v uint8 codes with
+ *                   second moment (v_scale[block] * (c/255)^2)^2; m_scale, v_scale: one fp32 per block.
+ *                   Each step writes the block's largest |m'| and sqrt(v') as its scales and the codes nearest to
+ *                   (|x|/scale)^(1/2), or, with dither != 0, floor(that + u) with u in [0,1) in steps of 2^-16
+ *                   from a hash of the element's state index (low 32 bits) and `seed`: give every step another
+ *                   seed. A nonzero second moment keeps a nonzero code. Dithering is what lets a second moment
+ *                   decay: a change of 0.1 % is far below half a code.
+ *
+ *   dmx_adamw_create     sizes: HOST, n entries >= 0 (n in 1..DMX_ADAMW_MAX_TENSORS); decay: HOST, n bytes, or
+ *                        NULL for all 1; param_dtype, grad_dtype: DMX_F32 or DMX_BF16. Synchronous.
+ *   dmx_adamw_bind       params, grads, copies: HOST arrays of n DEVICE pointers, copied to the handle's table on the
+ *                        stream (the arrays may be reused when the call returns). A NULL gradient leaves its
+ *                        tensor and its state alone. copies (NULL, or with NULL entries): bf16 copies of the
+ *                        parameters, written by every step. Pointers need their element's alignment only;
+ *                        16-byte aligned fp32 and 8-byte aligned bf16 tensors are faster. Bind again when a
+ *                        buffer moves; not inside a stream capture.
+ *   dmx_adamw_grad_norm  out[0] = sqrt(sum of squares of all bound gradients) (summed in fp64 from fp32 sums of
+ *                        eight; bitwise reproducible), out[1] = min(1, max_norm / (out[0] + 1e-6)), or NaN if
+ *                        out[0] is not finite
+ *   dmx_adamw_step       grad_scale: one fp32 or NULL (1), e.g. out + 1 of the norm. If it is NaN the step leaves
+ *                        everything as it is. t >= 1: this step's number; 0 <= beta1, beta2 < 1; eps, weight_decay >= 0
+ *   dmx_adamw_moments    the values of 8-bit moments, blocks*256 of them each, as fp32 or bf16 (out_dtype)
+ * m, v and the moments' outputs are 16-byte aligned. A handle's calls are issued on one stream at a time.
+ * Errors: DMX_ERR_ARG (also a call before bind), DMX_ERR_ALIGN, DMX_ERR_NOMEM, DMX_ERR_HANDLE, DMX_ERR_CUDA.
+ */
+#define DMX_ADAMW_BLOCK 256
+#define DMX_ADAMW_MAX_TENSORS 65536
+typedef struct dmx_adamw dmx_adamw;
+int dmx_adamw_create(int n, const int64_t* sizes, const uint8_t* decay, int param_dtype, int grad_dtype, int state_bits,
+                     dmx_adamw** out);
+int64_t dmx_adamw_blocks(const dmx_adamw* h);
+int64_t dmx_adamw_first_block(const dmx_adamw* h, int i);
+int dmx_adamw_bind(dmx_adamw* h, void* const* params, const void* const* grads, void* const* copies, void* cuda_stream);
+int dmx_adamw_grad_norm(dmx_adamw* h, float max_norm, float* out, void* cuda_stream);
+int dmx_adamw_step(dmx_adamw* h, void* m, void* v, float* m_scale, float* v_scale, const float* grad_scale, double lr,
+                   double beta1, double beta2, double eps, double weight_decay, int64_t t, int dither, uint32_t seed,
+                   void* cuda_stream);
+int dmx_adamw_moments(dmx_adamw* h, const void* m, const void* v, const float* m_scale, const float* v_scale, int out_dtype,
+                      void* out_m, void* out_v, void* cuda_stream);
+int dmx_adamw_destroy(dmx_adamw* h);   /* as dmx_destroy */
+
 /* Frees the tables and the scratch. NULL is accepted; a handle that is not live (destroyed
  * already) gives DMX_ERR_HANDLE. The caller makes sure no step of this handle is still running. */
 int dmx_destroy(dmx_handle* h);

@@ -23,7 +23,9 @@ EXPORTS = ("dmx_create", "dmx_state_len", "dmx_step", "dmx_step_adam", "dmx_step
            "dmx_launches_per_step", "dmx_destroy", "dmx_strerror", "dmx_last_cuda_error", "dmx_agg_create",
            "dmx_agg_push", "dmx_agg_destroy", "dmx_ctl_num_features", "dmx_ctl_num_weights", "dmx_ctl_decide", "dmx_plan_chunks",
            "dmx_shard_range", "dmx_shard_segments", "dmx_partials_len", "dmx_step_partial", "dmx_step_adam_partial",
-           "dmx_finalize_partials", "dmx_check_guards", "dmx_selftest_wait", "dmx_scratch_info")
+           "dmx_finalize_partials", "dmx_check_guards", "dmx_selftest_wait", "dmx_scratch_info",
+           "dmx_adamw_create", "dmx_adamw_blocks", "dmx_adamw_first_block", "dmx_adamw_bind", "dmx_adamw_grad_norm", "dmx_adamw_step",
+           "dmx_adamw_moments", "dmx_adamw_destroy")
 CTL_ACTIONS = (-100, -25, 0, 25, 100)
 
 _lib = None
@@ -98,6 +100,23 @@ def lib():
         L.dmx_check_guards.restype = i32
         L.dmx_selftest_wait.argtypes = [vp, ctypes.c_uint32, ctypes.POINTER(i32), ctypes.POINTER(ctypes.c_double), vp]
         L.dmx_selftest_wait.restype = i32
+        f64, u32 = ctypes.c_double, ctypes.c_uint32
+        L.dmx_adamw_create.argtypes = [i32, vp, vp, i32, i32, i32, ctypes.POINTER(vp)]
+        L.dmx_adamw_create.restype = i32
+        L.dmx_adamw_blocks.argtypes = [vp]
+        L.dmx_adamw_blocks.restype = i64
+        L.dmx_adamw_first_block.argtypes = [vp, i32]
+        L.dmx_adamw_first_block.restype = i64
+        L.dmx_adamw_bind.argtypes = [vp, vp, vp, vp, vp]
+        L.dmx_adamw_bind.restype = i32
+        L.dmx_adamw_grad_norm.argtypes = [vp, f32, vp, vp]
+        L.dmx_adamw_grad_norm.restype = i32
+        L.dmx_adamw_step.argtypes = [vp, vp, vp, vp, vp, vp, f64, f64, f64, f64, f64, i64, i32, u32, vp]
+        L.dmx_adamw_step.restype = i32
+        L.dmx_adamw_moments.argtypes = [vp, vp, vp, vp, vp, i32, vp, vp, vp]
+        L.dmx_adamw_moments.restype = i32
+        L.dmx_adamw_destroy.argtypes = [vp]
+        L.dmx_adamw_destroy.restype = i32
         L.dmx_destroy.argtypes = [vp]
         L.dmx_destroy.restype = i32
         L.dmx_strerror.argtypes = [i32]

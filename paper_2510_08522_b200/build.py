@@ -19,10 +19,10 @@ LIBDIR = os.path.join(_PKG, "lib")
 INCLUDE = os.path.join(_ROOT, "include")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-shared", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
+              "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 
 TARGETS = {
-    "libdmx.so": (["dmx.cu", "dmx_static.cu", "dmx_agg.cu", "dmx_ctl.cu"], ["dmx_kernels.cuh", "dmx_host.h", os.path.join(INCLUDE, "dmx.h")]),
+    "libdmx.so": (["dmx.cu", "dmx_static.cu", "dmx_agg.cu", "dmx_ctl.cu", "dmx_adamw.cu"], ["dmx_kernels.cuh", "dmx_host.h", os.path.join(INCLUDE, "dmx.h")]),
     "libdmx_gen.so": (["dmx_gen.cu"], []),
 }
 
@@ -34,6 +34,11 @@ def _nvcc() -> str:
     return "nvcc"
 
 
+def _newer(path: str, than: list) -> bool:
+    """path exists and is at least as new as every file of `than`."""
+    return os.path.exists(path) and all(os.path.getmtime(path) >= os.path.getmtime(d) for d in than)
+
+
 def lib_path(name: str) -> str:
     return os.path.join(LIBDIR, name)
 
@@ -42,36 +47,45 @@ CHECKED = {"libdmx_checked.so": TARGETS["libdmx.so"]}
 
 
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> None:
-    """Compile the targets that are missing or older than their sources; the nvcc runs of different
-    targets go side by side (each takes about a minute and a half, nearly all of it in dmx.cu)."""
+    """Bring the targets up to date: every source file is compiled to an object of its own (lib/_build/),
+    the missing and the stale ones side by side, and the objects are linked. (dmx.cu alone takes about a
+    minute and a half.)"""
     from concurrent.futures import ThreadPoolExecutor
     os.makedirs(LIBDIR, exist_ok=True)
     targets = dict(TARGETS)
     if checked:
         targets.update(CHECKED)
-    jobs = []
+    compiles, links = [], []
     for name, (srcs, deps) in targets.items():
         out = lib_path(name)
-        srcs_abs = [os.path.join(CSRC, s) for s in srcs]
-        deps_abs = srcs_abs + [d if os.path.isabs(d) else os.path.join(CSRC, d) for d in deps]
-        if not force and os.path.exists(out) and all(os.path.getmtime(out) >= os.path.getmtime(d) for d in deps_abs):
-            continue
-        tmp = "%s.%d.tmp" % (out, os.getpid())
-        cmd = ([_nvcc()] + NVCC_FLAGS + (["-DDMX_DEBUG"] if name in CHECKED else []) +
-               (["-Xptxas", "-v"] if verbose else []) + srcs_abs + ["-o", tmp])
-        jobs.append((cmd, tmp, out))
+        deps_abs = [d if os.path.isabs(d) else os.path.join(CSRC, d) for d in deps]
+        objs, stale = [], False
+        for src in (os.path.join(CSRC, s) for s in srcs):
+            obj = os.path.join(LIBDIR, "_build", "%s.%s.o" % (name[:-3], os.path.basename(src)))
+            objs.append(obj)
+            if force or not _newer(obj, [src] + deps_abs):
+                stale = True
+                flags = NVCC_FLAGS + (["-DDMX_DEBUG"] if name in CHECKED else []) + (["-Xptxas", "-v"] if verbose else [])
+                compiles.append(([_nvcc()] + flags + ["-c", src], obj))
+        if stale or not _newer(out, objs):
+            links.append(([_nvcc()] + NVCC_FLAGS + ["-shared"] + objs, out))
 
     def run(job):
-        cmd, tmp, out = job
+        cmd, out = job
+        tmp = "%s.%d.tmp" % (out, os.getpid())
+        cmd = cmd + ["-o", tmp]
         if verbose:
             print(" ".join(cmd), flush=True)
         subprocess.check_call(cmd)
         os.replace(tmp, out)
 
-    if jobs:
-        with ThreadPoolExecutor(max_workers=1 if verbose else len(jobs)) as pool:   # verbose: keep ptxas' output in order
-            for _ in pool.map(run, jobs):       # re-raises the first failure
-                pass
+    for jobs in (compiles, links):
+        if jobs:
+            os.makedirs(os.path.join(LIBDIR, "_build"), exist_ok=True)
+            # verbose: one at a time, which keeps ptxas' output in order
+            with ThreadPoolExecutor(max_workers=1 if verbose else min(len(jobs), os.cpu_count() or 1)) as pool:
+                for _ in pool.map(run, jobs):       # re-raises the first failure
+                    pass
 
 
 if __name__ == "__main__":

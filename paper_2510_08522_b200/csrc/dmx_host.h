@@ -40,7 +40,7 @@ void pack_workers(int K, const void* const* grad_ptrs, const int32_t* batch_size
 // points look it up instead of reading through the pointer, so a call on a destroyed handle
 // returns DMX_ERR_HANDLE without touching freed memory. (An address that a later create
 // happens to reuse names the new handle: the usual limit of pointer handles.)
-enum HandleKind { kStepHandle = 1, kAggHandle = 2 };
+enum HandleKind { kStepHandle = 1, kAggHandle = 2, kAdamwHandle = 3 };
 void live_add(const void* p, int kind);
 bool live_has(const void* p, int kind);
 bool live_remove(const void* p, int kind);   // false if it was not registered

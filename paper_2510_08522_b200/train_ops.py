@@ -1,0 +1,168 @@
+"""The training operators of include/dmx.h for torch callers: AdamW over many tensors.
+
+Tensors in, raw pointers through the C ABI; every call runs on the current stream of its tensors' device, takes its
+workspace from torch's allocator there, and raises DmxError with the library's code for arguments it refuses.
+Nothing synchronises.
+"""
+from __future__ import annotations
+
+import ctypes
+
+from . import binding as B
+
+ADAMW_BLOCK = 256
+
+_torch = None
+_dtypes = None
+
+
+def _t():
+    global _torch, _dtypes
+    if _torch is None:
+        import torch
+        _torch, _dtypes = torch, {torch.float32: B.F32, torch.bfloat16: B.BF16}
+    return _torch
+
+
+def _stream(x):
+    return _torch._C._cuda_getCurrentRawStream(x.device.index)
+
+
+def _refuse(where, code=B.ERR_ARG):
+    raise B.DmxError(code, where)
+
+
+class _on:
+    """Makes a tensor's device current for a call (launches go to the current device)."""
+    __slots__ = ("guard",)
+
+    def __init__(self, x):
+        self.guard = None if x.device.index == _torch.cuda.current_device() else _torch.cuda.device(x.device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *a):
+        if self.guard is not None:
+            self.guard.__exit__(*a)
+
+
+def _ptr(x):
+    return None if x is None else x.data_ptr()
+
+
+class AdamW:
+    """AdamW over a list of tensors (dmx_adamw_*). The tensors stay the caller's and are updated in place.
+
+    params, grads: lists of CUDA tensors, any shapes, dense; one dtype (fp32 or bf16) for all of each list. A None
+    gradient leaves its tensor alone. copies: bf16 tensors that receive the updated parameters (entries may be None).
+    decay: one truth value per tensor (default: all). state_bits: 32 or 8.
+    The moments are the caller's too: `new_state()` makes zeroed ones, `state_view(x, i)` is tensor i's part.
+    """
+
+    def __init__(self, params, grads, state_bits=32, copies=None, decay=None):
+        torch = _t()
+        self._h = None
+        params, n = list(params), len(params)
+        if n == 0 or (decay is not None and len(decay) != n) or params[0].dtype not in _dtypes or not params[0].is_cuda:
+            _refuse("AdamW (params)")
+        self.device, self.bits, self._params, self._dtype = params[0].device, int(state_bits), params, params[0].dtype
+        self._grad_dtype = next((g.dtype for g in grads if g is not None), torch.float32)
+        if self._grad_dtype not in _dtypes:
+            _refuse("AdamW (gradient dtype)")
+        self._sizes = [p.numel() for p in params]
+        sizes = (ctypes.c_int64 * n)(*self._sizes)
+        dec = None if decay is None else (ctypes.c_uint8 * n)(*[1 if d else 0 for d in decay])
+        h = ctypes.c_void_p()
+        with torch.cuda.device(self.device):
+            rc = B.lib().dmx_adamw_create(n, sizes, dec, _dtypes[self._dtype], _dtypes[self._grad_dtype], self.bits, ctypes.byref(h))
+        if rc != B.OK:
+            _refuse("dmx_adamw_create", rc)
+        self._h, self._destroy = h, B.lib().dmx_adamw_destroy     # (module globals may be gone when __del__ runs)
+        self.blocks = B.lib().dmx_adamw_blocks(h)
+        self.bind(grads, copies)
+
+    def bind(self, grads, copies=None):
+        """Take these gradient (and copy) tensors from now on; needed when their memory moves."""
+        n = len(self._params)
+        if len(grads) != n or (copies is not None and len(copies) != n):
+            _refuse("AdamW.bind")
+        for xs, dtype in ((self._params, self._dtype), (grads, self._grad_dtype), (copies or [], _torch.bfloat16)):
+            for x, size in zip(xs, self._sizes):
+                if x is not None and (x.dtype != dtype or x.numel() != size or x.device != self.device or not x.is_contiguous()):
+                    _refuse("AdamW.bind (tensor)")
+        arr = lambda xs: (ctypes.c_void_p * n)(*[None if x is None else x.data_ptr() for x in xs])  # noqa: E731
+        with _on(self._params[0]):
+            rc = B.lib().dmx_adamw_bind(self._h, arr(self._params), arr(grads), arr(copies) if copies is not None else None, _stream(self._params[0]))
+        if rc != B.OK:
+            _refuse("dmx_adamw_bind", rc)
+        self._grads, self._copies = list(grads), copies      # kept alive: the handle holds their addresses
+
+    def new_state(self):
+        """(m, v, m_scale, v_scale), zeroed; the scales are None for 32-bit moments."""
+        torch, n = _torch, self.blocks * ADAMW_BLOCK
+        if self.bits == 32:
+            return torch.zeros(n, device=self.device), torch.zeros(n, device=self.device), None, None
+        return (torch.zeros(n, dtype=torch.int8, device=self.device), torch.zeros(n, dtype=torch.uint8, device=self.device),
+                torch.zeros(self.blocks, device=self.device), torch.zeros(self.blocks, device=self.device))
+
+    def state_view(self, x, i):
+        """Tensor i's entries of a state array with one entry per element."""
+        first = B.lib().dmx_adamw_first_block(self._h, i)
+        if first < 0:
+            _refuse("dmx_adamw_first_block", int(first))
+        return x[first * ADAMW_BLOCK: first * ADAMW_BLOCK + self._sizes[i]].view(self._params[i].shape)
+
+    def _check(self, where, m, v, m_scale, v_scale):
+        t, n = _torch, self.blocks * ADAMW_BLOCK
+        kinds = ((m, t.float32, n), (v, t.float32, n)) if self.bits == 32 else (
+            (m, t.int8, n), (v, t.uint8, n), (m_scale, t.float32, self.blocks), (v_scale, t.float32, self.blocks))
+        for x, dtype, size in kinds:
+            if x is None or x.dtype != dtype or x.numel() != size or x.device != self.device or not x.is_contiguous():
+                _refuse(where)
+
+    def grad_norm(self, max_norm, out=None):
+        """out[0] = the gradients' global norm, out[1] = min(1, max_norm / (norm + 1e-6)) (NaN: not finite)."""
+        if out is None:
+            out = _torch.empty(2, device=self.device)
+        elif out.dtype != _torch.float32 or out.numel() != 2 or out.device != self.device or not out.is_contiguous():
+            _refuse("AdamW.grad_norm (out)")
+        with _on(out):
+            rc = B.lib().dmx_adamw_grad_norm(self._h, max_norm, out.data_ptr(), _stream(out))
+        if rc != B.OK:
+            _refuse("dmx_adamw_grad_norm", rc)
+        return out
+
+    def step(self, m, v, m_scale=None, v_scale=None, *, lr, t, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, grad_scale=None, seed=None):
+        """One update. t: this step's number, from 1. seed: dither 8-bit codes with it (None: to nearest)."""
+        self._check("AdamW.step (state)", m, v, m_scale, v_scale)
+        if grad_scale is not None and (grad_scale.dtype != _torch.float32 or grad_scale.numel() != 1 or grad_scale.device != self.device):
+            _refuse("AdamW.step (grad_scale)")
+        with _on(m):
+            rc = B.lib().dmx_adamw_step(self._h, m.data_ptr(), v.data_ptr(), _ptr(m_scale), _ptr(v_scale), _ptr(grad_scale), lr, beta1, beta2, eps,
+                                        weight_decay, t, 0 if seed is None else 1, 0 if seed is None else seed & 0xFFFFFFFF, _stream(m))
+        if rc != B.OK:
+            _refuse("dmx_adamw_step", rc)
+
+    def moments(self, m, v, m_scale, v_scale, out_m=None, out_v=None):
+        """The values of 8-bit moments (fp32 unless outputs are given)."""
+        self._check("AdamW.moments (state)", m, v, m_scale, v_scale)
+        out_m = _torch.empty(m.numel(), device=self.device) if out_m is None else out_m
+        out_v = _torch.empty(m.numel(), dtype=out_m.dtype, device=self.device) if out_v is None else out_v
+        for o in (out_m, out_v):
+            if o.dtype not in _dtypes or o.dtype != out_m.dtype or o.numel() != m.numel() or o.device != self.device or not o.is_contiguous():
+                _refuse("AdamW.moments (outputs)")
+        with _on(m):
+            rc = B.lib().dmx_adamw_moments(self._h, m.data_ptr(), v.data_ptr(), _ptr(m_scale), _ptr(v_scale), _dtypes[out_m.dtype],
+                                           out_m.data_ptr(), out_v.data_ptr(), _stream(m))
+        if rc != B.OK:
+            _refuse("dmx_adamw_moments", rc)
+        return out_m, out_v
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self._destroy(self._h)
+            self._h = None
+
+    __del__ = close
