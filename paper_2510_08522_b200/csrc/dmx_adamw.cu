@@ -14,8 +14,10 @@
 // to nearest, a second moment that decays by 0.1 % a step would never leave its code.
 // Everything between reading and writing the codes is fp32.
 //
-// Bound: HBM. A step moves 8 + grad + states (16, or 4 with 8-bit codes) + copy bytes per element and does
-// ~40 operations on them. A warp owns one block of 256 elements (its scales need a maximum over the block:
+// Bound: HBM. A step moves 8 + grad + states (16, or 4 with 8-bit codes) + copy bytes per element. Measured on
+// B200: 138 M parameters, all fp32: 566 us = 6.85 TB/s (measured copy rate 6.55); 340 M parameters, bf16
+// gradients and copies, 8-bit moments: 920 us = 5.9 TB/s, where some 70 instructions per element (a third of them the
+// dither) keep the issue slots nearly as busy as the memory; without dither 895 us. A warp owns one block of 256 elements (its scales need a maximum over the block:
 // one redux instruction), eight per lane as two groups of four neighbours, so every access of an aligned
 // tensor is 16 bytes of fp32, 8 of bf16 or 4 of codes per lane and a warp's lines are full. A tensor whose
 // start is not so aligned (a segment of a flat vector) takes its parameters and gradients element by element,
@@ -27,6 +29,7 @@
 #include <math.h>
 #include <new>
 #include <string.h>
+#include <type_traits>
 #include <vector>
 
 #include "dmx_host.h"
@@ -35,6 +38,14 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
+// A step's CTAs. With 8-bit moments a CTA is one warp with eight blocks, 32 CTAs per SM at 64 registers: the long
+// arithmetic makes warps drift apart, and a CTA of several holds its slot until the last one is done (340 M
+// parameters: 8 warps 1077 us, 4 warps 975 us, 2 warps 927 us, 1 warp 919-927 us). With fp32 moments there is
+// little arithmetic, and eight warps that sweep 32 neighbouring blocks do better (138 M: 566 us against 590).
+template <int BITS>
+constexpr int kStepThreads = BITS == 8 ? 32 : 256;
+template <int BITS>
+constexpr int kStepCtas = BITS == 8 ? 32 : 3;
 constexpr int kBlock = DMX_ADAMW_BLOCK;
 static_assert(kBlock == 256, "a lane holds eight elements of a block");
 
@@ -60,7 +71,7 @@ struct StepArgs {
   void *m, *v;
   float *m_scale, *v_scale;
   const float* grad_scale;
-  float b1, omb1, b2, omb2, eps, keep, rs_bc2, step;
+  float b1, omb1, b2, omb2, eps, keep, rs_bc2, step, one;
   unsigned key;
 };
 
@@ -92,89 +103,119 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, const float* x) {
   __stcs(reinterpret_cast<uint2*>(p), make_uint2(bf_pack(x[0], x[1]), bf_pack(x[2], x[3])));
 }
 
-// Eight elements of a lane: element e of the block is at slot j with e = at(j, lane, vec).
-// vec: two groups of four neighbours; otherwise neighbours go to neighbouring lanes.
-__device__ __forceinline__ int at(int j, int lane, bool vec) {
-  return vec ? (j >> 2) * 128 + lane * 4 + (j & 3) : j * 32 + lane;
+// A lane's eight elements of a block: slot j holds element at<VEC>(j, lane). VEC: two groups of four neighbours;
+// otherwise neighbours go to neighbouring lanes and `left` elements exist.
+template <bool VEC>
+__device__ __forceinline__ int at(int j, int lane) {
+  return VEC ? (j >> 2) * 128 + lane * 4 + (j & 3) : j * 32 + lane;
 }
-
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, float* x, int lane, bool vec, int left) {
-  if (vec && left >= kBlock) {
+template <bool VEC, typename T>
+__device__ __forceinline__ void load8(const T* p, float* x, int lane, int left) {
+  if constexpr (VEC) {
     load4(p + lane * 4, x);
     load4(p + 128 + lane * 4, x + 4);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int e = at(j, lane, vec);
-      x[j] = e < left ? wide(p[e]) : 0.f;
-    }
+    for (int j = 0; j < 8; ++j) x[j] = at<false>(j, lane) < left ? wide(p[at<false>(j, lane)]) : 0.f;
   }
 }
-template <typename T>
-__device__ __forceinline__ void store8(T* p, const float* x, int lane, bool vec, int left) {
-  if (vec && left >= kBlock) {
+template <bool VEC, typename T>
+__device__ __forceinline__ void store8(T* p, const float* x, int lane, int left) {
+  if constexpr (VEC) {
     store4(p + lane * 4, x);
     store4(p + 128 + lane * 4, x + 4);
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int e = at(j, lane, vec);
-      if (e < left) narrow(x[j], p + e);
-    }
+    for (int j = 0; j < 8; ++j)
+      if (at<false>(j, lane) < left) narrow(x[j], p + at<false>(j, lane));
   }
 }
+
+// A lane's eight codes as two words, slot j in byte j & 3 of word j >> 2. With VEC they lie so in memory. Otherwise
+// a slot's codes lie across the lanes: lane 4a + r of a quad takes the word of elements 4a..4a+3 of slot
+// 4q + r, and the quad transposes its four words of four bytes (an involution, so it serves both ways).
+__device__ __forceinline__ unsigned transpose4(unsigned w, int lane) {
+  unsigned p = __shfl_xor_sync(0xffffffffu, w, 1);
+  w = __byte_perm(w, p, lane & 1 ? 0x3715 : 0x6240);
+  p = __shfl_xor_sync(0xffffffffu, w, 2);
+  return __byte_perm(w, p, lane & 2 ? 0x3276 : 0x5410);
+}
+template <bool VEC>
+__device__ __forceinline__ int word_of(int q, int lane) {
+  return VEC ? q * 32 + lane : (q * 4 + (lane & 3)) * 8 + (lane >> 2);
+}
+template <bool VEC>
+__device__ __forceinline__ void load_codes(const void* p, unsigned* w, int lane) {
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    w[q] = __ldcs(static_cast<const unsigned*>(p) + word_of<VEC>(q, lane));
+    if constexpr (!VEC) w[q] = transpose4(w[q], lane);
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void store_codes(void* p, const unsigned* w, int lane) {
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+    __stcs(static_cast<unsigned*>(p) + word_of<VEC>(q, lane), VEC ? w[q] : transpose4(w[q], lane));
+}
+
+// Pairs of elements go through the packed fp32 instructions of sm_100 (each half IEEE fp32, round to nearest
+// unless named otherwise): half the issue slots.
+// A packed product that feeds a packed sum is contracted to one rounding even where both name theirs (seen in
+// results); where two are wanted the sum is an fma with a factor of 1 that only the launch knows.
+__device__ __forceinline__ unsigned long long bits2(float2 x) {
+  unsigned long long r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x.x), "f"(x.y));
+  return r;
+}
+__device__ __forceinline__ float2 float2_of(unsigned long long b) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(b));
+  return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)));
+  return float2_of(r);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  unsigned long long r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)));
+  return float2_of(r);
+}
+__device__ __forceinline__ float2 add2_down(float2 a, float2 b) {
+  unsigned long long r;
+  asm("add.rm.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)));
+  return float2_of(r);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  unsigned long long r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
+  return float2_of(r);
+}
+__device__ __forceinline__ float2 two(float x) { return make_float2(x, x); }
+__device__ __forceinline__ float2 abs2(float2 x) { return make_float2(fabsf(x.x), fabsf(x.y)); }
 
 // Codes as floats and back without the conversion unit (a quarter as fast as the multipliers, and busy with
 // the roots): a byte in the low mantissa bits of 2^23 is that number plus 2^23, and an addition to 2^23 that
 // rounds down leaves the floor in those bits.
 constexpr float kMagic = 8388608.f;   // 2^23
-__device__ __forceinline__ float byte_float(unsigned w, int j) {   // byte j of w, plus 2^23
-  return __uint_as_float(__byte_perm(w, 0x4b000000u, 0x7440 + j));
+template <int J>
+__device__ __forceinline__ float2 byte_floats(unsigned w) {   // bytes J and J+1 of w, plus 2^23
+  return make_float2(__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7440 + J)), __uint_as_float(__byte_perm(w, 0x4b000000u, 0x7440 + J + 1)));
 }
-__device__ __forceinline__ unsigned floor_bits(float x) {          // floor(x) in the low bits, x >= 0
-  return __float_as_uint(__fadd_rd(x, kMagic));
+// two codes of the first moment: S a |a|, a = c/127 (c is held as c + 128 by the xor)
+template <int J>
+__device__ __forceinline__ float2 decode_m(unsigned w, float S) {
+  const float2 a = mul2(add2(byte_floats<J>(w ^ 0x80808080u), two(-kMagic - 128.f)), two(1.f / 127.f));
+  return mul2(mul2(a, abs2(a)), two(S));
 }
-// four codes of the first moment: S a |a|, a = c/127 (c is held as c + 128 by the xor)
-__device__ __forceinline__ void decode_m(unsigned w, float S, float* x) {
-  w ^= 0x80808080u;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float a = (byte_float(w, j) - (kMagic + 128.f)) * (1.f / 127.f);
-    x[j] = a * fabsf(a) * S;
-  }
-}
-// four codes of the second: (R a^2)^2, a = c/255
-__device__ __forceinline__ void decode_v(unsigned w, float R, float* x) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float a = (byte_float(w, j) - kMagic) * (1.f / 255.f);
-    const float r = a * a * R;
-    x[j] = r * r;
-  }
-}
-// Two words of four codes per lane: aligned tensors take their own; the others' elements lie across the
-// lanes, so a lane fetches each element's byte.
-__device__ __forceinline__ void load_codes(const void* p, unsigned* w, int lane, bool vec) {
-  if (vec) {
-    w[0] = __ldcs(static_cast<const unsigned*>(p) + lane);
-    w[1] = __ldcs(static_cast<const unsigned*>(p) + 32 + lane);
-  } else {
-    const uint8_t* b = static_cast<const uint8_t*>(p) + lane;
-    w[0] = w[1] = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) w[j >> 2] |= (unsigned)b[j * 32] << (8 * (j & 3));
-  }
-}
-__device__ __forceinline__ void store_codes(void* p, const unsigned* w, int lane, bool vec) {
-  if (vec) {
-    __stcs(static_cast<unsigned*>(p) + lane, w[0]);
-    __stcs(static_cast<unsigned*>(p) + 32 + lane, w[1]);
-  } else {
-    uint8_t* b = static_cast<uint8_t*>(p) + lane;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) b[j * 32] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
-  }
+// two codes of the second: (R a^2)^2, a = c/255
+template <int J>
+__device__ __forceinline__ float2 decode_v(unsigned w, float R) {
+  const float2 a = mul2(add2(byte_floats<J>(w), two(-kMagic)), two(1.f / 255.f));
+  const float2 r = mul2(mul2(a, a), two(R));
+  return mul2(r, r);
 }
 __device__ __forceinline__ unsigned pack4(const unsigned* c) {     // the low bytes of four words
   return __byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410);
@@ -183,127 +224,245 @@ __device__ __forceinline__ unsigned pack4(const unsigned* c) {     // the low by
 // of elementary functions on the IBM RISC System/6000 processor", 1990), for what decides a code. A code is
 // read again in the next step, so a last bit there would grow into the parameters; the values that the codes
 // come from are therefore rounded operation by operation, as the formulas are written, and the codes are
-// those of plain fp32 arithmetic. Under 1.2e-38 the root loses accuracy, not its sign.
-__device__ __forceinline__ float root_of(float x) {
+// those of plain fp32 arithmetic. Under 2e-31 the root loses accuracy, not its sign.
+__device__ __forceinline__ float rsqrt_near(float x) {
   float y;
-  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(fmaxf(x, 1.1754944e-38f)));
-  const float s = x * y;
-  return fmaf(fmaf(-s, s, x), 0.5f * y, s);
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
-__device__ __forceinline__ float quotient(float a, float b, float rcp_b) {
-  const float q = a * rcp_b;
-  return fmaf(fmaf(-q, b, a), rcp_b, q);
+__device__ __forceinline__ float2 root2(float2 x) {
+  const float2 z = add2(x, two(1.2e-38f));    // nothing but a guard: x itself from 2e-31 on
+  const float2 y = make_float2(rsqrt_near(z.x), rsqrt_near(z.y));
+  const float2 s = mul2(x, y);
+  const float2 e = fma2(make_float2(-s.x, -s.y), s, x);
+  return fma2(e, mul2(y, two(0.5f)), s);
+}
+__device__ __forceinline__ float2 quotient2(float2 a, float b, float rcp_b) {
+  const float2 q = mul2(a, two(rcp_b));
+  return fma2(fma2(q, two(-b), a), two(rcp_b), q);
+}
+__device__ __forceinline__ float rcp_near(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 
-__device__ __forceinline__ unsigned mix(unsigned h) {   // Murmur3's 32-bit finaliser (Appleby)
+// The dither hash: Murmur3's 32-bit finaliser (Appleby) but for its last exchange, which only the low half sees:
+// the two uniforms are the halves of h ^ (h >> 16).
+__device__ __forceinline__ unsigned mix(unsigned h) {
   h ^= h >> 16; h *= 0x85ebca6bu;
   h ^= h >> 13; h *= 0xc2b2ae35u;
-  return h ^ (h >> 16);
+  return h;
+}
+__device__ __forceinline__ float half_float(unsigned w, unsigned sel) {   // 16 bits of w, plus 2^23
+  return __uint_as_float(__byte_perm(w, 0x4b000000u, sel));
 }
 
-template <bool ABS>
-__device__ __forceinline__ float block_max(const float* x) {   // of |x| or of non-negative x; a NaN wins
-  unsigned u = 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) u = max(u, __float_as_uint(ABS ? fabsf(x[j]) : x[j]));
-  return __uint_as_float(__reduce_max_sync(0xffffffffu, u));
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float block_max(float x) {   // over the warp, of non-negative values; a NaN wins
+  return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(x)));
 }
 
 constexpr float kTiny = 1.1754944e-38f;   // below it a reciprocal overflows: such a block is held as zeros
 
+// What a lane reads of a block.
+template <typename P, typename G, int BITS>
+struct Raw {
+  float p[8], g[8], m[BITS == 32 ? 8 : 1], v[BITS == 32 ? 8 : 1];
+  unsigned wm[2], wv[2];
+  float S, R;
+};
+
+// A chunk's places in memory; block i lies i*256 elements (i scales) further.
+template <typename P, typename G, int BITS>
+struct Place {
+  using S = typename std::conditional<BITS == 32, float, uint8_t>::type;
+  P* p;
+  const G* g;
+  __nv_bfloat16* copy;
+  S *m, *v;
+  float *ms, *vs;
+  unsigned s0;               // state index of its first element (low bits)
+};
+
+template <bool VEC, typename P, typename G, int BITS>
+__device__ __forceinline__ void fetch(Raw<P, G, BITS>& x, const Place<P, G, BITS>& at, int i, int left, int lane) {
+  const int e = i * kBlock;
+  load8<VEC>(at.g + e, x.g, lane, left);
+  load8<VEC>(at.p + e, x.p, lane, left);
+  if constexpr (BITS == 32) {
+    load8<VEC>(at.m + e, x.m, lane, kBlock);
+    load8<VEC>(at.v + e, x.v, lane, kBlock);
+  } else {
+    load_codes<VEC>(at.m + e, x.wm, lane);
+    load_codes<VEC>(at.v + e, x.wv, lane);
+    x.S = at.ms[i];
+    x.R = at.vs[i];
+  }
+}
+
+template <bool VEC, typename P, typename G, int BITS, bool DITHER>
+__device__ __forceinline__ void finish(const Raw<P, G, BITS>& x, const StepArgs& A, const Place<P, G, BITS>& to, int i, int left, float s, float keep, int lane) {
+  const int e = i * kBlock;
+  float p[8], m[8], v[8];
+  const float* g = x.g;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) p[j] = x.p[j];
+  if constexpr (BITS == 32) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { m[j] = x.m[j]; v[j] = x.v[j]; }
+  } else {
+    float2 *m2 = reinterpret_cast<float2*>(m), *v2 = reinterpret_cast<float2*>(v);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      m2[2 * q] = decode_m<0>(x.wm[q], x.S); m2[2 * q + 1] = decode_m<2>(x.wm[q], x.S);
+      v2[2 * q] = decode_v<0>(x.wv[q], x.R); v2[2 * q + 1] = decode_v<2>(x.wv[q], x.R);
+    }
+  }
+  float2 m2[4], root[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float2 gj = mul2(make_float2(g[2 * j], g[2 * j + 1]), two(s));
+    m2[j] = fma2(mul2(make_float2(m[2 * j], m[2 * j + 1]), two(A.b1)), two(A.one), mul2(gj, two(A.omb1)));
+    const float2 v2 = fma2(mul2(make_float2(v[2 * j], v[2 * j + 1]), two(A.b2)), two(A.one), mul2(mul2(gj, gj), two(A.omb2)));
+    root[j] = root2(v2);
+    const float2 den = fma2(root[j], two(A.rs_bc2), two(A.eps));
+    const float2 u = mul2(m2[j], make_float2(rcp_near(den.x), rcp_near(den.y)));
+    const float2 q = fma2(u, two(-A.step), mul2(make_float2(p[2 * j], p[2 * j + 1]), two(keep)));
+    p[2 * j] = q.x; p[2 * j + 1] = q.y;
+    m[2 * j] = m2[j].x; m[2 * j + 1] = m2[j].y;
+    v[2 * j] = v2.x; v[2 * j + 1] = v2.y;
+  }
+  store8<VEC>(to.p + e, p, lane, left);
+  if (to.copy) store8<VEC>(to.copy + e, p, lane, left);
+  if constexpr (BITS == 32) {
+    store8<VEC>(to.m + e, m, lane, kBlock);
+    store8<VEC>(to.v + e, v, lane, kBlock);
+  } else {
+    // elements past the tensor's end were read as zero gradients and zero codes: they stay zero
+    float S = 0.f, R = 0.f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      S = max_nan(S, max_nan(fabsf(m2[j].x), fabsf(m2[j].y)));
+      R = max_nan(R, max_nan(root[j].x, root[j].y));
+    }
+    S = block_max(S); R = block_max(R);
+    S = S < kTiny ? 0.f : S;
+    R = R < kTiny ? 0.f : R;
+    const float is = S == 0.f ? 0.f : 1.f / S, ir = R == 0.f ? 0.f : 1.f / R;
+    const unsigned h0 = (to.s0 + (unsigned)(e + at<VEC>(0, lane))) * 0x9e3779b1u + A.key;
+    unsigned wm[2], wv[2], cm[4], cv[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float2 um = two(0.5f), uv = two(0.5f);
+      if constexpr (DITHER) {
+        const unsigned a = mix(h0 + (unsigned)at<VEC>(2 * j, 0) * 0x9e3779b1u), b = mix(h0 + (unsigned)at<VEC>(2 * j + 1, 0) * 0x9e3779b1u);
+        um = mul2(add2(make_float2(half_float(a ^ (a >> 16), 0x7410), half_float(b ^ (b >> 16), 0x7410)), two(-kMagic)), two(0x1p-16f));
+        uv = mul2(add2(make_float2(half_float(a, 0x7432), half_float(b, 0x7432)), two(-kMagic)), two(0x1p-16f));
+      }
+      const float2 x = root2(quotient2(abs2(m2[j]), S, is)), y = root2(quotient2(root[j], R, ir));
+      float2 a = fma2(mul2(x, two(127.f)), two(A.one), um);
+      a = add2_down(a, two(kMagic));       // x <= 1 and u <= 1 - 2^-16: never above 127 (255)
+      a = add2(a, two(-kMagic));     // the code as a float; then its sign, and into the low bits as two's complement
+      a = add2(make_float2(copysignf(a.x, m2[j].x), copysignf(a.y, m2[j].y)), two(1.5f * kMagic));
+      float2 b = fma2(mul2(y, two(255.f)), two(A.one), uv);
+      // any nonzero y keeps a code of 1 at least
+      b.x = fmaxf(b.x, __saturatef(y.x * 1e38f));
+      b.y = fmaxf(b.y, __saturatef(y.y * 1e38f));
+      b = add2_down(b, two(kMagic));
+      cm[(2 * j) & 3] = __float_as_uint(a.x); cm[(2 * j + 1) & 3] = __float_as_uint(a.y);
+      cv[(2 * j) & 3] = __float_as_uint(b.x); cv[(2 * j + 1) & 3] = __float_as_uint(b.y);
+      if (j & 1) { wm[j >> 1] = pack4(cm); wv[j >> 1] = pack4(cv); }
+    }
+    store_codes<VEC>(to.m + e, wm, lane);
+    store_codes<VEC>(to.v + e, wv, lane);
+    if (lane == 0) {
+      to.ms[i] = S;
+      to.vs[i] = R;
+    }
+  }
+}
+
+// Blocks k, k + kWarps, ... below nb of a chunk that has `rest` elements, by one warp. With 8-bit moments a block's
+// loads are issued before the block ahead of it is computed: the arithmetic is long enough to idle the
+// memory otherwise. With fp32 moments the loads alone fill the
+// registers, and the SM's other warps hide them.
+template <bool VEC, typename P, typename G, int BITS, bool DITHER>
+__device__ __forceinline__ void run(const StepArgs& A, const Place<P, G, BITS>& at, int k, int nb, int64_t rest, float s, float keep, int lane) {
+  constexpr int kW = kStepThreads<BITS> / 32;
+  auto left = [&](int i) { return VEC || rest >= (i + 1) * kBlock ? kBlock : (int)(rest - i * kBlock); };
+  if (k >= nb) return;
+  Raw<P, G, BITS> x;
+  fetch<VEC>(x, at, k, left(k), lane);
+  for (; k < nb; k += kW) {
+    const int kn = k + kW;
+    if constexpr (BITS == 8) {
+      Raw<P, G, BITS> y;
+      if (kn < nb) fetch<VEC>(y, at, kn, left(kn), lane);
+      finish<VEC, P, G, BITS, DITHER>(x, A, at, k, left(k), s, keep, lane);
+      x = y;
+    } else {
+      finish<VEC, P, G, BITS, DITHER>(x, A, at, k, left(k), s, keep, lane);
+      if (kn < nb) fetch<VEC>(x, at, kn, left(kn), lane);
+    }
+  }
+}
+
 template <typename P, typename G, int BITS, bool DITHER>
-__global__ void __launch_bounds__(kThreads, 3) adamw_kernel(const __grid_constant__ StepArgs A) {
+__global__ void __launch_bounds__(kStepThreads<BITS>, kStepCtas<BITS>) adamw_kernel(const __grid_constant__ StepArgs A) {
   const float s = A.grad_scale ? __ldg(A.grad_scale) : 1.f;
   if (s != s) return;                       // the factor says: skip this step
   const Chunk c = A.chunks[blockIdx.x];
   const Tensor T = A.tensors[c.tensor];
   if (!T.g) return;
   const int lane = threadIdx.x & 31;
-  const bool vec = T.vec != 0;
   const float keep = T.decay ? A.keep : 1.f;
-  for (int k = threadIdx.x >> 5; k < c.nblocks; k += kWarps) {
-    const int64_t blk = c.first + k;
-    const int64_t e0 = blk * kBlock, rest = T.n - e0;
-    const int left = rest < kBlock ? (int)rest : kBlock;
-    const int64_t sb = T.block0 + blk, s0 = sb * kBlock;
-    float p[8], g[8], m[8], v[8];
-    P* pp = static_cast<P*>(T.p) + e0;
-    load8(static_cast<const G*>(T.g) + e0, g, lane, vec, left);
-    load8(static_cast<const P*>(pp), p, lane, vec, left);
-    if constexpr (BITS == 32) {
-      load8(static_cast<const float*>(A.m) + s0, m, lane, vec, kBlock);
-      load8(static_cast<const float*>(A.v) + s0, v, lane, vec, kBlock);
-    } else {
-      unsigned wm[2], wv[2];
-      load_codes(static_cast<const uint8_t*>(A.m) + s0, wm, lane, vec);
-      load_codes(static_cast<const uint8_t*>(A.v) + s0, wv, lane, vec);
-      const float S = A.m_scale[sb], R = A.v_scale[sb];
-      decode_m(wm[0], S, m); decode_m(wm[1], S, m + 4);
-      decode_v(wv[0], R, v); decode_v(wv[1], R, v + 4);
-    }
-    float root[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float gj = g[j] * s;
-      m[j] = __fadd_rn(__fmul_rn(m[j], A.b1), __fmul_rn(gj, A.omb1));
-      v[j] = __fadd_rn(__fmul_rn(v[j], A.b2), __fmul_rn(__fmul_rn(gj, gj), A.omb2));
-      root[j] = root_of(v[j]);
-      const float u = __fdividef(m[j], fmaf(root[j], A.rs_bc2, A.eps));
-      p[j] = fmaf(-A.step, u, p[j] * keep);
-    }
-    store8(pp, p, lane, vec, left);
-    if (T.copy) store8(T.copy + e0, p, lane, vec, left);
-    if constexpr (BITS == 32) {
-      store8(static_cast<float*>(A.m) + s0, m, lane, vec, kBlock);
-      store8(static_cast<float*>(A.v) + s0, v, lane, vec, kBlock);
-    } else {
-      // elements past the tensor's end were read as zero gradients and zero codes: they stay zero
-      float S = block_max<true>(m), R = block_max<false>(root);
-      S = S < kTiny ? 0.f : S;
-      R = R < kTiny ? 0.f : R;
-      const float is = S == 0.f ? 0.f : 1.f / S, ir = R == 0.f ? 0.f : 1.f / R;
-      unsigned cm[8], cv[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float um = 0.5f, uv = 0.5f;
-        if (DITHER) {
-          const unsigned h = mix((unsigned)(s0 + at(j, lane, vec)) * 0x9e3779b1u + A.key);
-          um = __uint_as_float(0x3f800000u | (h & 0xffffu) << 7) - 1.f;
-          uv = __uint_as_float(0x3f800000u | (h >> 16) << 7) - 1.f;
-        }
-        const float x = root_of(quotient(fabsf(m[j]), S, is)), y = root_of(quotient(root[j], R, ir));
-        const unsigned a = floor_bits(fminf(__fadd_rn(__fmul_rn(x, 127.f), um), 127.5f));
-        const unsigned neg = (unsigned)(__float_as_int(m[j]) >> 31);
-        cm[j] = (a ^ neg) - neg;
-        // any nonzero y keeps a code of 1 at least
-        cv[j] = floor_bits(fminf(fmaxf(__fadd_rn(__fmul_rn(y, 255.f), uv), __saturatef(y * 1e38f)), 255.5f));
-      }
-      unsigned wm[2] = {pack4(cm), pack4(cm + 4)}, wv[2] = {pack4(cv), pack4(cv + 4)};
-      store_codes(static_cast<uint8_t*>(A.m) + s0, wm, lane, vec);
-      store_codes(static_cast<uint8_t*>(A.v) + s0, wv, lane, vec);
-      if (lane == 0) {
-        A.m_scale[sb] = S;
-        A.v_scale[sb] = R;
-      }
-    }
+  constexpr int kW = kStepThreads<BITS> / 32;
+  const int w = threadIdx.x >> 5;
+  const int64_t e0 = c.first * kBlock, rest = T.n - e0, sb = T.block0 + c.first;
+  Place<P, G, BITS> at;
+  at.p = static_cast<P*>(T.p) + e0;
+  at.g = static_cast<const G*>(T.g) + e0;
+  at.copy = T.copy ? T.copy + e0 : nullptr;
+  at.m = static_cast<typename Place<P, G, BITS>::S*>(A.m) + sb * kBlock;
+  at.v = static_cast<typename Place<P, G, BITS>::S*>(A.v) + sb * kBlock;
+  at.ms = A.m_scale + sb;
+  at.vs = A.v_scale + sb;
+  at.s0 = (unsigned)(sb * kBlock);
+  if (T.vec) {
+    const int full = rest >= c.nblocks * kBlock ? c.nblocks : c.nblocks - 1;
+    run<true, P, G, BITS, DITHER>(A, at, w, full, rest, s, keep, lane);
+    if (full < c.nblocks && w == (full & (kW - 1)))       // the tensor's last block is a part
+      run<false, P, G, BITS, DITHER>(A, at, full, c.nblocks, rest, s, keep, lane);
+  } else {
+    run<false, P, G, BITS, DITHER>(A, at, w, c.nblocks, rest, s, keep, lane);
   }
 }
 
-// Values of 8-bit moments, for checkpoints and inspection: four codes of each moment per thread.
+// Values of 8-bit moments, for checkpoints and inspection: eight codes of each moment per thread.
+__device__ __forceinline__ void store8_flat(float* p, const float2* x) {
+  __stcs(reinterpret_cast<float4*>(p), make_float4(x[0].x, x[0].y, x[1].x, x[1].y));
+  __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(x[2].x, x[2].y, x[3].x, x[3].y));
+}
+__device__ __forceinline__ void store8_flat(__nv_bfloat16* p, const float2* x) {
+  __stcs(reinterpret_cast<uint4*>(p), make_uint4(bf_pack(x[0].x, x[0].y), bf_pack(x[1].x, x[1].y), bf_pack(x[2].x, x[2].y), bf_pack(x[3].x, x[3].y)));
+}
 template <typename O>
-__global__ void __launch_bounds__(kThreads) moments_kernel(const int8_t* __restrict__ m, const uint8_t* __restrict__ v,
+__global__ void __launch_bounds__(kThreads) moments_kernel(const uint2* __restrict__ m, const uint2* __restrict__ v,
                                                            const float* __restrict__ ms, const float* __restrict__ vs,
-                                                           O* __restrict__ om, O* __restrict__ ov, int64_t quads) {
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < quads; i += (int64_t)gridDim.x * kThreads) {
-    const unsigned a = __ldcs(reinterpret_cast<const unsigned*>(m) + i);
-    const unsigned b = __ldcs(reinterpret_cast<const unsigned*>(v) + i);
-    const float S = ms[i / (kBlock / 4)], R = vs[i / (kBlock / 4)];
-    float x[4], y[4];
-    decode_m(a, S, x);
-    decode_v(b, R, y);
-    store4(om + i * 4, x);
-    store4(ov + i * 4, y);
-  }
+                                                           O* __restrict__ om, O* __restrict__ ov, int64_t n8) {
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i >= n8) return;
+  const uint2 a = __ldcs(m + i), b = __ldcs(v + i);
+  const float S = ms[i / (kBlock / 8)], R = vs[i / (kBlock / 8)];
+  const float2 x[4] = {decode_m<0>(a.x, S), decode_m<2>(a.x, S), decode_m<0>(a.y, S), decode_m<2>(a.y, S)};
+  const float2 y[4] = {decode_v<0>(b.x, R), decode_v<2>(b.x, R), decode_v<0>(b.y, R), decode_v<2>(b.y, R)};
+  store8_flat(om + i * 8, x);
+  store8_flat(ov + i * 8, y);
 }
 
 // Global norm: a CTA's chunks by the grid's stride, squares summed eight at a time in fp32 and from there
@@ -324,7 +483,8 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const Tensor* __restrict
     for (int k = wid; k < c.nblocks; k += kWarps) {
       const int64_t e0 = (c.first + k) * kBlock, rest = T.n - e0;
       float g[8];
-      load8(static_cast<const G*>(T.g) + e0, g, lane, T.vec != 0, rest < kBlock ? (int)rest : kBlock);
+      if (T.vec && rest >= kBlock) load8<true>(static_cast<const G*>(T.g) + e0, g, lane, kBlock);
+      else load8<false>(static_cast<const G*>(T.g) + e0, g, lane, rest < kBlock ? (int)rest : kBlock);
       float q = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) q = fmaf(g[j], g[j], q);
@@ -388,9 +548,9 @@ void release(dmx_adamw* h) {
 
 template <typename P, typename G>
 void launch_step(const dmx_adamw* h, const StepArgs& A, bool dither, cudaStream_t st) {
-  if (h->bits == 32) adamw_kernel<P, G, 32, false><<<h->nchunks, kThreads, 0, st>>>(A);
-  else if (dither) adamw_kernel<P, G, 8, true><<<h->nchunks, kThreads, 0, st>>>(A);
-  else adamw_kernel<P, G, 8, false><<<h->nchunks, kThreads, 0, st>>>(A);
+  if (h->bits == 32) adamw_kernel<P, G, 32, false><<<h->nchunks, kStepThreads<32>, 0, st>>>(A);
+  else if (dither) adamw_kernel<P, G, 8, true><<<h->nchunks, kStepThreads<8>, 0, st>>>(A);
+  else adamw_kernel<P, G, 8, false><<<h->nchunks, kStepThreads<8>, 0, st>>>(A);
 }
 
 bool aligned(const void* p, unsigned a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -430,9 +590,10 @@ int dmx_adamw_create(int n, const int64_t* sizes, const uint8_t* decay, int para
   int sms = 0;
   ok = ok && dmxh::cuda_ok(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, h->device));
   if (!ok) { release(h); return DMX_ERR_CUDA; }
-  // A CTA takes four blocks per warp where that still gives every SM several CTAs; a small model is cut
-  // finer, one block per warp, so that all SMs have work.
-  const int per = blocks >= (int64_t)sms * 256 ? 4 * kWarps : kWarps;
+  // fp32 moments: four blocks per warp where that still gives every SM several CTAs; a small model is cut finer,
+  // one block per warp, so that all SMs have work (1 Mi parameters: 8.0 us cut finely, 9.0 us with twice the
+  // blocks). 8-bit moments: eight blocks for a CTA's one warp; 16 gain 1 % on 340 M and cost 10 % on 25 M.
+  const int per = state_bits == 8 || blocks < (int64_t)sms * 256 ? 8 : 32;
   try {
     h->host.resize(n);
     int64_t b0 = 0;
@@ -539,7 +700,7 @@ int dmx_adamw_step(dmx_adamw* h, void* m, void* v, float* m_scale, float* v_scal
   A.m = m; A.v = v; A.m_scale = m_scale; A.v_scale = v_scale; A.grad_scale = grad_scale;
   A.b1 = (float)beta1; A.omb1 = (float)(1.0 - beta1);
   A.b2 = (float)beta2; A.omb2 = (float)(1.0 - beta2);
-  A.eps = (float)eps;
+  A.eps = (float)eps; A.one = 1.f;
   A.keep = (float)(1.0 - lr * weight_decay);
   A.rs_bc2 = (float)(1.0 / sqrt(1.0 - pow(beta2, (double)t)));
   A.step = (float)(lr / (1.0 - pow(beta1, (double)t)));
@@ -562,18 +723,16 @@ int dmx_adamw_moments(dmx_adamw* h, const void* m, const void* v, const float* m
   if (!aligned(out_m, 16) || !aligned(out_v, 16)) return DMX_ERR_ALIGN;
   rc = dmxh::check_current_device(h->device);
   if (rc != DMX_OK) return rc;
-  const int64_t quads = h->blocks * (kBlock / 4);
-  if (quads == 0) return DMX_OK;
-  const int64_t want = (quads + kThreads - 1) / kThreads;
-  const int grid = want > 148 * 64 ? 148 * 64 : (int)want;
+  const int64_t n8 = h->blocks * (kBlock / 8);
+  if (n8 == 0) return DMX_OK;
+  const int grid = (int)((n8 + kThreads - 1) / kThreads);      // at most 2^40 / 8 / kThreads < 2^31
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const int8_t* cm = static_cast<const int8_t*>(m);
-  const uint8_t* cv = static_cast<const uint8_t*>(v);
+  const uint2 *cm = static_cast<const uint2*>(m), *cv = static_cast<const uint2*>(v);
   if (out_dtype == DMX_F32)
-    moments_kernel<float><<<grid, kThreads, 0, st>>>(cm, cv, m_scale, v_scale, static_cast<float*>(out_m), static_cast<float*>(out_v), quads);
+    moments_kernel<float><<<grid, kThreads, 0, st>>>(cm, cv, m_scale, v_scale, static_cast<float*>(out_m), static_cast<float*>(out_v), n8);
   else
     moments_kernel<__nv_bfloat16><<<grid, kThreads, 0, st>>>(cm, cv, m_scale, v_scale, static_cast<__nv_bfloat16*>(out_m),
-                                                             static_cast<__nv_bfloat16*>(out_v), quads);
+                                                             static_cast<__nv_bfloat16*>(out_v), n8);
   return dmxh::cuda_ok(cudaGetLastError()) ? DMX_OK : DMX_ERR_CUDA;
 }
 
