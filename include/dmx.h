@@ -424,6 +424,19 @@ int dmx_step_static(int K, int64_t P, const int64_t* seg_offsets, int S, int gra
                     void* cuda_stream);
 
 /*
+ * The operators on both sides of the gradient step: the layers whose backward pass makes a worker's gradient
+ * (dmx_group_norm_*) and an optimizer over a model's separate tensors (dmx_adamw_*). The paper
+ * names the models and optimizers it trains with and no formula for any of them; the formulas below are the
+ * contract. All pointers are DEVICE memory unless marked HOST, all calls are asynchronous on the given stream
+ * and copy nothing to the host, none allocates except the create call, and empty problems (a zero extent) are
+ * valid. Buffers must not overlap unless a call says so; this is the caller's to keep.
+ */
+
+/* activations of dmx_group_norm_*: u, max(u, 0), u / (1 + exp(-u)), u * Phi(u) (Phi: the normal
+ * distribution function, the erf form). The slope of DMX_ACT_RELU at 0 is 0. */
+enum { DMX_ACT_NONE = 0, DMX_ACT_RELU = 1, DMX_ACT_SILU = 2, DMX_ACT_GELU = 3 };
+
+/*
  * dmx_adamw_* — AdamW over n tensors in one launch, moments in fp32 or in 8-bit block codes.
  * Per element, with s the optional gradient factor:
  *   g = s*grad       m' = b1 m + (1-b1) g       v' = b2 v + (1-b2) g^2
@@ -475,6 +488,41 @@ int dmx_adamw_step(dmx_adamw* h, void* m, void* v, float* m_scale, float* v_scal
 int dmx_adamw_moments(dmx_adamw* h, const void* m, const void* v, const float* m_scale, const float* v_scale, int out_dtype,
                       void* out_m, void* out_v, void* cuda_stream);
 int dmx_adamw_destroy(dmx_adamw* h);   /* as dmx_destroy */
+
+/*
+ * dmx_group_norm_* — group norm with an activation on channels-last data, and its gradient.
+ * x is N images of L positions of C channels (DMX_F32 or DMX_BF16), G groups of C/G neighbouring channels:
+ *   mean, var over a group's L*C/G values (var without Bessel's correction), rstd = 1/sqrt(var + eps),
+ *   u = (x - mean) * rstd * weight + bias, y = act(u)
+ * backward, with xh = (x - mean)*rstd, du = dy * act'(u), n = L*C/G and sums over the group:
+ *   dweight = sum over images and positions of du*xh, dbias = the same of du,
+ *   dx = rstd * (weight*du - (sum(weight*du) + xh * sum(weight*du*xh)) / n)
+ * All arithmetic and all sums are fp32 (variances from deviations of the mean, never from a difference of
+ * squares); y and dx are rounded once. Group norm's statistics do not depend on the batch size, which is why
+ * it is the norm to use where a controller changes that.
+ *   x, y, dy, dx       element (n, l, c) at n*image + l*row + c, strides in elements, row >= C unless L <= 1;
+ *                      any alignment of the element type (16-byte aligned starts and strides are faster)
+ *   weight, bias       fp32, C entries, or NULL for ones and zeros
+ *   mean, rstd         fp32, N*G (written by forward, read by backward)
+ *   dweight, dbias     fp32, C entries, or NULL
+ *   workspace          at least dmx_group_norm_workspace(...) bytes, 16-byte aligned, contents undefined
+ * Results are bitwise reproducible. y may be x itself, and dx may be dy or x, with the same strides.
+ * Errors: DMX_ERR_ARG (C < 1, G not a divisor of C, C > DMX_GN_MAX_CHANNELS,
+ * C/G > DMX_GN_MAX_GROUP, extents, strides, eps < 0, null pointers, workspace
+ * too small), DMX_ERR_ALIGN, DMX_ERR_CUDA.
+ */
+#define DMX_GN_MAX_CHANNELS 65536
+#define DMX_GN_MAX_GROUP 1024
+int64_t dmx_group_norm_workspace(int64_t N, int64_t L, int C, int G, int dtype, int backward);
+int dmx_group_norm_forward(int64_t N, int64_t L, int C, int G, int dtype, const void* x, int64_t x_image, int64_t x_row,
+                           const float* weight, const float* bias, float eps, int act, void* y, int64_t y_image,
+                           int64_t y_row, float* mean, float* rstd, void* workspace, int64_t workspace_bytes,
+                           void* cuda_stream);
+int dmx_group_norm_backward(int64_t N, int64_t L, int C, int G, int dtype, const void* dy, int64_t dy_image,
+                            int64_t dy_row, const void* x, int64_t x_image, int64_t x_row, const float* mean,
+                            const float* rstd, const float* weight, const float* bias, int act, void* dx,
+                            int64_t dx_image, int64_t dx_row, float* dweight, float* dbias, void* workspace,
+                            int64_t workspace_bytes, void* cuda_stream);
 
 /* Frees the tables and the scratch. NULL is accepted; a handle that is not live (destroyed
  * already) gives DMX_ERR_HANDLE. The caller makes sure no step of this handle is still running. */

@@ -22,7 +22,8 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
               "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 
 TARGETS = {
-    "libdmx.so": (["dmx.cu", "dmx_static.cu", "dmx_agg.cu", "dmx_ctl.cu", "dmx_adamw.cu"], ["dmx_kernels.cuh", "dmx_host.h", os.path.join(INCLUDE, "dmx.h")]),
+    "libdmx.so": (["dmx.cu", "dmx_static.cu", "dmx_agg.cu", "dmx_ctl.cu", "dmx_adamw.cu", "dmx_group_norm.cu"],
+                  ["dmx_kernels.cuh", "dmx_act.cuh", "dmx_host.h", os.path.join(INCLUDE, "dmx.h")]),
     "libdmx_gen.so": (["dmx_gen.cu"], []),
 }
 

@@ -1,4 +1,5 @@
-"""The training operators of include/dmx.h for torch callers: AdamW over many tensors.
+"""The training operators of include/dmx.h for torch callers: AdamW over many tensors, and group norm with an
+activation on channels-last data.
 
 Tensors in, raw pointers through the C ABI; every call runs on the current stream of its tensors' device, takes its
 workspace from torch's allocator there, and raises DmxError with the library's code for arguments it refuses.
@@ -10,6 +11,8 @@ import ctypes
 
 from . import binding as B
 
+ACT = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = range(4)
 ADAMW_BLOCK = 256
 
 _torch = None
@@ -50,6 +53,12 @@ class _on:
 
 def _ptr(x):
     return None if x is None else x.data_ptr()
+
+
+def _workspace(nbytes, like, where):
+    if nbytes < 0:
+        _refuse(where, int(nbytes))
+    return _torch.empty(nbytes, dtype=_torch.uint8, device=like.device) if nbytes else None
 
 
 class AdamW:
@@ -166,3 +175,81 @@ class AdamW:
             self._h = None
 
     __del__ = close
+
+
+def _image(x, shape, dtype, like, where):
+    """Strides (image, row) of an (N, ..., C) tensor whose positions lie at one stride and whose channels are dense."""
+    if x.dtype != dtype or x.device != like.device or x.shape != shape:
+        _refuse(where)
+    st = x.stride()
+    if x.dim() == 3:
+        if shape[2] > 1 and st[2] != 1:
+            _refuse(where)
+        return st[0], st[1]
+    if shape[-1] > 1 and st[-1] != 1:
+        _refuse(where)
+    row = st[-2]
+    for i in range(x.dim() - 3, 0, -1):                  # (N, H, W, C): rows of the image must follow on
+        if shape[i] > 1 and st[i] != row * _prod(shape[i + 1:-1]):
+            _refuse(where)
+    return st[0], row
+
+
+def _prod(v):
+    n = 1
+    for x in v:
+        n *= x
+    return n
+
+
+def _norm_args(x, groups, weight, bias, act, where):
+    _t()
+    if x.dim() < 3 or x.dtype not in _dtypes or not x.is_cuda or act not in ACT:
+        _refuse(where)
+    C = x.shape[-1]
+    for p in (weight, bias):
+        if p is not None and (p.dtype != _torch.float32 or p.numel() != C or p.device != x.device or not p.is_contiguous()):
+            _refuse(where + " (weight, bias)")
+    return x.shape[0], _prod(x.shape[1:-1]), C, _dtypes[x.dtype]
+
+
+def group_norm(x, groups, weight=None, bias=None, eps=1e-5, act="none", out=None):
+    """act(group_norm(x)) of a channels-last tensor (N, ..., C), fp32 or bf16 -> (y, mean, rstd), the statistics
+    fp32 (N, groups). weight, bias: fp32 (C,). x may be a channel slice of a wider tensor; out may be x."""
+    N, L, C, dt = _norm_args(x, groups, weight, bias, act, "group_norm")
+    xs = _image(x, x.shape, x.dtype, x, "group_norm (x)")
+    y = _torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    ys = _image(y, x.shape, x.dtype, x, "group_norm (out)")
+    if groups < 1:
+        _refuse("group_norm (groups)")
+    stats = _torch.empty((2, N, groups), dtype=_torch.float32, device=x.device)
+    L_ = B.lib()
+    with _on(x):
+        ws = _workspace(L_.dmx_group_norm_workspace(N, L, C, groups, dt, 0), x, "group_norm")
+        rc = L_.dmx_group_norm_forward(N, L, C, groups, dt, x.data_ptr(), xs[0], xs[1], _ptr(weight), _ptr(bias), eps, ACT[act], y.data_ptr(), ys[0], ys[1],
+                                       stats.data_ptr(), stats.data_ptr() + 4 * N * groups, _ptr(ws), 0 if ws is None else ws.numel(), _stream(x))
+    if rc != B.OK:
+        _refuse("dmx_group_norm_forward", rc)
+    return y, stats[0], stats[1]
+
+
+def group_norm_backward(dy, x, mean, rstd, groups, weight=None, bias=None, act="none", out=None):
+    """Gradient of group_norm from its saved statistics -> (dx, dweight, dbias)."""
+    N, L, C, dt = _norm_args(x, groups, weight, bias, act, "group_norm_backward")
+    xs = _image(x, x.shape, x.dtype, x, "group_norm_backward (x)")
+    gs = _image(dy, x.shape, x.dtype, x, "group_norm_backward (dy)")
+    dx = _torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    ds = _image(dx, x.shape, x.dtype, x, "group_norm_backward (out)")
+    for s in (mean, rstd):
+        if s.dtype != _torch.float32 or s.numel() != N * groups or s.device != x.device or not s.is_contiguous():
+            _refuse("group_norm_backward (statistics)")
+    dp = _torch.empty((2, C), dtype=_torch.float32, device=x.device)
+    L_ = B.lib()
+    with _on(x):
+        ws = _workspace(L_.dmx_group_norm_workspace(N, L, C, groups, dt, 1), x, "group_norm_backward")
+        rc = L_.dmx_group_norm_backward(N, L, C, groups, dt, dy.data_ptr(), gs[0], gs[1], x.data_ptr(), xs[0], xs[1], mean.data_ptr(), rstd.data_ptr(),
+                                        _ptr(weight), _ptr(bias), ACT[act], dx.data_ptr(), ds[0], ds[1], dp.data_ptr(), dp.data_ptr() + 4 * C,
+                                        _ptr(ws), 0 if ws is None else ws.numel(), _stream(x))
+    if rc != B.OK:
+        _refuse("dmx_group_norm_backward", rc)
+    return dx, dp[0], dp[1]
