@@ -32,9 +32,12 @@
 #include <type_traits>
 #include <vector>
 
+#include "dmx_f32x2.cuh"
 #include "dmx_host.h"
 
 namespace {
+
+using namespace dmx_f32x2;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
@@ -158,43 +161,6 @@ __device__ __forceinline__ void store_codes(void* p, const unsigned* w, int lane
   for (int q = 0; q < 2; ++q)
     __stcs(static_cast<unsigned*>(p) + word_of<VEC>(q, lane), VEC ? w[q] : transpose4(w[q], lane));
 }
-
-// Pairs of elements go through the packed fp32 instructions of sm_100 (each half IEEE fp32, round to nearest
-// unless named otherwise): half the issue slots.
-// A packed product that feeds a packed sum is contracted to one rounding even where both name theirs (seen in
-// results); where two are wanted the sum is an fma with a factor of 1 that only the launch knows.
-__device__ __forceinline__ unsigned long long bits2(float2 x) {
-  unsigned long long r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x.x), "f"(x.y));
-  return r;
-}
-__device__ __forceinline__ float2 float2_of(unsigned long long b) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(b));
-  return r;
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-  unsigned long long r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)));
-  return float2_of(r);
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  unsigned long long r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)));
-  return float2_of(r);
-}
-__device__ __forceinline__ float2 add2_down(float2 a, float2 b) {
-  unsigned long long r;
-  asm("add.rm.f32x2 %0, %1, %2;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)));
-  return float2_of(r);
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  unsigned long long r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
-  return float2_of(r);
-}
-__device__ __forceinline__ float2 two(float x) { return make_float2(x, x); }
-__device__ __forceinline__ float2 abs2(float2 x) { return make_float2(fabsf(x.x), fabsf(x.y)); }
 
 // Codes as floats and back without the conversion unit (a quarter as fast as the multipliers, and busy with
 // the roots): a byte in the low mantissa bits of 2^23 is that number plus 2^23, and an addition to 2^23 that

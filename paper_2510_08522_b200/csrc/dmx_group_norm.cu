@@ -29,6 +29,11 @@
 
 namespace {
 
+using namespace dmx_f32x2;
+
+#ifndef CTAS
+#define CTAS 2
+#endif
 constexpr int kMaxCluster = 8;
 
 struct Operand {
@@ -42,13 +47,12 @@ struct Args {
   float *mean, *rstd;    // forward: outputs; backward: inputs
   float* part;           // partial sums (workspace)
   int64_t items;         // image slabs (and chunks)
-  int L, N, C, G, cpg, W, slabs, R, cols, rows;   // W channels per slab, R positions at a time, cols columns of V, rows positions per CTA
+  int L, N, C, G, cpg, W, gW, slabs, R, cols, rows;   // W channels (gW groups) per slab, R positions at a time, cols columns of V, rows positions per CTA
   int parts;             // CTAs (or chunks) per image and slab
   int slots;             // positions per thread
   int fold;              // neighbouring channels of a column that surely share a group (a power of two)
   int lanes;             // lanes of a warp that hold different columns, if that divides 32, else 0
   float eps;
-  int act;
 };
 
 template <typename T, int V>
@@ -58,30 +62,93 @@ template <> struct Vec<float, 1> { using type = unsigned; };
 template <> struct Vec<__nv_bfloat16, 8> { using type = uint4; };
 template <> struct Vec<__nv_bfloat16, 1> { using type = unsigned short; };
 
-__device__ __forceinline__ void widen(uint4 r, float (&x)[4]) {
-  x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
+// A thread computes on pairs: neighbouring channels of a column, or, where a column is one element, the elements of two
+// positions.
+template <int V> constexpr int kPairs = V > 1 ? V / 2 : 1;
+template <int V> constexpr int kSlots = V > 1 ? 1 : 2;
+
+__device__ __forceinline__ void widen(const uint4* s, bool, int, float2, float2 (&x)[2]) {
+  const uint4 r = *s;
+  x[0] = make_float2(__uint_as_float(r.x), __uint_as_float(r.y));
+  x[1] = make_float2(__uint_as_float(r.z), __uint_as_float(r.w));
 }
-__device__ __forceinline__ void widen(unsigned r, float (&x)[1]) { x[0] = __uint_as_float(r); }
-__device__ __forceinline__ void widen(unsigned short r, float (&x)[1]) { x[0] = __uint_as_float((unsigned)r << 16); }
-__device__ __forceinline__ void widen(uint4 r, float (&x)[8]) {
-  const unsigned w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-  for (int j = 0; j < 4; ++j) { x[2 * j] = __uint_as_float(w[j] << 16); x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
+__device__ __forceinline__ void widen(const uint4* s, bool, int, float2, float2 (&x)[4]) {
+  const uint4 r = *s;
+  x[0] = widen2(r.x); x[1] = widen2(r.y); x[2] = widen2(r.z); x[3] = widen2(r.w);
 }
-__device__ __forceinline__ unsigned pack2(float a, float b) {
-  __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+// `second`: the next position exists (`step` slots further); otherwise `fill` stands for its value
+__device__ __forceinline__ void widen(const unsigned* s, bool second, int step, float2 fill, float2 (&x)[1]) {
+  x[0] = make_float2(__uint_as_float(*s), second ? __uint_as_float(s[step]) : fill.y);
+}
+__device__ __forceinline__ void widen(const unsigned short* s, bool second, int step, float2 fill, float2 (&x)[1]) {
+  x[0] = make_float2(__uint_as_float((unsigned)*s << 16), second ? __uint_as_float((unsigned)s[step] << 16) : fill.y);
+}
+__device__ __forceinline__ unsigned pack2(float2 x) {
+  __nv_bfloat162 t = __floats2bfloat162_rn(x.x, x.y);
   return *reinterpret_cast<unsigned*>(&t);
 }
-__device__ __forceinline__ void put(float* p, const float (&x)[4]) { __stcs(reinterpret_cast<float4*>(p), make_float4(x[0], x[1], x[2], x[3])); }
-__device__ __forceinline__ void put(float* p, const float (&x)[1]) { __stcs(p, x[0]); }
-__device__ __forceinline__ void put(__nv_bfloat16* p, const float (&x)[8]) {
-  __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])));
+__device__ __forceinline__ void put(float* p, bool, int64_t, const float2 (&x)[2]) { __stcs(reinterpret_cast<float4*>(p), make_float4(x[0].x, x[0].y, x[1].x, x[1].y)); }
+__device__ __forceinline__ void put(__nv_bfloat16* p, bool, int64_t, const float2 (&x)[4]) {
+  __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack2(x[0]), pack2(x[1]), pack2(x[2]), pack2(x[3])));
 }
-__device__ __forceinline__ void put(__nv_bfloat16* p, const float (&x)[1]) { *p = __float2bfloat16_rn(x[0]); }
+__device__ __forceinline__ void put(float* p, bool second, int64_t step, const float2 (&x)[1]) {
+  __stcs(p, x[0].x);
+  if (second) __stcs(p + step, x[0].y);
+}
+__device__ __forceinline__ void put(__nv_bfloat16* p, bool second, int64_t step, const float2 (&x)[1]) {
+  *p = __float2bfloat16_rn(x[0].x);
+  if (second) p[step] = __float2bfloat16_rn(x[0].y);
+}
+// a channel's value for pair j, from per-channel reads: f(v) for channel v of the column
+template <int V, typename F>
+__device__ __forceinline__ void per_channel(float2 (&x)[kPairs<V>], F f) {
+  if constexpr (V == 1) {
+    const float t = f(0);
+    x[0] = make_float2(t, t);
+  } else {
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) {
+      x[j].x = f(2 * j);
+      x[j].y = f(2 * j + 1);
+    }
+  }
+}
+
+// ... from an array in shared memory with an entry per channel (p: the column's first)
+__device__ __forceinline__ void channels(const float* p, float2 (&x)[4]) {
+  const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
+  x[0] = make_float2(a.x, a.y); x[1] = make_float2(a.z, a.w); x[2] = make_float2(b.x, b.y); x[3] = make_float2(b.z, b.w);
+}
+__device__ __forceinline__ void channels(const float* p, float2 (&x)[2]) {
+  const float4 a = *reinterpret_cast<const float4*>(p);
+  x[0] = make_float2(a.x, a.y); x[1] = make_float2(a.z, a.w);
+}
+__device__ __forceinline__ void channels(const float* p, float2 (&x)[1]) { x[0] = two(*p); }
+__device__ __forceinline__ void to_channels(float* p, const float2 (&x)[4]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(x[0].x, x[0].y, x[1].x, x[1].y);
+  reinterpret_cast<float4*>(p)[1] = make_float4(x[2].x, x[2].y, x[3].x, x[3].y);
+}
+__device__ __forceinline__ void to_channels(float* p, const float2 (&x)[2]) { *reinterpret_cast<float4*>(p) = make_float4(x[0].x, x[0].y, x[1].x, x[1].y); }
+__device__ __forceinline__ void to_channels(float* p, const float2 (&x)[1]) { *p = x[0].x + x[0].y; }
+// ... from one with an entry per group; `one`: the whole column lies in group g
+template <int V>
+__device__ __forceinline__ void groups_of(const float* p, int g, int rem, int cpg, bool one, float2 (&x)[kPairs<V>]) {
+  if (one) {
+    const float t = p[g];
+#pragma unroll
+    for (int j = 0; j < kPairs<V>; ++j) x[j] = two(t);
+  } else {
+    per_channel<V>(x, [&](int) {
+      const float t = p[g];
+      if (++rem == cpg) { rem = 0; ++g; }
+      return t;
+    });
+  }
+}
 
 // One element or column into the thread's own slot. Two bytes are below what an asynchronous copy takes.
 __device__ __forceinline__ void bring(uint4* slot, const void* p) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((unsigned)__cvta_generic_to_shared(slot)), "l"(p));
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"((unsigned)__cvta_generic_to_shared(slot)), "l"(p));
 }
 __device__ __forceinline__ void bring(unsigned* slot, const void* p) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((unsigned)__cvta_generic_to_shared(slot)), "l"(p));
@@ -98,7 +165,7 @@ enum Mode { RESIDENT, STATS, APPLY };
 
 // A CTA's place in one item, and a thread's in that.
 struct Here {
-  int n, part, c0, Wl, groups, rows, r0;
+  int n, part, c0, g0, Wl, groups, rows, r0;
   int cnt;               // positions of this thread
   bool on;               // its column exists
 };
@@ -115,8 +182,9 @@ __device__ __forceinline__ Here place(const Args& A, int64_t item, int rl, int c
   const int slab = A.slabs > 1 ? b % (unsigned)A.slabs : 0;
   h.n = A.slabs > 1 ? b / (unsigned)A.slabs : b;
   h.c0 = slab * A.W;
+  h.g0 = slab * A.gW;
   h.Wl = min(A.W, A.C - h.c0);
-  h.groups = h.Wl == A.W ? A.W / A.cpg : h.Wl / A.cpg;
+  h.groups = min(A.gW, A.G - h.g0);
   h.r0 = min((int64_t)h.part * A.rows, (int64_t)A.L);
   h.rows = min(A.rows, A.L - h.r0);
   h.on = rl < A.R && col * V < h.Wl;
@@ -128,43 +196,90 @@ __device__ __forceinline__ T* start(const Operand& o, const Here& h, int rl, int
   return static_cast<T*>(o.p) + h.n * o.image + (int64_t)(h.r0 + rl) * o.row + h.c0 + col * V;
 }
 
-// Sums over groups of red[R][width], `per` neighbouring entries of a row being a group's: term(i, r, g) for
-// entry i in row r. `each` lanes (a power of two) take a group, in a fixed order.
-template <typename F>
-__device__ __forceinline__ float group_sum(int g, int groups, int per, int R, int width, int each, int l, F term) {
-  float s = 0.f;
-  if (g < groups) {
-    int r = l / per, c = l - r * per;
-    const int dr = each / per, dc = each - dr * per;
-    for (; r < R;) {
-      s += term(r * width + g * per + c, r, g);
-      r += dr; c += dc;
-      if (c >= per) { c -= per; ++r; }
-    }
-  }
-  for (int o = each >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  return s;
-}
 __device__ __forceinline__ int lanes_for(int total) {
   return total >= 32 ? 32 : total <= 1 ? 1 : 1 << (32 - __clz(total - 1));
 }
+// Sums over groups of an array [R][width], `per` neighbouring entries of a row being a group's. `each` lanes (a
+// power of two) take a group, in a fixed order; they all get its sum.
+struct Lanes {
+  int each, l, g1, gstep;      // lane within the group, group within a round, groups per round
+  int R, per, width, i0, r0, c0, dr, dc;
+};
+__device__ __forceinline__ Lanes lanes(int R, int per, int width) {
+  Lanes q;
+  q.each = lanes_for(R * per);
+  q.l = threadIdx.x & (q.each - 1);
+  const int sh = 31 - __clz(q.each);
+  q.g1 = threadIdx.x >> sh;
+  q.gstep = blockDim.x >> sh;
+  q.R = R; q.per = per; q.width = width;
+  q.r0 = q.l / per;
+  q.c0 = q.l - q.r0 * per;
+  q.dr = q.each / per;
+  q.dc = q.each - q.dr * per;
+  return q;
+}
+template <typename F>
+__device__ __forceinline__ float lane_sum(const Lanes& q, bool on, int g, F term) {    // term(i, r, c): entry i = r*width + c
+  float s = 0.f;
+  if (on) {
+    int r = q.r0, c = q.c0;
+    while (r < q.R) {
+      const int at = g * q.per + c;
+      s += term(r * q.width + at, r, at);
+      r += q.dr;
+      c += q.dc;
+      if (c >= q.per) { c -= q.per; ++r; }
+    }
+  }
+  for (int o = q.each >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  return s;
+}
 
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
 }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
-__device__ __forceinline__ float remote(const float* p, int rank) {
+// into the same place of another CTA's shared memory
+__device__ __forceinline__ void send(float* p, int rank, float v) {
   unsigned a;
-  float v;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((unsigned)__cvta_generic_to_shared(p)), "r"(rank));
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
-  return v;
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(a), "f"(v) : "memory");
+}
+// weight and bias of an item's channels and, backward, its groups' statistics, into shared memory beside the data
+struct Params {
+  float *w, *b, *mean, *rstd;
+};
+__device__ __forceinline__ Params params_at(float* base, int W, int groups) {
+  Params p;
+  p.w = base;
+  p.b = p.w + padded(W);
+  p.mean = p.b + padded(W);
+  p.rstd = p.mean + padded(groups);
+  return p;
+}
+__host__ __device__ constexpr int params_size(int W, int groups) { return 2 * padded(W) + 2 * padded(groups); }
+template <bool STATISTICS>
+__device__ __forceinline__ void bring_params(const Args& A, const Here& h, const Params& p) {
+  for (int c = threadIdx.x; c < h.Wl; c += blockDim.x) {
+    if (A.weight) bring(reinterpret_cast<unsigned*>(p.w + c), A.weight + h.c0 + c);
+    else p.w[c] = 1.f;
+    if (A.bias) bring(reinterpret_cast<unsigned*>(p.b + c), A.bias + h.c0 + c);
+    else p.b[c] = 0.f;
+  }
+  if (STATISTICS)
+    for (int g = threadIdx.x; g < h.groups; g += blockDim.x) {
+      const int64_t at = (int64_t)h.n * A.G + h.g0 + g;
+      bring(reinterpret_cast<unsigned*>(p.mean + g), A.mean + at);
+      bring(reinterpret_cast<unsigned*>(p.rstd + g), A.rstd + at);
+    }
 }
 
-template <typename T, int V, Mode M>
-__global__ void __launch_bounds__(V == 1 ? 1024 : 256) forward_kernel(const __grid_constant__ Args A) {
+template <typename T, int V, Mode M, int ACT>
+__global__ void __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : CTAS) forward_kernel(const __grid_constant__ Args A) {
   using U = typename Vec<T, V>::type;
+  constexpr int NP = kPairs<V>, SL = kSlots<V>;
   extern __shared__ __align__(16) float sm[];
   const int W = A.W, cpg = A.cpg, R = A.R, threads = blockDim.x;
   const int tid = threadIdx.x, rl = tid / A.cols, col = tid - rl * A.cols;
@@ -175,11 +290,16 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 256) forward_kernel(const __gr
   float* emean = sm + (size_t)A.slots * threads * sizeof(U) / sizeof(float);
   float* em2 = emean + padded(rows * width);
   float* en = em2 + padded(rows * width);
-  float* gsum = en + padded(rows);                 // per group: this CTA's sum and squared deviations (read by the cluster)
-  float* gm2 = gsum + padded(W / cpg);
-  float* gmean = gm2 + padded(W / cpg);            // per group: mean, rstd
-  float* grstd = gmean + padded(W / cpg);
-  const int each = lanes_for(rows * per), gl = tid & (each - 1), g1 = tid / each, gstep = threads / each;
+  // per group: every part's sum and squared deviations, in turn for one item and the next (the cluster's CTAs write to
+  // one another's: whoever writes for an item has seen all others' sums of the item before, so the buffer of two
+  // items ago is free); then mean and rstd
+  const int pG = padded(A.gW), gparts = M == RESIDENT ? A.parts : 1;
+  float* got = en + padded(rows);
+  float* gmean = got + 4 * gparts * pG;
+  float* grstd = gmean + pG;
+  float* par = grstd + pG;
+  int turn = 0;
+  const Lanes Q = lanes(rows, per, width);
   int grp0 = 0, rem0 = 0;                          // group of the column's first channel, and its place there
   if (rl < R) { grp0 = col * V / cpg; rem0 = col * V - grp0 * cpg; }
 
@@ -190,29 +310,39 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 256) forward_kernel(const __gr
   {
     const T* p = start<T, V>(A.x, h, rl, col);
     for (int i = 0; i < h.cnt; ++i) bring(slot + i * threads, p + (int64_t)i * R * A.x.row);
+    if (M != STATS) bring_params<false>(A, h, params_at(par, W, A.gW));
   }
+  if (M == RESIDENT && A.parts > 1) cluster_sync();      // all of the cluster runs: its memory may be written
   for (int64_t item = first; item < A.items; item += stride) {
-    float w[V], b[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      w[v] = h.on && A.weight ? __ldg(A.weight + h.c0 + col * V + v) : 1.f;
-      b[v] = h.on && A.bias ? __ldg(A.bias + h.c0 + col * V + v) : 0.f;
-    }
-    bring_wait();
+    const Params P = params_at(par + turn * params_size(W, A.gW), W, A.gW);
+    float* mine = got + turn * 2 * gparts * pG;
     if constexpr (M != APPLY) {
-      float x0[V], s[V], q[V];
+      bring_wait();
+      float2 p0[NP], ps[NP], pq[NP];
 #pragma unroll
-      for (int v = 0; v < V; ++v) { x0[v] = 0.f; s[v] = 0.f; q[v] = 0.f; }
-      if (h.cnt > 0) widen(*slot, x0);
+      for (int j = 0; j < NP; ++j) p0[j] = ps[j] = pq[j] = two(0.f);
+      if (h.cnt > 0) widen(slot, false, 0, two(0.f), p0);
+      if (V == 1) p0[0].y = p0[0].x;
 #pragma unroll 4
-      for (int i = 1; i < h.cnt; ++i) {
-        float x[V];
-        widen(slot[i * threads], x);
+      for (int i = 0; i < h.cnt; i += SL) {
+        float2 x[NP];
+        widen(slot + i * threads, i + 1 < h.cnt, threads, p0[0], x);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          const float d = x[v] - x0[v];
-          s[v] += d;
-          q[v] = fmaf(d, d, q[v]);
+        for (int j = 0; j < NP; ++j) {
+          const float2 d = sub2(x[j], p0[j]);
+          ps[j] = add2(ps[j], d);
+          pq[j] = fma2(d, d, pq[j]);
+        }
+      }
+      float x0[V], s[V], q[V];
+      if constexpr (V == 1) {
+        x0[0] = p0[0].x; s[0] = ps[0].x + ps[0].y; q[0] = pq[0].x + pq[0].y;
+      } else {
+#pragma unroll
+        for (int j = 0; j < NP; ++j) {
+          x0[2 * j] = p0[j].x; x0[2 * j + 1] = p0[j].y;
+          s[2 * j] = ps[j].x; s[2 * j + 1] = ps[j].y;
+          q[2 * j] = pq[j].x; q[2 * j + 1] = pq[j].y;
         }
       }
       // per value: mean and squared deviations of this thread's n entries, neighbours joined while they share a group
@@ -271,101 +401,115 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 256) forward_kernel(const __gr
       }
       __syncthreads();
       const float cnt = (float)h.rows * (float)cpg, icnt = h.rows > 0 ? 1.f / cnt : 0.f;
-      for (int g0 = 0; g0 < h.groups; g0 += gstep) {
-        const int g = g0 + g1;
-        const float sum = group_sum(g, h.groups, per, rows, width, each, gl, [&](int i, int r, int) { return en[r] > 0.f ? emean[i] * en[r] : 0.f; });
+      for (int gb = 0; gb < h.groups; gb += Q.gstep) {
+        const int g = gb + Q.g1;
+        const bool mineg = g < h.groups;
+        const float sum = lane_sum(Q, mineg, g, [&](int i, int r, int) { return en[r] > 0.f ? emean[i] * en[r] : 0.f; });
         const float mean = sum * icnt;
-        const float m2 = group_sum(g, h.groups, per, rows, width, each, gl, [&](int i, int r, int) {
+        const float m2 = lane_sum(Q, mineg, g, [&](int i, int r, int) {
           const float d = emean[i] - mean;
           return en[r] > 0.f ? fmaf(en[r] * d, d, em2[i]) : 0.f;
         });
-        if (g < h.groups && gl == 0) {
-          gsum[g] = mean * (float)h.rows;          // times channels below: keeps the product in range
-          gm2[g] = m2;
+        // the mean times the number of positions: the parts' sum over all positions is the mean
+        if (M == STATS) {
+          if (mineg && Q.l == 0)
+            reinterpret_cast<float2*>(A.part)[((int64_t)h.n * A.parts + h.part) * A.G + h.g0 + g] = make_float2(mean * (float)h.rows, m2);
+        } else if (A.parts > 1) {
+          if (mineg)
+            for (int k = Q.l; k < 2 * A.parts; k += Q.each)
+              send(mine + (2 * h.part + (k & 1)) * pG + g, k >> 1, k & 1 ? m2 : mean * (float)h.rows);
+        } else if (mineg && Q.l == 0) {
+          mine[g] = mean * (float)h.rows;
+          mine[pG + g] = m2;
         }
       }
-      if constexpr (M == STATS) {
-        __syncthreads();
-        float2* out = reinterpret_cast<float2*>(A.part) + ((int64_t)h.n * A.parts + h.part) * A.G + h.c0 / cpg;
-        for (int g = tid; g < h.groups; g += threads) out[g] = make_float2(gsum[g], gm2[g]);
-      } else if (A.parts > 1) {
-        cluster_sync();
-      } else {
-        __syncthreads();
-      }
+      if (M == RESIDENT && A.parts > 1) cluster_arrive();
+    }
+    // the next item's place and parameters, while the others arrive
+    const Here now = h;
+    const int64_t next = item + stride;
+    const T* np = nullptr;
+    int ncnt = 0;
+    if (next < A.items) {
+      h = place<V, M>(A, next, rl, col);
+      np = start<T, V>(A.x, h, rl, col);
+      ncnt = h.cnt;
+      if (M != STATS) bring_params<false>(A, h, params_at(par + (turn ^ 1) * params_size(W, A.gW), W, A.gW));
+    }
+    turn ^= 1;
+    if constexpr (M != APPLY) {
+      if (M == RESIDENT && A.parts > 1) cluster_wait();
+      else __syncthreads();
     }
     if constexpr (M != STATS) {
-      // join the parts of each group, in their order
-      for (int g = tid; g < h.groups; g += threads) {
-        const float2* src = reinterpret_cast<const float2*>(A.part) + (int64_t)h.n * A.parts * A.G + h.c0 / cpg + g;
-        float sum = 0.f, m2 = 0.f;
-        for (int k = 0; k < A.parts; ++k) {
-          if constexpr (M == RESIDENT) sum += A.parts > 1 ? remote(gsum + g, k) : gsum[g];
-          else sum += __ldg(&src[(int64_t)k * A.G]).x;
+      // join the parts of each group: a lane per part (or per 32nd part), added in a fixed order
+      const int kl = A.parts >= 32 ? 32 : lanes_for(A.parts), k0 = tid & (kl - 1);
+      const int64_t gat = (int64_t)now.n * A.G + now.g0;
+      for (int gb = 0; gb < now.groups; gb += threads / kl) {
+        const int g = gb + tid / kl;
+        const float2* src = reinterpret_cast<const float2*>(A.part) + (int64_t)now.n * A.parts * A.G + now.g0 + g;
+        float ps = 0.f, pm = 0.f, sum = 0.f, m2 = 0.f;
+        if (M == RESIDENT && g < now.groups && k0 < A.parts) {
+          sum = ps = mine[2 * k0 * pG + g];
+          pm = mine[(2 * k0 + 1) * pG + g];
         }
+        if (M == APPLY && g < now.groups)
+          for (int k = k0; k < A.parts; k += kl) sum += __ldg(&src[(int64_t)k * A.G]).x;
+        for (int o = kl >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         const float mean = sum / (float)A.L;
-        for (int k = 0; k < A.parts; ++k) {
-          const float have = (float)(min((int64_t)(k + 1) * A.rows, (int64_t)A.L) - min((int64_t)k * A.rows, (int64_t)A.L));
-          float ps, pm;
-          if constexpr (M == RESIDENT) {
-            ps = A.parts > 1 ? remote(gsum + g, k) : gsum[g];
-            pm = A.parts > 1 ? remote(gm2 + g, k) : gm2[g];
-          } else {
+        for (int k = k0; k < A.parts && g < now.groups; k += kl) {
+          if (M == APPLY) {
             const float2 t = __ldg(&src[(int64_t)k * A.G]);
             ps = t.x; pm = t.y;
           }
+          const float have = (float)(min((int64_t)(k + 1) * A.rows, (int64_t)A.L) - min((int64_t)k * A.rows, (int64_t)A.L));
           if (have > 0.f) {
             const float d = ps / have - mean;
             m2 += fmaf(have * (float)cpg * d, d, pm);
           }
         }
-        const float rstd = 1.f / sqrtf(m2 / ((float)A.L * (float)cpg) + A.eps);
-        gmean[g] = mean;
-        grstd[g] = rstd;
-        if (h.part == 0) {
-          const int64_t at = (int64_t)h.n * A.G + h.c0 / cpg + g;
-          A.mean[at] = mean;
-          A.rstd[at] = rstd;
+        for (int o = kl >> 1; o > 0; o >>= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
+        if (g < now.groups && k0 == 0) {
+          const float rstd = 1.f / sqrtf(m2 / ((float)A.L * (float)cpg) + A.eps);
+          gmean[g] = mean;
+          grstd[g] = rstd;
+          if (now.part == 0) {
+            A.mean[gat + g] = mean;
+            A.rstd[gat + g] = rstd;
+          }
         }
       }
-      if (M == RESIDENT && A.parts > 1) cluster_arrive();
+      if (M == APPLY) bring_wait();          // (the others have waited for their copies above)
       __syncthreads();
     }
     // results, each slot refilled for the next item behind its last use
-    const Here now = h;
-    const int64_t next = item + stride;
-    const bool more = next < A.items;
-    const T* np = nullptr;
-    int ncnt = 0;
-    if (more) {
-      h = place<V, M>(A, next, rl, col);
-      np = start<T, V>(A.x, h, rl, col);
-      ncnt = h.cnt;
-    }
     const int64_t in_step = (int64_t)R * A.x.row;
     if constexpr (M != STATS) {
-      float mu[V];
-      int g = grp0, rem = rem0;
+      float2 mu[NP], a[NP], b[NP];
+      if (now.on) {
+        groups_of<V>(gmean, grp0, rem0, cpg, A.fold == V, mu);
+        groups_of<V>(grstd, grp0, rem0, cpg, A.fold == V, a);
+        channels(P.w + col * V, b);
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        if (now.on) { mu[v] = gmean[g]; w[v] *= grstd[g]; }
-        if (++rem == cpg) { rem = 0; ++g; }
+        for (int j = 0; j < NP; ++j) a[j] = mul2(a[j], b[j]);
+        channels(P.b + col * V, b);
       }
       T* out = start<T, V>(A.out, now, rl, col);
       const int64_t out_step = (int64_t)R * A.out.row;
 #pragma unroll 2
-      for (int i = 0; i < now.cnt; ++i) {
-        float x[V];
-        widen(slot[i * threads], x);
+      for (int i = 0; i < now.cnt; i += SL) {
+        float2 x[NP];
+        const bool second = i + 1 < now.cnt;
+        widen(slot + i * threads, second, threads, two(0.f), x);
 #pragma unroll
-        for (int v = 0; v < V; ++v) x[v] = fmaf(x[v] - mu[v], w[v], b[v]);
-        dmx_act::apply<V>(x, A.act);
-        put(out, x);
-        out += out_step;
-        if (i < ncnt) { bring(slot + i * threads, np); np += in_step; }
+        for (int j = 0; j < NP; ++j) x[j] = dmx_act::apply<ACT>(fma2(sub2(x[j], mu[j]), a[j], b[j]));
+        put(out, second, out_step, x);
+        out += SL * out_step;
+#pragma unroll
+        for (int k = 0; k < SL; ++k)
+          if (i + k < ncnt) { bring(slot + (i + k) * threads, np); np += in_step; }
       }
-      for (int i = now.cnt; i < ncnt; ++i) { bring(slot + i * threads, np); np += in_step; }
-      if (M == RESIDENT && A.parts > 1) cluster_wait();        // the sums may be overwritten from here on
+      for (int i = (now.cnt + SL - 1) / SL * SL; i < ncnt; ++i) { bring(slot + i * threads, np); np += in_step; }
       if (M == APPLY) __syncthreads();                         // (the other modes pass a barrier before they write means)
     } else {
       for (int i = 0; i < ncnt; ++i) { bring(slot + i * threads, np); np += in_step; }
@@ -373,22 +517,41 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 256) forward_kernel(const __gr
   }
 }
 
+// du = dy act'(u) is kept between the two sweeps of a resident backward pass where it costs an exponential and fits where dy
+// was: in fp32. (For bf16, 32 bytes more per slot of eight made the slabs narrower, and cost more than they saved.)
+template <typename T>
+__host__ __device__ constexpr bool keeps(int act) { return (act == DMX_ACT_SILU || act == DMX_ACT_GELU) && sizeof(T) == 4; }
+__device__ __forceinline__ void keep(uint4* g, bool, int, const float2 (&x)[2]) {
+  *g = make_uint4(__float_as_uint(x[0].x), __float_as_uint(x[0].y), __float_as_uint(x[1].x), __float_as_uint(x[1].y));
+}
+__device__ __forceinline__ void keep(unsigned* g, bool second, int step, const float2 (&x)[1]) {
+  *g = __float_as_uint(x[0].x);
+  if (second) g[step] = __float_as_uint(x[0].y);
+}
+
 // Backward. Workspace: A and B per image (and chunk) and channel, [2][N*chunks][C].
-template <typename T, int V, Mode M>
-__global__ void __launch_bounds__(V == 1 ? 1024 : 256) backward_kernel(const __grid_constant__ Args A) {
+template <typename T, int V, Mode M, int ACT>
+__global__ void __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : CTAS) backward_kernel(const __grid_constant__ Args A) {
   using U = typename Vec<T, V>::type;
+  constexpr int NP = kPairs<V>, SL = kSlots<V>;
   extern __shared__ __align__(16) float sm[];
   const int W = A.W, cpg = A.cpg, R = A.R, threads = blockDim.x;
   const int tid = threadIdx.x, rl = tid / A.cols, col = tid - rl * A.cols;
   const int rows = A.lanes ? threads >> 5 : R;
   U* xs = reinterpret_cast<U*>(sm) + tid;
   U* gs = xs + (size_t)A.slots * threads;
-  float* red = sm + (size_t)2 * A.slots * threads * sizeof(U) / sizeof(float);   // rows of A, rows of B
-  float* ch = red + padded(2 * rows * W);          // this CTA's channel sums A, B (read by the cluster)
-  float* wch = ch + padded(2 * W);                 // their totals times weight
-  float* grp = wch + padded(2 * W);                // per group: sum w A, sum w B
-  const int groups_all = W / cpg;
-  const int each = lanes_for(cpg), gl = tid & (each - 1), g1 = tid / each, gstep = threads / each;
+  constexpr bool KEEP = M == RESIDENT && keeps<T>(ACT);
+  const size_t ends = (size_t)2 * A.slots * threads * sizeof(U);
+  float* red = reinterpret_cast<float*>(reinterpret_cast<char*>(sm) + ends);     // rows of A, rows of B
+  // every part's channel sums A, B, in turn as in the forward kernel; then per group the two factors that the
+  // sums of w A and w B give
+  const int pW = padded(W), pG = padded(A.gW), gparts = M == RESIDENT ? A.parts : 1;
+  float* got = red + padded(2 * rows * W);
+  float* grp = got + 4 * gparts * pW;
+  float* par = grp + 2 * pG;
+  int turn = 0;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const Lanes Q = lanes(gparts, cpg, 2 * pW);
   int grp0 = 0, rem0 = 0;
   if (rl < R) { grp0 = col * V / cpg; rem0 = col * V - grp0 * cpg; }
   const int64_t plane = (int64_t)A.N * (M == RESIDENT ? 1 : A.parts) * A.C;
@@ -403,100 +566,73 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 256) backward_kernel(const __g
       bring(xs + i * threads, p + (int64_t)i * R * A.x.row);
       bring(gs + i * threads, g + (int64_t)i * R * A.dy.row);
     }
+    bring_params<true>(A, h, params_at(par, W, A.gW));
   }
+  if (M == RESIDENT && A.parts > 1) cluster_sync();      // all of the cluster runs: its memory may be written
   for (int64_t item = first; item < A.items; item += stride) {
-    float w[V], b[V], mu[V], rs[V];
-    {
-      const int64_t sidx = (int64_t)h.n * A.G + h.c0 / cpg;
-      int g = grp0, rem = rem0;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        w[v] = h.on && A.weight ? __ldg(A.weight + h.c0 + col * V + v) : 1.f;
-        b[v] = h.on && A.bias ? __ldg(A.bias + h.c0 + col * V + v) : 0.f;
-        mu[v] = h.on ? __ldg(A.mean + sidx + g) : 0.f;
-        rs[v] = h.on ? __ldg(A.rstd + sidx + g) : 0.f;
-        if (++rem == cpg) { rem = 0; ++g; }
-      }
-    }
+    const Params P = params_at(par + turn * params_size(W, A.gW), W, A.gW);
+    float* mine = got + turn * 2 * gparts * pW;
     bring_wait();
+    __syncthreads();                 // the parameters are other threads' copies
+    // u = (x - mu) a + b with a = rstd weight
+    float2 mu[NP], a[NP], b[NP];
+    if (h.on) {
+      groups_of<V>(P.mean, grp0, rem0, cpg, A.fold == V, mu);
+      groups_of<V>(P.rstd, grp0, rem0, cpg, A.fold == V, a);
+      channels(P.w + col * V, b);
+#pragma unroll
+      for (int j = 0; j < NP; ++j) a[j] = mul2(a[j], b[j]);
+      channels(P.b + col * V, b);
+    }
     if constexpr (M != APPLY) {
-      float sa[V], sb[V];
+      float2 pa[NP], pb[NP];
 #pragma unroll
-      for (int v = 0; v < V; ++v) sa[v] = sb[v] = 0.f;
+      for (int j = 0; j < NP; ++j) pa[j] = pb[j] = two(0.f);
 #pragma unroll 2
-      for (int i = 0; i < h.cnt; ++i) {
-        float x[V], g[V], u[V];
-        widen(xs[i * threads], x);
-        widen(gs[i * threads], g);
+      for (int i = 0; i < h.cnt; i += SL) {
+        float2 x[NP], g[NP];
+        widen(xs + i * threads, i + 1 < h.cnt, threads, mu[0], x);
+        widen(gs + i * threads, i + 1 < h.cnt, threads, two(0.f), g);
 #pragma unroll
-        for (int v = 0; v < V; ++v) { x[v] = (x[v] - mu[v]) * rs[v]; u[v] = fmaf(x[v], w[v], b[v]); }
-        dmx_act::times_slope<V>(g, u, A.act);
-#pragma unroll
-        for (int v = 0; v < V; ++v) { sa[v] = fmaf(g[v], x[v], sa[v]); sb[v] += g[v]; }
+        for (int j = 0; j < NP; ++j) {
+          x[j] = sub2(x[j], mu[j]);
+          g[j] = dmx_act::times_slope<ACT>(g[j], fma2(x[j], a[j], b[j]));
+          pa[j] = fma2(g[j], x[j], pa[j]);
+          pb[j] = add2(pb[j], g[j]);
+        }
+        if constexpr (KEEP) keep(gs + i * threads, i + 1 < h.cnt, threads, g);
       }
-      if (A.lanes) {
-        const int lane = tid & 31, wid = tid >> 5;
+      // (the sums of A without their factor rstd)
+      const int lane = tid & 31, row = A.lanes ? tid >> 5 : rl;
+      if (A.lanes)
         for (int o = A.lanes; o < 32; o <<= 1)
 #pragma unroll
-          for (int v = 0; v < V; ++v) {
-            sa[v] += __shfl_xor_sync(0xffffffffu, sa[v], o);
-            sb[v] += __shfl_xor_sync(0xffffffffu, sb[v], o);
+          for (int j = 0; j < NP; ++j) {
+            pa[j] = add2(pa[j], make_float2(__shfl_xor_sync(0xffffffffu, pa[j].x, o), __shfl_xor_sync(0xffffffffu, pa[j].y, o)));
+            pb[j] = add2(pb[j], make_float2(__shfl_xor_sync(0xffffffffu, pb[j].x, o), __shfl_xor_sync(0xffffffffu, pb[j].y, o)));
           }
-        if (lane < A.lanes)
-#pragma unroll
-          for (int v = 0; v < V; ++v) {
-            red[wid * W + col * V + v] = sa[v];
-            red[(rows + wid) * W + col * V + v] = sb[v];
-          }
-      } else if (rl < R) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          red[rl * W + col * V + v] = sa[v];
-          red[(rows + rl) * W + col * V + v] = sb[v];
-        }
+      if (A.lanes ? lane < A.lanes : rl < R) {
+        to_channels(red + row * W + col * V, pa);
+        to_channels(red + (rows + row) * W + col * V, pb);
       }
       __syncthreads();
-      for (int c = tid; c < 2 * W; c += threads) {
-        const float* p = c < W ? red + c : red + rows * W + (c - W);
-        float t = 0.f;
-        for (int r = 0; r < rows; ++r) t += p[r * W];
-        ch[c] = t;
-      }
-      if constexpr (M == STATS) {
-        __syncthreads();
-        float* out = A.part + ((int64_t)h.n * A.parts + h.part) * A.C + h.c0;
-        for (int c = tid; c < h.Wl; c += threads) { out[c] = ch[c]; out[plane + c] = ch[W + c]; }
-      } else if (A.parts > 1) {
-        cluster_sync();
-      } else {
-        __syncthreads();
-      }
-    }
-    if constexpr (M != STATS) {
-      // channel totals over the parts, in their order; then the groups' weighted sums
       for (int c = tid; c < 2 * W; c += threads) {
         const int k = c < W ? c : c - W;
-        if (k >= h.Wl) continue;
+        const float* p = red + (c < W ? 0 : rows * W) + k;
         float t = 0.f;
-        if constexpr (M == RESIDENT) {
-          if (A.parts > 1) for (int p = 0; p < A.parts; ++p) t += remote(ch + c, p);
-          else t = ch[c];
-          if (h.part == 0) A.part[(c < W ? 0 : plane) + (int64_t)h.n * A.C + h.c0 + k] = t;
+#pragma unroll 8
+        for (int r = 0; r < rows; ++r) t += p[r * W];
+        if (M == STATS) {
+          if (k < h.Wl) A.part[(c < W ? 0 : plane) + ((int64_t)h.n * A.parts + h.part) * A.C + h.c0 + k] = t;
+        } else if (A.parts > 1) {
+          for (int q = 0; q < A.parts; ++q) send(mine + (2 * h.part + (c < W ? 0 : 1)) * pW + k, q, t);
         } else {
-          const float* src = A.part + (c < W ? 0 : plane) + (int64_t)h.n * A.parts * A.C + h.c0 + k;
-          for (int p = 0; p < A.parts; ++p) t += __ldg(src + (int64_t)p * A.C);
+          mine[(c < W ? 0 : pW) + k] = t;
         }
-        wch[c] = A.weight ? t * __ldg(A.weight + h.c0 + k) : t;
       }
       if (M == RESIDENT && A.parts > 1) cluster_arrive();
-      __syncthreads();
-      for (int g0 = 0; g0 < 2 * groups_all; g0 += gstep) {
-        const int g = g0 + g1;                       // the B half's groups follow the A half's: W / cpg whole groups
-        const float t = group_sum(g, 2 * groups_all, cpg, 1, 0, each, gl, [&](int i, int, int) { return wch[i]; });
-        if (g < 2 * groups_all && gl == 0) grp[g] = t;
-      }
-      __syncthreads();
     }
+    // the next item's place and parameters, while the others arrive
     const Here now = h;
     const int64_t next = item + stride;
     const T *nx = nullptr, *ng = nullptr;
@@ -506,63 +642,114 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 256) backward_kernel(const __g
       nx = start<T, V>(A.x, h, rl, col);
       ng = start<T, V>(A.dy, h, rl, col);
       ncnt = h.cnt;
+      bring_params<true>(A, h, params_at(par + (turn ^ 1) * params_size(W, A.gW), W, A.gW));
+    }
+    turn ^= 1;
+    if constexpr (M != APPLY) {
+      if (M == RESIDENT && A.parts > 1) cluster_wait();
+      else __syncthreads();
+    }
+    if constexpr (M == APPLY) {      // the chunks' sums, in their order
+      for (int c = tid; c < 2 * W; c += threads) {
+        const int k = c < W ? c : c - W;
+        float t = 0.f;
+        const float* src = A.part + (c < W ? 0 : plane) + (int64_t)now.n * A.parts * A.C + now.c0 + k;
+        if (k < now.Wl) {
+#pragma unroll 8
+          for (int p = 0; p < A.parts; ++p) t += __ldg(src + (int64_t)p * A.C);
+        }
+        mine[(c < W ? 0 : pW) + k] = t;
+      }
+      __syncthreads();
+    }
+    if constexpr (M != STATS) {
+      // the groups' weighted sums over parts and channels: rows 2k (A) and 2k + 1 (B) are part k's
+      for (int gb = 0; gb < now.groups; gb += Q.gstep) {
+        const int g = gb + Q.g1;
+        const bool mineg = g < now.groups;
+        const float ta = lane_sum(Q, mineg, g, [&](int i, int, int c) { return mine[i] * P.w[c]; });
+        const float tb = lane_sum(Q, mineg, g, [&](int i, int, int c) { return mine[i + pW] * P.w[c]; });
+        if (mineg && Q.l == 0) {
+          const float r = P.rstd[g], n = -1.f / ((float)A.L * (float)cpg);
+          grp[g] = ta * n * r * r * r;
+          grp[pG + g] = tb * n * r;
+        }
+      }
+      if (M == RESIDENT && now.part == 0)          // what dweight and dbias are summed from
+        for (int c = tid; c < 2 * W; c += threads) {
+          const int k = c < W ? c : c - W;
+          float t = 0.f;
+          for (int q = 0; q < gparts; ++q) t += mine[(2 * q + (c < W ? 0 : 1)) * pW + k];
+          if (k < now.Wl) A.part[(c < W ? 0 : plane) + (int64_t)now.n * A.C + now.c0 + k] = t;
+        }
+      __syncthreads();
     }
     const int64_t xstep = (int64_t)R * A.x.row, gstep2 = (int64_t)R * A.dy.row;
     if constexpr (M != STATS) {
-      float s1[V], s2[V];
-      const float n = 1.f / ((float)A.L * (float)cpg);
-      int g = grp0, rem = rem0;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        if (now.on) { s2[v] = grp[g] * n; s1[v] = grp[groups_all + g] * n; }
-        if (++rem == cpg) { rem = 0; ++g; }
+      // the sums A lack their factor rstd: dx = a du - rstd s1 / n - (x - mu) rstd^3 s2 / n
+      float2 k1[NP], k2[NP];
+      if (now.on) {
+        groups_of<V>(grp + pG, grp0, rem0, cpg, A.fold == V, k1);
+        groups_of<V>(grp, grp0, rem0, cpg, A.fold == V, k2);
       }
       T* out = start<T, V>(A.out, now, rl, col);
       const int64_t out_step = (int64_t)R * A.out.row;
 #pragma unroll 2
-      for (int i = 0; i < now.cnt; ++i) {
-        float x[V], gr[V], u[V];
-        widen(xs[i * threads], x);
-        widen(gs[i * threads], gr);
+      for (int i = 0; i < now.cnt; i += SL) {
+        float2 x[NP], gr[NP];
+        const bool second = i + 1 < now.cnt;
+        widen(xs + i * threads, second, threads, mu[0], x);
+        widen(gs + i * threads, second, threads, two(0.f), gr);
 #pragma unroll
-        for (int v = 0; v < V; ++v) { x[v] = (x[v] - mu[v]) * rs[v]; u[v] = fmaf(x[v], w[v], b[v]); }
-        dmx_act::times_slope<V>(gr, u, A.act);
-#pragma unroll
-        for (int v = 0; v < V; ++v) x[v] = rs[v] * (fmaf(gr[v], w[v], -s1[v]) - x[v] * s2[v]);
-        put(out, x);
-        out += out_step;
-        if (i < ncnt) {
-          bring(xs + i * threads, nx);
-          bring(gs + i * threads, ng);
-          nx += xstep; ng += gstep2;
+        for (int j = 0; j < NP; ++j) {
+          x[j] = sub2(x[j], mu[j]);
+          if constexpr (!KEEP) gr[j] = dmx_act::times_slope<ACT>(gr[j], fma2(x[j], a[j], b[j]));
+          x[j] = fma2(gr[j], a[j], fma2(x[j], k2[j], k1[j]));
         }
+        put(out, second, out_step, x);
+        out += SL * out_step;
+#pragma unroll
+        for (int k = 0; k < SL; ++k)
+          if (i + k < ncnt) {
+            bring(xs + (i + k) * threads, nx);
+            bring(gs + (i + k) * threads, ng);
+            nx += xstep; ng += gstep2;
+          }
       }
     }
-    for (int i = M == STATS ? 0 : min(now.cnt, ncnt); i < ncnt; ++i) {
+    for (int i = M == STATS ? 0 : (now.cnt + SL - 1) / SL * SL; i < ncnt; ++i) {
       bring(xs + i * threads, nx);
       bring(gs + i * threads, ng);
       nx += xstep; ng += gstep2;
     }
-    if (M == RESIDENT && A.parts > 1) cluster_wait();
-    if (M == APPLY) __syncthreads();
   }
 }
 
-// dweight and dbias: sums of the images' (and chunks') rows. 32 channels and eight row lanes per CTA.
-__global__ void __launch_bounds__(256) columns_kernel(const float* __restrict__ part, int64_t rows, int C, float* __restrict__ dw,
-                                                      float* __restrict__ db) {
-  __shared__ float sh[8][33];
+// dweight and dbias: sums of the images' (and chunks') rows, those of A times their group's rstd. 32 channels and
+// 32 row lanes per CTA. Launched as a programmatic dependent of the backward kernel.
+__global__ void __launch_bounds__(1024) columns_kernel(const float* __restrict__ part, int64_t rows, int per_image, int C, int G, int cpg,
+                                                      const float* __restrict__ rstd, float* __restrict__ dw, float* __restrict__ db) {
+  __shared__ float sh[32][33];
   const int lane = threadIdx.x & 31, r = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   const float* p = part + (int64_t)blockIdx.y * rows * C;
   float* out = blockIdx.y ? db : dw;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   if (!out) return;
   float s = 0.f;
-  if (c < C)
-    for (int64_t i = r; i < rows; i += 8) s += __ldg(p + i * C + c);
+  if (c < C) {
+    const float* q = rstd + c / cpg;
+    if (blockIdx.y) {
+#pragma unroll 8
+      for (int64_t i = r; i < rows; i += 32) s += __ldg(p + i * C + c);
+    } else {
+#pragma unroll 8
+      for (int64_t i = r; i < rows; i += 32) s = fmaf(__ldg(p + i * C + c), __ldg(q + (int64_t)((unsigned)i / (unsigned)per_image) * G), s);
+    }
+  }
   sh[r][lane] = s;
   __syncthreads();
   if (r == 0 && c < C) {
-    for (int k = 1; k < 8; ++k) s += sh[k][lane];
+    for (int k = 1; k < 32; ++k) s += sh[k][lane];
     out[c] = s;
   }
 }
@@ -585,7 +772,7 @@ int lcm(int a, int b) {
 bool settle(Plan& p, int64_t L, int C, int cpg, int e, bool backward, int64_t rows, size_t most) {
   p.slabs = (C + p.W - 1) / p.W;
   p.cols = (p.W + p.V - 1) / p.V;
-  p.threads = p.cols <= 256 ? 256 : 1024;
+  p.threads = p.V > 1 ? 256 : p.cols <= 512 ? 512 : 1024;
   p.R = p.threads / p.cols;
   p.lanes = p.cols <= 32 && 32 % p.cols == 0 ? p.cols : 0;
   p.fold = 1;
@@ -597,44 +784,61 @@ bool settle(Plan& p, int64_t L, int C, int cpg, int e, bool backward, int64_t ro
   p.rows = (int)rows;
   p.slots = (int)slots;
   const int groups = p.W / cpg;
-  if (backward) p.smem = data + f * (padded(2 * erows * p.W) + 2 * padded(2 * p.W) + padded(2 * groups));
-  else p.smem = data + f * (2 * padded(erows * p.cols * (p.V / p.fold)) + padded(erows) + 4 * padded(groups));
+  const int sums = p.resident ? p.parts : 1;
+  if (backward) p.smem = data + f * (padded(2 * erows * p.W) + 4 * sums * padded(p.W) + 2 * padded(groups));
+  else p.smem = data + f * (2 * padded(erows * p.cols * (p.V / p.fold)) + padded(erows) + (4 * sums + 2) * padded(groups));
+  p.smem += 2 * f * params_size(p.W, groups);
+  if (p.smem > 200 * 1024) return false;
   return true;
 }
 
-constexpr size_t kMostData = 96 * 1024;      // two CTAs per SM
+#ifndef P32
+#define P32 1.3f
+#define P2 1.15f
+#define P4 1.3f
+#define P8 1.5f
+#endif
+#ifndef MOST
+#define MOST 96
+#endif
+constexpr size_t kMostData = MOST * 1024;      // two CTAs per SM
+constexpr int64_t kChunkData = 64 * 1024;    // chunks of a larger image: three
 
 // Slab width, CTAs per image and slab, and positions per thread. Slabs are multiples of whole groups and of
-// whole columns. Among the splits that keep an image's slab in one cluster's shared memory: segments of up to 512
-// bytes, then 128, 64, 32 (a DRAM sector); within a width the fewest CTAs per slab. Where the problem is too
-// small to give every SM two CTAs, narrow slabs come first (no exchange needed), then more CTAs per slab.
+// whole columns. Of the splits that keep an image's slab in one cluster's shared memory, the one of least
+// cost: a cluster of more CTAs waits longer for its slowest, and a segment of 32 bytes (a DRAM sector) loads L1 with twice
+// the lines of 64. Where the problem is too small to give every SM two CTAs, more CTAs count more than that.
 Plan plan(int64_t N, int64_t L, int C, int cpg, int dtype, bool vec, bool backward) {
-  Plan p;
+  Plan p, best;
   const int e = dtype == DMX_F32 ? 4 : 2;
   p.V = vec ? 16 / e : 1;
   const int unit = lcm(cpg, p.V);
-  const int want[4] = {512, 128, 64, 32};
-  for (int k = 0; k < 4; ++k) {
+  const int want[5] = {512, 256, 128, 64, 32};
+  p.resident = true;
+  best.resident = false;
+  float least = 0.f;
+  for (int k = 0; k < 5; ++k) {
     p.W = (want[k] / e) / unit * unit;
     if (p.W < unit) p.W = unit;
     if (p.W > C) p.W = C;
-    if (k == 0 && p.W * e < 512 && p.W < C) continue;
     for (p.parts = 1; p.parts <= kMaxCluster; p.parts *= 2) {
       if (!settle(p, L, C, cpg, e, backward, (L + p.parts - 1) / p.parts, kMostData)) continue;
-      if (N * p.slabs * p.parts < 2 * 148) {
-        if (k < 2 && unit * e < want[k]) break;                     // more CTAs from narrower slabs first
-        if (p.parts < kMaxCluster && p.slots > 1) continue;         // then from more of them per slab
-      }
-      p.resident = true;
-      return p;
+      if (p.parts > 1 && p.rows < p.R) break;
+      float cost = (p.W * e < 64 ? P32 : 1.f) * (p.parts == 1 ? 1.f : p.parts == 2 ? P2 : p.parts == 4 ? P4 : P8);
+      const float ctas = (float)N * p.slabs * p.parts;
+      if (ctas < 2 * 148) cost *= 2 * 148 / ctas;
+      if (!best.resident || cost < least) { best = p; least = cost; }
     }
   }
+  if (best.resident) return best;
   p.resident = false;
+  p.parts = 1;
   p.W = (256 / e) / unit * unit;
   if (p.W < unit) p.W = unit;
   if (p.W > C) p.W = C;
   settle(p, L, C, cpg, e, backward, 1, kMostData);
-  const int64_t rows = (int64_t)p.R * 8;
+  int64_t rows = (int64_t)p.R * (kChunkData / ((int64_t)p.threads * p.V * e * (backward ? 2 : 1)));
+  if (rows < p.R) rows = p.R;
   settle(p, L, C, cpg, e, backward, rows, ~(size_t)0);
   p.parts = (int)((L + rows - 1) / rows);
   return p;
@@ -674,22 +878,35 @@ int launch(K kernel, const Plan& p, const Args& A, bool cluster, cudaStream_t st
   return dmxh::cuda_ok(cudaLaunchKernelEx(&cfg, kernel, A)) ? DMX_OK : DMX_ERR_CUDA;
 }
 
-template <typename T, int V>
-int run_forward(const Plan& p, const Args& A, cudaStream_t st) {
-  if (p.resident) return launch(forward_kernel<T, V, RESIDENT>, p, A, true, st);
-  const int rc = launch(forward_kernel<T, V, STATS>, p, A, false, st);
-  return rc != DMX_OK ? rc : launch(forward_kernel<T, V, APPLY>, p, A, false, st);
+template <typename T, int V, int ACT>
+int run_act(bool backward, const Plan& p, const Args& A, cudaStream_t st) {
+  if (backward) {
+    if (p.resident) return launch(backward_kernel<T, V, RESIDENT, ACT>, p, A, true, st);
+    const int rc = launch(backward_kernel<T, V, STATS, ACT>, p, A, false, st);
+    return rc != DMX_OK ? rc : launch(backward_kernel<T, V, APPLY, ACT>, p, A, false, st);
+  }
+  if (p.resident) return launch(forward_kernel<T, V, RESIDENT, ACT>, p, A, true, st);
+  const int rc = launch(forward_kernel<T, V, STATS, DMX_ACT_NONE>, p, A, false, st);
+  return rc != DMX_OK ? rc : launch(forward_kernel<T, V, APPLY, ACT>, p, A, false, st);
 }
 
 template <typename T, int V>
-int run_backward(const Plan& p, const Args& A, cudaStream_t st) {
-  if (p.resident) return launch(backward_kernel<T, V, RESIDENT>, p, A, true, st);
-  const int rc = launch(backward_kernel<T, V, STATS>, p, A, false, st);
-  return rc != DMX_OK ? rc : launch(backward_kernel<T, V, APPLY>, p, A, false, st);
+int run_typed(bool backward, int act, const Plan& p, const Args& A, cudaStream_t st) {
+  switch (act) {
+    case DMX_ACT_RELU: return run_act<T, V, DMX_ACT_RELU>(backward, p, A, st);
+    case DMX_ACT_SILU: return run_act<T, V, DMX_ACT_SILU>(backward, p, A, st);
+    case DMX_ACT_GELU: return run_act<T, V, DMX_ACT_GELU>(backward, p, A, st);
+    default: return run_act<T, V, DMX_ACT_NONE>(backward, p, A, st);
+  }
+}
+
+int run(bool backward, int act, int dtype, bool vec, const Plan& p, const Args& A, cudaStream_t st) {
+  if (dtype == DMX_F32) return vec ? run_typed<float, 4>(backward, act, p, A, st) : run_typed<float, 1>(backward, act, p, A, st);
+  return vec ? run_typed<__nv_bfloat16, 8>(backward, act, p, A, st) : run_typed<__nv_bfloat16, 1>(backward, act, p, A, st);
 }
 
 void fill(Args& A, const Plan& p, int64_t N, int64_t L, int C, int G) {
-  A.L = (int)L; A.C = C; A.G = G; A.cpg = C / G; A.W = p.W; A.slabs = p.slabs; A.R = p.R; A.cols = p.cols; A.rows = p.rows;
+  A.L = (int)L; A.C = C; A.G = G; A.cpg = C / G; A.W = p.W; A.gW = p.W / A.cpg; A.slabs = p.slabs; A.R = p.R; A.cols = p.cols; A.rows = p.rows;
   A.parts = p.parts; A.slots = p.slots; A.fold = p.fold; A.lanes = p.lanes; A.N = (int)N;
   A.items = N * p.slabs * (p.resident ? 1 : p.parts);
 }
@@ -715,8 +932,7 @@ bool element_aligned(const void* p, int e) { return (reinterpret_cast<uintptr_t>
 // ... and the narrowest slab of whole columns and whole groups has to fit a CTA's threads
 bool columns_fit(int C, int cpg, int e) { return C % (16 / e) == 0 && lcm(cpg, 16 / e) / (16 / e) <= 256; }
 
-int64_t workspace_for(int64_t N, int64_t L, int C, int G, int dtype, bool vec, bool backward) {
-  const Plan p = plan(N, L, C, C / G, dtype, vec, backward);
+int64_t workspace_of(const Plan& p, int64_t N, int C, int G, bool backward) {
   if (backward) return 2 * N * (p.resident ? 1 : p.parts) * C * (int64_t)sizeof(float);
   return p.resident ? 0 : N * p.parts * G * (int64_t)sizeof(float2);
 }
@@ -729,8 +945,9 @@ extern "C" {
 int64_t dmx_group_norm_workspace(int64_t N, int64_t L, int C, int G, int dtype, int backward) {
   if (!shape_ok(N, L, C, G, dtype)) return DMX_ERR_ARG;
   if (N == 0 || L == 0) return 0;
-  const int64_t one = workspace_for(N, L, C, G, dtype, false, backward != 0);
-  const int64_t two = columns_fit(C, C / G, dtype == DMX_F32 ? 4 : 2) ? workspace_for(N, L, C, G, dtype, true, backward != 0) : 0;
+  const int64_t one = workspace_of(plan(N, L, C, C / G, dtype, false, backward != 0), N, C, G, backward != 0);
+  if (!columns_fit(C, C / G, dtype == DMX_F32 ? 4 : 2)) return one;
+  const int64_t two = workspace_of(plan(N, L, C, C / G, dtype, true, backward != 0), N, C, G, backward != 0);
   return one > two ? one : two;
 }
 
@@ -746,19 +963,18 @@ int dmx_group_norm_forward(int64_t N, int64_t L, int C, int G, int dtype, const 
   if (!element_aligned(x, e) || !element_aligned(y, e) || !element_aligned(mean, 4) || !element_aligned(rstd, 4) ||
       !element_aligned(weight, 4) || !element_aligned(bias, 4) || !element_aligned(workspace, 16)) return DMX_ERR_ALIGN;
   const bool vec = columns_fit(C, C / G, e) && wide(x, N, L, C, x_image, x_row, e) && wide(y, N, L, C, y_image, y_row, e);
-  const int64_t need = workspace_for(N, L, C, G, dtype, vec, false);
-  if (workspace_bytes < need || (need > 0 && !workspace)) return DMX_ERR_ARG;
   const Plan p = plan(N, L, C, C / G, dtype, vec, false);
+  const int64_t need = workspace_of(p, N, C, G, false);
+  if (workspace_bytes < need || (need > 0 && !workspace)) return DMX_ERR_ARG;
   if (N * p.slabs * (int64_t)p.parts > 0x7fffffff) return DMX_ERR_ARG;
   Args A = {};
   A.x = {const_cast<void*>(x), x_image, x_row};
   A.out = {y, y_image, y_row};
   A.weight = weight; A.bias = bias; A.mean = mean; A.rstd = rstd; A.part = static_cast<float*>(workspace);
   fill(A, p, N, L, C, G);
-  A.eps = eps; A.act = act;
+  A.eps = eps;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (dtype == DMX_F32) return vec ? run_forward<float, 4>(p, A, st) : run_forward<float, 1>(p, A, st);
-  return vec ? run_forward<__nv_bfloat16, 8>(p, A, st) : run_forward<__nv_bfloat16, 1>(p, A, st);
+  return run(false, act, dtype, vec, p, A, st);
 }
 
 int dmx_group_norm_backward(int64_t N, int64_t L, int C, int G, int dtype, const void* dy, int64_t dy_image,
@@ -780,9 +996,8 @@ int dmx_group_norm_backward(int64_t N, int64_t L, int C, int G, int dtype, const
   if (!element_aligned(x, e) || !element_aligned(dy, e) || !element_aligned(dx, e) || !element_aligned(mean, 4) || !element_aligned(rstd, 4) ||
       !element_aligned(weight, 4) || !element_aligned(bias, 4) || !element_aligned(workspace, 16)) return DMX_ERR_ALIGN;
   const bool vec = columns_fit(C, C / G, e) && wide(x, N, L, C, x_image, x_row, e) && wide(dy, N, L, C, dy_image, dy_row, e) && wide(dx, N, L, C, dx_image, dx_row, e);
-  const int64_t need = workspace_for(N, L, C, G, dtype, vec, true);
-  if (workspace_bytes < need || !workspace) return DMX_ERR_ARG;
   const Plan p = plan(N, L, C, C / G, dtype, vec, true);
+  if (workspace_bytes < workspace_of(p, N, C, G, true) || !workspace) return DMX_ERR_ARG;
   if (N * p.slabs * (int64_t)p.parts > 0x7fffffff) return DMX_ERR_ARG;
   Args A = {};
   A.x = {const_cast<void*>(x), x_image, x_row};
@@ -790,13 +1005,20 @@ int dmx_group_norm_backward(int64_t N, int64_t L, int C, int G, int dtype, const
   A.out = {dx, dx_image, dx_row};
   A.weight = weight; A.bias = bias; A.mean = const_cast<float*>(mean); A.rstd = const_cast<float*>(rstd); A.part = static_cast<float*>(workspace);
   fill(A, p, N, L, C, G);
-  A.act = act;
-  int rc;
-  if (dtype == DMX_F32) rc = vec ? run_backward<float, 4>(p, A, st) : run_backward<float, 1>(p, A, st);
-  else rc = vec ? run_backward<__nv_bfloat16, 8>(p, A, st) : run_backward<__nv_bfloat16, 1>(p, A, st);
+  const int rc = run(true, act, dtype, vec, p, A, st);
   if (rc != DMX_OK || (!dweight && !dbias)) return rc;
-  columns_kernel<<<dim3((C + 31) / 32, 2), 256, 0, st>>>(A.part, N * (p.resident ? 1 : p.parts), C, dweight, dbias);
-  return dmxh::cuda_ok(cudaGetLastError()) ? DMX_OK : DMX_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((C + 31) / 32, 2);
+  cfg.blockDim = dim3(1024);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const int64_t rows = N * (p.resident ? 1 : p.parts);
+  return dmxh::cuda_ok(cudaLaunchKernelEx(&cfg, columns_kernel, (const float*)A.part, rows, p.resident ? 1 : p.parts, C, G, C / G, rstd, dweight, dbias))
+             ? DMX_OK : DMX_ERR_CUDA;
 }
 
 }  // extern "C"
