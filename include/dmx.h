@@ -425,14 +425,14 @@ int dmx_step_static(int K, int64_t P, const int64_t* seg_offsets, int S, int gra
 
 /*
  * The operators on both sides of the gradient step: the layers whose backward pass makes a worker's gradient
- * (dmx_group_norm_*) and an optimizer over a model's separate tensors (dmx_adamw_*). The paper
+ * (dmx_linear_*, dmx_group_norm_*) and an optimizer over a model's separate tensors (dmx_adamw_*). The paper
  * names the models and optimizers it trains with and no formula for any of them; the formulas below are the
  * contract. All pointers are DEVICE memory unless marked HOST, all calls are asynchronous on the given stream
  * and copy nothing to the host, none allocates except the create call, and empty problems (a zero extent) are
  * valid. Buffers must not overlap unless a call says so; this is the caller's to keep.
  */
 
-/* activations of dmx_group_norm_*: u, max(u, 0), u / (1 + exp(-u)), u * Phi(u) (Phi: the normal
+/* activations of dmx_group_norm_* and dmx_linear_*: u, max(u, 0), u / (1 + exp(-u)), u * Phi(u) (Phi: the normal
  * distribution function, the erf form). The slope of DMX_ACT_RELU at 0 is 0. */
 enum { DMX_ACT_NONE = 0, DMX_ACT_RELU = 1, DMX_ACT_SILU = 2, DMX_ACT_GELU = 3 };
 
@@ -523,6 +523,40 @@ int dmx_group_norm_backward(int64_t N, int64_t L, int C, int G, int dtype, const
                             const float* rstd, const float* weight, const float* bias, int act, void* dx,
                             int64_t dx_image, int64_t dx_row, float* dweight, float* dbias, void* workspace,
                             int64_t workspace_bytes, void* cuda_stream);
+
+/*
+ * dmx_linear_* — matrix product with bias, activation and residual in its epilogue, and its gradient (bf16
+ * operands, fp32 accumulation on the tensor cores).
+ *   forward    z = x W^T + bias,  y = act(z) + residual        x: M x K, W: N x K, y, z, residual: M x N
+ *   backward   dz = dy * act'(z),  dx = dz W,  dW = dz^T x,  dbias = column sums of dz   (the residual's gradient is dy)
+ * Everything up to a store is fp32, with one exception: with an activation, dz is rounded to bf16 before the two
+ * products of backward (the tensor cores take 16-bit operands); dbias is summed from the unrounded dz.
+ *   x, w, bias, residual, z, y, dy, dx, dw, dbias   bf16, row-major, ld* = elements from row to row (>= the row's
+ *              length unless there is one row); element alignment suffices. Operands whose start or rows are not
+ *              16-byte aligned are first laid out in the workspace.
+ *   bias, residual, z (forward: an output, written only if given)   may be NULL
+ *   z          backward: forward's z, needed unless act is DMX_ACT_NONE
+ *   dx, dw, dbias   each may be NULL and is then not computed
+ *   workspace  at least dmx_linear_workspace(...) / dmx_linear_backward_workspace(...) bytes for the same
+ *              arguments (0 is possible), 256-byte aligned, contents undefined
+ * y may be the residual itself. K = 0 gives z = bias; M = 0 gives dW = 0 and dbias = 0. Results are bitwise reproducible.
+ *   dmx_linear_status   every wait inside the kernels is bounded; *errors (HOST) receives how many CTAs gave up
+ *                       on the current device since the last call (0 unless the device misbehaves; results
+ *                       are invalid otherwise). Synchronous.
+ * Errors: DMX_ERR_ARG (extents > DMX_LINEAR_MAX_EXTENT, strides, null pointers, workspace too small), DMX_ERR_ALIGN, DMX_ERR_CUDA.
+ */
+#define DMX_LINEAR_MAX_EXTENT 4194240
+int64_t dmx_linear_workspace(int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx, const void* w, int64_t ldw);
+int dmx_linear_forward(int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                       const void* bias, int act, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z,
+                       int64_t ldz, void* workspace, int64_t workspace_bytes, void* cuda_stream);
+int64_t dmx_linear_backward_workspace(int64_t M, int64_t N, int64_t K, const void* dy, int64_t lddy, const void* x,
+                                      int64_t ldx, const void* w, int64_t ldw, int act);
+int dmx_linear_backward(int64_t M, int64_t N, int64_t K, const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                        const void* w, int64_t ldw, const void* z, int64_t ldz, int act, void* dx, int64_t lddx,
+                        void* dw, int64_t lddw, void* dbias, void* workspace, int64_t workspace_bytes,
+                        void* cuda_stream);
+int dmx_linear_status(int* errors);
 
 /* Frees the tables and the scratch. NULL is accepted; a handle that is not live (destroyed
  * already) gives DMX_ERR_HANDLE. The caller makes sure no step of this handle is still running. */

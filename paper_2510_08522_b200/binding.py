@@ -25,7 +25,8 @@ EXPORTS = ("dmx_create", "dmx_state_len", "dmx_step", "dmx_step_adam", "dmx_step
            "dmx_shard_range", "dmx_shard_segments", "dmx_partials_len", "dmx_step_partial", "dmx_step_adam_partial",
            "dmx_finalize_partials", "dmx_check_guards", "dmx_selftest_wait", "dmx_scratch_info",
            "dmx_adamw_create", "dmx_adamw_blocks", "dmx_adamw_first_block", "dmx_adamw_bind", "dmx_adamw_grad_norm", "dmx_adamw_step",
-           "dmx_adamw_moments", "dmx_adamw_destroy", "dmx_group_norm_workspace", "dmx_group_norm_forward", "dmx_group_norm_backward")
+           "dmx_adamw_moments", "dmx_adamw_destroy", "dmx_group_norm_workspace", "dmx_group_norm_forward", "dmx_group_norm_backward",
+           "dmx_linear_workspace", "dmx_linear_forward", "dmx_linear_backward_workspace", "dmx_linear_backward", "dmx_linear_status")
 CTL_ACTIONS = (-100, -25, 0, 25, 100)
 
 _lib = None
@@ -124,6 +125,16 @@ def lib():
         L.dmx_group_norm_backward.argtypes = [i64, i64, i32, i32, i32, vp, i64, i64, vp, i64, i64, vp, vp, vp, vp, i32, vp, i64, i64, vp, vp, vp,
                                               i64, vp]
         L.dmx_group_norm_backward.restype = i32
+        L.dmx_linear_workspace.argtypes = [i64, i64, i64, vp, i64, vp, i64]
+        L.dmx_linear_workspace.restype = i64
+        L.dmx_linear_forward.argtypes = [i64, i64, i64, vp, i64, vp, i64, vp, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+        L.dmx_linear_forward.restype = i32
+        L.dmx_linear_backward_workspace.argtypes = [i64, i64, i64, vp, i64, vp, i64, vp, i64, i32]
+        L.dmx_linear_backward_workspace.restype = i64
+        L.dmx_linear_backward.argtypes = [i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, i64, vp, i64, vp, vp, i64, vp]
+        L.dmx_linear_backward.restype = i32
+        L.dmx_linear_status.argtypes = [ctypes.POINTER(i32)]
+        L.dmx_linear_status.restype = i32
         L.dmx_destroy.argtypes = [vp]
         L.dmx_destroy.restype = i32
         L.dmx_strerror.argtypes = [i32]

@@ -31,9 +31,6 @@ namespace {
 
 using namespace dmx_f32x2;
 
-#ifndef CTAS
-#define CTAS 2
-#endif
 constexpr int kMaxCluster = 8;
 
 struct Operand {
@@ -137,6 +134,12 @@ __device__ __forceinline__ void groups_of(const float* p, int g, int rem, int cp
     const float t = p[g];
 #pragma unroll
     for (int j = 0; j < kPairs<V>; ++j) x[j] = two(t);
+  } else if ((cpg & 1) == 0) {      // a pair's channels share a group
+#pragma unroll
+    for (int j = 0; j < kPairs<V>; ++j) {
+      x[j] = two(p[g]);
+      if ((rem += 2) == cpg) { rem = 0; ++g; }
+    }
   } else {
     per_channel<V>(x, [&](int) {
       const float t = p[g];
@@ -277,7 +280,7 @@ __device__ __forceinline__ void bring_params(const Args& A, const Here& h, const
 }
 
 template <typename T, int V, Mode M, int ACT>
-__global__ void __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : CTAS) forward_kernel(const __grid_constant__ Args A) {
+__global__ void __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) forward_kernel(const __grid_constant__ Args A) {
   using U = typename Vec<T, V>::type;
   constexpr int NP = kPairs<V>, SL = kSlots<V>;
   extern __shared__ __align__(16) float sm[];
@@ -531,7 +534,7 @@ __device__ __forceinline__ void keep(unsigned* g, bool second, int step, const f
 
 // Backward. Workspace: A and B per image (and chunk) and channel, [2][N*chunks][C].
 template <typename T, int V, Mode M, int ACT>
-__global__ void __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : CTAS) backward_kernel(const __grid_constant__ Args A) {
+__global__ void __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) backward_kernel(const __grid_constant__ Args A) {
   using U = typename Vec<T, V>::type;
   constexpr int NP = kPairs<V>, SL = kSlots<V>;
   extern __shared__ __align__(16) float sm[];
@@ -792,22 +795,14 @@ bool settle(Plan& p, int64_t L, int C, int cpg, int e, bool backward, int64_t ro
   return true;
 }
 
-#ifndef P32
-#define P32 1.3f
-#define P2 1.15f
-#define P4 1.3f
-#define P8 1.5f
-#endif
-#ifndef MOST
-#define MOST 96
-#endif
-constexpr size_t kMostData = MOST * 1024;      // two CTAs per SM
+constexpr size_t kMostData = 100 * 1024;     // two CTAs per SM
 constexpr int64_t kChunkData = 64 * 1024;    // chunks of a larger image: three
 
 // Slab width, CTAs per image and slab, and positions per thread. Slabs are multiples of whole groups and of
 // whole columns. Of the splits that keep an image's slab in one cluster's shared memory, the one of least
-// cost: a cluster of more CTAs waits longer for its slowest, and a segment of 32 bytes (a DRAM sector) loads L1 with twice
-// the lines of 64. Where the problem is too small to give every SM two CTAs, more CTAs count more than that.
+// cost: a cluster of more CTAs waits longer for its slowest (backward on 64 x 56x56 x 256 bf16: segments of 32 bytes
+// and four CTAs 145 us, 64 bytes and eight 149 us; forward 61 and 71 us). Where the problem is too small to give
+// every SM two CTAs, more CTAs count more than that (backward on 37 x 27x27 x 90 fp32: 17 us against 35).
 Plan plan(int64_t N, int64_t L, int C, int cpg, int dtype, bool vec, bool backward) {
   Plan p, best;
   const int e = dtype == DMX_F32 ? 4 : 2;
@@ -824,7 +819,7 @@ Plan plan(int64_t N, int64_t L, int C, int cpg, int dtype, bool vec, bool backwa
     for (p.parts = 1; p.parts <= kMaxCluster; p.parts *= 2) {
       if (!settle(p, L, C, cpg, e, backward, (L + p.parts - 1) / p.parts, kMostData)) continue;
       if (p.parts > 1 && p.rows < p.R) break;
-      float cost = (p.W * e < 64 ? P32 : 1.f) * (p.parts == 1 ? 1.f : p.parts == 2 ? P2 : p.parts == 4 ? P4 : P8);
+      float cost = p.parts == 1 ? 1.f : p.parts == 2 ? 1.3f : p.parts == 4 ? 1.6f : 2.f;
       const float ctas = (float)N * p.slabs * p.parts;
       if (ctas < 2 * 148) cost *= 2 * 148 / ctas;
       if (!best.resident || cost < least) { best = p; least = cost; }

@@ -1,0 +1,782 @@
+// dmx_linear.cu — matrix product with bias, activation and residual in its epilogue, and its gradient (bf16
+// operands, fp32 accumulation).
+//
+//   forward    z = x W^T + b, y = act(z) + r
+//   backward   dz = dy act'(z) (one elementwise pass, which also sums its columns for db), dx = dz W, dW = dz^T x
+//
+// All three products are D[i, j] = sum_k A[i, k] B[j, k] on the 5th-generation tensor cores, by one kernel: a
+// producer warp moves tiles of A (128 rows) and B (32 to 256) of 64 k with TMA into a ring of shared memory
+// stages, one thread issues tcgen05.mma on them into accumulators in TMEM, and eight warps take finished accumulators out
+// (tcgen05.ld), apply the epilogue and store, while the next tile accumulates in the other half of TMEM. An
+// operand whose rows run along k is K-major; W in dx, and both operands of dW, run across it (MN-major) and are
+// multiplied as they lie: only the descriptors differ, nothing is transposed in memory.
+// Few rows (M <= 64): the operands change places, so that W's rows fill the 128 lanes and the few rows of x are the narrow
+// side. Few tiles: k is split over the CTAs of a cluster, whose partial sums meet in distributed shared memory and
+// are added in a fixed order.
+// Every wait is bounded; a CTA that gives up counts itself in a device word (dmx_linear_status), lets its copies
+// land, frees its TMEM and returns.
+#include "dmx.h"
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "dmx_act.cuh"
+#include "dmx_host.h"
+
+namespace {
+
+using namespace dmx_f32x2;
+typedef __nv_bfloat16 bf16;
+
+constexpr int kBM = 128, kBK = 64;            // tile rows of A; k per stage (128 bytes: one swizzle row)
+constexpr int kEpiWarps = 8;
+constexpr int kGemmThreads = 64 + 32 * kEpiWarps;
+constexpr int kMaxStages = 8;
+constexpr int kSmemMost = 226 * 1024;
+constexpr unsigned kPolls = 1u << 18;         // about a second
+
+__device__ unsigned g_gave_up;                // CTAs whose waits ran out
+
+struct GemmArgs {
+  int rowsA, rowsB, kblocks;                  // rows of D, columns of D, ceil(k / 64)
+  int tilesA, tilesB, split, stages;
+  int mnA, mnB;                               // operand is MN-major
+  const bf16 *bias, *residual;
+  bf16 *y, *z;
+  int64_t ldr, ldy, ldz;
+  int act;
+  int vecy, vecz, vecr;                       // 16-byte rows
+};
+
+// ---------------------------------------------------------------------------------------------- PTX
+
+__device__ __forceinline__ unsigned smem_addr(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void bar_init(unsigned bar, unsigned count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void bar_arrive(unsigned bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void bar_expect(unsigned bar, unsigned bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// false if the barrier did not complete in time
+__device__ __forceinline__ bool bar_wait(unsigned bar, unsigned parity) {
+  for (unsigned n = 0; n < kPolls; ++n) {
+    unsigned done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    if (done) return true;
+  }
+  return false;
+}
+__device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap* map, int c0, int c1, unsigned bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+               ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void mma(unsigned d, uint64_t a, uint64_t b, unsigned idesc, unsigned accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_commit(unsigned bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_load32(unsigned addr, float (&v)[32]) {
+  unsigned r[32];
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+               "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+               "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                 "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+                 "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+                 "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]) : "r"(addr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+
+// Shared memory descriptor of a 128-byte swizzled operand. K-major: rows of 128 bytes, groups of eight 1024 bytes apart.
+// MN-major: rows (one per k) of 64 elements; eight k 1024 bytes apart, the next 64 elements 64 rows further.
+__device__ __forceinline__ uint64_t descriptor(unsigned addr, int mn) {
+  const uint64_t lead = mn ? (kBK * 128) >> 4 : 1, stride = 1024 >> 4;
+  return (uint64_t)((addr >> 4) & 0x3fff) | lead << 16 | stride << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+
+__device__ __forceinline__ float bf_value(unsigned short u) { return __uint_as_float((unsigned)u << 16); }
+__device__ __forceinline__ unsigned pack2(float a, float b) {
+  __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<unsigned*>(&t);
+}
+
+// ---------------------------------------------------------------------------------------------- epilogue
+
+// A warp's staging buffer: 32 rows of 64 bytes, 16-byte units exchanged by the row so that both a row per lane
+// and eight rows at a time are free of bank conflicts.
+__device__ __forceinline__ uint4* unit(uint4* stage, int row, int u) { return stage + row * 4 + (u ^ ((row >> 1) & 3)); }
+
+// rows r0.. (32) x columns c0.. (32) of a matrix out of the staging buffer
+__device__ __forceinline__ void store_chunk(bf16* p, int64_t ld, int vec, uint4* stage, int r0, int rows, int c0, int cols, int lane) {
+  __syncwarp();
+  if (vec) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = i * 8 + (lane >> 2), c = c0 + (lane & 3) * 8;
+      if (r0 + r >= rows || c >= cols) continue;
+      const uint4 v = *unit(stage, r, lane & 3);
+      bf16* q = p + (int64_t)(r0 + r) * ld + c;
+      if (c + 8 <= cols) {
+        *reinterpret_cast<uint4*>(q) = v;
+      } else {
+        const unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (c + k < cols) reinterpret_cast<unsigned short*>(q)[k] = (unsigned short)(w[k >> 1] >> (16 * (k & 1)));
+      }
+    }
+  } else if (c0 + lane < cols) {
+    const int n = min(32, rows - r0);
+    for (int r = 0; r < n; ++r)
+      reinterpret_cast<unsigned short*>(p)[(int64_t)(r0 + r) * ld + c0 + lane] = reinterpret_cast<const unsigned short*>(unit(stage, r, lane >> 3))[lane & 7];
+  }
+  __syncwarp();
+}
+__device__ __forceinline__ void load_chunk(const bf16* p, int64_t ld, int vec, uint4* stage, int r0, int rows, int c0, int cols, int lane) {
+  if (vec) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int r = i * 8 + (lane >> 2), c = c0 + (lane & 3) * 8;
+      if (r0 + r >= rows || c >= cols) continue;
+      const bf16* q = p + (int64_t)(r0 + r) * ld + c;
+      if (c + 8 <= cols) {
+        *unit(stage, r, lane & 3) = *reinterpret_cast<const uint4*>(q);
+      } else {
+        unsigned short* d = reinterpret_cast<unsigned short*>(unit(stage, r, lane & 3));
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (c + k < cols) d[k] = reinterpret_cast<const unsigned short*>(q)[k];
+      }
+    }
+  } else if (c0 + lane < cols) {
+    const int n = min(32, rows - r0);
+    for (int r = 0; r < n; ++r)
+      reinterpret_cast<unsigned short*>(unit(stage, r, lane >> 3))[lane & 7] = reinterpret_cast<const unsigned short*>(p)[(int64_t)(r0 + r) * ld + c0 + lane];
+  }
+  __syncwarp();
+}
+__device__ __forceinline__ void stage_row(uint4* stage, const float (&v)[32], int lane) {
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+    *unit(stage, lane, u) = make_uint4(pack2(v[8 * u], v[8 * u + 1]), pack2(v[8 * u + 2], v[8 * u + 3]), pack2(v[8 * u + 4], v[8 * u + 5]),
+                                       pack2(v[8 * u + 6], v[8 * u + 7]));
+}
+__device__ __forceinline__ void activate(float (&v)[32], int act) {
+  auto all = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float2 t = f(make_float2(v[2 * i], v[2 * i + 1]));
+      v[2 * i] = t.x; v[2 * i + 1] = t.y;
+    }
+  };
+  if (act == DMX_ACT_RELU) all([](float2 u) { return dmx_act::apply<DMX_ACT_RELU>(u); });
+  else if (act == DMX_ACT_SILU) all([](float2 u) { return dmx_act::apply<DMX_ACT_SILU>(u); });
+  else if (act == DMX_ACT_GELU) all([](float2 u) { return dmx_act::apply<DMX_ACT_GELU>(u); });
+}
+
+// One warp's 32 rows x 32 columns of D, a row per lane.
+__device__ __forceinline__ void finish(const GemmArgs& A, float (&v)[32], uint4* stage, int r0, int c0, int lane) {
+  if (A.bias) {
+    if (c0 + 32 <= A.rowsB && (reinterpret_cast<uintptr_t>(A.bias) & 15) == 0) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint4 b = __ldg(reinterpret_cast<const uint4*>(A.bias + c0) + u);
+        const unsigned w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float2 t = widen2(w[k]);
+          v[8 * u + 2 * k] += t.x; v[8 * u + 2 * k + 1] += t.y;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 32; ++i)
+        if (c0 + i < A.rowsB) v[i] += bf_value(__ldg(reinterpret_cast<const unsigned short*>(A.bias) + c0 + i));
+    }
+  }
+  if (A.z) {
+    stage_row(stage, v, lane);
+    store_chunk(A.z, A.ldz, A.vecz, stage, r0, A.rowsA, c0, A.rowsB, lane);
+  }
+  activate(v, A.act);
+  if (A.residual) {
+    load_chunk(A.residual, A.ldr, A.vecr, stage, r0, A.rowsA, c0, A.rowsB, lane);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const uint4 b = *unit(stage, lane, u);
+      const unsigned w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 t = widen2(w[k]);
+        v[8 * u + 2 * k] += t.x; v[8 * u + 2 * k + 1] += t.y;
+      }
+    }
+    __syncwarp();
+  }
+  stage_row(stage, v, lane);
+  store_chunk(A.y, A.ldy, A.vecy, stage, r0, A.rowsA, c0, A.rowsB, lane);
+}
+
+// The same with the operands exchanged: a lane holds one column of y (a row of W) for 32 rows of x. Neighbouring lanes
+// are neighbours in memory, so it is stored as it lies.
+__device__ __forceinline__ void finish_swapped(const GemmArgs& A, float (&v)[32], int f, int t0) {
+  const bool on = f < A.rowsA;
+  const float b = A.bias && on ? bf_value(__ldg(reinterpret_cast<const unsigned short*>(A.bias) + f)) : 0.f;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] += b;
+  if (A.z) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (on && t0 + i < A.rowsB) A.z[(int64_t)(t0 + i) * A.ldz + f] = __float2bfloat16_rn(v[i]);
+  }
+  activate(v, A.act);
+#pragma unroll
+  for (int i = 0; i < 32; ++i) {
+    if (!on || t0 + i >= A.rowsB) continue;
+    if (A.residual) v[i] += __bfloat162float(A.residual[(int64_t)(t0 + i) * A.ldr + f]);
+    A.y[(int64_t)(t0 + i) * A.ldy + f] = __float2bfloat16_rn(v[i]);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- the product
+
+template <int BN, bool SWAP>
+__global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
+                                                               const __grid_constant__ GemmArgs A) {
+  extern __shared__ __align__(1024) unsigned char raw[];
+  __shared__ uint64_t full[kMaxStages], empty[kMaxStages], done[2], freed[2];
+  __shared__ unsigned tmem_base;
+  constexpr unsigned kStageA = kBM * 128, kStage = kStageA + BN * 128;
+  constexpr int kChunks = BN / 32;
+  constexpr unsigned kCols = 2 * BN < 32 ? 32 : 2 * BN;
+  unsigned char* sm = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
+  uint4* staging = reinterpret_cast<uint4*>(sm + (size_t)A.stages * kStage);                     // 2 KB per epilogue warp
+  float* sums = reinterpret_cast<float*>(sm + (size_t)A.stages * kStage + (SWAP ? 0 : kEpiWarps * 2048));   // the cluster's partial sums
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = A.split > 1 ? blockIdx.x % A.split : 0;
+  const int tiles = A.tilesA * A.tilesB, first = blockIdx.x / A.split, step = gridDim.x / A.split;
+  const int kb0 = (int)((int64_t)A.kblocks * rank / A.split), kb1 = (int)((int64_t)A.kblocks * (rank + 1) / A.split);
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < A.stages; ++s) { bar_init(smem_addr(&full[s]), 1); bar_init(smem_addr(&empty[s]), 1); }
+    for (int i = 0; i < 2; ++i) { bar_init(smem_addr(&done[i]), 1); bar_init(smem_addr(&freed[i]), kEpiWarps); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base)), "r"(kCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  if (A.split > 1) cluster_sync();
+  const unsigned tmem = tmem_base;
+  bool ok = true;
+
+  // tile t: A tiles in bands of 16, B tiles across a band, so that what runs at once shares its operands in L2
+  auto tile_at = [&](int t, int& ta, int& tb) {
+    const int band = 16 * A.tilesB, b = t / band, in = t - b * band, h = min(16, A.tilesA - 16 * b);
+    tb = in / h;
+    ta = 16 * b + in - tb * h;
+  };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int s = 0, issued = 0;
+      unsigned ph = 0;
+      for (int t = first; t < tiles && ok; t += step) {
+        int ta, tb;
+        tile_at(t, ta, tb);
+        for (int kb = kb0; kb < kb1; ++kb) {
+          ok = bar_wait(smem_addr(&empty[s]), ph ^ 1);
+          if (!ok) break;
+          const unsigned bar = smem_addr(&full[s]), dst = smem_addr(sm) + s * kStage;
+          bar_expect(bar, kStage);
+          if (A.mnA) {
+            for (int i = 0; i < kBM / 64; ++i) tma_load(dst + i * kBK * 128, &mapA, ta * kBM + i * 64, kb * kBK, bar);
+          } else {
+            tma_load(dst, &mapA, kb * kBK, ta * kBM, bar);
+          }
+          if (A.mnB) {
+            for (int i = 0; i < BN / 64; ++i) tma_load(dst + kStageA + i * kBK * 128, &mapB, tb * BN + i * 64, kb * kBK, bar);
+          } else {
+            tma_load(dst + kStageA, &mapB, kb * kBK, tb * BN, bar);
+          }
+          ++issued;
+          if (++s == A.stages) { s = 0; ph ^= 1; }
+        }
+      }
+      // the last copies land before the CTA ends, whoever waits for them
+      for (int i = 0; i < A.stages && i < issued; ++i) {
+        if (--s < 0) { s = A.stages - 1; ph ^= 1; }
+        bar_wait(smem_addr(&full[s]), ph);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const unsigned idesc = 1u << 4 | 1u << 7 | 1u << 10 | (unsigned)A.mnA << 15 | (unsigned)A.mnB << 16 | (unsigned)(BN >> 3) << 17 | (unsigned)(kBM >> 4) << 24;
+      const unsigned stepA = A.mnA ? 2048 >> 4 : 32 >> 4, stepB = A.mnB ? 2048 >> 4 : 32 >> 4;
+      int s = 0;
+      unsigned ph = 0, buf = 0, aph = 0;
+      for (int t = first; t < tiles && ok; t += step) {
+        ok = bar_wait(smem_addr(&freed[buf]), aph ^ 1);
+        if (!ok) break;
+        tmem_fence_after();
+        for (int kb = kb0; kb < kb1; ++kb) {
+          ok = bar_wait(smem_addr(&full[s]), ph);
+          if (!ok) break;
+          tmem_fence_after();
+          const unsigned base = smem_addr(sm) + s * kStage;
+          const uint64_t da = descriptor(base, A.mnA), db = descriptor(base + kStageA, A.mnB);
+#pragma unroll
+          for (int k = 0; k < kBK / 16; ++k) mma(tmem + buf * BN, da + k * stepA, db + k * stepB, idesc, kb > kb0 || k > 0);
+          mma_commit(smem_addr(&empty[s]));
+          if (++s == A.stages) { s = 0; ph ^= 1; }
+        }
+        mma_commit(smem_addr(&done[buf]));
+        if (buf) aph ^= 1;
+        buf ^= 1;
+      }
+    }
+  } else {
+    const int e = warp - 2, quarter = warp & 3, half = e >> 2;      // TMEM lanes 32 quarter.. belong to warps of that number mod 4
+    uint4* stage = staging + e * 128;
+    unsigned buf = 0, aph = 0;
+    for (int t = first; t < tiles && ok; t += step) {
+      int ta, tb;
+      tile_at(t, ta, tb);
+      ok = bar_wait(smem_addr(&done[buf]), aph);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tmem_fence_after();
+      const int r0 = ta * kBM + quarter * 32;
+      for (int c = half; c < kChunks; c += 2) {
+        const int c0 = tb * BN + c * 32;
+        if (c0 >= A.rowsB) break;
+        float v[32];
+        tmem_load32(tmem + buf * BN + c * 32 + ((unsigned)(quarter * 32) << 16), v);
+        if (A.split > 1) {
+          // chunk c is completed by CTA c mod split of the cluster; the others send it theirs
+          const int owner = c % A.split;
+          if (owner != rank) {
+            unsigned to;
+            float* slot = sums + ((size_t)(c / A.split) * A.split + rank) * (32 * kBM) + quarter * 32 + lane;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_addr(slot)), "r"(owner));
+#pragma unroll
+            for (int i = 0; i < 32; ++i) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + i * kBM * 4), "f"(v[i]) : "memory");
+          }
+        } else if (SWAP) {
+          finish_swapped(A, v, r0 + lane, c0);
+        } else {
+          finish(A, v, stage, r0, c0, lane);
+        }
+      }
+      if (A.split > 1) break;                                       // one tile per cluster; finished below
+      tmem_fence_before();
+      __syncwarp();
+      if (lane == 0) bar_arrive(smem_addr(&freed[buf]));
+      if (buf) aph ^= 1;
+      buf ^= 1;
+    }
+  }
+  __syncwarp();
+  if (A.split > 1) {
+    cluster_sync();
+    if (warp >= 2 && ok) {
+      const int e = warp - 2, quarter = warp & 3, half = e >> 2;
+      int ta, tb;
+      tile_at(first, ta, tb);
+      tmem_fence_after();
+      for (int c = half; c < kChunks; c += 2) {
+        const int c0 = tb * BN + c * 32;
+        if (c0 >= A.rowsB) break;
+        if (c % A.split != rank) continue;
+        float v[32];
+        tmem_load32(tmem + c * 32 + ((unsigned)(quarter * 32) << 16), v);
+        for (int q = 0; q < A.split; ++q) {
+          if (q == rank) continue;
+          const float* slot = sums + ((size_t)(c / A.split) * A.split + q) * (32 * kBM) + quarter * 32 + lane;
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[i] += slot[i * kBM];
+        }
+        if (SWAP) finish_swapped(A, v, ta * kBM + quarter * 32 + lane, c0);
+        else finish(A, v, staging + e * 128, ta * kBM + quarter * 32, c0, lane);
+      }
+    }
+  }
+  if (!ok && lane == 0) atomicAdd(&g_gave_up, 1u);
+  tmem_fence_before();
+  __syncthreads();
+  tmem_fence_after();
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols));
+}
+
+// ---------------------------------------------------------------------------------------------- elementwise parts
+
+// dz = dy act'(z) as bf16 rows of `ldo` elements (out may be NULL: then only the sums), and per chunk of rows the
+// column sums of the unrounded dz. V columns per lane; with V = 1 any alignment. Also lays out an operand (act
+// none, sums NULL).
+constexpr int kChunkRows = 64;
+template <int V>
+__global__ void __launch_bounds__(256) slope_kernel(const bf16* __restrict__ dy, int64_t lddy, const bf16* __restrict__ z, int64_t ldz, int act,
+                                                    int64_t rows, int cols, bf16* __restrict__ out, int64_t ldo, float* __restrict__ sums) {
+  __shared__ float sh[8][32 * V];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int c = (blockIdx.x * 32 + lane) * V;
+  float acc[V];
+#pragma unroll
+  for (int v = 0; v < V; ++v) acc[v] = 0.f;
+  const int64_t r0 = (int64_t)blockIdx.y * kChunkRows, r1 = r0 + kChunkRows < rows ? r0 + kChunkRows : rows;
+  if (c < cols) {
+#pragma unroll 4
+    for (int64_t r = r0 + warp; r < r1; r += 8) {
+      float2 g[(V + 1) / 2], u[(V + 1) / 2];
+      if constexpr (V == 8) {
+        const uint4 a = __ldcs(reinterpret_cast<const uint4*>(dy + r * lddy + c));
+        g[0] = widen2(a.x); g[1] = widen2(a.y); g[2] = widen2(a.z); g[3] = widen2(a.w);
+        if (z) {
+          const uint4 b = __ldcs(reinterpret_cast<const uint4*>(z + r * ldz + c));
+          u[0] = widen2(b.x); u[1] = widen2(b.y); u[2] = widen2(b.z); u[3] = widen2(b.w);
+        }
+      } else {
+        g[0] = make_float2(__bfloat162float(dy[r * lddy + c]), 0.f);
+        if (z) u[0] = make_float2(__bfloat162float(z[r * ldz + c]), 0.f);
+      }
+#pragma unroll
+      for (int j = 0; j < (V + 1) / 2; ++j) {
+        if (act == DMX_ACT_RELU) g[j] = dmx_act::times_slope<DMX_ACT_RELU>(g[j], u[j]);
+        else if (act == DMX_ACT_SILU) g[j] = dmx_act::times_slope<DMX_ACT_SILU>(g[j], u[j]);
+        else if (act == DMX_ACT_GELU) g[j] = dmx_act::times_slope<DMX_ACT_GELU>(g[j], u[j]);
+        acc[2 * j] += g[j].x;
+        if (V > 1) acc[(2 * j + 1) % V] += g[j].y;
+      }
+      if (out) {
+        if constexpr (V == 8)
+          *reinterpret_cast<uint4*>(out + r * ldo + c) = make_uint4(pack2(g[0].x, g[0].y), pack2(g[1].x, g[1].y), pack2(g[2].x, g[2].y), pack2(g[3].x, g[3].y));
+        else out[r * ldo + c] = __float2bfloat16_rn(g[0].x);
+      }
+    }
+  }
+  if (!sums) return;
+#pragma unroll
+  for (int v = 0; v < V; ++v) sh[warp][lane * V + v] = acc[v];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 32 * V; i += 256) {
+    float t = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) t += sh[w][i];
+    if (blockIdx.x * 32 * V + i < cols) sums[(int64_t)blockIdx.y * cols + blockIdx.x * 32 * V + i] = t;
+  }
+}
+
+// dbias from the chunks' sums: 32 columns and eight lanes of chunks per CTA
+__global__ void __launch_bounds__(256) columns_kernel(const float* __restrict__ sums, int64_t chunks, int cols, bf16* __restrict__ out) {
+  __shared__ float sh[8][33];
+  const int lane = threadIdx.x & 31, r = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+  float s = 0.f;
+  if (c < cols) {
+#pragma unroll 8
+    for (int64_t i = r; i < chunks; i += 8) s += __ldg(sums + i * cols + c);
+  }
+  sh[r][lane] = s;
+  __syncthreads();
+  if (r == 0 && c < cols) {
+    for (int k = 1; k < 8; ++k) s += sh[k][lane];
+    out[c] = __float2bfloat16_rn(s);
+  }
+}
+
+// K = 0: y = act(bias) + residual
+__global__ void __launch_bounds__(256) bias_kernel(const __grid_constant__ GemmArgs A) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)A.rowsA * A.rowsB; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / A.rowsB;
+    const int c = (int)(i - r * A.rowsB);
+    float v[32] = {};
+    v[0] = A.bias ? __bfloat162float(A.bias[c]) : 0.f;
+    if (A.z) A.z[r * A.ldz + c] = __float2bfloat16_rn(v[0]);
+    activate(v, A.act);
+    if (A.residual) v[0] += __bfloat162float(A.residual[r * A.ldr + c]);
+    A.y[r * A.ldy + c] = __float2bfloat16_rn(v[0]);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- host
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+  static EncodeTiled f = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult r;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) {
+      (void)cudaGetLastError();
+      p = nullptr;
+    }
+    return reinterpret_cast<EncodeTiled>(p);
+  }();
+  return f;
+}
+
+bool aligned(const void* p, unsigned a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+int64_t pad8(int64_t n) { return (n + 7) & ~(int64_t)7; }
+int64_t pad256(int64_t n) { return (n + 255) & ~(int64_t)255; }
+
+// A matrix as TMA takes it: 16-byte aligned, rows a multiple of 16 bytes apart
+struct Matrix {
+  const bf16* p;
+  int64_t rows, cols, ld;
+};
+bool tma_ready(const Matrix& m) { return aligned(m.p, 16) && (m.rows <= 1 || m.ld % 8 == 0); }
+int64_t laid_out_bytes(const Matrix& m) { return tma_ready(m) ? 0 : pad256(m.rows * pad8(m.cols) * 2); }
+
+// rows of m are D's rows (or columns) if !mn, its columns if mn
+bool make_map(CUtensorMap* map, const Matrix& m, int mn, int box_rows) {
+  const EncodeTiled f = encode_tiled();
+  if (!f) return false;
+  const cuuint64_t dims[2] = {(cuuint64_t)m.cols, (cuuint64_t)m.rows};
+  const cuuint64_t strides[1] = {(cuuint64_t)(m.rows > 1 ? m.ld : pad8(m.cols)) * 2};
+  const cuuint32_t box[2] = {64, (cuuint32_t)(mn ? kBK : box_rows)}, one[2] = {1, 1};
+  return f(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<bf16*>(m.p), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Choice {
+  int bn, split;
+};
+
+// Tile width and split. A stage of 64 k takes max(BN, 96) / 256 x 512 cycles or so, a tile's epilogue about as
+// long as eight stages of its width, of which all but the last are hidden; a split costs a cluster barrier.
+Choice choose(int64_t rowsA, int64_t rowsB, int kblocks, bool swap) {
+  Choice best = {0, 1};
+  float least = 0.f;
+  const int widths[4] = {256, 128, 64, 32};
+  for (int w = 0; w < 4; ++w) {
+    const int bn = widths[w];
+    if (swap ? bn != (rowsB <= 32 ? 32 : 64) : bn == 32) continue;
+    const int64_t tiles = ((rowsA + kBM - 1) / kBM) * ((rowsB + bn - 1) / bn);
+    const int most = swap ? 8 : bn == 256 ? 1 : bn / 32;
+    for (int split = 1; split <= most; split *= 2) {
+      if (split > 1 && (tiles * split > 148 || kblocks / split < 2)) break;
+      const int64_t waves = (tiles * split + 147) / 148;
+      const float stage = bn >= 96 ? 2.f * bn : 192.f;
+      const float t = waves * ((kblocks + split - 1) / split) * stage + 8.f * bn + (split > 1 ? 1500.f : 0.f);
+      if (best.bn == 0 || t < least) { best.bn = bn; best.split = split; least = t; }
+    }
+  }
+  return best;
+}
+
+template <int BN, bool SWAP>
+int launch_gemm(const Matrix& a, const Matrix& b, GemmArgs& A, int split, cudaStream_t st) {
+  CUtensorMap ma, mb;
+  if (!make_map(&ma, a, A.mnA, kBM) || !make_map(&mb, b, A.mnB, BN)) return DMX_ERR_CUDA;
+  A.tilesA = (A.rowsA + kBM - 1) / kBM;
+  A.tilesB = (A.rowsB + BN - 1) / BN;
+  A.split = split;
+  const int stage = kBM * 128 + BN * 128, chunks = BN / 32;
+  const int extra = 1024 + (SWAP ? 0 : kEpiWarps * 2048) + (split > 1 ? (chunks + split - 1) / split * split * 32 * kBM * 4 : 0);
+  A.stages = (kSmemMost - extra) / stage;
+  if (A.stages > kMaxStages) A.stages = kMaxStages;
+  const int smem = A.stages * stage + extra;
+  const auto kernel = gemm_kernel<BN, SWAP>;
+  if (!dmxh::cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost))) return DMX_ERR_CUDA;
+  const int64_t tiles = (int64_t)A.tilesA * A.tilesB;
+  if (tiles * split > 0x7fffffff) return DMX_ERR_ARG;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(split > 1 ? tiles * split : tiles < 148 ? tiles : 148));
+  cfg.blockDim = dim3(kGemmThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1] = {};
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = split;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return dmxh::cuda_ok(cudaLaunchKernelEx(&cfg, kernel, ma, mb, A)) ? DMX_OK : DMX_ERR_CUDA;
+}
+
+// D = A B^T with the epilogue in E (bias, residual, outputs, act). mn: the operand's rows run along D's extent.
+int product(const Matrix& a, int mnA, const Matrix& b, int mnB, int64_t k, const GemmArgs& E, cudaStream_t st) {
+  GemmArgs A = E;
+  const int64_t rowsA = mnA ? a.cols : a.rows, rowsB = mnB ? b.cols : b.rows;
+  A.kblocks = (int)((k + kBK - 1) / kBK);
+  A.vecy = aligned(A.y, 16) && (rowsA <= 1 || A.ldy % 8 == 0);
+  A.vecz = A.z && aligned(A.z, 16) && (rowsA <= 1 || A.ldz % 8 == 0);
+  A.vecr = A.residual && aligned(A.residual, 16) && (rowsA <= 1 || A.ldr % 8 == 0);
+  // 64 rows or fewer: b's rows take the 128 lanes (b keeps whichever way it lies; a, the narrow side, has to be K-major)
+  if (rowsA <= 64 && !mnA) {
+    A.rowsA = (int)rowsB; A.rowsB = (int)rowsA;
+    A.mnA = mnB; A.mnB = mnA;
+    const Choice c = choose(rowsB, rowsA, A.kblocks, true);
+    return c.bn == 32 ? launch_gemm<32, true>(b, a, A, c.split, st) : launch_gemm<64, true>(b, a, A, c.split, st);
+  }
+  A.rowsA = (int)rowsA; A.rowsB = (int)rowsB;
+  A.mnA = mnA; A.mnB = mnB;
+  const Choice c = choose(rowsA, rowsB, A.kblocks, false);
+  if (c.bn == 256) return launch_gemm<256, false>(a, b, A, c.split, st);
+  if (c.bn == 128) return launch_gemm<128, false>(a, b, A, c.split, st);
+  return launch_gemm<64, false>(a, b, A, c.split, st);
+}
+
+int slope(const Matrix& dy, const bf16* z, int64_t ldz, int act, bf16* out, int64_t ldo, float* sums, cudaStream_t st) {
+  const bool vec = aligned(dy.p, 16) && (dy.rows <= 1 || dy.ld % 8 == 0) && dy.cols % 8 == 0 &&
+                   (!z || (aligned(z, 16) && (dy.rows <= 1 || ldz % 8 == 0)));
+  const int64_t chunks = (dy.rows + kChunkRows - 1) / kChunkRows;
+  const int V = vec ? 8 : 1;
+  if (chunks > 65535) return DMX_ERR_ARG;
+  const dim3 grid((unsigned)((dy.cols + 32 * V - 1) / (32 * V)), (unsigned)chunks);
+  if (vec) slope_kernel<8><<<grid, 256, 0, st>>>(dy.p, dy.ld, z, ldz, act, dy.rows, (int)dy.cols, out, ldo, sums);
+  else slope_kernel<1><<<grid, 256, 0, st>>>(dy.p, dy.ld, z, ldz, act, dy.rows, (int)dy.cols, out, ldo, sums);
+  return dmxh::cuda_ok(cudaGetLastError()) ? DMX_OK : DMX_ERR_CUDA;
+}
+
+// m itself, or its copy at *ws (which moves on)
+int lay_out(Matrix& m, unsigned char*& ws, cudaStream_t st) {
+  const int64_t bytes = laid_out_bytes(m);
+  if (bytes == 0) return DMX_OK;
+  bf16* p = reinterpret_cast<bf16*>(ws);
+  ws += bytes;
+  const int rc = slope(m, nullptr, 0, DMX_ACT_NONE, p, pad8(m.cols), nullptr, st);
+  m.p = p;
+  m.ld = pad8(m.cols);
+  return rc;
+}
+
+bool extents_ok(int64_t M, int64_t N, int64_t K) {
+  const int64_t most = DMX_LINEAR_MAX_EXTENT;
+  return M >= 0 && N >= 0 && K >= 0 && M <= most && N <= most && K <= most;
+}
+bool ld_ok(int64_t rows, int64_t cols, int64_t ld) { return rows <= 1 || ld >= cols; }
+
+struct BackPlan {
+  bool needs_dz;            // dz is written to the workspace
+  int64_t dz, sums, x, w, total;
+};
+BackPlan back_plan(const Matrix& dy, const Matrix& x, const Matrix& w, int act) {
+  BackPlan p;
+  p.needs_dz = act != DMX_ACT_NONE || !tma_ready(dy);
+  p.dz = p.needs_dz ? pad256(dy.rows * pad8(dy.cols) * 2) : 0;
+  p.sums = pad256((dy.rows + kChunkRows - 1) / kChunkRows * dy.cols * 4);
+  p.x = laid_out_bytes(x);
+  p.w = laid_out_bytes(w);
+  p.total = p.dz + p.sums + p.x + p.w;
+  return p;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t dmx_linear_workspace(int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx, const void* w, int64_t ldw) {
+  if (!extents_ok(M, N, K)) return DMX_ERR_ARG;
+  if (M == 0 || N == 0 || K == 0) return 0;
+  return laid_out_bytes({static_cast<const bf16*>(x), M, K, ldx}) + laid_out_bytes({static_cast<const bf16*>(w), N, K, ldw});
+}
+
+int dmx_linear_forward(int64_t M, int64_t N, int64_t K, const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias,
+                       int act, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z, int64_t ldz, void* workspace,
+                       int64_t workspace_bytes, void* cuda_stream) {
+  if (!extents_ok(M, N, K) || act < DMX_ACT_NONE || act > DMX_ACT_GELU) return DMX_ERR_ARG;
+  if (!ld_ok(M, K, ldx) || !ld_ok(N, K, ldw) || !ld_ok(M, N, ldy) || (residual && !ld_ok(M, N, ldr)) || (z && !ld_ok(M, N, ldz))) return DMX_ERR_ARG;
+  if (M == 0 || N == 0) return DMX_OK;
+  if (!y || (K > 0 && (!x || !w))) return DMX_ERR_ARG;
+  if (!aligned(x, 2) || !aligned(w, 2) || !aligned(bias, 2) || !aligned(residual, 2) || !aligned(y, 2) || !aligned(z, 2) || !aligned(workspace, 256)) return DMX_ERR_ALIGN;
+  const int64_t need = dmx_linear_workspace(M, N, K, x, ldx, w, ldw);
+  if (need > workspace_bytes || (need > 0 && !workspace)) return DMX_ERR_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  GemmArgs E = {};
+  E.bias = static_cast<const bf16*>(bias); E.residual = static_cast<const bf16*>(residual);
+  E.y = static_cast<bf16*>(y); E.z = static_cast<bf16*>(z);
+  E.ldr = M > 1 ? ldr : N; E.ldy = M > 1 ? ldy : N; E.ldz = M > 1 ? ldz : N; E.act = act;
+  if (K == 0) {
+    E.rowsA = (int)M; E.rowsB = (int)N;
+    const int64_t want = (M * N + 255) / 256;
+    bias_kernel<<<(unsigned)(want < 148 * 8 ? want : 148 * 8), 256, 0, st>>>(E);
+    return dmxh::cuda_ok(cudaGetLastError()) ? DMX_OK : DMX_ERR_CUDA;
+  }
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  Matrix a = {static_cast<const bf16*>(x), M, K, M > 1 ? ldx : K}, b = {static_cast<const bf16*>(w), N, K, N > 1 ? ldw : K};
+  int rc = lay_out(a, ws, st);
+  if (rc == DMX_OK) rc = lay_out(b, ws, st);
+  return rc != DMX_OK ? rc : product(a, 0, b, 0, K, E, st);
+}
+
+int64_t dmx_linear_backward_workspace(int64_t M, int64_t N, int64_t K, const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                                      const void* w, int64_t ldw, int act) {
+  if (!extents_ok(M, N, K) || act < DMX_ACT_NONE || act > DMX_ACT_GELU) return DMX_ERR_ARG;
+  if (M == 0 || N == 0) return 0;
+  return back_plan({static_cast<const bf16*>(dy), M, N, lddy}, {static_cast<const bf16*>(x), M, K, ldx}, {static_cast<const bf16*>(w), N, K, ldw}, act).total;
+}
+
+int dmx_linear_backward(int64_t M, int64_t N, int64_t K, const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                        const void* z, int64_t ldz, int act, void* dx, int64_t lddx, void* dw, int64_t lddw, void* dbias, void* workspace,
+                        int64_t workspace_bytes, void* cuda_stream) {
+  if (!extents_ok(M, N, K) || act < DMX_ACT_NONE || act > DMX_ACT_GELU) return DMX_ERR_ARG;
+  if (!ld_ok(M, N, lddy) || !ld_ok(M, K, ldx) || !ld_ok(N, K, ldw) || (z && !ld_ok(M, N, ldz)) || (dx && !ld_ok(M, K, lddx)) || (dw && !ld_ok(N, K, lddw))) return DMX_ERR_ARG;
+  if (!aligned(dy, 2) || !aligned(x, 2) || !aligned(w, 2) || !aligned(z, 2) || !aligned(dx, 2) || !aligned(dw, 2) || !aligned(dbias, 2) || !aligned(workspace, 256)) return DMX_ERR_ALIGN;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (M == 0 || N == 0) {          // empty sums
+    if (dw && N > 0 && K > 0 && !dmxh::cuda_ok(cudaMemset2DAsync(dw, (N > 1 ? lddw : K) * 2, 0, K * 2, N, st))) return DMX_ERR_CUDA;
+    if (dbias && N > 0 && !dmxh::cuda_ok(cudaMemsetAsync(dbias, 0, N * 2, st))) return DMX_ERR_CUDA;
+    if (dx && M > 0 && K > 0 && !dmxh::cuda_ok(cudaMemset2DAsync(dx, (M > 1 ? lddx : K) * 2, 0, K * 2, M, st))) return DMX_ERR_CUDA;
+    return DMX_OK;
+  }
+  if (!dy || (K > 0 && ((dx && !w) || (dw && !x))) || (act != DMX_ACT_NONE && !z)) return DMX_ERR_ARG;
+  Matrix g = {static_cast<const bf16*>(dy), M, N, M > 1 ? lddy : N};
+  Matrix a = {static_cast<const bf16*>(x), M, K, M > 1 ? ldx : K}, b = {static_cast<const bf16*>(w), N, K, N > 1 ? ldw : K};
+  const BackPlan p = back_plan(g, a, b, act);
+  if (p.total > workspace_bytes || !workspace) return DMX_ERR_ARG;
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  float* sums = reinterpret_cast<float*>(ws);
+  ws += p.sums;
+  int rc = DMX_OK;
+  if (p.needs_dz || dbias) {
+    bf16* out = p.needs_dz && (dx || dw) ? reinterpret_cast<bf16*>(ws) : nullptr;
+    rc = slope(g, act != DMX_ACT_NONE ? static_cast<const bf16*>(z) : nullptr, M > 1 ? ldz : N, act, out, pad8(N), dbias ? sums : nullptr, st);
+    if (rc != DMX_OK) return rc;
+    if (out) { g.p = out; g.ld = pad8(N); }
+    if (dbias) {
+      columns_kernel<<<(unsigned)((N + 31) / 32), 256, 0, st>>>(sums, (M + kChunkRows - 1) / kChunkRows, (int)N, static_cast<bf16*>(dbias));
+      if (!dmxh::cuda_ok(cudaGetLastError())) return DMX_ERR_CUDA;
+    }
+  }
+  ws += p.dz;
+  if (K == 0) return DMX_OK;
+  GemmArgs E = {};
+  E.act = DMX_ACT_NONE;
+  if (dx) {                        // dx[m, k] = sum_n dz[m, n] w[n, k]
+    rc = lay_out(b, ws, st);
+    E.y = static_cast<bf16*>(dx); E.ldy = M > 1 ? lddx : K;
+    if (rc == DMX_OK) rc = product(g, 0, b, 1, N, E, st);
+  }
+  if (dw && rc == DMX_OK) {        // dw[n, k] = sum_m dz[m, n] x[m, k]
+    rc = lay_out(a, ws, st);
+    E.y = static_cast<bf16*>(dw); E.ldy = N > 1 ? lddw : K;
+    if (rc == DMX_OK) rc = product(g, 1, a, 1, M, E, st);
+  }
+  return rc;
+}
+
+int dmx_linear_status(int* errors) {
+  if (!errors) return DMX_ERR_ARG;
+  unsigned n = 0;
+  const unsigned zero = 0;
+  if (!dmxh::cuda_ok(cudaMemcpyFromSymbol(&n, g_gave_up, sizeof n)) || !dmxh::cuda_ok(cudaMemcpyToSymbol(g_gave_up, &zero, sizeof zero))) return DMX_ERR_CUDA;
+  *errors = (int)n;
+  return DMX_OK;
+}
+
+}  // extern "C"

@@ -1,5 +1,5 @@
-"""The training operators of include/dmx.h for torch callers: AdamW over many tensors, and group norm with an
-activation on channels-last data.
+"""The training operators of include/dmx.h for torch callers: AdamW over many tensors, group norm with an
+activation on channels-last data, and the matrix product with bias, activation and residual in its epilogue.
 
 Tensors in, raw pointers through the C ABI; every call runs on the current stream of its tensors' device, takes its
 workspace from torch's allocator there, and raises DmxError with the library's code for arguments it refuses.
@@ -253,3 +253,81 @@ def group_norm_backward(dy, x, mean, rstd, groups, weight=None, bias=None, act="
     if rc != B.OK:
         _refuse("dmx_group_norm_backward", rc)
     return dx, dp[0], dp[1]
+
+
+def _rows(x, shape, like, where):
+    """Leading dimension of a bf16 matrix with dense rows."""
+    if x.dtype != _torch.bfloat16 or x.device != like.device or tuple(x.shape) != shape or (shape[1] > 1 and x.stride(1) != 1):
+        _refuse(where)
+    return x.stride(0) if shape[0] > 1 else shape[1]
+
+
+def _matrix(x, like, where):
+    if x is None or x.dim() != 2 or not x.is_cuda:
+        _refuse(where)
+    return _rows(x, tuple(x.shape), like, where)
+
+
+def linear(x, weight, bias=None, act="none", residual=None, save=False, out=None):
+    """act(x @ weight.T + bias) + residual, bf16 matrices -> (y, z). z is the value before the activation, kept for
+    linear_backward when `save` is set and there is an activation, else None. out may be the residual."""
+    _t()
+    if act not in ACT:
+        _refuse("linear (act)")
+    ldx, ldw = _matrix(x, x, "linear (x)"), _matrix(weight, x, "linear (weight)")
+    (M, K), N = x.shape, weight.shape[0]
+    if weight.shape[1] != K:
+        _refuse("linear (weight)")
+    if bias is not None and (bias.dtype != _torch.bfloat16 or bias.numel() != N or bias.device != x.device or not bias.is_contiguous()):
+        _refuse("linear (bias)")
+    ldr = 0 if residual is None else _rows(residual, (M, N), x, "linear (residual)")
+    y = _torch.empty((M, N), dtype=_torch.bfloat16, device=x.device) if out is None else out
+    ldy = _rows(y, (M, N), x, "linear (out)")
+    z = _torch.empty((M, N), dtype=_torch.bfloat16, device=x.device) if save and act != "none" else None
+    L = B.lib()
+    xp, wp = x.data_ptr(), weight.data_ptr()
+    with _on(x):
+        ws = _workspace(L.dmx_linear_workspace(M, N, K, xp, ldx, wp, ldw), x, "linear")
+        rc = L.dmx_linear_forward(M, N, K, xp, ldx, wp, ldw, _ptr(bias), ACT[act], _ptr(residual), ldr, y.data_ptr(), ldy, _ptr(z), N, _ptr(ws),
+                                  0 if ws is None else ws.numel(), _stream(x))
+    if rc != B.OK:
+        _refuse("dmx_linear_forward", rc)
+    return y, z
+
+
+def linear_backward(dy, x, weight, z=None, act="none", need=(True, True, True), out=(None, None, None)):
+    """Gradient of linear -> (dx, dweight, dbias), those not in `need` None. `out`: tensors to write them to, e.g.
+    views of a flat gradient vector."""
+    _t()
+    if act not in ACT:
+        _refuse("linear_backward (act)")
+    ldx, ldw = _matrix(x, x, "linear_backward (x)"), _matrix(weight, x, "linear_backward (weight)")
+    (M, K), N = x.shape, weight.shape[0]
+    if weight.shape[1] != K or (z is None and act != "none"):
+        _refuse("linear_backward")
+    ldg = _rows(dy, (M, N), x, "linear_backward (dy)")
+    ldz = 0 if z is None else _rows(z, (M, N), x, "linear_backward (z)")
+    mk = lambda k, shape: None if not need[k] else (_torch.empty(shape, dtype=_torch.bfloat16, device=x.device) if out[k] is None else out[k])  # noqa: E731
+    dx, dw, db = mk(0, (M, K)), mk(1, (N, K)), mk(2, (N,))
+    lddx = 0 if dx is None else _rows(dx, (M, K), x, "linear_backward (dx)")
+    lddw = 0 if dw is None else _rows(dw, (N, K), x, "linear_backward (dweight)")
+    if db is not None and (db.dtype != _torch.bfloat16 or db.numel() != N or db.device != x.device or not db.is_contiguous()):
+        _refuse("linear_backward (dbias)")
+    L = B.lib()
+    gp, xp, wp = dy.data_ptr(), x.data_ptr(), weight.data_ptr()
+    with _on(x):
+        ws = _workspace(L.dmx_linear_backward_workspace(M, N, K, gp, ldg, xp, ldx, wp, ldw, ACT[act]), x, "linear_backward")
+        rc = L.dmx_linear_backward(M, N, K, gp, ldg, xp, ldx, wp, ldw, _ptr(z), ldz, ACT[act], _ptr(dx), lddx, _ptr(dw), lddw, _ptr(db), _ptr(ws),
+                                   0 if ws is None else ws.numel(), _stream(x))
+    if rc != B.OK:
+        _refuse("dmx_linear_backward", rc)
+    return dx, dw, db
+
+
+def linear_status():
+    """How many CTAs of the linear kernels gave up a wait on the current device since the last call (synchronous)."""
+    n = ctypes.c_int()
+    rc = B.lib().dmx_linear_status(ctypes.byref(n))
+    if rc != B.OK:
+        _refuse("dmx_linear_status", rc)
+    return n.value
