@@ -53,6 +53,13 @@ struct GemmArgs {
 // ---------------------------------------------------------------------------------------------- PTX
 
 __device__ __forceinline__ unsigned smem_addr(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
+// One lane of a converged warp, chosen so that the compiler knows it is one (tensor core and copy instructions take
+// warp-uniform operands).
+__device__ __forceinline__ bool elect() {
+  unsigned p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
 __device__ __forceinline__ void bar_init(unsigned bar, unsigned count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ void bar_arrive(unsigned bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void bar_expect(unsigned bar, unsigned bytes) {
@@ -62,7 +69,7 @@ __device__ __forceinline__ void bar_expect(unsigned bar, unsigned bytes) {
 __device__ __forceinline__ bool bar_wait(unsigned bar, unsigned parity) {
   for (unsigned n = 0; n < kPolls; ++n) {
     unsigned done;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                  : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     if (done) return true;
   }
@@ -71,6 +78,24 @@ __device__ __forceinline__ bool bar_wait(unsigned bar, unsigned parity) {
 __device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap* map, int c0, int c1, unsigned bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
+}
+// In a pair of CTAs the loads of both count on the first one's barrier.
+__device__ __forceinline__ void tma_load_pair(unsigned dst, const CUtensorMap* map, int c0, int c1, unsigned bar) {
+  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+               ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
+}
+__device__ __forceinline__ unsigned in_cta(unsigned addr, int rank) {     // the same place in another CTA of the cluster
+  unsigned a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+  return a;
+}
+__device__ __forceinline__ void bar_arrive_cluster(unsigned bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void mma_pair(unsigned d, uint64_t a, uint64_t b, unsigned idesc, unsigned accumulate) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_commit_pair(unsigned bar) {           // to that barrier of both CTAs
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((unsigned short)3) : "memory");
 }
 __device__ __forceinline__ void mma(unsigned d, uint64_t a, uint64_t b, unsigned idesc, unsigned accumulate) {
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
@@ -251,36 +276,49 @@ __device__ __forceinline__ void finish_swapped(const GemmArgs& A, float (&v)[32]
 
 // ---------------------------------------------------------------------------------------------- the product
 
-template <int BN, bool SWAP>
+// PAIR: two CTAs on neighbouring SMs (a cluster) work on one tile of 256 rows: each loads half of A and half of B, the
+// first one's MMA thread multiplies on both SMs at once, and each holds its 128 rows of D in its own TMEM.
+// That halves what an SM has to fetch per product: 128 x 256 tiles by single CTAs are bound by the traffic out of L2
+// (8192^3: 820 TFLOP/s).
+template <int BN, bool SWAP, bool PAIR>
 __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                                                                const __grid_constant__ GemmArgs A) {
   extern __shared__ __align__(1024) unsigned char raw[];
   __shared__ uint64_t full[kMaxStages], empty[kMaxStages], done[2], freed[2];
   __shared__ unsigned tmem_base;
-  constexpr unsigned kStageA = kBM * 128, kStage = kStageA + BN * 128;
+  constexpr int kHalf = PAIR ? BN / 2 : BN;                         // rows of B that this CTA loads
+  constexpr int kRows = PAIR ? 2 * kBM : kBM;                       // rows of a tile
+  constexpr unsigned kStageA = kBM * 128, kStage = kStageA + kHalf * 128;
   constexpr int kChunks = BN / 32;
   constexpr unsigned kCols = 2 * BN < 32 ? 32 : 2 * BN;
   unsigned char* sm = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
   uint4* staging = reinterpret_cast<uint4*>(sm + (size_t)A.stages * kStage);                     // 2 KB per epilogue warp
   float* sums = reinterpret_cast<float*>(sm + (size_t)A.stages * kStage + (SWAP ? 0 : kEpiWarps * 2048));   // the cluster's partial sums
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rank = A.split > 1 ? blockIdx.x % A.split : 0;
-  const int tiles = A.tilesA * A.tilesB, first = blockIdx.x / A.split, step = gridDim.x / A.split;
-  const int kb0 = (int)((int64_t)A.kblocks * rank / A.split), kb1 = (int)((int64_t)A.kblocks * (rank + 1) / A.split);
+  const int split = PAIR ? 1 : A.split, side = PAIR ? blockIdx.x & 1 : 0;
+  const int rank = split > 1 ? blockIdx.x % split : 0;
+  const int per = PAIR ? 2 : split;
+  const int tiles = A.tilesA * A.tilesB, first = blockIdx.x / per, step = gridDim.x / per;
+  const int kb0 = (int)((int64_t)A.kblocks * rank / split), kb1 = (int)((int64_t)A.kblocks * (rank + 1) / split);
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < A.stages; ++s) { bar_init(smem_addr(&full[s]), 1); bar_init(smem_addr(&empty[s]), 1); }
-    for (int i = 0; i < 2; ++i) { bar_init(smem_addr(&done[i]), 1); bar_init(smem_addr(&freed[i]), kEpiWarps); }
+    for (int i = 0; i < 2; ++i) { bar_init(smem_addr(&done[i]), 1); bar_init(smem_addr(&freed[i]), PAIR ? 2 * kEpiWarps : kEpiWarps); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base)), "r"(kCols) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    if constexpr (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base)), "r"(kCols) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_base)), "r"(kCols) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
   }
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
-  if (A.split > 1) cluster_sync();
+  if (PAIR || split > 1) cluster_sync();
   const unsigned tmem = tmem_base;
   bool ok = true;
 
@@ -292,7 +330,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   };
 
   if (warp == 0) {
-    if (lane == 0) {
+    if (elect()) {
       int s = 0, issued = 0;
       unsigned ph = 0;
       for (int t = first; t < tiles && ok; t += step) {
@@ -301,31 +339,38 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
         for (int kb = kb0; kb < kb1; ++kb) {
           ok = bar_wait(smem_addr(&empty[s]), ph ^ 1);
           if (!ok) break;
-          const unsigned bar = smem_addr(&full[s]), dst = smem_addr(sm) + s * kStage;
-          bar_expect(bar, kStage);
+          const unsigned dst = smem_addr(sm) + s * kStage;
+          unsigned bar = smem_addr(&full[s]);
+          if (side == 0) bar_expect(bar, PAIR ? 2 * kStage : kStage);
+          if (PAIR) bar = in_cta(bar, 0);
+          auto load = [&](unsigned to, const CUtensorMap* map, int c0, int c1) {
+            if constexpr (PAIR) tma_load_pair(to, map, c0, c1, bar);
+            else tma_load(to, map, c0, c1, bar);
+          };
+          const int ra = ta * kRows + side * kBM, rb = tb * BN + side * kHalf;
           if (A.mnA) {
-            for (int i = 0; i < kBM / 64; ++i) tma_load(dst + i * kBK * 128, &mapA, ta * kBM + i * 64, kb * kBK, bar);
+            for (int i = 0; i < kBM / 64; ++i) load(dst + i * kBK * 128, &mapA, ra + i * 64, kb * kBK);
           } else {
-            tma_load(dst, &mapA, kb * kBK, ta * kBM, bar);
+            load(dst, &mapA, kb * kBK, ra);
           }
           if (A.mnB) {
-            for (int i = 0; i < BN / 64; ++i) tma_load(dst + kStageA + i * kBK * 128, &mapB, tb * BN + i * 64, kb * kBK, bar);
+            for (int i = 0; i < kHalf / 64; ++i) load(dst + kStageA + i * kBK * 128, &mapB, rb + i * 64, kb * kBK);
           } else {
-            tma_load(dst + kStageA, &mapB, kb * kBK, tb * BN, bar);
+            load(dst + kStageA, &mapB, kb * kBK, rb);
           }
           ++issued;
           if (++s == A.stages) { s = 0; ph ^= 1; }
         }
       }
-      // the last copies land before the CTA ends, whoever waits for them
-      for (int i = 0; i < A.stages && i < issued; ++i) {
+      // the last copies land before the CTA ends, whoever waits for them (a pair's second CTA stays until the first has seen them)
+      for (int i = 0; i < A.stages && i < issued && side == 0; ++i) {
         if (--s < 0) { s = A.stages - 1; ph ^= 1; }
         bar_wait(smem_addr(&full[s]), ph);
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      const unsigned idesc = 1u << 4 | 1u << 7 | 1u << 10 | (unsigned)A.mnA << 15 | (unsigned)A.mnB << 16 | (unsigned)(BN >> 3) << 17 | (unsigned)(kBM >> 4) << 24;
+    if (side == 0 && elect()) {
+      const unsigned idesc = 1u << 4 | 1u << 7 | 1u << 10 | (unsigned)A.mnA << 15 | (unsigned)A.mnB << 16 | (unsigned)(BN >> 3) << 17 | (unsigned)(kRows >> 4) << 24;
       const unsigned stepA = A.mnA ? 2048 >> 4 : 32 >> 4, stepB = A.mnB ? 2048 >> 4 : 32 >> 4;
       int s = 0;
       unsigned ph = 0, buf = 0, aph = 0;
@@ -340,11 +385,16 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
           const unsigned base = smem_addr(sm) + s * kStage;
           const uint64_t da = descriptor(base, A.mnA), db = descriptor(base + kStageA, A.mnB);
 #pragma unroll
-          for (int k = 0; k < kBK / 16; ++k) mma(tmem + buf * BN, da + k * stepA, db + k * stepB, idesc, kb > kb0 || k > 0);
-          mma_commit(smem_addr(&empty[s]));
+          for (int k = 0; k < kBK / 16; ++k) {
+            if constexpr (PAIR) mma_pair(tmem + buf * BN, da + k * stepA, db + k * stepB, idesc, kb > kb0 || k > 0);
+            else mma(tmem + buf * BN, da + k * stepA, db + k * stepB, idesc, kb > kb0 || k > 0);
+          }
+          if constexpr (PAIR) mma_commit_pair(smem_addr(&empty[s]));
+          else mma_commit(smem_addr(&empty[s]));
           if (++s == A.stages) { s = 0; ph ^= 1; }
         }
-        mma_commit(smem_addr(&done[buf]));
+        if constexpr (PAIR) mma_commit_pair(smem_addr(&done[buf]));
+        else mma_commit(smem_addr(&done[buf]));
         if (buf) aph ^= 1;
         buf ^= 1;
       }
@@ -360,19 +410,17 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       tmem_fence_after();
-      const int r0 = ta * kBM + quarter * 32;
+      const int r0 = ta * kRows + side * kBM + quarter * 32;
       for (int c = half; c < kChunks; c += 2) {
         const int c0 = tb * BN + c * 32;
         if (c0 >= A.rowsB) break;
         float v[32];
         tmem_load32(tmem + buf * BN + c * 32 + ((unsigned)(quarter * 32) << 16), v);
-        if (A.split > 1) {
+        if (split > 1) {
           // chunk c is completed by CTA c mod split of the cluster; the others send it theirs
-          const int owner = c % A.split;
+          const int owner = c % split;
           if (owner != rank) {
-            unsigned to;
-            float* slot = sums + ((size_t)(c / A.split) * A.split + rank) * (32 * kBM) + quarter * 32 + lane;
-            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_addr(slot)), "r"(owner));
+            const unsigned to = in_cta(smem_addr(sums + ((size_t)(c / split) * split + rank) * (32 * kBM) + quarter * 32 + lane), owner);
 #pragma unroll
             for (int i = 0; i < 32; ++i) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + i * kBM * 4), "f"(v[i]) : "memory");
           }
@@ -382,16 +430,19 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
           finish(A, v, stage, r0, c0, lane);
         }
       }
-      if (A.split > 1) break;                                       // one tile per cluster; finished below
+      if (split > 1) break;                                       // one tile per cluster; finished below
       tmem_fence_before();
       __syncwarp();
-      if (lane == 0) bar_arrive(smem_addr(&freed[buf]));
+      if (lane == 0) {
+        if (PAIR) bar_arrive_cluster(in_cta(smem_addr(&freed[buf]), 0));
+        else bar_arrive(smem_addr(&freed[buf]));
+      }
       if (buf) aph ^= 1;
       buf ^= 1;
     }
   }
   __syncwarp();
-  if (A.split > 1) {
+  if (split > 1) {
     cluster_sync();
     if (warp >= 2 && ok) {
       const int e = warp - 2, quarter = warp & 3, half = e >> 2;
@@ -401,12 +452,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       for (int c = half; c < kChunks; c += 2) {
         const int c0 = tb * BN + c * 32;
         if (c0 >= A.rowsB) break;
-        if (c % A.split != rank) continue;
+        if (c % split != rank) continue;
         float v[32];
         tmem_load32(tmem + c * 32 + ((unsigned)(quarter * 32) << 16), v);
-        for (int q = 0; q < A.split; ++q) {
+        for (int q = 0; q < split; ++q) {
           if (q == rank) continue;
-          const float* slot = sums + ((size_t)(c / A.split) * A.split + q) * (32 * kBM) + quarter * 32 + lane;
+          const float* slot = sums + ((size_t)(c / split) * split + q) * (32 * kBM) + quarter * 32 + lane;
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] += slot[i * kBM];
         }
@@ -415,11 +466,15 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       }
     }
   }
-  if (!ok && lane == 0) atomicAdd(&g_gave_up, 1u);
+  if (!ok && (warp < 2 || lane == 0)) atomicAdd(&g_gave_up, 1u);
   tmem_fence_before();
   __syncthreads();
+  if (PAIR) cluster_sync();        // neither leaves while the other's MMA, copies or arrivals may reach it
   tmem_fence_after();
-  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols));
+  if (warp == 1) {
+    if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols));
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols));
+  }
 }
 
 // ---------------------------------------------------------------------------------------------- elementwise parts
@@ -554,54 +609,59 @@ bool make_map(CUtensorMap* map, const Matrix& m, int mn, int box_rows) {
 
 struct Choice {
   int bn, split;
+  bool pair;
 };
 
-// Tile width and split. A stage of 64 k takes max(BN, 96) / 256 x 512 cycles or so, a tile's epilogue about as
-// long as eight stages of its width, of which all but the last are hidden; a split costs a cluster barrier.
+// Tile width, split and pairing. In cycles: a stage of 64 k takes a pair 2 BN per 256 rows (the tensor cores' rate), a single CTA about
+// twice that per 128 rows (fetching bounds it), and no less than 192 or so; the last tile's epilogue adds to it, a split costs a cluster barrier.
 Choice choose(int64_t rowsA, int64_t rowsB, int kblocks, bool swap) {
-  Choice best = {0, 1};
+  Choice best = {0, 1, false};
   float least = 0.f;
   const int widths[4] = {256, 128, 64, 32};
-  for (int w = 0; w < 4; ++w) {
-    const int bn = widths[w];
-    if (swap ? bn != (rowsB <= 32 ? 32 : 64) : bn == 32) continue;
-    const int64_t tiles = ((rowsA + kBM - 1) / kBM) * ((rowsB + bn - 1) / bn);
-    const int most = swap ? 8 : bn == 256 ? 1 : bn / 32;
-    for (int split = 1; split <= most; split *= 2) {
-      if (split > 1 && (tiles * split > 148 || kblocks / split < 2)) break;
-      const int64_t waves = (tiles * split + 147) / 148;
-      const float stage = bn >= 96 ? 2.f * bn : 192.f;
-      const float t = waves * ((kblocks + split - 1) / split) * stage + 8.f * bn + (split > 1 ? 1500.f : 0.f);
-      if (best.bn == 0 || t < least) { best.bn = bn; best.split = split; least = t; }
+  for (int pair = 0; pair < 2; ++pair)
+    for (int w = 0; w < 4; ++w) {
+      const int bn = widths[w], rows = pair ? 2 * kBM : kBM;
+      if (swap ? bn != (rowsB <= 32 ? 32 : 64) : bn == 32) continue;
+      if (pair && (swap || bn < 128)) continue;
+      const int64_t tiles = ((rowsA + rows - 1) / rows) * ((rowsB + bn - 1) / bn);
+      const int most = pair ? 1 : swap ? 8 : bn == 256 ? 1 : bn / 32;
+      for (int split = 1; split <= most; split *= 2) {
+        if (split > 1 && (tiles * split > 148 || kblocks / split < 2)) break;
+        const int64_t at_once = pair ? 74 : 148, waves = (tiles * split + at_once - 1) / at_once;
+        const float stage = pair ? 2.2f * bn : bn >= 96 ? 3.5f * bn : 280.f;
+        const float t = waves * ((kblocks + split - 1) / split) * stage + 8.f * bn + (split > 1 ? 1500.f : 0.f);
+        if (best.bn == 0 || t < least) { best.bn = bn; best.split = split; best.pair = pair != 0; least = t; }
+      }
     }
-  }
   return best;
 }
 
-template <int BN, bool SWAP>
+template <int BN, bool SWAP, bool PAIR>
 int launch_gemm(const Matrix& a, const Matrix& b, GemmArgs& A, int split, cudaStream_t st) {
+  constexpr int kHalf = PAIR ? BN / 2 : BN, kRows = PAIR ? 2 * kBM : kBM;
   CUtensorMap ma, mb;
-  if (!make_map(&ma, a, A.mnA, kBM) || !make_map(&mb, b, A.mnB, BN)) return DMX_ERR_CUDA;
-  A.tilesA = (A.rowsA + kBM - 1) / kBM;
+  if (!make_map(&ma, a, A.mnA, kBM) || !make_map(&mb, b, A.mnB, kHalf)) return DMX_ERR_CUDA;
+  A.tilesA = (A.rowsA + kRows - 1) / kRows;
   A.tilesB = (A.rowsB + BN - 1) / BN;
   A.split = split;
-  const int stage = kBM * 128 + BN * 128, chunks = BN / 32;
+  const int stage = (kBM + kHalf) * 128, chunks = BN / 32;
   const int extra = 1024 + (SWAP ? 0 : kEpiWarps * 2048) + (split > 1 ? (chunks + split - 1) / split * split * 32 * kBM * 4 : 0);
   A.stages = (kSmemMost - extra) / stage;
   if (A.stages > kMaxStages) A.stages = kMaxStages;
   const int smem = A.stages * stage + extra;
-  const auto kernel = gemm_kernel<BN, SWAP>;
+  const auto kernel = gemm_kernel<BN, SWAP, PAIR>;
   if (!dmxh::cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost))) return DMX_ERR_CUDA;
   const int64_t tiles = (int64_t)A.tilesA * A.tilesB;
-  if (tiles * split > 0x7fffffff) return DMX_ERR_ARG;
+  const int per = PAIR ? 2 : split;
+  if (tiles * per > 0x7fffffff) return DMX_ERR_ARG;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(split > 1 ? tiles * split : tiles < 148 ? tiles : 148));
+  cfg.gridDim = dim3((unsigned)(split > 1 || tiles * per < 148 ? tiles * per : 148));
   cfg.blockDim = dim3(kGemmThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute attr[1] = {};
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = split;
+  attr[0].val.clusterDim.x = per;
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
@@ -621,14 +681,15 @@ int product(const Matrix& a, int mnA, const Matrix& b, int mnB, int64_t k, const
     A.rowsA = (int)rowsB; A.rowsB = (int)rowsA;
     A.mnA = mnB; A.mnB = mnA;
     const Choice c = choose(rowsB, rowsA, A.kblocks, true);
-    return c.bn == 32 ? launch_gemm<32, true>(b, a, A, c.split, st) : launch_gemm<64, true>(b, a, A, c.split, st);
+    return c.bn == 32 ? launch_gemm<32, true, false>(b, a, A, c.split, st) : launch_gemm<64, true, false>(b, a, A, c.split, st);
   }
   A.rowsA = (int)rowsA; A.rowsB = (int)rowsB;
   A.mnA = mnA; A.mnB = mnB;
   const Choice c = choose(rowsA, rowsB, A.kblocks, false);
-  if (c.bn == 256) return launch_gemm<256, false>(a, b, A, c.split, st);
-  if (c.bn == 128) return launch_gemm<128, false>(a, b, A, c.split, st);
-  return launch_gemm<64, false>(a, b, A, c.split, st);
+  if (c.pair) return c.bn == 256 ? launch_gemm<256, false, true>(a, b, A, 1, st) : launch_gemm<128, false, true>(a, b, A, 1, st);
+  if (c.bn == 256) return launch_gemm<256, false, false>(a, b, A, c.split, st);
+  if (c.bn == 128) return launch_gemm<128, false, false>(a, b, A, c.split, st);
+  return launch_gemm<64, false, false>(a, b, A, c.split, st);
 }
 
 int slope(const Matrix& dy, const bf16* z, int64_t ldz, int act, bf16* out, int64_t ldo, float* sums, cudaStream_t st) {
