@@ -6,7 +6,7 @@
 //
 // All three products are D[i, j] = sum_k A[i, k] B[j, k] on the 5th-generation tensor cores, by one kernel: a
 // producer warp moves tiles of A (128 rows) and B (32 to 256) of 64 k with TMA into a ring of shared memory
-// stages, one thread issues tcgen05.mma on them into accumulators in TMEM, and eight warps take finished accumulators out
+// stages, one thread issues tcgen05.mma on them into accumulators in TMEM, and sixteen warps take finished accumulators out
 // (tcgen05.ld), apply the epilogue and store, while the next tile accumulates in the other half of TMEM. An
 // operand whose rows run along k is K-major; W in dx, and both operands of dW, run across it (MN-major) and are
 // multiplied as they lie: only the descriptors differ, nothing is transposed in memory.
@@ -31,7 +31,7 @@ using namespace dmx_f32x2;
 typedef __nv_bfloat16 bf16;
 
 constexpr int kBM = 128, kBK = 64;            // tile rows of A; k per stage (128 bytes: one swizzle row)
-constexpr int kEpiWarps = 8;
+constexpr int kEpiWarps = 16;                 // four per scheduler: with two a GELU epilogue took longer than 1024 k
 constexpr int kGemmThreads = 64 + 32 * kEpiWarps;
 constexpr int kMaxStages = 8;
 constexpr int kSmemMost = 226 * 1024;
@@ -69,12 +69,13 @@ __device__ __forceinline__ void bar_expect(unsigned bar, unsigned bytes) {
 __device__ __forceinline__ bool bar_wait(unsigned bar, unsigned parity) {
   for (unsigned n = 0; n < kPolls; ++n) {
     unsigned done;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                  : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     if (done) return true;
   }
   return false;
 }
+__device__ __forceinline__ bool warp_wait(unsigned bar, unsigned parity) { return __all_sync(0xffffffffu, bar_wait(bar, parity)); }
 __device__ __forceinline__ void tma_load(unsigned dst, const CUtensorMap* map, int c0, int c1, unsigned bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(bar) : "memory");
@@ -129,6 +130,11 @@ __device__ __forceinline__ uint64_t descriptor(unsigned addr, int mn) {
   const uint64_t lead = mn ? (kBK * 128) >> 4 : 1, stride = 1024 >> 4;
   return (uint64_t)((addr >> 4) & 0x3fff) | lead << 16 | stride << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
+
+// Launched as programmatic dependents: what needs no data is set up while the kernel before still runs; then all of its
+// (and earlier) writes are waited for. The kernel after may begin likewise.
+__device__ __forceinline__ void start_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 __device__ __forceinline__ float bf_value(unsigned short u) { return __uint_as_float((unsigned)u << 16); }
 __device__ __forceinline__ unsigned pack2(float a, float b) {
@@ -301,7 +307,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   const int tiles = A.tilesA * A.tilesB, first = blockIdx.x / per, step = gridDim.x / per;
   const int kb0 = (int)((int64_t)A.kblocks * rank / split), kb1 = (int)((int64_t)A.kblocks * (rank + 1) / split);
 
+  start_dependents();
   if (threadIdx.x == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&mapA) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&mapB) : "memory");
     for (int s = 0; s < A.stages; ++s) { bar_init(smem_addr(&full[s]), 1); bar_init(smem_addr(&empty[s]), 1); }
     for (int i = 0; i < 2; ++i) { bar_init(smem_addr(&done[i]), 1); bar_init(smem_addr(&freed[i]), PAIR ? 2 * kEpiWarps : kEpiWarps); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -319,6 +328,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   __syncthreads();
   tmem_fence_after();
   if (PAIR || split > 1) cluster_sync();
+  wait_for_previous();
   const unsigned tmem = tmem_base;
   bool ok = true;
 
@@ -330,20 +340,22 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   };
 
   if (warp == 0) {
-    if (elect()) {
+    const bool issuer = elect();     // the warp stays together; one lane issues
+    {
       int s = 0, issued = 0;
       unsigned ph = 0;
       for (int t = first; t < tiles && ok; t += step) {
         int ta, tb;
         tile_at(t, ta, tb);
         for (int kb = kb0; kb < kb1; ++kb) {
-          ok = bar_wait(smem_addr(&empty[s]), ph ^ 1);
+          ok = warp_wait(smem_addr(&empty[s]), ph ^ 1);
           if (!ok) break;
           const unsigned dst = smem_addr(sm) + s * kStage;
           unsigned bar = smem_addr(&full[s]);
-          if (side == 0) bar_expect(bar, PAIR ? 2 * kStage : kStage);
+          if (issuer && side == 0) bar_expect(bar, PAIR ? 2 * kStage : kStage);
           if (PAIR) bar = in_cta(bar, 0);
           auto load = [&](unsigned to, const CUtensorMap* map, int c0, int c1) {
+            if (!issuer) return;
             if constexpr (PAIR) tma_load_pair(to, map, c0, c1, bar);
             else tma_load(to, map, c0, c1, bar);
           };
@@ -358,6 +370,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
           } else {
             load(dst + kStageA, &mapB, kb * kBK, rb);
           }
+          __syncwarp();
           ++issued;
           if (++s == A.stages) { s = 0; ph ^= 1; }
         }
@@ -369,49 +382,55 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       }
     }
   } else if (warp == 1) {
-    if (side == 0 && elect()) {
+    if (side == 0) {
+      const bool issuer = elect();
       const unsigned idesc = 1u << 4 | 1u << 7 | 1u << 10 | (unsigned)A.mnA << 15 | (unsigned)A.mnB << 16 | (unsigned)(BN >> 3) << 17 | (unsigned)(kRows >> 4) << 24;
       const unsigned stepA = A.mnA ? 2048 >> 4 : 32 >> 4, stepB = A.mnB ? 2048 >> 4 : 32 >> 4;
       int s = 0;
       unsigned ph = 0, buf = 0, aph = 0;
       for (int t = first; t < tiles && ok; t += step) {
-        ok = bar_wait(smem_addr(&freed[buf]), aph ^ 1);
+        ok = warp_wait(smem_addr(&freed[buf]), aph ^ 1);
         if (!ok) break;
         tmem_fence_after();
         for (int kb = kb0; kb < kb1; ++kb) {
-          ok = bar_wait(smem_addr(&full[s]), ph);
+          ok = warp_wait(smem_addr(&full[s]), ph);
           if (!ok) break;
           tmem_fence_after();
           const unsigned base = smem_addr(sm) + s * kStage;
           const uint64_t da = descriptor(base, A.mnA), db = descriptor(base + kStageA, A.mnB);
+          if (issuer) {
 #pragma unroll
-          for (int k = 0; k < kBK / 16; ++k) {
-            if constexpr (PAIR) mma_pair(tmem + buf * BN, da + k * stepA, db + k * stepB, idesc, kb > kb0 || k > 0);
-            else mma(tmem + buf * BN, da + k * stepA, db + k * stepB, idesc, kb > kb0 || k > 0);
+            for (int k = 0; k < kBK / 16; ++k) {
+              if constexpr (PAIR) mma_pair(tmem + buf * BN, da + k * stepA, db + k * stepB, idesc, kb > kb0 || k > 0);
+              else mma(tmem + buf * BN, da + k * stepA, db + k * stepB, idesc, kb > kb0 || k > 0);
+            }
+            if constexpr (PAIR) mma_commit_pair(smem_addr(&empty[s]));
+            else mma_commit(smem_addr(&empty[s]));
           }
-          if constexpr (PAIR) mma_commit_pair(smem_addr(&empty[s]));
-          else mma_commit(smem_addr(&empty[s]));
+          __syncwarp();
           if (++s == A.stages) { s = 0; ph ^= 1; }
         }
-        if constexpr (PAIR) mma_commit_pair(smem_addr(&done[buf]));
-        else mma_commit(smem_addr(&done[buf]));
+        if (issuer) {
+          if constexpr (PAIR) mma_commit_pair(smem_addr(&done[buf]));
+          else mma_commit(smem_addr(&done[buf]));
+        }
+        __syncwarp();
         if (buf) aph ^= 1;
         buf ^= 1;
       }
     }
   } else {
-    const int e = warp - 2, quarter = warp & 3, half = e >> 2;      // TMEM lanes 32 quarter.. belong to warps of that number mod 4
+    const int e = warp - 2, quarter = warp & 3, group = e >> 2;      // TMEM lanes 32 quarter.. belong to warps of that number mod 4
     uint4* stage = staging + e * 128;
     unsigned buf = 0, aph = 0;
     for (int t = first; t < tiles && ok; t += step) {
       int ta, tb;
       tile_at(t, ta, tb);
-      ok = bar_wait(smem_addr(&done[buf]), aph);
-      ok = __all_sync(0xffffffffu, ok);
+      ok = warp_wait(smem_addr(&done[buf]), aph);
       if (!ok) break;
       tmem_fence_after();
       const int r0 = ta * kRows + side * kBM + quarter * 32;
-      for (int c = half; c < kChunks; c += 2) {
+      for (int c = group; c < kChunks; c += kEpiWarps / 4) {
         const int c0 = tb * BN + c * 32;
         if (c0 >= A.rowsB) break;
         float v[32];
@@ -445,11 +464,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   if (split > 1) {
     cluster_sync();
     if (warp >= 2 && ok) {
-      const int e = warp - 2, quarter = warp & 3, half = e >> 2;
+      const int e = warp - 2, quarter = warp & 3, group = e >> 2;
       int ta, tb;
       tile_at(first, ta, tb);
       tmem_fence_after();
-      for (int c = half; c < kChunks; c += 2) {
+      for (int c = group; c < kChunks; c += kEpiWarps / 4) {
         const int c0 = tb * BN + c * 32;
         if (c0 >= A.rowsB) break;
         if (c % split != rank) continue;
@@ -466,7 +485,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       }
     }
   }
-  if (!ok && (warp < 2 || lane == 0)) atomicAdd(&g_gave_up, 1u);
+  if (!ok && lane == 0) atomicAdd(&g_gave_up, 1u);
   tmem_fence_before();
   __syncthreads();
   if (PAIR) cluster_sync();        // neither leaves while the other's MMA, copies or arrivals may reach it
@@ -487,6 +506,8 @@ template <int V>
 __global__ void __launch_bounds__(256) slope_kernel(const bf16* __restrict__ dy, int64_t lddy, const bf16* __restrict__ z, int64_t ldz, int act,
                                                     int64_t rows, int cols, bf16* __restrict__ out, int64_t ldo, float* __restrict__ sums) {
   __shared__ float sh[8][32 * V];
+  start_dependents();
+  wait_for_previous();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int c = (blockIdx.x * 32 + lane) * V;
   float acc[V];
@@ -538,6 +559,8 @@ __global__ void __launch_bounds__(256) slope_kernel(const bf16* __restrict__ dy,
 // dbias from the chunks' sums: 32 columns and eight lanes of chunks per CTA
 __global__ void __launch_bounds__(256) columns_kernel(const float* __restrict__ sums, int64_t chunks, int cols, bf16* __restrict__ out) {
   __shared__ float sh[8][33];
+  start_dependents();
+  wait_for_previous();
   const int lane = threadIdx.x & 31, r = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   float s = 0.f;
   if (c < cols) {
@@ -554,6 +577,8 @@ __global__ void __launch_bounds__(256) columns_kernel(const float* __restrict__ 
 
 // K = 0: y = act(bias) + residual
 __global__ void __launch_bounds__(256) bias_kernel(const __grid_constant__ GemmArgs A) {
+  start_dependents();
+  wait_for_previous();
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)A.rowsA * A.rowsB; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / A.rowsB;
     const int c = (int)(i - r * A.rowsB);
@@ -607,32 +632,51 @@ bool make_map(CUtensorMap* map, const Matrix& m, int mn, int box_rows) {
            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+template <typename... P, typename... V>
+int start(cudaLaunchConfig_t cfg, int cluster, void (*kernel)(P...), V... args) {
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return dmxh::cuda_ok(cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...)) ? DMX_OK : DMX_ERR_CUDA;
+}
+template <typename... P, typename... V>
+int start(dim3 grid, cudaStream_t st, void (*kernel)(P...), V... args) {      // 256 threads
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(256);
+  cfg.stream = st;
+  return start(cfg, 1, kernel, args...);
+}
+
 struct Choice {
   int bn, split;
   bool pair;
 };
 
-// Tile width, split and pairing. In cycles: a stage of 64 k takes a pair 2 BN per 256 rows (the tensor cores' rate), a single CTA about
-// twice that per 128 rows (fetching bounds it), and no less than 192 or so; the last tile's epilogue adds to it, a split costs a cluster barrier.
+// Tile width, split and pairing, by the time they take: what a stage of 64 k took measured on 8192^3 (ns; the narrow tiles are bound
+// by what the SMs fetch from L2), the last tile's epilogue, a split's cluster barrier and exchange.
 Choice choose(int64_t rowsA, int64_t rowsB, int kblocks, bool swap) {
   Choice best = {0, 1, false};
   float least = 0.f;
-  const int widths[4] = {256, 128, 64, 32};
-  for (int pair = 0; pair < 2; ++pair)
-    for (int w = 0; w < 4; ++w) {
-      const int bn = widths[w], rows = pair ? 2 * kBM : kBM;
-      if (swap ? bn != (rowsB <= 32 ? 32 : 64) : bn == 32) continue;
-      if (pair && (swap || bn < 128)) continue;
-      const int64_t tiles = ((rowsA + rows - 1) / rows) * ((rowsB + bn - 1) / bn);
-      const int most = pair ? 1 : swap ? 8 : bn == 256 ? 1 : bn / 32;
-      for (int split = 1; split <= most; split *= 2) {
-        if (split > 1 && (tiles * split > 148 || kblocks / split < 2)) break;
-        const int64_t at_once = pair ? 74 : 148, waves = (tiles * split + at_once - 1) / at_once;
-        const float stage = pair ? 2.2f * bn : bn >= 96 ? 3.5f * bn : 280.f;
-        const float t = waves * ((kblocks + split - 1) / split) * stage + 8.f * bn + (split > 1 ? 1500.f : 0.f);
-        if (best.bn == 0 || t < least) { best.bn = bn; best.split = split; best.pair = pair != 0; least = t; }
-      }
+  const struct { int bn; bool pair; float stage; } forms[6] = {{256, true, 405.f}, {256, false, 435.f}, {128, true, 290.f},
+                                                                {128, false, 290.f}, {64, false, 245.f}, {32, false, 200.f}};
+  for (const auto& f : forms) {
+    if (swap ? f.pair || f.bn != (rowsB <= 32 ? 32 : 64) : f.bn == 32) continue;
+    const int rows = f.pair ? 2 * kBM : kBM, at_once = f.pair ? 74 : 148;
+    const int64_t tiles = ((rowsA + rows - 1) / rows) * ((rowsB + f.bn - 1) / f.bn);
+    const int most = f.pair ? 1 : swap ? 4 : f.bn == 256 ? 1 : f.bn / 32;
+    for (int split = 1; split <= most; split *= 2) {
+      if (split > 1 && (tiles * split > 148 || kblocks / split < 2)) break;
+      const int64_t waves = (tiles * split + at_once - 1) / at_once;
+      const float t = waves * ((kblocks + split - 1) / split) * f.stage + 8.f * f.bn + (split > 1 ? 1500.f : 0.f);
+      if (best.bn == 0 || t < least) { best.bn = f.bn; best.split = split; best.pair = f.pair; least = t; }
     }
+  }
   return best;
 }
 
@@ -659,13 +703,7 @@ int launch_gemm(const Matrix& a, const Matrix& b, GemmArgs& A, int split, cudaSt
   cfg.blockDim = dim3(kGemmThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1] = {};
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = per;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return dmxh::cuda_ok(cudaLaunchKernelEx(&cfg, kernel, ma, mb, A)) ? DMX_OK : DMX_ERR_CUDA;
+  return start(cfg, per, kernel, ma, mb, A);
 }
 
 // D = A B^T with the epilogue in E (bias, residual, outputs, act). mn: the operand's rows run along D's extent.
@@ -699,9 +737,7 @@ int slope(const Matrix& dy, const bf16* z, int64_t ldz, int act, bf16* out, int6
   const int V = vec ? 8 : 1;
   if (chunks > 65535) return DMX_ERR_ARG;
   const dim3 grid((unsigned)((dy.cols + 32 * V - 1) / (32 * V)), (unsigned)chunks);
-  if (vec) slope_kernel<8><<<grid, 256, 0, st>>>(dy.p, dy.ld, z, ldz, act, dy.rows, (int)dy.cols, out, ldo, sums);
-  else slope_kernel<1><<<grid, 256, 0, st>>>(dy.p, dy.ld, z, ldz, act, dy.rows, (int)dy.cols, out, ldo, sums);
-  return dmxh::cuda_ok(cudaGetLastError()) ? DMX_OK : DMX_ERR_CUDA;
+  return start(grid, st, vec ? slope_kernel<8> : slope_kernel<1>, dy.p, dy.ld, z, ldz, act, dy.rows, (int)dy.cols, out, ldo, sums);
 }
 
 // m itself, or its copy at *ws (which moves on)
@@ -765,8 +801,7 @@ int dmx_linear_forward(int64_t M, int64_t N, int64_t K, const void* x, int64_t l
   if (K == 0) {
     E.rowsA = (int)M; E.rowsB = (int)N;
     const int64_t want = (M * N + 255) / 256;
-    bias_kernel<<<(unsigned)(want < 148 * 8 ? want : 148 * 8), 256, 0, st>>>(E);
-    return dmxh::cuda_ok(cudaGetLastError()) ? DMX_OK : DMX_ERR_CUDA;
+    return start(dim3((unsigned)(want < 148 * 8 ? want : 148 * 8)), st, bias_kernel, E);
   }
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   Matrix a = {static_cast<const bf16*>(x), M, K, M > 1 ? ldx : K}, b = {static_cast<const bf16*>(w), N, K, N > 1 ? ldw : K};
@@ -810,8 +845,8 @@ int dmx_linear_backward(int64_t M, int64_t N, int64_t K, const void* dy, int64_t
     if (rc != DMX_OK) return rc;
     if (out) { g.p = out; g.ld = pad8(N); }
     if (dbias) {
-      columns_kernel<<<(unsigned)((N + 31) / 32), 256, 0, st>>>(sums, (M + kChunkRows - 1) / kChunkRows, (int)N, static_cast<bf16*>(dbias));
-      if (!dmxh::cuda_ok(cudaGetLastError())) return DMX_ERR_CUDA;
+      rc = start(dim3((unsigned)((N + 31) / 32)), st, columns_kernel, (const float*)sums, (M + kChunkRows - 1) / kChunkRows, (int)N, static_cast<bf16*>(dbias));
+      if (rc != DMX_OK) return rc;
     }
   }
   ws += p.dz;
