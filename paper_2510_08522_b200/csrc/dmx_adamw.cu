@@ -380,7 +380,8 @@ __device__ __forceinline__ void run(const StepArgs& A, const Place<P, G, BITS>& 
 
 template <typename P, typename G, int BITS, bool DITHER>
 __global__ void __launch_bounds__(kStepThreads<BITS>, kStepCtas<BITS>) adamw_kernel(const __grid_constant__ StepArgs A) {
-  const float s = A.grad_scale ? __ldg(A.grad_scale) : 1.f;
+  asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
+  const float s = A.grad_scale ? __ldcg(A.grad_scale) : 1.f;
   if (s != s) return;                       // the factor says: skip this step
   const Chunk c = A.chunks[blockIdx.x];
   const Tensor T = A.tensors[c.tensor];
@@ -440,6 +441,7 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const Tensor* __restrict
                                                         unsigned* __restrict__ ticket, float* __restrict__ out) {
   __shared__ double sh[kWarps];
   __shared__ bool last;
+  asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
   const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
   double sum = 0.0;
   for (int ci = blockIdx.x; ci < nchunks; ci += gridDim.x) {
@@ -512,11 +514,27 @@ void release(dmx_adamw* h) {
   delete h;
 }
 
+// As programmatic dependents: a step behind its gradient norm is resident when that ends (the kernels' first act is to
+// wait for it; 1 Mi parameters: 2 us less for the two).
+template <typename... K, typename... V>
+int start(int grid, int threads, cudaStream_t st, void (*kernel)(K...), V... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return dmxh::cuda_ok(cudaLaunchKernelEx(&cfg, kernel, static_cast<K>(args)...)) ? DMX_OK : DMX_ERR_CUDA;
+}
+
 template <typename P, typename G>
-void launch_step(const dmx_adamw* h, const StepArgs& A, bool dither, cudaStream_t st) {
-  if (h->bits == 32) adamw_kernel<P, G, 32, false><<<h->nchunks, kStepThreads<32>, 0, st>>>(A);
-  else if (dither) adamw_kernel<P, G, 8, true><<<h->nchunks, kStepThreads<8>, 0, st>>>(A);
-  else adamw_kernel<P, G, 8, false><<<h->nchunks, kStepThreads<8>, 0, st>>>(A);
+int launch_step(const dmx_adamw* h, const StepArgs& A, bool dither, cudaStream_t st) {
+  if (h->bits == 32) return start(h->nchunks, kStepThreads<32>, st, adamw_kernel<P, G, 32, false>, A);
+  if (dither) return start(h->nchunks, kStepThreads<8>, st, adamw_kernel<P, G, 8, true>, A);
+  return start(h->nchunks, kStepThreads<8>, st, adamw_kernel<P, G, 8, false>, A);
 }
 
 bool aligned(const void* p, unsigned a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -641,11 +659,8 @@ int dmx_adamw_grad_norm(dmx_adamw* h, float max_norm, float* out, void* cuda_str
   const int rc = dmxh::check_current_device(h->device);
   if (rc != DMX_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (h->grad_dtype == DMX_F32)
-    norm_kernel<float><<<h->norm_grid, kThreads, 0, st>>>(h->tensors, h->chunks, h->nchunks, max_norm, h->part, h->ticket, out);
-  else
-    norm_kernel<__nv_bfloat16><<<h->norm_grid, kThreads, 0, st>>>(h->tensors, h->chunks, h->nchunks, max_norm, h->part, h->ticket, out);
-  return dmxh::cuda_ok(cudaGetLastError()) ? DMX_OK : DMX_ERR_CUDA;
+  return start(h->norm_grid, kThreads, st, h->grad_dtype == DMX_F32 ? norm_kernel<float> : norm_kernel<__nv_bfloat16>, (const Tensor*)h->tensors,
+               (const Chunk*)h->chunks, h->nchunks, max_norm, h->part, h->ticket, out);
 }
 
 int dmx_adamw_step(dmx_adamw* h, void* m, void* v, float* m_scale, float* v_scale, const float* grad_scale, double lr,
@@ -673,11 +688,10 @@ int dmx_adamw_step(dmx_adamw* h, void* m, void* v, float* m_scale, float* v_scal
   A.key = seed * 0x85ebca6bu + 0x1b873593u;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const bool pf = h->param_dtype == DMX_F32, gf = h->grad_dtype == DMX_F32;
-  if (pf && gf) launch_step<float, float>(h, A, dither != 0, st);
-  else if (pf) launch_step<float, __nv_bfloat16>(h, A, dither != 0, st);
-  else if (gf) launch_step<__nv_bfloat16, float>(h, A, dither != 0, st);
-  else launch_step<__nv_bfloat16, __nv_bfloat16>(h, A, dither != 0, st);
-  return dmxh::cuda_ok(cudaGetLastError()) ? DMX_OK : DMX_ERR_CUDA;
+  if (pf && gf) return launch_step<float, float>(h, A, dither != 0, st);
+  if (pf) return launch_step<float, __nv_bfloat16>(h, A, dither != 0, st);
+  return gf ? launch_step<__nv_bfloat16, float>(h, A, dither != 0, st)
+            : launch_step<__nv_bfloat16, __nv_bfloat16>(h, A, dither != 0, st);
 }
 
 int dmx_adamw_moments(dmx_adamw* h, const void* m, const void* v, const float* m_scale, const float* v_scale, int out_dtype,

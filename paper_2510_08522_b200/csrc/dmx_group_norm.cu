@@ -309,6 +309,7 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) forward_k
   const int64_t first = M == RESIDENT ? blockIdx.x / (unsigned)A.parts : blockIdx.x;
   const int64_t stride = M == RESIDENT ? gridDim.x / (unsigned)A.parts : gridDim.x;
   if (first >= A.items) return;                    // the whole cluster
+  asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
   Here h = place<V, M>(A, first, rl, col);
   {
     const T* p = start<T, V>(A.x, h, rl, col);
@@ -553,7 +554,6 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) backward_
   float* grp = got + 4 * gparts * pW;
   float* par = grp + 2 * pG;
   int turn = 0;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const Lanes Q = lanes(gparts, cpg, 2 * pW);
   int grp0 = 0, rem0 = 0;
   if (rl < R) { grp0 = col * V / cpg; rem0 = col * V - grp0 * cpg; }
@@ -562,6 +562,7 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) backward_
   const int64_t first = M == RESIDENT ? blockIdx.x / (unsigned)A.parts : blockIdx.x;
   const int64_t stride = M == RESIDENT ? gridDim.x / (unsigned)A.parts : gridDim.x;
   if (first >= A.items) return;
+  asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
   Here h = place<V, M>(A, first, rl, col);
   {
     const T *p = start<T, V>(A.x, h, rl, col), *g = start<T, V>(A.dy, h, rl, col);
@@ -846,13 +847,15 @@ int launch(K kernel, const Plan& p, const Args& A, bool cluster, cudaStream_t st
   cfg.blockDim = dim3(p.threads);
   cfg.dynamicSmemBytes = p.smem;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1] = {};
-  attr[0].id = cudaLaunchAttributeClusterDimension;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
   const int per = cluster ? p.parts : 1;
-  attr[0].val.clusterDim.x = per;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].val.clusterDim.x = per;
+  attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = per > 1 ? 2 : 1;
   // as many clusters as run at once; each takes item after item
   int64_t clusters = A.items;
   if (clusters * per > 148) {

@@ -21,6 +21,7 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+#include <atomic>
 
 #include "dmx_act.cuh"
 #include "dmx_host.h"
@@ -169,6 +170,7 @@ __device__ __forceinline__ void store_chunk(bf16* p, int64_t ld, int vec, uint4*
     }
   } else if (c0 + lane < cols) {
     const int n = min(32, rows - r0);
+#pragma unroll 8
     for (int r = 0; r < n; ++r)
       reinterpret_cast<unsigned short*>(p)[(int64_t)(r0 + r) * ld + c0 + lane] = reinterpret_cast<const unsigned short*>(unit(stage, r, lane >> 3))[lane & 7];
   }
@@ -192,6 +194,7 @@ __device__ __forceinline__ void load_chunk(const bf16* p, int64_t ld, int vec, u
     }
   } else if (c0 + lane < cols) {
     const int n = min(32, rows - r0);
+#pragma unroll 8
     for (int r = 0; r < n; ++r)
       reinterpret_cast<unsigned short*>(unit(stage, r, lane >> 3))[lane & 7] = reinterpret_cast<const unsigned short*>(p)[(int64_t)(r0 + r) * ld + c0 + lane];
   }
@@ -498,61 +501,97 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
 
 // ---------------------------------------------------------------------------------------------- elementwise parts
 
-// dz = dy act'(z) as bf16 rows of `ldo` elements (out may be NULL: then only the sums), and per chunk of rows the
-// column sums of the unrounded dz. V columns per lane; with V = 1 any alignment. Also lays out an operand (act
-// none, sums NULL).
+// Row-wise jobs, up to three to a launch (blockIdx.z): dz = dy act'(z) as bf16 rows of `ldo` elements with, per chunk of
+// rows, the column sums of the unrounded dz; and the laying out of an operand whose rows TMA cannot take. Bound: HBM (dz
+// reads two matrices and writes one: 8192 x 4096, 201 MB).
 constexpr int kChunkRows = 64;
-template <int V>
-__global__ void __launch_bounds__(256) slope_kernel(const bf16* __restrict__ dy, int64_t lddy, const bf16* __restrict__ z, int64_t ldz, int act,
-                                                    int64_t rows, int cols, bf16* __restrict__ out, int64_t ldo, float* __restrict__ sums) {
-  __shared__ float sh[8][32 * V];
-  start_dependents();
-  wait_for_previous();
+struct Job {
+  const bf16 *in, *z;       // dy (or the operand), and z if the slope is taken
+  bf16* out;                // or NULL
+  float* sums;              // or NULL
+  int64_t ldi, ldz, ldo, rows;
+  int cols, vec;            // vec: 16-byte accesses everywhere
+};
+struct Jobs {
+  Job job[3];
+};
+
+template <int V, int ACT>
+__device__ __forceinline__ void row_job(const Job& J, float* sh) {
+  constexpr int NP = (V + 1) / 2;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int c = (blockIdx.x * 32 + lane) * V;
-  float acc[V];
+  if (blockIdx.x * 32 * V >= J.cols) return;
+  const int64_t r0 = (int64_t)blockIdx.y * kChunkRows + warp, r1 = min((int64_t)(blockIdx.y + 1) * kChunkRows, J.rows);
+  float2 acc[NP];
 #pragma unroll
-  for (int v = 0; v < V; ++v) acc[v] = 0.f;
-  const int64_t r0 = (int64_t)blockIdx.y * kChunkRows, r1 = r0 + kChunkRows < rows ? r0 + kChunkRows : rows;
-  if (c < cols) {
-#pragma unroll 4
-    for (int64_t r = r0 + warp; r < r1; r += 8) {
-      float2 g[(V + 1) / 2], u[(V + 1) / 2];
-      if constexpr (V == 8) {
-        const uint4 a = __ldcs(reinterpret_cast<const uint4*>(dy + r * lddy + c));
-        g[0] = widen2(a.x); g[1] = widen2(a.y); g[2] = widen2(a.z); g[3] = widen2(a.w);
-        if (z) {
-          const uint4 b = __ldcs(reinterpret_cast<const uint4*>(z + r * ldz + c));
-          u[0] = widen2(b.x); u[1] = widen2(b.y); u[2] = widen2(b.z); u[3] = widen2(b.w);
+  for (int j = 0; j < NP; ++j) acc[j] = two(0.f);
+  if (c < J.cols) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {             // four rows' loads, then four rows' work
+      float2 g[4][NP], u[4][NP];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t r = r0 + 8 * (4 * half + i);
+        if (r >= r1) continue;
+        if constexpr (V == 8) {
+          const uint4 a = __ldcs(reinterpret_cast<const uint4*>(J.in + r * J.ldi + c));
+          g[i][0] = widen2(a.x); g[i][1] = widen2(a.y); g[i][2] = widen2(a.z); g[i][3] = widen2(a.w);
+          if constexpr (ACT != DMX_ACT_NONE) {
+            const uint4 b = __ldcs(reinterpret_cast<const uint4*>(J.z + r * J.ldz + c));
+            u[i][0] = widen2(b.x); u[i][1] = widen2(b.y); u[i][2] = widen2(b.z); u[i][3] = widen2(b.w);
+          }
+        } else {
+          g[i][0] = make_float2(__bfloat162float(J.in[r * J.ldi + c]), 0.f);
+          if constexpr (ACT != DMX_ACT_NONE) u[i][0] = make_float2(__bfloat162float(J.z[r * J.ldz + c]), 0.f);
         }
-      } else {
-        g[0] = make_float2(__bfloat162float(dy[r * lddy + c]), 0.f);
-        if (z) u[0] = make_float2(__bfloat162float(z[r * ldz + c]), 0.f);
       }
 #pragma unroll
-      for (int j = 0; j < (V + 1) / 2; ++j) {
-        if (act == DMX_ACT_RELU) g[j] = dmx_act::times_slope<DMX_ACT_RELU>(g[j], u[j]);
-        else if (act == DMX_ACT_SILU) g[j] = dmx_act::times_slope<DMX_ACT_SILU>(g[j], u[j]);
-        else if (act == DMX_ACT_GELU) g[j] = dmx_act::times_slope<DMX_ACT_GELU>(g[j], u[j]);
-        acc[2 * j] += g[j].x;
-        if (V > 1) acc[(2 * j + 1) % V] += g[j].y;
-      }
-      if (out) {
-        if constexpr (V == 8)
-          *reinterpret_cast<uint4*>(out + r * ldo + c) = make_uint4(pack2(g[0].x, g[0].y), pack2(g[1].x, g[1].y), pack2(g[2].x, g[2].y), pack2(g[3].x, g[3].y));
-        else out[r * ldo + c] = __float2bfloat16_rn(g[0].x);
+      for (int i = 0; i < 4; ++i) {
+        const int64_t r = r0 + 8 * (4 * half + i);
+        if (r >= r1) continue;
+#pragma unroll
+        for (int j = 0; j < NP; ++j) {
+          if constexpr (ACT != DMX_ACT_NONE) g[i][j] = dmx_act::times_slope<ACT>(g[i][j], u[i][j]);
+          acc[j] = add2(acc[j], g[i][j]);
+        }
+        if (J.out) {
+          if constexpr (V == 8)
+            *reinterpret_cast<uint4*>(J.out + r * J.ldo + c) = make_uint4(pack2(g[i][0].x, g[i][0].y), pack2(g[i][1].x, g[i][1].y), pack2(g[i][2].x, g[i][2].y), pack2(g[i][3].x, g[i][3].y));
+          else J.out[r * J.ldo + c] = __float2bfloat16_rn(g[i][0].x);
+        }
       }
     }
   }
-  if (!sums) return;
+  if (!J.sums) return;
+  float* mine = sh + (warp * 32 + lane) * V;
 #pragma unroll
-  for (int v = 0; v < V; ++v) sh[warp][lane * V + v] = acc[v];
+  for (int j = 0; j < NP; ++j) {
+    mine[2 * j] = acc[j].x;
+    if (V > 1) mine[(2 * j + 1) % V] = acc[j].y;
+  }
   __syncthreads();
   for (int i = threadIdx.x; i < 32 * V; i += 256) {
     float t = 0.f;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) t += sh[w][i];
-    if (blockIdx.x * 32 * V + i < cols) sums[(int64_t)blockIdx.y * cols + blockIdx.x * 32 * V + i] = t;
+    for (int w = 0; w < 8; ++w) t += sh[w * 32 * V + i];
+    if (blockIdx.x * 32 * V + i < J.cols) J.sums[(int64_t)blockIdx.y * J.cols + blockIdx.x * 32 * V + i] = t;
+  }
+}
+
+// ACT: of the first job; the others are copies
+template <int ACT>
+__global__ void __launch_bounds__(256) rows_kernel(const __grid_constant__ Jobs all) {
+  __shared__ __align__(16) float sh[8 * 32 * 8];
+  start_dependents();
+  wait_for_previous();
+  const Job& J = all.job[blockIdx.z];
+  if ((int64_t)blockIdx.y * kChunkRows >= J.rows) return;
+  if (blockIdx.z == 0) {
+    if (J.vec) row_job<8, ACT>(J, sh);
+    else row_job<1, ACT>(J, sh);
+  } else {
+    row_job<1, DMX_ACT_NONE>(J, sh);
   }
 }
 
@@ -669,11 +708,11 @@ Choice choose(int64_t rowsA, int64_t rowsB, int kblocks, bool swap) {
     if (swap ? f.pair || f.bn != (rowsB <= 32 ? 32 : 64) : f.bn == 32) continue;
     const int rows = f.pair ? 2 * kBM : kBM, at_once = f.pair ? 74 : 148;
     const int64_t tiles = ((rowsA + rows - 1) / rows) * ((rowsB + f.bn - 1) / f.bn);
-    const int most = f.pair ? 1 : swap ? 4 : f.bn == 256 ? 1 : f.bn / 32;
+    const int most = swap ? 4 : f.pair || f.bn == 256 ? 1 : 2;
     for (int split = 1; split <= most; split *= 2) {
       if (split > 1 && (tiles * split > 148 || kblocks / split < 2)) break;
       const int64_t waves = (tiles * split + at_once - 1) / at_once;
-      const float t = waves * ((kblocks + split - 1) / split) * f.stage + 8.f * f.bn + (split > 1 ? 1500.f : 0.f);
+      const float t = waves * ((kblocks + split - 1) / split) * f.stage + 8.f * f.bn + (split > 1 ? 2000.f : 0.f);
       if (best.bn == 0 || t < least) { best.bn = f.bn; best.split = split; best.pair = f.pair; least = t; }
     }
   }
@@ -694,7 +733,14 @@ int launch_gemm(const Matrix& a, const Matrix& b, GemmArgs& A, int split, cudaSt
   if (A.stages > kMaxStages) A.stages = kMaxStages;
   const int smem = A.stages * stage + extra;
   const auto kernel = gemm_kernel<BN, SWAP, PAIR>;
-  if (!dmxh::cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost))) return DMX_ERR_CUDA;
+  static std::atomic<uint64_t> set{0};         // devices on which this kernel may use that much shared memory
+  int device = 0;
+  if (!dmxh::cuda_ok(cudaGetDevice(&device))) return DMX_ERR_CUDA;
+  const uint64_t bit = (uint64_t)1 << (device & 63);
+  if (!(set.load(std::memory_order_relaxed) & bit) || device > 63) {
+    if (!dmxh::cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost))) return DMX_ERR_CUDA;
+    set.fetch_or(bit, std::memory_order_relaxed);
+  }
   const int64_t tiles = (int64_t)A.tilesA * A.tilesB;
   const int per = PAIR ? 2 : split;
   if (tiles * per > 0x7fffffff) return DMX_ERR_ARG;
@@ -730,26 +776,35 @@ int product(const Matrix& a, int mnA, const Matrix& b, int mnB, int64_t k, const
   return launch_gemm<64, false, false>(a, b, A, c.split, st);
 }
 
-int slope(const Matrix& dy, const bf16* z, int64_t ldz, int act, bf16* out, int64_t ldo, float* sums, cudaStream_t st) {
-  const bool vec = aligned(dy.p, 16) && (dy.rows <= 1 || dy.ld % 8 == 0) && dy.cols % 8 == 0 &&
-                   (!z || (aligned(z, 16) && (dy.rows <= 1 || ldz % 8 == 0)));
-  const int64_t chunks = (dy.rows + kChunkRows - 1) / kChunkRows;
-  const int V = vec ? 8 : 1;
-  if (chunks > 65535) return DMX_ERR_ARG;
-  const dim3 grid((unsigned)((dy.cols + 32 * V - 1) / (32 * V)), (unsigned)chunks);
-  return start(grid, st, vec ? slope_kernel<8> : slope_kernel<1>, dy.p, dy.ld, z, ldz, act, dy.rows, (int)dy.cols, out, ldo, sums);
+int run_jobs(const Jobs& jobs, int n, int act, cudaStream_t st) {
+  int64_t columns = 0, chunks = 0;
+  for (int i = 0; i < n; ++i) {
+    const Job& j = jobs.job[i];
+    const int64_t c = (j.cols + (j.vec ? 255 : 31)) / (j.vec ? 256 : 32), r = (j.rows + kChunkRows - 1) / kChunkRows;
+    columns = c > columns ? c : columns;
+    chunks = r > chunks ? r : chunks;
+  }
+  const dim3 grid((unsigned)columns, (unsigned)chunks, (unsigned)n);
+  switch (act) {
+    case DMX_ACT_RELU: return start(grid, st, rows_kernel<DMX_ACT_RELU>, jobs);
+    case DMX_ACT_SILU: return start(grid, st, rows_kernel<DMX_ACT_SILU>, jobs);
+    case DMX_ACT_GELU: return start(grid, st, rows_kernel<DMX_ACT_GELU>, jobs);
+    default: return start(grid, st, rows_kernel<DMX_ACT_NONE>, jobs);
+  }
 }
 
-// m itself, or its copy at *ws (which moves on)
-int lay_out(Matrix& m, unsigned char*& ws, cudaStream_t st) {
+// m's copy at *ws (which moves on), if it needs one
+void lay_out(Matrix& m, unsigned char*& ws, Jobs& jobs, int& n) {
   const int64_t bytes = laid_out_bytes(m);
-  if (bytes == 0) return DMX_OK;
-  bf16* p = reinterpret_cast<bf16*>(ws);
+  if (bytes == 0) return;
+  Job& j = jobs.job[n++];
+  j = Job();
+  j.in = m.p; j.ldi = m.ld; j.rows = m.rows; j.cols = (int)m.cols;
+  j.out = reinterpret_cast<bf16*>(ws);
+  j.ldo = pad8(m.cols);
   ws += bytes;
-  const int rc = slope(m, nullptr, 0, DMX_ACT_NONE, p, pad8(m.cols), nullptr, st);
-  m.p = p;
-  m.ld = pad8(m.cols);
-  return rc;
+  m.p = j.out;
+  m.ld = j.ldo;
 }
 
 bool extents_ok(int64_t M, int64_t N, int64_t K) {
@@ -805,8 +860,11 @@ int dmx_linear_forward(int64_t M, int64_t N, int64_t K, const void* x, int64_t l
   }
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   Matrix a = {static_cast<const bf16*>(x), M, K, M > 1 ? ldx : K}, b = {static_cast<const bf16*>(w), N, K, N > 1 ? ldw : K};
-  int rc = lay_out(a, ws, st);
-  if (rc == DMX_OK) rc = lay_out(b, ws, st);
+  Jobs jobs;
+  int n = 0;
+  lay_out(a, ws, jobs, n);
+  lay_out(b, ws, jobs, n);
+  const int rc = n > 0 ? run_jobs(jobs, n, DMX_ACT_NONE, st) : DMX_OK;
   return rc != DMX_OK ? rc : product(a, 0, b, 0, K, E, st);
 }
 
@@ -838,30 +896,39 @@ int dmx_linear_backward(int64_t M, int64_t N, int64_t K, const void* dy, int64_t
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   float* sums = reinterpret_cast<float*>(ws);
   ws += p.sums;
-  int rc = DMX_OK;
-  if (p.needs_dz || dbias) {
-    bf16* out = p.needs_dz && (dx || dw) ? reinterpret_cast<bf16*>(ws) : nullptr;
-    rc = slope(g, act != DMX_ACT_NONE ? static_cast<const bf16*>(z) : nullptr, M > 1 ? ldz : N, act, out, pad8(N), dbias ? sums : nullptr, st);
-    if (rc != DMX_OK) return rc;
-    if (out) { g.p = out; g.ld = pad8(N); }
-    if (dbias) {
-      rc = start(dim3((unsigned)((N + 31) / 32)), st, columns_kernel, (const float*)sums, (M + kChunkRows - 1) / kChunkRows, (int)N, static_cast<bf16*>(dbias));
-      if (rc != DMX_OK) return rc;
+  Jobs jobs;
+  int n = 0, rc = DMX_OK;
+  const bool products = K > 0 && (dx || dw);
+  if ((p.needs_dz && products) || dbias) {
+    Job& j = jobs.job[n++];
+    j = Job();
+    j.in = g.p; j.ldi = g.ld; j.rows = M; j.cols = (int)N;
+    j.z = act != DMX_ACT_NONE ? static_cast<const bf16*>(z) : nullptr;
+    j.ldz = M > 1 ? ldz : N;
+    j.sums = dbias ? sums : nullptr;
+    j.vec = aligned(g.p, 16) && (M <= 1 || g.ld % 8 == 0) && N % 8 == 0 && (!j.z || (aligned(j.z, 16) && (M <= 1 || j.ldz % 8 == 0)));
+    if (p.needs_dz && products) {
+      g.p = j.out = reinterpret_cast<bf16*>(ws);
+      g.ld = j.ldo = pad8(N);
     }
+  } else {                         // (only the first job takes the activation)
+    act = DMX_ACT_NONE;
   }
   ws += p.dz;
-  if (K == 0) return DMX_OK;
+  if (K > 0 && dx) lay_out(b, ws, jobs, n);
+  if (K > 0 && dw) lay_out(a, ws, jobs, n);
+  if (n > 0) rc = run_jobs(jobs, n, act, st);
+  if (rc == DMX_OK && dbias)
+    rc = start(dim3((unsigned)((N + 31) / 32)), st, columns_kernel, (const float*)sums, (M + kChunkRows - 1) / kChunkRows, (int)N, static_cast<bf16*>(dbias));
   GemmArgs E = {};
   E.act = DMX_ACT_NONE;
-  if (dx) {                        // dx[m, k] = sum_n dz[m, n] w[n, k]
-    rc = lay_out(b, ws, st);
+  if (products && dx && rc == DMX_OK) {        // dx[m, k] = sum_n dz[m, n] w[n, k]
     E.y = static_cast<bf16*>(dx); E.ldy = M > 1 ? lddx : K;
-    if (rc == DMX_OK) rc = product(g, 0, b, 1, N, E, st);
+    rc = product(g, 0, b, 1, N, E, st);
   }
-  if (dw && rc == DMX_OK) {        // dw[n, k] = sum_m dz[m, n] x[m, k]
-    rc = lay_out(a, ws, st);
+  if (products && dw && rc == DMX_OK) {        // dw[n, k] = sum_m dz[m, n] x[m, k]
     E.y = static_cast<bf16*>(dw); E.ldy = N > 1 ? lddw : K;
-    if (rc == DMX_OK) rc = product(g, 1, a, 1, M, E, st);
+    rc = product(g, 1, a, 1, M, E, st);
   }
   return rc;
 }

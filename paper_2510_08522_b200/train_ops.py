@@ -8,6 +8,7 @@ Nothing synchronises.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 from . import binding as B
 
@@ -35,20 +36,20 @@ def _refuse(where, code=B.ERR_ARG):
     raise B.DmxError(code, where)
 
 
-class _on:
-    """Makes a tensor's device current for a call (launches go to the current device)."""
-    __slots__ = ("guard",)
-
-    def __init__(self, x):
-        self.guard = None if x.device.index == _torch.cuda.current_device() else _torch.cuda.device(x.device)
-
+class _Nothing:
     def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
+        pass
 
     def __exit__(self, *a):
-        if self.guard is not None:
-            self.guard.__exit__(*a)
+        pass
+
+
+_nothing = _Nothing()
+
+
+def _on(x):
+    """A context in which x's device is current (launches go to the current device)."""
+    return _nothing if x.device.index == _torch._C._cuda_getDevice() else _torch.cuda.device(x.device)
 
 
 def _ptr(x):
@@ -179,7 +180,7 @@ class AdamW:
 
 def _image(x, shape, dtype, like, where):
     """Strides (image, row) of an (N, ..., C) tensor whose positions lie at one stride and whose channels are dense."""
-    if x.dtype != dtype or x.device != like.device or x.shape != shape:
+    if x is not like and (x.dtype != dtype or x.device != like.device or x.shape != shape):
         _refuse(where)
     st = x.stride()
     if x.dim() == 3:
@@ -206,11 +207,17 @@ def _norm_args(x, groups, weight, bias, act, where):
     _t()
     if x.dim() < 3 or x.dtype not in _dtypes or not x.is_cuda or act not in ACT:
         _refuse(where)
-    C = x.shape[-1]
+    shape = x.shape
+    C = shape[-1]
     for p in (weight, bias):
         if p is not None and (p.dtype != _torch.float32 or p.numel() != C or p.device != x.device or not p.is_contiguous()):
             _refuse(where + " (weight, bias)")
-    return x.shape[0], _prod(x.shape[1:-1]), C, _dtypes[x.dtype]
+    return shape[0], shape[1] if len(shape) == 3 else _prod(shape[1:-1]), C, _dtypes[x.dtype]
+
+
+@functools.lru_cache(maxsize=256)
+def _norm_workspace(*shape):
+    return B.lib().dmx_group_norm_workspace(*shape)
 
 
 def group_norm(x, groups, weight=None, bias=None, eps=1e-5, act="none", out=None):
@@ -218,19 +225,23 @@ def group_norm(x, groups, weight=None, bias=None, eps=1e-5, act="none", out=None
     fp32 (N, groups). weight, bias: fp32 (C,). x may be a channel slice of a wider tensor; out may be x."""
     N, L, C, dt = _norm_args(x, groups, weight, bias, act, "group_norm")
     xs = _image(x, x.shape, x.dtype, x, "group_norm (x)")
-    y = _torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-    ys = _image(y, x.shape, x.dtype, x, "group_norm (out)")
+    if out is None:
+        y = _torch.empty_like(x, memory_format=_torch.contiguous_format)
+        ys = (L * C, C)
+    else:
+        y = out
+        ys = _image(y, x.shape, x.dtype, x, "group_norm (out)")
     if groups < 1:
         _refuse("group_norm (groups)")
-    stats = _torch.empty((2, N, groups), dtype=_torch.float32, device=x.device)
-    L_ = B.lib()
+    mean, rstd = _torch.empty((2, N, groups), dtype=_torch.float32, device=x.device).unbind()
+    need = _norm_workspace(N, L, C, groups, dt, 0)
+    ws = _workspace(need, x, "group_norm") if need else None
     with _on(x):
-        ws = _workspace(L_.dmx_group_norm_workspace(N, L, C, groups, dt, 0), x, "group_norm")
-        rc = L_.dmx_group_norm_forward(N, L, C, groups, dt, x.data_ptr(), xs[0], xs[1], _ptr(weight), _ptr(bias), eps, ACT[act], y.data_ptr(), ys[0], ys[1],
-                                       stats.data_ptr(), stats.data_ptr() + 4 * N * groups, _ptr(ws), 0 if ws is None else ws.numel(), _stream(x))
+        rc = B.lib().dmx_group_norm_forward(N, L, C, groups, dt, x.data_ptr(), xs[0], xs[1], _ptr(weight), _ptr(bias), eps, ACT[act], y.data_ptr(), ys[0], ys[1],
+                                            mean.data_ptr(), rstd.data_ptr(), _ptr(ws), need, _stream(x))
     if rc != B.OK:
         _refuse("dmx_group_norm_forward", rc)
-    return y, stats[0], stats[1]
+    return y, mean, rstd
 
 
 def group_norm_backward(dy, x, mean, rstd, groups, weight=None, bias=None, act="none", out=None):
@@ -238,21 +249,25 @@ def group_norm_backward(dy, x, mean, rstd, groups, weight=None, bias=None, act="
     N, L, C, dt = _norm_args(x, groups, weight, bias, act, "group_norm_backward")
     xs = _image(x, x.shape, x.dtype, x, "group_norm_backward (x)")
     gs = _image(dy, x.shape, x.dtype, x, "group_norm_backward (dy)")
-    dx = _torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-    ds = _image(dx, x.shape, x.dtype, x, "group_norm_backward (out)")
+    if out is None:
+        dx = _torch.empty_like(x, memory_format=_torch.contiguous_format)
+        ds = (L * C, C)
+    else:
+        dx = out
+        ds = _image(dx, x.shape, x.dtype, x, "group_norm_backward (out)")
     for s in (mean, rstd):
         if s.dtype != _torch.float32 or s.numel() != N * groups or s.device != x.device or not s.is_contiguous():
             _refuse("group_norm_backward (statistics)")
-    dp = _torch.empty((2, C), dtype=_torch.float32, device=x.device)
-    L_ = B.lib()
+    dweight, dbias = _torch.empty((2, C), dtype=_torch.float32, device=x.device).unbind()
+    need = _norm_workspace(N, L, C, groups, dt, 1)
+    ws = _workspace(need, x, "group_norm_backward") if need else None
     with _on(x):
-        ws = _workspace(L_.dmx_group_norm_workspace(N, L, C, groups, dt, 1), x, "group_norm_backward")
-        rc = L_.dmx_group_norm_backward(N, L, C, groups, dt, dy.data_ptr(), gs[0], gs[1], x.data_ptr(), xs[0], xs[1], mean.data_ptr(), rstd.data_ptr(),
-                                        _ptr(weight), _ptr(bias), ACT[act], dx.data_ptr(), ds[0], ds[1], dp.data_ptr(), dp.data_ptr() + 4 * C,
-                                        _ptr(ws), 0 if ws is None else ws.numel(), _stream(x))
+        rc = B.lib().dmx_group_norm_backward(N, L, C, groups, dt, dy.data_ptr(), gs[0], gs[1], x.data_ptr(), xs[0], xs[1], mean.data_ptr(), rstd.data_ptr(),
+                                        _ptr(weight), _ptr(bias), ACT[act], dx.data_ptr(), ds[0], ds[1], dweight.data_ptr(),
+                                             dbias.data_ptr(), _ptr(ws), need, _stream(x))
     if rc != B.OK:
         _refuse("dmx_group_norm_backward", rc)
-    return dx, dp[0], dp[1]
+    return dx, dweight, dbias
 
 
 def _rows(x, shape, like, where):
@@ -281,13 +296,16 @@ def linear(x, weight, bias=None, act="none", residual=None, save=False, out=None
     if bias is not None and (bias.dtype != _torch.bfloat16 or bias.numel() != N or bias.device != x.device or not bias.is_contiguous()):
         _refuse("linear (bias)")
     ldr = 0 if residual is None else _rows(residual, (M, N), x, "linear (residual)")
-    y = _torch.empty((M, N), dtype=_torch.bfloat16, device=x.device) if out is None else out
-    ldy = _rows(y, (M, N), x, "linear (out)")
-    z = _torch.empty((M, N), dtype=_torch.bfloat16, device=x.device) if save and act != "none" else None
+    y = x.new_empty((M, N)) if out is None else out
+    ldy = N if out is None else _rows(y, (M, N), x, "linear (out)")
+    z = x.new_empty((M, N)) if save and act != "none" else None
     L = B.lib()
     xp, wp = x.data_ptr(), weight.data_ptr()
     with _on(x):
-        ws = _workspace(L.dmx_linear_workspace(M, N, K, xp, ldx, wp, ldw), x, "linear")
+        if (xp | wp | 2 * ldx | 2 * ldw) & 15:           # an operand has to be laid out (or is one row)
+            ws = _workspace(L.dmx_linear_workspace(M, N, K, xp, ldx, wp, ldw), x, "linear")
+        else:
+            ws = None
         rc = L.dmx_linear_forward(M, N, K, xp, ldx, wp, ldw, _ptr(bias), ACT[act], _ptr(residual), ldr, y.data_ptr(), ldy, _ptr(z), N, _ptr(ws),
                                   0 if ws is None else ws.numel(), _stream(x))
     if rc != B.OK:
