@@ -42,7 +42,7 @@ __device__ unsigned g_gave_up;                // CTAs whose waits ran out
 
 struct GemmArgs {
   int rowsA, rowsB, kblocks;                  // rows of D, columns of D, ceil(k / 64)
-  int tilesA, tilesB, split, stages;
+  int tilesA, tilesB, stages;
   int mnA, mnB;                               // operand is MN-major
   const bf16 *bias, *residual;
   bf16 *y, *z;
@@ -149,15 +149,17 @@ __device__ __forceinline__ unsigned pack2(float a, float b) {
 // and eight rows at a time are free of bank conflicts.
 __device__ __forceinline__ uint4* unit(uint4* stage, int row, int u) { return stage + row * 4 + (u ^ ((row >> 1) & 3)); }
 
-// rows r0.. (32) x columns c0.. (32) of a matrix out of the staging buffer
-__device__ __forceinline__ void store_chunk(bf16* p, int64_t ld, int vec, uint4* stage, int r0, int rows, int c0, int cols, int lane) {
+// ROWS rows from r0 and COLS (8 to 32) columns from c0 of a matrix, out of and into the staging buffer
+template <int ROWS, int COLS>
+__device__ __forceinline__ void store_tile(bf16* p, int64_t ld, int vec, uint4* stage, int r0, int rows, int c0, int cols, int lane) {
+  constexpr int kUnits = COLS / 8, kAtOnce = 32 / kUnits;
   __syncwarp();
   if (vec) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = i * 8 + (lane >> 2), c = c0 + (lane & 3) * 8;
-      if (r0 + r >= rows || c >= cols) continue;
-      const uint4 v = *unit(stage, r, lane & 3);
+    for (int i = 0; i < (ROWS + kAtOnce - 1) / kAtOnce; ++i) {
+      const int r = i * kAtOnce + lane / kUnits, u = lane % kUnits, c = c0 + u * 8;
+      if (r >= ROWS || r0 + r >= rows || c >= cols) continue;
+      const uint4 v = *unit(stage, r, u);
       bf16* q = p + (int64_t)(r0 + r) * ld + c;
       if (c + 8 <= cols) {
         *reinterpret_cast<uint4*>(q) = v;
@@ -168,48 +170,45 @@ __device__ __forceinline__ void store_chunk(bf16* p, int64_t ld, int vec, uint4*
           if (c + k < cols) reinterpret_cast<unsigned short*>(q)[k] = (unsigned short)(w[k >> 1] >> (16 * (k & 1)));
       }
     }
-  } else if (c0 + lane < cols) {
-    const int n = min(32, rows - r0);
+  } else if (lane < COLS && c0 + lane < cols) {
+    const int n = min(ROWS, rows - r0);
 #pragma unroll 8
     for (int r = 0; r < n; ++r)
       reinterpret_cast<unsigned short*>(p)[(int64_t)(r0 + r) * ld + c0 + lane] = reinterpret_cast<const unsigned short*>(unit(stage, r, lane >> 3))[lane & 7];
   }
   __syncwarp();
 }
-__device__ __forceinline__ void load_chunk(const bf16* p, int64_t ld, int vec, uint4* stage, int r0, int rows, int c0, int cols, int lane) {
+template <int ROWS, int COLS>
+__device__ __forceinline__ void load_tile(const bf16* p, int64_t ld, int vec, uint4* stage, int r0, int rows, int c0, int cols, int lane) {
+  constexpr int kUnits = COLS / 8, kAtOnce = 32 / kUnits;
   if (vec) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int r = i * 8 + (lane >> 2), c = c0 + (lane & 3) * 8;
-      if (r0 + r >= rows || c >= cols) continue;
+    for (int i = 0; i < (ROWS + kAtOnce - 1) / kAtOnce; ++i) {
+      const int r = i * kAtOnce + lane / kUnits, u = lane % kUnits, c = c0 + u * 8;
+      if (r >= ROWS || r0 + r >= rows || c >= cols) continue;
       const bf16* q = p + (int64_t)(r0 + r) * ld + c;
       if (c + 8 <= cols) {
-        *unit(stage, r, lane & 3) = *reinterpret_cast<const uint4*>(q);
+        *unit(stage, r, u) = *reinterpret_cast<const uint4*>(q);
       } else {
-        unsigned short* d = reinterpret_cast<unsigned short*>(unit(stage, r, lane & 3));
+        unsigned short* d = reinterpret_cast<unsigned short*>(unit(stage, r, u));
 #pragma unroll
         for (int k = 0; k < 8; ++k)
           if (c + k < cols) d[k] = reinterpret_cast<const unsigned short*>(q)[k];
       }
     }
-  } else if (c0 + lane < cols) {
-    const int n = min(32, rows - r0);
+  } else if (lane < COLS && c0 + lane < cols) {
+    const int n = min(ROWS, rows - r0);
 #pragma unroll 8
     for (int r = 0; r < n; ++r)
       reinterpret_cast<unsigned short*>(unit(stage, r, lane >> 3))[lane & 7] = reinterpret_cast<const unsigned short*>(p)[(int64_t)(r0 + r) * ld + c0 + lane];
   }
   __syncwarp();
 }
-__device__ __forceinline__ void stage_row(uint4* stage, const float (&v)[32], int lane) {
-#pragma unroll
-  for (int u = 0; u < 4; ++u)
-    *unit(stage, lane, u) = make_uint4(pack2(v[8 * u], v[8 * u + 1]), pack2(v[8 * u + 2], v[8 * u + 3]), pack2(v[8 * u + 4], v[8 * u + 5]),
-                                       pack2(v[8 * u + 6], v[8 * u + 7]));
-}
-__device__ __forceinline__ void activate(float (&v)[32], int act) {
+template <int NC>
+__device__ __forceinline__ void activate(float (&v)[NC], int act) {
   auto all = [&](auto f) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < NC / 2; ++i) {
       const float2 t = f(make_float2(v[2 * i], v[2 * i + 1]));
       v[2 * i] = t.x; v[2 * i + 1] = t.y;
     }
@@ -219,68 +218,74 @@ __device__ __forceinline__ void activate(float (&v)[32], int act) {
   else if (act == DMX_ACT_GELU) all([](float2 u) { return dmx_act::apply<DMX_ACT_GELU>(u); });
 }
 
-// One warp's 32 rows x 32 columns of D, a row per lane.
-__device__ __forceinline__ void finish(const GemmArgs& A, float (&v)[32], uint4* stage, int r0, int c0, int lane) {
+// One warp's 32 rows x NC columns of D, a row per lane.
+template <int NC>
+__device__ __forceinline__ void finish(const GemmArgs& A, float (&v)[NC], uint4* stage, int r0, int c0, int lane) {
+  auto to_stage = [&] {
+#pragma unroll
+    for (int u = 0; u < NC / 8; ++u)
+      *unit(stage, lane, u) = make_uint4(pack2(v[8 * u], v[8 * u + 1]), pack2(v[8 * u + 2], v[8 * u + 3]), pack2(v[8 * u + 4], v[8 * u + 5]),
+                                         pack2(v[8 * u + 6], v[8 * u + 7]));
+  };
+  auto add8 = [&](int u, uint4 b) {
+    const unsigned w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float2 t = widen2(w[k]);
+      v[8 * u + 2 * k] += t.x; v[8 * u + 2 * k + 1] += t.y;
+    }
+  };
   if (A.bias) {
-    if (c0 + 32 <= A.rowsB && (reinterpret_cast<uintptr_t>(A.bias) & 15) == 0) {
+    if (c0 + NC <= A.rowsB && (reinterpret_cast<uintptr_t>(A.bias) & 15) == 0) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const uint4 b = __ldg(reinterpret_cast<const uint4*>(A.bias + c0) + u);
-        const unsigned w[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float2 t = widen2(w[k]);
-          v[8 * u + 2 * k] += t.x; v[8 * u + 2 * k + 1] += t.y;
-        }
-      }
+      for (int u = 0; u < NC / 8; ++u) add8(u, __ldg(reinterpret_cast<const uint4*>(A.bias + c0) + u));
     } else {
 #pragma unroll
-      for (int i = 0; i < 32; ++i)
+      for (int i = 0; i < NC; ++i)
         if (c0 + i < A.rowsB) v[i] += bf_value(__ldg(reinterpret_cast<const unsigned short*>(A.bias) + c0 + i));
     }
   }
   if (A.z) {
-    stage_row(stage, v, lane);
-    store_chunk(A.z, A.ldz, A.vecz, stage, r0, A.rowsA, c0, A.rowsB, lane);
+    to_stage();
+    store_tile<32, NC>(A.z, A.ldz, A.vecz, stage, r0, A.rowsA, c0, A.rowsB, lane);
   }
   activate(v, A.act);
   if (A.residual) {
-    load_chunk(A.residual, A.ldr, A.vecr, stage, r0, A.rowsA, c0, A.rowsB, lane);
+    load_tile<32, NC>(A.residual, A.ldr, A.vecr, stage, r0, A.rowsA, c0, A.rowsB, lane);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const uint4 b = *unit(stage, lane, u);
-      const unsigned w[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float2 t = widen2(w[k]);
-        v[8 * u + 2 * k] += t.x; v[8 * u + 2 * k + 1] += t.y;
-      }
-    }
+    for (int u = 0; u < NC / 8; ++u) add8(u, *unit(stage, lane, u));
     __syncwarp();
   }
-  stage_row(stage, v, lane);
-  store_chunk(A.y, A.ldy, A.vecy, stage, r0, A.rowsA, c0, A.rowsB, lane);
+  to_stage();
+  store_tile<32, NC>(A.y, A.ldy, A.vecy, stage, r0, A.rowsA, c0, A.rowsB, lane);
 }
 
-// The same with the operands exchanged: a lane holds one column of y (a row of W) for 32 rows of x. Neighbouring lanes
-// are neighbours in memory, so it is stored as it lies.
-__device__ __forceinline__ void finish_swapped(const GemmArgs& A, float (&v)[32], int f, int t0) {
-  const bool on = f < A.rowsA;
-  const float b = A.bias && on ? bf_value(__ldg(reinterpret_cast<const unsigned short*>(A.bias) + f)) : 0.f;
+// The same with the operands exchanged: a lane holds one column of y (a row of W) for NC rows of x from t0; the
+// staging buffer turns them.
+template <int NC>
+__device__ __forceinline__ void finish_swapped(const GemmArgs& A, float (&v)[NC], uint4* stage, int f0, int t0, float bias, int lane) {
+  unsigned short* at[4];         // this lane's column in rows of each exchange pattern
 #pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] += b;
+  for (int k = 0; k < 4; ++k) at[k] = reinterpret_cast<unsigned short*>(stage + ((lane >> 3) ^ k)) + (lane & 7);
+  auto to_stage = [&] {
+#pragma unroll
+    for (int i = 0; i < NC; ++i) at[(i >> 1) & 3][i * 32] = __bfloat16_as_ushort(__float2bfloat16_rn(v[i]));
+  };
+#pragma unroll
+  for (int i = 0; i < NC; ++i) v[i] += bias;
   if (A.z) {
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (on && t0 + i < A.rowsB) A.z[(int64_t)(t0 + i) * A.ldz + f] = __float2bfloat16_rn(v[i]);
+    to_stage();
+    store_tile<NC, 32>(A.z, A.ldz, A.vecz, stage, t0, A.rowsB, f0, A.rowsA, lane);
   }
   activate(v, A.act);
+  if (A.residual) {
+    load_tile<NC, 32>(A.residual, A.ldr, A.vecr, stage, t0, A.rowsB, f0, A.rowsA, lane);
 #pragma unroll
-  for (int i = 0; i < 32; ++i) {
-    if (!on || t0 + i >= A.rowsB) continue;
-    if (A.residual) v[i] += __bfloat162float(A.residual[(int64_t)(t0 + i) * A.ldr + f]);
-    A.y[(int64_t)(t0 + i) * A.ldy + f] = __float2bfloat16_rn(v[i]);
+    for (int i = 0; i < NC; ++i) v[i] += bf_value(at[(i >> 1) & 3][i * 32]);
+    __syncwarp();
   }
+  to_stage();
+  store_tile<NC, 32>(A.y, A.ldy, A.vecy, stage, t0, A.rowsB, f0, A.rowsA, lane);
 }
 
 // ---------------------------------------------------------------------------------------------- the product
@@ -289,7 +294,8 @@ __device__ __forceinline__ void finish_swapped(const GemmArgs& A, float (&v)[32]
 // first one's MMA thread multiplies on both SMs at once, and each holds its 128 rows of D in its own TMEM.
 // That halves what an SM has to fetch per product: 128 x 256 tiles by single CTAs are bound by the traffic out of L2
 // (8192^3: 820 TFLOP/s).
-template <int BN, bool SWAP, bool PAIR>
+// SPLIT: that many CTAs (a cluster) share a tile's k; each then completes 1/SPLIT of every 32 columns.
+template <int BN, bool SWAP, bool PAIR, int SPLIT>
 __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                                                                const __grid_constant__ GemmArgs A) {
   extern __shared__ __align__(1024) unsigned char raw[];
@@ -302,13 +308,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   constexpr unsigned kCols = 2 * BN < 32 ? 32 : 2 * BN;
   unsigned char* sm = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
   uint4* staging = reinterpret_cast<uint4*>(sm + (size_t)A.stages * kStage);                     // 2 KB per epilogue warp
-  float* sums = reinterpret_cast<float*>(sm + (size_t)A.stages * kStage + (SWAP ? 0 : kEpiWarps * 2048));   // the cluster's partial sums
+  float* sums = reinterpret_cast<float*>(sm + (size_t)A.stages * kStage + kEpiWarps * 2048);     // the cluster's partial sums
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int split = PAIR ? 1 : A.split, side = PAIR ? blockIdx.x & 1 : 0;
-  const int rank = split > 1 ? blockIdx.x % split : 0;
-  const int per = PAIR ? 2 : split;
+  static_assert(!PAIR || SPLIT == 1, "a pair does not split k");
+  constexpr int per = PAIR ? 2 : SPLIT, kOwn = 32 / SPLIT;
+  const int side = PAIR ? blockIdx.x & 1 : 0, rank = SPLIT > 1 ? blockIdx.x % SPLIT : 0;
   const int tiles = A.tilesA * A.tilesB, first = blockIdx.x / per, step = gridDim.x / per;
-  const int kb0 = (int)((int64_t)A.kblocks * rank / split), kb1 = (int)((int64_t)A.kblocks * (rank + 1) / split);
+  const int kb0 = (int)((int64_t)A.kblocks * rank / SPLIT), kb1 = (int)((int64_t)A.kblocks * (rank + 1) / SPLIT);
 
   start_dependents();
   if (threadIdx.x == 0) {
@@ -330,7 +336,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   tmem_fence_before();
   __syncthreads();
   tmem_fence_after();
-  if (PAIR || split > 1) cluster_sync();
+  if (PAIR || SPLIT > 1) cluster_sync();
   wait_for_previous();
   const unsigned tmem = tmem_base;
   bool ok = true;
@@ -423,71 +429,77 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       }
     }
   } else {
-    const int e = warp - 2, quarter = warp & 3, group = e >> 2;      // TMEM lanes 32 quarter.. belong to warps of that number mod 4
+    const int e = warp - 2, quarter = warp & 3, group = e >> 2;     // TMEM lanes 32 quarter.. belong to warps of that number mod 4
     uint4* stage = staging + e * 128;
     unsigned buf = 0, aph = 0;
     for (int t = first; t < tiles && ok; t += step) {
       int ta, tb;
       tile_at(t, ta, tb);
+      const int r0 = ta * kRows + side * kBM + quarter * 32;
+      float bias = 0.f;                                             // fetched before the wait
+      if (SWAP && A.bias && r0 + lane < A.rowsA) bias = bf_value(__ldg(reinterpret_cast<const unsigned short*>(A.bias) + r0 + lane));
+      if (!SWAP && A.bias && tb * BN + group * 32 < A.rowsB) asm volatile("prefetch.global.L1 [%0];" ::"l"(A.bias + tb * BN + group * 32));
       ok = warp_wait(smem_addr(&done[buf]), aph);
       if (!ok) break;
       tmem_fence_after();
-      const int r0 = ta * kRows + side * kBM + quarter * 32;
-      for (int c = group; c < kChunks; c += kEpiWarps / 4) {
-        const int c0 = tb * BN + c * 32;
-        if (c0 >= A.rowsB) break;
-        float v[32];
-        tmem_load32(tmem + buf * BN + c * 32 + ((unsigned)(quarter * 32) << 16), v);
-        if (split > 1) {
-          // chunk c is completed by CTA c mod split of the cluster; the others send it theirs
-          const int owner = c % split;
-          if (owner != rank) {
-            const unsigned to = in_cta(smem_addr(sums + ((size_t)(c / split) * split + rank) * (32 * kBM) + quarter * 32 + lane), owner);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + i * kBM * 4), "f"(v[i]) : "memory");
-          }
-        } else if (SWAP) {
-          finish_swapped(A, v, r0 + lane, c0);
-        } else {
-          finish(A, v, stage, r0, c0, lane);
+      if constexpr (SPLIT == 1) {
+        for (int c = group; c < kChunks; c += kEpiWarps / 4) {
+          const int c0 = tb * BN + c * 32;
+          if (c0 >= A.rowsB) break;
+          float v[32];
+          tmem_load32(tmem + buf * BN + c * 32 + ((unsigned)(quarter * 32) << 16), v);
+          if constexpr (SWAP) finish_swapped<32>(A, v, stage, r0, c0, bias, lane);
+          else finish<32>(A, v, stage, r0, c0, lane);
         }
+        tmem_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (PAIR) bar_arrive_cluster(in_cta(smem_addr(&freed[buf]), 0));
+          else bar_arrive(smem_addr(&freed[buf]));
+        }
+        if (buf) aph ^= 1;
+        buf ^= 1;
+      } else {
+        // one tile per cluster, at most one chunk per warp: what others complete goes to them, the rest stays
+        static_assert(SPLIT == 1 || kChunks <= kEpiWarps / 4, "a warp keeps its chunk in registers");
+        const int c0 = tb * BN + group * 32;
+        const bool mine = group < kChunks && c0 < A.rowsB;
+        float v[32], own[kOwn];
+        float* slots = sums + (size_t)group * SPLIT * kOwn * kBM + quarter * 32 + lane;       // [SPLIT sources][kOwn][128]
+        if (mine) {
+          tmem_load32(tmem + group * 32 + ((unsigned)(quarter * 32) << 16), v);
+#pragma unroll
+          for (int o = 0; o < SPLIT; ++o) {
+            if (o == rank) {
+#pragma unroll
+              for (int i = 0; i < kOwn; ++i) own[i] = v[o * kOwn + i];
+            } else if (c0 + o * kOwn < A.rowsB) {
+              const unsigned to = in_cta(smem_addr(slots + rank * kOwn * kBM), o);
+#pragma unroll
+              for (int i = 0; i < kOwn; ++i) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to + i * kBM * 4), "f"(v[o * kOwn + i]) : "memory");
+            }
+          }
+        }
+        __syncwarp();
+        cluster_sync();
+        if (mine && c0 + rank * kOwn < A.rowsB) {
+#pragma unroll
+          for (int q = 0; q < SPLIT; ++q)
+            if (q != rank) {
+#pragma unroll
+              for (int i = 0; i < kOwn; ++i) own[i] += slots[(q * kOwn + i) * kBM];
+            }
+          if constexpr (SWAP) finish_swapped<kOwn>(A, own, stage, r0, c0 + rank * kOwn, bias, lane);
+          else finish<kOwn>(A, own, stage, r0, c0 + rank * kOwn, lane);
+        }
+        break;
       }
-      if (split > 1) break;                                       // one tile per cluster; finished below
-      tmem_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        if (PAIR) bar_arrive_cluster(in_cta(smem_addr(&freed[buf]), 0));
-        else bar_arrive(smem_addr(&freed[buf]));
-      }
-      if (buf) aph ^= 1;
-      buf ^= 1;
     }
+    // a CTA that gave up before the exchange still takes its part in the barrier
+    if (SPLIT > 1 && !ok) cluster_sync();
   }
   __syncwarp();
-  if (split > 1) {
-    cluster_sync();
-    if (warp >= 2 && ok) {
-      const int e = warp - 2, quarter = warp & 3, group = e >> 2;
-      int ta, tb;
-      tile_at(first, ta, tb);
-      tmem_fence_after();
-      for (int c = group; c < kChunks; c += kEpiWarps / 4) {
-        const int c0 = tb * BN + c * 32;
-        if (c0 >= A.rowsB) break;
-        if (c % split != rank) continue;
-        float v[32];
-        tmem_load32(tmem + c * 32 + ((unsigned)(quarter * 32) << 16), v);
-        for (int q = 0; q < split; ++q) {
-          if (q == rank) continue;
-          const float* slot = sums + ((size_t)(c / split) * split + q) * (32 * kBM) + quarter * 32 + lane;
-#pragma unroll
-          for (int i = 0; i < 32; ++i) v[i] += slot[i * kBM];
-        }
-        if (SWAP) finish_swapped(A, v, ta * kBM + quarter * 32 + lane, c0);
-        else finish(A, v, staging + e * 128, ta * kBM + quarter * 32, c0, lane);
-      }
-    }
-  }
+  if (SPLIT > 1 && warp < 2) cluster_sync();
   if (!ok && lane == 0) atomicAdd(&g_gave_up, 1u);
   tmem_fence_before();
   __syncthreads();
@@ -621,7 +633,7 @@ __global__ void __launch_bounds__(256) bias_kernel(const __grid_constant__ GemmA
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)A.rowsA * A.rowsB; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / A.rowsB;
     const int c = (int)(i - r * A.rowsB);
-    float v[32] = {};
+    float v[2] = {};
     v[0] = A.bias ? __bfloat162float(A.bias[c]) : 0.f;
     if (A.z) A.z[r * A.ldz + c] = __float2bfloat16_rn(v[0]);
     activate(v, A.act);
@@ -712,27 +724,26 @@ Choice choose(int64_t rowsA, int64_t rowsB, int kblocks, bool swap) {
     for (int split = 1; split <= most; split *= 2) {
       if (split > 1 && (tiles * split > 148 || kblocks / split < 2)) break;
       const int64_t waves = (tiles * split + at_once - 1) / at_once;
-      const float t = waves * ((kblocks + split - 1) / split) * f.stage + 8.f * f.bn + (split > 1 ? 2000.f : 0.f);
+      const float t = waves * ((kblocks + split - 1) / split) * f.stage + 8.f * f.bn + (split > 1 ? 1300.f : 0.f);
       if (best.bn == 0 || t < least) { best.bn = f.bn; best.split = split; best.pair = f.pair; least = t; }
     }
   }
   return best;
 }
 
-template <int BN, bool SWAP, bool PAIR>
-int launch_gemm(const Matrix& a, const Matrix& b, GemmArgs& A, int split, cudaStream_t st) {
+template <int BN, bool SWAP, bool PAIR, int SPLIT>
+int launch_gemm(const Matrix& a, const Matrix& b, GemmArgs& A, cudaStream_t st) {
   constexpr int kHalf = PAIR ? BN / 2 : BN, kRows = PAIR ? 2 * kBM : kBM;
   CUtensorMap ma, mb;
   if (!make_map(&ma, a, A.mnA, kBM) || !make_map(&mb, b, A.mnB, kHalf)) return DMX_ERR_CUDA;
   A.tilesA = (A.rowsA + kRows - 1) / kRows;
   A.tilesB = (A.rowsB + BN - 1) / BN;
-  A.split = split;
   const int stage = (kBM + kHalf) * 128, chunks = BN / 32;
-  const int extra = 1024 + (SWAP ? 0 : kEpiWarps * 2048) + (split > 1 ? (chunks + split - 1) / split * split * 32 * kBM * 4 : 0);
+  const int extra = 1024 + kEpiWarps * 2048 + (SPLIT > 1 ? chunks * 32 * kBM * 4 : 0);
   A.stages = (kSmemMost - extra) / stage;
   if (A.stages > kMaxStages) A.stages = kMaxStages;
   const int smem = A.stages * stage + extra;
-  const auto kernel = gemm_kernel<BN, SWAP, PAIR>;
+  const auto kernel = gemm_kernel<BN, SWAP, PAIR, SPLIT>;
   static std::atomic<uint64_t> set{0};         // devices on which this kernel may use that much shared memory
   int device = 0;
   if (!dmxh::cuda_ok(cudaGetDevice(&device))) return DMX_ERR_CUDA;
@@ -742,10 +753,10 @@ int launch_gemm(const Matrix& a, const Matrix& b, GemmArgs& A, int split, cudaSt
     set.fetch_or(bit, std::memory_order_relaxed);
   }
   const int64_t tiles = (int64_t)A.tilesA * A.tilesB;
-  const int per = PAIR ? 2 : split;
+  constexpr int per = PAIR ? 2 : SPLIT;
   if (tiles * per > 0x7fffffff) return DMX_ERR_ARG;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(split > 1 || tiles * per < 148 ? tiles * per : 148));
+  cfg.gridDim = dim3((unsigned)(SPLIT > 1 || tiles * per < 148 ? tiles * per : 148));
   cfg.blockDim = dim3(kGemmThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
@@ -765,15 +776,20 @@ int product(const Matrix& a, int mnA, const Matrix& b, int mnB, int64_t k, const
     A.rowsA = (int)rowsB; A.rowsB = (int)rowsA;
     A.mnA = mnB; A.mnB = mnA;
     const Choice c = choose(rowsB, rowsA, A.kblocks, true);
-    return c.bn == 32 ? launch_gemm<32, true, false>(b, a, A, c.split, st) : launch_gemm<64, true, false>(b, a, A, c.split, st);
+    if (c.bn == 32) {
+      if (c.split == 4) return launch_gemm<32, true, false, 4>(b, a, A, st);
+      return c.split == 2 ? launch_gemm<32, true, false, 2>(b, a, A, st) : launch_gemm<32, true, false, 1>(b, a, A, st);
+    }
+    if (c.split == 4) return launch_gemm<64, true, false, 4>(b, a, A, st);
+    return c.split == 2 ? launch_gemm<64, true, false, 2>(b, a, A, st) : launch_gemm<64, true, false, 1>(b, a, A, st);
   }
   A.rowsA = (int)rowsA; A.rowsB = (int)rowsB;
   A.mnA = mnA; A.mnB = mnB;
   const Choice c = choose(rowsA, rowsB, A.kblocks, false);
-  if (c.pair) return c.bn == 256 ? launch_gemm<256, false, true>(a, b, A, 1, st) : launch_gemm<128, false, true>(a, b, A, 1, st);
-  if (c.bn == 256) return launch_gemm<256, false, false>(a, b, A, c.split, st);
-  if (c.bn == 128) return launch_gemm<128, false, false>(a, b, A, c.split, st);
-  return launch_gemm<64, false, false>(a, b, A, c.split, st);
+  if (c.pair) return c.bn == 256 ? launch_gemm<256, false, true, 1>(a, b, A, st) : launch_gemm<128, false, true, 1>(a, b, A, st);
+  if (c.bn == 256) return launch_gemm<256, false, false, 1>(a, b, A, st);
+  if (c.bn == 128) return c.split == 2 ? launch_gemm<128, false, false, 2>(a, b, A, st) : launch_gemm<128, false, false, 1>(a, b, A, st);
+  return c.split == 2 ? launch_gemm<64, false, false, 2>(a, b, A, st) : launch_gemm<64, false, false, 1>(a, b, A, st);
 }
 
 int run_jobs(const Jobs& jobs, int n, int act, cudaStream_t st) {
