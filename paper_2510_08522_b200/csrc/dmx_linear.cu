@@ -540,38 +540,29 @@ __device__ __forceinline__ void row_job(const Job& J, float* sh) {
   for (int j = 0; j < NP; ++j) acc[j] = two(0.f);
   if (c < J.cols) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {             // four rows' loads, then four rows' work
-      float2 g[4][NP], u[4][NP];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t r = r0 + 8 * (4 * half + i);
-        if (r >= r1) continue;
-        if constexpr (V == 8) {
-          const uint4 a = __ldcs(reinterpret_cast<const uint4*>(J.in + r * J.ldi + c));
-          g[i][0] = widen2(a.x); g[i][1] = widen2(a.y); g[i][2] = widen2(a.z); g[i][3] = widen2(a.w);
-          if constexpr (ACT != DMX_ACT_NONE) {
-            const uint4 b = __ldcs(reinterpret_cast<const uint4*>(J.z + r * J.ldz + c));
-            u[i][0] = widen2(b.x); u[i][1] = widen2(b.y); u[i][2] = widen2(b.z); u[i][3] = widen2(b.w);
-          }
-        } else {
-          g[i][0] = make_float2(__bfloat162float(J.in[r * J.ldi + c]), 0.f);
-          if constexpr (ACT != DMX_ACT_NONE) u[i][0] = make_float2(__bfloat162float(J.z[r * J.ldz + c]), 0.f);
+    for (int i = 0; i < kChunkRows / 8; ++i) {
+      const int64_t r = r0 + 8 * i;
+      if (r >= r1) continue;
+      float2 g[NP], u[NP];
+      if constexpr (V == 8) {
+        const uint4 a = __ldcs(reinterpret_cast<const uint4*>(J.in + r * J.ldi + c));
+        g[0] = widen2(a.x); g[1] = widen2(a.y); g[2] = widen2(a.z); g[3] = widen2(a.w);
+        if constexpr (ACT != DMX_ACT_NONE) {
+          const uint4 b = __ldcs(reinterpret_cast<const uint4*>(J.z + r * J.ldz + c));
+          u[0] = widen2(b.x); u[1] = widen2(b.y); u[2] = widen2(b.z); u[3] = widen2(b.w);
         }
+      } else {
+        g[0] = make_float2(__bfloat162float(J.in[r * J.ldi + c]), 0.f);
+        if constexpr (ACT != DMX_ACT_NONE) u[0] = make_float2(__bfloat162float(J.z[r * J.ldz + c]), 0.f);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t r = r0 + 8 * (4 * half + i);
-        if (r >= r1) continue;
-#pragma unroll
-        for (int j = 0; j < NP; ++j) {
-          if constexpr (ACT != DMX_ACT_NONE) g[i][j] = dmx_act::times_slope<ACT>(g[i][j], u[i][j]);
-          acc[j] = add2(acc[j], g[i][j]);
-        }
-        if (J.out) {
-          if constexpr (V == 8)
-            *reinterpret_cast<uint4*>(J.out + r * J.ldo + c) = make_uint4(pack2(g[i][0].x, g[i][0].y), pack2(g[i][1].x, g[i][1].y), pack2(g[i][2].x, g[i][2].y), pack2(g[i][3].x, g[i][3].y));
-          else J.out[r * J.ldo + c] = __float2bfloat16_rn(g[i][0].x);
-        }
+      for (int j = 0; j < NP; ++j) {
+        if constexpr (ACT != DMX_ACT_NONE) g[j] = dmx_act::times_slope<ACT>(g[j], u[j]);
+        acc[j] = add2(acc[j], g[j]);
+      }
+      if (J.out) {
+        if constexpr (V == 8) *reinterpret_cast<uint4*>(J.out + r * J.ldo + c) = make_uint4(pack2(g[0].x, g[0].y), pack2(g[1].x, g[1].y), pack2(g[2].x, g[2].y), pack2(g[3].x, g[3].y));
+        else J.out[r * J.ldo + c] = __float2bfloat16_rn(g[0].x);
       }
     }
   }
@@ -591,9 +582,10 @@ __device__ __forceinline__ void row_job(const Job& J, float* sh) {
   }
 }
 
-// ACT: of the first job; the others are copies
+// ACT: of the first job; the others are copies. Six CTAs per SM hide the loads better than more rows in flight per thread:
+// dz of 8192 x 4096 with GELU takes 33 us (6.1 TB/s), with two rows ahead and four CTAs 40 us, four rows and three 49 us.
 template <int ACT>
-__global__ void __launch_bounds__(256) rows_kernel(const __grid_constant__ Jobs all) {
+__global__ void __launch_bounds__(256, 6) rows_kernel(const __grid_constant__ Jobs all) {
   __shared__ __align__(16) float sh[8 * 32 * 8];
   start_dependents();
   wait_for_previous();
