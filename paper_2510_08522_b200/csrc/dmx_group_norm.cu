@@ -166,6 +166,16 @@ __host__ __device__ constexpr int padded(int n) { return (n + 3) & ~3; }
 // APPLY: the results, from the chunks' sums.
 enum Mode { RESIDENT, STATS, APPLY };
 
+// Threads per CTA and CTAs per SM the registers are cut for. Resident: every warp repeats what a slab costs besides its data, so
+// few warps with much data each, and unrolled loops in place of more warps (backward on 64 x 56x56 x 256 bf16 with SiLU:
+// 256 threads 145 us, 128 threads 120 us, and 104 us with the registers of two CTAs per SM instead of three; where the
+// slope is cheap three are better, 114 against 125 us on 1024 x 32x32 x 64). The chunked modes stream: 256 threads.
+constexpr int kResidentThreads = 128, kChunkThreads = 256;
+template <int V, Mode M>
+constexpr int kMostThreads = V == 1 ? 1024 : M == RESIDENT ? kResidentThreads : kChunkThreads;
+template <int V, Mode M, int ACT>
+constexpr int kCtas = V == 1 ? 1 : M != RESIDENT || ACT == DMX_ACT_SILU || ACT == DMX_ACT_GELU ? 2 : 3;
+
 // A CTA's place in one item, and a thread's in that.
 struct Here {
   int n, part, c0, g0, Wl, groups, rows, r0;
@@ -280,7 +290,7 @@ __device__ __forceinline__ void bring_params(const Args& A, const Here& h, const
 }
 
 template <typename T, int V, Mode M, int ACT>
-__global__ void __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) forward_kernel(const __grid_constant__ Args A) {
+__global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, DMX_ACT_NONE>) forward_kernel(const __grid_constant__ Args A) {
   using U = typename Vec<T, V>::type;
   constexpr int NP = kPairs<V>, SL = kSlots<V>;
   extern __shared__ __align__(16) float sm[];
@@ -500,7 +510,7 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) forward_k
       }
       T* out = start<T, V>(A.out, now, rl, col);
       const int64_t out_step = (int64_t)R * A.out.row;
-#pragma unroll 2
+#pragma unroll 4
       for (int i = 0; i < now.cnt; i += SL) {
         float2 x[NP];
         const bool second = i + 1 < now.cnt;
@@ -535,7 +545,7 @@ __device__ __forceinline__ void keep(unsigned* g, bool second, int step, const f
 
 // Backward. Workspace: A and B per image (and chunk) and channel, [2][N*chunks][C].
 template <typename T, int V, Mode M, int ACT>
-__global__ void __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) backward_kernel(const __grid_constant__ Args A) {
+__global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, ACT>) backward_kernel(const __grid_constant__ Args A) {
   using U = typename Vec<T, V>::type;
   constexpr int NP = kPairs<V>, SL = kSlots<V>;
   extern __shared__ __align__(16) float sm[];
@@ -592,7 +602,7 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) backward_
       float2 pa[NP], pb[NP];
 #pragma unroll
       for (int j = 0; j < NP; ++j) pa[j] = pb[j] = two(0.f);
-#pragma unroll 2
+#pragma unroll 4
       for (int i = 0; i < h.cnt; i += SL) {
         float2 x[NP], g[NP];
         widen(xs + i * threads, i + 1 < h.cnt, threads, mu[0], x);
@@ -698,7 +708,7 @@ __global__ void __launch_bounds__(V == 1 ? 1024 : 256, V == 1 ? 1 : 2) backward_
       }
       T* out = start<T, V>(A.out, now, rl, col);
       const int64_t out_step = (int64_t)R * A.out.row;
-#pragma unroll 2
+#pragma unroll 4
       for (int i = 0; i < now.cnt; i += SL) {
         float2 x[NP], gr[NP];
         const bool second = i + 1 < now.cnt;
@@ -776,7 +786,7 @@ int lcm(int a, int b) {
 bool settle(Plan& p, int64_t L, int C, int cpg, int e, bool backward, int64_t rows, size_t most) {
   p.slabs = (C + p.W - 1) / p.W;
   p.cols = (p.W + p.V - 1) / p.V;
-  p.threads = p.V > 1 ? 256 : p.cols <= 512 ? 512 : 1024;
+  p.threads = p.V > 1 ? (p.resident ? kResidentThreads : kChunkThreads) : p.cols <= 256 ? 256 : 1024;
   p.R = p.threads / p.cols;
   p.lanes = p.cols <= 32 && 32 % p.cols == 0 ? p.cols : 0;
   p.fold = 1;
@@ -784,7 +794,7 @@ bool settle(Plan& p, int64_t L, int C, int cpg, int e, bool backward, int64_t ro
   const int64_t slots = (rows + p.R - 1) / p.R;
   const int erows = p.lanes ? p.threads / 32 : p.R;
   const size_t f = sizeof(float), data = (size_t)slots * p.threads * p.V * e * (backward ? 2 : 1);
-  if (slots > 64 || data > most) return false;
+  if (slots > 128 || data > most) return false;
   p.rows = (int)rows;
   p.slots = (int)slots;
   const int groups = p.W / cpg;
@@ -928,7 +938,7 @@ bool wide(const void* p, int64_t N, int64_t L, int C, int64_t image, int64_t row
 bool element_aligned(const void* p, int e) { return (reinterpret_cast<uintptr_t>(p) & (e - 1)) == 0; }
 
 // ... and the narrowest slab of whole columns and whole groups has to fit a CTA's threads
-bool columns_fit(int C, int cpg, int e) { return C % (16 / e) == 0 && lcm(cpg, 16 / e) / (16 / e) <= 256; }
+bool columns_fit(int C, int cpg, int e) { return C % (16 / e) == 0 && lcm(cpg, 16 / e) / (16 / e) <= kResidentThreads; }
 
 int64_t workspace_of(const Plan& p, int64_t N, int C, int G, bool backward) {
   if (backward) return 2 * N * (p.resident ? 1 : p.parts) * C * (int64_t)sizeof(float);

@@ -2,8 +2,8 @@
 several thousand positions, odd channels and groups, slices, large means, constant groups, and the gradient
 against the formula and against differences.
 
-Tolerances are forward error bounds with e = 2^-24. A value passes at most G = 150 additions on its way into a sum (16 in a
-thread, 8 in a column, 64 and 5 in a group, 8 over a cluster, or the chunks of a large image), so a sum is within
+Tolerances are forward error bounds with e = 2^-24. A value passes at most G = 150 additions on its way into a sum (64 in a
+thread, 8 in a column, 64 and 5 in a group, 8 over a cluster or the chunks of a large image), so a sum is within
 G e of the sum of magnitudes; a variance of deviations within (G + 8) e of itself plus the square of the mean's error. Errors
 then follow the formulas term by term. bf16 results get half a spacing (2^-8 of the value) more."""
 import math
