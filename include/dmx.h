@@ -500,7 +500,8 @@ int dmx_adamw_destroy(dmx_adamw* h);   /* as dmx_destroy */
  * All arithmetic and all sums are fp32 (variances from deviations of the mean, never from a difference of
  * squares); y and dx are rounded once. Group norm's statistics do not depend on the batch size, which is why
  * it is the norm to use where a controller changes that.
- *   x, y, dy, dx       element (n, l, c) at n*image + l*row + c, strides in elements, row >= C unless L <= 1;
+ *   x, y, dy, dx       element (n, l, c) at n*image + l*row + c, strides in elements >= 0, of y and dx also row >= C
+ *                      unless L <= 1 (x and dy may repeat rows or images with strides 0: a broadcast gradient);
  *                      any alignment of the element type (16-byte aligned starts and strides are faster)
  *   weight, bias       fp32, C entries, or NULL for ones and zeros
  *   mean, rstd         fp32, N*G (written by forward, read by backward)
@@ -531,9 +532,9 @@ int dmx_group_norm_backward(int64_t N, int64_t L, int C, int G, int dtype, const
  *   backward   dz = dy * act'(z),  dx = dz W,  dW = dz^T x,  dbias = column sums of dz   (the residual's gradient is dy)
  * Everything up to a store is fp32, with one exception: with an activation, dz is rounded to bf16 before the two
  * products of backward (the tensor cores take 16-bit operands); dbias is summed from the unrounded dz.
- *   x, w, bias, residual, z, y, dy, dx, dw, dbias   bf16, row-major, ld* = elements from row to row (>= the row's
- *              length unless there is one row); element alignment suffices. Operands whose start or rows are not
- *              16-byte aligned are first laid out in the workspace.
+ *   x, w, bias, residual, z, y, dy, dx, dw, dbias   bf16, row-major, ld* = elements from row to row (>= 0; of outputs
+ *              >= the row's length unless there is one row; inputs may repeat rows with 0); element alignment suffices. Operands whose start or rows are not
+ *              16-byte aligned, or repeat, are first laid out in the workspace.
  *   bias, residual, z (forward: an output, written only if given)   may be NULL
  *   z          backward: forward's z, needed unless act is DMX_ACT_NONE
  *   dx, dw, dbias   each may be NULL and is then not computed

@@ -656,12 +656,12 @@ bool aligned(const void* p, unsigned a) { return (reinterpret_cast<uintptr_t>(p)
 int64_t pad8(int64_t n) { return (n + 7) & ~(int64_t)7; }
 int64_t pad256(int64_t n) { return (n + 255) & ~(int64_t)255; }
 
-// A matrix as TMA takes it: 16-byte aligned, rows a multiple of 16 bytes apart
+// A matrix; TMA takes it if it is 16-byte aligned, its rows a multiple of 16 bytes apart and none repeated
 struct Matrix {
   const bf16* p;
   int64_t rows, cols, ld;
 };
-bool tma_ready(const Matrix& m) { return aligned(m.p, 16) && (m.rows <= 1 || m.ld % 8 == 0); }
+bool tma_ready(const Matrix& m) { return aligned(m.p, 16) && (m.rows <= 1 || (m.ld % 8 == 0 && m.ld >= m.cols)); }
 int64_t laid_out_bytes(const Matrix& m) { return tma_ready(m) ? 0 : pad256(m.rows * pad8(m.cols) * 2); }
 
 // rows of m are D's rows (or columns) if !mn, its columns if mn
@@ -819,7 +819,9 @@ bool extents_ok(int64_t M, int64_t N, int64_t K) {
   const int64_t most = DMX_LINEAR_MAX_EXTENT;
   return M >= 0 && N >= 0 && K >= 0 && M <= most && N <= most && K <= most;
 }
-bool ld_ok(int64_t rows, int64_t cols, int64_t ld) { return rows <= 1 || ld >= cols; }
+// what is only read may repeat rows (0) or overlap them; what is written may not
+bool in_ok(int64_t rows, int64_t ld) { return rows <= 1 || ld >= 0; }
+bool out_ok(int64_t rows, int64_t cols, int64_t ld) { return rows <= 1 || ld >= cols; }
 
 struct BackPlan {
   bool needs_dz;            // dz is written to the workspace
@@ -850,7 +852,7 @@ int dmx_linear_forward(int64_t M, int64_t N, int64_t K, const void* x, int64_t l
                        int act, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z, int64_t ldz, void* workspace,
                        int64_t workspace_bytes, void* cuda_stream) {
   if (!extents_ok(M, N, K) || act < DMX_ACT_NONE || act > DMX_ACT_GELU) return DMX_ERR_ARG;
-  if (!ld_ok(M, K, ldx) || !ld_ok(N, K, ldw) || !ld_ok(M, N, ldy) || (residual && !ld_ok(M, N, ldr)) || (z && !ld_ok(M, N, ldz))) return DMX_ERR_ARG;
+  if (!in_ok(M, ldx) || !in_ok(N, ldw) || !out_ok(M, N, ldy) || (residual && !in_ok(M, ldr)) || (z && !out_ok(M, N, ldz))) return DMX_ERR_ARG;
   if (M == 0 || N == 0) return DMX_OK;
   if (!y || (K > 0 && (!x || !w))) return DMX_ERR_ARG;
   if (!aligned(x, 2) || !aligned(w, 2) || !aligned(bias, 2) || !aligned(residual, 2) || !aligned(y, 2) || !aligned(z, 2) || !aligned(workspace, 256)) return DMX_ERR_ALIGN;
@@ -887,7 +889,7 @@ int dmx_linear_backward(int64_t M, int64_t N, int64_t K, const void* dy, int64_t
                         const void* z, int64_t ldz, int act, void* dx, int64_t lddx, void* dw, int64_t lddw, void* dbias, void* workspace,
                         int64_t workspace_bytes, void* cuda_stream) {
   if (!extents_ok(M, N, K) || act < DMX_ACT_NONE || act > DMX_ACT_GELU) return DMX_ERR_ARG;
-  if (!ld_ok(M, N, lddy) || !ld_ok(M, K, ldx) || !ld_ok(N, K, ldw) || (z && !ld_ok(M, N, ldz)) || (dx && !ld_ok(M, K, lddx)) || (dw && !ld_ok(N, K, lddw))) return DMX_ERR_ARG;
+  if (!in_ok(M, lddy) || !in_ok(M, ldx) || !in_ok(N, ldw) || (z && !in_ok(M, ldz)) || (dx && !out_ok(M, K, lddx)) || (dw && !out_ok(N, K, lddw))) return DMX_ERR_ARG;
   if (!aligned(dy, 2) || !aligned(x, 2) || !aligned(w, 2) || !aligned(z, 2) || !aligned(dx, 2) || !aligned(dw, 2) || !aligned(dbias, 2) || !aligned(workspace, 256)) return DMX_ERR_ALIGN;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   if (M == 0 || N == 0) {          // empty sums

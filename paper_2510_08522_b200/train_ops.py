@@ -302,7 +302,7 @@ def linear(x, weight, bias=None, act="none", residual=None, save=False, out=None
     L = B.lib()
     xp, wp = x.data_ptr(), weight.data_ptr()
     with _on(x):
-        if (xp | wp | 2 * ldx | 2 * ldw) & 15:           # an operand has to be laid out (or is one row)
+        if (xp | wp | 2 * ldx | 2 * ldw) & 15 or ldx < K or ldw < K:           # an operand has to be laid out (or is one row)
             ws = _workspace(L.dmx_linear_workspace(M, N, K, xp, ldx, wp, ldw), x, "linear")
         else:
             ws = None

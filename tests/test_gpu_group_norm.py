@@ -205,6 +205,19 @@ def test_image_tensors_and_transposed_batches():
     assert all(torch.equal(p, q) for p, q in zip(back, D.group_norm_backward(dy, t, got[1], got[2], 6, w, b, "silu")))
 
 
+def test_broadcast_inputs():
+    torch, D = _d()
+    x, dy, w, b = make(4, 60, 32, torch.bfloat16)
+    _, mean, rstd = D.group_norm(x, 4, w, b, act="silu")
+    for one in (dy[:, :1], dy[:1]):
+        wide = one.expand(4, 60, 32)
+        a = D.group_norm_backward(wide, x, mean, rstd, 4, w, b, "silu")
+        c = D.group_norm_backward(wide.contiguous(), x, mean, rstd, 4, w, b, "silu")
+        assert all(torch.equal(p, q) for p, q in zip(a, c))
+    r = x[:1].expand(4, 60, 32)
+    assert all(torch.equal(p, q) for p, q in zip(D.group_norm(r, 4, w, b), D.group_norm(r.contiguous(), 4, w, b)))
+
+
 def test_against_differences():
     torch, D = _d()
     x, dy, w, b = make(2, 11, 12, torch.float32, seed=8)

@@ -189,6 +189,20 @@ def test_nan_and_infinity_stay_in_their_rows():
         assert torch.isnan(y[7]).all() and not torch.isfinite(y[11]).any() and torch.equal(y[rows], clean[rows])
 
 
+def test_broadcast_inputs():
+    torch, D = _d()
+    g = torch.Generator(device="cuda").manual_seed(7)
+    for M in (40, 200):
+        x, w, r, dy = mat(g, 1, 64).expand(M, 64), mat(g, 72, 64), mat(g, 1, 72).expand(M, 72), mat(g, 1, 72).expand(M, 72)
+        y, z = D.linear(x, w, act="gelu", residual=r, save=True)
+        same = D.linear(x.contiguous(), w, act="gelu", residual=r.contiguous(), save=True)
+        assert torch.equal(y, same[0]) and torch.equal(z, same[1])
+        a, b = D.linear_backward(dy, x, w, z, act="gelu"), D.linear_backward(dy.contiguous(), x.contiguous(), w, z, act="gelu")
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
+        a, b = D.linear_backward(dy, x, w), D.linear_backward(dy.contiguous(), x.contiguous(), w)
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
 def test_other_stream_and_graph():
     torch, D = _d()
     g = torch.Generator(device="cuda").manual_seed(6)
@@ -213,7 +227,7 @@ def test_refusals():
     e = lambda *s: torch.ones(*s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
     for f in (lambda: D.linear(e(4, 8).float(), e(16, 8)), lambda: D.linear(e(4, 8), e(16, 9)), lambda: D.linear(e(4, 8), e(16, 8), e(15)),
               lambda: D.linear(e(4, 8), e(16, 8), act="tanh"), lambda: D.linear(e(4, 8), e(16, 8), residual=e(4, 15)), lambda: D.linear(e(8, 4).t(), e(16, 8)),
-              lambda: D.linear(e(4, 8).cpu(), e(16, 8)), lambda: D.linear(e(1, 8).expand(4, 8), e(16, 8)), lambda: D.linear_backward(e(4, 16), e(4, 8), e(16, 8), act="relu"),
+              lambda: D.linear(e(4, 8).cpu(), e(16, 8)), lambda: D.linear(e(4, 8), e(16, 8), out=e(1, 16).expand(4, 16)), lambda: D.linear_backward(e(4, 16), e(4, 8), e(16, 8), act="relu"),
               lambda: D.linear_backward(e(4, 15), e(4, 8), e(16, 8)), lambda: D.linear(e(8), e(16, 8))):
         with pytest.raises(D.DmxError):
             f()
