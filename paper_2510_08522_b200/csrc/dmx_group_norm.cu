@@ -811,9 +811,10 @@ constexpr int64_t kChunkData = 64 * 1024;    // chunks of a larger image: three
 
 // Slab width, CTAs per image and slab, and positions per thread. Slabs are multiples of whole groups and of
 // whole columns. Of the splits that keep an image's slab in one cluster's shared memory, the one of least
-// cost: a cluster of more CTAs waits longer for its slowest (backward on 64 x 56x56 x 256 bf16: segments of 32 bytes
-// and four CTAs 145 us, 64 bytes and eight 149 us; forward 61 and 71 us). Where the problem is too small to give
-// every SM two CTAs, more CTAs count more than that (backward on 37 x 27x27 x 90 fp32: 17 us against 35).
+// cost: a cluster of more CTAs waits longer for its slowest, and rows of 32 bytes (a DRAM sector) take L1 twice the
+// lines that 64 do. Measured, bf16 backward: 64 x 56x56 x 256 with 32 bytes and two CTAs 104 us, 64 bytes and four 112 us; 1024 x
+// 32x32 x 64 with 32 bytes and one CTA 114 us, 64 bytes and two 107 us. Where the problem is too small to give every
+// SM two CTAs, more CTAs count more than that (37 x 27x27 x 90 fp32, single elements: 17 us against 34).
 Plan plan(int64_t N, int64_t L, int C, int cpg, int dtype, bool vec, bool backward) {
   Plan p, best;
   const int e = dtype == DMX_F32 ? 4 : 2;
@@ -830,7 +831,8 @@ Plan plan(int64_t N, int64_t L, int C, int cpg, int dtype, bool vec, bool backwa
     for (p.parts = 1; p.parts <= kMaxCluster; p.parts *= 2) {
       if (!settle(p, L, C, cpg, e, backward, (L + p.parts - 1) / p.parts, kMostData)) continue;
       if (p.parts > 1 && p.rows < p.R) break;
-      float cost = p.parts == 1 ? 1.f : p.parts == 2 ? 1.3f : p.parts == 4 ? 1.6f : 2.f;
+      float cost = p.parts == 1 ? 1.f : p.parts == 2 ? 1.2f : p.parts == 4 ? 1.55f : 2.f;
+      if (p.V > 1 && p.W * e < 64) cost *= 1.25f;
       const float ctas = (float)N * p.slabs * p.parts;
       if (ctas < 2 * 148) cost *= 2 * 148 / ctas;
       if (!best.resident || cost < least) { best = p; least = cost; }
