@@ -12,7 +12,7 @@
 // a cluster share an image's slab and exchange their sums through distributed shared memory. The CTAs stay and
 // take slab after slab; a slot is refilled for the next slab as soon as its result is out, so loads run while
 // sums are exchanged and results stored. One read, one write. An image too large for that is cut into chunks:
-// one launch for the chunks' sums, one that reads again, mostly from L2.
+// one launch for the chunks' sums, a small one that joins them, one that reads again, mostly from L2.
 // Variances: a thread sums deviations from its own first value, s = sum d, q = sum d^2, and takes q - s^2/n. That
 // cancels only if the first value is far off, and then the group's variance contains that distance itself:
 // the error stays within n (at most 40 or so) roundings of the result. From there on deviations of means are added
@@ -289,6 +289,18 @@ __device__ __forceinline__ void bring_params(const Args& A, const Here& h, const
     }
 }
 
+// Over `lanes` lanes: parts with mean times positions ps, squared deviations pm and `have` positions of cpg values
+// each -> the mean and variance of all L positions.
+__device__ __forceinline__ float2 join(float ps, float pm, float have, float cpg, float L, int lanes) {
+  float mean = ps;
+  for (int o = lanes >> 1; o > 0; o >>= 1) mean += __shfl_xor_sync(0xffffffffu, mean, o);
+  mean /= L;
+  const float d = have > 0.f ? ps / have - mean : 0.f;
+  float m2 = have > 0.f ? fmaf(have * cpg * d, d, pm) : 0.f;
+  for (int o = lanes >> 1; o > 0; o >>= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
+  return make_float2(mean, m2 / (L * cpg));
+}
+
 template <typename T, int V, Mode M, int ACT>
 __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, DMX_ACT_NONE>) forward_kernel(const __grid_constant__ Args A) {
   using U = typename Vec<T, V>::type;
@@ -324,7 +336,7 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, DMX_ACT_NONE>)
   {
     const T* p = start<T, V>(A.x, h, rl, col);
     for (int i = 0; i < h.cnt; ++i) bring(slot + i * threads, p + (int64_t)i * R * A.x.row);
-    if (M != STATS) bring_params<false>(A, h, params_at(par, W, A.gW));
+    if (M != STATS) bring_params<M == APPLY>(A, h, params_at(par, W, A.gW));
   }
   if (M == RESIDENT && A.parts > 1) cluster_sync();      // all of the cluster runs: its memory may be written
   for (int64_t item = first; item < A.items; item += stride) {
@@ -448,7 +460,7 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, DMX_ACT_NONE>)
       h = place<V, M>(A, next, rl, col);
       np = start<T, V>(A.x, h, rl, col);
       ncnt = h.cnt;
-      if (M != STATS) bring_params<false>(A, h, params_at(par + (turn ^ 1) * params_size(W, A.gW), W, A.gW));
+      if (M != STATS) bring_params<M == APPLY>(A, h, params_at(par + (turn ^ 1) * params_size(W, A.gW), W, A.gW));
     }
     turn ^= 1;
     if constexpr (M != APPLY) {
@@ -456,40 +468,27 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, DMX_ACT_NONE>)
       else __syncthreads();
     }
     if constexpr (M != STATS) {
-      // join the parts of each group: a lane per part (or per 32nd part), added in a fixed order
-      const int kl = A.parts >= 32 ? 32 : lanes_for(A.parts), k0 = tid & (kl - 1);
-      const int64_t gat = (int64_t)now.n * A.G + now.g0;
-      for (int gb = 0; gb < now.groups; gb += threads / kl) {
-        const int g = gb + tid / kl;
-        const float2* src = reinterpret_cast<const float2*>(A.part) + (int64_t)now.n * A.parts * A.G + now.g0 + g;
-        float ps = 0.f, pm = 0.f, sum = 0.f, m2 = 0.f;
-        if (M == RESIDENT && g < now.groups && k0 < A.parts) {
-          sum = ps = mine[2 * k0 * pG + g];
-          pm = mine[(2 * k0 + 1) * pG + g];
-        }
-        if (M == APPLY && g < now.groups)
-          for (int k = k0; k < A.parts; k += kl) sum += __ldg(&src[(int64_t)k * A.G]).x;
-        for (int o = kl >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        const float mean = sum / (float)A.L;
-        for (int k = k0; k < A.parts && g < now.groups; k += kl) {
-          if (M == APPLY) {
-            const float2 t = __ldg(&src[(int64_t)k * A.G]);
-            ps = t.x; pm = t.y;
+      if constexpr (M == RESIDENT) {
+        // join the parts of each group: a lane per part, added in a fixed order
+        const int kl = lanes_for(A.parts), k0 = tid & (kl - 1);
+        const int64_t gat = (int64_t)now.n * A.G + now.g0;
+        for (int gb = 0; gb < now.groups; gb += threads / kl) {
+          const int g = gb + tid / kl;
+          const float have = (float)(min((int64_t)(k0 + 1) * A.rows, (int64_t)A.L) - min((int64_t)k0 * A.rows, (int64_t)A.L));
+          float ps = 0.f, pm = 0.f;
+          if (g < now.groups) {
+            ps = mine[2 * k0 * pG + g];
+            pm = mine[(2 * k0 + 1) * pG + g];
           }
-          const float have = (float)(min((int64_t)(k + 1) * A.rows, (int64_t)A.L) - min((int64_t)k * A.rows, (int64_t)A.L));
-          if (have > 0.f) {
-            const float d = ps / have - mean;
-            m2 += fmaf(have * (float)cpg * d, d, pm);
-          }
-        }
-        for (int o = kl >> 1; o > 0; o >>= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
-        if (g < now.groups && k0 == 0) {
-          const float rstd = 1.f / sqrtf(m2 / ((float)A.L * (float)cpg) + A.eps);
-          gmean[g] = mean;
-          grstd[g] = rstd;
-          if (now.part == 0) {
-            A.mean[gat + g] = mean;
-            A.rstd[gat + g] = rstd;
+          float2 t = join(ps, pm, have, (float)cpg, (float)A.L, kl);
+          if (g < now.groups && k0 == 0) {
+            t.y = 1.f / sqrtf(t.y + A.eps);
+            gmean[g] = t.x;
+            grstd[g] = t.y;
+            if (now.part == 0) {
+              A.mean[gat + g] = t.x;
+              A.rstd[gat + g] = t.y;
+            }
           }
         }
       }
@@ -501,8 +500,8 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, DMX_ACT_NONE>)
     if constexpr (M != STATS) {
       float2 mu[NP], a[NP], b[NP];
       if (now.on) {
-        groups_of<V>(gmean, grp0, rem0, cpg, A.fold == V, mu);
-        groups_of<V>(grstd, grp0, rem0, cpg, A.fold == V, a);
+        groups_of<V>(M == APPLY ? P.mean : gmean, grp0, rem0, cpg, A.fold == V, mu);
+        groups_of<V>(M == APPLY ? P.rstd : grstd, grp0, rem0, cpg, A.fold == V, a);
         channels(P.w + col * V, b);
 #pragma unroll
         for (int j = 0; j < NP; ++j) a[j] = mul2(a[j], b[j]);
@@ -663,16 +662,10 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, ACT>) backward
       if (M == RESIDENT && A.parts > 1) cluster_wait();
       else __syncthreads();
     }
-    if constexpr (M == APPLY) {      // the chunks' sums, in their order
+    if constexpr (M == APPLY) {      // the image's sums
       for (int c = tid; c < 2 * W; c += threads) {
         const int k = c < W ? c : c - W;
-        float t = 0.f;
-        const float* src = A.part + (c < W ? 0 : plane) + (int64_t)now.n * A.parts * A.C + now.c0 + k;
-        if (k < now.Wl) {
-#pragma unroll 8
-          for (int p = 0; p < A.parts; ++p) t += __ldg(src + (int64_t)p * A.C);
-        }
-        mine[(c < W ? 0 : pW) + k] = t;
+        if (k < now.Wl) mine[(c < W ? 0 : pW) + k] = __ldg(A.part + 2 * plane + ((c < W ? 0 : (int64_t)A.N) + now.n) * A.C + now.c0 + k);
       }
       __syncthreads();
     }
@@ -739,9 +732,56 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, ACT>) backward
   }
 }
 
-// dweight and dbias: sums of the images' (and chunks') rows, those of A times their group's rstd. 32 channels and
-// 32 row lanes per CTA. Launched as a programmatic dependent of the backward kernel.
-__global__ void __launch_bounds__(1024) columns_kernel(const float* __restrict__ part, int64_t rows, int per_image, int C, int G, int cpg,
+// The chunks' sums of an image, joined between the two launches that read it. Forward: a warp per image and group.
+__global__ void __launch_bounds__(256) join_groups_kernel(const float2* __restrict__ part, int64_t groups, int parts, int rows, int L, int G, int cpg,
+                                                          float eps, float* __restrict__ mean, float* __restrict__ rstd) {
+  asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
+  const int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);       // image * G + group
+  const int lane = threadIdx.x & 31;
+  if (i >= groups) return;
+  const float2* src = part + i / G * parts * G + i % G;
+  // 32nd parts by lane: each lane joins its own first
+  float sum = 0.f, have = 0.f;
+  for (int k = lane; k < parts; k += 32) {
+    sum += __ldg(&src[(int64_t)k * G]).x;
+    have += (float)(min((int64_t)(k + 1) * rows, (int64_t)L) - (int64_t)k * rows);
+  }
+  const float mu = have > 0.f ? sum / have : 0.f;
+  float m2 = 0.f;
+  for (int k = lane; k < parts; k += 32) {
+    const float2 t = __ldg(&src[(int64_t)k * G]);
+    const float n = (float)(min((int64_t)(k + 1) * rows, (int64_t)L) - (int64_t)k * rows), d = t.x / n - mu;
+    m2 += fmaf(n * (float)cpg * d, d, t.y);
+  }
+  const float2 t = join(sum, m2, have, (float)cpg, (float)L, 32);
+  if (lane == 0) {
+    mean[i] = t.x;
+    rstd[i] = 1.f / sqrtf(t.y + eps);
+  }
+}
+// Backward: the rows of an image's chunks to one row, for A and for B. 32 channels and eight row lanes per CTA.
+__global__ void __launch_bounds__(256) join_rows_kernel(const float* __restrict__ part, float* __restrict__ out, int N, int parts, int C) {
+  __shared__ float sh[8][33];
+  asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
+  const int lane = threadIdx.x & 31, r = threadIdx.x >> 5, blocks = (C + 31) / 32;
+  const int64_t row = blockIdx.x / blocks;                               // [2][N]
+  const int c = (blockIdx.x % blocks) * 32 + lane;
+  float s = 0.f;
+  if (c < C) {
+    const float* p = part + row * parts * C + c;
+#pragma unroll 8
+    for (int i = r; i < parts; i += 8) s += __ldg(p + (int64_t)i * C);
+  }
+  sh[r][lane] = s;
+  __syncthreads();
+  if (r == 0 && c < C) {
+    for (int k = 1; k < 8; ++k) s += sh[k][lane];
+    out[row * C + c] = s;
+  }
+}
+
+// dweight and dbias: sums of the images' rows, those of A times their group's rstd. 32 channels and 32 row lanes per CTA.
+__global__ void __launch_bounds__(1024) columns_kernel(const float* __restrict__ part, int64_t rows, int C, int G, int cpg,
                                                       const float* __restrict__ rstd, float* __restrict__ dw, float* __restrict__ db) {
   __shared__ float sh[32][33];
   const int lane = threadIdx.x & 31, r = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
@@ -757,7 +797,7 @@ __global__ void __launch_bounds__(1024) columns_kernel(const float* __restrict__
       for (int64_t i = r; i < rows; i += 32) s += __ldg(p + i * C + c);
     } else {
 #pragma unroll 8
-      for (int64_t i = r; i < rows; i += 32) s = fmaf(__ldg(p + i * C + c), __ldg(q + (int64_t)((unsigned)i / (unsigned)per_image) * G), s);
+      for (int64_t i = r; i < rows; i += 32) s = fmaf(__ldg(p + i * C + c), __ldg(q + i * G), s);
     }
   }
   sh[r][lane] = s;
@@ -888,15 +928,35 @@ int launch(K kernel, const Plan& p, const Args& A, bool cluster, cudaStream_t st
   return dmxh::cuda_ok(cudaLaunchKernelEx(&cfg, kernel, A)) ? DMX_OK : DMX_ERR_CUDA;
 }
 
+template <typename... P, typename... V>
+int start(int64_t ctas, int rows, int threads, cudaStream_t st, void (*kernel)(P...), V... args) {     // a dependent of the launch before
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)ctas, rows);
+  cfg.blockDim = dim3(threads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return dmxh::cuda_ok(cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...)) ? DMX_OK : DMX_ERR_CUDA;
+}
+
 template <typename T, int V, int ACT>
 int run_act(bool backward, const Plan& p, const Args& A, cudaStream_t st) {
   if (backward) {
     if (p.resident) return launch(backward_kernel<T, V, RESIDENT, ACT>, p, A, true, st);
-    const int rc = launch(backward_kernel<T, V, STATS, ACT>, p, A, false, st);
+    int rc = launch(backward_kernel<T, V, STATS, ACT>, p, A, false, st);
+    if (rc != DMX_OK) return rc;
+    rc = start((int64_t)2 * A.N * ((A.C + 31) / 32), 1, 256, st, join_rows_kernel, A.part, A.part + 2 * (int64_t)A.N * A.parts * A.C, A.N, A.parts, A.C);
     return rc != DMX_OK ? rc : launch(backward_kernel<T, V, APPLY, ACT>, p, A, false, st);
   }
   if (p.resident) return launch(forward_kernel<T, V, RESIDENT, ACT>, p, A, true, st);
-  const int rc = launch(forward_kernel<T, V, STATS, DMX_ACT_NONE>, p, A, false, st);
+  int rc = launch(forward_kernel<T, V, STATS, DMX_ACT_NONE>, p, A, false, st);
+  if (rc != DMX_OK) return rc;
+  const int64_t groups = (int64_t)A.N * A.G;
+  rc = start((groups + 7) / 8, 1, 256, st, join_groups_kernel, reinterpret_cast<const float2*>(A.part), groups, A.parts, A.rows, A.L, A.G, A.cpg, A.eps,
+             A.mean, A.rstd);
   return rc != DMX_OK ? rc : launch(forward_kernel<T, V, APPLY, ACT>, p, A, false, st);
 }
 
@@ -942,7 +1002,7 @@ bool element_aligned(const void* p, int e) { return (reinterpret_cast<uintptr_t>
 bool columns_fit(int C, int cpg, int e) { return C % (16 / e) == 0 && lcm(cpg, 16 / e) / (16 / e) <= kResidentThreads; }
 
 int64_t workspace_of(const Plan& p, int64_t N, int C, int G, bool backward) {
-  if (backward) return 2 * N * (p.resident ? 1 : p.parts) * C * (int64_t)sizeof(float);
+  if (backward) return 2 * N * (p.resident ? 1 : p.parts + 1) * C * (int64_t)sizeof(float);
   return p.resident ? 0 : N * p.parts * G * (int64_t)sizeof(float2);
 }
 
@@ -975,7 +1035,7 @@ int dmx_group_norm_forward(int64_t N, int64_t L, int C, int G, int dtype, const 
   const Plan p = plan(N, L, C, C / G, dtype, vec, false);
   const int64_t need = workspace_of(p, N, C, G, false);
   if (workspace_bytes < need || (need > 0 && !workspace)) return DMX_ERR_ARG;
-  if (N * p.slabs * (int64_t)p.parts > 0x7fffffff) return DMX_ERR_ARG;
+  if (N * p.slabs * (int64_t)p.parts > 0x7fffffff || 2 * N * ((C + 31) / 32) > 0x7fffffff) return DMX_ERR_ARG;
   Args A = {};
   A.x = {const_cast<void*>(x), x_image, x_row};
   A.out = {y, y_image, y_row};
@@ -1007,7 +1067,7 @@ int dmx_group_norm_backward(int64_t N, int64_t L, int C, int G, int dtype, const
   const bool vec = columns_fit(C, C / G, e) && wide(x, N, L, C, x_image, x_row, e) && wide(dy, N, L, C, dy_image, dy_row, e) && wide(dx, N, L, C, dx_image, dx_row, e);
   const Plan p = plan(N, L, C, C / G, dtype, vec, true);
   if (workspace_bytes < workspace_of(p, N, C, G, true) || !workspace) return DMX_ERR_ARG;
-  if (N * p.slabs * (int64_t)p.parts > 0x7fffffff) return DMX_ERR_ARG;
+  if (N * p.slabs * (int64_t)p.parts > 0x7fffffff || 2 * N * ((C + 31) / 32) > 0x7fffffff) return DMX_ERR_ARG;
   Args A = {};
   A.x = {const_cast<void*>(x), x_image, x_row};
   A.dy = {const_cast<void*>(dy), dy_image, dy_row};
@@ -1016,18 +1076,7 @@ int dmx_group_norm_backward(int64_t N, int64_t L, int C, int G, int dtype, const
   fill(A, p, N, L, C, G);
   const int rc = run(true, act, dtype, vec, p, A, st);
   if (rc != DMX_OK || (!dweight && !dbias)) return rc;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((C + 31) / 32, 2);
-  cfg.blockDim = dim3(1024);
-  cfg.stream = st;
-  cudaLaunchAttribute attr[1] = {};
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  const int64_t rows = N * (p.resident ? 1 : p.parts);
-  return dmxh::cuda_ok(cudaLaunchKernelEx(&cfg, columns_kernel, (const float*)A.part, rows, p.resident ? 1 : p.parts, C, G, C / G, rstd, dweight, dbias))
-             ? DMX_OK : DMX_ERR_CUDA;
+  return start((C + 31) / 32, 2, 1024, st, columns_kernel, A.part + (p.resident ? 0 : 2 * N * p.parts * C), N, C, G, C / G, rstd, dweight, dbias);
 }
 
 }  // extern "C"
