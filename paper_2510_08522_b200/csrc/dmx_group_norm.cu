@@ -444,9 +444,12 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, DMX_ACT_NONE>)
           if (mineg)
             for (int k = Q.l; k < 2 * A.parts; k += Q.each)
               send(mine + (2 * h.part + (k & 1)) * pG + g, k >> 1, k & 1 ? m2 : mean * (float)h.rows);
-        } else if (mineg && Q.l == 0) {
-          mine[g] = mean * (float)h.rows;
-          mine[pG + g] = m2;
+        } else if (mineg && Q.l == 0) {              // nothing to join
+          const float rstd = 1.f / sqrtf(m2 * icnt + A.eps);
+          gmean[g] = mean;
+          grstd[g] = rstd;
+          A.mean[(int64_t)h.n * A.G + h.g0 + g] = mean;
+          A.rstd[(int64_t)h.n * A.G + h.g0 + g] = rstd;
         }
       }
       if (M == RESIDENT && A.parts > 1) cluster_arrive();
@@ -467,7 +470,7 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, DMX_ACT_NONE>)
       if (M == RESIDENT && A.parts > 1) cluster_wait();
       else __syncthreads();
     }
-    if constexpr (M != STATS) {
+    if (M == APPLY || (M == RESIDENT && A.parts > 1)) {
       if constexpr (M == RESIDENT) {
         // join the parts of each group: a lane per part, added in a fixed order
         const int kl = lanes_for(A.parts), k0 = tid & (kl - 1);
@@ -682,6 +685,7 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, ACT>) backward
           grp[pG + g] = tb * n * r;
         }
       }
+      __syncthreads();
       if (M == RESIDENT && now.part == 0)          // what dweight and dbias are summed from
         for (int c = tid; c < 2 * W; c += threads) {
           const int k = c < W ? c : c - W;
@@ -689,7 +693,6 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, ACT>) backward
           for (int q = 0; q < gparts; ++q) t += mine[(2 * q + (c < W ? 0 : 1)) * pW + k];
           if (k < now.Wl) A.part[(c < W ? 0 : plane) + (int64_t)now.n * A.C + now.c0 + k] = t;
         }
-      __syncthreads();
     }
     const int64_t xstep = (int64_t)R * A.x.row, gstep2 = (int64_t)R * A.dy.row;
     if constexpr (M != STATS) {
@@ -822,6 +825,10 @@ int lcm(int a, int b) {
   return a / x * b;
 }
 
+constexpr int kMostSlots = 128;               // what the error bound of a thread's sums is taken for
+constexpr size_t kMostData = 100 * 1024;     // two CTAs per SM
+constexpr int64_t kChunkData = 64 * 1024;    // chunks of a larger image: three
+
 // The rest of a plan whose slab width and parts are chosen; false if its slots need more than `most` bytes.
 bool settle(Plan& p, int64_t L, int C, int cpg, int e, bool backward, int64_t rows, size_t most) {
   p.slabs = (C + p.W - 1) / p.W;
@@ -834,7 +841,7 @@ bool settle(Plan& p, int64_t L, int C, int cpg, int e, bool backward, int64_t ro
   const int64_t slots = (rows + p.R - 1) / p.R;
   const int erows = p.lanes ? p.threads / 32 : p.R;
   const size_t f = sizeof(float), data = (size_t)slots * p.threads * p.V * e * (backward ? 2 : 1);
-  if (slots > 128 || data > most) return false;
+  if (slots > kMostSlots || data > most) return false;
   p.rows = (int)rows;
   p.slots = (int)slots;
   const int groups = p.W / cpg;
@@ -846,8 +853,6 @@ bool settle(Plan& p, int64_t L, int C, int cpg, int e, bool backward, int64_t ro
   return true;
 }
 
-constexpr size_t kMostData = 100 * 1024;     // two CTAs per SM
-constexpr int64_t kChunkData = 64 * 1024;    // chunks of a larger image: three
 
 // Slab width, CTAs per image and slab, and positions per thread. Slabs are multiples of whole groups and of
 // whole columns. Of the splits that keep an image's slab in one cluster's shared memory, the one of least
@@ -885,8 +890,9 @@ Plan plan(int64_t N, int64_t L, int C, int cpg, int dtype, bool vec, bool backwa
   if (p.W < unit) p.W = unit;
   if (p.W > C) p.W = C;
   settle(p, L, C, cpg, e, backward, 1, kMostData);
-  int64_t rows = (int64_t)p.R * (kChunkData / ((int64_t)p.threads * p.V * e * (backward ? 2 : 1)));
-  if (rows < p.R) rows = p.R;
+  int64_t slots = kChunkData / ((int64_t)p.threads * p.V * e * (backward ? 2 : 1));
+  slots = slots < 1 ? 1 : slots > kMostSlots ? kMostSlots : slots;
+  const int64_t rows = p.R * slots;
   settle(p, L, C, cpg, e, backward, rows, ~(size_t)0);
   p.parts = (int)((L + rows - 1) / rows);
   return p;
