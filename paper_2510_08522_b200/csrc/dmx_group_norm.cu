@@ -869,10 +869,12 @@ Plan plan(int64_t N, int64_t L, int C, int cpg, int dtype, bool vec, bool backwa
   p.resident = true;
   best.resident = false;
   float least = 0.f;
-  for (int k = 0; k < 5; ++k) {
+  for (int k = 0, last = 0; k < 5; ++k) {
     p.W = (want[k] / e) / unit * unit;
     if (p.W < unit) p.W = unit;
     if (p.W > C) p.W = C;
+    if (p.W == last) continue;
+    last = p.W;
     for (p.parts = 1; p.parts <= kMaxCluster; p.parts *= 2) {
       if (!settle(p, L, C, cpg, e, backward, (L + p.parts - 1) / p.parts, kMostData)) continue;
       if (p.parts > 1 && p.rows < p.R) break;
@@ -881,6 +883,7 @@ Plan plan(int64_t N, int64_t L, int C, int cpg, int dtype, bool vec, bool backwa
       const float ctas = (float)N * p.slabs * p.parts;
       if (ctas < 2 * 148) cost *= 2 * 148 / ctas;
       if (!best.resident || cost < least) { best = p; least = cost; }
+      if (ctas >= 2 * 148) break;                  // more CTAs per slab would only cost more
     }
   }
   if (best.resident) return best;

@@ -59,7 +59,8 @@ def _ptr(x):
 def _workspace(nbytes, like, where):
     if nbytes < 0:
         _refuse(where, int(nbytes))
-    return _torch.empty(nbytes, dtype=_torch.uint8, device=like.device) if nbytes else None
+    # (bf16 and fp32 callers alike: of the caller's type, which is the cheapest to ask torch for)
+    return like.new_empty((nbytes + 1) // 2) if nbytes else None
 
 
 class AdamW:
@@ -215,6 +216,10 @@ def _norm_args(x, groups, weight, bias, act, where):
     return shape[0], shape[1] if len(shape) == 3 else _prod(shape[1:-1]), C, _dtypes[x.dtype]
 
 
+def _fp32(shape, x, weight):
+    return x.new_empty(shape) if x.dtype == _torch.float32 else weight.new_empty(shape) if weight is not None else _torch.empty(shape, dtype=_torch.float32, device=x.device)
+
+
 @functools.lru_cache(maxsize=256)
 def _norm_workspace(*shape):
     return B.lib().dmx_group_norm_workspace(*shape)
@@ -233,7 +238,7 @@ def group_norm(x, groups, weight=None, bias=None, eps=1e-5, act="none", out=None
         ys = _image(y, x.shape, x.dtype, x, "group_norm (out)")
     if groups < 1:
         _refuse("group_norm (groups)")
-    mean, rstd = _torch.empty((2, N, groups), dtype=_torch.float32, device=x.device).unbind()
+    mean, rstd = _fp32((2, N, groups), x, weight).unbind()
     need = _norm_workspace(N, L, C, groups, dt, 0)
     ws = _workspace(need, x, "group_norm") if need else None
     with _on(x):
@@ -258,7 +263,7 @@ def group_norm_backward(dy, x, mean, rstd, groups, weight=None, bias=None, act="
     for s in (mean, rstd):
         if s.dtype != _torch.float32 or s.numel() != N * groups or s.device != x.device or not s.is_contiguous():
             _refuse("group_norm_backward (statistics)")
-    dweight, dbias = _torch.empty((2, C), dtype=_torch.float32, device=x.device).unbind()
+    dweight, dbias = _fp32((2, C), x, weight).unbind()
     need = _norm_workspace(N, L, C, groups, dt, 1)
     ws = _workspace(need, x, "group_norm_backward") if need else None
     with _on(x):
@@ -307,7 +312,7 @@ def linear(x, weight, bias=None, act="none", residual=None, save=False, out=None
         else:
             ws = None
         rc = L.dmx_linear_forward(M, N, K, xp, ldx, wp, ldw, _ptr(bias), ACT[act], _ptr(residual), ldr, y.data_ptr(), ldy, _ptr(z), N, _ptr(ws),
-                                  0 if ws is None else ws.numel(), _stream(x))
+                                  0 if ws is None else ws.numel() * ws.element_size(), _stream(x))
     if rc != B.OK:
         _refuse("dmx_linear_forward", rc)
     return y, z
@@ -325,7 +330,7 @@ def linear_backward(dy, x, weight, z=None, act="none", need=(True, True, True), 
         _refuse("linear_backward")
     ldg = _rows(dy, (M, N), x, "linear_backward (dy)")
     ldz = 0 if z is None else _rows(z, (M, N), x, "linear_backward (z)")
-    mk = lambda k, shape: None if not need[k] else (_torch.empty(shape, dtype=_torch.bfloat16, device=x.device) if out[k] is None else out[k])  # noqa: E731
+    mk = lambda k, shape: None if not need[k] else (x.new_empty(shape) if out[k] is None else out[k])  # noqa: E731
     dx, dw, db = mk(0, (M, K)), mk(1, (N, K)), mk(2, (N,))
     lddx = 0 if dx is None else _rows(dx, (M, K), x, "linear_backward (dx)")
     lddw = 0 if dw is None else _rows(dw, (N, K), x, "linear_backward (dweight)")
@@ -336,7 +341,7 @@ def linear_backward(dy, x, weight, z=None, act="none", need=(True, True, True), 
     with _on(x):
         ws = _workspace(L.dmx_linear_backward_workspace(M, N, K, gp, ldg, xp, ldx, wp, ldw, ACT[act]), x, "linear_backward")
         rc = L.dmx_linear_backward(M, N, K, gp, ldg, xp, ldx, wp, ldw, _ptr(z), ldz, ACT[act], _ptr(dx), lddx, _ptr(dw), lddw, _ptr(db), _ptr(ws),
-                                   0 if ws is None else ws.numel(), _stream(x))
+                                   0 if ws is None else ws.numel() * ws.element_size(), _stream(x))
     if rc != B.OK:
         _refuse("dmx_linear_backward", rc)
     return dx, dw, db
