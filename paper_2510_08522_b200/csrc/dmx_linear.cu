@@ -13,8 +13,11 @@
 // Few rows (M <= 64): the operands change places, so that W's rows fill the 128 lanes and the few rows of x are the narrow
 // side. Few tiles: k is split over the CTAs of a cluster, whose partial sums meet in distributed shared memory and
 // are added in a fixed order.
-// Every wait is bounded; a CTA that gives up counts itself in a device word (dmx_linear_status), lets its copies
-// land, frees its TMEM and returns.
+// Every wait is bounded; a warp that gives up counts itself in a device word (dmx_linear_status), and its CTA lets its
+// copies land, frees its TMEM and returns.
+// Bound: the tensor cores for large products, what an SM fetches from L2 (64 bytes a cycle) for narrow tiles, HBM for few rows.
+// Measured on B200: 8192^3 735 us = 1.50 PFLOP/s (the library's 685-691 us in the same runs); 8192 x 4096 x 1024 with GELU, y and z written,
+// 67 us = 1.03 PFLOP/s (the library's bare product 67-71 us); its gradient 133 us; one row x 4096 x 4096 7.8 us = 4.3 TB/s.
 #include "dmx.h"
 
 #include <cuda.h>
@@ -38,7 +41,7 @@ constexpr int kMaxStages = 8;
 constexpr int kSmemMost = 226 * 1024;
 constexpr unsigned kPolls = 1u << 18;         // about a second
 
-__device__ unsigned g_gave_up;                // CTAs whose waits ran out
+__device__ unsigned g_gave_up;                // warps whose waits ran out
 
 struct GemmArgs {
   int rowsA, rowsB, kblocks;                  // rows of D, columns of D, ceil(k / 64)

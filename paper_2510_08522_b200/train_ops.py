@@ -348,7 +348,7 @@ def linear_backward(dy, x, weight, z=None, act="none", need=(True, True, True), 
 
 
 def linear_status():
-    """How many CTAs of the linear kernels gave up a wait on the current device since the last call (synchronous)."""
+    """How many warps of the linear kernels gave up a wait on the current device since the last call (synchronous)."""
     n = ctypes.c_int()
     rc = B.lib().dmx_linear_status(ctypes.byref(n))
     if rc != B.OK:
