@@ -500,8 +500,9 @@ int dmx_adamw_destroy(dmx_adamw* h);   /* as dmx_destroy */
  * All arithmetic and all sums are fp32 (variances from deviations of the mean, never from a difference of
  * squares); y and dx are rounded once. Group norm's statistics do not depend on the batch size, which is why
  * it is the norm to use where a controller changes that.
- *   x, y, dy, dx       element (n, l, c) at n*image + l*row + c, strides in elements >= 0, of y and dx also row >= C
- *                      unless L <= 1 (x and dy may repeat rows or images with strides 0: a broadcast gradient);
+ *   x, y, dy, dx       element (n, l, c) at n*image + l*row + c, strides in elements >= 0; x and dy may repeat rows or
+ *                      images with strides 0 (a broadcast gradient); y and dx have each element in a place of its
+ *                      own: images one after the other, or their rows in turn (DMX_ERR_ARG otherwise);
  *                      any alignment of the element type (16-byte aligned starts and strides are faster)
  *   weight, bias       fp32, C entries, or NULL for ones and zeros
  *   mean, rstd         fp32, N*G (written by forward, read by backward)

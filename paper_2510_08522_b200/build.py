@@ -35,6 +35,20 @@ def _nvcc() -> str:
     return "nvcc"
 
 
+TORCH_MODULE = "_dmx_torch.so"
+
+
+def _torch_command():
+    """g++ for the torch module. Its undefined symbols are those of the torch libraries that `import torch` has loaded."""
+    import importlib.util
+    import sysconfig
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    cuda = os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include") if os.path.isabs(_nvcc()) else "/usr/local/cuda/include"
+    inc = [os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"], cuda, INCLUDE]
+    return (["g++", "-std=c++17", "-O2", "-fPIC", "-shared", "-fvisibility=hidden", "-Wno-attributes"] + ["-isystem" + i for i in inc[:-1]] + ["-I", INCLUDE] +
+            [os.path.join(CSRC, "dmx_torch.cpp"), "-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"])
+
+
 def _newer(path: str, than: list) -> bool:
     """path exists and is at least as new as every file of `than`."""
     return os.path.exists(path) and all(os.path.getmtime(path) >= os.path.getmtime(d) for d in than)
@@ -70,6 +84,10 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
                 compiles.append(([_nvcc()] + flags + ["-c", src], obj))
         if stale or not _newer(out, objs):
             links.append(([_nvcc()] + NVCC_FLAGS + ["-shared"] + objs, out))
+
+    out = lib_path(TORCH_MODULE)
+    if force or not _newer(out, [os.path.join(CSRC, "dmx_torch.cpp"), os.path.join(INCLUDE, "dmx.h")]):
+        compiles.append((_torch_command(), out))
 
     def run(job):
         cmd, out = job

@@ -999,8 +999,14 @@ bool shape_ok(int64_t N, int64_t L, int C, int G, int dtype) {
   return dtype == DMX_F32 || dtype == DMX_BF16;
 }
 
-// what is only read may repeat rows or images (stride 0); what is written may not
-bool strides_ok(int64_t L, int C, int64_t image, int64_t row, bool written) { return row >= 0 && image >= 0 && (!written || L <= 1 || row >= C); }
+// what is only read may repeat rows or images (stride 0); what is written has every element in a place of its own: image
+// after image, or the images' rows in turn
+bool strides_ok(int64_t N, int64_t L, int C, int64_t image, int64_t row, bool written) {
+  if (row < 0 || image < 0) return false;
+  if (!written || N == 0 || L == 0) return true;
+  if (L > 1 && row < C) return false;
+  return N <= 1 || image >= (L - 1) * row + C || (image >= C && row >= (N - 1) * image + C);
+}
 
 // 16-byte columns need every one of them to start on 16 bytes
 bool wide(const void* p, int64_t N, int64_t L, int C, int64_t image, int64_t row, int e) {
@@ -1037,7 +1043,7 @@ int dmx_group_norm_forward(int64_t N, int64_t L, int C, int G, int dtype, const 
                            int64_t y_row, float* mean, float* rstd, void* workspace, int64_t workspace_bytes,
                            void* cuda_stream) {
   if (!shape_ok(N, L, C, G, dtype) || act < DMX_ACT_NONE || act > DMX_ACT_GELU || !(eps >= 0.f)) return DMX_ERR_ARG;
-  if (!strides_ok(L, C, x_image, x_row, false) || !strides_ok(L, C, y_image, y_row, true)) return DMX_ERR_ARG;
+  if (!strides_ok(N, L, C, x_image, x_row, false) || !strides_ok(N, L, C, y_image, y_row, true)) return DMX_ERR_ARG;
   if (N == 0 || L == 0) return DMX_OK;
   if (!x || !y || !mean || !rstd) return DMX_ERR_ARG;
   const int e = dtype == DMX_F32 ? 4 : 2;
@@ -1064,7 +1070,7 @@ int dmx_group_norm_backward(int64_t N, int64_t L, int C, int G, int dtype, const
                             int64_t dx_image, int64_t dx_row, float* dweight, float* dbias, void* workspace,
                             int64_t workspace_bytes, void* cuda_stream) {
   if (!shape_ok(N, L, C, G, dtype) || act < DMX_ACT_NONE || act > DMX_ACT_GELU) return DMX_ERR_ARG;
-  if (!strides_ok(L, C, x_image, x_row, false) || !strides_ok(L, C, dy_image, dy_row, false) || !strides_ok(L, C, dx_image, dx_row, true)) return DMX_ERR_ARG;
+  if (!strides_ok(N, L, C, x_image, x_row, false) || !strides_ok(N, L, C, dy_image, dy_row, false) || !strides_ok(N, L, C, dx_image, dx_row, true)) return DMX_ERR_ARG;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   if (!element_aligned(dweight, 4) || !element_aligned(dbias, 4)) return DMX_ERR_ALIGN;
   if (N == 0 || L == 0) {

@@ -3,14 +3,16 @@ activation on channels-last data, and the matrix product with bias, activation a
 
 Tensors in, raw pointers through the C ABI; every call runs on the current stream of its tensors' device, takes its
 workspace from torch's allocator there, and raises DmxError with the library's code for arguments it refuses.
-Nothing synchronises.
+Nothing synchronises. The functional operators go through a compiled module (csrc/dmx_torch.cpp), which checks their
+arguments; AdamW holds a handle and goes through ctypes.
 """
 from __future__ import annotations
 
 import ctypes
-import functools
+import os
 
 from . import binding as B
+from . import build as _build
 
 ACT = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = range(4)
@@ -54,13 +56,6 @@ def _on(x):
 
 def _ptr(x):
     return None if x is None else x.data_ptr()
-
-
-def _workspace(nbytes, like, where):
-    if nbytes < 0:
-        _refuse(where, int(nbytes))
-    # (bf16 and fp32 callers alike: of the caller's type, which is the cheapest to ask torch for)
-    return like.new_empty((nbytes + 1) // 2) if nbytes else None
 
 
 class AdamW:
@@ -179,172 +174,54 @@ class AdamW:
     __del__ = close
 
 
-def _image(x, shape, dtype, like, where):
-    """Strides (image, row) of an (N, ..., C) tensor whose positions lie at one stride and whose channels are dense."""
-    if x is not like and (x.dtype != dtype or x.device != like.device or x.shape != shape):
-        _refuse(where)
-    st = x.stride()
-    if x.dim() == 3:
-        if shape[2] > 1 and st[2] != 1:
-            _refuse(where)
-        return st[0], st[1]
-    if shape[-1] > 1 and st[-1] != 1:
-        _refuse(where)
-    row = st[-2]
-    for i in range(x.dim() - 3, 0, -1):                  # (N, H, W, C): rows of the image must follow on
-        if shape[i] > 1 and st[i] != row * _prod(shape[i + 1:-1]):
-            _refuse(where)
-    return st[0], row
+_fast = None
 
 
-def _prod(v):
-    n = 1
-    for x in v:
-        n *= x
-    return n
-
-
-def _norm_args(x, groups, weight, bias, act, where):
-    _t()
-    if x.dim() < 3 or x.dtype not in _dtypes or not x.is_cuda or act not in ACT:
-        _refuse(where)
-    shape = x.shape
-    C = shape[-1]
-    for p in (weight, bias):
-        if p is not None and (p.dtype != _torch.float32 or p.numel() != C or p.device != x.device or not p.is_contiguous()):
-            _refuse(where + " (weight, bias)")
-    return shape[0], shape[1] if len(shape) == 3 else _prod(shape[1:-1]), C, _dtypes[x.dtype]
-
-
-def _fp32(shape, x, weight):
-    return x.new_empty(shape) if x.dtype == _torch.float32 else weight.new_empty(shape) if weight is not None else _torch.empty(shape, dtype=_torch.float32, device=x.device)
-
-
-@functools.lru_cache(maxsize=256)
-def _norm_workspace(*shape):
-    return B.lib().dmx_group_norm_workspace(*shape)
+def _module():
+    """The compiled module (lib/_dmx_torch.so), connected to the library that the binding loads."""
+    global _fast
+    if _fast is None:
+        import importlib.machinery
+        import importlib.util
+        _t()
+        L, path = B.lib(), _build.lib_path(_build.TORCH_MODULE)
+        if not os.path.exists(path):
+            raise RuntimeError("%s is not built; run `python -m paper_2510_08522_b200.build`" % path)
+        loader = importlib.machinery.ExtensionFileLoader("_dmx_torch", path)
+        m = importlib.util.module_from_spec(importlib.util.spec_from_file_location("_dmx_torch", path, loader=loader))
+        loader.exec_module(m)
+        m.connect(*[ctypes.cast(f, ctypes.c_void_p).value for f in (
+            L.dmx_group_norm_workspace, L.dmx_group_norm_forward, L.dmx_group_norm_backward, L.dmx_linear_workspace, L.dmx_linear_forward,
+            L.dmx_linear_backward_workspace, L.dmx_linear_backward)])
+        _fast = m
+    return _fast
 
 
 def group_norm(x, groups, weight=None, bias=None, eps=1e-5, act="none", out=None):
     """act(group_norm(x)) of a channels-last tensor (N, ..., C), fp32 or bf16 -> (y, mean, rstd), the statistics
     fp32 (N, groups). weight, bias: fp32 (C,). x may be a channel slice of a wider tensor; out may be x."""
-    N, L, C, dt = _norm_args(x, groups, weight, bias, act, "group_norm")
-    xs = _image(x, x.shape, x.dtype, x, "group_norm (x)")
-    if out is None:
-        y = _torch.empty_like(x, memory_format=_torch.contiguous_format)
-        ys = (L * C, C)
-    else:
-        y = out
-        ys = _image(y, x.shape, x.dtype, x, "group_norm (out)")
-    if groups < 1:
-        _refuse("group_norm (groups)")
-    mean, rstd = _fp32((2, N, groups), x, weight).unbind()
-    need = _norm_workspace(N, L, C, groups, dt, 0)
-    ws = _workspace(need, x, "group_norm") if need else None
-    with _on(x):
-        rc = B.lib().dmx_group_norm_forward(N, L, C, groups, dt, x.data_ptr(), xs[0], xs[1], _ptr(weight), _ptr(bias), eps, ACT[act], y.data_ptr(), ys[0], ys[1],
-                                            mean.data_ptr(), rstd.data_ptr(), _ptr(ws), need, _stream(x))
-    if rc != B.OK:
-        _refuse("dmx_group_norm_forward", rc)
-    return y, mean, rstd
+    r = (_fast or _module()).group_norm(x, groups, weight, bias, eps, ACT.get(act, -1), out)
+    return r if r.__class__ is tuple else _refuse("group_norm", r)
 
 
 def group_norm_backward(dy, x, mean, rstd, groups, weight=None, bias=None, act="none", out=None):
-    """Gradient of group_norm from its saved statistics -> (dx, dweight, dbias)."""
-    N, L, C, dt = _norm_args(x, groups, weight, bias, act, "group_norm_backward")
-    xs = _image(x, x.shape, x.dtype, x, "group_norm_backward (x)")
-    gs = _image(dy, x.shape, x.dtype, x, "group_norm_backward (dy)")
-    if out is None:
-        dx = _torch.empty_like(x, memory_format=_torch.contiguous_format)
-        ds = (L * C, C)
-    else:
-        dx = out
-        ds = _image(dx, x.shape, x.dtype, x, "group_norm_backward (out)")
-    for s in (mean, rstd):
-        if s.dtype != _torch.float32 or s.numel() != N * groups or s.device != x.device or not s.is_contiguous():
-            _refuse("group_norm_backward (statistics)")
-    dweight, dbias = _fp32((2, C), x, weight).unbind()
-    need = _norm_workspace(N, L, C, groups, dt, 1)
-    ws = _workspace(need, x, "group_norm_backward") if need else None
-    with _on(x):
-        rc = B.lib().dmx_group_norm_backward(N, L, C, groups, dt, dy.data_ptr(), gs[0], gs[1], x.data_ptr(), xs[0], xs[1], mean.data_ptr(), rstd.data_ptr(),
-                                        _ptr(weight), _ptr(bias), ACT[act], dx.data_ptr(), ds[0], ds[1], dweight.data_ptr(),
-                                             dbias.data_ptr(), _ptr(ws), need, _stream(x))
-    if rc != B.OK:
-        _refuse("dmx_group_norm_backward", rc)
-    return dx, dweight, dbias
-
-
-def _rows(x, shape, like, where):
-    """Leading dimension of a bf16 matrix with dense rows."""
-    if x.dtype != _torch.bfloat16 or x.device != like.device or tuple(x.shape) != shape or (shape[1] > 1 and x.stride(1) != 1):
-        _refuse(where)
-    return x.stride(0) if shape[0] > 1 else shape[1]
-
-
-def _matrix(x, like, where):
-    if x is None or x.dim() != 2 or not x.is_cuda:
-        _refuse(where)
-    return _rows(x, tuple(x.shape), like, where)
+    """Gradient of group_norm from its saved statistics -> (dx, dweight, dbias). out may be dy or x."""
+    r = (_fast or _module()).group_norm_backward(dy, x, mean, rstd, groups, weight, bias, ACT.get(act, -1), out)
+    return r if r.__class__ is tuple else _refuse("group_norm_backward", r)
 
 
 def linear(x, weight, bias=None, act="none", residual=None, save=False, out=None):
     """act(x @ weight.T + bias) + residual, bf16 matrices -> (y, z). z is the value before the activation, kept for
     linear_backward when `save` is set and there is an activation, else None. out may be the residual."""
-    _t()
-    if act not in ACT:
-        _refuse("linear (act)")
-    ldx, ldw = _matrix(x, x, "linear (x)"), _matrix(weight, x, "linear (weight)")
-    (M, K), N = x.shape, weight.shape[0]
-    if weight.shape[1] != K:
-        _refuse("linear (weight)")
-    if bias is not None and (bias.dtype != _torch.bfloat16 or bias.numel() != N or bias.device != x.device or not bias.is_contiguous()):
-        _refuse("linear (bias)")
-    ldr = 0 if residual is None else _rows(residual, (M, N), x, "linear (residual)")
-    y = x.new_empty((M, N)) if out is None else out
-    ldy = N if out is None else _rows(y, (M, N), x, "linear (out)")
-    z = x.new_empty((M, N)) if save and act != "none" else None
-    L = B.lib()
-    xp, wp = x.data_ptr(), weight.data_ptr()
-    with _on(x):
-        if (xp | wp | 2 * ldx | 2 * ldw) & 15 or ldx < K or ldw < K:           # an operand has to be laid out (or is one row)
-            ws = _workspace(L.dmx_linear_workspace(M, N, K, xp, ldx, wp, ldw), x, "linear")
-        else:
-            ws = None
-        rc = L.dmx_linear_forward(M, N, K, xp, ldx, wp, ldw, _ptr(bias), ACT[act], _ptr(residual), ldr, y.data_ptr(), ldy, _ptr(z), N, _ptr(ws),
-                                  0 if ws is None else ws.numel() * ws.element_size(), _stream(x))
-    if rc != B.OK:
-        _refuse("dmx_linear_forward", rc)
-    return y, z
+    r = (_fast or _module()).linear(x, weight, bias, ACT.get(act, -1), residual, save, out)
+    return r if r.__class__ is tuple else _refuse("linear", r)
 
 
 def linear_backward(dy, x, weight, z=None, act="none", need=(True, True, True), out=(None, None, None)):
     """Gradient of linear -> (dx, dweight, dbias), those not in `need` None. `out`: tensors to write them to, e.g.
     views of a flat gradient vector."""
-    _t()
-    if act not in ACT:
-        _refuse("linear_backward (act)")
-    ldx, ldw = _matrix(x, x, "linear_backward (x)"), _matrix(weight, x, "linear_backward (weight)")
-    (M, K), N = x.shape, weight.shape[0]
-    if weight.shape[1] != K or (z is None and act != "none"):
-        _refuse("linear_backward")
-    ldg = _rows(dy, (M, N), x, "linear_backward (dy)")
-    ldz = 0 if z is None else _rows(z, (M, N), x, "linear_backward (z)")
-    mk = lambda k, shape: None if not need[k] else (x.new_empty(shape) if out[k] is None else out[k])  # noqa: E731
-    dx, dw, db = mk(0, (M, K)), mk(1, (N, K)), mk(2, (N,))
-    lddx = 0 if dx is None else _rows(dx, (M, K), x, "linear_backward (dx)")
-    lddw = 0 if dw is None else _rows(dw, (N, K), x, "linear_backward (dweight)")
-    if db is not None and (db.dtype != _torch.bfloat16 or db.numel() != N or db.device != x.device or not db.is_contiguous()):
-        _refuse("linear_backward (dbias)")
-    L = B.lib()
-    gp, xp, wp = dy.data_ptr(), x.data_ptr(), weight.data_ptr()
-    with _on(x):
-        ws = _workspace(L.dmx_linear_backward_workspace(M, N, K, gp, ldg, xp, ldx, wp, ldw, ACT[act]), x, "linear_backward")
-        rc = L.dmx_linear_backward(M, N, K, gp, ldg, xp, ldx, wp, ldw, _ptr(z), ldz, ACT[act], _ptr(dx), lddx, _ptr(dw), lddw, _ptr(db), _ptr(ws),
-                                   0 if ws is None else ws.numel() * ws.element_size(), _stream(x))
-    if rc != B.OK:
-        _refuse("dmx_linear_backward", rc)
-    return dx, dw, db
+    r = (_fast or _module()).linear_backward(dy, x, weight, z, ACT.get(act, -1), (1 if need[0] else 0) + (2 if need[1] else 0) + (4 if need[2] else 0), *out)
+    return r if r.__class__ is tuple else _refuse("linear_backward", r)
 
 
 def linear_status():

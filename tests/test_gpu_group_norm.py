@@ -284,3 +284,17 @@ def test_refusals():
     m = torch.zeros(2, 3, device="cuda")
     with pytest.raises(D.DmxError):
         D.group_norm_backward(dy, x, m[:1], m, 3, w, b)
+
+
+def test_results_may_be_written_where_images_take_turns_by_rows():
+    torch, D = _d()
+    x, dy, w, b = make(3, 20, 16, torch.float32, seed=9)
+    y, mean, rstd = D.group_norm(x, 4, w, b, act="silu")
+    dx, dw, db = D.group_norm_backward(dy, x, mean, rstd, 4, w, b, act="silu")
+    turns = torch.zeros(20, 3, 24, device="cuda")
+    got = D.group_norm(x, 4, w, b, act="silu", out=turns.transpose(0, 1)[:, :, :16])
+    assert torch.equal(got[0], y) and torch.equal(turns[..., :16].transpose(0, 1), y) and not turns[..., 16:].any()
+    got = D.group_norm_backward(dy, x, mean, rstd, 4, w, b, act="silu", out=turns.transpose(0, 1)[:, :, :16])
+    assert torch.equal(got[0], dx) and torch.equal(got[1], dw) and torch.equal(got[2], db) and not turns[..., 16:].any()
+    with pytest.raises(D.DmxError):
+        D.group_norm(x, 4, w, b, out=torch.empty(1, 20, 16, device="cuda").expand(3, 20, 16))

@@ -2,7 +2,9 @@
 before any device call."""
 import ctypes
 
-import paper_2510_08522_b200  # noqa: F401
+import pytest
+
+import paper_2510_08522_b200 as D
 from paper_2510_08522_b200 import binding as B
 
 
@@ -47,6 +49,7 @@ def test_group_norm_refuses_bad_shapes_strides_and_pointers():
     assert forward(yr=11) == B.ERR_ARG and forward(xr=-12) == B.ERR_ARG and forward(act=4) == B.ERR_ARG and forward(eps=-1.0) == B.ERR_ARG
     assert forward(eps=float("nan")) == B.ERR_ARG and forward(x=18) == B.ERR_ALIGN and forward(rstd=2050) == B.ERR_ALIGN
     assert L.dmx_group_norm_forward(0, 10, 12, 3, 0, None, 0, 12, None, None, 1e-5, 0, None, 0, 12, None, None, None, 0, None) == B.OK
+    assert forward(yi=0) == B.ERR_ARG and forward(yi=119) == B.ERR_ARG and forward(yi=12, yr=23) == B.ERR_ARG and forward(yi=11, yr=24) == B.ERR_ARG   # two elements in one place
     back = lambda ws, n: L.dmx_group_norm_backward(2, 10, 12, 3, 0, 16, 120, 12, 1024, 120, 12, 2048, 3072, None, None, 0, 4096, 120, 12, None, None,  # noqa: E731
                                                    ws, n, None)
     assert back(None, 0) == B.ERR_ARG and back(8192, 64) == B.ERR_ARG and back(8200, 1 << 20) == B.ERR_ALIGN
@@ -75,3 +78,14 @@ def test_linear_refuses_bad_extents_strides_and_pointers():
     assert backward(act=1) == B.ERR_ARG and backward(dy=None) == B.ERR_ARG and backward(w=None) == B.ERR_ARG and backward(x=None) == B.ERR_ARG
     assert backward(lddx=15) == B.ERR_ARG and backward(ws=None) == B.ERR_ARG and backward(n=16) == B.ERR_ARG and backward(dw=4097) == B.ERR_ALIGN
     assert L.dmx_linear_status(None) == B.ERR_ARG
+
+
+def test_torch_callers_get_errors_for_what_is_no_cuda_tensor():
+    torch = pytest.importorskip("torch")
+    x, m = torch.zeros(2, 5, 8), torch.zeros(4, 8, dtype=torch.bfloat16)
+    for call in (lambda: D.group_norm(x, 2), lambda: D.group_norm(None, 2), lambda: D.group_norm([1.0], 2), lambda: D.group_norm(x, "2"),
+                 lambda: D.group_norm(x, 2, eps="small"), lambda: D.group_norm(x.double(), 2), lambda: D.group_norm_backward(x, x, x[0], x[0], 2),
+                 lambda: D.linear(m, m), lambda: D.linear(m, None), lambda: D.linear(m.float(), m.float()), lambda: D.linear_backward(m, m, m),
+                 lambda: D.linear_backward(m, 1, m)):
+        with pytest.raises(D.DmxError):
+            call()
