@@ -1,6 +1,6 @@
-// dmx_torch.cpp — the functional training operators (group_norm, linear and their gradients) for torch callers, compiled:
-// argument checks, allocation from torch's caching allocator and the call into the C ABI of include/dmx.h in one
-// Python call (a call through ctypes took 11-28 us on the host, mostly checks and argument marshalling; the kernels of a small
+// dmx_torch.cpp — what a training step calls (group_norm, linear and their gradients, AdamW's norm and step) for torch callers,
+// compiled: argument checks, allocation from torch's caching allocator and the call into the C ABI of include/dmx.h in one
+// Python call (through ctypes the calls took 5-28 us on the host, mostly checks and argument marshalling; now 3-14; the kernels of a small
 // problem take 4-8 us). train_ops.py wraps these and documents them. A function returns its result, or a negative
 // DMX_ERR_* code for arguments it refuses; torch's own errors (out of memory) are raised as Python exceptions.
 #include <Python.h>
@@ -25,6 +25,8 @@ decltype(&dmx_linear_workspace) linear_workspace;
 decltype(&dmx_linear_forward) linear_forward;
 decltype(&dmx_linear_backward_workspace) linear_backward_workspace;
 decltype(&dmx_linear_backward) linear_backward;
+decltype(&dmx_adamw_grad_norm) adamw_norm;
+decltype(&dmx_adamw_step) adamw_step;
 
 struct Refused {
   int64_t code;
@@ -43,6 +45,14 @@ const at::Tensor* maybe(PyObject* o) { return o == Py_None ? nullptr : &tensor(o
 long whole(PyObject* o) {
   const long v = PyLong_AsLong(o);
   if (v == -1 && PyErr_Occurred()) {
+    PyErr_Clear();
+    refuse();
+  }
+  return v;
+}
+double number(PyObject* o) {
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) {
     PyErr_Clear();
     refuse();
   }
@@ -128,8 +138,7 @@ PyObject* group_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor& x = tensor(a[0]);
     const long G = whole(a[1]);
     const at::Tensor *w = maybe(a[2]), *b = maybe(a[3]), *given = maybe(a[6]);
-    const double eps = PyFloat_AsDouble(a[4]);
-    if (eps == -1.0 && PyErr_Occurred()) { PyErr_Clear(); refuse(); }
+    const double eps = number(a[4]);
     const int act = (int)whole(a[5]), type = type_of(x);
     const Images X = images(x);
     const float *wp = vector(w, x, X.C), *bp = vector(b, x, X.C);
@@ -249,11 +258,62 @@ PyObject* linear_gradient(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// addresses of the seven entry points, in the order of the declarations above
+// ---------------------------------------------------------------------------------------------- AdamW
+
+// One of the optimizer's arrays: n entries of a type, dense, on its device.
+void* part(const at::Tensor* t, at::ScalarType type, int64_t n, long device) {
+  need(t && t->scalar_type() == type && t->numel() == n && t->is_cuda() && t->device().index() == device && t->is_contiguous());
+  return t->mutable_data_ptr();
+}
+dmx_adamw* handle(PyObject* o) {
+  void* p = PyLong_AsVoidPtr(o);
+  if (!p && PyErr_Occurred()) PyErr_Clear();
+  if (!p) refuse(DMX_ERR_HANDLE);
+  return static_cast<dmx_adamw*>(p);
+}
+
+// handle, device, max_norm, out -> out
+PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    need(n == 4);
+    const at::Tensor& to = tensor(a[3]);
+    void* p = part(&to, at::kFloat, 2, whole(a[1]));
+    Call call(to);
+    const int rc = adamw_norm(handle(a[0]), (float)number(a[2]), static_cast<float*>(p), call.stream);
+    if (rc != DMX_OK) refuse(rc);
+    return item(&to);
+  });
+}
+
+// handle, device, state bits, blocks, m, v, m_scale, v_scale, grad_scale, lr, beta1, beta2, eps, weight_decay, t, seed -> None
+PyObject* step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    need(n == 16);
+    const long device = whole(a[1]), blocks = whole(a[3]);
+    const bool codes = whole(a[2]) == 8;
+    const at::Tensor &m = tensor(a[4]), &v = tensor(a[5]);
+    const at::Tensor *ms = maybe(a[6]), *vs = maybe(a[7]), *gs = maybe(a[8]);
+    void *mp = part(&m, codes ? at::kChar : at::kFloat, blocks * 256, device), *vp = part(&v, codes ? at::kByte : at::kFloat, blocks * 256, device);
+    void *msp = codes ? part(ms, at::kFloat, blocks, device) : out(ms), *vsp = codes ? part(vs, at::kFloat, blocks, device) : out(vs);
+    void* gsp = gs ? part(gs, at::kFloat, 1, device) : nullptr;
+    uint32_t seed = 0;
+    if (a[15] != Py_None) {
+      seed = (uint32_t)PyLong_AsUnsignedLongMask(a[15]);
+      if (PyErr_Occurred()) { PyErr_Clear(); refuse(); }
+    }
+    Call call(m);
+    const int rc = adamw_step(handle(a[0]), mp, vp, static_cast<float*>(msp), static_cast<float*>(vsp), static_cast<float*>(gsp), number(a[9]), number(a[10]),
+                              number(a[11]), number(a[12]), number(a[13]), whole(a[14]), a[15] != Py_None, seed, call.stream);
+    if (rc != DMX_OK) refuse(rc);
+    Py_RETURN_NONE;
+  });
+}
+
+// addresses of the nine entry points, in the order of the declarations above
 PyObject* connect(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void* p[7];
-  if (n != 7) return PyErr_SetString(PyExc_TypeError, "seven addresses"), nullptr;
-  for (int i = 0; i < 7; ++i)
+  void* p[9];
+  if (n != 9) return PyErr_SetString(PyExc_TypeError, "nine addresses"), nullptr;
+  for (int i = 0; i < 9; ++i)
     if (!(p[i] = PyLong_AsVoidPtr(a[i]))) return PyErr_Occurred() ? nullptr : (PyErr_SetString(PyExc_ValueError, "null address"), nullptr);
   norm_workspace = reinterpret_cast<decltype(norm_workspace)>(p[0]);
   norm_forward = reinterpret_cast<decltype(norm_forward)>(p[1]);
@@ -262,6 +322,8 @@ PyObject* connect(PyObject*, PyObject* const* a, Py_ssize_t n) {
   linear_forward = reinterpret_cast<decltype(linear_forward)>(p[4]);
   linear_backward_workspace = reinterpret_cast<decltype(linear_backward_workspace)>(p[5]);
   linear_backward = reinterpret_cast<decltype(linear_backward)>(p[6]);
+  adamw_norm = reinterpret_cast<decltype(adamw_norm)>(p[7]);
+  adamw_step = reinterpret_cast<decltype(adamw_step)>(p[8]);
   Py_RETURN_NONE;
 }
 
@@ -271,6 +333,8 @@ PyMethodDef methods[] = {{"connect", FAST(connect)},
                          {"group_norm_backward", FAST(group_norm_backward)},
                          {"linear", FAST(linear)},
                          {"linear_backward", FAST(linear_gradient)},
+                         {"adamw_grad_norm", FAST(grad_norm)},
+                         {"adamw_step", FAST(step)},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_dmx_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

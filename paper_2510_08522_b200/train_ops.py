@@ -4,7 +4,7 @@ activation on channels-last data, and the matrix product with bias, activation a
 Tensors in, raw pointers through the C ABI; every call runs on the current stream of its tensors' device, takes its
 workspace from torch's allocator there, and raises DmxError with the library's code for arguments it refuses.
 Nothing synchronises. The functional operators go through a compiled module (csrc/dmx_torch.cpp), which checks their
-arguments; AdamW holds a handle and goes through ctypes.
+arguments, and so do AdamW's norm and step; the rest of AdamW goes through ctypes.
 """
 from __future__ import annotations
 
@@ -69,7 +69,7 @@ class AdamW:
 
     def __init__(self, params, grads, state_bits=32, copies=None, decay=None):
         torch = _t()
-        self._h = None
+        self._h, self._fast = None, _module()
         params, n = list(params), len(params)
         if n == 0 or (decay is not None and len(decay) != n) or params[0].dtype not in _dtypes or not params[0].is_cuda:
             _refuse("AdamW (params)")
@@ -85,6 +85,7 @@ class AdamW:
             rc = B.lib().dmx_adamw_create(n, sizes, dec, _dtypes[self._dtype], _dtypes[self._grad_dtype], self.bits, ctypes.byref(h))
         if rc != B.OK:
             _refuse("dmx_adamw_create", rc)
+        self._at = h.value
         self._h, self._destroy = h, B.lib().dmx_adamw_destroy     # (module globals may be gone when __del__ runs)
         self.blocks = B.lib().dmx_adamw_blocks(h)
         self.bind(grads, copies)
@@ -132,24 +133,15 @@ class AdamW:
         """out[0] = the gradients' global norm, out[1] = min(1, max_norm / (norm + 1e-6)) (NaN: not finite)."""
         if out is None:
             out = _torch.empty(2, device=self.device)
-        elif out.dtype != _torch.float32 or out.numel() != 2 or out.device != self.device or not out.is_contiguous():
-            _refuse("AdamW.grad_norm (out)")
-        with _on(out):
-            rc = B.lib().dmx_adamw_grad_norm(self._h, max_norm, out.data_ptr(), _stream(out))
-        if rc != B.OK:
-            _refuse("dmx_adamw_grad_norm", rc)
-        return out
+        r = self._fast.adamw_grad_norm(self._at, self.device.index, max_norm, out)
+        return _refuse("AdamW.grad_norm", r) if r.__class__ is int else r
 
     def step(self, m, v, m_scale=None, v_scale=None, *, lr, t, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, grad_scale=None, seed=None):
         """One update. t: this step's number, from 1. seed: dither 8-bit codes with it (None: to nearest)."""
-        self._check("AdamW.step (state)", m, v, m_scale, v_scale)
-        if grad_scale is not None and (grad_scale.dtype != _torch.float32 or grad_scale.numel() != 1 or grad_scale.device != self.device):
-            _refuse("AdamW.step (grad_scale)")
-        with _on(m):
-            rc = B.lib().dmx_adamw_step(self._h, m.data_ptr(), v.data_ptr(), _ptr(m_scale), _ptr(v_scale), _ptr(grad_scale), lr, beta1, beta2, eps,
-                                        weight_decay, t, 0 if seed is None else 1, 0 if seed is None else seed & 0xFFFFFFFF, _stream(m))
-        if rc != B.OK:
-            _refuse("dmx_adamw_step", rc)
+        r = self._fast.adamw_step(self._at, self.device.index, self.bits, self.blocks, m, v, m_scale, v_scale, grad_scale, lr, beta1, beta2, eps,
+                                  weight_decay, t, seed)
+        if r is not None:
+            _refuse("AdamW.step", r)
 
     def moments(self, m, v, m_scale, v_scale, out_m=None, out_v=None):
         """The values of 8-bit moments (fp32 unless outputs are given)."""
@@ -169,7 +161,7 @@ class AdamW:
     def close(self):
         if getattr(self, "_h", None):
             self._destroy(self._h)
-            self._h = None
+            self._h = self._at = None
 
     __del__ = close
 
@@ -192,7 +184,7 @@ def _module():
         loader.exec_module(m)
         m.connect(*[ctypes.cast(f, ctypes.c_void_p).value for f in (
             L.dmx_group_norm_workspace, L.dmx_group_norm_forward, L.dmx_group_norm_backward, L.dmx_linear_workspace, L.dmx_linear_forward,
-            L.dmx_linear_backward_workspace, L.dmx_linear_backward)])
+            L.dmx_linear_backward_workspace, L.dmx_linear_backward, L.dmx_adamw_grad_norm, L.dmx_adamw_step)])
         _fast = m
     return _fast
 

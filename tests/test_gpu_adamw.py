@@ -283,6 +283,16 @@ def test_refusals_on_the_device():
         opt.step(m, v, **ok)                           # scales missing
     with pytest.raises(D.DmxError):
         opt.step(m[:256], v, ms, vs, **ok)
+    for bad in ((m.float(), v, ms, vs), (m, v, ms[:1], vs), (m, v, ms, vs.double()), (m.cpu(), v, ms, vs), (m, None, ms, vs)):
+        with pytest.raises(D.DmxError):
+            opt.step(*bad, **ok)
+    for bad in (dict(ok, grad_scale=ms), dict(ok, grad_scale=1.0), dict(ok, seed="a"), dict(ok, t="1"), dict(ok, lr=None)):
+        with pytest.raises(D.DmxError):
+            opt.step(m, v, ms, vs, **bad)
+    for out in (torch.empty(3, device="cuda"), torch.empty(2), torch.empty(2, device="cuda", dtype=torch.float64), torch.empty(4, device="cuda")[::2]):
+        with pytest.raises(D.DmxError):
+            opt.grad_norm(1.0, out=out)
+    assert opt.grad_norm(1.0, out=(n := torch.empty(2, device="cuda"))) is n
     with pytest.raises(D.DmxError):
         opt.grad_norm(0.0)
     with pytest.raises(D.DmxError):
