@@ -505,7 +505,7 @@ int dmx_adamw_destroy(dmx_adamw* h);   /* as dmx_destroy */
  *                      own: images one after the other, or their rows in turn (DMX_ERR_ARG otherwise);
  *                      any alignment of the element type (16-byte aligned starts and strides are faster)
  *   weight, bias       fp32, C entries, or NULL for ones and zeros
- *   mean, rstd         fp32, N*G (written by forward, read by backward)
+ *   mean, rstd         fp32, N*G (written by forward, read by backward); NaN where L = 0: there is nothing to average
  *   dweight, dbias     fp32, C entries, or NULL
  *   workspace          at least dmx_group_norm_workspace(...) bytes, 16-byte aligned, contents undefined
  * Results are bitwise reproducible. y may be x itself, and dx may be dy or x, with the same strides.

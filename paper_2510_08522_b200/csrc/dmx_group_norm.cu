@@ -1044,11 +1044,18 @@ int dmx_group_norm_forward(int64_t N, int64_t L, int C, int G, int dtype, const 
                            void* cuda_stream) {
   if (!shape_ok(N, L, C, G, dtype) || act < DMX_ACT_NONE || act > DMX_ACT_GELU || !(eps >= 0.f)) return DMX_ERR_ARG;
   if (!strides_ok(N, L, C, x_image, x_row, false) || !strides_ok(N, L, C, y_image, y_row, true)) return DMX_ERR_ARG;
-  if (N == 0 || L == 0) return DMX_OK;
+  if (N == 0) return DMX_OK;
+  if (!element_aligned(mean, 4) || !element_aligned(rstd, 4)) return DMX_ERR_ALIGN;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (L == 0) {                    // nothing over nothing: bytes of ones are a NaN
+    for (float* p : {mean, rstd})
+      if (p && !dmxh::cuda_ok(cudaMemsetAsync(p, 0xff, sizeof(float) * N * G, st))) return DMX_ERR_CUDA;
+    return DMX_OK;
+  }
   if (!x || !y || !mean || !rstd) return DMX_ERR_ARG;
   const int e = dtype == DMX_F32 ? 4 : 2;
-  if (!element_aligned(x, e) || !element_aligned(y, e) || !element_aligned(mean, 4) || !element_aligned(rstd, 4) ||
-      !element_aligned(weight, 4) || !element_aligned(bias, 4) || !element_aligned(workspace, 16)) return DMX_ERR_ALIGN;
+  if (!element_aligned(x, e) || !element_aligned(y, e) || !element_aligned(weight, 4) || !element_aligned(bias, 4) || !element_aligned(workspace, 16))
+    return DMX_ERR_ALIGN;
   const bool vec = columns_fit(C, C / G, e) && wide(x, N, L, C, x_image, x_row, e) && wide(y, N, L, C, y_image, y_row, e);
   const Plan p = plan(N, L, C, C / G, dtype, vec, false);
   const int64_t need = workspace_of(p, N, C, G, false);
@@ -1060,7 +1067,6 @@ int dmx_group_norm_forward(int64_t N, int64_t L, int C, int G, int dtype, const 
   A.weight = weight; A.bias = bias; A.mean = mean; A.rstd = rstd; A.part = static_cast<float*>(workspace);
   fill(A, p, N, L, C, G);
   A.eps = eps;
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   return run(false, act, dtype, vec, p, A, st);
 }
 
