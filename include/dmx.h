@@ -441,7 +441,8 @@ enum { DMX_ACT_NONE = 0, DMX_ACT_RELU = 1, DMX_ACT_SILU = 2, DMX_ACT_GELU = 3 };
  * Per element, with s the optional gradient factor:
  *   g = s*grad       m' = b1 m + (1-b1) g       v' = b2 v + (1-b2) g^2
  *   p' = p (1 - lr*wd) - lr/(1-b1^t) * m' / (sqrt(v') / sqrt(1-b2^t) + eps)       (wd = 0 where decay[i] is 0)
- * Arithmetic is fp32; parameters of type DMX_BF16 are rounded once when written.
+ * Arithmetic is fp32; parameters of type DMX_BF16 are rounded once when written. Where g^2 overflows (|g| > 1.8e19) v' is
+ * infinite and the update zero.
  *
  * State. Tensor i owns ceil(sizes[i]/256) consecutive blocks of DMX_ADAMW_BLOCK elements, the first one at
  * dmx_adamw_first_block(h, i), dmx_adamw_blocks(h) in all; element j of the tensor is element first*256 + j of
@@ -453,7 +454,7 @@ enum { DMX_ACT_NONE = 0, DMX_ACT_RELU = 1, DMX_ACT_SILU = 2, DMX_ACT_GELU = 3 };
  *                   Each step writes the block's largest |m'| and sqrt(v') as its scales and the codes nearest to
  *                   (|x|/scale)^(1/2), or, with dither != 0, floor(that + u) with u in [0,1) in steps of 2^-16
  *                   from a hash of the element's state index (low 32 bits) and `seed`: give every step another
- *                   seed. A nonzero second moment keeps a nonzero code. Dithering is what lets a second moment
+ *                   seed. A nonzero second moment keeps a nonzero code; an infinite one is held as 3.4e38. Dithering is what lets a second moment
  *                   decay: a change of 0.1 % is far below half a code.
  *
  *   dmx_adamw_create     sizes: HOST, n entries >= 0 (n in 1..DMX_ADAMW_MAX_TENSORS); decay: HOST, n bytes, or

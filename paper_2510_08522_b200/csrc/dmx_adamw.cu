@@ -26,6 +26,7 @@
 
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <float.h>
 #include <math.h>
 #include <new>
 #include <string.h>
@@ -203,6 +204,11 @@ __device__ __forceinline__ float2 root2(float2 x) {
   const float2 e = fma2(make_float2(-s.x, -s.y), s, x);
   return fma2(e, mul2(y, two(0.5f)), s);
 }
+// An infinite second moment (a finite gradient above 1.8e19) has an infinite root, and its update is zero.
+__device__ __forceinline__ float2 any_root2(float2 x) {
+  const float2 r = root2(x);
+  return make_float2(x.x == INFINITY ? INFINITY : r.x, x.y == INFINITY ? INFINITY : r.y);
+}
 __device__ __forceinline__ float2 quotient2(float2 a, float b, float rcp_b) {
   const float2 q = mul2(a, two(rcp_b));
   return fma2(fma2(q, two(-b), a), two(rcp_b), q);
@@ -234,6 +240,7 @@ __device__ __forceinline__ float block_max(float x) {   // over the warp, of non
 }
 
 constexpr float kTiny = 1.1754944e-38f;   // below it a reciprocal overflows: such a block is held as zeros
+constexpr float kMostRoot = 1.8446742e19f;   // its square is finite: where a second moment is not, codes hold it as this one
 
 // What a lane reads of a block.
 template <typename P, typename G, int BITS>
@@ -289,20 +296,29 @@ __device__ __forceinline__ void finish(const Raw<P, G, BITS>& x, const StepArgs&
       v2[2 * q] = decode_v<0>(x.wv[q], x.R); v2[2 * q + 1] = decode_v<2>(x.wv[q], x.R);
     }
   }
-  float2 m2[4], root[4];
+  float2 m2[4], v2[4], g2[4], root[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const float2 gj = mul2(make_float2(g[2 * j], g[2 * j + 1]), two(s));
-    m2[j] = fma2(mul2(make_float2(m[2 * j], m[2 * j + 1]), two(A.b1)), two(A.one), mul2(gj, two(A.omb1)));
-    const float2 v2 = fma2(mul2(make_float2(v[2 * j], v[2 * j + 1]), two(A.b2)), two(A.one), mul2(mul2(gj, gj), two(A.omb2)));
-    root[j] = root2(v2);
-    const float2 den = fma2(root[j], two(A.rs_bc2), two(A.eps));
-    const float2 u = mul2(m2[j], make_float2(rcp_near(den.x), rcp_near(den.y)));
-    const float2 q = fma2(u, two(-A.step), mul2(make_float2(p[2 * j], p[2 * j + 1]), two(keep)));
-    p[2 * j] = q.x; p[2 * j + 1] = q.y;
-    m[2 * j] = m2[j].x; m[2 * j + 1] = m2[j].y;
-    v[2 * j] = v2.x; v[2 * j + 1] = v2.y;
+    g2[j] = mul2(make_float2(g[2 * j], g[2 * j + 1]), two(s));
+    v2[j] = fma2(mul2(make_float2(v[2 * j], v[2 * j + 1]), two(A.b2)), two(A.one), mul2(mul2(g2[j], g2[j]), two(A.omb2)));
   }
+  auto update = [&](auto root_of) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      m2[j] = fma2(mul2(make_float2(m[2 * j], m[2 * j + 1]), two(A.b1)), two(A.one), mul2(g2[j], two(A.omb1)));
+      root[j] = root_of(v2[j]);
+      const float2 den = fma2(root[j], two(A.rs_bc2), two(A.eps));
+      const float2 u = mul2(m2[j], make_float2(rcp_near(den.x), rcp_near(den.y)));
+      const float2 q = fma2(u, two(-A.step), mul2(make_float2(p[2 * j], p[2 * j + 1]), two(keep)));
+      p[2 * j] = q.x; p[2 * j + 1] = q.y;
+      m[2 * j] = m2[j].x; m[2 * j + 1] = m2[j].y;
+      v[2 * j] = v2[j].x; v[2 * j + 1] = v2[j].y;
+    }
+  };
+  // (the sum of a lane's second moments tells whether one of them is infinite: half an instruction per element)
+  const float2 sum = add2(add2(v2[0], v2[1]), add2(v2[2], v2[3]));
+  if (sum.x + sum.y <= FLT_MAX) update([](float2 x) { return root2(x); });
+  else update([](float2 x) { return any_root2(x); });
   store8<VEC>(to.p + e, p, lane, left);
   if (to.copy) store8<VEC>(to.copy + e, p, lane, left);
   if constexpr (BITS == 32) {
@@ -319,6 +335,11 @@ __device__ __forceinline__ void finish(const Raw<P, G, BITS>& x, const StepArgs&
     S = block_max(S); R = block_max(R);
     S = S < kTiny ? 0.f : S;
     R = R < kTiny ? 0.f : R;
+    if (R > kMostRoot) {
+      R = kMostRoot;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) root[j] = make_float2(fminf(root[j].x, kMostRoot), fminf(root[j].y, kMostRoot));
+    }
     const float is = S == 0.f ? 0.f : 1.f / S, ir = R == 0.f ? 0.f : 1.f / R;
     const unsigned h0 = (to.s0 + (unsigned)(e + at<VEC>(0, lane))) * 0x9e3779b1u + A.key;
     unsigned wm[2], wv[2], cm[4], cv[4];

@@ -1,9 +1,11 @@
 """Edges of the training operators' domain that a user meets: nothing to sum over, values that overflow or underflow, images cut out
 of wider ones, tensors in other dense orders, calls from several threads and streams."""
+import math
 
 import pytest
 
 pytestmark = pytest.mark.gpu
+E = 2.0 ** -24
 
 
 def _d():
@@ -24,3 +26,42 @@ def test_statistics_of_no_positions_are_nan(dtype):
         y, mean, rstd = D.group_norm(x, groups)
         assert y.shape == x.shape and mean.shape == rstd.shape == (N, groups)
         assert torch.isnan(mean).all() and torch.isnan(rstd).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_a_second_moment_that_overflows_stops_its_parameter(bits, offset):
+    # (1 - b2) g^2 is above fp32's range for |g| = 1e21: v' is infinite, m' is not, and m'/inf = 0 leaves the parameter to its decay.
+    # 8-bit codes hold such a block at the largest scale whose square is finite, so that no value of the block is lost.
+    torch, D = _d()
+    n, at = 700, 300
+    g0 = torch.Generator(device="cuda").manual_seed(1)
+    p = torch.randn(n + offset, generator=g0, device="cuda")[offset:]
+    g = torch.randn(n + offset, generator=g0, device="cuda")[offset:]
+    q, clean = p.clone(), g.clone()
+    g[at] = -1e21
+    opt, ref = D.AdamW([p], [g], state_bits=bits), D.AdamW([q], [clean], state_bits=bits)
+    st, sr = opt.new_state(), ref.new_state()
+    was = p.clone()
+    h = dict(lr=1e-2, beta1=0.9, beta2=0.999, weight_decay=0.1)
+    opt.step(*st, t=1, **h)
+    ref.step(*sr, t=1, **h)
+    others = torch.arange(n, device="cuda") != at
+    assert torch.equal(p[others], q[others])
+    assert abs(float(p[at]) - float(was[at]) * (1 - 1e-3)) <= 2 * E * abs(float(was[at]))
+    if bits == 32:
+        assert torch.equal(st[0][:n][others], sr[0][:n][others]) and torch.equal(st[1][:n][others], sr[1][:n][others])
+        assert math.isinf(float(st[1][at])) and abs(float(st[0][at]) + 1e20) < 1e14
+    else:
+        assert torch.isfinite(st[2]).all() and torch.isfinite(st[3]).all() and float(st[3][1]) > 1.8e19
+        m, v = opt.moments(*st)
+        assert torch.isfinite(m).all() and torch.isfinite(v).all() and float(v[at]) > 3.3e38 and (v[:n] > 0).all()
+        out = torch.arange(768, device="cuda") // 256 != 1                    # the other blocks
+        rm, rv = ref.moments(*sr)
+        assert torch.equal(m[out], rm[out]) and torch.equal(v[out], rv[out])
+    # and the next step
+    g[at] = 0.5
+    was = p.clone()
+    opt.step(*st, t=2, **h)
+    # (8 bits: v' is held at 2^128 (1 - 2^-22) at most, which lets lr * 0.9e20/0.19 / (1.84e19/0.0447) through)
+    assert torch.isfinite(p).all() and abs(float(p[at]) - float(was[at]) * (1 - 1e-3)) <= 2 * E * abs(float(was[at])) + (0.012 if bits == 8 else 0)
