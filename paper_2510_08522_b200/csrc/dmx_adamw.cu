@@ -76,6 +76,7 @@ struct StepArgs {
   float *m_scale, *v_scale;
   const float* grad_scale;
   float b1, omb1, b2, omb2, eps, keep, rs_bc2, step, one;
+  float quick_from;       // sum of a lane's second moments from which root2 serves
   unsigned key;
 };
 
@@ -191,7 +192,8 @@ __device__ __forceinline__ unsigned pack4(const unsigned* c) {     // the low by
 // of elementary functions on the IBM RISC System/6000 processor", 1990), for what decides a code. A code is
 // read again in the next step, so a last bit there would grow into the parameters; the values that the codes
 // come from are therefore rounded operation by operation, as the formulas are written, and the codes are
-// those of plain fp32 arithmetic. Under 2e-31 the root loses accuracy, not its sign.
+// those of plain fp32 arithmetic. The root is right to a unit in the last place from 5e-35 on (the guard's share of the
+// approximation's error, squared by the correction); below that it comes out too small.
 __device__ __forceinline__ float rsqrt_near(float x) {
   float y;
   asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -204,9 +206,12 @@ __device__ __forceinline__ float2 root2(float2 x) {
   const float2 e = fma2(make_float2(-s.x, -s.y), s, x);
   return fma2(e, mul2(y, two(0.5f)), s);
 }
-// An infinite second moment (a finite gradient above 1.8e19) has an infinite root, and its update is zero.
+// The root of any second moment. An infinite one (a finite gradient above 1.8e19) has an infinite root, and its update is
+// zero. Small ones are taken 2^96 times as large, where the remainder is exact.
 __device__ __forceinline__ float2 any_root2(float2 x) {
-  const float2 r = root2(x);
+  const float2 up = make_float2(x.x < 0x1p-60f ? 0x1p96f : 1.f, x.y < 0x1p-60f ? 0x1p96f : 1.f);
+  const float2 down = make_float2(x.x < 0x1p-60f ? 0x1p-48f : 1.f, x.y < 0x1p-60f ? 0x1p-48f : 1.f);
+  const float2 r = mul2(root2(mul2(x, up)), down);
   return make_float2(x.x == INFINITY ? INFINITY : r.x, x.y == INFINITY ? INFINITY : r.y);
 }
 __device__ __forceinline__ float2 quotient2(float2 a, float b, float rcp_b) {
@@ -315,9 +320,11 @@ __device__ __forceinline__ void finish(const Raw<P, G, BITS>& x, const StepArgs&
       v[2 * j] = v2[j].x; v[2 * j + 1] = v2[j].y;
     }
   };
-  // (the sum of a lane's second moments tells whether one of them is infinite: half an instruction per element)
-  const float2 sum = add2(add2(v2[0], v2[1]), add2(v2[2], v2[3]));
-  if (sum.x + sum.y <= FLT_MAX) update([](float2 x) { return root2(x); });
+  // The sum of a lane's second moments tells whether one is infinite, and whether all are so small that their codes would
+  // show the quick root's error (a small one beside larger ones has a code of a few units at most): half an instruction per element.
+  const float2 pair = add2(add2(v2[0], v2[1]), add2(v2[2], v2[3]));
+  const float sum = pair.x + pair.y;
+  if (__builtin_expect((sum <= FLT_MAX && sum >= A.quick_from) || sum == 0.f, 1)) update([](float2 x) { return root2(x); });
   else update([](float2 x) { return any_root2(x); });
   store8<VEC>(to.p + e, p, lane, left);
   if (to.copy) store8<VEC>(to.copy + e, p, lane, left);
@@ -706,6 +713,9 @@ int dmx_adamw_step(dmx_adamw* h, void* m, void* v, float* m_scale, float* v_scal
   A.keep = (float)(1.0 - lr * weight_decay);
   A.rs_bc2 = (float)(1.0 / sqrt(1.0 - pow(beta2, (double)t)));
   A.step = (float)(lr / (1.0 - pow(beta1, (double)t)));
+  // Where v' < 5e-35 the quick root is off by up to 7e-18, which eps hides in the denominator if half its last place is more
+  // than that; otherwise every root is taken with care.
+  A.quick_from = (double)A.eps >= 7e-18 * 0x1p25 * (double)A.rs_bc2 ? 1e-26f : INFINITY;
   A.key = seed * 0x85ebca6bu + 0x1b873593u;
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const bool pf = h->param_dtype == DMX_F32, gf = h->grad_dtype == DMX_F32;

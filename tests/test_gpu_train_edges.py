@@ -65,3 +65,50 @@ def test_a_second_moment_that_overflows_stops_its_parameter(bits, offset):
     opt.step(*st, t=2, **h)
     # (8 bits: v' is held at 2^128 (1 - 2^-22) at most, which lets lr * 0.9e20/0.19 / (1.84e19/0.0447) through)
     assert torch.isfinite(p).all() and abs(float(p[at]) - float(was[at]) * (1 - 1e-3)) <= 2 * E * abs(float(was[at])) + (0.012 if bits == 8 else 0)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_tiny_second_moments_with_no_epsilon(bits):
+    # the first step without eps and decay is lr * sign(g), whatever g's size. v' = (1-b2) g^2 is rounded in units of 2^-149 where
+    # it is subnormal (three roundings, half of it after the root); everything else is relative: 5 e for m', 14 e for the
+    # quotient, 3 e for the parameter.
+    torch, D = _d()
+    size = torch.logspace(-20.5, 3, 2048, dtype=torch.float64, device="cuda")
+    sign = torch.where(torch.arange(2048, device="cuda") % 3 == 0, -1.0, 1.0)
+    g = (size * sign).float()
+    p = torch.zeros(2048, device="cuda")
+    opt = D.AdamW([p], [g], state_bits=bits)
+    st = opt.new_state()
+    opt.step(*st, t=1, lr=1.0, eps=0.0, weight_decay=0.0, beta1=0.9, beta2=0.999)
+    v = 1e-3 * g.double() ** 2
+    tol = 22 * E + 1.5 * 2.0 ** -149 / v
+    err = (p.double() + sign).abs()
+    assert torch.all(err <= tol), float((err / tol).max())
+    if bits == 8:
+        want = v.view(-1, 256).amax(1).sqrt()
+        assert torch.all((st[3].double() - want).abs() <= want * (8 * E + 1.5 * 2.0 ** -149 / want ** 2) + 1.2e-38)
+    # a later step with a small eps of its own, moments given
+    if bits == 32:
+        st[0].copy_(g)
+        st[1].copy_(g.square())
+        q0 = p.clone()
+        g0, v0 = st[0].double(), st[1].double()
+        opt.bind([torch.zeros_like(g)])
+        opt.step(*st, t=5, lr=1.0, eps=1e-20, weight_decay=0.0, beta1=0.9, beta2=0.999)
+        want = q0.double() - 0.9 * g0 / (1 - 0.9 ** 5) / ((0.999 * v0).sqrt() / math.sqrt(1 - 0.999 ** 5) + 1e-20)
+        scale = (want - q0.double()).abs()
+        keep = v0 > 0
+        assert torch.all(((p.double() - want).abs() <= scale * (25 * E + 2.0 ** -149 / v0) + 2 * E * (want.abs() + 1))[keep])
+
+
+def test_a_block_that_is_all_tiny_keeps_its_second_moments():
+    # 8-bit codes of a block whose largest sqrt(v') is 1e-19: its scale is the root, to rounding
+    torch, D = _d()
+    for size in (3e-21, 1e-18, 3e-17, 1e-15):
+        g = torch.full((256,), size, device="cuda")
+        opt = D.AdamW([torch.zeros(256, device="cuda")], [g], state_bits=8)
+        st = opt.new_state()
+        opt.step(*st, t=1, lr=0.0)
+        v = 1e-3 * float(g[0]) ** 2
+        assert abs(float(st[3][0]) - math.sqrt(v)) <= math.sqrt(v) * (8 * E + 1.5 * 2.0 ** -149 / v), size
+        assert (st[1] == 255).all()
