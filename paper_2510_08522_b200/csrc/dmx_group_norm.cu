@@ -26,6 +26,7 @@
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
+#include <atomic>
 
 #include "dmx_act.cuh"
 #include "dmx_host.h"
@@ -831,6 +832,7 @@ int lcm(int a, int b) {
 constexpr int kMostSlots = 128;               // what the error bound of a thread's sums is taken for
 constexpr size_t kMostData = 100 * 1024;     // two CTAs per SM
 constexpr int64_t kChunkData = 64 * 1024;    // chunks of a larger image: three
+constexpr size_t kMostShared = 200 * 1024;   // of a plan, with its sums and parameters
 
 // The rest of a plan whose slab width and parts are chosen; false if its slots need more than `most` bytes.
 bool settle(Plan& p, int64_t L, int C, int cpg, int e, bool backward, int64_t rows, size_t most) {
@@ -852,7 +854,7 @@ bool settle(Plan& p, int64_t L, int C, int cpg, int e, bool backward, int64_t ro
   if (backward) p.smem = data + f * (padded(2 * erows * p.W) + 4 * sums * padded(p.W) + 2 * padded(groups));
   else p.smem = data + f * (2 * padded(erows * p.cols * (p.V / p.fold)) + padded(erows) + (4 * sums + 2) * padded(groups));
   p.smem += 2 * f * params_size(p.W, groups);
-  if (p.smem > 200 * 1024) return false;
+  if (p.smem > kMostShared) return false;
   return true;
 }
 
@@ -904,9 +906,18 @@ Plan plan(int64_t N, int64_t L, int C, int cpg, int dtype, bool vec, bool backwa
   return p;
 }
 
-template <typename K>
-int launch(K kernel, const Plan& p, const Args& A, bool cluster, cudaStream_t st) {
-  if (p.smem > 48 * 1024 && !dmxh::cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)p.smem))) return DMX_ERR_CUDA;
+// A kernel's limit of shared memory belongs to the kernel, not to a launch, and host threads share it: it is raised once per
+// device, to the most that any plan takes.
+template <auto kernel>
+int launch(const Plan& p, const Args& A, bool cluster, cudaStream_t st) {
+  static std::atomic<uint64_t> raised{0};
+  int device = 0;
+  if (!dmxh::cuda_ok(cudaGetDevice(&device))) return DMX_ERR_CUDA;
+  const uint64_t bit = (uint64_t)1 << (device & 63);
+  if (device > 63 || !(raised.load(std::memory_order_relaxed) & bit)) {
+    if (!dmxh::cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared))) return DMX_ERR_CUDA;
+    raised.fetch_or(bit, std::memory_order_relaxed);
+  }
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(p.threads);
   cfg.dynamicSmemBytes = p.smem;
@@ -957,19 +968,19 @@ int start(int64_t ctas, int rows, int threads, cudaStream_t st, void (*kernel)(P
 template <typename T, int V, int ACT>
 int run_act(bool backward, const Plan& p, const Args& A, cudaStream_t st) {
   if (backward) {
-    if (p.resident) return launch(backward_kernel<T, V, RESIDENT, ACT>, p, A, true, st);
-    int rc = launch(backward_kernel<T, V, STATS, ACT>, p, A, false, st);
+    if (p.resident) return launch<backward_kernel<T, V, RESIDENT, ACT>>(p, A, true, st);
+    int rc = launch<backward_kernel<T, V, STATS, ACT>>(p, A, false, st);
     if (rc != DMX_OK) return rc;
     rc = start((int64_t)2 * A.N * ((A.C + 31) / 32), 1, 256, st, join_rows_kernel, A.part, A.part + 2 * (int64_t)A.N * A.parts * A.C, A.N, A.parts, A.C);
-    return rc != DMX_OK ? rc : launch(backward_kernel<T, V, APPLY, ACT>, p, A, false, st);
+    return rc != DMX_OK ? rc : launch<backward_kernel<T, V, APPLY, ACT>>(p, A, false, st);
   }
-  if (p.resident) return launch(forward_kernel<T, V, RESIDENT, ACT>, p, A, true, st);
-  int rc = launch(forward_kernel<T, V, STATS, DMX_ACT_NONE>, p, A, false, st);
+  if (p.resident) return launch<forward_kernel<T, V, RESIDENT, ACT>>(p, A, true, st);
+  int rc = launch<forward_kernel<T, V, STATS, DMX_ACT_NONE>>(p, A, false, st);
   if (rc != DMX_OK) return rc;
   const int64_t groups = (int64_t)A.N * A.G;
   rc = start((groups + 7) / 8, 1, 256, st, join_groups_kernel, reinterpret_cast<const float2*>(A.part), groups, A.parts, A.rows, A.L, A.G, A.cpg, A.eps,
              A.mean, A.rstd);
-  return rc != DMX_OK ? rc : launch(forward_kernel<T, V, APPLY, ACT>, p, A, false, st);
+  return rc != DMX_OK ? rc : launch<forward_kernel<T, V, APPLY, ACT>>(p, A, false, st);
 }
 
 template <typename T, int V>

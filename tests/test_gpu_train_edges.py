@@ -1,6 +1,8 @@
 """Edges of the training operators' domain that a user meets: nothing to sum over, values that overflow or underflow, images cut out
 of wider ones, tensors in other dense orders, calls from several threads and streams."""
+import ctypes
 import math
+import threading
 
 import pytest
 
@@ -112,3 +114,34 @@ def test_a_block_that_is_all_tiny_keeps_its_second_moments():
         v = 1e-3 * float(g[0]) ** 2
         assert abs(float(st[3][0]) - math.sqrt(v)) <= math.sqrt(v) * (8 * E + 1.5 * 2.0 ** -149 / v), size
         assert (st[1] == 255).all()
+
+
+def test_group_norm_from_two_threads():
+    # two sizes of one kernel whose shared memory differs, launched through the C entry by two host threads
+    torch, D = _d()
+    from paper_2510_08522_b200 import binding as B
+    L = B.lib()
+    bad = {}
+
+    def work(name, positions):
+        torch.cuda.set_device(0)
+        s = torch.cuda.Stream()
+        with torch.cuda.stream(s):
+            x = torch.randn(300, positions, 32, device="cuda")
+            y, mean, rstd = torch.empty_like(x), torch.empty(300, 4, device="cuda"), torch.empty(300, 4, device="cuda")
+            f = L.dmx_group_norm_forward
+            args = (300, positions, 32, 4, B.F32, x.data_ptr(), positions * 32, 32, None, None, ctypes.c_float(1e-5), 0, y.data_ptr(), positions * 32, 32,
+                    mean.data_ptr(), rstd.data_ptr(), None, 0, s.cuda_stream)
+            f(*args)
+            go.wait()
+            codes = [f(*args) for _ in range(4000)]
+        s.synchronize()
+        bad[name] = [c for c in codes if c != B.OK]
+
+    go = threading.Barrier(2)
+    ts = [threading.Thread(target=work, args=a) for a in (("large", 768), ("small", 448))]
+    for t in ts:
+        t.start()
+    for t in ts:
+        t.join()
+    assert bad == {"large": [], "small": []}, {k: (len(v), v[:3]) for k, v in bad.items()}
