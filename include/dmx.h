@@ -545,7 +545,8 @@ int dmx_group_norm_backward(int64_t N, int64_t L, int C, int G, int dtype, const
  * y may be the residual itself. K = 0 gives z = bias; M = 0 gives dW = 0 and dbias = 0. Results are bitwise reproducible.
  *   dmx_linear_status   every wait inside the kernels is bounded; *errors (HOST) receives how many warps gave up
  *                       on the current device since the last call (0 unless the device misbehaves; results
- *                       are invalid otherwise). Synchronous.
+ *                       are invalid otherwise). Waits for everything issued to the device so far, on whatever stream, and
+ *                       counts it; not inside a stream capture.
  * Errors: DMX_ERR_ARG (extents > DMX_LINEAR_MAX_EXTENT, strides, null pointers, workspace too small), DMX_ERR_ALIGN, DMX_ERR_CUDA.
  */
 #define DMX_LINEAR_MAX_EXTENT 4194240

@@ -25,6 +25,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 #include <atomic>
+#include <mutex>
 
 #include "dmx_act.cuh"
 #include "dmx_host.h"
@@ -948,10 +949,17 @@ int dmx_linear_backward(int64_t M, int64_t N, int64_t K, const void* dy, int64_t
 
 int dmx_linear_status(int* errors) {
   if (!errors) return DMX_ERR_ARG;
+  // The kernels' count only grows, so nothing is lost between a read and a reset; what was reported is kept here.
+  static std::mutex one_at_a_time;
+  static unsigned reported[256] = {};
+  int device = 0;
+  if (!dmxh::cuda_ok(cudaGetDevice(&device)) || !dmxh::cuda_ok(cudaDeviceSynchronize())) return DMX_ERR_CUDA;
+  const std::lock_guard<std::mutex> lock(one_at_a_time);
   unsigned n = 0;
-  const unsigned zero = 0;
-  if (!dmxh::cuda_ok(cudaMemcpyFromSymbol(&n, g_gave_up, sizeof n)) || !dmxh::cuda_ok(cudaMemcpyToSymbol(g_gave_up, &zero, sizeof zero))) return DMX_ERR_CUDA;
-  *errors = (int)n;
+  if (!dmxh::cuda_ok(cudaMemcpyFromSymbol(&n, g_gave_up, sizeof n))) return DMX_ERR_CUDA;
+  unsigned& before = reported[device & 255];
+  *errors = (int)(n >= before ? n - before : n);       // (below it: the device was reset)
+  before = n;
   return DMX_OK;
 }
 

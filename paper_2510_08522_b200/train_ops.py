@@ -217,7 +217,8 @@ def linear_backward(dy, x, weight, z=None, act="none", need=(True, True, True), 
 
 
 def linear_status():
-    """How many warps of the linear kernels gave up a wait on the current device since the last call (synchronous)."""
+    """How many warps of the linear kernels gave up a wait on the current device since the last call. Waits for the
+    device's work on all streams."""
     n = ctypes.c_int()
     rc = B.lib().dmx_linear_status(ctypes.byref(n))
     if rc != B.OK:

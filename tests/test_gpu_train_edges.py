@@ -116,6 +116,20 @@ def test_a_block_that_is_all_tiny_keeps_its_second_moments():
         assert (st[1] == 255).all()
 
 
+def test_status_waits_for_work_on_every_stream():
+    torch, D = _d()
+    x = torch.ones(256, 256, dtype=torch.bfloat16, device="cuda")
+    D.linear(x, x)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)               # about a tenth of a second
+        D.linear(x, x)
+    assert D.linear_status() == 0
+    assert side.query(), "the count was taken before the product had run"
+    assert D.linear_status() == 0
+
+
 def test_group_norm_from_two_threads():
     # two sizes of one kernel whose shared memory differs, launched through the C entry by two host threads
     torch, D = _d()
