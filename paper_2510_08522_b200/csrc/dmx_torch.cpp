@@ -107,6 +107,7 @@ Images images(const at::Tensor& x) {
   const auto shape = x.sizes(), st = x.strides();
   const int64_t d = x.dim();
   Images r{shape[0], 1, shape[d - 1], st[0], st[d - 2]};
+  need(r.C <= DMX_GN_MAX_CHANNELS);                      // (the C entry takes an int)
   need(r.C <= 1 || st[d - 1] == 1);
   int64_t after = 1;                                     // positions covered by the dimensions behind i
   for (int64_t i = d - 2; i >= 1; --i) {                 // (N, H, W, C): the image's rows have to follow on

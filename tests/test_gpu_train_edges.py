@@ -116,6 +116,15 @@ def test_a_block_that_is_all_tiny_keeps_its_second_moments():
         assert (st[1] == 255).all()
 
 
+def test_channel_counts_beyond_32_bits_are_refused():
+    torch, D = _d()
+    x = torch.empty(1, 1, 2 ** 32 + 8, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(D.DmxError):
+        D.group_norm(x, 2)
+    with pytest.raises(D.DmxError):
+        D.group_norm_backward(x, x, torch.zeros(1, 2, device="cuda"), torch.ones(1, 2, device="cuda"), 2)
+
+
 def test_status_waits_for_work_on_every_stream():
     torch, D = _d()
     x = torch.ones(256, 256, dtype=torch.bfloat16, device="cuda")
