@@ -106,12 +106,17 @@ Images images(const at::Tensor& x) {
   need(x.dim() >= 3 && x.is_cuda());
   const auto shape = x.sizes(), st = x.strides();
   const int64_t d = x.dim();
-  Images r{shape[0], 1, shape[d - 1], st[0], st[d - 2]};
+  Images r{shape[0], 1, shape[d - 1], st[0], shape[d - 1]};
   need(r.C <= DMX_GN_MAX_CHANNELS);                      // (the C entry takes an int)
   need(r.C <= 1 || st[d - 1] == 1);
+  bool first = true;                                     // the innermost dimension of several positions has their stride
   int64_t after = 1;                                     // positions covered by the dimensions behind i
   for (int64_t i = d - 2; i >= 1; --i) {                 // (N, H, W, C): the image's rows have to follow on
-    need(shape[i] <= 1 || st[i] == r.row * after);
+    if (shape[i] > 1) {
+      if (first) r.row = st[i];
+      need(st[i] == r.row * after);
+      first = false;
+    }
     after *= shape[i];
   }
   r.L = after;

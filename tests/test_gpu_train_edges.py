@@ -125,6 +125,27 @@ def test_channel_counts_beyond_32_bits_are_refused():
         D.group_norm_backward(x, x, torch.zeros(1, 2, device="cuda"), torch.ones(1, 2, device="cuda"), 2)
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_images_one_position_wide_cut_out_of_wider_ones(dtype):
+    torch, D = _d()
+    g = torch.Generator(device="cuda").manual_seed(2)
+    wide = torch.randn(3, 9, 5, 16, generator=g, device="cuda").to(getattr(torch, dtype))
+    for x in (wide[:, :, 2:3], wide[:, 4:5], wide[:, 4:5, 1:2], wide[1:2, :, 2:3], wide[:, :, 2:3, 4:12], wide[:, ::2, 2:3]):
+        dense = x.contiguous()
+        want = D.group_norm(dense, 2, act="silu")
+        got = D.group_norm(x, 2, act="silu")
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        back = D.group_norm_backward(x, x, got[1], got[2], 2, act="silu")
+        assert all(torch.equal(a, b) for a, b in zip(back, D.group_norm_backward(dense, dense, want[1], want[2], 2, act="silu")))
+        out = x.clone(memory_format=torch.preserve_format)
+        room = torch.zeros(x.shape[0], x.shape[1], x.shape[2] + 2, x.shape[3], dtype=x.dtype, device="cuda")
+        if x.shape[2] == 1:
+            D.group_norm(x, 2, act="silu", out=room[:, :, 1:2])
+            assert torch.equal(room[:, :, 1:2], want[0]) and not room[:, :, 0].any() and not room[:, :, 2].any()
+        D.group_norm(out, 2, act="silu", out=out)
+        assert torch.equal(out, want[0])
+
+
 def test_status_waits_for_work_on_every_stream():
     torch, D = _d()
     x = torch.ones(256, 256, dtype=torch.bfloat16, device="cuda")
