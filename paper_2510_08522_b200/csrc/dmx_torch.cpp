@@ -58,6 +58,14 @@ double number(PyObject* o) {
   }
   return v;
 }
+bool truth(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) {
+    PyErr_Clear();
+    refuse();
+  }
+  return v == 1;
+}
 const void* in(const at::Tensor* t) { return t ? t->const_data_ptr() : nullptr; }
 void* out(const at::Tensor* t) { return t ? t->mutable_data_ptr() : nullptr; }
 
@@ -217,7 +225,7 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor &x = tensor(a[0]), &w = tensor(a[1]);
     const at::Tensor *b = maybe(a[2]), *r = maybe(a[4]), *given = maybe(a[6]);
     const int act = (int)whole(a[3]);
-    const bool save = PyObject_IsTrue(a[5]) == 1 && act != DMX_ACT_NONE;
+    const bool save = truth(a[5]) && act != DMX_ACT_NONE;
     const Rows X = rows(x), W = rows(w);
     const int64_t M = X.M, N = W.M, K = X.N;
     need(W.N == K && w.device() == x.device());
