@@ -104,7 +104,7 @@ class AdamW:
             rc = B.lib().dmx_adamw_bind(self._h, arr(self._params), arr(grads), arr(copies) if copies is not None else None, _stream(self._params[0]))
         if rc != B.OK:
             _refuse("dmx_adamw_bind", rc)
-        self._grads, self._copies = list(grads), copies      # kept alive: the handle holds their addresses
+        self._grads, self._copies = list(grads), None if copies is None else list(copies)      # kept alive: the handle holds their addresses
 
     def new_state(self):
         """(m, v, m_scale, v_scale), zeroed; the scales are None for 32-bit moments."""

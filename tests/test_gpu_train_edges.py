@@ -1,8 +1,10 @@
 """Edges of the training operators' domain that a user meets: nothing to sum over, values that overflow or underflow, images cut out
 of wider ones, tensors in other dense orders, calls from several threads and streams."""
 import ctypes
+import gc
 import math
 import threading
+import weakref
 
 import pytest
 
@@ -189,3 +191,15 @@ def test_group_norm_from_two_threads():
     for t in ts:
         t.join()
     assert bad == {"large": [], "small": []}, {k: (len(v), v[:3]) for k, v in bad.items()}
+
+
+def test_copies_stay_alive_whatever_becomes_of_the_callers_list():
+    torch, D = _d()
+    p, g = [torch.ones(300, device="cuda")], [torch.ones(300, device="cuda")]
+    copies = [torch.zeros(300, dtype=torch.bfloat16, device="cuda")]
+    ref = weakref.ref(copies[0])
+    opt = D.AdamW(p, g, copies=copies)
+    copies.clear()
+    gc.collect()
+    assert ref() is not None, "the step would write to memory that is someone else's"
+    opt.close()
