@@ -569,8 +569,9 @@ bool aligned(const void* p, unsigned a) { return (reinterpret_cast<uintptr_t>(p)
 
 // 8-bit moments need their scales, fp32 moments take none
 int check_state(const dmx_adamw* h, const void* m, const void* v, const float* ms, const float* vs) {
-  if (!m || !v || m == v) return DMX_ERR_ARG;
-  if (h->bits == 8 && (!ms || !vs || ms == vs)) return DMX_ERR_ARG;
+  const bool some = h->blocks > 0;         // (empty arrays need no address)
+  if (some && (!m || !v || m == v)) return DMX_ERR_ARG;
+  if (some && h->bits == 8 && (!ms || !vs || ms == vs)) return DMX_ERR_ARG;
   if (h->bits == 32 && (ms || vs)) return DMX_ERR_ARG;
   if (!aligned(m, 16) || !aligned(v, 16) || !aligned(ms, 4) || !aligned(vs, 4)) return DMX_ERR_ALIGN;
   return DMX_OK;
@@ -728,7 +729,7 @@ int dmx_adamw_step(dmx_adamw* h, void* m, void* v, float* m_scale, float* v_scal
 int dmx_adamw_moments(dmx_adamw* h, const void* m, const void* v, const float* m_scale, const float* v_scale, int out_dtype,
                       void* out_m, void* out_v, void* cuda_stream) {
   if (!live(h)) return DMX_ERR_HANDLE;
-  if (h->bits != 8 || !out_m || !out_v || out_m == out_v || (out_dtype != DMX_F32 && out_dtype != DMX_BF16)) return DMX_ERR_ARG;
+  if (h->bits != 8 || (h->blocks > 0 && (!out_m || !out_v || out_m == out_v)) || (out_dtype != DMX_F32 && out_dtype != DMX_BF16)) return DMX_ERR_ARG;
   int rc = check_state(h, m, v, m_scale, v_scale);
   if (rc != DMX_OK) return rc;
   if (!aligned(out_m, 16) || !aligned(out_v, 16)) return DMX_ERR_ALIGN;

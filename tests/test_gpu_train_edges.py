@@ -203,3 +203,16 @@ def test_copies_stay_alive_whatever_becomes_of_the_callers_list():
     gc.collect()
     assert ref() is not None, "the step would write to memory that is someone else's"
     opt.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_model_of_empty_tensors(bits):
+    torch, D = _d()
+    opt = D.AdamW([torch.empty(0, device="cuda"), torch.empty(3, 0, device="cuda")], [torch.empty(0, device="cuda"), None], state_bits=bits)
+    st = opt.new_state()
+    n = opt.grad_norm(1.0)
+    assert float(n[0]) == 0 and float(n[1]) == 1
+    opt.step(*st, t=1, lr=1e-3, grad_scale=n[1:])
+    if bits == 8:
+        m, v = opt.moments(*st)
+        assert m.numel() == v.numel() == 0
