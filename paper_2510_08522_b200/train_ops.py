@@ -61,8 +61,8 @@ def _ptr(x):
 class AdamW:
     """AdamW over a list of tensors (dmx_adamw_*). The tensors stay the caller's and are updated in place.
 
-    params, grads: lists of CUDA tensors, any shapes, dense; one dtype (fp32 or bf16) for all of each list. A None
-    gradient leaves its tensor alone. copies: bf16 tensors that receive the updated parameters (entries may be None).
+    params, grads: lists of CUDA tensors, any shapes, dense; one dtype (fp32 or bf16) for all of each list, that of gradients
+    set by the first one bound. A None gradient leaves its tensor alone. copies: bf16 tensors that receive the updated parameters (entries may be None).
     decay: one truth value per tensor (default: all). state_bits: 32 or 8.
     The moments are the caller's too: `new_state()` makes zeroed ones, `state_view(x, i)` is tensor i's part.
     """
@@ -74,36 +74,49 @@ class AdamW:
         if n == 0 or (decay is not None and len(decay) != n) or params[0].dtype not in _dtypes or not params[0].is_cuda:
             _refuse("AdamW (params)")
         self.device, self.bits, self._params, self._dtype = params[0].device, int(state_bits), params, params[0].dtype
-        self._grad_dtype = next((g.dtype for g in grads if g is not None), torch.float32)
-        if self._grad_dtype not in _dtypes:
-            _refuse("AdamW (gradient dtype)")
         self._sizes = [p.numel() for p in params]
+        self._decay = None if decay is None else [1 if d else 0 for d in decay]
+        self._grad_dtype, self._settled, self._set_aside = None, False, []     # settled: a gradient has shown the type
+        self._create(next((g.dtype for g in grads if g is not None), torch.float32))
+        self.blocks = B.lib().dmx_adamw_blocks(self._h)
+        self.bind(grads, copies)
+
+    def _create(self, grad_dtype):
+        if grad_dtype not in _dtypes:
+            _refuse("AdamW (gradient dtype)")
+        n = len(self._sizes)
         sizes = (ctypes.c_int64 * n)(*self._sizes)
-        dec = None if decay is None else (ctypes.c_uint8 * n)(*[1 if d else 0 for d in decay])
+        dec = None if self._decay is None else (ctypes.c_uint8 * n)(*self._decay)
         h = ctypes.c_void_p()
-        with torch.cuda.device(self.device):
-            rc = B.lib().dmx_adamw_create(n, sizes, dec, _dtypes[self._dtype], _dtypes[self._grad_dtype], self.bits, ctypes.byref(h))
+        with _torch.cuda.device(self.device):
+            rc = B.lib().dmx_adamw_create(n, sizes, dec, _dtypes[self._dtype], _dtypes[grad_dtype], self.bits, ctypes.byref(h))
         if rc != B.OK:
             _refuse("dmx_adamw_create", rc)
-        self._at = h.value
+        if self._h:
+            self._set_aside.append(self._h)      # a captured step may still read its tables
+        self._grad_dtype, self._at = grad_dtype, h.value
         self._h, self._destroy = h, B.lib().dmx_adamw_destroy     # (module globals may be gone when __del__ runs)
-        self.blocks = B.lib().dmx_adamw_blocks(h)
-        self.bind(grads, copies)
 
     def bind(self, grads, copies=None):
         """Take these gradient (and copy) tensors from now on; needed when their memory moves."""
         n = len(self._params)
         if len(grads) != n or (copies is not None and len(copies) != n):
             _refuse("AdamW.bind")
-        for xs, dtype in ((self._params, self._dtype), (grads, self._grad_dtype), (copies or [], _torch.bfloat16)):
+        given = next((g.dtype for g in grads if g is not None), self._grad_dtype)
+        if given != self._grad_dtype and self._settled:
+            _refuse("AdamW.bind (gradient dtype)")
+        for xs, dtype in ((self._params, self._dtype), (grads, given), (copies or [], _torch.bfloat16)):
             for x, size in zip(xs, self._sizes):
                 if x is not None and (x.dtype != dtype or x.numel() != size or x.device != self.device or not x.is_contiguous()):
                     _refuse("AdamW.bind (tensor)")
+        if given != self._grad_dtype:            # the first gradients there are
+            self._create(given)
         arr = lambda xs: (ctypes.c_void_p * n)(*[None if x is None else x.data_ptr() for x in xs])  # noqa: E731
         with _on(self._params[0]):
             rc = B.lib().dmx_adamw_bind(self._h, arr(self._params), arr(grads), arr(copies) if copies is not None else None, _stream(self._params[0]))
         if rc != B.OK:
             _refuse("dmx_adamw_bind", rc)
+        self._settled = self._settled or any(g is not None for g in grads)
         self._grads, self._copies = list(grads), None if copies is None else list(copies)      # kept alive: the handle holds their addresses
 
     def new_state(self):
@@ -160,8 +173,9 @@ class AdamW:
 
     def close(self):
         if getattr(self, "_h", None):
-            self._destroy(self._h)
-            self._h = self._at = None
+            for h in self._set_aside + [self._h]:
+                self._destroy(h)
+            self._h, self._at, self._set_aside = None, None, []
 
     __del__ = close
 

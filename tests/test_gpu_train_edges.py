@@ -216,3 +216,22 @@ def test_a_model_of_empty_tensors(bits):
     if bits == 8:
         m, v = opt.moments(*st)
         assert m.numel() == v.numel() == 0
+
+
+def test_gradients_that_come_later_choose_their_type():
+    torch, D = _d()
+    for later in (torch.bfloat16, torch.float32):
+        p = [torch.ones(300, device="cuda"), torch.ones(40, device="cuda")]
+        q = [x.clone() for x in p]
+        g = [torch.full((300,), 0.5, dtype=later, device="cuda"), torch.full((40,), -0.25, dtype=later, device="cuda")]
+        opt, ref = D.AdamW(p, [None, None]), D.AdamW(q, g)
+        st, sr = opt.new_state(), ref.new_state()
+        opt.step(*st, t=1, lr=0.1)
+        assert float(p[0].min()) == 1.0 and not st[0].any()            # nothing to do yet
+        opt.bind(g)
+        opt.step(*st, t=1, lr=0.1)
+        ref.step(*sr, t=1, lr=0.1)
+        assert all(torch.equal(a, b) for a, b in zip(p, q)) and torch.equal(st[1], sr[1])
+        other = torch.float32 if later == torch.bfloat16 else torch.bfloat16
+        with pytest.raises(D.DmxError):
+            opt.bind([x.to(other) for x in g])
