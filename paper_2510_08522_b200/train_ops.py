@@ -58,11 +58,31 @@ def _ptr(x):
     return None if x is None else x.data_ptr()
 
 
+def _order(x):
+    """x's (extent, stride) pairs where extents are above one; None unless its elements fill one range, each in a place of its own."""
+    dims = [(n, s) for n, s in zip(x.shape, x.stride()) if n != 1]
+    at = 1
+    for n, s in sorted(dims, key=lambda d: d[1]):
+        if s != at:
+            return None
+        at *= n
+    return dims
+
+
+def _lies_like(x, p):
+    """x has p's elements in p's order in memory (contiguous tensors of any shapes lie alike)."""
+    if x.is_contiguous() and p.is_contiguous():
+        return True
+    order = _order(x)
+    return order is not None and order == _order(p)
+
+
 class AdamW:
     """AdamW over a list of tensors (dmx_adamw_*). The tensors stay the caller's and are updated in place.
 
-    params, grads: lists of CUDA tensors, any shapes, dense; one dtype (fp32 or bf16) for all of each list, that of gradients
-    set by the first one bound. A None gradient leaves its tensor alone. copies: bf16 tensors that receive the updated parameters (entries may be None).
+    params, grads: lists of CUDA tensors, any shapes, dense in any order of dimensions (channels last, transposed), a gradient
+    in its parameter's; one dtype (fp32 or bf16) for all of each list, that of gradients set by the first one bound. A None
+    gradient leaves its tensor alone. copies: bf16 tensors that receive the updated parameters (entries may be None).
     decay: one truth value per tensor (default: all). state_bits: 32 or 8.
     The moments are the caller's too: `new_state()` makes zeroed ones, `state_view(x, i)` is tensor i's part.
     """
@@ -106,8 +126,8 @@ class AdamW:
         if given != self._grad_dtype and self._settled:
             _refuse("AdamW.bind (gradient dtype)")
         for xs, dtype in ((self._params, self._dtype), (grads, given), (copies or [], _torch.bfloat16)):
-            for x, size in zip(xs, self._sizes):
-                if x is not None and (x.dtype != dtype or x.numel() != size or x.device != self.device or not x.is_contiguous()):
+            for x, p, size in zip(xs, self._params, self._sizes):
+                if x is not None and (x.dtype != dtype or x.numel() != size or x.device != self.device or not _lies_like(x, p)):
                     _refuse("AdamW.bind (tensor)")
         if given != self._grad_dtype:            # the first gradients there are
             self._create(given)
@@ -132,7 +152,8 @@ class AdamW:
         first = B.lib().dmx_adamw_first_block(self._h, i)
         if first < 0:
             _refuse("dmx_adamw_first_block", int(first))
-        return x[first * ADAMW_BLOCK: first * ADAMW_BLOCK + self._sizes[i]].view(self._params[i].shape)
+        p, x = self._params[i], x[first * ADAMW_BLOCK: first * ADAMW_BLOCK + self._sizes[i]]
+        return x.view(p.shape) if p.is_contiguous() else x.as_strided(p.shape, p.stride())
 
     def _check(self, where, m, v, m_scale, v_scale):
         t, n = _torch, self.blocks * ADAMW_BLOCK

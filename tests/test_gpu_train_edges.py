@@ -235,3 +235,34 @@ def test_gradients_that_come_later_choose_their_type():
         other = torch.float32 if later == torch.bfloat16 else torch.bfloat16
         with pytest.raises(D.DmxError):
             opt.bind([x.to(other) for x in g])
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_dense_tensors_in_any_order(bits):
+    # AdamW takes a tensor's elements as they lie; parameter, gradient and copy have to lie alike
+    torch, D = _d()
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    mk = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+    a, b = mk(24, 5, 3, 3), mk(40, 30)
+    p = [a.to(memory_format=torch.channels_last), b.t()]
+    g = [mk(24, 5, 3, 3).to(memory_format=torch.channels_last), mk(40, 30).t()]
+    c = [torch.zeros_like(x, dtype=torch.bfloat16) for x in p]
+    assert c[0].stride() == p[0].stride()
+    flat = lambda x: x.permute(0, 2, 3, 1).reshape(-1).clone() if x.dim() == 4 else x.t().reshape(-1).clone()  # noqa: E731  (memory order)
+    q, h = [flat(x) for x in p], [flat(x) for x in g]
+    opt, ref = D.AdamW(p, g, state_bits=bits, copies=c), D.AdamW(q, h, state_bits=bits)
+    st, sr = opt.new_state(), ref.new_state()
+    for t in (1, 2):
+        opt.step(*st, t=t, lr=0.1, seed=t)
+        ref.step(*sr, t=t, lr=0.1, seed=t)
+    assert all(torch.equal(flat(x), y) for x, y in zip(p, q)) and all(torch.equal(x, y.bfloat16()) for x, y in zip(c, p))
+    m = st[0] if bits == 32 else opt.moments(*st)[0]
+    r = sr[0] if bits == 32 else ref.moments(*sr)[0]
+    for i in range(2):
+        v = opt.state_view(m, i)
+        assert v.shape == p[i].shape and torch.equal(flat(v), ref.state_view(r, i))
+    for bad in ([g[0].contiguous(), g[1]], [g[0], g[1].contiguous()], [g[0], mk(1, 1).expand(30, 40)], [g[0], mk(30, 80)[:, ::2]]):
+        with pytest.raises(D.DmxError):
+            opt.bind(bad, c)
+    one = mk(24, 1, 1, 1)                                   # where extents of one leave the order open, any strides do
+    D.AdamW([one], [torch.empty_strided((24, 1, 1, 1), (1, 24, 24, 24), device="cuda")]).close()
