@@ -8,6 +8,7 @@
 #include <ATen/core/LegacyTypeDispatch.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -65,6 +66,12 @@ bool truth(PyObject* o) {
     refuse();
   }
   return v == 1;
+}
+// An operator whose inputs require a gradient comes back through train_grad.py, which calls it again unrecorded.
+constexpr long kRecord = 1;
+template <typename... T>
+bool recorded(const at::Tensor* given, const T*... inputs) {
+  return !given && c10::GradMode::is_enabled() && ((inputs && inputs->requires_grad()) || ...);
 }
 const void* in(const at::Tensor* t) { return t ? t->const_data_ptr() : nullptr; }
 void* out(const at::Tensor* t) { return t ? t->mutable_data_ptr() : nullptr; }
@@ -152,6 +159,7 @@ PyObject* group_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor& x = tensor(a[0]);
     const long G = whole(a[1]);
     const at::Tensor *w = maybe(a[2]), *b = maybe(a[3]), *given = maybe(a[6]);
+    if (recorded(given, &x, w, b)) return PyLong_FromLong(kRecord);
     const double eps = number(a[4]);
     const int act = (int)whole(a[5]), type = type_of(x);
     const Images X = images(x);
@@ -226,6 +234,7 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor *b = maybe(a[2]), *r = maybe(a[4]), *given = maybe(a[6]);
     const int act = (int)whole(a[3]);
     const bool save = truth(a[5]) && act != DMX_ACT_NONE;
+    if (recorded(given, &x, &w, b, r)) return PyLong_FromLong(kRecord);
     const Rows X = rows(x), W = rows(w);
     const int64_t M = X.M, N = W.M, K = X.N;
     need(W.N == K && w.device() == x.device());

@@ -202,6 +202,7 @@ class AdamW:
 
 
 _fast = None
+_RECORD = 1          # the compiled module's answer where torch has to record the call
 
 
 def _module():
@@ -226,9 +227,15 @@ def _module():
 
 def group_norm(x, groups, weight=None, bias=None, eps=1e-5, act="none", out=None):
     """act(group_norm(x)) of a channels-last tensor (N, ..., C), fp32 or bf16 -> (y, mean, rstd), the statistics
-    fp32 (N, groups). weight, bias: fp32 (C,). x may be a channel slice of a wider tensor; out may be x."""
+    fp32 (N, groups). weight, bias: fp32 (C,). x may be a channel slice of a wider tensor; out may be x. Where an input
+    requires a gradient torch records the call (y's gradient; the statistics carry none), unless `out` is given."""
     r = (_fast or _module()).group_norm(x, groups, weight, bias, eps, ACT.get(act, -1), out)
-    return r if r.__class__ is tuple else _refuse("group_norm", r)
+    if r.__class__ is tuple:
+        return r
+    if r != _RECORD:
+        _refuse("group_norm", r)
+    from .train_grad import GroupNorm
+    return GroupNorm.apply(x, groups, weight, bias, eps, act)
 
 
 def group_norm_backward(dy, x, mean, rstd, groups, weight=None, bias=None, act="none", out=None):
@@ -239,9 +246,16 @@ def group_norm_backward(dy, x, mean, rstd, groups, weight=None, bias=None, act="
 
 def linear(x, weight, bias=None, act="none", residual=None, save=False, out=None):
     """act(x @ weight.T + bias) + residual, bf16 matrices -> (y, z). z is the value before the activation, kept for
-    linear_backward when `save` is set and there is an activation, else None. out may be the residual."""
+    linear_backward when `save` is set and there is an activation, else None. out may be the residual. Where an input
+    requires a gradient torch records the call (y's gradient; z carries none), unless `out` is given."""
     r = (_fast or _module()).linear(x, weight, bias, ACT.get(act, -1), residual, save, out)
-    return r if r.__class__ is tuple else _refuse("linear", r)
+    if r.__class__ is tuple:
+        return r
+    if r != _RECORD:
+        _refuse("linear", r)
+    from .train_grad import Linear
+    r = Linear.apply(x, weight, bias, act, residual, save)
+    return r if r.__class__ is tuple else (r, None)
 
 
 def linear_backward(dy, x, weight, z=None, act="none", need=(True, True, True), out=(None, None, None)):
