@@ -73,6 +73,10 @@ template <typename... T>
 bool recorded(const at::Tensor* given, const T*... inputs) {
   return !given && c10::GradMode::is_enabled() && ((inputs && inputs->requires_grad()) || ...);
 }
+// what torch's differentiation has kept of t is stale now
+void written(const at::Tensor* t) {
+  if (t && t->defined() && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
 const void* in(const at::Tensor* t) { return t ? t->const_data_ptr() : nullptr; }
 void* out(const at::Tensor* t) { return t ? t->mutable_data_ptr() : nullptr; }
 
@@ -175,6 +179,7 @@ PyObject* group_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int rc = norm_forward(X.N, X.L, (int)X.C, (int)G, type, in(&x), X.image, X.row, wp, bp, (float)eps, act, out(&y), Y.image, Y.row,
                                 static_cast<float*>(out(&mean)), static_cast<float*>(out(&rstd)), start_of(ws), bytes, call.stream);
     if (rc != DMX_OK) refuse(rc);
+    written(given);
     return tuple(&y, &mean, &rstd);
   });
 }
@@ -201,6 +206,7 @@ PyObject* group_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int rc = norm_backward(X.N, X.L, (int)X.C, (int)G, type, in(&dy), D.image, D.row, in(&x), X.image, X.row, mp, rp, wp, bp, act, out(&dx),
                                  O.image, O.row, static_cast<float*>(out(&dw)), static_cast<float*>(out(&db)), start_of(ws), bytes, call.stream);
     if (rc != DMX_OK) refuse(rc);
+    written(given);
     return tuple(&dx, &dw, &db);
   });
 }
@@ -249,6 +255,7 @@ PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int rc = linear_forward(M, N, K, in(&x), X.ld, in(&w), W.ld, in(b), act, in(r), R.ld, out(&y), Y.ld, save ? out(&z) : nullptr, N,
                                   start_of(ws), bytes, call.stream);
     if (rc != DMX_OK) refuse(rc);
+    written(given);
     return tuple(&y, &z, nullptr);
   });
 }
@@ -277,6 +284,9 @@ PyObject* linear_gradient(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int rc = linear_backward(M, N, K, in(&dy), G.ld, in(&x), X.ld, in(&w), W.ld, in(z), Z.ld, act, dx.defined() ? out(&dx) : nullptr, DX.ld,
                                    dw.defined() ? out(&dw) : nullptr, DW.ld, db.defined() ? out(&db) : nullptr, start_of(ws), bytes, call.stream);
     if (rc != DMX_OK) refuse(rc);
+    if (want & 1) written(g0);
+    if (want & 2) written(g1);
+    if (want & 4) written(g2);
     return tuple(&dx, &dw, &db);
   });
 }
@@ -304,14 +314,16 @@ PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     Call call(to);
     const int rc = adamw_norm(handle(a[0]), (float)number(a[2]), static_cast<float*>(p), call.stream);
     if (rc != DMX_OK) refuse(rc);
+    written(&to);
     return item(&to);
   });
 }
 
-// handle, device, state bits, blocks, m, v, m_scale, v_scale, grad_scale, lr, beta1, beta2, eps, weight_decay, t, seed -> None
+// handle, device, state bits, blocks, m, v, m_scale, v_scale, grad_scale, lr, beta1, beta2, eps, weight_decay, t, seed, the list of
+// parameters and copies that the step writes -> None
 PyObject* step(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    need(n == 16);
+    need(n == 17 && PyList_CheckExact(a[16]));
     const long device = whole(a[1]), blocks = whole(a[3]);
     const bool codes = whole(a[2]) == 8;
     const at::Tensor &m = tensor(a[4]), &v = tensor(a[5]);
@@ -328,6 +340,8 @@ PyObject* step(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const int rc = adamw_step(handle(a[0]), mp, vp, static_cast<float*>(msp), static_cast<float*>(vsp), static_cast<float*>(gsp), number(a[9]), number(a[10]),
                               number(a[11]), number(a[12]), number(a[13]), whole(a[14]), a[15] != Py_None, seed, call.stream);
     if (rc != DMX_OK) refuse(rc);
+    for (const at::Tensor* t : {&m, &v, ms, vs}) written(t);
+    for (Py_ssize_t i = 0; i < PyList_GET_SIZE(a[16]); ++i) written(&tensor(PyList_GET_ITEM(a[16], i)));
     Py_RETURN_NONE;
   });
 }

@@ -137,6 +137,7 @@ class AdamW:
         if rc != B.OK:
             _refuse("dmx_adamw_bind", rc)
         self._settled = self._settled or any(g is not None for g in grads)
+        self._written = [x for xs in (self._params, copies or []) for x, g in zip(xs, grads) if x is not None and g is not None]
         self._grads, self._copies = list(grads), None if copies is None else list(copies)      # kept alive: the handle holds their addresses
 
     def new_state(self):
@@ -173,7 +174,7 @@ class AdamW:
     def step(self, m, v, m_scale=None, v_scale=None, *, lr, t, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, grad_scale=None, seed=None):
         """One update. t: this step's number, from 1. seed: dither 8-bit codes with it (None: to nearest)."""
         r = self._fast.adamw_step(self._at, self.device.index, self.bits, self.blocks, m, v, m_scale, v_scale, grad_scale, lr, beta1, beta2, eps,
-                                  weight_decay, t, seed)
+                                  weight_decay, t, seed, self._written)
         if r is not None:
             _refuse("AdamW.step", r)
 
@@ -190,6 +191,7 @@ class AdamW:
                                            out_m.data_ptr(), out_v.data_ptr(), _stream(m))
         if rc != B.OK:
             _refuse("dmx_adamw_moments", rc)
+        _torch.autograd.graph.increment_version([o for o in (out_m, out_v) if not o.is_inference()])
         return out_m, out_v
 
     def close(self):

@@ -1,5 +1,5 @@
 """The training operators under torch's differentiation: gradients are those of the explicit backward calls, bit for bit, and are not
-lost silently."""
+lost silently; writes to given tensors are seen by it."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -81,3 +81,42 @@ def test_what_is_not_recorded():
     (gx,) = torch.autograd.grad(y.float().square().sum(), w, create_graph=True)
     with pytest.raises(RuntimeError):
         gx.float().sum().backward()         # first derivatives only
+
+
+def test_writes_are_seen():
+    torch, D = _d()
+    x, w = torch.ones(4, 8, dtype=torch.bfloat16, device="cuda"), torch.nn.Parameter(torch.ones(16, 8, dtype=torch.bfloat16, device="cuda"))
+    # the optimizer changes a weight between forward and backward: an error, not a wrong gradient
+    y = D.linear(x.clone().requires_grad_(True), w)[0]
+    opt = D.AdamW([w], [torch.ones_like(w)], copies=None)
+    st = opt.new_state()
+    opt.step(*st, t=1, lr=0.1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
+    n = torch.empty(2, device="cuda")
+    was = [t._version for t in (w, st[0], st[1], n)]
+    opt.grad_norm(1.0, out=n)
+    opt.step(*st, t=2, lr=0.1, grad_scale=n[1:])
+    assert all(t._version > v for t, v in zip((w, st[0], st[1], n), was))
+    # copies, 8-bit states and their values; a tensor without a gradient is left alone
+    p, q, c = torch.ones(300, device="cuda"), torch.ones(30, device="cuda"), torch.zeros(300, dtype=torch.bfloat16, device="cuda")
+    opt = D.AdamW([p, q], [torch.ones(300, device="cuda"), None], state_bits=8, copies=[c, None])
+    st = opt.new_state()
+    om, ov = torch.empty(768, device="cuda"), torch.empty(768, device="cuda")
+    seen = (p, c, *st)
+    was = [t._version for t in seen]
+    opt.step(*st, t=1, lr=0.1)
+    opt.moments(*st, om, ov)
+    assert all(t._version > v for t, v in zip(seen, was)) and q._version == 0 and om._version == ov._version == 1
+    # given outputs
+    out, dx, img = torch.empty(4, 16, dtype=torch.bfloat16, device="cuda"), torch.empty(4, 8, dtype=torch.bfloat16, device="cuda"), torch.empty(1, 4, 8, device="cuda")
+    D.linear(x, w, out=out)
+    D.linear_backward(out, x, w, need=(True, False, False), out=(dx, None, None))
+    _, mean, rstd = D.group_norm(img, 2, out=img)
+    D.group_norm_backward(img, img, mean, rstd, 2, out=img)
+    assert out._version == 1 and dx._version == 1 and img._version == 2
+    with torch.inference_mode():
+        a = torch.ones(4, 8, dtype=torch.bfloat16, device="cuda")
+        D.linear(a, a, out=torch.empty(4, 4, dtype=torch.bfloat16, device="cuda"))
+    D.linear(a, a, out=(b := torch.empty(4, 4, dtype=torch.bfloat16, device="cuda")))
+    assert (b == 8).all()
