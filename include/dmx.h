@@ -509,6 +509,9 @@ int dmx_adamw_destroy(dmx_adamw* h);   /* as dmx_destroy */
  *   mean, rstd         fp32, N*G (written by forward, read by backward); NaN where L = 0: there is nothing to average
  *   dweight, dbias     fp32, C entries, or NULL
  *   workspace          at least dmx_group_norm_workspace(...) bytes, 16-byte aligned, contents undefined
+ *   dmx_group_norm_plan   for inspection and tests (no device needed): plan (HOST) receives elements per access, whether an
+ *                      image's slab stays on the chip (0/1), CTAs that share it (or chunks of an image), items that the CTAs
+ *                      (clusters) take in turn, threads and shared memory of a CTA. wide: 16-byte accesses are possible.
  * Results are bitwise reproducible. y may be x itself, and dx may be dy or x, with the same strides.
  * Errors: DMX_ERR_ARG (C < 1, G not a divisor of C, C > DMX_GN_MAX_CHANNELS,
  * C/G > DMX_GN_MAX_GROUP, extents, strides, eps < 0, null pointers, workspace
@@ -517,6 +520,7 @@ int dmx_adamw_destroy(dmx_adamw* h);   /* as dmx_destroy */
 #define DMX_GN_MAX_CHANNELS 65536
 #define DMX_GN_MAX_GROUP 1024
 int64_t dmx_group_norm_workspace(int64_t N, int64_t L, int C, int G, int dtype, int backward);
+int dmx_group_norm_plan(int64_t N, int64_t L, int C, int G, int dtype, int wide, int backward, int64_t* plan);
 int dmx_group_norm_forward(int64_t N, int64_t L, int C, int G, int dtype, const void* x, int64_t x_image, int64_t x_row,
                            const float* weight, const float* bias, float eps, int act, void* y, int64_t y_image,
                            int64_t y_row, float* mean, float* rstd, void* workspace, int64_t workspace_bytes,
@@ -547,6 +551,9 @@ int dmx_group_norm_backward(int64_t N, int64_t L, int C, int G, int dtype, const
  *                       on the current device since the last call (0 unless the device misbehaves; results
  *                       are invalid otherwise). Waits for everything issued to the device so far, on whatever stream, and
  *                       counts it; not inside a stream capture.
+ *   dmx_linear_plan     for inspection and tests (no device needed): how a product of rows x cols over k is cut. plan (HOST)
+ *                       receives tile width, pairing of CTAs (0/1), ranges of k, exchanged operands (0/1), most tiles a CTA takes.
+ *                       rows_across: the operand that D's rows come from lies across k (dw); 0 for y and dx.
  * Errors: DMX_ERR_ARG (extents > DMX_LINEAR_MAX_EXTENT, strides, null pointers, workspace too small), DMX_ERR_ALIGN, DMX_ERR_CUDA.
  */
 #define DMX_LINEAR_MAX_EXTENT 4194240
@@ -560,6 +567,7 @@ int dmx_linear_backward(int64_t M, int64_t N, int64_t K, const void* dy, int64_t
                         const void* w, int64_t ldw, const void* z, int64_t ldz, int act, void* dx, int64_t lddx,
                         void* dw, int64_t lddw, void* dbias, void* workspace, int64_t workspace_bytes,
                         void* cuda_stream);
+int dmx_linear_plan(int64_t rows, int64_t cols, int64_t k, int rows_across, int64_t* plan);
 int dmx_linear_status(int* errors);
 
 /* Frees the tables and the scratch. NULL is accepted; a handle that is not live (destroyed

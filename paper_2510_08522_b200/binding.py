@@ -26,7 +26,8 @@ EXPORTS = ("dmx_create", "dmx_state_len", "dmx_step", "dmx_step_adam", "dmx_step
            "dmx_finalize_partials", "dmx_check_guards", "dmx_selftest_wait", "dmx_scratch_info",
            "dmx_adamw_create", "dmx_adamw_blocks", "dmx_adamw_first_block", "dmx_adamw_bind", "dmx_adamw_grad_norm", "dmx_adamw_step",
            "dmx_adamw_moments", "dmx_adamw_destroy", "dmx_group_norm_workspace", "dmx_group_norm_forward", "dmx_group_norm_backward",
-           "dmx_linear_workspace", "dmx_linear_forward", "dmx_linear_backward_workspace", "dmx_linear_backward", "dmx_linear_status")
+           "dmx_linear_workspace", "dmx_linear_forward", "dmx_linear_backward_workspace", "dmx_linear_backward", "dmx_linear_status",
+           "dmx_group_norm_plan", "dmx_linear_plan")
 CTL_ACTIONS = (-100, -25, 0, 25, 100)
 
 _lib = None
@@ -133,6 +134,10 @@ def lib():
         L.dmx_linear_backward_workspace.restype = i64
         L.dmx_linear_backward.argtypes = [i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, i64, vp, i64, vp, vp, i64, vp]
         L.dmx_linear_backward.restype = i32
+        L.dmx_group_norm_plan.argtypes = [i64, i64, i32, i32, i32, i32, i32, ctypes.POINTER(i64)]
+        L.dmx_group_norm_plan.restype = i32
+        L.dmx_linear_plan.argtypes = [i64, i64, i64, i32, ctypes.POINTER(i64)]
+        L.dmx_linear_plan.restype = i32
         L.dmx_linear_status.argtypes = [ctypes.POINTER(i32)]
         L.dmx_linear_status.restype = i32
         L.dmx_destroy.argtypes = [vp]

@@ -1049,6 +1049,13 @@ int64_t dmx_group_norm_workspace(int64_t N, int64_t L, int C, int G, int dtype, 
   return one > two ? one : two;
 }
 
+int dmx_group_norm_plan(int64_t N, int64_t L, int C, int G, int dtype, int wide_access, int backward, int64_t* out) {
+  if (!shape_ok(N, L, C, G, dtype) || N < 1 || L < 1 || !out) return DMX_ERR_ARG;
+  const Plan p = plan(N, L, C, C / G, dtype, wide_access && columns_fit(C, C / G, dtype == DMX_F32 ? 4 : 2), backward != 0);
+  out[0] = p.V; out[1] = p.resident; out[2] = p.parts; out[3] = N * p.slabs * (p.resident ? 1 : p.parts); out[4] = p.threads; out[5] = (int64_t)p.smem;
+  return DMX_OK;
+}
+
 int dmx_group_norm_forward(int64_t N, int64_t L, int C, int G, int dtype, const void* x, int64_t x_image, int64_t x_row,
                            const float* weight, const float* bias, float eps, int act, void* y, int64_t y_image,
                            int64_t y_row, float* mean, float* rstd, void* workspace, int64_t workspace_bytes,

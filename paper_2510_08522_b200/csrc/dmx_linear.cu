@@ -727,6 +727,16 @@ Choice choose(int64_t rowsA, int64_t rowsB, int kblocks, bool swap) {
   return best;
 }
 
+// 64 rows or fewer: b's rows take the 128 lanes (b keeps whichever way it lies; a, the narrow side, has to be K-major)
+struct Form {
+  bool exchanged;
+  Choice choice;
+};
+Form form_of(int64_t rowsA, int64_t rowsB, int kblocks, int mnA) {
+  const bool exchanged = rowsA <= 64 && !mnA;
+  return {exchanged, exchanged ? choose(rowsB, rowsA, kblocks, true) : choose(rowsA, rowsB, kblocks, false)};
+}
+
 template <int BN, bool SWAP, bool PAIR, int SPLIT>
 int launch_gemm(const Matrix& a, const Matrix& b, GemmArgs& A, cudaStream_t st) {
   constexpr int kHalf = PAIR ? BN / 2 : BN, kRows = PAIR ? 2 * kBM : kBM;
@@ -767,11 +777,11 @@ int product(const Matrix& a, int mnA, const Matrix& b, int mnB, int64_t k, const
   A.vecy = aligned(A.y, 16) && (rowsA <= 1 || A.ldy % 8 == 0);
   A.vecz = A.z && aligned(A.z, 16) && (rowsA <= 1 || A.ldz % 8 == 0);
   A.vecr = A.residual && aligned(A.residual, 16) && (rowsA <= 1 || A.ldr % 8 == 0);
-  // 64 rows or fewer: b's rows take the 128 lanes (b keeps whichever way it lies; a, the narrow side, has to be K-major)
-  if (rowsA <= 64 && !mnA) {
+  const Form f = form_of(rowsA, rowsB, A.kblocks, mnA);
+  const Choice& c = f.choice;
+  if (f.exchanged) {
     A.rowsA = (int)rowsB; A.rowsB = (int)rowsA;
     A.mnA = mnB; A.mnB = mnA;
-    const Choice c = choose(rowsB, rowsA, A.kblocks, true);
     if (c.bn == 32) {
       if (c.split == 4) return launch_gemm<32, true, false, 4>(b, a, A, st);
       return c.split == 2 ? launch_gemm<32, true, false, 2>(b, a, A, st) : launch_gemm<32, true, false, 1>(b, a, A, st);
@@ -781,7 +791,6 @@ int product(const Matrix& a, int mnA, const Matrix& b, int mnB, int64_t k, const
   }
   A.rowsA = (int)rowsA; A.rowsB = (int)rowsB;
   A.mnA = mnA; A.mnB = mnB;
-  const Choice c = choose(rowsA, rowsB, A.kblocks, false);
   if (c.pair) return c.bn == 256 ? launch_gemm<256, false, true, 1>(a, b, A, st) : launch_gemm<128, false, true, 1>(a, b, A, st);
   if (c.bn == 256) return launch_gemm<256, false, false, 1>(a, b, A, st);
   if (c.bn == 128) return c.split == 2 ? launch_gemm<128, false, false, 2>(a, b, A, st) : launch_gemm<128, false, false, 1>(a, b, A, st);
@@ -945,6 +954,16 @@ int dmx_linear_backward(int64_t M, int64_t N, int64_t K, const void* dy, int64_t
     rc = product(g, 1, a, 1, M, E, st);
   }
   return rc;
+}
+
+int dmx_linear_plan(int64_t rows, int64_t cols, int64_t k, int rows_across, int64_t* plan) {
+  if (!extents_ok(rows, cols, k) || rows < 1 || cols < 1 || k < 1 || !plan) return DMX_ERR_ARG;
+  const Form f = form_of(rows, cols, (int)((k + kBK - 1) / kBK), rows_across);
+  const int64_t r = f.exchanged ? cols : rows, c = f.exchanged ? rows : cols, high = f.choice.pair ? 2 * kBM : kBM, at_once = f.choice.pair ? 74 : 148;
+  const int64_t tiles = ((r + high - 1) / high) * ((c + f.choice.bn - 1) / f.choice.bn);
+  plan[0] = f.choice.bn; plan[1] = f.choice.pair; plan[2] = f.choice.split; plan[3] = f.exchanged;
+  plan[4] = f.choice.split > 1 ? 1 : (tiles + at_once - 1) / at_once;
+  return DMX_OK;
 }
 
 int dmx_linear_status(int* errors) {
