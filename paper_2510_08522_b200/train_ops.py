@@ -91,6 +91,8 @@ class AdamW:
         torch = _t()
         self._h, self._fast = None, _module()
         params, n = list(params), len(params)
+        if not all(isinstance(p, torch.Tensor) for p in params) or not all(g is None or isinstance(g, torch.Tensor) for g in grads):
+            _refuse("AdamW (what is no tensor)")
         if n == 0 or (decay is not None and len(decay) != n) or params[0].dtype not in _dtypes or not params[0].is_cuda:
             _refuse("AdamW (params)")
         self.device, self.bits, self._params, self._dtype = params[0].device, int(state_bits), params, params[0].dtype
@@ -122,6 +124,8 @@ class AdamW:
         n = len(self._params)
         if len(grads) != n or (copies is not None and len(copies) != n):
             _refuse("AdamW.bind")
+        if not all(x is None or isinstance(x, _torch.Tensor) for x in (*grads, *(copies or []))):
+            _refuse("AdamW.bind (what is no tensor)")
         given = next((g.dtype for g in grads if g is not None), self._grad_dtype)
         if given != self._grad_dtype and self._settled:
             _refuse("AdamW.bind (gradient dtype)")

@@ -266,3 +266,14 @@ def test_dense_tensors_in_any_order(bits):
             opt.bind(bad, c)
     one = mk(24, 1, 1, 1)                                   # where extents of one leave the order open, any strides do
     D.AdamW([one], [torch.empty_strided((24, 1, 1, 1), (1, 24, 24, 24), device="cuda")]).close()
+
+
+def test_entries_that_are_no_tensors_are_refused():
+    torch, D = _d()
+    p, g = torch.ones(30, device="cuda"), torch.ones(30, device="cuda")
+    for params, grads, copies in (([p, None], [g, None], None), ([p], [1.0], None), ([p], ["g"], None), ([p], [g], [3])):
+        with pytest.raises(D.DmxError):
+            D.AdamW(params, grads, copies=copies)
+    opt = D.AdamW([p], [g])
+    with pytest.raises(D.DmxError):
+        opt.bind([0])
