@@ -433,7 +433,8 @@ int dmx_step_static(int K, int64_t P, const int64_t* seg_offsets, int S, int gra
  */
 
 /* activations of dmx_group_norm_* and dmx_linear_*: u, max(u, 0), u / (1 + exp(-u)), u * Phi(u) (Phi: the normal
- * distribution function, the erf form). The slope of DMX_ACT_RELU at 0 is 0. */
+ * distribution function, the erf form). The slope of DMX_ACT_RELU at 0 is 0. All are computed in fp32: Phi to 3e-7 absolutely (so
+ * that u * Phi(u) is good to 4e-6 of itself at u = -2 and to 5e-4 at u = -4), exponentials and reciprocals to 2 ulp. */
 enum { DMX_ACT_NONE = 0, DMX_ACT_RELU = 1, DMX_ACT_SILU = 2, DMX_ACT_GELU = 3 };
 
 /*
@@ -455,7 +456,9 @@ enum { DMX_ACT_NONE = 0, DMX_ACT_RELU = 1, DMX_ACT_SILU = 2, DMX_ACT_GELU = 3 };
  *                   (|x|/scale)^(1/2), or, with dither != 0, floor(that + u) with u in [0,1) in steps of 2^-16
  *                   from a hash of the element's state index (low 32 bits) and `seed`: give every step another
  *                   seed. A nonzero second moment keeps a nonzero code; an infinite one is held as 3.4e38. Dithering is what lets a second moment
- *                   decay: a change of 0.1 % is far below half a code.
+ *                   decay: a change of 0.1 % is far below half a code. It is unbiased in the code x, not in the value, whose mean
+ *                   comes out larger by 6 f (1-f) / x^2 of itself for x^4 (f: x's fraction): a second moment at code c without
+ *                   gradient loses 1 - 1.5/c of what beta2 takes away, until it rests at code 1.
  *
  *   dmx_adamw_create     sizes: HOST, n entries >= 0 (n in 1..DMX_ADAMW_MAX_TENSORS); decay: HOST, n bytes, or
  *                        NULL for all 1; param_dtype, grad_dtype: DMX_F32 or DMX_BF16. Synchronous.
@@ -498,8 +501,9 @@ int dmx_adamw_destroy(dmx_adamw* h);   /* as dmx_destroy */
  * backward, with xh = (x - mean)*rstd, du = dy * act'(u), n = L*C/G and sums over the group:
  *   dweight = sum over images and positions of du*xh, dbias = the same of du,
  *   dx = rstd * (weight*du - (sum(weight*du) + xh * sum(weight*du*xh)) / n)
- * All arithmetic and all sums are fp32 (variances from deviations of the mean, never from a difference of
- * squares); y and dx are rounded once. Group norm's statistics do not depend on the batch size, which is why
+ * All arithmetic and all sums are fp32; y and dx are rounded once. A variance is summed from deviations: a thread's (at
+ * most 128 values) from its first value, corrected by their mean, the threads', CTAs' and chunks' from one another's means, so
+ * a mean far from zero costs no accuracy. Group norm's statistics do not depend on the batch size, which is why
  * it is the norm to use where a controller changes that.
  *   x, y, dy, dx       element (n, l, c) at n*image + l*row + c, strides in elements >= 0; x and dy may repeat rows or
  *                      images with strides 0 (a broadcast gradient); y and dx have each element in a place of its

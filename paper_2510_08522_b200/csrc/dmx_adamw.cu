@@ -16,8 +16,8 @@
 //
 // Bound: HBM. A step moves 8 + grad + states (16, or 4 with 8-bit codes) + copy bytes per element. Measured on
 // B200: 138 M parameters, all fp32: 566 us = 6.85 TB/s (measured copy rate 6.55); 340 M parameters, bf16
-// gradients and copies, 8-bit moments: 920 us = 5.9 TB/s, where some 70 instructions per element (a third of them the
-// dither) keep the issue slots nearly as busy as the memory; without dither 895 us. A warp owns one block of 256 elements (its scales need a maximum over the block:
+// gradients and copies, 8-bit moments: 938 us = 5.8 TB/s, where some 75 instructions per element (a third of them the
+// dither) keep the issue slots nearly as busy as the memory (under the power limit, where the clock falls: 1056 us). A warp owns one block of 256 elements (its scales need a maximum over the block:
 // one redux instruction), eight per lane as two groups of four neighbours, so every access of an aligned
 // tensor is 16 bytes of fp32, 8 of bf16 or 4 of codes per lane and a warp's lines are full. A tensor whose
 // start is not so aligned (a segment of a flat vector) takes its parameters and gradients element by element,

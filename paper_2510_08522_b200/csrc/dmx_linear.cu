@@ -16,8 +16,9 @@
 // Every wait is bounded; a warp that gives up counts itself in a device word (dmx_linear_status), and its CTA lets its
 // copies land, frees its TMEM and returns.
 // Bound: the tensor cores for large products, what an SM fetches from L2 (64 bytes a cycle) for narrow tiles, HBM for few rows.
-// Measured on B200: 8192^3 735 us = 1.50 PFLOP/s (the library's 685-691 us in the same runs); 8192 x 4096 x 1024 with GELU, y and z written,
-// 67 us = 1.03 PFLOP/s (the library's bare product 67-71 us); its gradient 133 us; one row x 4096 x 4096 7.8 us = 4.3 TB/s.
+// Measured on B200 in bursts at full clock / back to back for seconds under the power limit: 8192^3 714 / 833 us = 1.54 / 1.32 PFLOP/s
+// (the library's 669 / 774 us); 8192 x 4096 x 1024 with GELU, y and z written, 65 / 77 us = 1.06 / 0.89 PFLOP/s (the library's bare product
+// 56 / 60 us); its gradient 132 / 151 us; one row x 4096 x 4096 7.9 / 7.6 us = 4.3 TB/s.
 #include "dmx.h"
 
 #include <cuda.h>
