@@ -16,7 +16,9 @@
 // Variances: a thread sums deviations from its own first value, s = sum d, q = sum d^2, and takes q - s^2/n. That
 // cancels only if the first value is far off, and then the group's variance contains that distance itself:
 // the error stays within n (at most 128) roundings of the result. From there on deviations of means are added
-// (Chan, Golub, LeVeque 1983). Nothing is added atomically; the order of all sums is fixed by the shape.
+// (Chan, Golub, LeVeque 1983), each mean held as a float and what its rounding lost, and deviations taken from a rough mean whose own
+// deviation is summed beside them: a mean a million deviations away costs the variance nothing (with means in one float, rstd was
+// off by 1e-7 times mean over deviation where the spread lies between channels). Nothing is added atomically; the order of all sums is fixed by the shape.
 // Measured on B200, bf16: forward on 1024 x 32x32 x 64 54 us (5.0 TB/s of algorithmic bytes; 41 us at the measured copy
 // rate), backward on 64 x 56x56 x 256 with SiLU 103 us (3.0 TB/s; 47 us); what keeps them from it is what each slab costs
 // besides its data (reductions, exchange, parameters: a third of a slab's time) at two or three CTAs per SM.
@@ -24,6 +26,7 @@
 
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <float.h>
 #include <math.h>
 #include <stdint.h>
 #include <atomic>
@@ -180,6 +183,10 @@ constexpr int kMostThreads = V == 1 ? 1024 : M == RESIDENT ? kResidentThreads : 
 template <int V, Mode M, int ACT>
 constexpr int kCtas = V == 1 ? 1 : M != RESIDENT || ACT == DMX_ACT_SILU || ACT == DMX_ACT_GELU ? 2 : 3;
 
+// Forward: four for fp32, whose columns take half the registers (1024 x 8x8 x 64 with SiLU: 8.3 us, with three 10.4 us).
+template <int V, Mode M>
+constexpr int kForwardCtas = V == 1 ? 1 : M != RESIDENT ? 2 : V == 4 ? 4 : 3;
+
 // A CTA's place in one item, and a thread's in that.
 struct Here {
   int n, part, c0, g0, Wl, groups, rows, r0;
@@ -253,6 +260,24 @@ __device__ __forceinline__ float lane_sum(const Lanes& q, bool on, int g, F term
   return s;
 }
 
+// ... of two terms at once
+template <typename F>
+__device__ __forceinline__ float2 lane_sums(const Lanes& q, bool on, int g, F term) {
+  float2 s = make_float2(0.f, 0.f);
+  if (on) {
+    int r = q.r0, c = q.c0;
+    while (r < q.R) {
+      const int at = g * q.per + c;
+      s = add2(s, term(r * q.width + at, r));
+      r += q.dr;
+      c += q.dc;
+      if (c >= q.per) { c -= q.per; ++r; }
+    }
+  }
+  for (int o = q.each >> 1; o > 0; o >>= 1) s = add2(s, make_float2(__shfl_xor_sync(0xffffffffu, s.x, o), __shfl_xor_sync(0xffffffffu, s.y, o)));
+  return s;
+}
+
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 __device__ __forceinline__ void cluster_sync() {
@@ -293,20 +318,33 @@ __device__ __forceinline__ void bring_params(const Args& A, const Here& h, const
     }
 }
 
-// Over `lanes` lanes: parts with mean times positions ps, squared deviations pm and `have` positions of cpg values
-// each -> the mean and variance of all L positions.
-__device__ __forceinline__ float2 join(float ps, float pm, float have, float cpg, float L, int lanes) {
-  float mean = ps;
-  for (int o = lanes >> 1; o > 0; o >>= 1) mean += __shfl_xor_sync(0xffffffffu, mean, o);
-  mean /= L;
-  const float d = have > 0.f ? ps / have - mean : 0.f;
-  float m2 = have > 0.f ? fmaf(have * cpg * d, d, pm) : 0.f;
-  for (int o = lanes >> 1; o > 0; o >>= 1) m2 += __shfl_xor_sync(0xffffffffu, m2, o);
-  return make_float2(mean, m2 / (L * cpg));
+// A mean and what its rounding to a float lost. The sum of n values' deviations from a rough mean is c = n times what the rough one
+// lacks, that of their squares m2' = m2 + c^2/n.
+struct Mean {
+  float hi, lo;
+};
+__device__ __forceinline__ Mean corrected(float rough, float by) {
+  by = fabsf(by) <= FLT_MAX ? by : 0.f;             // (an infinite mean stays infinite)
+  const float hi = rough + by;
+  return {hi, (rough - hi) + by};
+}
+__device__ __forceinline__ float squares(float m2, float c, float by) { return dmx_act::relu(fmaf(-c, by, m2)); }   // by = c/n; a NaN stays one
+
+// Over `lanes` lanes: parts' means, squared deviations pm and `have` positions of cpg values each -> the mean and variance
+// of all L positions.
+__device__ __forceinline__ float2 join(Mean part, float pm, float have, float cpg, float L, int lanes) {
+  float rough = have > 0.f ? part.hi * have : 0.f;
+  for (int o = lanes >> 1; o > 0; o >>= 1) rough += __shfl_xor_sync(0xffffffffu, rough, o);
+  rough /= L;
+  const float d = have > 0.f ? (part.hi - rough) + part.lo : 0.f;
+  float2 s = make_float2(have * d, have > 0.f ? fmaf(have * cpg * d, d, pm) : 0.f);
+  for (int o = lanes >> 1; o > 0; o >>= 1) s = add2(s, make_float2(__shfl_xor_sync(0xffffffffu, s.x, o), __shfl_xor_sync(0xffffffffu, s.y, o)));
+  const float by = s.x / L;
+  return make_float2(corrected(rough, by).hi, squares(s.y, s.x * cpg, by) / (L * cpg));
 }
 
 template <typename T, int V, Mode M, int ACT>
-__global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, DMX_ACT_NONE>) forward_kernel(const __grid_constant__ Args A) {
+__global__ void __launch_bounds__(kMostThreads<V, M>, kForwardCtas<V, M>) forward_kernel(const __grid_constant__ Args A) {
   using U = typename Vec<T, V>::type;
   constexpr int NP = kPairs<V>, SL = kSlots<V>;
   extern __shared__ __align__(16) float sm[];
@@ -317,14 +355,15 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, DMX_ACT_NONE>)
   const int rows = A.lanes ? threads >> 5 : R;
   U* slot = reinterpret_cast<U*>(sm) + tid;
   float* emean = sm + (size_t)A.slots * threads * sizeof(U) / sizeof(float);
-  float* em2 = emean + padded(rows * width);
+  float* elo = emean + padded(rows * width);
+  float* em2 = elo + padded(rows * width);
   float* en = em2 + padded(rows * width);
-  // per group: every part's sum and squared deviations, in turn for one item and the next (the cluster's CTAs write to
+  // per group: every part's mean (two floats) and squared deviations, in turn for one item and the next (the cluster's CTAs write to
   // one another's: whoever writes for an item has seen all others' sums of the item before, so the buffer of two
   // items ago is free); then mean and rstd
   const int pG = padded(A.gW), gparts = M == RESIDENT ? A.parts : 1;
   float* got = en + padded(rows);
-  float* gmean = got + 4 * gparts * pG;
+  float* gmean = got + 6 * gparts * pG;
   float* grstd = gmean + pG;
   float* par = grstd + pG;
   int turn = 0;
@@ -345,7 +384,7 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, DMX_ACT_NONE>)
   if (M == RESIDENT && A.parts > 1) cluster_sync();      // all of the cluster runs: its memory may be written
   for (int64_t item = first; item < A.items; item += stride) {
     const Params P = params_at(par + turn * params_size(W, A.gW), W, A.gW);
-    float* mine = got + turn * 2 * gparts * pG;
+    float* mine = got + turn * 3 * gparts * pG;
     if constexpr (M != APPLY) {
       bring_wait();
       float2 p0[NP], ps[NP], pq[NP];
@@ -364,7 +403,7 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, DMX_ACT_NONE>)
           pq[j] = fma2(d, d, pq[j]);
         }
       }
-      float x0[V], s[V], q[V];
+      float x0[V], s[V], q[V], lo[V];
       if constexpr (V == 1) {
         x0[0] = p0[0].x; s[0] = ps[0].x + ps[0].y; q[0] = pq[0].x + pq[0].y;
       } else {
@@ -383,15 +422,17 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, DMX_ACT_NONE>)
         const float d = s[v] * inv;
         q[v] = fmaxf(fmaf(-s[v], d, q[v]), 0.f) + 0.f * d;      // (a NaN or infinity stays one)
         s[v] = x0[v] + d;
+        lo[v] = (x0[v] - s[v]) + d;
       }
 #pragma unroll
       for (int f = 1; f < V; f *= 2) {
         if (A.fold <= f) break;
 #pragma unroll
         for (int j = 0; j < V / (2 * f); ++j) {
-          const float d = s[2 * j] - s[2 * j + 1];
+          const float b = s[2 * j + 1], d = (s[2 * j] - b) + (lo[2 * j] - lo[2 * j + 1]);
           q[j] = q[2 * j] + q[2 * j + 1] + 0.5f * n * d * d;
-          s[j] = 0.5f * (s[2 * j] + s[2 * j + 1]);
+          s[j] = b + 0.5f * d;
+          lo[j] = ((b - s[j]) + 0.5f * d) + lo[2 * j + 1];
         }
         n *= 2.f;
       }
@@ -405,10 +446,12 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, DMX_ACT_NONE>)
           float t = s[j] * n;
           for (int o = A.lanes; o < 32; o <<= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
           t *= iN;
-          const float d = s[j] - t;
-          float m = n > 0.f ? fmaf(n * d, d, q[j]) : 0.f;
-          for (int o = A.lanes; o < 32; o <<= 1) m += __shfl_xor_sync(0xffffffffu, m, o);
-          s[j] = t; q[j] = m;
+          const float d = n > 0.f ? (s[j] - t) + lo[j] : 0.f;
+          float2 c = make_float2(n * d, n > 0.f ? fmaf(n * d, d, q[j]) : 0.f);
+          for (int o = A.lanes; o < 32; o <<= 1) c = add2(c, make_float2(__shfl_xor_sync(0xffffffffu, c.x, o), __shfl_xor_sync(0xffffffffu, c.y, o)));
+          const float by = c.x * iN;
+          const Mean mean = corrected(t, by);
+          s[j] = mean.hi; lo[j] = mean.lo; q[j] = squares(c.y, c.x, by);
         }
         const int lane = tid & 31, wid = tid >> 5;
         if (lane < A.lanes) {
@@ -416,6 +459,7 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, DMX_ACT_NONE>)
           for (int j = 0; j < V; ++j) {
             if (j >= vals) break;
             emean[wid * width + col * vals + j] = s[j];
+            elo[wid * width + col * vals + j] = lo[j];
             em2[wid * width + col * vals + j] = q[j];
           }
           if (lane == 0) en[wid] = N;
@@ -425,6 +469,7 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, DMX_ACT_NONE>)
         for (int j = 0; j < V; ++j) {
           if (j >= vals) break;
           emean[rl * width + col * vals + j] = s[j];
+          elo[rl * width + col * vals + j] = lo[j];
           em2[rl * width + col * vals + j] = q[j];
         }
         if (col == 0) en[rl] = n;
@@ -435,24 +480,29 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, DMX_ACT_NONE>)
         const int g = gb + Q.g1;
         const bool mineg = g < h.groups;
         const float sum = lane_sum(Q, mineg, g, [&](int i, int r, int) { return en[r] > 0.f ? emean[i] * en[r] : 0.f; });
-        const float mean = sum * icnt;
-        const float m2 = lane_sum(Q, mineg, g, [&](int i, int r, int) {
-          const float d = emean[i] - mean;
-          return en[r] > 0.f ? fmaf(en[r] * d, d, em2[i]) : 0.f;
+        const float rough = sum * icnt;
+        const float2 c = lane_sums(Q, mineg, g, [&](int i, int r) {
+          const float d = (emean[i] - rough) + elo[i];
+          return en[r] > 0.f ? make_float2(en[r] * d, fmaf(en[r] * d, d, em2[i])) : make_float2(0.f, 0.f);
         });
-        // the mean times the number of positions: the parts' sum over all positions is the mean
+        const Mean mean = corrected(rough, c.x * icnt);
+        const float m2 = squares(c.y, c.x, c.x * icnt);
         if (M == STATS) {
-          if (mineg && Q.l == 0)
-            reinterpret_cast<float2*>(A.part)[((int64_t)h.n * A.parts + h.part) * A.G + h.g0 + g] = make_float2(mean * (float)h.rows, m2);
+          if (mineg && Q.l == 0) {
+            float* to = A.part + 3 * (((int64_t)h.n * A.parts + h.part) * A.G + h.g0 + g);
+            to[0] = mean.hi; to[1] = mean.lo; to[2] = m2;
+          }
         } else if (A.parts > 1) {
           if (mineg)
-            for (int k = Q.l; k < 2 * A.parts; k += Q.each)
-              send(mine + (2 * h.part + (k & 1)) * pG + g, k >> 1, k & 1 ? m2 : mean * (float)h.rows);
+            for (int k = Q.l; k < 3 * A.parts; k += Q.each) {
+              const int to = k / 3, which = k - 3 * to;
+              send(mine + (3 * h.part + which) * pG + g, to, which == 0 ? mean.hi : which == 1 ? mean.lo : m2);
+            }
         } else if (mineg && Q.l == 0) {              // nothing to join
           const float rstd = 1.f / sqrtf(m2 * icnt + A.eps);
-          gmean[g] = mean;
+          gmean[g] = mean.hi;
           grstd[g] = rstd;
-          A.mean[(int64_t)h.n * A.G + h.g0 + g] = mean;
+          A.mean[(int64_t)h.n * A.G + h.g0 + g] = mean.hi;
           A.rstd[(int64_t)h.n * A.G + h.g0 + g] = rstd;
         }
       }
@@ -482,12 +532,13 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, DMX_ACT_NONE>)
         for (int gb = 0; gb < now.groups; gb += threads / kl) {
           const int g = gb + tid / kl;
           const float have = (float)(min((int64_t)(k0 + 1) * A.rows, (int64_t)A.L) - min((int64_t)k0 * A.rows, (int64_t)A.L));
-          float ps = 0.f, pm = 0.f;
+          Mean part = {0.f, 0.f};
+          float pm = 0.f;
           if (g < now.groups) {
-            ps = mine[2 * k0 * pG + g];
-            pm = mine[(2 * k0 + 1) * pG + g];
+            part = {mine[3 * k0 * pG + g], mine[(3 * k0 + 1) * pG + g]};
+            pm = mine[(3 * k0 + 2) * pG + g];
           }
-          float2 t = join(ps, pm, have, (float)cpg, (float)A.L, kl);
+          float2 t = join(part, pm, have, (float)cpg, (float)A.L, kl);
           if (g < now.groups && k0 == 0) {
             t.y = 1.f / sqrtf(t.y + A.eps);
             gmean[g] = t.x;
@@ -740,27 +791,30 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, ACT>) backward
 }
 
 // The chunks' sums of an image, joined between the two launches that read it. Forward: a warp per image and group.
-__global__ void __launch_bounds__(256) join_groups_kernel(const float2* __restrict__ part, int64_t groups, int parts, int rows, int L, int G, int cpg,
+__global__ void __launch_bounds__(256) join_groups_kernel(const float* __restrict__ part, int64_t groups, int parts, int rows, int L, int G, int cpg,
                                                           float eps, float* __restrict__ mean, float* __restrict__ rstd) {
   asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
   const int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);       // image * G + group
   const int lane = threadIdx.x & 31;
   if (i >= groups) return;
-  const float2* src = part + i / G * parts * G + i % G;
+  const float* src = part + 3 * (i / G * parts * G + i % G);
+  auto positions = [&](int k) { return (float)(min((int64_t)(k + 1) * rows, (int64_t)L) - (int64_t)k * rows); };
   // 32nd parts by lane: each lane joins its own first
   float sum = 0.f, have = 0.f;
   for (int k = lane; k < parts; k += 32) {
-    sum += __ldg(&src[(int64_t)k * G]).x;
-    have += (float)(min((int64_t)(k + 1) * rows, (int64_t)L) - (int64_t)k * rows);
+    sum = fmaf(__ldg(src + (int64_t)k * 3 * G), positions(k), sum);
+    have += positions(k);
   }
   const float mu = have > 0.f ? sum / have : 0.f;
-  float m2 = 0.f;
+  float c = 0.f, m2 = 0.f;
   for (int k = lane; k < parts; k += 32) {
-    const float2 t = __ldg(&src[(int64_t)k * G]);
-    const float n = (float)(min((int64_t)(k + 1) * rows, (int64_t)L) - (int64_t)k * rows), d = t.x / n - mu;
-    m2 += fmaf(n * (float)cpg * d, d, t.y);
+    const float* p = src + (int64_t)k * 3 * G;
+    const float n = positions(k), d = (__ldg(p) - mu) + __ldg(p + 1);
+    c = fmaf(n, d, c);
+    m2 += fmaf(n * (float)cpg * d, d, __ldg(p + 2));
   }
-  const float2 t = join(sum, m2, have, (float)cpg, (float)L, 32);
+  const float by = have > 0.f ? c / have : 0.f;
+  const float2 t = join(corrected(mu, by), squares(m2, c * (float)cpg, by), have, (float)cpg, (float)L, 32);
   if (lane == 0) {
     mean[i] = t.x;
     rstd[i] = 1.f / sqrtf(t.y + eps);
@@ -852,7 +906,7 @@ bool settle(Plan& p, int64_t L, int C, int cpg, int e, bool backward, int64_t ro
   const int groups = p.W / cpg;
   const int sums = p.resident ? p.parts : 1;
   if (backward) p.smem = data + f * (padded(2 * erows * p.W) + 4 * sums * padded(p.W) + 2 * padded(groups));
-  else p.smem = data + f * (2 * padded(erows * p.cols * (p.V / p.fold)) + padded(erows) + (4 * sums + 2) * padded(groups));
+  else p.smem = data + f * (3 * padded(erows * p.cols * (p.V / p.fold)) + padded(erows) + (6 * sums + 2) * padded(groups));
   p.smem += 2 * f * params_size(p.W, groups);
   if (p.smem > kMostShared) return false;
   return true;
@@ -978,7 +1032,7 @@ int run_act(bool backward, const Plan& p, const Args& A, cudaStream_t st) {
   int rc = launch<forward_kernel<T, V, STATS, DMX_ACT_NONE>>(p, A, false, st);
   if (rc != DMX_OK) return rc;
   const int64_t groups = (int64_t)A.N * A.G;
-  rc = start((groups + 7) / 8, 1, 256, st, join_groups_kernel, reinterpret_cast<const float2*>(A.part), groups, A.parts, A.rows, A.L, A.G, A.cpg, A.eps,
+  rc = start((groups + 7) / 8, 1, 256, st, join_groups_kernel, (const float*)A.part, groups, A.parts, A.rows, A.L, A.G, A.cpg, A.eps,
              A.mean, A.rstd);
   return rc != DMX_OK ? rc : launch<forward_kernel<T, V, APPLY, ACT>>(p, A, false, st);
 }
@@ -1032,7 +1086,7 @@ bool columns_fit(int C, int cpg, int e) { return C % (16 / e) == 0 && lcm(cpg, 1
 
 int64_t workspace_of(const Plan& p, int64_t N, int C, int G, bool backward) {
   if (backward) return 2 * N * (p.resident ? 1 : p.parts + 1) * C * (int64_t)sizeof(float);
-  return p.resident ? 0 : N * p.parts * G * (int64_t)sizeof(float2);
+  return p.resident ? 0 : 3 * N * p.parts * G * (int64_t)sizeof(float);
 }
 
 }  // namespace
