@@ -19,8 +19,8 @@
 // (Chan, Golub, LeVeque 1983), each mean held as a float and what its rounding lost, and deviations taken from a rough mean whose own
 // deviation is summed beside them: a mean a million deviations away costs the variance nothing (with means in one float, rstd was
 // off by 1e-7 times mean over deviation where the spread lies between channels). Nothing is added atomically; the order of all sums is fixed by the shape.
-// Measured on B200, bf16: forward on 1024 x 32x32 x 64 54 us (5.0 TB/s of algorithmic bytes; 41 us at the measured copy
-// rate), backward on 64 x 56x56 x 256 with SiLU 103 us (3.0 TB/s; 47 us); what keeps them from it is what each slab costs
+// Measured on B200, bf16: forward on 1024 x 32x32 x 64 55 us (4.9 TB/s of algorithmic bytes; 41 us at the measured copy
+// rate), backward on 64 x 56x56 x 256 with SiLU 104 us (3.0 TB/s; 47 us); what keeps them from it is what each slab costs
 // besides its data (reductions, exchange, parameters: a third of a slab's time) at two or three CTAs per SM.
 #include "dmx.h"
 
