@@ -574,6 +574,36 @@ int dmx_linear_backward(int64_t M, int64_t N, int64_t K, const void* dy, int64_t
 int dmx_linear_plan(int64_t rows, int64_t cols, int64_t k, int rows_across, int64_t* plan);
 int dmx_linear_status(int* errors);
 
+/*
+ * dmx_layer_norm_* — layer norm over the rows of a matrix, and its gradient.
+ * x is M rows of D values (DMX_F32 or DMX_BF16):
+ *   mean, var over a row's D values (var without Bessel's correction), rstd = 1/sqrt(var + eps), y = (x - mean) * rstd * weight + bias
+ * backward, with xh = (x - mean)*rstd and g = weight*dy, sums over the row:
+ *   dx = rstd * (g - (sum(g) + xh * sum(g*xh)) / D) + add,  dweight = sum over rows of dy*xh,  dbias = the same of dy
+ * All arithmetic and all sums are fp32; y and dx are rounded once. var is the sum of squared deviations from the rounded mean,
+ * corrected by that mean's own deviation: a mean far from zero costs it no accuracy (the mean itself is one float).
+ *   x, y, dy, add, dx  element (m, d) at m*ld + d, strides in elements; inputs may repeat rows (ld 0) or overlap them, y's and dx's
+ *                      ld is >= D unless there is one row. Element alignment suffices (16-byte aligned rows are faster).
+ *   weight, bias       fp32, D entries, or NULL for ones and zeros
+ *   mean, rstd         fp32, M entries (written by forward, read by backward)
+ *   add                what is added to dx before it is rounded (e.g. the gradient that reaches x past the norm), or NULL
+ *   dweight, dbias     fp32, D entries, or NULL
+ *   workspace          backward, if dweight or dbias is wanted: at least dmx_layer_norm_workspace(...) bytes, 16-byte aligned,
+ *                      contents undefined
+ * Results are bitwise reproducible. y may be x, and dx may be dy, x or add, with the same strides (unless rows repeat). M = 0 gives dweight = 0 and
+ * dbias = 0.
+ * Errors: DMX_ERR_ARG (D < 1, D > DMX_LN_MAX_WIDTH, M >= 2^40, strides, eps < 0, null pointers, workspace too small), DMX_ERR_ALIGN,
+ * DMX_ERR_CUDA.
+ */
+#define DMX_LN_MAX_WIDTH 65536
+int64_t dmx_layer_norm_workspace(int64_t M, int D, int dtype);
+int dmx_layer_norm_forward(int64_t M, int D, int dtype, const void* x, int64_t ldx, const float* weight, const float* bias,
+                           float eps, void* y, int64_t ldy, float* mean, float* rstd, void* cuda_stream);
+int dmx_layer_norm_backward(int64_t M, int D, int dtype, const void* dy, int64_t lddy, const void* x, int64_t ldx,
+                            const float* mean, const float* rstd, const float* weight, const void* add, int64_t ldadd,
+                            void* dx, int64_t lddx, float* dweight, float* dbias, void* workspace,
+                            int64_t workspace_bytes, void* cuda_stream);
+
 /* Frees the tables and the scratch. NULL is accepted; a handle that is not live (destroyed
  * already) gives DMX_ERR_HANDLE. The caller makes sure no step of this handle is still running. */
 int dmx_destroy(dmx_handle* h);

@@ -1,0 +1,375 @@
+// dmx_layer_norm.cu — layer norm over rows, and its gradient.
+//
+// forward    mean and variance of a row's D values, y = (x - mean) rstd w + b
+// backward   xh = (x - mean) rstd, g = w dy; dx = rstd (g - (sum g + xh sum g xh) / D) + add; dw = sum of dy xh over the rows, db = sum of dy
+//
+// Bound: HBM. A team of threads (8 lanes, a warp, a CTA, or a cluster of CTAs, by the row's width) holds a row in registers, up to
+// 32 values a thread, so that everything is read once; teams stay and take row after row. In backward a thread's columns are the
+// same in every row: it sums its share of dw and db in registers, a CTA's teams join theirs in shared memory, and a small second launch
+// adds the CTAs' in a fixed order.
+// Variance: deviations from the rounded mean are summed beside their squares, and what that mean was off is taken out again:
+// a mean a million deviations away costs the variance nothing.
+#include "dmx_rows.cuh"
+
+namespace {
+
+using namespace dmx_rows;
+
+constexpr int kMaxCluster = 8, kMaxWarps = 8;      // of a CTA that is one team
+
+struct Args {
+  const void *x, *dy, *add;
+  void* out;                                       // y or dx
+  int64_t ldx, lddy, ldadd, ldout, M;
+  const float *weight, *bias;
+  float *mean, *rstd;                              // forward: outputs; backward: inputs
+  float* part;                                     // backward: [CTAs of a cluster's rows][2][D]
+  int D, wvec;                                     // wvec: weight and bias in 16-byte accesses
+  float eps;
+};
+
+// How a row is held. TEAM: lanes of a warp that share a row, 0 a CTA, -1 a cluster. N values per thread in accesses of V.
+template <typename T, int V, int TEAM, int N>
+struct Held {
+  static constexpr int kAccesses = N / V;
+  typedef typename Vec<T, V>::type Raw;
+
+  // this thread's place in its team, the team's size, its row and the rows between its rows
+  static __device__ __forceinline__ void place(int& t, int& size, int64_t& row, int64_t& step) {
+    if constexpr (TEAM > 0) {
+      const int teams = blockDim.x / TEAM;
+      t = threadIdx.x % TEAM; size = TEAM;
+      row = (int64_t)blockIdx.x * teams + threadIdx.x / TEAM; step = (int64_t)gridDim.x * teams;
+    } else if constexpr (TEAM == 0) {
+      t = threadIdx.x; size = blockDim.x;
+      row = blockIdx.x; step = gridDim.x;
+    } else {
+      unsigned rank, n;
+      asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+      asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+      t = rank * blockDim.x + threadIdx.x; size = n * blockDim.x;
+      row = blockIdx.x / n; step = gridDim.x / n;
+    }
+  }
+  static __device__ __forceinline__ void load(const void* p, int64_t ld, int64_t row, int t, int size, int D, Raw (&r)[kAccesses]) {
+    const T* q = static_cast<const T*>(p) + row * ld;
+#pragma unroll
+    for (int i = 0; i < kAccesses; ++i) {
+      const int c = (i * size + t) * V;
+      if (c < D) r[i] = *reinterpret_cast<const Raw*>(q + c);
+      else r[i] = Raw{};
+    }
+  }
+  static __device__ __forceinline__ void store(void* p, int64_t ld, int64_t row, int t, int size, int D, const float (&x)[N]) {
+    T* q = static_cast<T*>(p) + row * ld;
+#pragma unroll
+    for (int i = 0; i < kAccesses; ++i) {
+      const int c = (i * size + t) * V;
+      if (c < D) *reinterpret_cast<Raw*>(q + c) = narrow<T, V>(x + i * V);
+    }
+  }
+  static __device__ __forceinline__ void unpack(const Raw (&r)[kAccesses], float (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < kAccesses; ++i) widen<T>(r[i], x + i * V);
+  }
+  // an fp32 vector's values at this thread's columns; `otherwise` where there is no vector
+  static __device__ __forceinline__ void vector(const float* w, int wvec, float otherwise, int t, int size, int D, float (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < kAccesses; ++i) {
+      const int c = (i * size + t) * V;
+      if (V > 1 && w && wvec) {
+#pragma unroll
+        for (int k = 0; k < V; k += 4) {
+          const float4 v = c < D ? __ldg(reinterpret_cast<const float4*>(w + c + k)) : make_float4(0.f, 0.f, 0.f, 0.f);
+          x[i * V + k] = v.x; x[(i * V + k + 1) % N] = v.y; x[(i * V + k + 2) % N] = v.z; x[(i * V + k + 3) % N] = v.w;
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < V; ++k) x[i * V + k] = w ? (c < D ? __ldg(w + c + k) : 0.f) : otherwise;
+      }
+    }
+  }
+};
+
+// Sums of two values over a team. `red`: two buffers of kMaxCluster x kMaxWarps pairs, used in turn (`turn` flips).
+template <int TEAM>
+__device__ __forceinline__ float2 team_sum(float2 v, float2 (*red)[kMaxCluster * kMaxWarps], int& turn) {
+#pragma unroll
+  for (int o = (TEAM > 0 ? TEAM : 32) / 2; o > 0; o >>= 1) {
+    v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+    v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+  }
+  if constexpr (TEAM > 0) return v;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  int count = warps;
+  if constexpr (TEAM == 0) {
+    if (lane == 0) red[turn][warp] = v;
+    __syncthreads();
+  } else {
+    unsigned rank, n;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+    count = warps * n;
+    if (lane < n) {
+      unsigned to;
+      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"((unsigned)__cvta_generic_to_shared(&red[turn][rank * warps + warp])), "r"(lane));
+      asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(v.x), "f"(v.y) : "memory");
+    }
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+  }
+  v = make_float2(0.f, 0.f);
+  for (int i = 0; i < count; ++i) {
+    const float2 u = red[turn][i];
+    v.x += u.x; v.y += u.y;
+  }
+  turn ^= 1;
+  return v;
+}
+
+template <typename T, int V, int TEAM, int N>
+__global__ void __launch_bounds__(TEAM > 0 ? 128 : 256) forward_kernel(const __grid_constant__ Args A) {
+  typedef Held<T, V, TEAM, N> H;
+  __shared__ float2 red[2][kMaxCluster * kMaxWarps];
+  int t, size, turn = 0;
+  int64_t row, step;
+  H::place(t, size, row, step);
+  start_dependents();
+  if constexpr (TEAM < 0) asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");   // all of it is there
+  wait_for_previous();
+  float w[N], b[N];
+  H::vector(A.weight, A.wvec, 1.f, t, size, A.D, w);
+  H::vector(A.bias, A.wvec, 0.f, t, size, A.D, b);
+  const float per = 1.f / (float)A.D;
+  // (a warp's lanes stay together: those of a team without a row left repeat the last one and store nothing)
+  for (int64_t base = row - (TEAM > 0 ? threadIdx.x % 32 / (TEAM > 0 ? TEAM : 1) : 0); base < A.M; base += step, row += step) {
+    const bool live = row < A.M;
+    typename H::Raw raw[H::kAccesses];
+    H::load(A.x, A.ldx, live ? row : A.M - 1, t, size, A.D, raw);
+    float x[N];
+    H::unpack(raw, x);
+    float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) s.x += x[i];
+    s = team_sum<TEAM>(s, red, turn);
+    const float rough = s.x * per;
+    s = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      x[i] -= rough;
+      if ((i / V * size + t) * V < A.D) { s.x += x[i]; s.y = fmaf(x[i], x[i], s.y); }
+    }
+    s = team_sum<TEAM>(s, red, turn);
+    const float off = s.x * per, var = fmaf(-off, off, s.y * per), rstd = __frsqrt_rn((var < 0.f ? 0.f : var) + A.eps);   // (a NaN stays)
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = fmaf((x[i] - off) * rstd, w[i], b[i]);
+    if (!live) continue;
+    H::store(A.out, A.ldout, row, t, size, A.D, x);
+    if (t == 0) { A.mean[row] = rough + off; A.rstd[row] = rstd; }
+  }
+}
+
+template <typename T, int V, int TEAM, int N>
+__global__ void __launch_bounds__(TEAM > 0 ? 128 : 256) backward_kernel(const __grid_constant__ Args A) {
+  typedef Held<T, V, TEAM, N> H;
+  __shared__ float2 red[2][kMaxCluster * kMaxWarps];
+  __shared__ __align__(16) float joined[TEAM > 0 ? 4 * 2 * N * 32 : 1];
+  int t, size, turn = 0;
+  int64_t row, step;
+  H::place(t, size, row, step);
+  start_dependents();
+  if constexpr (TEAM < 0) asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+  wait_for_previous();
+  const float per = 1.f / (float)A.D;
+  float dw[N], db[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) dw[i] = db[i] = 0.f;
+  for (int64_t base = row - (TEAM > 0 ? threadIdx.x % 32 / (TEAM > 0 ? TEAM : 1) : 0); base < A.M; base += step, row += step) {
+    const bool live = row < A.M;
+    const int64_t at = live ? row : A.M - 1;
+    typename H::Raw rx[H::kAccesses], rg[H::kAccesses], ra[H::kAccesses];
+    H::load(A.x, A.ldx, at, t, size, A.D, rx);
+    H::load(A.dy, A.lddy, at, t, size, A.D, rg);
+    if (A.add) H::load(A.add, A.ldadd, at, t, size, A.D, ra);
+    const float mean = A.mean[at], rstd = A.rstd[at];
+    float h[N], g[N], w[N];
+    H::unpack(rx, h);
+    H::unpack(rg, g);
+    H::vector(A.weight, A.wvec, 1.f, t, size, A.D, w);
+    float2 s = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      h[i] = (h[i] - mean) * rstd;
+      if (live) { dw[i] = fmaf(g[i], h[i], dw[i]); db[i] += g[i]; }
+      g[i] *= w[i];
+      if ((i / V * size + t) * V < A.D) { s.x += g[i]; s.y = fmaf(g[i], h[i], s.y); }
+    }
+    s = team_sum<TEAM>(s, red, turn);
+    s.x *= per; s.y *= per;
+#pragma unroll
+    for (int i = 0; i < N; ++i) g[i] = rstd * (g[i] - fmaf(h[i], s.y, s.x));
+    if (A.add) {
+      H::unpack(ra, h);
+#pragma unroll
+      for (int i = 0; i < N; ++i) g[i] += h[i];
+    }
+    if (live) H::store(A.out, A.ldout, row, t, size, A.D, g);
+  }
+  if (!A.part) return;
+  float* part = A.part + (TEAM < 0 ? step > 0 ? (int64_t)(blockIdx.x / (size / blockDim.x)) : 0 : (int64_t)blockIdx.x) * 2 * A.D;
+  if constexpr (TEAM > 0) {
+    // the lanes of a warp that hold the same columns, then the warps
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 16; o >= TEAM; o >>= 1) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        dw[i] += __shfl_xor_sync(0xffffffffu, dw[i], o);
+        db[i] += __shfl_xor_sync(0xffffffffu, db[i], o);
+      }
+    }
+    if (lane < TEAM) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        joined[(warp * 2 * N + i) * 32 + lane] = dw[i];
+        joined[((warp * 2 + 1) * N + i) * 32 + lane] = db[i];
+      }
+    }
+    __syncthreads();
+    const int warps = blockDim.x >> 5;
+    for (int j = threadIdx.x; j < 2 * N * 32; j += blockDim.x) {
+      const int l = j & 31, i = (j >> 5) % N, which = (j >> 5) / N;
+      const int c = (i / V * size + l) * V + i % V;
+      if (l >= TEAM || c >= A.D) continue;
+      float v = 0.f;
+      for (int k = 0; k < warps; ++k) v += joined[((k * 2 + which) * N + i) * 32 + l];
+      part[which * (int64_t)A.D + c] = v;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int c = (i / V * size + t) * V + i % V;
+      if (c < A.D) { part[c] = dw[i]; part[(int64_t)A.D + c] = db[i]; }
+    }
+  }
+}
+
+// dweight and dbias from the CTAs' sums: 32 columns a CTA, its warps take every 32nd row of sums
+__global__ void __launch_bounds__(1024) columns_kernel(const float* part, int64_t rows, int D, float* dweight, float* dbias) {
+  __shared__ float sh[32][33];
+  start_dependents();
+  wait_for_previous();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, which = blockIdx.y;
+  float s = 0.f;
+  if (c < D) {
+#pragma unroll 4
+    for (int64_t r = warp; r < rows; r += 32) s += part[(r * 2 + which) * D + c];
+  }
+  sh[warp][lane] = s;
+  __syncthreads();
+  if (warp == 0 && c < D) {
+    s = 0.f;
+    for (int k = 0; k < 32; ++k) s += sh[k][lane];
+    float* out = which ? dbias : dweight;
+    if (out) out[c] = s;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- host
+
+// A row's team by its width: 8 lanes to 64 values, a warp to 1024, a CTA to 8192, a cluster above. (Wider teams leave fewer
+// values to a thread and add a barrier to every sum.)
+struct Plan {
+  int team, values, threads, cluster;
+  int64_t groups;            // CTAs, or clusters of them
+};
+Plan plan_of(int64_t M, int D, int backward) {
+  Plan p = {};
+  p.cluster = 1;
+  p.threads = 128;
+  p.team = D <= 64 ? 8 : D <= 1024 ? 32 : D <= 8192 ? 0 : -1;
+  p.values = D <= 256 ? 8 : D <= 512 ? 16 : 32;
+  if (D > 1024) {
+    while (p.cluster * 8192 < D) p.cluster *= 2;
+    const int share = (D + p.cluster - 1) / p.cluster;
+    p.threads = ((share + 31) / 32 + 31) / 32 * 32;
+  }
+  const int rows = p.team > 0 ? 128 / p.team : 1;
+  const int64_t want = (M + rows - 1) / rows, most = p.team < 0 ? 148 * 2 / p.cluster : p.team == 0 ? 148 * (512 / p.threads) : 148 * (backward ? 3 : 4);
+  p.groups = want < most ? want : most;
+  return p;
+}
+
+template <typename T, int V, int TEAM, int N>
+int launch(const Args& A, const Plan& p, int backward, cudaStream_t st) {
+  const dim3 grid((unsigned)(p.groups * p.cluster));
+  return backward ? start(grid, p.threads, p.cluster, 0, st, backward_kernel<T, V, TEAM, N>, A) : start(grid, p.threads, p.cluster, 0, st, forward_kernel<T, V, TEAM, N>, A);
+}
+template <typename T, int V>
+int launch(const Args& A, const Plan& p, int backward, cudaStream_t st) {
+  if (p.team == 8) return launch<T, V, 8, 8>(A, p, backward, st);
+  if (p.team < 0) return launch<T, V, -1, 32>(A, p, backward, st);
+  if (p.team == 0) return launch<T, V, 0, 32>(A, p, backward, st);
+  if (p.values == 8) return launch<T, V, 32, 8>(A, p, backward, st);
+  return p.values == 16 ? launch<T, V, 32, 16>(A, p, backward, st) : launch<T, V, 32, 32>(A, p, backward, st);
+}
+int launch(const Args& A, const Plan& p, int dtype, bool wide, int backward, cudaStream_t st) {
+  if (dtype == DMX_F32) return wide ? launch<float, 4>(A, p, backward, st) : launch<float, 1>(A, p, backward, st);
+  return wide ? launch<bf16, 8>(A, p, backward, st) : launch<bf16, 1>(A, p, backward, st);
+}
+
+bool shape_ok(int64_t M, int D, int dtype) { return M >= 0 && M < ((int64_t)1 << 40) && D >= 1 && D <= DMX_LN_MAX_WIDTH && (dtype == DMX_F32 || dtype == DMX_BF16); }
+
+}  // namespace
+
+extern "C" {
+
+int64_t dmx_layer_norm_workspace(int64_t M, int D, int dtype) {
+  if (!shape_ok(M, D, dtype)) return DMX_ERR_ARG;
+  return M == 0 ? 0 : pad256(plan_of(M, D, 1).groups * 2 * D * (int64_t)sizeof(float));
+}
+
+int dmx_layer_norm_forward(int64_t M, int D, int dtype, const void* x, int64_t ldx, const float* weight, const float* bias, float eps, void* y,
+                           int64_t ldy, float* mean, float* rstd, void* cuda_stream) {
+  if (!shape_ok(M, D, dtype) || !(eps >= 0.f) || (M > 1 && (ldx < 0 || ldy < D))) return DMX_ERR_ARG;
+  if (M == 0) return DMX_OK;
+  if (!x || !y || !mean || !rstd) return DMX_ERR_ARG;
+  const unsigned e = element_size(dtype);
+  if (!aligned(x, e) || !aligned(y, e) || !aligned(weight, 4) || !aligned(bias, 4) || !aligned(mean, 4) || !aligned(rstd, 4)) return DMX_ERR_ALIGN;
+  Args A = {};
+  A.x = x; A.out = y; A.ldx = M > 1 ? ldx : D; A.ldout = M > 1 ? ldy : D; A.M = M; A.D = D;
+  A.weight = weight; A.bias = bias; A.mean = mean; A.rstd = rstd; A.eps = eps;
+  A.wvec = aligned(weight, 16) && aligned(bias, 16);
+  return launch(A, plan_of(M, D, 0), dtype, wide_rows(x, M, ldx, D, dtype) && wide_rows(y, M, ldy, D, dtype), 0, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int dmx_layer_norm_backward(int64_t M, int D, int dtype, const void* dy, int64_t lddy, const void* x, int64_t ldx, const float* mean, const float* rstd,
+                            const float* weight, const void* add, int64_t ldadd, void* dx, int64_t lddx, float* dweight, float* dbias,
+                            void* workspace, int64_t workspace_bytes, void* cuda_stream) {
+  if (!shape_ok(M, D, dtype) || (M > 1 && (lddy < 0 || ldx < 0 || (add && ldadd < 0) || lddx < D))) return DMX_ERR_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (!aligned(dweight, 4) || !aligned(dbias, 4)) return DMX_ERR_ALIGN;
+  if (M == 0) {              // empty sums
+    if (dweight && !dmxh::cuda_ok(cudaMemsetAsync(dweight, 0, sizeof(float) * D, st))) return DMX_ERR_CUDA;
+    if (dbias && !dmxh::cuda_ok(cudaMemsetAsync(dbias, 0, sizeof(float) * D, st))) return DMX_ERR_CUDA;
+    return DMX_OK;
+  }
+  if (!dy || !x || !mean || !rstd || !dx) return DMX_ERR_ARG;
+  const bool sums = dweight || dbias;
+  if (sums && (workspace_bytes < dmx_layer_norm_workspace(M, D, dtype) || !workspace)) return DMX_ERR_ARG;
+  const unsigned e = element_size(dtype);
+  if (!aligned(dy, e) || !aligned(x, e) || !aligned(add, e) || !aligned(dx, e) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(weight, 4) ||
+      !aligned(workspace, 16)) return DMX_ERR_ALIGN;
+  Args A = {};
+  A.x = x; A.dy = dy; A.add = add; A.out = dx; A.M = M; A.D = D;
+  A.ldx = M > 1 ? ldx : D; A.lddy = M > 1 ? lddy : D; A.ldadd = M > 1 ? ldadd : D; A.ldout = M > 1 ? lddx : D;
+  A.weight = weight; A.mean = const_cast<float*>(mean); A.rstd = const_cast<float*>(rstd);
+  A.part = sums ? static_cast<float*>(workspace) : nullptr;
+  A.wvec = aligned(weight, 16);
+  const Plan p = plan_of(M, D, 1);
+  const bool wide = wide_rows(x, M, ldx, D, dtype) && wide_rows(dy, M, lddy, D, dtype) && wide_rows(dx, M, lddx, D, dtype) && (!add || wide_rows(add, M, ldadd, D, dtype));
+  const int rc = launch(A, p, dtype, wide, 1, st);
+  if (rc != DMX_OK || !sums) return rc;
+  return start(dim3((D + 31) / 32, 2), 1024, 1, 0, st, columns_kernel, (const float*)A.part, p.groups, D, dweight, dbias);
+}
+
+}  // extern "C"

@@ -1,4 +1,4 @@
-// dmx_torch.cpp — what a training step calls (group_norm, linear and their gradients, AdamW's norm and step) for torch callers,
+// dmx_torch.cpp — what a training step calls (group_norm, layer_norm, linear and their gradients, AdamW's norm and step) for torch callers,
 // compiled: argument checks, allocation from torch's caching allocator and the call into the C ABI of include/dmx.h in one
 // Python call (through ctypes the calls took 5-28 us on the host, mostly checks and argument marshalling; now 3-14; the kernels of a small
 // problem take 4-8 us). train_ops.py wraps these and documents them. A function returns its result, or a negative
@@ -14,6 +14,8 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <type_traits>
+
 #include "dmx.h"
 
 namespace {
@@ -28,6 +30,9 @@ decltype(&dmx_linear_backward_workspace) linear_backward_workspace;
 decltype(&dmx_linear_backward) linear_backward;
 decltype(&dmx_adamw_grad_norm) adamw_norm;
 decltype(&dmx_adamw_step) adamw_step;
+decltype(&dmx_layer_norm_workspace) layer_workspace;
+decltype(&dmx_layer_norm_forward) layer_forward;
+decltype(&dmx_layer_norm_backward) layer_backward;
 
 struct Refused {
   int64_t code;
@@ -291,6 +296,89 @@ PyObject* linear_gradient(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---------------------------------------------------------------------------------------------- layer norm
+
+struct Flat {            // a (..., D) tensor whose rows are dense and lie at one stride
+  int64_t M, D, ld;
+};
+Flat flat(const at::Tensor& x) {
+  need(x.dim() >= 1 && x.is_cuda());
+  const auto shape = x.sizes(), st = x.strides();
+  const int64_t d = x.dim();
+  Flat r{1, shape[d - 1], shape[d - 1]};
+  need(r.D <= 1 || st[d - 1] == 1);
+  bool first = true;                                     // the innermost dimension of several rows has their stride
+  for (int64_t i = d - 2; i >= 0; --i) {
+    if (shape[i] > 1) {
+      if (first) r.ld = st[i];
+      need(st[i] == r.ld * r.M);
+      first = false;
+    }
+    r.M *= shape[i];
+    if (r.M == 0) break;
+  }
+  if (r.M == 0) r.ld = r.D;
+  return r;
+}
+Flat same_rows(const at::Tensor& t, const at::Tensor& x) {
+  need(t.scalar_type() == x.scalar_type() && t.device() == x.device() && t.sizes() == x.sizes());
+  return flat(t);
+}
+int layer_width(const Flat& X) {
+  need(X.D >= 1 && X.D <= DMX_LN_MAX_WIDTH);             // (the C entry takes an int)
+  return (int)X.D;
+}
+
+// x, weight, bias, eps, out -> (y, mean, rstd)
+PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    need(n == 5);
+    const at::Tensor& x = tensor(a[0]);
+    const at::Tensor *w = maybe(a[1]), *b = maybe(a[2]), *given = maybe(a[4]);
+    if (recorded(given, &x, w, b)) return PyLong_FromLong(kRecord);
+    const double eps = number(a[3]);
+    const int type = type_of(x);
+    const Flat X = flat(x);
+    const int D = layer_width(X);
+    const float *wp = vector(w, x, D), *bp = vector(b, x, D);
+    Call call(x);
+    at::Tensor y = given ? *given : at::empty(x.sizes(), x.options());
+    const Flat Y = same_rows(y, x);
+    const at::IntArrayRef lead = x.sizes().slice(0, x.dim() - 1);
+    at::Tensor mean = at::empty(lead, x.options().dtype(at::kFloat)), rstd = at::empty(lead, x.options().dtype(at::kFloat));
+    const int rc = layer_forward(X.M, D, type, in(&x), X.ld, wp, bp, (float)eps, out(&y), Y.ld, static_cast<float*>(out(&mean)),
+                                 static_cast<float*>(out(&rstd)), call.stream);
+    if (rc != DMX_OK) refuse(rc);
+    written(given);
+    return tuple(&y, &mean, &rstd);
+  });
+}
+
+// dy, x, mean, rstd, weight, add, out -> (dx, dweight, dbias)
+PyObject* layer_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    need(n == 7);
+    const at::Tensor &dy = tensor(a[0]), &x = tensor(a[1]), &mean = tensor(a[2]), &rstd = tensor(a[3]);
+    const at::Tensor *w = maybe(a[4]), *add = maybe(a[5]), *given = maybe(a[6]);
+    const int type = type_of(x);
+    const Flat X = flat(x), G = same_rows(dy, x), E = add ? same_rows(*add, x) : X;
+    const int D = layer_width(X);
+    const float *wp = vector(w, x, D), *mp = vector(&mean, x, X.M), *rp = vector(&rstd, x, X.M);
+    const int64_t bytes = layer_workspace(X.M, D, type);
+    if (bytes < 0) refuse(bytes);
+    Call call(x);
+    at::Tensor dx = given ? *given : at::empty(x.sizes(), x.options());
+    const Flat O = same_rows(dx, x);
+    at::Tensor dw = at::empty({D}, x.options().dtype(at::kFloat)), db = at::empty({D}, x.options().dtype(at::kFloat));
+    at::Tensor ws = workspace(bytes, x);
+    const int rc = layer_backward(X.M, D, type, in(&dy), G.ld, in(&x), X.ld, mp, rp, wp, in(add), E.ld, out(&dx), O.ld, static_cast<float*>(out(&dw)),
+                                  static_cast<float*>(out(&db)), start_of(ws), bytes, call.stream);
+    if (rc != DMX_OK) refuse(rc);
+    written(given);
+    return tuple(&dx, &dw, &db);
+  });
+}
+
 // ---------------------------------------------------------------------------------------------- AdamW
 
 // One of the optimizer's arrays: n entries of a type, dense, on its device.
@@ -346,21 +434,19 @@ PyObject* step(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// addresses of the nine entry points, in the order of the declarations above
+// addresses of the entry points, in the order of the declarations above
 PyObject* connect(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  void* p[9];
-  if (n != 9) return PyErr_SetString(PyExc_TypeError, "nine addresses"), nullptr;
-  for (int i = 0; i < 9; ++i)
-    if (!(p[i] = PyLong_AsVoidPtr(a[i]))) return PyErr_Occurred() ? nullptr : (PyErr_SetString(PyExc_ValueError, "null address"), nullptr);
-  norm_workspace = reinterpret_cast<decltype(norm_workspace)>(p[0]);
-  norm_forward = reinterpret_cast<decltype(norm_forward)>(p[1]);
-  norm_backward = reinterpret_cast<decltype(norm_backward)>(p[2]);
-  linear_workspace = reinterpret_cast<decltype(linear_workspace)>(p[3]);
-  linear_forward = reinterpret_cast<decltype(linear_forward)>(p[4]);
-  linear_backward_workspace = reinterpret_cast<decltype(linear_backward_workspace)>(p[5]);
-  linear_backward = reinterpret_cast<decltype(linear_backward)>(p[6]);
-  adamw_norm = reinterpret_cast<decltype(adamw_norm)>(p[7]);
-  adamw_step = reinterpret_cast<decltype(adamw_step)>(p[8]);
+  Py_ssize_t i = 0;
+  auto take = [&](auto& f) {
+    void* p = i < n ? PyLong_AsVoidPtr(a[i]) : nullptr;
+    ++i;
+    f = reinterpret_cast<std::decay_t<decltype(f)>>(p);
+    return p != nullptr;
+  };
+  auto all = [&](auto&... f) { return (take(f) && ...); };
+  if (!all(norm_workspace, norm_forward, norm_backward, linear_workspace, linear_forward, linear_backward_workspace, linear_backward, adamw_norm,
+           adamw_step, layer_workspace, layer_forward, layer_backward) || i != n)
+    return PyErr_Occurred() ? nullptr : (PyErr_SetString(PyExc_ValueError, "the entry points' addresses"), nullptr);
   Py_RETURN_NONE;
 }
 
@@ -370,6 +456,8 @@ PyMethodDef methods[] = {{"connect", FAST(connect)},
                          {"group_norm_backward", FAST(group_norm_backward)},
                          {"linear", FAST(linear)},
                          {"linear_backward", FAST(linear_gradient)},
+                         {"layer_norm", FAST(layer_norm)},
+                         {"layer_norm_backward", FAST(layer_norm_backward)},
                          {"adamw_grad_norm", FAST(grad_norm)},
                          {"adamw_step", FAST(step)},
                          {nullptr, nullptr, 0, nullptr}};

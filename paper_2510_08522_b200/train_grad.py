@@ -1,5 +1,5 @@
-"""What torch's differentiation does with the training operators: linear and group_norm record themselves where an
-input requires a gradient, and their gradients are linear_backward and group_norm_backward. First derivatives only."""
+"""What torch's differentiation does with the training operators: linear, group_norm and layer_norm record themselves where
+an input requires a gradient, and their gradients are the explicit backward calls. First derivatives only."""
 from __future__ import annotations
 
 import torch
@@ -47,3 +47,21 @@ class GroupNorm(torch.autograd.Function):
         need_x, _, need_w, need_b, _, _ = ctx.needs_input_grad
         dx, dw, db = T.group_norm_backward(dy.contiguous(), x, mean, rstd, ctx.groups, weight, bias, ctx.act)
         return dx if need_x else None, None, dw.view(weight.shape) if need_w else None, db.view(bias.shape) if need_b else None, None, None
+
+
+class LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        y, mean, rstd = T.layer_norm(x, weight, bias, eps)
+        ctx.save_for_backward(x, mean, rstd, weight)
+        ctx.bias_shape = None if bias is None else bias.shape
+        ctx.mark_non_differentiable(mean, rstd)
+        return y, mean, rstd
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, *_):
+        x, mean, rstd, weight = ctx.saved_tensors
+        need_x, need_w, need_b, _ = ctx.needs_input_grad
+        dx, dw, db = T.layer_norm_backward(dy.contiguous(), x, mean, rstd, weight)
+        return dx if need_x else None, dw.view(weight.shape) if need_w else None, db.view(ctx.bias_shape) if need_b else None, None

@@ -226,7 +226,8 @@ def _module():
         loader.exec_module(m)
         m.connect(*[ctypes.cast(f, ctypes.c_void_p).value for f in (
             L.dmx_group_norm_workspace, L.dmx_group_norm_forward, L.dmx_group_norm_backward, L.dmx_linear_workspace, L.dmx_linear_forward,
-            L.dmx_linear_backward_workspace, L.dmx_linear_backward, L.dmx_adamw_grad_norm, L.dmx_adamw_step)])
+            L.dmx_linear_backward_workspace, L.dmx_linear_backward, L.dmx_adamw_grad_norm, L.dmx_adamw_step,
+            L.dmx_layer_norm_workspace, L.dmx_layer_norm_forward, L.dmx_layer_norm_backward)])
         _fast = m
     return _fast
 
@@ -248,6 +249,26 @@ def group_norm_backward(dy, x, mean, rstd, groups, weight=None, bias=None, act="
     """Gradient of group_norm from its saved statistics -> (dx, dweight, dbias). out may be dy or x."""
     r = (_fast or _module()).group_norm_backward(dy, x, mean, rstd, groups, weight, bias, ACT.get(act, -1), out)
     return r if r.__class__ is tuple else _refuse("group_norm_backward", r)
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None):
+    """Layer norm of x's last dimension, fp32 or bf16 -> (y, mean, rstd), the statistics fp32 with x's leading dimensions.
+    weight, bias: fp32 (D,). x's rows are dense and lie at one stride (a slice of wider rows does); out may be x. Where an
+    input requires a gradient torch records the call (y's gradient; the statistics carry none), unless `out` is given."""
+    r = (_fast or _module()).layer_norm(x, weight, bias, eps, out)
+    if r.__class__ is tuple:
+        return r
+    if r != _RECORD:
+        _refuse("layer_norm", r)
+    from .train_grad import LayerNorm
+    return LayerNorm.apply(x, weight, bias, eps)
+
+
+def layer_norm_backward(dy, x, mean, rstd, weight=None, add=None, out=None):
+    """Gradient of layer_norm from its saved statistics -> (dx, dweight, dbias). add: a tensor that is added to dx before it
+    is rounded (the gradient that reaches x past the norm). out may be dy, x or add."""
+    r = (_fast or _module()).layer_norm_backward(dy, x, mean, rstd, weight, add, out)
+    return r if r.__class__ is tuple else _refuse("layer_norm_backward", r)
 
 
 def linear(x, weight, bias=None, act="none", residual=None, save=False, out=None):
