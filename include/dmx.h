@@ -604,6 +604,30 @@ int dmx_layer_norm_backward(int64_t M, int D, int dtype, const void* dy, int64_t
                             void* dx, int64_t lddx, float* dweight, float* dbias, void* workspace,
                             int64_t workspace_bytes, void* cuda_stream);
 
+/*
+ * dmx_embedding_* — rows of a table by token, scaled, and the table's gradient.
+ *   forward    y[n] = scale * table[ids[n]]                       table: V x D, y: N x D (DMX_F32 or DMX_BF16, both of dtype)
+ *   backward   dtable[v] = scale * (sum over n with ids[n] = v of dy[n])   (+ dtable[v] if accumulate)
+ * An id outside 0..V-1 (padding, an ignored place) gives a row of zeros and takes no gradient. Sums are fp32, in the order of n within
+ * chunks of neighbouring places in the sorted order; results are rounded once and are bitwise reproducible.
+ *   ids          N integers of id_bytes (4 or 8) bytes, aligned to their size
+ *   dtable       V x D of out_dtype. Without accumulate every row is written, zeros where no token is. With it rows without
+ *                a token are neither read nor written (a table tied to a head whose gradient is there already).
+ *   table, y, dy, dtable   rows ld* elements apart; inputs may repeat rows (0); outputs' ld >= D unless there is one row. Element alignment
+ *                suffices (16-byte aligned rows are faster).
+ *   workspace    at least dmx_embedding_backward_workspace(...) bytes, 256-byte aligned, contents undefined
+ * Errors: DMX_ERR_ARG (N or V > DMX_EMBEDDING_MAX, D > DMX_EMBEDDING_MAX_WIDTH, types, strides, null pointers, workspace too small),
+ * DMX_ERR_ALIGN, DMX_ERR_CUDA.
+ */
+#define DMX_EMBEDDING_MAX 0x7fffffff
+#define DMX_EMBEDDING_MAX_WIDTH 65536
+int dmx_embedding_forward(int64_t N, int64_t V, int64_t D, int dtype, int id_bytes, const void* ids, const void* table,
+                          int64_t ldt, float scale, void* y, int64_t ldy, void* cuda_stream);
+int64_t dmx_embedding_backward_workspace(int64_t N, int64_t V, int64_t D);
+int dmx_embedding_backward(int64_t N, int64_t V, int64_t D, int id_bytes, const void* ids, int dtype, const void* dy,
+                           int64_t lddy, float scale, int out_dtype, void* dtable, int64_t ldt, int accumulate,
+                           void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
 /* Frees the tables and the scratch. NULL is accepted; a handle that is not live (destroyed
  * already) gives DMX_ERR_HANDLE. The caller makes sure no step of this handle is still running. */
 int dmx_destroy(dmx_handle* h);

@@ -1,4 +1,4 @@
-// dmx_torch.cpp — what a training step calls (group_norm, layer_norm, linear and their gradients, AdamW's norm and step) for torch callers,
+// dmx_torch.cpp — what a training step calls (group_norm, layer_norm, embedding, linear and their gradients, AdamW's norm and step) for torch callers,
 // compiled: argument checks, allocation from torch's caching allocator and the call into the C ABI of include/dmx.h in one
 // Python call (through ctypes the calls took 5-28 us on the host, mostly checks and argument marshalling; now 3-14; the kernels of a small
 // problem take 4-8 us). train_ops.py wraps these and documents them. A function returns its result, or a negative
@@ -15,6 +15,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <type_traits>
+#include <vector>
 
 #include "dmx.h"
 
@@ -33,6 +34,9 @@ decltype(&dmx_adamw_step) adamw_step;
 decltype(&dmx_layer_norm_workspace) layer_workspace;
 decltype(&dmx_layer_norm_forward) layer_forward;
 decltype(&dmx_layer_norm_backward) layer_backward;
+decltype(&dmx_embedding_forward) lookup_forward;
+decltype(&dmx_embedding_backward_workspace) lookup_workspace;
+decltype(&dmx_embedding_backward) lookup_backward;
 
 struct Refused {
   int64_t code;
@@ -379,6 +383,79 @@ PyObject* layer_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---------------------------------------------------------------------------------------------- embedding
+
+int id_bytes(const at::Tensor& ids, const at::Tensor& on) {
+  need(ids.device() == on.device());
+  if (ids.scalar_type() == at::kLong) return 8;
+  need(ids.scalar_type() == at::kInt);
+  return 4;
+}
+Rows table_rows(const at::Tensor& t) {                   // of either type
+  need(t.dim() == 2 && t.is_cuda());
+  const Rows r{t.size(0), t.size(1), t.size(0) > 1 ? t.stride(0) : t.size(1)};
+  need(r.N <= 1 || t.stride(1) == 1);
+  return r;
+}
+// ids' leading dimensions and then D
+void of_tokens(const at::Tensor& t, const at::Tensor& ids, int64_t D) {
+  need(t.dim() == ids.dim() + 1 && t.size(-1) == D);
+  for (int64_t i = 0; i < ids.dim(); ++i) need(t.size(i) == ids.size(i));
+}
+
+// ids, table, scale, out -> y
+PyObject* embedding(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    need(n == 4);
+    const at::Tensor &ids = tensor(a[0]), &table = tensor(a[1]);
+    const double scale = number(a[2]);
+    const at::Tensor* given = maybe(a[3]);
+    if (recorded(given, &table)) return PyLong_FromLong(kRecord);
+    const Rows T = table_rows(table);
+    const int type = type_of(table), bytes = id_bytes(ids, table);
+    Call call(table);
+    std::vector<int64_t> shape(ids.sizes().begin(), ids.sizes().end());
+    shape.push_back(T.N);
+    at::Tensor y = given ? *given : at::empty(shape, table.options());
+    need(y.scalar_type() == table.scalar_type() && y.device() == table.device());
+    of_tokens(y, ids, T.N);
+    const Flat Y = flat(y);
+    const at::Tensor dense = ids.contiguous();
+    const int rc = lookup_forward(dense.numel(), T.M, T.N, type, bytes, in(&dense), in(&table), T.ld, (float)scale, out(&y), Y.ld, call.stream);
+    if (rc != DMX_OK) refuse(rc);
+    written(given);
+    return item(&y);
+  });
+}
+
+// dy, ids, rows, scale, out, accumulate -> dtable
+PyObject* embedding_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    need(n == 6);
+    const at::Tensor &dy = tensor(a[0]), &ids = tensor(a[1]);
+    const long V = whole(a[2]);
+    const double scale = number(a[3]);
+    const at::Tensor* given = maybe(a[4]);
+    const bool add = truth(a[5]);
+    need(V >= 0 && (given || !add));
+    const int type = type_of(dy), bytes_id = id_bytes(ids, dy);
+    const Flat G = flat(dy);
+    of_tokens(dy, ids, G.D);
+    const int64_t N = ids.numel(), bytes = lookup_workspace(N, V, G.D);
+    if (bytes < 0) refuse(bytes);
+    Call call(dy);
+    at::Tensor to = given ? *given : at::empty({V, G.D}, dy.options());
+    const Rows O = table_rows(to);
+    need(to.device() == dy.device() && O.M == V && O.N == G.D);
+    const at::Tensor dense = ids.contiguous();
+    at::Tensor ws = workspace(bytes, dy);
+    const int rc = lookup_backward(N, V, G.D, bytes_id, in(&dense), type, in(&dy), G.ld, (float)scale, type_of(to), out(&to), O.ld, add, start_of(ws), bytes, call.stream);
+    if (rc != DMX_OK) refuse(rc);
+    written(given);
+    return item(&to);
+  });
+}
+
 // ---------------------------------------------------------------------------------------------- AdamW
 
 // One of the optimizer's arrays: n entries of a type, dense, on its device.
@@ -445,7 +522,7 @@ PyObject* connect(PyObject*, PyObject* const* a, Py_ssize_t n) {
   };
   auto all = [&](auto&... f) { return (take(f) && ...); };
   if (!all(norm_workspace, norm_forward, norm_backward, linear_workspace, linear_forward, linear_backward_workspace, linear_backward, adamw_norm,
-           adamw_step, layer_workspace, layer_forward, layer_backward) || i != n)
+           adamw_step, layer_workspace, layer_forward, layer_backward, lookup_forward, lookup_workspace, lookup_backward) || i != n)
     return PyErr_Occurred() ? nullptr : (PyErr_SetString(PyExc_ValueError, "the entry points' addresses"), nullptr);
   Py_RETURN_NONE;
 }
@@ -458,6 +535,8 @@ PyMethodDef methods[] = {{"connect", FAST(connect)},
                          {"linear_backward", FAST(linear_gradient)},
                          {"layer_norm", FAST(layer_norm)},
                          {"layer_norm_backward", FAST(layer_norm_backward)},
+                         {"embedding", FAST(embedding)},
+                         {"embedding_backward", FAST(embedding_backward)},
                          {"adamw_grad_norm", FAST(grad_norm)},
                          {"adamw_step", FAST(step)},
                          {nullptr, nullptr, 0, nullptr}};

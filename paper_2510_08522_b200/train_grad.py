@@ -1,5 +1,5 @@
-"""What torch's differentiation does with the training operators: linear, group_norm and layer_norm record themselves where
-an input requires a gradient, and their gradients are the explicit backward calls. First derivatives only."""
+"""What torch's differentiation does with the training operators: linear, group_norm, layer_norm and embedding record
+themselves where an input requires a gradient, and their gradients are the explicit backward calls. First derivatives only."""
 from __future__ import annotations
 
 import torch
@@ -65,3 +65,16 @@ class LayerNorm(torch.autograd.Function):
         need_x, need_w, need_b, _ = ctx.needs_input_grad
         dx, dw, db = T.layer_norm_backward(dy.contiguous(), x, mean, rstd, weight)
         return dx if need_x else None, dw.view(weight.shape) if need_w else None, db.view(ctx.bias_shape) if need_b else None, None
+
+
+class Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, ids, table, scale):
+        ctx.rows, ctx.scale = table.shape[0], scale
+        ctx.save_for_backward(ids)
+        return T.embedding(ids, table, scale)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        return None, T.embedding_backward(dy.contiguous(), *ctx.saved_tensors, ctx.rows, ctx.scale), None

@@ -227,7 +227,8 @@ def _module():
         m.connect(*[ctypes.cast(f, ctypes.c_void_p).value for f in (
             L.dmx_group_norm_workspace, L.dmx_group_norm_forward, L.dmx_group_norm_backward, L.dmx_linear_workspace, L.dmx_linear_forward,
             L.dmx_linear_backward_workspace, L.dmx_linear_backward, L.dmx_adamw_grad_norm, L.dmx_adamw_step,
-            L.dmx_layer_norm_workspace, L.dmx_layer_norm_forward, L.dmx_layer_norm_backward)])
+            L.dmx_layer_norm_workspace, L.dmx_layer_norm_forward, L.dmx_layer_norm_backward, L.dmx_embedding_forward,
+            L.dmx_embedding_backward_workspace, L.dmx_embedding_backward)])
         _fast = m
     return _fast
 
@@ -269,6 +270,25 @@ def layer_norm_backward(dy, x, mean, rstd, weight=None, add=None, out=None):
     is rounded (the gradient that reaches x past the norm). out may be dy, x or add."""
     r = (_fast or _module()).layer_norm_backward(dy, x, mean, rstd, weight, add, out)
     return r if r.__class__ is tuple else _refuse("layer_norm_backward", r)
+
+
+def embedding(ids, table, scale=1.0, out=None):
+    """scale * table[ids] -> ids' shape + (D,), of the table's type (fp32 or bf16). ids: int32 or int64, any shape; an id outside
+    the table's rows gives zeros. Where the table requires a gradient torch records the call, unless `out` is given."""
+    r = (_fast or _module()).embedding(ids, table, scale, out)
+    if r.__class__ is not int:
+        return r
+    if r != _RECORD:
+        _refuse("embedding", r)
+    from .train_grad import Embedding
+    return Embedding.apply(ids, table, scale)
+
+
+def embedding_backward(dy, ids, rows, scale=1.0, out=None, accumulate=False):
+    """Gradient of embedding in its table of `rows` rows -> (rows, D), of dy's type or as `out` is (fp32 or bf16). All of it is
+    written, or, with accumulate, the tokens' shares are added to what `out` holds (the gradient of a tied head)."""
+    r = (_fast or _module()).embedding_backward(dy, ids, rows, scale, out, accumulate)
+    return r if r.__class__ is not int else _refuse("embedding_backward", r)
 
 
 def linear(x, weight, bias=None, act="none", residual=None, save=False, out=None):

@@ -1,4 +1,4 @@
-"""Argument checks of layer norm that need no GPU: the C entry points refuse what they document before any device call."""
+"""Argument checks of layer norm and of the embedding lookup that need no GPU: the C entry points refuse what they document before any device call."""
 import pytest
 
 import paper_2510_08522_b200 as D
@@ -29,10 +29,35 @@ def test_layer_norm_refuses_bad_shapes_strides_and_pointers():
         assert backward(**bad) == B.ERR_ALIGN, bad
 
 
+def test_embedding_refuses_bad_sizes_types_strides_and_pointers():
+    L = B.lib()
+    big = 1 << 31
+    for a in ((-1, 4, 8), (4, -1, 8), (4, 4, -1), (big, 4, 8), (4, big, 8), (4, 4, 65537)):
+        assert L.dmx_embedding_backward_workspace(*a) == B.ERR_ARG
+    assert L.dmx_embedding_backward_workspace(0, 4, 8) == 0 and L.dmx_embedding_backward_workspace(100, 4, 8) >= 4 * 400
+
+    def forward(N=4, V=5, n=8, dt=0, ib=8, ids=64, table=128, ldt=8, scale=1.0, y=1024, ldy=8):
+        return L.dmx_embedding_forward(N, V, n, dt, ib, ids, table, ldt, scale, y, ldy, None)
+    for bad in (dict(N=-1), dict(N=big), dict(V=big), dict(n=65537), dict(dt=2), dict(ib=2), dict(ids=None), dict(table=None), dict(y=None), dict(ldt=-1), dict(ldy=7)):
+        assert forward(**bad) == B.ERR_ARG, bad
+    for bad in (dict(ids=68), dict(ids=66, ib=4), dict(table=130), dict(y=1026), dict(dt=1, table=129)):
+        assert forward(**bad) == B.ERR_ALIGN, bad
+    assert forward(N=0) == B.OK and forward(n=0, ldy=0) == B.OK
+
+    def backward(N=4, V=5, n=8, ib=8, ids=64, dt=0, dy=128, lddy=8, odt=0, out=1024, ldt=8, add=0, ws=4096, size=1 << 20):
+        return L.dmx_embedding_backward(N, V, n, ib, ids, dt, dy, lddy, 1.0, odt, out, ldt, add, ws, size, None)
+    for bad in (dict(N=big), dict(V=-1), dict(n=65537), dict(ib=1), dict(dt=3), dict(odt=-1), dict(lddy=-1), dict(ldt=7), dict(ids=None), dict(dy=None), dict(out=None), dict(ws=None), dict(size=100)):
+        assert backward(**bad) == B.ERR_ARG, bad
+    for bad in (dict(ids=60), dict(dy=130), dict(out=1026), dict(ws=4112)):
+        assert backward(**bad) == B.ERR_ALIGN, bad
+    assert backward(V=0) == B.OK and backward(n=0, ldt=0) == B.OK and backward(N=0, add=1) == B.OK
+
+
 def test_torch_callers_get_errors_for_what_is_no_cuda_tensor():
     torch = pytest.importorskip("torch")
     x, m = torch.zeros(4, 8), torch.zeros(4)
     for call in (lambda: D.layer_norm(x), lambda: D.layer_norm(None), lambda: D.layer_norm(x, "w"), lambda: D.layer_norm([1.0]),
-                 lambda: D.layer_norm_backward(x, x, m, m), lambda: D.layer_norm_backward(x, None, m, m), lambda: D.layer_norm_backward(x, x, m, 3)):
+                 lambda: D.embedding(m.long(), x), lambda: D.embedding(3, x), lambda: D.embedding(m.long(), None), lambda: D.embedding_backward(x, m.long(), 5),
+                 lambda: D.embedding_backward(x, [1], 5), lambda: D.layer_norm_backward(x, x, m, m), lambda: D.layer_norm_backward(x, None, m, m), lambda: D.layer_norm_backward(x, x, m, 3)):
         with pytest.raises(D.DmxError):
             call()
