@@ -628,6 +628,40 @@ int dmx_embedding_backward(int64_t N, int64_t V, int64_t D, int id_bytes, const 
                            int64_t lddy, float scale, int out_dtype, void* dtable, int64_t ldt, int accumulate,
                            void* workspace, int64_t workspace_bytes, void* cuda_stream);
 
+/*
+ * dmx_cross_entropy_* — softmax cross entropy of a linear layer over a vocabulary, its logits never kept, and its gradient (bf16 operands, fp32
+ * accumulation on the tensor cores).
+ *   forward    z = x W^T + bias,  lse[n] = log(sum over v of exp(z[n, v])),  loss[n] = lse[n] - z[n, target[n]]     x: N x D, W: V x D
+ *   backward   G[n, v] = (exp(z[n, v] - lse[n]) - [v = target[n]]) * dloss[n],  dx = G W,  dW = G^T x,  dbias = column sums of G
+ * A row whose target lies outside 0..V-1 (an ignored place) has loss 0 and no gradient; its lse is computed all the same. backward
+ * computes the logits again and goes through the vocabulary in pieces: the workspace holds a piece of G (256 MB at most, or 256 words), and,
+ * where there are several, dx in fp32. Everything up to a store is fp32, with one exception: G is rounded to bf16 before the two
+ * products (the tensor cores take 16-bit operands); dbias is summed from the unrounded G. Exponentials are good to 2 ulp. Logits
+ * of -inf (a bias of -inf) are words that do not occur; a logit of +inf or NaN makes its row's loss and gradient NaN, as does a row without
+ * any finite logit.
+ *   x, w, bias, dx, dw, dbias   bf16, row-major, ld* = elements from row to row (>= 0; of outputs >= D unless there is one row; inputs may
+ *              repeat rows with 0); element alignment suffices. Operands whose start or rows are not 16-byte aligned, or repeat, are first
+ *              laid out in the workspace.
+ *   bias       V entries, or NULL
+ *   target     N integers of target_bytes (4 or 8) bytes, aligned to their size
+ *   loss, lse, dloss   fp32, N entries; dloss with a stride in elements (0: one value for all rows)
+ *   dx, dw, dbias   each may be NULL and is then not computed
+ *   workspace  at least dmx_cross_entropy_workspace(...) / dmx_cross_entropy_backward_workspace(...) bytes for the same arguments, 256-byte
+ *              aligned, contents undefined
+ * N = 0 gives dW = 0 and dbias = 0. Results are bitwise reproducible. Waits inside the kernels are bounded; dmx_linear_status counts these too.
+ * Errors: DMX_ERR_ARG (extents < 1 of V or D, or > DMX_LINEAR_MAX_EXTENT, strides, null pointers, workspace too small), DMX_ERR_ALIGN,
+ * DMX_ERR_CUDA.
+ */
+int64_t dmx_cross_entropy_workspace(int64_t N, int64_t V, int64_t D, const void* x, int64_t ldx, const void* w, int64_t ldw);
+int dmx_cross_entropy_forward(int64_t N, int64_t V, int64_t D, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                              const void* bias, int target_bytes, const void* target, float* loss, float* lse, void* workspace,
+                              int64_t workspace_bytes, void* cuda_stream);
+int64_t dmx_cross_entropy_backward_workspace(int64_t N, int64_t V, int64_t D, const void* x, int64_t ldx, const void* w, int64_t ldw);
+int dmx_cross_entropy_backward(int64_t N, int64_t V, int64_t D, const float* dloss, int64_t dloss_stride, const void* x, int64_t ldx,
+                               const void* w, int64_t ldw, const void* bias, int target_bytes, const void* target,
+                               const float* lse, void* dx, int64_t lddx, void* dw, int64_t lddw, void* dbias, void* workspace,
+                               int64_t workspace_bytes, void* cuda_stream);
+
 /* Frees the tables and the scratch. NULL is accepted; a handle that is not live (destroyed
  * already) gives DMX_ERR_HANDLE. The caller makes sure no step of this handle is still running. */
 int dmx_destroy(dmx_handle* h);

@@ -29,7 +29,8 @@ EXPORTS = ("dmx_create", "dmx_state_len", "dmx_step", "dmx_step_adam", "dmx_step
            "dmx_linear_workspace", "dmx_linear_forward", "dmx_linear_backward_workspace", "dmx_linear_backward", "dmx_linear_status",
            "dmx_group_norm_plan", "dmx_linear_plan",
            "dmx_layer_norm_workspace", "dmx_layer_norm_forward", "dmx_layer_norm_backward",
-           "dmx_embedding_forward", "dmx_embedding_backward_workspace", "dmx_embedding_backward")
+           "dmx_embedding_forward", "dmx_embedding_backward_workspace", "dmx_embedding_backward",
+           "dmx_cross_entropy_workspace", "dmx_cross_entropy_forward", "dmx_cross_entropy_backward_workspace", "dmx_cross_entropy_backward")
 CTL_ACTIONS = (-100, -25, 0, 25, 100)
 
 _lib = None
@@ -152,6 +153,13 @@ def lib():
         L.dmx_embedding_backward_workspace.restype = i64
         L.dmx_embedding_backward.argtypes = [i64, i64, i64, i32, vp, i32, vp, i64, f32, i32, vp, i64, i32, vp, i64, vp]
         L.dmx_embedding_backward.restype = i32
+        for f in (L.dmx_cross_entropy_workspace, L.dmx_cross_entropy_backward_workspace):
+            f.argtypes = [i64, i64, i64, vp, i64, vp, i64]
+            f.restype = i64
+        L.dmx_cross_entropy_forward.argtypes = [i64, i64, i64, vp, i64, vp, i64, vp, i32, vp, vp, vp, vp, i64, vp]
+        L.dmx_cross_entropy_forward.restype = i32
+        L.dmx_cross_entropy_backward.argtypes = [i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i32, vp, vp, vp, i64, vp, i64, vp, vp, i64, vp]
+        L.dmx_cross_entropy_backward.restype = i32
         L.dmx_linear_status.argtypes = [ctypes.POINTER(i32)]
         L.dmx_linear_status.restype = i32
         L.dmx_destroy.argtypes = [vp]

@@ -22,8 +22,8 @@ NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", 
               "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC]
 
 TARGETS = {
-    "libdmx.so": (["dmx.cu", "dmx_static.cu", "dmx_agg.cu", "dmx_ctl.cu", "dmx_adamw.cu", "dmx_group_norm.cu", "dmx_linear.cu", "dmx_layer_norm.cu", "dmx_embedding.cu"],
-                  ["dmx_kernels.cuh", "dmx_act.cuh", "dmx_f32x2.cuh", "dmx_host.h", "dmx_rows.cuh", os.path.join(INCLUDE, "dmx.h")]),
+    "libdmx.so": (["dmx.cu", "dmx_static.cu", "dmx_agg.cu", "dmx_ctl.cu", "dmx_adamw.cu", "dmx_group_norm.cu", "dmx_linear.cu", "dmx_layer_norm.cu", "dmx_embedding.cu", "dmx_cross_entropy.cu"],
+                  ["dmx_kernels.cuh", "dmx_act.cuh", "dmx_f32x2.cuh", "dmx_host.h", "dmx_rows.cuh", "dmx_gemm.cuh", os.path.join(INCLUDE, "dmx.h")]),
     "libdmx_gen.so": (["dmx_gen.cu"], []),
 }
 

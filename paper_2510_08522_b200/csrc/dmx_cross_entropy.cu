@@ -1,0 +1,394 @@
+// dmx_cross_entropy.cu — softmax cross entropy of a linear layer over a vocabulary, logits never kept, and its gradient.
+//
+//   forward    z = x W^T + b, lse[n] = log sum_v exp z[n, v], loss[n] = lse[n] - z[n, t_n]
+//   backward   G = (exp(z - lse) - [v = t_n]) dloss[n], dx = G W, dW = G^T x, db = column sums of G
+//
+// forward is one product (dmx_gemm.cuh) whose epilogue keeps, of a row's 32-column chunks, the running maximum and the sum of powers
+// of two of the distances from it (one pass, in units of log2 e: no rounding between a sum and the maximum that belongs to it); a
+// small launch joins the tiles' pairs. backward goes through the vocabulary in pieces: a product as forward's whose epilogue
+// makes a piece of G, bf16, then the two products that take it. dx is summed over the pieces in fp32.
+// G is rounded to bf16 because the tensor cores take 16-bit operands; everything else up to a store is fp32.
+// Bound: the tensor cores, 2 N V D operations forward and 6 N V D backward (the logits are computed again).
+#include "dmx.h"
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "dmx_act.cuh"
+#include "dmx_gemm.cuh"
+
+namespace {
+
+using namespace dmx_gemm;
+using dmx_act::ex2;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+
+// ---------------------------------------------------------------------------------------------- forward
+
+__device__ __forceinline__ int64_t target_at(const void* targets, int wide, int n) {
+  return wide ? __ldg(static_cast<const long long*>(targets) + n) : (int64_t)__ldg(static_cast<const int*>(targets) + n);
+}
+
+template <int NC>
+__device__ __forceinline__ void add_bias(const bf16* bias, int cols, float (&v)[NC], int c0) {
+  if (!bias) return;
+  if (c0 + NC <= cols && (reinterpret_cast<uintptr_t>(bias + c0) & 15) == 0) {
+#pragma unroll
+    for (int u = 0; u < NC / 8; ++u) {
+      const uint4 b = __ldg(reinterpret_cast<const uint4*>(bias + c0) + u);
+      const unsigned w[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float2 t = widen2(w[k]);
+        v[8 * u + 2 * k] += t.x; v[8 * u + 2 * k + 1] += t.y;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+      if (c0 + i < cols) v[i] += bf_value(__ldg(reinterpret_cast<const unsigned short*>(bias) + c0 + i));
+  }
+}
+
+struct SumArgs : GemmShape {
+  const bf16* bias;
+  const void* target;
+  int wide_target, groups;        // groups: warps that share a row of a tile
+  float* hit;                     // the targets' logits
+  float2* part;                   // [tiles across x groups][rows]: maximum in units of log2 e, sum
+};
+
+struct SumEpilogue {
+  typedef SumArgs Args;
+  float top = -INFINITY, sum = 0.f;
+  int64_t target = -1;
+  __device__ __forceinline__ void begin(const Args& A, int r0, int c0, int lane) {
+    if (r0 + lane < A.rowsA) target = target_at(A.target, A.wide_target, r0 + lane);
+  }
+  template <int NC>
+  __device__ __forceinline__ void chunk(const Args& A, float (&v)[NC], uint4*, int r0, int c0, int lane) {
+    add_bias(A.bias, A.rowsB, v, c0);
+    if (c0 + NC > A.rowsB) {
+#pragma unroll
+      for (int i = 0; i < NC; ++i)
+        if (c0 + i >= A.rowsB) v[i] = -INFINITY;
+    }
+    const bool here = target >= c0 && target < c0 + NC && target < A.rowsB;
+    if (__any_sync(0xffffffffu, here)) {
+#pragma unroll
+      for (int i = 0; i < NC; ++i)
+        if (here && target == c0 + i) A.hit[r0 + lane] = v[i];
+    }
+    float most = v[0];
+#pragma unroll
+    for (int i = 1; i < NC; ++i) most = fmaxf(most, v[i]);
+    most = fmaxf(top, most * kLog2e);
+    const float from = most == -INFINITY ? 0.f : most;         // (nothing but -inf so far)
+    float s = sum * ex2(top - from);
+#pragma unroll
+    for (int i = 0; i < NC; ++i) s += ex2(fmaf(v[i], kLog2e, -from));
+    top = most;
+    sum = s;
+  }
+  __device__ __forceinline__ void end(const Args& A, int r0, int tb, int group, int lane) {
+    if (group < A.groups && r0 + lane < A.rowsA) A.part[(int64_t)(tb * A.groups + group) * A.rowsA + r0 + lane] = make_float2(top, sum);
+  }
+};
+
+// 32 rows a CTA, its warps take every eighth pair
+__global__ void __launch_bounds__(256) join_kernel(const float2* part, int parts, int N, int V, const float* hit, const void* target, int wide_target, float* loss, float* lse) {
+  __shared__ float2 sh[8][32];
+  start_dependents();
+  wait_for_previous();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = blockIdx.x * 32 + lane;
+  float top = -INFINITY, sum = 0.f;
+  auto take = [&](float2 p) {
+    const float most = fmaxf(top, p.x), from = most == -INFINITY ? 0.f : most;
+    sum = sum * ex2(top - from) + p.y * ex2(p.x - from);
+    top = most;
+  };
+  if (n < N) {
+#pragma unroll 8
+    for (int i = warp; i < parts; i += 8) take(part[(int64_t)i * N + n]);
+  }
+  sh[warp][lane] = make_float2(top, sum);
+  __syncthreads();
+  if (warp > 0 || n >= N) return;
+  for (int w = 1; w < 8; ++w) take(sh[w][lane]);
+  const float l = (top + log2f(sum)) * kLn2;
+  const int64_t t = target_at(target, wide_target, n);
+  lse[n] = l;
+  loss[n] = t >= 0 && t < V ? l - hit[n] : 0.f;
+}
+
+// ---------------------------------------------------------------------------------------------- backward
+
+struct SlopeArgs : GemmShape {
+  const bf16* bias;               // of the piece
+  const void* target;
+  int wide_target, first, vocabulary, vec;    // first: the piece's first word
+  const float *lse, *dloss;
+  int64_t stride;                 // of dloss: 1 or 0
+  bf16* g;
+  int64_t ldg;
+  float* columns;                 // [rows / 32][piece]: sums over 32 rows, or NULL
+};
+
+struct SlopeEpilogue {
+  typedef SlopeArgs Args;
+  float lse2 = 0.f, scale = 0.f;
+  int64_t target = -1;
+  __device__ __forceinline__ void begin(const Args& A, int r0, int, int lane) {
+    const int n = r0 + lane;
+    if (n >= A.rowsA) return;
+    const int64_t t = target_at(A.target, A.wide_target, n);
+    const bool live = t >= 0 && t < A.vocabulary;
+    lse2 = __ldg(A.lse + n) * kLog2e;
+    scale = live ? __ldg(A.dloss + n * A.stride) : 0.f;
+    target = live ? t - A.first : -1;
+  }
+  template <int NC>
+  __device__ __forceinline__ void chunk(const Args& A, float (&v)[NC], uint4* stage, int r0, int c0, int lane) {
+    add_bias(A.bias, A.rowsB, v, c0);
+    // a row without a target has scale 0: its values are zeros whatever its logits are
+#pragma unroll
+    for (int i = 0; i < NC; ++i) v[i] = scale == 0.f ? 0.f : ex2(fmaf(v[i], kLog2e, -lse2)) * scale;
+    const bool here = target >= c0 && target < c0 + NC;
+    if (__any_sync(0xffffffffu, here)) {
+#pragma unroll
+      for (int i = 0; i < NC; ++i)
+        if (here && target == c0 + i) v[i] -= scale;
+    }
+#pragma unroll
+    for (int u = 0; u < NC / 8; ++u)
+      *unit(stage, lane, u) = make_uint4(pack2(v[8 * u], v[8 * u + 1]), pack2(v[8 * u + 2], v[8 * u + 3]), pack2(v[8 * u + 4], v[8 * u + 5]),
+                                         pack2(v[8 * u + 6], v[8 * u + 7]));
+    store_tile<32, NC>(A.g, A.ldg, A.vec, stage, r0, A.rowsA, c0, A.rowsB, lane);
+    if (A.columns) {
+      // lane i ends with column i's sum: in every step half of the columns go to the lane across
+      static_assert(NC == 32, "a column per lane");
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) {
+        const bool high = lane & o;
+#pragma unroll
+        for (int i = 0; i < o; ++i) {
+          const float keep = high ? v[i + o] : v[i], give = high ? v[i] : v[i + o];
+          v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+        }
+      }
+      if (r0 < A.rowsA && c0 + lane < A.rowsB) A.columns[(int64_t)(r0 >> 5) * A.rowsB + c0 + lane] = v[0];
+    }
+  }
+  __device__ __forceinline__ void end(const Args&, int, int, int, int) {}
+};
+
+// dx over several pieces: sums in fp32, in an order of their own (a warp's 32 rows x 32 columns after one another, a column of lanes at a time)
+struct AddArgs : GemmShape {
+  float* sums;
+  bf16* y;
+  int64_t ldy;
+  int first, last, vec;
+};
+
+template <int BN>
+struct AddEpilogue {
+  typedef AddArgs Args;
+  __device__ __forceinline__ void begin(const Args&, int, int, int) {}
+  template <int NC>
+  __device__ __forceinline__ void chunk(const Args& A, float (&v)[NC], uint4* stage, int r0, int c0, int lane) {
+    float* at = A.sums + ((int64_t)(r0 >> 5) * (A.tilesB * (BN / 32)) + (c0 >> 5)) * 1024 + lane;
+    if (!A.first) {
+#pragma unroll
+      for (int i = 0; i < NC; ++i) v[i] += __ldcs(at + i * 32);
+    }
+    if (!A.last) {
+#pragma unroll
+      for (int i = 0; i < NC; ++i) __stcs(at + i * 32, v[i]);
+      return;
+    }
+#pragma unroll
+    for (int u = 0; u < NC / 8; ++u)
+      *unit(stage, lane, u) = make_uint4(pack2(v[8 * u], v[8 * u + 1]), pack2(v[8 * u + 2], v[8 * u + 3]), pack2(v[8 * u + 4], v[8 * u + 5]),
+                                         pack2(v[8 * u + 6], v[8 * u + 7]));
+    store_tile<32, NC>(A.y, A.ldy, A.vec, stage, r0, A.rowsA, c0, A.rowsB, lane);
+  }
+  __device__ __forceinline__ void end(const Args&, int, int, int, int) {}
+};
+
+// db from the sums over 32 rows each: 32 columns a CTA
+__global__ void __launch_bounds__(1024) columns_kernel(const float* sums, int rows, int cols, bf16* out) {
+  __shared__ float sh[32][33];
+  start_dependents();
+  wait_for_previous();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+  float s = 0.f;
+  if (c < cols) {
+#pragma unroll 4
+    for (int r = warp; r < rows; r += 32) s += sums[(int64_t)r * cols + c];
+  }
+  sh[warp][lane] = s;
+  __syncthreads();
+  if (warp > 0 || c >= cols) return;
+  for (int w = 1; w < 32; ++w) s += sh[w][lane];
+  out[c] = __float2bfloat16_rn(s);
+}
+
+// ---------------------------------------------------------------------------------------------- host
+
+template <class E>
+int product_rows(const Matrix& a, const Matrix& b, typename E::Args& A, const Choice& c, cudaStream_t st) {      // D's rows are a's
+  if (c.pair) return c.bn == 256 ? launch_gemm<256, true, 1, E>(a, b, A, st) : launch_gemm<128, true, 1, E>(a, b, A, st);
+  if (c.bn == 256) return launch_gemm<256, false, 1, E>(a, b, A, st);
+  return c.bn == 128 ? launch_gemm<128, false, 1, E>(a, b, A, st) : launch_gemm<64, false, 1, E>(a, b, A, st);
+}
+Choice choose_rows(int64_t N, int64_t V, int64_t D) { return choose(N, V, (int)((D + kBK - 1) / kBK), false, false); }
+int groups_of(const Choice& c) { return c.bn / 32 < kEpiWarps / 4 ? c.bn / 32 : kEpiWarps / 4; }
+
+bool sizes_ok(int64_t N, int64_t V, int64_t D) {
+  const int64_t most = DMX_LINEAR_MAX_EXTENT;
+  return N >= 0 && V >= 1 && D >= 1 && N <= most && V <= most && D <= most;
+}
+bool in_ok(int64_t rows, int64_t ld) { return rows <= 1 || ld >= 0; }
+bool out_ok(int64_t rows, int64_t cols, int64_t ld) { return rows <= 1 || ld >= cols; }
+Matrix matrix(const void* p, int64_t rows, int64_t cols, int64_t ld) { return {static_cast<const bf16*>(p), rows, cols, rows > 1 ? ld : cols}; }
+
+struct ForwardPlan {
+  Choice choice;
+  int64_t parts, part, hit, total;
+};
+ForwardPlan forward_plan(const Matrix& x, const Matrix& w) {
+  ForwardPlan p;
+  p.choice = choose_rows(x.rows, w.rows, x.cols);
+  p.parts = (w.rows + p.choice.bn - 1) / p.choice.bn * groups_of(p.choice);
+  p.part = pad256(p.parts * x.rows * 8);
+  p.hit = pad256(x.rows * 4);
+  p.total = p.part + p.hit + laid_out_bytes(x) + laid_out_bytes(w);
+  return p;
+}
+
+// Pieces of the vocabulary: G of a piece takes 256 MB at most (but 256 words at least).
+struct BackPlan {
+  int64_t pieces, words, g, columns, sums, total;
+};
+BackPlan back_plan(const Matrix& x, const Matrix& w) {
+  const int64_t N = x.rows, V = w.rows, D = x.cols;
+  BackPlan p;
+  int64_t most = ((int64_t)1 << 28) / (2 * N) / 256 * 256;
+  if (most < 256) most = 256;
+  p.pieces = (V + most - 1) / most;
+  p.words = ((V + p.pieces - 1) / p.pieces + 255) / 256 * 256;
+  p.pieces = (V + p.words - 1) / p.words;
+  const int64_t cols = p.words < V ? p.words : V;
+  p.g = pad256(N * pad8(cols) * 2);
+  p.columns = pad256((N + 31) / 32 * cols * 4);
+  p.sums = p.pieces > 1 ? ((N + 255) / 256 * 256) * ((D + 255) / 256 * 256) * 4 : 0;
+  p.total = p.g + p.columns + p.sums + laid_out_bytes(x) + laid_out_bytes(w);
+  return p;
+}
+
+}  // namespace
+
+namespace dmx_gemm {
+
+bool loss_gave_up(unsigned* n) { return dmxh::cuda_ok(cudaMemcpyFromSymbol(n, g_gave_up, sizeof *n)); }
+
+}  // namespace dmx_gemm
+
+extern "C" {
+
+int64_t dmx_cross_entropy_workspace(int64_t N, int64_t V, int64_t D, const void* x, int64_t ldx, const void* w, int64_t ldw) {
+  if (!sizes_ok(N, V, D)) return DMX_ERR_ARG;
+  return N == 0 ? 0 : forward_plan(matrix(x, N, D, ldx), matrix(w, V, D, ldw)).total;
+}
+
+int dmx_cross_entropy_forward(int64_t N, int64_t V, int64_t D, const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, int target_bytes,
+                              const void* target, float* loss, float* lse, void* workspace, int64_t workspace_bytes, void* cuda_stream) {
+  if (!sizes_ok(N, V, D) || !in_ok(N, ldx) || !in_ok(V, ldw) || (target_bytes != 4 && target_bytes != 8)) return DMX_ERR_ARG;
+  if (N == 0) return DMX_OK;
+  if (!x || !w || !target || !loss || !lse) return DMX_ERR_ARG;
+  if (!aligned(x, 2) || !aligned(w, 2) || !aligned(bias, 2) || !aligned(target, target_bytes) || !aligned(loss, 4) || !aligned(lse, 4) || !aligned(workspace, 256)) return DMX_ERR_ALIGN;
+  Matrix a = matrix(x, N, D, ldx), b = matrix(w, V, D, ldw);
+  const ForwardPlan p = forward_plan(a, b);
+  if (workspace_bytes < p.total || !workspace) return DMX_ERR_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  SumArgs A = {};
+  A.rowsA = (int)N; A.rowsB = (int)V; A.kblocks = (int)((D + kBK - 1) / kBK);
+  A.bias = static_cast<const bf16*>(bias); A.target = target; A.wide_target = target_bytes == 8; A.groups = groups_of(p.choice);
+  A.part = reinterpret_cast<float2*>(ws);
+  A.hit = reinterpret_cast<float*>(ws + p.part);
+  ws += p.part + p.hit;
+  Jobs jobs;
+  int n = 0;
+  lay_out(a, ws, jobs, n);
+  lay_out(b, ws, jobs, n);
+  int rc = n > 0 ? run_jobs(jobs, n, DMX_ACT_NONE, st) : DMX_OK;
+  if (rc == DMX_OK) rc = product_rows<SumEpilogue>(a, b, A, p.choice, st);
+  if (rc != DMX_OK) return rc;
+  return start(dim3((unsigned)((N + 31) / 32)), st, join_kernel, (const float2*)A.part, (int)p.parts, (int)N, (int)V, (const float*)A.hit, target, A.wide_target, loss, lse);
+}
+
+int64_t dmx_cross_entropy_backward_workspace(int64_t N, int64_t V, int64_t D, const void* x, int64_t ldx, const void* w, int64_t ldw) {
+  if (!sizes_ok(N, V, D)) return DMX_ERR_ARG;
+  return N == 0 ? 0 : back_plan(matrix(x, N, D, ldx), matrix(w, V, D, ldw)).total;
+}
+
+int dmx_cross_entropy_backward(int64_t N, int64_t V, int64_t D, const float* dloss, int64_t dloss_stride, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                               const void* bias, int target_bytes, const void* target, const float* lse, void* dx, int64_t lddx, void* dw, int64_t lddw, void* dbias,
+                               void* workspace, int64_t workspace_bytes, void* cuda_stream) {
+  if (!sizes_ok(N, V, D) || !in_ok(N, ldx) || !in_ok(V, ldw) || (N > 1 && dloss_stride < 0) || (target_bytes != 4 && target_bytes != 8) || (dx && !out_ok(N, D, lddx)) ||
+      (dw && !out_ok(V, D, lddw))) return DMX_ERR_ARG;
+  if (!aligned(x, 2) || !aligned(w, 2) || !aligned(bias, 2) || !aligned(target, target_bytes) || !aligned(dloss, 4) || !aligned(lse, 4) || !aligned(dx, 2) || !aligned(dw, 2) ||
+      !aligned(dbias, 2) || !aligned(workspace, 256)) return DMX_ERR_ALIGN;
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (N == 0) {                                // empty sums
+    if (dw && !dmxh::cuda_ok(cudaMemset2DAsync(dw, (V > 1 ? lddw : D) * 2, 0, D * 2, V, st))) return DMX_ERR_CUDA;
+    if (dbias && !dmxh::cuda_ok(cudaMemsetAsync(dbias, 0, V * 2, st))) return DMX_ERR_CUDA;
+    return DMX_OK;
+  }
+  if (!dx && !dw && !dbias) return DMX_OK;
+  if (!x || !w || !target || !lse || !dloss) return DMX_ERR_ARG;
+  Matrix a = matrix(x, N, D, ldx), b = matrix(w, V, D, ldw);
+  const BackPlan p = back_plan(a, b);
+  if (workspace_bytes < p.total || !workspace) return DMX_ERR_ARG;
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  bf16* g = reinterpret_cast<bf16*>(ws);
+  float* columns = reinterpret_cast<float*>(ws + p.g);
+  float* sums = reinterpret_cast<float*>(ws + p.g + p.columns);
+  ws += p.g + p.columns + p.sums;
+  Jobs jobs;
+  int n = 0;
+  lay_out(a, ws, jobs, n);
+  lay_out(b, ws, jobs, n);
+  int rc = n > 0 ? run_jobs(jobs, n, DMX_ACT_NONE, st) : DMX_OK;
+  for (int64_t first = 0; first < V && rc == DMX_OK; first += p.words) {
+    const int64_t words = V - first < p.words ? V - first : p.words;
+    const Matrix piece = {b.p + first * b.ld, words, D, b.ld};
+    SlopeArgs A = {};
+    A.rowsA = (int)N; A.rowsB = (int)words; A.kblocks = (int)((D + kBK - 1) / kBK);
+    A.bias = bias ? static_cast<const bf16*>(bias) + first : nullptr; A.target = target; A.wide_target = target_bytes == 8;
+    A.first = (int)first; A.vocabulary = (int)V; A.lse = lse; A.dloss = dloss; A.stride = N > 1 ? dloss_stride : 0;
+    A.g = g; A.ldg = pad8(words); A.vec = 1; A.columns = dbias ? columns : nullptr;
+    rc = product_rows<SlopeEpilogue>(a, piece, A, choose_rows(N, words, D), st);
+    if (rc == DMX_OK && dbias)
+      rc = start(dim3((unsigned)((words + 31) / 32)), 1024, st, columns_kernel, (const float*)columns, (int)((N + 31) / 32), (int)words, static_cast<bf16*>(dbias) + first);
+    const Matrix G = {g, N, words, A.ldg};
+    if (rc == DMX_OK && dw) rc = plain_product(G, 1, a, 1, N, static_cast<bf16*>(dw) + first * (V > 1 ? lddw : D), V > 1 ? lddw : D, st);
+    if (rc != DMX_OK || !dx) continue;
+    if (p.pieces == 1) {
+      rc = plain_product(G, 0, piece, 1, words, static_cast<bf16*>(dx), N > 1 ? lddx : D, st);
+      continue;
+    }
+    AddArgs E = {};
+    E.rowsA = (int)N; E.rowsB = (int)D; E.kblocks = (int)((words + kBK - 1) / kBK); E.mnB = 1;
+    E.sums = sums; E.y = static_cast<bf16*>(dx); E.ldy = N > 1 ? lddx : D; E.first = first == 0; E.last = first + words >= V;
+    E.vec = aligned(dx, 16) && (N <= 1 || E.ldy % 8 == 0);
+    rc = launch_gemm<256, true, 1, AddEpilogue<256>>(G, piece, E, st);
+  }
+  return rc;
+}
+
+}  // extern "C"

@@ -1,4 +1,4 @@
-// dmx_torch.cpp — what a training step calls (group_norm, layer_norm, embedding, linear and their gradients, AdamW's norm and step) for torch callers,
+// dmx_torch.cpp — what a training step calls (group_norm, layer_norm, embedding, linear, linear_cross_entropy and their gradients, AdamW's norm and step) for torch callers,
 // compiled: argument checks, allocation from torch's caching allocator and the call into the C ABI of include/dmx.h in one
 // Python call (through ctypes the calls took 5-28 us on the host, mostly checks and argument marshalling; now 3-14; the kernels of a small
 // problem take 4-8 us). train_ops.py wraps these and documents them. A function returns its result, or a negative
@@ -37,6 +37,10 @@ decltype(&dmx_layer_norm_backward) layer_backward;
 decltype(&dmx_embedding_forward) lookup_forward;
 decltype(&dmx_embedding_backward_workspace) lookup_workspace;
 decltype(&dmx_embedding_backward) lookup_backward;
+decltype(&dmx_cross_entropy_workspace) loss_workspace;
+decltype(&dmx_cross_entropy_forward) loss_forward;
+decltype(&dmx_cross_entropy_backward_workspace) loss_backward_workspace;
+decltype(&dmx_cross_entropy_backward) loss_backward;
 
 struct Refused {
   int64_t code;
@@ -456,6 +460,69 @@ PyObject* embedding_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---------------------------------------------------------------------------------------------- cross entropy of a linear layer
+
+// x, weight, target, bias -> (loss, lse)
+PyObject* cross_entropy(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    need(n == 4);
+    const at::Tensor &x = tensor(a[0]), &w = tensor(a[1]), &target = tensor(a[2]);
+    const at::Tensor* b = maybe(a[3]);
+    if (recorded(nullptr, &x, &w, b)) return PyLong_FromLong(kRecord);
+    const Rows X = rows(x), W = rows(w);
+    const int64_t N = X.M, V = W.M, D = X.N;
+    need(W.N == D && w.device() == x.device() && target.dim() == 1 && target.size(0) == N);
+    bf16_vector(b, x, V);
+    const int tb = id_bytes(target, x);
+    const int64_t bytes = loss_workspace(N, V, D, in(&x), X.ld, in(&w), W.ld);
+    if (bytes < 0) refuse(bytes);
+    Call call(x);
+    const at::Tensor dense = target.contiguous();
+    at::Tensor loss = at::empty({N}, x.options().dtype(at::kFloat)), lse = at::empty({N}, x.options().dtype(at::kFloat));
+    at::Tensor ws = workspace(bytes, x);
+    const int rc = loss_forward(N, V, D, in(&x), X.ld, in(&w), W.ld, in(b), tb, in(&dense), static_cast<float*>(out(&loss)), static_cast<float*>(out(&lse)),
+                                start_of(ws), bytes, call.stream);
+    if (rc != DMX_OK) refuse(rc);
+    return tuple(&loss, &lse, nullptr);
+  });
+}
+
+// dloss, x, weight, target, lse, bias, need (bits), three outputs -> (dx, dweight, dbias)
+PyObject* cross_entropy_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    need(n == 10);
+    const at::Tensor &dloss = tensor(a[0]), &x = tensor(a[1]), &w = tensor(a[2]), &target = tensor(a[3]), &lse = tensor(a[4]);
+    const at::Tensor *b = maybe(a[5]), *g0 = maybe(a[7]), *g1 = maybe(a[8]), *g2 = maybe(a[9]);
+    const long want = whole(a[6]);
+    const Rows X = rows(x), W = rows(w);
+    const int64_t N = X.M, V = W.M, D = X.N;
+    need(W.N == D && w.device() == x.device() && target.dim() == 1 && target.size(0) == N);
+    need(dloss.dim() == 1 && dloss.size(0) == N && dloss.scalar_type() == at::kFloat && dloss.device() == x.device());
+    bf16_vector(b, x, V);
+    const float* lp = vector(&lse, x, N);
+    const int tb = id_bytes(target, x);
+    const int64_t bytes = loss_backward_workspace(N, V, D, in(&x), X.ld, in(&w), W.ld);
+    if (bytes < 0) refuse(bytes);
+    Call call(x);
+    const at::Tensor dense = target.contiguous();
+    at::Tensor dx, dw, db;
+    if (want & 1) dx = g0 ? *g0 : at::empty({N, D}, x.options());
+    if (want & 2) dw = g1 ? *g1 : at::empty({V, D}, x.options());
+    if (want & 4) db = g2 ? *g2 : at::empty({V}, x.options());
+    const Rows DX = rows_like(dx.defined() ? &dx : nullptr, x, N, D), DW = rows_like(dw.defined() ? &dw : nullptr, x, V, D);
+    bf16_vector(db.defined() ? &db : nullptr, x, V);
+    at::Tensor ws = workspace(bytes, x);
+    const int rc = loss_backward(N, V, D, static_cast<const float*>(in(&dloss)), N > 1 ? dloss.stride(0) : 0, in(&x), X.ld, in(&w), W.ld, in(b), tb, in(&dense), lp,
+                                 dx.defined() ? out(&dx) : nullptr, DX.ld, dw.defined() ? out(&dw) : nullptr, DW.ld, db.defined() ? out(&db) : nullptr,
+                                 start_of(ws), bytes, call.stream);
+    if (rc != DMX_OK) refuse(rc);
+    if (want & 1) written(g0);
+    if (want & 2) written(g1);
+    if (want & 4) written(g2);
+    return tuple(&dx, &dw, &db);
+  });
+}
+
 // ---------------------------------------------------------------------------------------------- AdamW
 
 // One of the optimizer's arrays: n entries of a type, dense, on its device.
@@ -522,7 +589,8 @@ PyObject* connect(PyObject*, PyObject* const* a, Py_ssize_t n) {
   };
   auto all = [&](auto&... f) { return (take(f) && ...); };
   if (!all(norm_workspace, norm_forward, norm_backward, linear_workspace, linear_forward, linear_backward_workspace, linear_backward, adamw_norm,
-           adamw_step, layer_workspace, layer_forward, layer_backward, lookup_forward, lookup_workspace, lookup_backward) || i != n)
+           adamw_step, layer_workspace, layer_forward, layer_backward, lookup_forward, lookup_workspace, lookup_backward, loss_workspace, loss_forward,
+           loss_backward_workspace, loss_backward) || i != n)
     return PyErr_Occurred() ? nullptr : (PyErr_SetString(PyExc_ValueError, "the entry points' addresses"), nullptr);
   Py_RETURN_NONE;
 }
@@ -537,6 +605,8 @@ PyMethodDef methods[] = {{"connect", FAST(connect)},
                          {"layer_norm_backward", FAST(layer_norm_backward)},
                          {"embedding", FAST(embedding)},
                          {"embedding_backward", FAST(embedding_backward)},
+                         {"cross_entropy", FAST(cross_entropy)},
+                         {"cross_entropy_backward", FAST(cross_entropy_backward)},
                          {"adamw_grad_norm", FAST(grad_norm)},
                          {"adamw_step", FAST(step)},
                          {nullptr, nullptr, 0, nullptr}};

@@ -1,5 +1,5 @@
-"""What torch's differentiation does with the training operators: linear, group_norm, layer_norm and embedding record
-themselves where an input requires a gradient, and their gradients are the explicit backward calls. First derivatives only."""
+"""What torch's differentiation does with the training operators: linear, group_norm, layer_norm, embedding and
+linear_cross_entropy record themselves where an input requires a gradient, and their gradients are the explicit backward calls. First derivatives only."""
 from __future__ import annotations
 
 import torch
@@ -78,3 +78,20 @@ class Embedding(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy):
         return None, T.embedding_backward(dy.contiguous(), *ctx.saved_tensors, ctx.rows, ctx.scale), None
+
+
+class LinearCrossEntropy(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, target, bias):
+        loss, lse = T.linear_cross_entropy(x, weight, target, bias)
+        ctx.save_for_backward(x, weight, target, lse, bias)
+        ctx.mark_non_differentiable(lse)
+        return loss, lse
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dloss, *_):
+        x, weight, target, lse, bias = ctx.saved_tensors
+        need_x, need_w, _, need_b = ctx.needs_input_grad
+        dx, dw, db = T.linear_cross_entropy_backward(dloss, x, weight, target, lse, bias, need=(need_x, need_w, need_b))
+        return dx, dw, None, None if db is None else db.view(bias.shape)

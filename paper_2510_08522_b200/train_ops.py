@@ -228,7 +228,8 @@ def _module():
             L.dmx_group_norm_workspace, L.dmx_group_norm_forward, L.dmx_group_norm_backward, L.dmx_linear_workspace, L.dmx_linear_forward,
             L.dmx_linear_backward_workspace, L.dmx_linear_backward, L.dmx_adamw_grad_norm, L.dmx_adamw_step,
             L.dmx_layer_norm_workspace, L.dmx_layer_norm_forward, L.dmx_layer_norm_backward, L.dmx_embedding_forward,
-            L.dmx_embedding_backward_workspace, L.dmx_embedding_backward)])
+            L.dmx_embedding_backward_workspace, L.dmx_embedding_backward, L.dmx_cross_entropy_workspace, L.dmx_cross_entropy_forward,
+            L.dmx_cross_entropy_backward_workspace, L.dmx_cross_entropy_backward)])
         _fast = m
     return _fast
 
@@ -312,8 +313,28 @@ def linear_backward(dy, x, weight, z=None, act="none", need=(True, True, True), 
     return r if r.__class__ is tuple else _refuse("linear_backward", r)
 
 
+def linear_cross_entropy(x, weight, target, bias=None):
+    """Softmax cross entropy of x @ weight.T + bias (bf16 matrices (N, D) and (V, D)) without keeping the logits -> (loss, lse), fp32 (N,):
+    every row's loss, 0 where its target (int32 or int64) lies outside 0..V-1, and the logarithm of its sum of exponentials. Where an
+    input requires a gradient torch records the call (loss's gradient; lse carries none)."""
+    r = (_fast or _module()).cross_entropy(x, weight, target, bias)
+    if r.__class__ is tuple:
+        return r
+    if r != _RECORD:
+        _refuse("linear_cross_entropy", r)
+    from .train_grad import LinearCrossEntropy
+    return LinearCrossEntropy.apply(x, weight, target, bias)
+
+
+def linear_cross_entropy_backward(dloss, x, weight, target, lse, bias=None, need=(True, True, True), out=(None, None, None)):
+    """Gradient of linear_cross_entropy -> (dx, dweight, dbias), those not in `need` None. dloss: fp32 (N,), also one value expanded.
+    `out`: tensors to write them to, e.g. views of a flat gradient vector."""
+    r = (_fast or _module()).cross_entropy_backward(dloss, x, weight, target, lse, bias, (1 if need[0] else 0) + (2 if need[1] else 0) + (4 if need[2] else 0), *out)
+    return r if r.__class__ is tuple else _refuse("linear_cross_entropy_backward", r)
+
+
 def linear_status():
-    """How many warps of the linear kernels gave up a wait on the current device since the last call. Waits for the
+    """How many warps of the linear and cross entropy kernels gave up a wait on the current device since the last call. Waits for the
     device's work on all streams."""
     n = ctypes.c_int()
     rc = B.lib().dmx_linear_status(ctypes.byref(n))

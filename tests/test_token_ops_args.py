@@ -1,4 +1,4 @@
-"""Argument checks of layer norm and of the embedding lookup that need no GPU: the C entry points refuse what they document before any device call."""
+"""Argument checks of layer norm, the embedding lookup and the cross entropy that need no GPU: the C entry points refuse what they document before any device call."""
 import pytest
 
 import paper_2510_08522_b200 as D
@@ -53,10 +53,38 @@ def test_embedding_refuses_bad_sizes_types_strides_and_pointers():
     assert backward(V=0) == B.OK and backward(n=0, ldt=0) == B.OK and backward(N=0, add=1) == B.OK
 
 
+def test_cross_entropy_refuses_bad_extents_strides_and_pointers():
+    L = B.lib()
+    big = 4194241
+    for f in (L.dmx_cross_entropy_workspace, L.dmx_cross_entropy_backward_workspace):
+        for a in ((-1, 8, 8), (big, 8, 8), (4, 0, 8), (4, big, 8), (4, 8, 0), (4, 8, big)):
+            assert f(*a, 256, 8, 512, 8) == B.ERR_ARG
+        assert f(0, 8, 8, None, 8, 512, 8) == 0 and 0 < f(4, 8, 8, 256, 8, 512, 8) < f(4, 8, 8, 258, 8, 512, 8)
+
+    def forward(N=4, V=8, n=16, x=256, ldx=16, w=512, ldw=16, bias=None, tb=8, t=1024, loss=2048, lse=4096, ws=8192, size=1 << 20):
+        return L.dmx_cross_entropy_forward(N, V, n, x, ldx, w, ldw, bias, tb, t, loss, lse, ws, size, None)
+    for bad in (dict(N=-1), dict(V=0), dict(n=0), dict(V=big), dict(ldx=-1), dict(ldw=-1), dict(tb=2), dict(x=None), dict(w=None), dict(t=None), dict(loss=None), dict(lse=None), dict(ws=None), dict(size=64)):
+        assert forward(**bad) == B.ERR_ARG, bad
+    for bad in (dict(x=257), dict(w=513), dict(bias=3), dict(t=1028), dict(loss=2050), dict(lse=4097), dict(ws=8200)):
+        assert forward(**bad) == B.ERR_ALIGN, bad
+    assert forward(N=0, x=None, t=None) == B.OK
+
+    def backward(N=4, V=8, n=16, g=128, gs=1, x=256, ldx=16, w=512, ldw=16, bias=None, tb=4, t=1024, lse=2048, dx=4096, lddx=16, dw=8192, lddw=16, db=6144, ws=16384, size=1 << 20):
+        return L.dmx_cross_entropy_backward(N, V, n, g, gs, x, ldx, w, ldw, bias, tb, t, lse, dx, lddx, dw, lddw, db, ws, size, None)
+    for bad in (dict(N=big), dict(V=0), dict(gs=-1), dict(ldx=-1), dict(lddx=15), dict(lddw=0), dict(tb=1), dict(g=None), dict(x=None), dict(w=None), dict(t=None), dict(lse=None), dict(ws=None),
+                dict(size=64)):
+        assert backward(**bad) == B.ERR_ARG, bad
+    for bad in (dict(g=130), dict(x=257), dict(w=513), dict(bias=3), dict(t=1026), dict(lse=2049), dict(dx=4097), dict(dw=8193), dict(db=6145), dict(ws=16388)):
+        assert backward(**bad) == B.ERR_ALIGN, bad
+    assert backward(dx=None, dw=None, db=None) == B.OK
+
+
 def test_torch_callers_get_errors_for_what_is_no_cuda_tensor():
     torch = pytest.importorskip("torch")
     x, m = torch.zeros(4, 8), torch.zeros(4)
-    for call in (lambda: D.layer_norm(x), lambda: D.layer_norm(None), lambda: D.layer_norm(x, "w"), lambda: D.layer_norm([1.0]),
+    h = x.bfloat16()
+    for call in (lambda: D.linear_cross_entropy(h, h, m.long()), lambda: D.linear_cross_entropy(h, None, m.long()), lambda: D.linear_cross_entropy(h, h, 3),
+                 lambda: D.linear_cross_entropy_backward(m, h, h, m.long(), m), lambda: D.linear_cross_entropy_backward(None, h, h, m.long(), m), lambda: D.layer_norm(x), lambda: D.layer_norm(None), lambda: D.layer_norm(x, "w"), lambda: D.layer_norm([1.0]),
                  lambda: D.embedding(m.long(), x), lambda: D.embedding(3, x), lambda: D.embedding(m.long(), None), lambda: D.embedding_backward(x, m.long(), 5),
                  lambda: D.embedding_backward(x, [1], 5), lambda: D.layer_norm_backward(x, x, m, m), lambda: D.layer_norm_backward(x, None, m, m), lambda: D.layer_norm_backward(x, x, m, 3)):
         with pytest.raises(D.DmxError):
