@@ -636,7 +636,7 @@ int dmx_embedding_backward(int64_t N, int64_t V, int64_t D, int id_bytes, const 
  * A row whose target lies outside 0..V-1 (an ignored place) has loss 0 and no gradient; its lse is computed all the same. backward
  * computes the logits again and goes through the vocabulary in pieces: the workspace holds a piece of G (256 MB at most, or 256 words), and,
  * where there are several, dx in fp32. Everything up to a store is fp32, with one exception: G is rounded to bf16 before the two
- * products (the tensor cores take 16-bit operands); dbias is summed from the unrounded G. Exponentials are good to 2 ulp. Logits
+ * products (the tensor cores take 16-bit operands), in units of the largest finite |dloss|'s significand; dbias is summed from the unrounded G. Exponentials are good to 2 ulp. Logits
  * of -inf (a bias of -inf) are words that do not occur; a logit of +inf or NaN makes its row's loss and gradient NaN, as does a row without
  * any finite logit.
  *   x, w, bias, dx, dw, dbias   bf16, row-major, ld* = elements from row to row (>= 0; of outputs >= D unless there is one row; inputs may

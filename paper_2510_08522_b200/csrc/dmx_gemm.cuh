@@ -558,8 +558,8 @@ struct Jobs {
 int run_jobs(const Jobs& jobs, int n, int act, cudaStream_t st);
 // m's copy at *ws (which moves on), if it needs one
 void lay_out(Matrix& m, unsigned char*& ws, Jobs& jobs, int& n);
-// y = A B^T, rounded to bf16. mn: the operand's rows run along D's extent.
-int plain_product(const Matrix& a, int mnA, const Matrix& b, int mnB, int64_t k, bf16* y, int64_t ldy, cudaStream_t st);
+// y = A B^T, times *unit (device memory) if there is one, rounded to bf16. mn: the operand's rows run along D's extent.
+int plain_product(const Matrix& a, int mnA, const Matrix& b, int mnB, int64_t k, const float* unit, bf16* y, int64_t ldy, cudaStream_t st);
 
 // the cross entropy's count of warps that gave up
 bool loss_gave_up(unsigned* n);

@@ -31,6 +31,7 @@ struct GemmArgs : GemmShape {
   int64_t ldr, ldy, ldz;
   int act;
   int vecy, vecz, vecr;                       // 16-byte rows
+  const float* unit;                          // of one operand, if it is held in units of something
 };
 
 // ---------------------------------------------------------------------------------------------- epilogue
@@ -118,8 +119,8 @@ __device__ __forceinline__ void finish_swapped(const GemmArgs& A, float (&v)[NC]
   to_stage();
   store_tile<NC, 32>(A.y, A.ldy, A.vecy, stage, t0, A.rowsB, f0, A.rowsA, lane);
 }
-// D, or with the operands exchanged its transpose
-template <bool SWAP>
+// D, or with the operands exchanged its transpose. UNIT: times *A.unit.
+template <bool SWAP, bool UNIT>
 struct LinearEpilogue {
   typedef GemmArgs Args;
   float bias = 0.f;
@@ -129,6 +130,11 @@ struct LinearEpilogue {
   }
   template <int NC>
   __device__ __forceinline__ void chunk(const Args& A, float (&v)[NC], uint4* stage, int r0, int c0, int lane) {
+    if constexpr (UNIT) {
+      const float unit = __ldg(A.unit);
+#pragma unroll
+      for (int i = 0; i < NC; ++i) v[i] *= unit;
+    }
     if constexpr (SWAP) finish_swapped<NC>(A, v, stage, r0, c0, bias, lane);
     else finish<NC>(A, v, stage, r0, c0, lane);
   }
@@ -258,6 +264,7 @@ Form form_of(int64_t rowsA, int64_t rowsB, int kblocks, int mnA) {
 }
 
 // D = A B^T with the epilogue in E (bias, residual, outputs, act). mn: the operand's rows run along D's extent.
+template <bool UNIT>
 int product(const Matrix& a, int mnA, const Matrix& b, int mnB, int64_t k, const GemmArgs& E, cudaStream_t st) {
   GemmArgs A = E;
   const int64_t rowsA = mnA ? a.cols : a.rows, rowsB = mnB ? b.cols : b.rows;
@@ -271,18 +278,18 @@ int product(const Matrix& a, int mnA, const Matrix& b, int mnB, int64_t k, const
     A.rowsA = (int)rowsB; A.rowsB = (int)rowsA;
     A.mnA = mnB; A.mnB = mnA;
     if (c.bn == 32) {
-      if (c.split == 4) return launch_gemm<32, false, 4, LinearEpilogue<true>>(b, a, A, st);
-      return c.split == 2 ? launch_gemm<32, false, 2, LinearEpilogue<true>>(b, a, A, st) : launch_gemm<32, false, 1, LinearEpilogue<true>>(b, a, A, st);
+      if (c.split == 4) return launch_gemm<32, false, 4, LinearEpilogue<true, UNIT>>(b, a, A, st);
+      return c.split == 2 ? launch_gemm<32, false, 2, LinearEpilogue<true, UNIT>>(b, a, A, st) : launch_gemm<32, false, 1, LinearEpilogue<true, UNIT>>(b, a, A, st);
     }
-    if (c.split == 4) return launch_gemm<64, false, 4, LinearEpilogue<true>>(b, a, A, st);
-    return c.split == 2 ? launch_gemm<64, false, 2, LinearEpilogue<true>>(b, a, A, st) : launch_gemm<64, false, 1, LinearEpilogue<true>>(b, a, A, st);
+    if (c.split == 4) return launch_gemm<64, false, 4, LinearEpilogue<true, UNIT>>(b, a, A, st);
+    return c.split == 2 ? launch_gemm<64, false, 2, LinearEpilogue<true, UNIT>>(b, a, A, st) : launch_gemm<64, false, 1, LinearEpilogue<true, UNIT>>(b, a, A, st);
   }
   A.rowsA = (int)rowsA; A.rowsB = (int)rowsB;
   A.mnA = mnA; A.mnB = mnB;
-  if (c.pair) return c.bn == 256 ? launch_gemm<256, true, 1, LinearEpilogue<false>>(a, b, A, st) : launch_gemm<128, true, 1, LinearEpilogue<false>>(a, b, A, st);
-  if (c.bn == 256) return launch_gemm<256, false, 1, LinearEpilogue<false>>(a, b, A, st);
-  if (c.bn == 128) return c.split == 2 ? launch_gemm<128, false, 2, LinearEpilogue<false>>(a, b, A, st) : launch_gemm<128, false, 1, LinearEpilogue<false>>(a, b, A, st);
-  return c.split == 2 ? launch_gemm<64, false, 2, LinearEpilogue<false>>(a, b, A, st) : launch_gemm<64, false, 1, LinearEpilogue<false>>(a, b, A, st);
+  if (c.pair) return c.bn == 256 ? launch_gemm<256, true, 1, LinearEpilogue<false, UNIT>>(a, b, A, st) : launch_gemm<128, true, 1, LinearEpilogue<false, UNIT>>(a, b, A, st);
+  if (c.bn == 256) return launch_gemm<256, false, 1, LinearEpilogue<false, UNIT>>(a, b, A, st);
+  if (c.bn == 128) return c.split == 2 ? launch_gemm<128, false, 2, LinearEpilogue<false, UNIT>>(a, b, A, st) : launch_gemm<128, false, 1, LinearEpilogue<false, UNIT>>(a, b, A, st);
+  return c.split == 2 ? launch_gemm<64, false, 2, LinearEpilogue<false, UNIT>>(a, b, A, st) : launch_gemm<64, false, 1, LinearEpilogue<false, UNIT>>(a, b, A, st);
 }
 
 }  // namespace
@@ -320,11 +327,11 @@ void lay_out(Matrix& m, unsigned char*& ws, Jobs& jobs, int& n) {
   m.ld = j.ldo;
 }
 
-int plain_product(const Matrix& a, int mnA, const Matrix& b, int mnB, int64_t k, bf16* y, int64_t ldy, cudaStream_t st) {
+int plain_product(const Matrix& a, int mnA, const Matrix& b, int mnB, int64_t k, const float* unit, bf16* y, int64_t ldy, cudaStream_t st) {
   GemmArgs E = {};
   E.act = DMX_ACT_NONE;
-  E.y = y; E.ldy = ldy;
-  return product(a, mnA, b, mnB, k, E, st);
+  E.y = y; E.ldy = ldy; E.unit = unit;
+  return unit ? product<true>(a, mnA, b, mnB, k, E, st) : product<false>(a, mnA, b, mnB, k, E, st);
 }
 
 }  // namespace dmx_gemm
@@ -391,7 +398,7 @@ int dmx_linear_forward(int64_t M, int64_t N, int64_t K, const void* x, int64_t l
   lay_out(a, ws, jobs, n);
   lay_out(b, ws, jobs, n);
   const int rc = n > 0 ? run_jobs(jobs, n, DMX_ACT_NONE, st) : DMX_OK;
-  return rc != DMX_OK ? rc : product(a, 0, b, 0, K, E, st);
+  return rc != DMX_OK ? rc : product<false>(a, 0, b, 0, K, E, st);
 }
 
 int64_t dmx_linear_backward_workspace(int64_t M, int64_t N, int64_t K, const void* dy, int64_t lddy, const void* x, int64_t ldx,
@@ -447,9 +454,9 @@ int dmx_linear_backward(int64_t M, int64_t N, int64_t K, const void* dy, int64_t
   if (rc == DMX_OK && dbias)
     rc = start(dim3((unsigned)((N + 31) / 32)), st, columns_kernel, (const float*)sums, (M + kChunkRows - 1) / kChunkRows, (int)N, static_cast<bf16*>(dbias));
   if (products && dx && rc == DMX_OK)          // dx[m, k] = sum_n dz[m, n] w[n, k]
-    rc = plain_product(g, 0, b, 1, N, static_cast<bf16*>(dx), M > 1 ? lddx : K, st);
+    rc = plain_product(g, 0, b, 1, N, nullptr, static_cast<bf16*>(dx), M > 1 ? lddx : K, st);
   if (products && dw && rc == DMX_OK)          // dw[n, k] = sum_m dz[m, n] x[m, k]
-    rc = plain_product(g, 1, a, 1, M, static_cast<bf16*>(dw), N > 1 ? lddw : K, st);
+    rc = plain_product(g, 1, a, 1, M, nullptr, static_cast<bf16*>(dw), N > 1 ? lddw : K, st);
   return rc;
 }
 

@@ -176,6 +176,31 @@ def test_rows_that_are_not_finite_stay_alone():
     assert torch.equal(got[0][~hit], dx[~hit]) and got[0][[7, 299]].isnan().all() and not got[0][130].any()
 
 
+def test_weights_of_rows():
+    """dloss of any size and sign, zeros, and values that are not finite, which stay in their rows of dx."""
+    torch, D = _d()
+    x, w, t, b = problem(torch, 300, 400, 64)
+    g = torch.Generator(device="cuda").manual_seed(11)
+    r = torch.randn(300, generator=g, device="cuda")
+    for d in (r, r * 1e-30, r * 1e20, r * torch.exp(20 * torch.randn(300, generator=g, device="cuda")), torch.where(r > 0, r, 0.0), r * 0, -torch.ones(300, device="cuda")):
+        compare(torch, D, x, w, t, b, dloss=d)
+    lse = D.linear_cross_entropy(x, w, t, b)[1]
+    want = D.linear_cross_entropy_backward(r, x, w, t, lse, b)[0]
+    for odd in (float("nan"), float("inf")):
+        d = r.clone()
+        live = torch.nonzero((t >= 0) & (t < 400))[:, 0]
+        d[live[5]] = odd
+        keep = torch.ones(300, dtype=torch.bool, device="cuda")
+        keep[live[5]] = False
+        if float(r[live[5]].abs()) == float(r.abs().max()):
+            continue
+        dx, dw, db = D.linear_cross_entropy_backward(d, x, w, t, lse, b)
+        assert torch.equal(dx[keep], want[keep]) and not dx[live[5]].isfinite().any() and not dw.isfinite().any() and not db.isfinite().any()
+    d = torch.zeros(300, device="cuda")
+    d[live[5]] = float("nan")
+    assert D.linear_cross_entropy_backward(d, x, w, t, lse, b)[0][live[5]].isnan().all()
+
+
 def test_nothing_to_do():
     torch, D = _d()
     w = torch.randn(30, 16, device="cuda").bfloat16()
