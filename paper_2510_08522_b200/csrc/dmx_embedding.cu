@@ -15,7 +15,7 @@ namespace {
 
 using namespace dmx_rows;
 
-constexpr int kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kDigits = 256;
+constexpr int kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kDigits = 256, kKept = 8;
 
 // ---------------------------------------------------------------------------------------------- forward
 
@@ -96,10 +96,13 @@ __device__ void clear_rows(const SortArgs& A, int64_t cta, int64_t ctas) {
     for (int64_t i = lane * 2; i < A.zero_bytes; i += 64) *reinterpret_cast<unsigned short*>(p + v * A.zero_ld + i) = 0;
 }
 
+// One pass takes a digit: every warp counts its keys' digits in order (a key's rank among the warp's own equal digits is what it finds, plus
+// the equal ones in lanes below), the counts become places by prefix sums over warps, CTAs and digits, and keys go there. A warp's keys
+// stay in registers in between if they are no more than eight a lane; else they are ranked a second time.
 __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads) sort_kernel(const __grid_constant__ SortArgs A) {
   extern __shared__ unsigned counts[];                    // [warps][digits]: a warp's digits, then where its next one goes
   __shared__ unsigned totals[kSortCtas][kDigits];         // every CTA's digits
-  __shared__ unsigned scan[8];
+  __shared__ unsigned quarter[4][kDigits], scan[4][8];
   start_dependents();
   wait_for_previous();
   if (blockIdx.x >= kSortCtas) {
@@ -108,81 +111,122 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
   }
   cluster_sync();                                         // all of it is there
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x;
+  const int digit = threadIdx.x & 255, group = threadIdx.x >> 8;      // of the prefix sums: a digit of eight warps
   const unsigned below = (1u << lane) - 1;
   // a warp's share: whole rounds of 32
   const int64_t rounds = (A.N + 32 * kSortWarps * kSortCtas - 1) / (32 * kSortWarps * kSortCtas);
   const int64_t first = ((int64_t)rank * kSortWarps + warp) * rounds * 32;
+  const bool keep = rounds <= kKept;
   unsigned* mine = counts + warp * kDigits;
   for (int pass = 0; pass < A.passes; ++pass) {
     const int from = (A.passes - pass) & 1, shift = 8 * pass;
-    auto key_at = [&](int64_t n) -> unsigned {
-      if (pass > 0) return __ldcg(A.key[from] + n);
-      const int64_t id = id_at(A.ids, A.wide_ids, n);
-      return id >= 0 && id < A.V ? (unsigned)id : (unsigned)A.V;     // what is in no row comes last
+    auto fetch = [&](int64_t n, unsigned& k, unsigned& p) {
+      k = p = 0;
+      if (n >= A.N) return;
+      if (pass > 0) {
+        k = __ldcg(A.key[from] + n);
+        p = __ldcg(A.place[from] + n);
+      } else {
+        const int64_t id = id_at(A.ids, A.wide_ids, n);
+        k = id >= 0 && id < A.V ? (unsigned)id : (unsigned)A.V;      // what is in no row comes last
+        p = (unsigned)n;
+      }
     };
+    // the key's rank behind what `mine` holds for its digit, which moves on
+    auto ranked = [&](bool live, unsigned k) {
+      const unsigned d = live ? k >> shift & 255 : 256;
+      const unsigned same = __match_any_sync(0xffffffffu, d);
+      const unsigned before = live ? mine[d] : 0;
+      __syncwarp();
+      if (live && (same & below) == 0) mine[d] = before + __popc(same);
+      __syncwarp();
+      return before + __popc(same & below);
+    };
+    unsigned key[kKept], place[kKept], at[kKept];
+    if (keep) {
+#pragma unroll
+      for (int r = 0; r < kKept; ++r)
+        if (r < rounds) fetch(first + r * 32 + lane, key[r], place[r]);
+    }
     for (int i = lane; i < kDigits; i += 32) mine[i] = 0;
     __syncwarp();
-    for (int64_t r = 0; r < rounds; ++r) {
-      const int64_t n = first + r * 32 + lane;
-      const bool live = n < A.N;
-      if (!__any_sync(0xffffffffu, live)) break;
-      const unsigned d = live ? key_at(n) >> shift & 255 : 256;
-      const unsigned same = __match_any_sync(0xffffffffu, d);
-      if (live && (same & below) == 0) mine[d] += __popc(same);
-      __syncwarp();
+    if (keep) {
+#pragma unroll
+      for (int r = 0; r < kKept; ++r)
+        if (r < rounds) at[r] = ranked(first + r * 32 + lane < A.N, key[r]);
+    } else {
+      for (int64_t n = first; n < first + rounds * 32 && n < A.N; n += 32) {
+        unsigned k, p;
+        fetch(n + lane, k, p);
+        ranked(n + lane < A.N, k);
+      }
     }
     __syncthreads();
-    if (threadIdx.x < kDigits) {                          // prefix over the warps; the CTA's total goes to every CTA
-      unsigned sum = 0;
-      for (int w = 0; w < kSortWarps; ++w) {
-        const unsigned c = counts[w * kDigits + threadIdx.x];
-        counts[w * kDigits + threadIdx.x] = sum;
-        sum += c;
-      }
-      for (int to = 0; to < kSortCtas; ++to) {
-        unsigned at;
-        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((unsigned)__cvta_generic_to_shared(&totals[rank][threadIdx.x])), "r"(to));
-        asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(sum) : "memory");
-      }
+    unsigned c[8], sum = 0;                               // prefix over the warps; the CTA's total goes to every CTA
+#pragma unroll
+    for (int w = 0; w < 8; ++w) c[w] = counts[(group * 8 + w) * kDigits + digit];
+#pragma unroll
+    for (int w = 0; w < 8; ++w) {
+      const unsigned t = c[w];
+      c[w] = sum;
+      sum += t;
+    }
+    quarter[group][digit] = sum;
+    __syncthreads();
+    unsigned earlier = 0, total = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const unsigned t = quarter[q][digit];
+      earlier += q < group ? t : 0;
+      total += t;
+    }
+#pragma unroll
+    for (int to = 0; to < kSortCtas / 4; ++to) {
+      unsigned there;
+      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((unsigned)__cvta_generic_to_shared(&totals[rank][digit])), "r"(group * (kSortCtas / 4) + to));
+      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(there), "r"(total) : "memory");
     }
     cluster_sync();
-    if (threadIdx.x < kDigits) {                          // where this CTA's first key of a digit goes
-      unsigned all = 0, before = 0;
-      for (int r = 0; r < kSortCtas; ++r) {
-        const unsigned c = totals[r][threadIdx.x];
-        before += r < rank ? c : 0;
-        all += c;
-      }
-      unsigned up = all;
+    unsigned all = 0;                                     // where this CTA's first key of a digit goes
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const unsigned t = __shfl_up_sync(0xffffffffu, up, o);
-        if (lane >= o) up += t;
-      }
-      if (lane == 31) scan[warp] = up;
-      asm volatile("bar.sync 1, 256;" ::: "memory");
-      unsigned start = up - all + before;
-      for (int w = 0; w < warp; ++w) start += scan[w];
-      for (int w = 0; w < kSortWarps; ++w) counts[w * kDigits + threadIdx.x] += start;
+    for (int r = 0; r < kSortCtas; ++r) {
+      const unsigned t = totals[r][digit];
+      earlier += r < rank ? t : 0;
+      all += t;
     }
+    unsigned up = all;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned t = __shfl_up_sync(0xffffffffu, up, o);
+      if (lane >= o) up += t;
+    }
+    if (lane == 31) scan[group][warp & 7] = up;
+    asm volatile("bar.sync %0, 256;" ::"r"(1 + group) : "memory");
+    earlier += up - all;
+    for (int w = 0; w < (warp & 7); ++w) earlier += scan[group][w];
+#pragma unroll
+    for (int w = 0; w < 8; ++w) counts[(group * 8 + w) * kDigits + digit] = c[w] + earlier;
     __syncthreads();
-    for (int64_t r = 0; r < rounds; ++r) {
-      const int64_t n = first + r * 32 + lane;
-      const bool live = n < A.N;
-      if (!__any_sync(0xffffffffu, live)) break;
-      const unsigned k = live ? key_at(n) : 0, d = live ? k >> shift & 255 : 256;
-      const unsigned same = __match_any_sync(0xffffffffu, d);
-      unsigned at = 0;
-      if (live) at = mine[d] + __popc(same & below);
-      __syncwarp();
-      if (live && (same & below) == 0) mine[d] += __popc(same);
-      __syncwarp();
-      if (live) {
-        const unsigned p = pass > 0 ? __ldcg(A.place[from] + n) : (unsigned)n;
-        A.key[from ^ 1][at] = k;
-        A.place[from ^ 1][at] = p;
+    if (keep) {
+#pragma unroll
+      for (int r = 0; r < kKept; ++r)
+        if (r < rounds && first + r * 32 + lane < A.N) {
+          const unsigned to = at[r] + mine[key[r] >> shift & 255];
+          A.key[from ^ 1][to] = key[r];
+          A.place[from ^ 1][to] = place[r];
+        }
+    } else {
+      for (int64_t n = first; n < first + rounds * 32 && n < A.N; n += 32) {
+        unsigned k, p;
+        fetch(n + lane, k, p);
+        const unsigned to = ranked(n + lane < A.N, k);
+        if (n + lane < A.N) {
+          A.key[from ^ 1][to] = k;
+          A.place[from ^ 1][to] = p;
+        }
       }
     }
+    if (pass + 1 == A.passes) break;
     __threadfence();
     cluster_sync();
   }
@@ -200,41 +244,96 @@ struct SumArgs {
   float scale;
 };
 
-template <typename O, int W>
-__device__ __forceinline__ void finish_row(const SumArgs& A, unsigned v, int c, const float* acc) {
-  O* q = static_cast<O*>(A.out) + (int64_t)v * A.ldout + c;
+// How a lane holds its share of 32 x W columns: W neighbours in one access (of dy's type; 16 bytes), or, where alignment allows no
+// more, every 32nd element.
+template <int W, bool WIDE>
+struct Columns {
+  int c, D;
+  __device__ __forceinline__ Columns(int slice, int lane, int D_) : c(slice * 32 * W + (WIDE ? lane * W : lane)), D(D_) {}
+  __device__ __forceinline__ int at(int i) const { return WIDE ? c + i : c + i * 32; }
+  __device__ __forceinline__ bool has(int i) const { return WIDE ? c < D : c + i * 32 < D; }
+};
+
+template <typename T, int W, bool WIDE>
+struct Share {
+  typedef typename Vec<T, WIDE ? W : 1>::type Raw;
+  Raw r[WIDE ? 1 : W];
+  __device__ __forceinline__ void load(const T* row, const Columns<W, WIDE>& at, bool live) {
+#pragma unroll
+    for (int i = 0; i < (WIDE ? 1 : W); ++i) {
+      r[i] = Raw{};
+      if (live && at.has(i)) r[i] = *reinterpret_cast<const Raw*>(row + at.at(i));
+    }
+  }
+  __device__ __forceinline__ void add_to(float (&acc)[W]) const {
+    float x[W];
+#pragma unroll
+    for (int i = 0; i < (WIDE ? 1 : W); ++i) widen<T>(r[i], x + i);
+#pragma unroll
+    for (int i = 0; i < W; ++i) acc[i] += x[i];
+  }
+};
+
+// W neighbours of a row of the table's gradient: one or two accesses
+template <typename O, int W> struct Whole;
+template <> struct Whole<float, 8> { typedef uint4 type; static constexpr int n = 4; };
+template <> struct Whole<float, 4> { typedef uint4 type; static constexpr int n = 4; };
+template <> struct Whole<bf16, 8> { typedef uint4 type; static constexpr int n = 8; };
+template <> struct Whole<bf16, 4> { typedef uint2 type; static constexpr int n = 4; };
+
+template <typename O, int W, bool WIDE>
+__device__ __forceinline__ void finish_row(const SumArgs& A, unsigned v, const Columns<W, WIDE>& at, const float (&acc)[W]) {
+  O* row = static_cast<O*>(A.out) + (int64_t)v * A.ldout;
   float x[W];
 #pragma unroll
   for (int i = 0; i < W; ++i) x[i] = acc[i] * A.scale;
-  constexpr int kOut = W == 1 ? 1 : kWide<O>;
-  static_assert(W % kOut == 0, "whole accesses");
+  if constexpr (WIDE) {
+    typedef Whole<O, W> H;
+    if (!at.has(0)) return;
 #pragma unroll
-  for (int k = 0; k < W; k += kOut) {
-    typedef typename Vec<O, kOut>::type Raw;
-    if (A.accumulate) {
-      float old[kOut];
-      widen<O>(*reinterpret_cast<const Raw*>(q + k), old);
+    for (int k = 0; k < W; k += H::n) {
+      typename H::type* q = reinterpret_cast<typename H::type*>(row + at.at(k));
+      if (A.accumulate) {
+        const typename H::type old = *q;
+        if constexpr (sizeof(O) == 4) {
+          float o[4];
+          widen<O>(old, o);
 #pragma unroll
-      for (int i = 0; i < kOut; ++i) x[k + i] += old[i];
+          for (int i = 0; i < 4; ++i) x[k + i] += o[i];
+        } else {
+          const unsigned* w = reinterpret_cast<const unsigned*>(&old);
+#pragma unroll
+          for (int i = 0; i < H::n / 2; ++i) { x[k + 2 * i] += __uint_as_float(w[i] << 16); x[k + 2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u); }
+        }
+      }
+      if constexpr (sizeof(O) == 4 || H::n == 8) *q = narrow<O, H::n>(x + k);
+      else *q = make_uint2(pack2(x[k], x[k + 1]), pack2(x[k + 2], x[k + 3]));
     }
-    *reinterpret_cast<Raw*>(q + k) = narrow<O, kOut>(x + k);
+  } else {
+    float old[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+      if (A.accumulate && at.has(i)) widen<O>(*reinterpret_cast<const typename Vec<O, 1>::type*>(row + at.at(i)), old + i);
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      if (!at.has(i)) continue;
+      if (A.accumulate) x[i] += old[i];
+      *reinterpret_cast<typename Vec<O, 1>::type*>(row + at.at(i)) = narrow<O, 1>(x + i);
+    }
   }
 }
 
-// T: type of dy, O: of the table's gradient; W elements a lane (8 or 1, so that either type's accesses are whole)
-template <typename T, typename O, int W>
+// T: type of dy, O: of the table's gradient. A warp: a chunk of the sorted tokens, 32 x W columns, eight rows of dy on their way at a time.
+template <typename T, typename O, int W, bool WIDE>
 __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArgs A) {
-  constexpr int kIn = W == 1 ? 1 : kWide<T>;
-  typedef typename Vec<T, kIn>::type Raw;
   start_dependents();
   wait_for_previous();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int slices = (A.D + 32 * W - 1) / (32 * W);
   const int64_t unit = (int64_t)blockIdx.x * 8 + warp, chunk = unit / slices;
-  const int c = ((int)(unit - chunk * slices) * 32 + lane) * W;
+  const Columns<W, WIDE> at((int)(unit - chunk * slices), lane, A.D);
   const int64_t n0 = chunk * A.chunk, n1 = min(n0 + A.chunk, A.N);
   if (n0 >= A.N) return;
-  const bool mine = c < A.D;
   const unsigned none = (unsigned)A.V;
   unsigned current = __ldg(A.key + n0);
   bool joined = n0 > 0 && __ldg(A.key + n0 - 1) == current;            // the row began in an earlier chunk
@@ -243,79 +342,84 @@ __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArg
 #pragma unroll
   for (int i = 0; i < W; ++i) acc[i] = 0.f;
   auto leave = [&](int which) {
-    if (!mine) return;
-    float* p = A.part + (chunk * 2 + which) * A.D + c;
+    float* p = A.part + (chunk * 2 + which) * A.D;
 #pragma unroll
-    for (int i = 0; i < W; ++i) p[i] = acc[i];
+    for (int i = 0; i < W; ++i)
+      if (at.has(i)) p[at.at(i)] = acc[i];
   };
   auto flush = [&]() {
     if (joined) leave(0);
-    else if (mine) finish_row<O, W>(A, current, c, acc);
+    else finish_row<O, W, WIDE>(A, current, at, acc);
   };
-  bool over = false;
-  for (int64_t n = n0; n < n1 && !over; n += 32) {
+  for (int64_t n = n0; n < n1; n += 32) {
     const unsigned key = n + lane < n1 ? __ldg(A.key + n + lane) : none, place = n + lane < n1 ? __ldg(A.place + n + lane) : 0;
-    const int count = (int)min((int64_t)32, n1 - n);
-    for (int i = 0; i < count && !over; i += 8) {
-      Raw r[8][W / kIn];
+    const int count = __popc(__ballot_sync(0xffffffffu, key != none));     // (what is in no row comes last)
+    for (int i = 0; i < count; i += 8) {
+      Share<T, W, WIDE> r[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const unsigned k = __shfl_sync(0xffffffffu, key, i + j), p = __shfl_sync(0xffffffffu, place, i + j);
-#pragma unroll
-        for (int q = 0; q < W / kIn; ++q) {
-          r[j][q] = Raw{};
-          if (mine && k != none) r[j][q] = *reinterpret_cast<const Raw*>(static_cast<const T*>(A.dy) + (int64_t)p * A.lddy + c + q * kIn);
-        }
-      }
+      for (int j = 0; j < 8; ++j) r[j].load(static_cast<const T*>(A.dy) + (int64_t)__shfl_sync(0xffffffffu, place, i + j) * A.lddy, at, i + j < count);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const unsigned k = __shfl_sync(0xffffffffu, key, i + j);
-        if (i + j >= count) break;
-        if (k != current) {
-          flush();
-          current = k;
-          joined = false;
+        if (i + j < count) {
+          if (k != current) {
+            flush();
+            current = k;
+            joined = false;
 #pragma unroll
-          for (int q = 0; q < W; ++q) acc[q] = 0.f;
-          if (k == none) { over = true; break; }
+            for (int q = 0; q < W; ++q) acc[q] = 0.f;
+          }
+          r[j].add_to(acc);
         }
-        float x[W];
-#pragma unroll
-        for (int q = 0; q < W / kIn; ++q) widen<T>(r[j][q], x + q * kIn);
-#pragma unroll
-        for (int q = 0; q < W; ++q) acc[q] += x[q];
       }
     }
+    if (count < 32) break;
   }
-  if (over) return;
   if (n1 < A.N && __ldg(A.key + n1) == current) leave(joined ? 0 : 1);     // it goes on in the next chunk
   else flush();
 }
 
-// The rows that reach over chunks: a CTA for each chunk in which one begins that goes on, and 32 columns of it. Its eight warps take the
+// The rows that reach over chunks: a CTA for each chunk in which one begins that goes on, and 128 columns of it. Its eight warps take the
 // chunks behind it in turn.
 template <typename O>
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ SumArgs A) {
-  __shared__ float sh[8][32];
+  __shared__ float sh[8][4][32];
   start_dependents();
   wait_for_previous();
-  const int64_t chunk = blockIdx.x, n0 = chunk * A.chunk, n1 = n0 + A.chunk;
+  const int64_t chunk = blockIdx.x, n0 = chunk * A.chunk, n1 = n0 + A.chunk, chunks = (A.N + A.chunk - 1) / A.chunk;
   if (n1 >= A.N) return;
-  const unsigned k = __ldg(A.key + n1);
-  if (k == (unsigned)A.V || __ldg(A.key + n1 - 1) != k) return;
-  if (__ldg(A.key + n0) == k && n0 > 0 && __ldg(A.key + n0 - 1) == k) return;            // it began earlier
+  const unsigned k = __ldg(A.key + n1), last = __ldg(A.key + n1 - 1), front = __ldg(A.key + n0), ahead = n0 > 0 ? __ldg(A.key + n0 - 1) : ~k;
+  if (k == (unsigned)A.V || last != k || (front == k && ahead == k)) return;       // nothing goes on here, or it began earlier
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int c0 = blockIdx.y * 32; c0 < A.D; c0 += gridDim.y * 32) {
-    const int c = c0 + lane;
-    float s = 0.f;
-    for (int64_t j = chunk + 1 + warp; j * A.chunk < A.N && __ldg(A.key + j * A.chunk) == k; j += 8)
-      if (c < A.D) s += A.part[j * 2 * A.D + c];
-    sh[warp][lane] = s;
+  for (int slice = blockIdx.y; slice * 128 < A.D; slice += gridDim.y) {
+    const Columns<4, false> at(slice, lane, A.D);
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int64_t j = chunk + 1 + warp; j < chunks; j += 32) {
+      float x[4][4];
+      bool on[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {                        // (what is read of a chunk that is not in the row is left out)
+        const int64_t q = j + 8 * u;
+        on[u] = q < chunks && __ldg(A.key + q * A.chunk) == k;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[u][i] = q < chunks && at.has(i) ? A.part[q * 2 * A.D + at.at(i)] : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] += on[u] ? x[u][i] : 0.f;
+      if (!on[3]) break;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sh[warp][i][lane] = s[i];
     __syncthreads();
-    if (warp == 0 && c < A.D) {
-      s = A.part[(chunk * 2 + 1) * A.D + c];
-      for (int w = 0; w < 8; ++w) s += sh[w][lane];
-      finish_row<O, 1>(A, k, c, &s);
+    if (warp == 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[i] = at.has(i) ? A.part[(chunk * 2 + 1) * A.D + at.at(i)] : 0.f;
+        for (int w = 0; w < 8; ++w) s[i] += sh[w][i][lane];
+      }
+      finish_row<O, 4, false>(A, k, at, s);
     }
     __syncthreads();
   }
@@ -323,9 +427,9 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ SumAr
 
 // ---------------------------------------------------------------------------------------------- host
 
-// Tokens a chunk: enough chunks for 16 warps on every SM, and 32 tokens at least (a chunk's ends cost it two rows of fp32).
+// Tokens a chunk: enough chunks for 24 warps on every SM, and 32 tokens at least (a chunk's ends cost it two rows of fp32). W: columns a lane.
 int chunk_of(int64_t N, int64_t D, int W) {
-  const int64_t slices = (D + 32 * W - 1) / (32 * W), chunks = (148 * 16 + slices - 1) / slices;
+  const int64_t slices = (D + 32 * W - 1) / (32 * W), chunks = (148 * 24 + slices - 1) / slices;
   const int64_t per = (N + chunks - 1) / chunks;
   return (int)((per + 31) / 32 * 32);
 }
@@ -336,7 +440,7 @@ struct BackPlan {
 BackPlan back_plan(int64_t N, int64_t D) {
   BackPlan p;
   p.keys = pad256(N * 4);
-  const int64_t chunk = chunk_of(N, D, 8), chunk1 = chunk_of(N, D, 1), least = chunk < chunk1 ? chunk : chunk1;
+  const int64_t chunk = chunk_of(N, D, 8), chunk4 = chunk_of(N, D, 4), least = chunk < chunk4 ? chunk : chunk4;
   p.part = pad256((N + least - 1) / least * 2 * D * (int64_t)sizeof(float));
   p.total = 4 * p.keys + p.part;
   return p;
@@ -346,12 +450,14 @@ bool type_ok(int t) { return t == DMX_F32 || t == DMX_BF16; }
 bool sizes_ok(int64_t N, int64_t V, int64_t D) { return N >= 0 && V >= 0 && D >= 0 && N <= DMX_EMBEDDING_MAX && V <= DMX_EMBEDDING_MAX && D <= DMX_EMBEDDING_MAX_WIDTH; }
 
 template <typename T, typename O>
-int sums(const SumArgs& A, bool wide, cudaStream_t st) {
-  const int W = wide ? 8 : 1;
+int sums(SumArgs A, bool wide, cudaStream_t st) {
+  constexpr int kW = kWide<T>;
+  const int W = wide ? kW : 4;
+  A.chunk = chunk_of(A.N, A.D, W);
   const int64_t chunks = (A.N + A.chunk - 1) / A.chunk, slices = (A.D + 32 * W - 1) / (32 * W), ctas = (chunks * slices + 7) / 8;
-  const int rc = wide ? start(dim3((unsigned)ctas), 256, 1, 0, st, sum_kernel<T, O, 8>, A) : start(dim3((unsigned)ctas), 256, 1, 0, st, sum_kernel<T, O, 1>, A);
+  const int rc = wide ? start(dim3((unsigned)ctas), 256, 1, 0, st, sum_kernel<T, O, kW, true>, A) : start(dim3((unsigned)ctas), 256, 1, 0, st, sum_kernel<T, O, 4, false>, A);
   if (rc != DMX_OK || chunks == 1) return rc;
-  return start(dim3((unsigned)(chunks - 1), (unsigned)((A.D + 31) / 32 < 64 ? (A.D + 31) / 32 : 64)), 256, 1, 0, st, join_kernel<O>, A);
+  return start(dim3((unsigned)(chunks - 1), (unsigned)((A.D + 127) / 128 < 8 ? (A.D + 127) / 128 : 8)), 256, 1, 0, st, join_kernel<O>, A);
 }
 
 }  // namespace
@@ -402,9 +508,10 @@ int dmx_embedding_backward(int64_t N, int64_t V, int64_t D, int id_bytes, const 
   constexpr int kShared = kSortWarps * kDigits * 4;       // 32 KB
   const int rc = start(dim3(accumulate ? kSortCtas : 144), kSortThreads, 1, kShared, st, sort_kernel, S);
   if (rc != DMX_OK) return rc;
-  const bool wide = wide_rows(dy, N, lddy, D, dtype) && wide_rows(dtable, V, ldt, D, out_dtype) && D % 8 == 0;
-  SumArgs A = {S.key[0], S.place[0], dy, dtable, reinterpret_cast<float*>(ws + 4 * p.keys), N, V, N > 1 ? lddy : D, V > 1 ? ldt : D, (int)D,
-               chunk_of(N, D, wide ? 8 : 1), accumulate != 0, scale};
+  // 16-byte accesses of dy, and as many elements of the table's rows: 8 to 32 bytes
+  const int W = 16 / e;
+  const bool wide = wide_rows(dy, N, lddy, D, dtype) && aligned(dtable, W * eo < 16 ? W * eo : 16) && (V <= 1 || ldt % (W * eo < 16 ? W : 16 / (int)eo) == 0);
+  SumArgs A = {S.key[0], S.place[0], dy, dtable, reinterpret_cast<float*>(ws + 4 * p.keys), N, V, N > 1 ? lddy : D, V > 1 ? ldt : D, (int)D, 0, accumulate != 0, scale};
   if (dtype == DMX_F32) return out_dtype == DMX_F32 ? sums<float, float>(A, wide, st) : sums<float, bf16>(A, wide, st);
   return out_dtype == DMX_F32 ? sums<bf16, float>(A, wide, st) : sums<bf16, bf16>(A, wide, st);
 }
