@@ -69,7 +69,7 @@ struct SortArgs {
   const void* ids;
   int wide_ids, passes;
   int64_t N, V;
-  unsigned *key[2], *place[2];     // passes go from one to the other; the last one ends in 0
+  uint2* pair[2];                  // key and place; passes go from one to the other, the last one ends in 0
   void* zero;                      // rows to clear, or NULL
   int64_t zero_ld;                 // in bytes
   int64_t zero_bytes;              // of a row
@@ -124,8 +124,9 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
       k = p = 0;
       if (n >= A.N) return;
       if (pass > 0) {
-        k = __ldcg(A.key[from] + n);
-        p = __ldcg(A.place[from] + n);
+        const uint2 t = __ldcg(A.pair[from] + n);
+        k = t.x;
+        p = t.y;
       } else {
         const int64_t id = id_at(A.ids, A.wide_ids, n);
         k = id >= 0 && id < A.V ? (unsigned)id : (unsigned)A.V;      // what is in no row comes last
@@ -212,18 +213,14 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
       for (int r = 0; r < kKept; ++r)
         if (r < rounds && first + r * 32 + lane < A.N) {
           const unsigned to = at[r] + mine[key[r] >> shift & 255];
-          A.key[from ^ 1][to] = key[r];
-          A.place[from ^ 1][to] = place[r];
+          A.pair[from ^ 1][to] = make_uint2(key[r], place[r]);
         }
     } else {
       for (int64_t n = first; n < first + rounds * 32 && n < A.N; n += 32) {
         unsigned k, p;
         fetch(n + lane, k, p);
         const unsigned to = ranked(n + lane < A.N, k);
-        if (n + lane < A.N) {
-          A.key[from ^ 1][to] = k;
-          A.place[from ^ 1][to] = p;
-        }
+        if (n + lane < A.N) A.pair[from ^ 1][to] = make_uint2(k, p);
       }
     }
     if (pass + 1 == A.passes) break;
@@ -235,7 +232,7 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
 // ---------------------------------------------------------------------------------------------- the sums
 
 struct SumArgs {
-  const unsigned *key, *place;
+  const uint2* pair;               // sorted: key and place
   const void* dy;
   void* out;
   float* part;                     // [chunks][2][D]: what a chunk's first and last row got, where they go on
@@ -335,8 +332,8 @@ __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArg
   const int64_t n0 = chunk * A.chunk, n1 = min(n0 + A.chunk, A.N);
   if (n0 >= A.N) return;
   const unsigned none = (unsigned)A.V;
-  unsigned current = __ldg(A.key + n0);
-  bool joined = n0 > 0 && __ldg(A.key + n0 - 1) == current;            // the row began in an earlier chunk
+  unsigned current = __ldg(A.pair + n0).x;
+  bool joined = n0 > 0 && __ldg(A.pair + n0 - 1).x == current;            // the row began in an earlier chunk
   if (current == none) return;
   float acc[W];
 #pragma unroll
@@ -352,7 +349,8 @@ __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArg
     else finish_row<O, W, WIDE>(A, current, at, acc);
   };
   for (int64_t n = n0; n < n1; n += 32) {
-    const unsigned key = n + lane < n1 ? __ldg(A.key + n + lane) : none, place = n + lane < n1 ? __ldg(A.place + n + lane) : 0;
+    const uint2 pair = n + lane < n1 ? __ldg(A.pair + n + lane) : make_uint2(none, 0);
+    const unsigned key = pair.x, place = pair.y;
     const int count = __popc(__ballot_sync(0xffffffffu, key != none));     // (what is in no row comes last)
     for (int i = 0; i < count; i += 8) {
       Share<T, W, WIDE> r[8];
@@ -375,53 +373,67 @@ __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArg
     }
     if (count < 32) break;
   }
-  if (n1 < A.N && __ldg(A.key + n1) == current) leave(joined ? 0 : 1);     // it goes on in the next chunk
+  if (n1 < A.N && __ldg(A.pair + n1).x == current) leave(joined ? 0 : 1);     // it goes on in the next chunk
   else flush();
 }
 
-// The rows that reach over chunks: a CTA for each chunk in which one begins that goes on, and 128 columns of it. Its eight warps take the
-// chunks behind it in turn.
+// The rows that reach over chunks. A CTA looks at eight chunks and takes those in which a row begins that goes on; 128 columns of it, its
+// eight warps the chunks behind in turn.
 template <typename O>
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ SumArgs A) {
   __shared__ float sh[8][4][32];
+  __shared__ unsigned rows[8];
   start_dependents();
   wait_for_previous();
-  const int64_t chunk = blockIdx.x, n0 = chunk * A.chunk, n1 = n0 + A.chunk, chunks = (A.N + A.chunk - 1) / A.chunk;
-  if (n1 >= A.N) return;
-  const unsigned k = __ldg(A.key + n1), last = __ldg(A.key + n1 - 1), front = __ldg(A.key + n0), ahead = n0 > 0 ? __ldg(A.key + n0 - 1) : ~k;
-  if (k == (unsigned)A.V || last != k || (front == k && ahead == k)) return;       // nothing goes on here, or it began earlier
+  const int64_t chunks = (A.N + A.chunk - 1) / A.chunk;
+  if (threadIdx.x < 8) {
+    const int64_t n0 = ((int64_t)blockIdx.x * 8 + threadIdx.x) * A.chunk, n1 = n0 + A.chunk;
+    unsigned k = (unsigned)A.V;
+    if (n1 < A.N) {
+      k = __ldg(A.pair + n1).x;
+      const unsigned last = __ldg(A.pair + n1 - 1).x, front = __ldg(A.pair + n0).x, ahead = n0 > 0 ? __ldg(A.pair + n0 - 1).x : ~k;
+      if (last != k || (front == k && ahead == k)) k = (unsigned)A.V;       // nothing goes on here, or it began earlier
+    }
+    rows[threadIdx.x] = k;
+  }
+  __syncthreads();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int slice = blockIdx.y; slice * 128 < A.D; slice += gridDim.y) {
-    const Columns<4, false> at(slice, lane, A.D);
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t j = chunk + 1 + warp; j < chunks; j += 32) {
-      float x[4][4];
-      bool on[4];
+  for (int r = 0; r < 8; ++r) {
+    const unsigned k = rows[r];
+    if (k == (unsigned)A.V) continue;
+    const int64_t chunk = (int64_t)blockIdx.x * 8 + r;
+    for (int slice = blockIdx.y; slice * 128 < A.D; slice += gridDim.y) {
+      const Columns<4, false> at(slice, lane, A.D);
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int64_t j = chunk + 1 + warp; j < chunks; j += 32) {
+        float x[4][4];
+        bool on[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {                        // (what is read of a chunk that is not in the row is left out)
-        const int64_t q = j + 8 * u;
-        on[u] = q < chunks && __ldg(A.key + q * A.chunk) == k;
+        for (int u = 0; u < 4; ++u) {                      // (what is read of a chunk that is not in the row is left out)
+          const int64_t q = j + 8 * u;
+          on[u] = q < chunks && __ldg(A.pair + q * A.chunk).x == k;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[u][i] = q < chunks && at.has(i) ? A.part[q * 2 * A.D + at.at(i)] : 0.f;
+          for (int i = 0; i < 4; ++i) x[u][i] = q < chunks && at.has(i) ? A.part[q * 2 * A.D + at.at(i)] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[i] += on[u] ? x[u][i] : 0.f;
+        if (!on[3]) break;
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int i = 0; i < 4; ++i) sh[warp][i][lane] = s[i];
+      __syncthreads();
+      if (warp == 0) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] += on[u] ? x[u][i] : 0.f;
-      if (!on[3]) break;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sh[warp][i][lane] = s[i];
-    __syncthreads();
-    if (warp == 0) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[i] = at.has(i) ? A.part[(chunk * 2 + 1) * A.D + at.at(i)] : 0.f;
-        for (int w = 0; w < 8; ++w) s[i] += sh[w][i][lane];
+        for (int i = 0; i < 4; ++i) {
+          s[i] = at.has(i) ? A.part[(chunk * 2 + 1) * A.D + at.at(i)] : 0.f;
+          for (int w = 0; w < 8; ++w) s[i] += sh[w][i][lane];
+        }
+        finish_row<O, 4, false>(A, k, at, s);
       }
-      finish_row<O, 4, false>(A, k, at, s);
+      __syncthreads();
     }
-    __syncthreads();
   }
 }
 
@@ -439,10 +451,10 @@ struct BackPlan {
 };
 BackPlan back_plan(int64_t N, int64_t D) {
   BackPlan p;
-  p.keys = pad256(N * 4);
+  p.keys = pad256(N * 8);
   const int64_t chunk = chunk_of(N, D, 8), chunk4 = chunk_of(N, D, 4), least = chunk < chunk4 ? chunk : chunk4;
   p.part = pad256((N + least - 1) / least * 2 * D * (int64_t)sizeof(float));
-  p.total = 4 * p.keys + p.part;
+  p.total = 2 * p.keys + p.part;
   return p;
 }
 
@@ -457,7 +469,7 @@ int sums(SumArgs A, bool wide, cudaStream_t st) {
   const int64_t chunks = (A.N + A.chunk - 1) / A.chunk, slices = (A.D + 32 * W - 1) / (32 * W), ctas = (chunks * slices + 7) / 8;
   const int rc = wide ? start(dim3((unsigned)ctas), 256, 1, 0, st, sum_kernel<T, O, kW, true>, A) : start(dim3((unsigned)ctas), 256, 1, 0, st, sum_kernel<T, O, 4, false>, A);
   if (rc != DMX_OK || chunks == 1) return rc;
-  return start(dim3((unsigned)(chunks - 1), (unsigned)((A.D + 127) / 128 < 8 ? (A.D + 127) / 128 : 8)), 256, 1, 0, st, join_kernel<O>, A);
+  return start(dim3((unsigned)((chunks + 6) / 8), (unsigned)((A.D + 127) / 128 < 8 ? (A.D + 127) / 128 : 8)), 256, 1, 0, st, join_kernel<O>, A);
 }
 
 }  // namespace
@@ -500,10 +512,7 @@ int dmx_embedding_backward(int64_t N, int64_t V, int64_t D, int id_bytes, const 
   SortArgs S = {};
   S.ids = ids; S.wide_ids = id_bytes == 8; S.N = N; S.V = V;
   for (S.passes = 1; (uint64_t)V >> (8 * S.passes); ++S.passes) {}
-  for (int i = 0; i < 2; ++i) {
-    S.key[i] = reinterpret_cast<unsigned*>(ws + 2 * i * p.keys);
-    S.place[i] = reinterpret_cast<unsigned*>(ws + (2 * i + 1) * p.keys);
-  }
+  for (int i = 0; i < 2; ++i) S.pair[i] = reinterpret_cast<uint2*>(ws + i * p.keys);
   if (!accumulate) { S.zero = dtable; S.zero_ld = (V > 1 ? ldt : D) * eo; S.zero_bytes = D * eo; }
   constexpr int kShared = kSortWarps * kDigits * 4;       // 32 KB
   const int rc = start(dim3(accumulate ? kSortCtas : 144), kSortThreads, 1, kShared, st, sort_kernel, S);
@@ -511,7 +520,7 @@ int dmx_embedding_backward(int64_t N, int64_t V, int64_t D, int id_bytes, const 
   // 16-byte accesses of dy, and as many elements of the table's rows: 8 to 32 bytes
   const int W = 16 / e;
   const bool wide = wide_rows(dy, N, lddy, D, dtype) && aligned(dtable, W * eo < 16 ? W * eo : 16) && (V <= 1 || ldt % (W * eo < 16 ? W : 16 / (int)eo) == 0);
-  SumArgs A = {S.key[0], S.place[0], dy, dtable, reinterpret_cast<float*>(ws + 4 * p.keys), N, V, N > 1 ? lddy : D, V > 1 ? ldt : D, (int)D, 0, accumulate != 0, scale};
+  SumArgs A = {S.pair[0], dy, dtable, reinterpret_cast<float*>(ws + 2 * p.keys), N, V, N > 1 ? lddy : D, V > 1 ? ldt : D, (int)D, 0, accumulate != 0, scale};
   if (dtype == DMX_F32) return out_dtype == DMX_F32 ? sums<float, float>(A, wide, st) : sums<float, bf16>(A, wide, st);
   return out_dtype == DMX_F32 ? sums<bf16, float>(A, wide, st) : sums<bf16, bf16>(A, wide, st);
 }

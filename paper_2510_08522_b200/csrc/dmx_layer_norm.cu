@@ -4,18 +4,26 @@
 // backward   xh = (x - mean) rstd, g = w dy; dx = rstd (g - (sum g + xh sum g xh) / D) + add; dw = sum of dy xh over the rows, db = sum of dy
 //
 // Bound: HBM. A team of threads (8 lanes, a warp, a CTA, or a cluster of CTAs, by the row's width) holds a row in registers, up to
-// 32 values a thread, so that everything is read once; teams stay and take row after row. In backward a thread's columns are the
-// same in every row: it sums its share of dw and db in registers, a CTA's teams join theirs in shared memory, and a small second launch
-// adds the CTAs' in a fixed order.
+// 32 values a thread, so that everything is read once; teams stay and take row after row. Rows to come are on their way into shared
+// memory by asynchronous copies, every thread its own columns into slots of its own (no barrier between copy and use). In backward a
+// thread's columns are the same in every row: it sums its share of dw and db in registers, a CTA's teams join theirs in shared memory, and a
+// small second launch adds the CTAs' in a fixed order.
 // Variance: deviations from the rounded mean are summed beside their squares, and what that mean was off is taken out again:
 // a mean a million deviations away costs the variance nothing.
+#include <atomic>
+
+#include "dmx_f32x2.cuh"
 #include "dmx_rows.cuh"
 
 namespace {
 
 using namespace dmx_rows;
+using namespace dmx_f32x2;
 
 constexpr int kMaxCluster = 8, kMaxWarps = 8;      // of a CTA that is one team
+// Rows on their way to a team: what fills the 40 KB that an SM has to have on its way, and leaves room for two CTAs
+constexpr int kForwardStages = 4;
+template <typename T> constexpr int kBackwardStages = sizeof(T) == 2 ? 4 : 2;
 
 struct Args {
   const void *x, *dy, *add;
@@ -31,7 +39,8 @@ struct Args {
 // How a row is held. TEAM: lanes of a warp that share a row, 0 a CTA, -1 a cluster. N values per thread in accesses of V.
 template <typename T, int V, int TEAM, int N>
 struct Held {
-  static constexpr int kAccesses = N / V;
+  static constexpr int kAccesses = N / V, kThreads = TEAM > 0 ? 128 : 256;
+  static constexpr bool kAhead = V * sizeof(T) >= 4;       // asynchronous copies take 4 bytes at least
   typedef typename Vec<T, V>::type Raw;
 
   // this thread's place in its team, the team's size, its row and the rows between its rows
@@ -51,14 +60,32 @@ struct Held {
       row = blockIdx.x / n; step = gridDim.x / n;
     }
   }
-  static __device__ __forceinline__ void load(const void* p, int64_t ld, int64_t row, int t, int size, int D, Raw (&r)[kAccesses]) {
+  // A row's values on their way to this thread's slots (kAccesses of them, blockDim.x apart), zeros behind its end
+  static __device__ __forceinline__ void send(Raw* slots, const void* p, int64_t ld, int64_t row, int t, int size, int D) {
     const T* q = static_cast<const T*>(p) + row * ld;
 #pragma unroll
     for (int i = 0; i < kAccesses; ++i) {
-      const int c = (i * size + t) * V;
-      if (c < D) r[i] = *reinterpret_cast<const Raw*>(q + c);
-      else r[i] = Raw{};
+      const int c = (i * size + t) * V, bytes = c < D ? (int)sizeof(Raw) : 0;
+      const unsigned to = (unsigned)__cvta_generic_to_shared(slots + i * blockDim.x);
+      if constexpr (sizeof(Raw) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(c < D ? q + c : q), "r"(bytes) : "memory");
+      else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(c < D ? q + c : q), "r"(bytes) : "memory");
     }
+  }
+  static __device__ __forceinline__ void take(const Raw* slots, float (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < kAccesses; ++i) widen<T>(slots[i * blockDim.x], x + i * V);
+  }
+  static __device__ __forceinline__ void load(const void* p, int64_t ld, int64_t row, int t, int size, int D, float (&x)[N]) {
+    const T* q = static_cast<const T*>(p) + row * ld;
+    Raw r[kAccesses];
+#pragma unroll
+    for (int i = 0; i < kAccesses; ++i) {
+      const int c = (i * size + t) * V;
+      r[i] = Raw{};
+      if (c < D) r[i] = *reinterpret_cast<const Raw*>(q + c);
+    }
+#pragma unroll
+    for (int i = 0; i < kAccesses; ++i) widen<T>(r[i], x + i * V);
   }
   static __device__ __forceinline__ void store(void* p, int64_t ld, int64_t row, int t, int size, int D, const float (&x)[N]) {
     T* q = static_cast<T*>(p) + row * ld;
@@ -67,10 +94,6 @@ struct Held {
       const int c = (i * size + t) * V;
       if (c < D) *reinterpret_cast<Raw*>(q + c) = narrow<T, V>(x + i * V);
     }
-  }
-  static __device__ __forceinline__ void unpack(const Raw (&r)[kAccesses], float (&x)[N]) {
-#pragma unroll
-    for (int i = 0; i < kAccesses; ++i) widen<T>(r[i], x + i * V);
   }
   // an fp32 vector's values at this thread's columns; `otherwise` where there is no vector
   static __device__ __forceinline__ void vector(const float* w, int wvec, float otherwise, int t, int size, int D, float (&x)[N]) {
@@ -89,7 +112,23 @@ struct Held {
       }
     }
   }
+  // zeros behind the row's end
+  static __device__ __forceinline__ void cut(int t, int size, int D, float (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < kAccesses; ++i) {
+      if ((i + 1) * size * V <= D) continue;               // (the same for all)
+#pragma unroll
+      for (int k = 0; k < V; ++k) x[i * V + k] = (i * size + t) * V < D ? x[i * V + k] : 0.f;
+    }
+  }
 };
+
+template <int STAGES>
+__device__ __forceinline__ void copies_landed() { asm volatile("cp.async.wait_group %0;" ::"n"(STAGES) : "memory"); }
+__device__ __forceinline__ void copies_sent() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+
+__device__ __forceinline__ float2 pair(const float* x, int i) { return make_float2(x[2 * i], x[2 * i + 1]); }
+__device__ __forceinline__ void set_pair(float* x, int i, float2 v) { x[2 * i] = v.x; x[2 * i + 1] = v.y; }
 
 // Sums of two values over a team. `red`: two buffers of kMaxCluster x kMaxWarps pairs, used in turn (`turn` flips).
 template <int TEAM>
@@ -126,98 +165,147 @@ __device__ __forceinline__ float2 team_sum(float2 v, float2 (*red)[kMaxCluster *
   return v;
 }
 
+// (A warp's lanes stay together: those of a team without a row left take the last one again and store nothing.)
 template <typename T, int V, int TEAM, int N>
-__global__ void __launch_bounds__(TEAM > 0 ? 128 : 256) forward_kernel(const __grid_constant__ Args A) {
+__global__ void __launch_bounds__(Held<T, V, TEAM, N>::kThreads) forward_kernel(const __grid_constant__ Args A) {
   typedef Held<T, V, TEAM, N> H;
+  extern __shared__ __align__(16) unsigned char raw[];
   __shared__ float2 red[2][kMaxCluster * kMaxWarps];
+  typename H::Raw* slots = reinterpret_cast<typename H::Raw*>(raw) + threadIdx.x;
+  const int stage = H::kAccesses * blockDim.x;             // slots from stage to stage
   int t, size, turn = 0;
   int64_t row, step;
   H::place(t, size, row, step);
   start_dependents();
   if constexpr (TEAM < 0) asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");   // all of it is there
   wait_for_previous();
+  auto send = [&](int s, int64_t r) {
+    if constexpr (H::kAhead) {
+      if (r < A.M) H::send(slots + s * stage, A.x, A.ldx, r, t, size, A.D);
+      copies_sent();
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < kForwardStages; ++s) send(s, row + s * step);
   float w[N], b[N];
   H::vector(A.weight, A.wvec, 1.f, t, size, A.D, w);
   H::vector(A.bias, A.wvec, 0.f, t, size, A.D, b);
   const float per = 1.f / (float)A.D;
-  // (a warp's lanes stay together: those of a team without a row left repeat the last one and store nothing)
+  int s = 0;
   for (int64_t base = row - (TEAM > 0 ? threadIdx.x % 32 / (TEAM > 0 ? TEAM : 1) : 0); base < A.M; base += step, row += step) {
     const bool live = row < A.M;
-    typename H::Raw raw[H::kAccesses];
-    H::load(A.x, A.ldx, live ? row : A.M - 1, t, size, A.D, raw);
     float x[N];
-    H::unpack(raw, x);
-    float2 s = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < N; ++i) s.x += x[i];
-    s = team_sum<TEAM>(s, red, turn);
-    const float rough = s.x * per;
-    s = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      x[i] -= rough;
-      if ((i / V * size + t) * V < A.D) { s.x += x[i]; s.y = fmaf(x[i], x[i], s.y); }
+    if constexpr (H::kAhead) {
+      copies_landed<kForwardStages - 1>();
+      H::take(slots + s * stage, x);
+    } else {
+      H::load(A.x, A.ldx, live ? row : A.M - 1, t, size, A.D, x);
     }
-    s = team_sum<TEAM>(s, red, turn);
-    const float off = s.x * per, var = fmaf(-off, off, s.y * per), rstd = __frsqrt_rn((var < 0.f ? 0.f : var) + A.eps);   // (a NaN stays)
+    float2 a = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = fmaf((x[i] - off) * rstd, w[i], b[i]);
+    for (int i = 0; i < N / 2; ++i) a = add2(a, pair(x, i));
+    const float rough = team_sum<TEAM>(make_float2(a.x + a.y, 0.f), red, turn).x * per;
+    send(s, row + kForwardStages * step);                  // (its values are in registers by now)
+    if (++s == kForwardStages) s = 0;
+    float2 q = make_float2(0.f, 0.f);
+    a = q;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) set_pair(x, i, add2(pair(x, i), two(-rough)));
+    H::cut(t, size, A.D, x);
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) { a = add2(a, pair(x, i)); q = fma2(pair(x, i), pair(x, i), q); }
+    const float2 sum = team_sum<TEAM>(make_float2(a.x + a.y, q.x + q.y), red, turn);
+    const float off = sum.x * per, var = fmaf(-off, off, sum.y * per), rstd = __frsqrt_rn((var < 0.f ? 0.f : var) + A.eps);   // (a NaN stays)
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) set_pair(x, i, fma2(mul2(add2(pair(x, i), two(-off)), two(rstd)), pair(w, i), pair(b, i)));
     if (!live) continue;
     H::store(A.out, A.ldout, row, t, size, A.D, x);
     if (t == 0) { A.mean[row] = rough + off; A.rstd[row] = rstd; }
   }
+  if constexpr (H::kAhead) copies_landed<0>();
 }
 
 template <typename T, int V, int TEAM, int N>
-__global__ void __launch_bounds__(TEAM > 0 ? 128 : 256) backward_kernel(const __grid_constant__ Args A) {
+__global__ void __launch_bounds__(Held<T, V, TEAM, N>::kThreads) backward_kernel(const __grid_constant__ Args A) {
   typedef Held<T, V, TEAM, N> H;
+  constexpr int kStages = kBackwardStages<T>;
+  extern __shared__ __align__(16) unsigned char raw[];
   __shared__ float2 red[2][kMaxCluster * kMaxWarps];
-  __shared__ __align__(16) float joined[TEAM > 0 ? 4 * 2 * N * 32 : 1];
+  typename H::Raw* slots = reinterpret_cast<typename H::Raw*>(raw) + threadIdx.x;
+  const int part = H::kAccesses * blockDim.x, stage = part * (A.add ? 3 : 2);      // slots from input to input, from stage to stage
   int t, size, turn = 0;
   int64_t row, step;
   H::place(t, size, row, step);
   start_dependents();
   if constexpr (TEAM < 0) asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
   wait_for_previous();
+  auto send = [&](int s, int64_t r) {
+    if constexpr (H::kAhead) {
+      if (r < A.M) {
+        H::send(slots + s * stage, A.x, A.ldx, r, t, size, A.D);
+        H::send(slots + s * stage + part, A.dy, A.lddy, r, t, size, A.D);
+        if (A.add) H::send(slots + s * stage + 2 * part, A.add, A.ldadd, r, t, size, A.D);
+      }
+      copies_sent();
+    }
+  };
+#pragma unroll
+  for (int s = 0; s < kStages; ++s) send(s, row + s * step);
   const float per = 1.f / (float)A.D;
   float dw[N], db[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) dw[i] = db[i] = 0.f;
+  float next_mean = 0.f, next_rstd = 0.f;
+  if (row < A.M) { next_mean = A.mean[row]; next_rstd = A.rstd[row]; }
+  int s = 0;
   for (int64_t base = row - (TEAM > 0 ? threadIdx.x % 32 / (TEAM > 0 ? TEAM : 1) : 0); base < A.M; base += step, row += step) {
     const bool live = row < A.M;
-    const int64_t at = live ? row : A.M - 1;
-    typename H::Raw rx[H::kAccesses], rg[H::kAccesses], ra[H::kAccesses];
-    H::load(A.x, A.ldx, at, t, size, A.D, rx);
-    H::load(A.dy, A.lddy, at, t, size, A.D, rg);
-    if (A.add) H::load(A.add, A.ldadd, at, t, size, A.D, ra);
-    const float mean = A.mean[at], rstd = A.rstd[at];
+    const float mean = next_mean, rstd = next_rstd;
+    if (row + step < A.M) { next_mean = A.mean[row + step]; next_rstd = A.rstd[row + step]; }
     float h[N], g[N], w[N];
-    H::unpack(rx, h);
-    H::unpack(rg, g);
     H::vector(A.weight, A.wvec, 1.f, t, size, A.D, w);
-    float2 s = make_float2(0.f, 0.f);
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      h[i] = (h[i] - mean) * rstd;
-      if (live) { dw[i] = fmaf(g[i], h[i], dw[i]); db[i] += g[i]; }
-      g[i] *= w[i];
-      if ((i / V * size + t) * V < A.D) { s.x += g[i]; s.y = fmaf(g[i], h[i], s.y); }
+    if constexpr (H::kAhead) {
+      copies_landed<kStages - 1>();
+      H::take(slots + s * stage, h);
+      H::take(slots + s * stage + part, g);
+    } else {
+      H::load(A.x, A.ldx, live ? row : A.M - 1, t, size, A.D, h);
+      H::load(A.dy, A.lddy, live ? row : A.M - 1, t, size, A.D, g);
     }
-    s = team_sum<TEAM>(s, red, turn);
-    s.x *= per; s.y *= per;
+    float2 a = make_float2(0.f, 0.f), q = a;
 #pragma unroll
-    for (int i = 0; i < N; ++i) g[i] = rstd * (g[i] - fmaf(h[i], s.y, s.x));
+    for (int i = 0; i < N / 2; ++i) {                      // (behind the row's end dy is 0)
+      const float2 u = mul2(add2(pair(h, i), two(-mean)), two(rstd)), v = pair(g, i), x = mul2(v, pair(w, i));
+      if (live) {
+        set_pair(dw, i, fma2(v, u, pair(dw, i)));
+        set_pair(db, i, add2(pair(db, i), v));
+      }
+      a = add2(a, x);
+      q = fma2(x, u, q);
+      set_pair(h, i, u);
+      set_pair(g, i, x);
+    }
+    float2 sum = team_sum<TEAM>(make_float2(a.x + a.y, q.x + q.y), red, turn);
+    sum.x *= per; sum.y *= per;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) set_pair(g, i, mul2(sub2(pair(g, i), fma2(pair(h, i), two(sum.y), two(sum.x))), two(rstd)));
     if (A.add) {
-      H::unpack(ra, h);
+      if constexpr (H::kAhead) H::take(slots + s * stage + 2 * part, h);
+      else H::load(A.add, A.ldadd, live ? row : A.M - 1, t, size, A.D, h);
 #pragma unroll
-      for (int i = 0; i < N; ++i) g[i] += h[i];
+      for (int i = 0; i < N / 2; ++i) set_pair(g, i, add2(pair(g, i), pair(h, i)));
     }
     if (live) H::store(A.out, A.ldout, row, t, size, A.D, g);
+    send(s, row + kStages * step);                         // (its values have been used)
+    if (++s == kStages) s = 0;
   }
+  if constexpr (H::kAhead) copies_landed<0>();
   if (!A.part) return;
-  float* part = A.part + (TEAM < 0 ? step > 0 ? (int64_t)(blockIdx.x / (size / blockDim.x)) : 0 : (int64_t)blockIdx.x) * 2 * A.D;
+  float* part_of = A.part + (TEAM < 0 ? (int64_t)(blockIdx.x / (size / blockDim.x)) : (int64_t)blockIdx.x) * 2 * A.D;
   if constexpr (TEAM > 0) {
     // the lanes of a warp that hold the same columns, then the warps
+    __syncthreads();                                       // the slots are free
+    float* joined = reinterpret_cast<float*>(raw);         // [warps][2][N][32]
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
     for (int o = 16; o >= TEAM; o >>= 1) {
@@ -242,13 +330,13 @@ __global__ void __launch_bounds__(TEAM > 0 ? 128 : 256) backward_kernel(const __
       if (l >= TEAM || c >= A.D) continue;
       float v = 0.f;
       for (int k = 0; k < warps; ++k) v += joined[((k * 2 + which) * N + i) * 32 + l];
-      part[which * (int64_t)A.D + c] = v;
+      part_of[which * (int64_t)A.D + c] = v;
     }
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int c = (i / V * size + t) * V + i % V;
-      if (c < A.D) { part[c] = dw[i]; part[(int64_t)A.D + c] = db[i]; }
+      if (c < A.D) { part_of[c] = dw[i]; part_of[(int64_t)A.D + c] = db[i]; }
     }
   }
 }
@@ -261,7 +349,7 @@ __global__ void __launch_bounds__(1024) columns_kernel(const float* part, int64_
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, which = blockIdx.y;
   float s = 0.f;
   if (c < D) {
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t r = warp; r < rows; r += 32) s += part[(r * 2 + which) * D + c];
   }
   sh[warp][lane] = s;
@@ -293,8 +381,9 @@ Plan plan_of(int64_t M, int D, int backward) {
     const int share = (D + p.cluster - 1) / p.cluster;
     p.threads = ((share + 31) / 32 + 31) / 32 * 32;
   }
-  const int rows = p.team > 0 ? 128 / p.team : 1;
-  const int64_t want = (M + rows - 1) / rows, most = p.team < 0 ? 148 * 2 / p.cluster : p.team == 0 ? 148 * (512 / p.threads) : 148 * (backward ? 3 : 4);
+  // CTAs on an SM: two in backward with 32 values a thread (its registers), more where a thread holds less
+  const int rows = p.team > 0 ? 128 / p.team : 1, at_once = p.team <= 0 ? (backward ? 256 : 512) / p.threads : p.values == 32 ? (backward ? 2 : 4) : p.values == 16 ? 4 : 6;
+  const int64_t want = (M + rows - 1) / rows, most = 148 * (at_once > 0 ? at_once : 1) / p.cluster;
   p.groups = want < most ? want : most;
   return p;
 }
@@ -302,7 +391,21 @@ Plan plan_of(int64_t M, int D, int backward) {
 template <typename T, int V, int TEAM, int N>
 int launch(const Args& A, const Plan& p, int backward, cudaStream_t st) {
   const dim3 grid((unsigned)(p.groups * p.cluster));
-  return backward ? start(grid, p.threads, p.cluster, 0, st, backward_kernel<T, V, TEAM, N>, A) : start(grid, p.threads, p.cluster, 0, st, forward_kernel<T, V, TEAM, N>, A);
+  const int input = p.threads * N * (int)sizeof(T);       // a CTA's rows of one input
+  int shared = !Held<T, V, TEAM, N>::kAhead ? 0 : backward ? kBackwardStages<T> * (A.add ? 3 : 2) * input : kForwardStages * input;
+  if (backward && TEAM > 0 && shared < 4 * 2 * N * 32 * 4) shared = 4 * 2 * N * 32 * 4;        // the warps' sums
+  static std::atomic<uint64_t> set[2];                    // devices on which the kernel may use that much
+  int device = 0;
+  if (!dmxh::cuda_ok(cudaGetDevice(&device))) return DMX_ERR_CUDA;
+  const uint64_t bit = (uint64_t)1 << (device & 63);
+  if (!(set[backward].load(std::memory_order_relaxed) & bit) || device > 63) {
+    constexpr int kMost = 200 * 1024;
+    const auto f = backward ? cudaFuncSetAttribute(backward_kernel<T, V, TEAM, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost)
+                            : cudaFuncSetAttribute(forward_kernel<T, V, TEAM, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
+    if (!dmxh::cuda_ok(f)) return DMX_ERR_CUDA;
+    set[backward].fetch_or(bit, std::memory_order_relaxed);
+  }
+  return backward ? start(grid, p.threads, p.cluster, shared, st, backward_kernel<T, V, TEAM, N>, A) : start(grid, p.threads, p.cluster, shared, st, forward_kernel<T, V, TEAM, N>, A);
 }
 template <typename T, int V>
 int launch(const Args& A, const Plan& p, int backward, cudaStream_t st) {
