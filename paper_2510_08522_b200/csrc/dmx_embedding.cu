@@ -9,6 +9,8 @@
 // tokens over its columns, row after row in registers: each gradient row is read once, each row of the table written once. A row whose
 // tokens reach over chunks leaves fp32 sums, one per chunk, which a third launch joins. Work is cut by tokens, not by rows: how
 // often a token comes does not matter. Nothing is added atomically; the order of all sums is fixed by the shape and the ids.
+#include <type_traits>
+
 #include "dmx_rows.cuh"
 
 namespace {
@@ -70,6 +72,7 @@ struct SortArgs {
   int wide_ids, passes;
   int64_t N, V;
   uint2* pair[2];                  // key and place; passes go from one to the other, the last one ends in 0
+  unsigned* crossing;              // to be zeroed
   void* zero;                      // rows to clear, or NULL
   int64_t zero_ld;                 // in bytes
   int64_t zero_bytes;              // of a row
@@ -109,6 +112,7 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
     clear_rows(A, blockIdx.x - kSortCtas, gridDim.x - kSortCtas);
     return;
   }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *A.crossing = 0;
   cluster_sync();                                         // all of it is there
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x;
   const int digit = threadIdx.x & 255, group = threadIdx.x >> 8;      // of the prefix sums: a digit of eight warps
@@ -235,6 +239,7 @@ struct SumArgs {
   const uint2* pair;               // sorted: key and place
   const void* dy;
   void* out;
+  unsigned* crossing;              // how many chunks have a last row that begins there and goes on, then which (in any order)
   float* part;                     // [chunks][2][D]: what a chunk's first and last row got, where they go on
   int64_t N, V, lddy, ldout;
   int D, chunk, accumulate;        // chunk: tokens, a multiple of 32
@@ -258,8 +263,7 @@ struct Share {
   __device__ __forceinline__ void load(const T* row, const Columns<W, WIDE>& at, bool live) {
 #pragma unroll
     for (int i = 0; i < (WIDE ? 1 : W); ++i) {
-      r[i] = Raw{};
-      if (live && at.has(i)) r[i] = *reinterpret_cast<const Raw*>(row + at.at(i));
+      load_if(r[i], row + at.at(i), live && at.has(i));
     }
   }
   __device__ __forceinline__ void add_to(float (&acc)[W]) const {
@@ -278,8 +282,25 @@ template <> struct Whole<float, 4> { typedef uint4 type; static constexpr int n 
 template <> struct Whole<bf16, 8> { typedef uint4 type; static constexpr int n = 8; };
 template <> struct Whole<bf16, 4> { typedef uint2 type; static constexpr int n = 4; };
 
+// A lane's share of a row of the table's gradient
 template <typename O, int W, bool WIDE>
-__device__ __forceinline__ void finish_row(const SumArgs& A, unsigned v, const Columns<W, WIDE>& at, const float (&acc)[W]) {
+struct Row {
+  typedef Whole<O, WIDE ? W : 4> H;
+  typedef typename std::conditional<WIDE, typename H::type, typename Vec<O, 1>::type>::type Unit;
+  Unit r[WIDE ? W / H::n : W];
+  __device__ __forceinline__ void load(const O* row, const Columns<W, WIDE>& at, bool live) {
+    constexpr int n = WIDE ? W / H::n : W;
+#pragma unroll
+    for (int k = 0; k < n; ++k) {
+      const int i = WIDE ? k * H::n : k;
+      load_if(r[k], row + at.at(i), live && at.has(i));
+    }
+  }
+};
+
+// acc * scale (+ old) to the row
+template <typename O, int W, bool WIDE>
+__device__ __forceinline__ void finish_row(const SumArgs& A, unsigned v, const Columns<W, WIDE>& at, const float (&acc)[W], const Row<O, W, WIDE>& old) {
   O* row = static_cast<O*>(A.out) + (int64_t)v * A.ldout;
   float x[W];
 #pragma unroll
@@ -288,53 +309,56 @@ __device__ __forceinline__ void finish_row(const SumArgs& A, unsigned v, const C
     typedef Whole<O, W> H;
     if (!at.has(0)) return;
 #pragma unroll
-    for (int k = 0; k < W; k += H::n) {
-      typename H::type* q = reinterpret_cast<typename H::type*>(row + at.at(k));
+    for (int k = 0; k < W / H::n; ++k) {
+      float* y = x + k * H::n;
       if (A.accumulate) {
-        const typename H::type old = *q;
         if constexpr (sizeof(O) == 4) {
           float o[4];
-          widen<O>(old, o);
+          widen<O>(old.r[k], o);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[k + i] += o[i];
+          for (int i = 0; i < 4; ++i) y[i] += o[i];
         } else {
-          const unsigned* w = reinterpret_cast<const unsigned*>(&old);
+          const unsigned* w = reinterpret_cast<const unsigned*>(&old.r[k]);
 #pragma unroll
-          for (int i = 0; i < H::n / 2; ++i) { x[k + 2 * i] += __uint_as_float(w[i] << 16); x[k + 2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u); }
+          for (int i = 0; i < H::n / 2; ++i) { y[2 * i] += __uint_as_float(w[i] << 16); y[2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u); }
         }
       }
-      if constexpr (sizeof(O) == 4 || H::n == 8) *q = narrow<O, H::n>(x + k);
-      else *q = make_uint2(pack2(x[k], x[k + 1]), pack2(x[k + 2], x[k + 3]));
+      typename H::type* q = reinterpret_cast<typename H::type*>(row + at.at(k * H::n));
+      if constexpr (sizeof(O) == 4 || H::n == 8) *q = narrow<O, H::n>(y);
+      else *q = make_uint2(pack2(y[0], y[1]), pack2(y[2], y[3]));
     }
   } else {
-    float old[W];
-#pragma unroll
-    for (int i = 0; i < W; ++i)
-      if (A.accumulate && at.has(i)) widen<O>(*reinterpret_cast<const typename Vec<O, 1>::type*>(row + at.at(i)), old + i);
 #pragma unroll
     for (int i = 0; i < W; ++i) {
       if (!at.has(i)) continue;
-      if (A.accumulate) x[i] += old[i];
+      if (A.accumulate) {
+        float o;
+        widen<O>(old.r[i], &o);
+        x[i] += o;
+      }
       *reinterpret_cast<typename Vec<O, 1>::type*>(row + at.at(i)) = narrow<O, 1>(x + i);
     }
   }
 }
 
-// T: type of dy, O: of the table's gradient. A warp: a chunk of the sorted tokens, 32 x W columns, eight rows of dy on their way at a time.
-template <typename T, typename O, int W, bool WIDE>
-__global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArgs A) {
+// T: type of dy, O: of the table's gradient. A warp: a chunk of the sorted tokens, 32 x W columns, `kAhead` rows of dy on their way at a time,
+// with ADD also what the table holds where a row ends.
+template <typename T, typename O, int W, bool WIDE, bool ADD>
+__global__ void __launch_bounds__(256, 3) sum_kernel(const __grid_constant__ SumArgs A) {
+  constexpr int kAhead = ADD ? 4 : 8;
   start_dependents();
   wait_for_previous();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int slices = (A.D + 32 * W - 1) / (32 * W);
   const int64_t unit = (int64_t)blockIdx.x * 8 + warp, chunk = unit / slices;
-  const Columns<W, WIDE> at((int)(unit - chunk * slices), lane, A.D);
+  const int slice = (int)(unit - chunk * slices);
+  const Columns<W, WIDE> at(slice, lane, A.D);
   const int64_t n0 = chunk * A.chunk, n1 = min(n0 + A.chunk, A.N);
   if (n0 >= A.N) return;
   const unsigned none = (unsigned)A.V;
-  unsigned current = __ldg(A.pair + n0).x;
-  bool joined = n0 > 0 && __ldg(A.pair + n0 - 1).x == current;            // the row began in an earlier chunk
-  if (current == none) return;
+  const unsigned front = __ldg(A.pair + n0).x;
+  bool joined = n0 > 0 && __ldg(A.pair + n0 - 1).x == front;             // the row began in an earlier chunk
+  if (front == none) return;
   float acc[W];
 #pragma unroll
   for (int i = 0; i < W; ++i) acc[i] = 0.f;
@@ -344,96 +368,95 @@ __global__ void __launch_bounds__(256) sum_kernel(const __grid_constant__ SumArg
     for (int i = 0; i < W; ++i)
       if (at.has(i)) p[at.at(i)] = acc[i];
   };
-  auto flush = [&]() {
-    if (joined) leave(0);
-    else finish_row<O, W, WIDE>(A, current, at, acc);
-  };
+  bool open = false;                                                     // the last row goes on in the next chunk
   for (int64_t n = n0; n < n1; n += 32) {
     const uint2 pair = n + lane < n1 ? __ldg(A.pair + n + lane) : make_uint2(none, 0);
-    const unsigned key = pair.x, place = pair.y;
-    const int count = __popc(__ballot_sync(0xffffffffu, key != none));     // (what is in no row comes last)
-    for (int i = 0; i < count; i += 8) {
-      Share<T, W, WIDE> r[8];
+    const unsigned key = pair.x, place = pair.y, after = n + lane + 1 < A.N ? __ldg(A.pair + n + lane + 1).x : none;
+    const unsigned some = __ballot_sync(0xffffffffu, key != none), ends = __ballot_sync(0xffffffffu, key != after) & some;
+    const int count = __popc(some);                                      // (what is in no row comes last)
+    for (int i = 0; i < count; i += kAhead) {
+      // Shuffles before the loads: one among them waits for those that are on their way (the hardware has few counters for both), which
+      // took 160 us instead of 60 where a lane's share is four loads.
+      unsigned p[kAhead], k[kAhead];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) r[j].load(static_cast<const T*>(A.dy) + (int64_t)__shfl_sync(0xffffffffu, place, i + j) * A.lddy, at, i + j < count);
+      for (int j = 0; j < kAhead; ++j) {
+        p[j] = __shfl_sync(0xffffffffu, place, i + j);
+        k[j] = __shfl_sync(0xffffffffu, key, i + j);
+      }
+      Share<T, W, WIDE> r[kAhead];
+      Row<O, W, WIDE> old[ADD ? kAhead : 1];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const unsigned k = __shfl_sync(0xffffffffu, key, i + j);
-        if (i + j < count) {
-          if (k != current) {
-            flush();
-            current = k;
-            joined = false;
+      for (int j = 0; j < kAhead; ++j) r[j].load(static_cast<const T*>(A.dy) + (int64_t)p[j] * A.lddy, at, i + j < count);
+      if constexpr (ADD) {
 #pragma unroll
-            for (int q = 0; q < W; ++q) acc[q] = 0.f;
-          }
-          r[j].add_to(acc);
+        for (int j = 0; j < kAhead; ++j) old[j].load(static_cast<const O*>(A.out) + (int64_t)k[j] * A.ldout, at, ends >> (i + j) & 1);
+      }
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        if (i + j >= count) continue;
+        r[j].add_to(acc);
+        open = true;
+        if (ends >> (i + j) & 1) {
+          if (joined) leave(0);
+          else finish_row<O, W, WIDE>(A, k[j], at, acc, old[ADD ? j : 0]);
+          joined = open = false;
+#pragma unroll
+          for (int q = 0; q < W; ++q) acc[q] = 0.f;
         }
       }
     }
     if (count < 32) break;
   }
-  if (n1 < A.N && __ldg(A.pair + n1).x == current) leave(joined ? 0 : 1);     // it goes on in the next chunk
-  else flush();
+  if (!open) return;
+  leave(joined ? 0 : 1);
+  if (!joined && slice == 0 && lane == 0) A.crossing[1 + atomicAdd(A.crossing, 1u)] = (unsigned)chunk;
 }
 
-// The rows that reach over chunks. A CTA looks at eight chunks and takes those in which a row begins that goes on; 128 columns of it, its
-// eight warps the chunks behind in turn.
+// The rows that reach over chunks, by the chunk in which they begin: a CTA takes 128 columns of one at a time, its eight warps the chunks
+// behind in turn.
 template <typename O>
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ SumArgs A) {
   __shared__ float sh[8][4][32];
-  __shared__ unsigned rows[8];
   start_dependents();
   wait_for_previous();
   const int64_t chunks = (A.N + A.chunk - 1) / A.chunk;
-  if (threadIdx.x < 8) {
-    const int64_t n0 = ((int64_t)blockIdx.x * 8 + threadIdx.x) * A.chunk, n1 = n0 + A.chunk;
-    unsigned k = (unsigned)A.V;
-    if (n1 < A.N) {
-      k = __ldg(A.pair + n1).x;
-      const unsigned last = __ldg(A.pair + n1 - 1).x, front = __ldg(A.pair + n0).x, ahead = n0 > 0 ? __ldg(A.pair + n0 - 1).x : ~k;
-      if (last != k || (front == k && ahead == k)) k = (unsigned)A.V;       // nothing goes on here, or it began earlier
-    }
-    rows[threadIdx.x] = k;
-  }
-  __syncthreads();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  for (int r = 0; r < 8; ++r) {
-    const unsigned k = rows[r];
-    if (k == (unsigned)A.V) continue;
-    const int64_t chunk = (int64_t)blockIdx.x * 8 + r;
-    for (int slice = blockIdx.y; slice * 128 < A.D; slice += gridDim.y) {
-      const Columns<4, false> at(slice, lane, A.D);
-      float s[4] = {0.f, 0.f, 0.f, 0.f};
-      for (int64_t j = chunk + 1 + warp; j < chunks; j += 32) {
-        float x[4][4];
-        bool on[4];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slices = (A.D + 127) / 128;
+  const int64_t units = (int64_t)*A.crossing * slices;
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int64_t chunk = A.crossing[1 + unit / slices];
+    const unsigned k = __ldg(A.pair + (chunk + 1) * A.chunk).x;
+    const Columns<4, false> at((int)(unit % slices), lane, A.D);
+    Row<O, 4, false> old;
+    if (warp == 0) old.load(static_cast<const O*>(A.out) + (int64_t)k * A.ldout, at, A.accumulate);
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int64_t j = chunk + 1 + warp; j < chunks; j += 32) {
+      float x[4][4];
+      bool on[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {                      // (what is read of a chunk that is not in the row is left out)
-          const int64_t q = j + 8 * u;
-          on[u] = q < chunks && __ldg(A.pair + q * A.chunk).x == k;
+      for (int u = 0; u < 4; ++u) {                        // (what is read of a chunk that is not in the row is left out)
+        const int64_t q = j + 8 * u;
+        on[u] = q < chunks && __ldg(A.pair + q * A.chunk).x == k;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[u][i] = q < chunks && at.has(i) ? A.part[q * 2 * A.D + at.at(i)] : 0.f;
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[i] += on[u] ? x[u][i] : 0.f;
-        if (!on[3]) break;
+        for (int i = 0; i < 4; ++i) x[u][i] = q < chunks && at.has(i) ? A.part[q * 2 * A.D + at.at(i)] : 0.f;
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sh[warp][i][lane] = s[i];
-      __syncthreads();
-      if (warp == 0) {
+      for (int u = 0; u < 4; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[i] = at.has(i) ? A.part[(chunk * 2 + 1) * A.D + at.at(i)] : 0.f;
-          for (int w = 0; w < 8; ++w) s[i] += sh[w][i][lane];
-        }
-        finish_row<O, 4, false>(A, k, at, s);
-      }
-      __syncthreads();
+        for (int i = 0; i < 4; ++i) s[i] += on[u] ? x[u][i] : 0.f;
+      if (!on[3]) break;
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sh[warp][i][lane] = s[i];
+    __syncthreads();
+    if (warp == 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s[i] = at.has(i) ? A.part[(chunk * 2 + 1) * A.D + at.at(i)] : 0.f;
+        for (int w = 0; w < 8; ++w) s[i] += sh[w][i][lane];
+      }
+      finish_row<O, 4, false>(A, k, at, s, old);
+    }
+    __syncthreads();
   }
 }
 
@@ -447,14 +470,15 @@ int chunk_of(int64_t N, int64_t D, int W) {
 }
 
 struct BackPlan {
-  int64_t keys, part, total;
+  int64_t keys, part, crossing, total;
 };
 BackPlan back_plan(int64_t N, int64_t D) {
   BackPlan p;
   p.keys = pad256(N * 8);
   const int64_t chunk = chunk_of(N, D, 8), chunk4 = chunk_of(N, D, 4), least = chunk < chunk4 ? chunk : chunk4;
   p.part = pad256((N + least - 1) / least * 2 * D * (int64_t)sizeof(float));
-  p.total = 2 * p.keys + p.part;
+  p.crossing = pad256((1 + (N + least - 1) / least) * 4);
+  p.total = 2 * p.keys + p.part + p.crossing;
   return p;
 }
 
@@ -467,9 +491,13 @@ int sums(SumArgs A, bool wide, cudaStream_t st) {
   const int W = wide ? kW : 4;
   A.chunk = chunk_of(A.N, A.D, W);
   const int64_t chunks = (A.N + A.chunk - 1) / A.chunk, slices = (A.D + 32 * W - 1) / (32 * W), ctas = (chunks * slices + 7) / 8;
-  const int rc = wide ? start(dim3((unsigned)ctas), 256, 1, 0, st, sum_kernel<T, O, kW, true>, A) : start(dim3((unsigned)ctas), 256, 1, 0, st, sum_kernel<T, O, 4, false>, A);
+  const dim3 grid((unsigned)ctas);
+  int rc;
+  if (A.accumulate) rc = wide ? start(grid, 256, 1, 0, st, sum_kernel<T, O, kW, true, true>, A) : start(grid, 256, 1, 0, st, sum_kernel<T, O, 4, false, true>, A);
+  else rc = wide ? start(grid, 256, 1, 0, st, sum_kernel<T, O, kW, true, false>, A) : start(grid, 256, 1, 0, st, sum_kernel<T, O, 4, false, false>, A);
   if (rc != DMX_OK || chunks == 1) return rc;
-  return start(dim3((unsigned)((chunks + 6) / 8), (unsigned)((A.D + 127) / 128 < 8 ? (A.D + 127) / 128 : 8)), 256, 1, 0, st, join_kernel<O>, A);
+  const int64_t most = (chunks - 1) * ((A.D + 127) / 128);
+  return start(dim3((unsigned)(most < 148 * 4 ? most : 148 * 4)), 256, 1, 0, st, join_kernel<O>, A);
 }
 
 }  // namespace
@@ -513,6 +541,7 @@ int dmx_embedding_backward(int64_t N, int64_t V, int64_t D, int id_bytes, const 
   S.ids = ids; S.wide_ids = id_bytes == 8; S.N = N; S.V = V;
   for (S.passes = 1; (uint64_t)V >> (8 * S.passes); ++S.passes) {}
   for (int i = 0; i < 2; ++i) S.pair[i] = reinterpret_cast<uint2*>(ws + i * p.keys);
+  S.crossing = reinterpret_cast<unsigned*>(ws + 2 * p.keys + p.part);
   if (!accumulate) { S.zero = dtable; S.zero_ld = (V > 1 ? ldt : D) * eo; S.zero_bytes = D * eo; }
   constexpr int kShared = kSortWarps * kDigits * 4;       // 32 KB
   const int rc = start(dim3(accumulate ? kSortCtas : 144), kSortThreads, 1, kShared, st, sort_kernel, S);
@@ -520,7 +549,7 @@ int dmx_embedding_backward(int64_t N, int64_t V, int64_t D, int id_bytes, const 
   // 16-byte accesses of dy, and as many elements of the table's rows: 8 to 32 bytes
   const int W = 16 / e;
   const bool wide = wide_rows(dy, N, lddy, D, dtype) && aligned(dtable, W * eo < 16 ? W * eo : 16) && (V <= 1 || ldt % (W * eo < 16 ? W : 16 / (int)eo) == 0);
-  SumArgs A = {S.pair[0], dy, dtable, reinterpret_cast<float*>(ws + 2 * p.keys), N, V, N > 1 ? lddy : D, V > 1 ? ldt : D, (int)D, 0, accumulate != 0, scale};
+  SumArgs A = {S.pair[0], dy, dtable, S.crossing, reinterpret_cast<float*>(ws + 2 * p.keys), N, V, N > 1 ? lddy : D, V > 1 ? ldt : D, (int)D, 0, accumulate != 0, scale};
   if (dtype == DMX_F32) return out_dtype == DMX_F32 ? sums<float, float>(A, wide, st) : sums<float, bf16>(A, wide, st);
   return out_dtype == DMX_F32 ? sums<bf16, float>(A, wide, st) : sums<bf16, bf16>(A, wide, st);
 }

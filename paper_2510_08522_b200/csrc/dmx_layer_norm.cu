@@ -21,9 +21,11 @@ using namespace dmx_rows;
 using namespace dmx_f32x2;
 
 constexpr int kMaxCluster = 8, kMaxWarps = 8;      // of a CTA that is one team
-// Rows on their way to a team: what fills the 40 KB that an SM has to have on its way, and leaves room for two CTAs
-constexpr int kForwardStages = 4;
-template <typename T> constexpr int kBackwardStages = sizeof(T) == 2 ? 4 : 2;
+// Rows on their way to a team: with the warps there are, more than the 40 KB that an SM has to have on its way
+constexpr int kForwardStages = 4, kBackwardStages = 2;
+// CTAs on an SM, for their registers (a thread of backward holds its sums, 2 N, and a row's values, 2 N)
+constexpr int forward_ctas(int values, bool wide) { return values == 32 ? 3 + wide : values == 16 ? 4 + wide : 6; }
+constexpr int backward_ctas(int values, int bytes) { return values == 32 ? (bytes == 2 ? 3 : 2) : values == 16 ? 4 : 6; }
 
 struct Args {
   const void *x, *dy, *add;
@@ -36,70 +38,103 @@ struct Args {
   float eps;
 };
 
-// How a row is held. TEAM: lanes of a warp that share a row, 0 a CTA, -1 a cluster. N values per thread in accesses of V.
+// How a row is held. TEAM: lanes of a warp that share a row, 0 a CTA, -1 a cluster. N values per thread, in accesses of V neighbours: 16 bytes,
+// or single elements where alignment allows no more. Rows to come are copied 16 bytes at a time in either case: with single elements a
+// team's threads copy what covers the row from one 16-byte border to the next (the bytes before its start lie in the same 16, and are not used).
 template <typename T, int V, int TEAM, int N>
 struct Held {
   static constexpr int kAccesses = N / V, kThreads = TEAM > 0 ? 128 : 256;
-  static constexpr bool kAhead = V * sizeof(T) >= 4;       // asynchronous copies take 4 bytes at least
+  static constexpr int kForwardCtas = TEAM > 0 ? forward_ctas(N, V > 1) : 2, kBackwardCtas = TEAM > 0 ? backward_ctas(N, sizeof(T)) : 1;
   typedef typename Vec<T, V>::type Raw;
 
-  // this thread's place in its team, the team's size, its row and the rows between its rows
-  static __device__ __forceinline__ void place(int& t, int& size, int64_t& row, int64_t& step) {
+  int t, size;          // access i has the columns from (i * size + t) * V on
+  int own, first, D;    // this thread among its team's in this CTA; this CTA's first column
+  int threads;          // of the team in this CTA
+  int64_t row, step, group;      // the team's first row, the rows between its rows; the CTA (or cluster)
+
+  __device__ __forceinline__ explicit Held(int D_) : D(D_) {
+    first = 0;
     if constexpr (TEAM > 0) {
       const int teams = blockDim.x / TEAM;
-      t = threadIdx.x % TEAM; size = TEAM;
-      row = (int64_t)blockIdx.x * teams + threadIdx.x / TEAM; step = (int64_t)gridDim.x * teams;
-    } else if constexpr (TEAM == 0) {
-      t = threadIdx.x; size = blockDim.x;
-      row = blockIdx.x; step = gridDim.x;
+      own = threadIdx.x % TEAM; threads = size = TEAM;
+      group = blockIdx.x;
+      row = group * teams + threadIdx.x / TEAM; step = (int64_t)gridDim.x * teams;
+      t = own;
     } else {
-      unsigned rank, n;
-      asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-      asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
-      t = rank * blockDim.x + threadIdx.x; size = n * blockDim.x;
-      row = blockIdx.x / n; step = gridDim.x / n;
+      unsigned rank = 0, n = 1;
+      if constexpr (TEAM < 0) {
+        asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+        asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(n));
+      }
+      own = threadIdx.x; threads = blockDim.x;
+      row = group = blockIdx.x / n; step = gridDim.x / n;
+      if constexpr (V > 1) { t = rank * blockDim.x + own; size = n * blockDim.x; }          // all CTAs' accesses in turn
+      else { first = rank * N * blockDim.x; t = first + own; size = blockDim.x; }           // each CTA a range
     }
   }
-  // A row's values on their way to this thread's slots (kAccesses of them, blockDim.x apart), zeros behind its end
-  static __device__ __forceinline__ void send(Raw* slots, const void* p, int64_t ld, int64_t row, int t, int size, int D) {
-    const T* q = static_cast<const T*>(p) + row * ld;
+  __device__ __forceinline__ int column(int i) const { return (i * size + t) * V; }
+  // bytes that one row of one input takes in a stage, of all teams of the CTA
+  static __host__ __device__ constexpr int stage_bytes(int ctaThreads) { return ctaThreads * N * (int)sizeof(T) + (V > 1 ? 0 : 32 * (TEAM > 0 ? ctaThreads / (TEAM > 0 ? TEAM : 1) : 1)); }
+  // where this thread (V > 1) or its team (V = 1) finds its part of a stage
+  __device__ __forceinline__ unsigned char* slot(unsigned char* stage) const {
+    if constexpr (V > 1) return stage + threadIdx.x * sizeof(Raw);
+    else return stage + threadIdx.x / threads * (threads * N * (int)sizeof(T) + 32);
+  }
+  __device__ __forceinline__ void send(unsigned char* to, const void* p, int64_t ld, int64_t r) const {
+    const unsigned dst = (unsigned)__cvta_generic_to_shared(to);
+    if constexpr (V > 1) {
+      const T* q = static_cast<const T*>(p) + r * ld + t * V;
+      const unsigned apart = blockDim.x * sizeof(Raw);
+      if (D == N * size) {
 #pragma unroll
-    for (int i = 0; i < kAccesses; ++i) {
-      const int c = (i * size + t) * V, bytes = c < D ? (int)sizeof(Raw) : 0;
-      const unsigned to = (unsigned)__cvta_generic_to_shared(slots + i * blockDim.x);
-      if constexpr (sizeof(Raw) == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(c < D ? q + c : q), "r"(bytes) : "memory");
-      else asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(c < D ? q + c : q), "r"(bytes) : "memory");
+        for (int i = 0; i < kAccesses; ++i) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + i * apart), "l"(q + i * size * V) : "memory");
+      } else {
+#pragma unroll
+        for (int i = 0; i < kAccesses; ++i) {
+          const bool in = column(i) < D;                   // behind the row's end: zeros
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + i * apart), "l"(in ? q + i * size * V : static_cast<const T*>(p)), "r"(in ? 16 : 0) : "memory");
+        }
+      }
+    } else {
+      const T* q = static_cast<const T*>(p) + r * ld + first;
+      const int count = min(D - first, N * threads), shift = (int)(reinterpret_cast<uintptr_t>(q) & 15);
+      const unsigned char* from = reinterpret_cast<const unsigned char*>(q) - shift;
+      const int bytes = count > 0 ? shift + count * (int)sizeof(T) : 0;
+#pragma unroll
+      for (int i = 0; i <= N * (int)sizeof(T) / 16; ++i) {
+        const int at = (i * threads + own) * 16;
+        if (at < bytes) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + at), "l"(from + at), "r"(min(16, bytes - at)) : "memory");
+      }
     }
   }
-  static __device__ __forceinline__ void take(const Raw* slots, float (&x)[N]) {
-#pragma unroll
-    for (int i = 0; i < kAccesses; ++i) widen<T>(slots[i * blockDim.x], x + i * V);
-  }
-  static __device__ __forceinline__ void load(const void* p, int64_t ld, int64_t row, int t, int size, int D, float (&x)[N]) {
-    const T* q = static_cast<const T*>(p) + row * ld;
-    Raw r[kAccesses];
-#pragma unroll
-    for (int i = 0; i < kAccesses; ++i) {
-      const int c = (i * size + t) * V;
-      r[i] = Raw{};
-      if (c < D) r[i] = *reinterpret_cast<const Raw*>(q + c);
+  // (With single elements they come from other threads' copies: the team meets before it takes them.)
+  static __device__ __forceinline__ void meet() {
+    if constexpr (V == 1) {
+      if constexpr (TEAM > 0) __syncwarp();
+      else __syncthreads();
     }
-#pragma unroll
-    for (int i = 0; i < kAccesses; ++i) widen<T>(r[i], x + i * V);
   }
-  static __device__ __forceinline__ void store(void* p, int64_t ld, int64_t row, int t, int size, int D, const float (&x)[N]) {
-    T* q = static_cast<T*>(p) + row * ld;
-#pragma unroll
-    for (int i = 0; i < kAccesses; ++i) {
-      const int c = (i * size + t) * V;
-      if (c < D) *reinterpret_cast<Raw*>(q + c) = narrow<T, V>(x + i * V);
+  // access i of row r out of the slot
+  __device__ __forceinline__ void take(int i, const unsigned char* slot, const void* p, int64_t ld, int64_t r, float* x) const {
+    if constexpr (V > 1) {
+      widen<T>(*reinterpret_cast<const Raw*>(slot + i * blockDim.x * sizeof(Raw)), x);
+    } else {
+      const int shift = (int)(reinterpret_cast<uintptr_t>(static_cast<const T*>(p) + r * ld + first) & 15);
+      x[0] = 0.f;
+      if (column(i) < D) widen<T>(*reinterpret_cast<const Raw*>(slot + shift + (i * threads + own) * sizeof(T)), x);
     }
+  }
+  __device__ __forceinline__ void store(void* p, int64_t ld, int64_t r, const float (&x)[N]) const {
+    T* q = static_cast<T*>(p) + r * ld;
+#pragma unroll
+    for (int i = 0; i < kAccesses; ++i)
+      if (column(i) < D) *reinterpret_cast<Raw*>(q + column(i)) = narrow<T, V>(x + i * V);
   }
   // an fp32 vector's values at this thread's columns; `otherwise` where there is no vector
-  static __device__ __forceinline__ void vector(const float* w, int wvec, float otherwise, int t, int size, int D, float (&x)[N]) {
+  __device__ __forceinline__ void vector(const float* w, int wvec, float otherwise, float (&x)[N]) const {
 #pragma unroll
     for (int i = 0; i < kAccesses; ++i) {
-      const int c = (i * size + t) * V;
+      const int c = column(i);
       if (V > 1 && w && wvec) {
 #pragma unroll
         for (int k = 0; k < V; k += 4) {
@@ -112,13 +147,32 @@ struct Held {
       }
     }
   }
+  // The vector in shared memory, [N / 4][threads] float4 or [N][threads] floats: a thread reads what it (and others alike) wrote.
+  __device__ __forceinline__ void keep(float* held, const float (&x)[N]) const {
+#pragma unroll
+    for (int j = 0; j < N; j += V > 1 ? 4 : 1) {
+      if constexpr (V > 1) reinterpret_cast<float4*>(held)[j / 4 * threads + own] = make_float4(x[j], x[(j + 1) % N], x[(j + 2) % N], x[(j + 3) % N]);
+      else held[j * threads + own] = x[j];
+    }
+  }
+  __device__ __forceinline__ void kept(const float* held, int i, float (&x)[V]) const {
+    if constexpr (V > 1) {
+#pragma unroll
+      for (int k = 0; k < V; k += 4) {
+        const float4 v = reinterpret_cast<const float4*>(held)[(i * V + k) / 4 * threads + own];
+        x[k] = v.x; x[(k + 1) % V] = v.y; x[(k + 2) % V] = v.z; x[(k + 3) % V] = v.w;
+      }
+    } else {
+      x[0] = held[i * threads + own];
+    }
+  }
   // zeros behind the row's end
-  static __device__ __forceinline__ void cut(int t, int size, int D, float (&x)[N]) {
+  __device__ __forceinline__ void cut(float (&x)[N]) const {
 #pragma unroll
     for (int i = 0; i < kAccesses; ++i) {
-      if ((i + 1) * size * V <= D) continue;               // (the same for all)
+      if (first + (i + 1) * size * V <= D) continue;       // (the same for all)
 #pragma unroll
-      for (int k = 0; k < V; ++k) x[i * V + k] = (i * size + t) * V < D ? x[i * V + k] : 0.f;
+      for (int k = 0; k < V; ++k) x[i * V + k] = column(i) < D ? x[i * V + k] : 0.f;
     }
   }
 };
@@ -165,146 +219,165 @@ __device__ __forceinline__ float2 team_sum(float2 v, float2 (*red)[kMaxCluster *
   return v;
 }
 
-// (A warp's lanes stay together: those of a team without a row left take the last one again and store nothing.)
+template <int TEAM>
+__device__ __forceinline__ float team_sum(float v, float2 (*red)[kMaxCluster * kMaxWarps], int& turn) {
+  if constexpr (TEAM > 0) {
+#pragma unroll
+    for (int o = TEAM / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+  }
+  return team_sum<TEAM>(make_float2(v, 0.f), red, turn).x;
+}
+
+// (A warp's lanes stay together: those of a team without a row left take part in its sums and store nothing.)
 template <typename T, int V, int TEAM, int N>
-__global__ void __launch_bounds__(Held<T, V, TEAM, N>::kThreads) forward_kernel(const __grid_constant__ Args A) {
-  typedef Held<T, V, TEAM, N> H;
+__global__ void __launch_bounds__(Held<T, V, TEAM, N>::kThreads, Held<T, V, TEAM, N>::kForwardCtas) forward_kernel(const __grid_constant__ Args A) {
   extern __shared__ __align__(16) unsigned char raw[];
   __shared__ float2 red[2][kMaxCluster * kMaxWarps];
-  typename H::Raw* slots = reinterpret_cast<typename H::Raw*>(raw) + threadIdx.x;
-  const int stage = H::kAccesses * blockDim.x;             // slots from stage to stage
-  int t, size, turn = 0;
-  int64_t row, step;
-  H::place(t, size, row, step);
+  typedef Held<T, V, TEAM, N> H;
+  const H held(A.D);
+  const int stage = H::stage_bytes(blockDim.x);
+  unsigned char* slot = held.slot(raw);
+  int turn = 0;
+  int64_t row = held.row;
   start_dependents();
   if constexpr (TEAM < 0) asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");   // all of it is there
   wait_for_previous();
   auto send = [&](int s, int64_t r) {
-    if constexpr (H::kAhead) {
-      if (r < A.M) H::send(slots + s * stage, A.x, A.ldx, r, t, size, A.D);
-      copies_sent();
-    }
+    if (r < A.M) held.send(slot + s * stage, A.x, A.ldx, r);
+    copies_sent();
   };
 #pragma unroll
-  for (int s = 0; s < kForwardStages; ++s) send(s, row + s * step);
+  for (int s = 0; s < kForwardStages; ++s) send(s, row + s * held.step);
   float w[N], b[N];
-  H::vector(A.weight, A.wvec, 1.f, t, size, A.D, w);
-  H::vector(A.bias, A.wvec, 0.f, t, size, A.D, b);
+  held.vector(A.weight, A.wvec, 1.f, w);
+  held.vector(A.bias, A.wvec, 0.f, b);
   const float per = 1.f / (float)A.D;
   int s = 0;
-  for (int64_t base = row - (TEAM > 0 ? threadIdx.x % 32 / (TEAM > 0 ? TEAM : 1) : 0); base < A.M; base += step, row += step) {
-    const bool live = row < A.M;
+  for (int64_t base = row - (TEAM > 0 ? threadIdx.x % 32 / (TEAM > 0 ? TEAM : 1) : 0); base < A.M; base += held.step, row += held.step) {
+    const bool live = TEAM != 8 || row < A.M;
     float x[N];
-    if constexpr (H::kAhead) {
-      copies_landed<kForwardStages - 1>();
-      H::take(slots + s * stage, x);
-    } else {
-      H::load(A.x, A.ldx, live ? row : A.M - 1, t, size, A.D, x);
-    }
+    copies_landed<kForwardStages - 1>();
+    H::meet();
+#pragma unroll
+    for (int i = 0; i < H::kAccesses; ++i) held.take(i, slot + s * stage, A.x, A.ldx, row, x + i * V);
     float2 a = make_float2(0.f, 0.f);
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) a = add2(a, pair(x, i));
-    const float rough = team_sum<TEAM>(make_float2(a.x + a.y, 0.f), red, turn).x * per;
-    send(s, row + kForwardStages * step);                  // (its values are in registers by now)
+    const float rough = team_sum<TEAM>(a.x + a.y, red, turn) * per;
+    send(s, row + kForwardStages * held.step);             // (its values are in registers by now, the whole team's)
     if (++s == kForwardStages) s = 0;
     float2 q = make_float2(0.f, 0.f);
     a = q;
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) set_pair(x, i, add2(pair(x, i), two(-rough)));
-    H::cut(t, size, A.D, x);
+    held.cut(x);
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) { a = add2(a, pair(x, i)); q = fma2(pair(x, i), pair(x, i), q); }
     const float2 sum = team_sum<TEAM>(make_float2(a.x + a.y, q.x + q.y), red, turn);
-    const float off = sum.x * per, var = fmaf(-off, off, sum.y * per), rstd = __frsqrt_rn((var < 0.f ? 0.f : var) + A.eps);   // (a NaN stays)
+    const float off = sum.x * per, var = fmaf(-off, off, sum.y * per), rstd = rsqrtf((var < 0.f ? 0.f : var) + A.eps);   // (a NaN stays)
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i) set_pair(x, i, fma2(mul2(add2(pair(x, i), two(-off)), two(rstd)), pair(w, i), pair(b, i)));
+    for (int i = 0; i < N / 2; ++i) set_pair(x, i, fma2(fma2(pair(x, i), two(rstd), two(-off * rstd)), pair(w, i), pair(b, i)));
     if (!live) continue;
-    H::store(A.out, A.ldout, row, t, size, A.D, x);
-    if (t == 0) { A.mean[row] = rough + off; A.rstd[row] = rstd; }
+    held.store(A.out, A.ldout, row, x);
+    if (held.t == 0) { A.mean[row] = rough + off; A.rstd[row] = rstd; }
   }
-  if constexpr (H::kAhead) copies_landed<0>();
+  copies_landed<0>();
 }
 
 template <typename T, int V, int TEAM, int N>
-__global__ void __launch_bounds__(Held<T, V, TEAM, N>::kThreads) backward_kernel(const __grid_constant__ Args A) {
-  typedef Held<T, V, TEAM, N> H;
-  constexpr int kStages = kBackwardStages<T>;
-  extern __shared__ __align__(16) unsigned char raw[];
+__global__ void __launch_bounds__(Held<T, V, TEAM, N>::kThreads, Held<T, V, TEAM, N>::kBackwardCtas) backward_kernel(const __grid_constant__ Args A) {
+  constexpr int kStages = kBackwardStages;
+  extern __shared__ __align__(16) unsigned char raw[];     // weights, then the stages
   __shared__ float2 red[2][kMaxCluster * kMaxWarps];
-  typename H::Raw* slots = reinterpret_cast<typename H::Raw*>(raw) + threadIdx.x;
-  const int part = H::kAccesses * blockDim.x, stage = part * (A.add ? 3 : 2);      // slots from input to input, from stage to stage
-  int t, size, turn = 0;
-  int64_t row, step;
-  H::place(t, size, row, step);
+  typedef Held<T, V, TEAM, N> H;
+  const H held(A.D);
+  const int part = H::stage_bytes(blockDim.x), stage = part * (A.add ? 3 : 2);      // from input to input, from stage to stage
+  float* weights = reinterpret_cast<float*>(raw);
+  unsigned char* slot = held.slot(raw + held.threads * N * sizeof(float));
+  int turn = 0;
+  int64_t row = held.row;
   start_dependents();
   if constexpr (TEAM < 0) asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
   wait_for_previous();
   auto send = [&](int s, int64_t r) {
-    if constexpr (H::kAhead) {
-      if (r < A.M) {
-        H::send(slots + s * stage, A.x, A.ldx, r, t, size, A.D);
-        H::send(slots + s * stage + part, A.dy, A.lddy, r, t, size, A.D);
-        if (A.add) H::send(slots + s * stage + 2 * part, A.add, A.ldadd, r, t, size, A.D);
-      }
-      copies_sent();
+    if (r < A.M) {
+      held.send(slot + s * stage, A.x, A.ldx, r);
+      held.send(slot + s * stage + part, A.dy, A.lddy, r);
+      if (A.add) held.send(slot + s * stage + 2 * part, A.add, A.ldadd, r);
     }
+    copies_sent();
   };
 #pragma unroll
-  for (int s = 0; s < kStages; ++s) send(s, row + s * step);
+  for (int s = 0; s < kStages; ++s) send(s, row + s * held.step);
   const float per = 1.f / (float)A.D;
   float dw[N], db[N];
+  held.vector(A.weight, A.wvec, 1.f, dw);
+  held.keep(weights, dw);
 #pragma unroll
   for (int i = 0; i < N; ++i) dw[i] = db[i] = 0.f;
   float next_mean = 0.f, next_rstd = 0.f;
   if (row < A.M) { next_mean = A.mean[row]; next_rstd = A.rstd[row]; }
   int s = 0;
-  for (int64_t base = row - (TEAM > 0 ? threadIdx.x % 32 / (TEAM > 0 ? TEAM : 1) : 0); base < A.M; base += step, row += step) {
-    const bool live = row < A.M;
+  for (int64_t base = row - (TEAM > 0 ? threadIdx.x % 32 / (TEAM > 0 ? TEAM : 1) : 0); base < A.M; base += held.step, row += held.step) {
+    const bool live = TEAM != 8 || row < A.M;
     const float mean = next_mean, rstd = next_rstd;
-    if (row + step < A.M) { next_mean = A.mean[row + step]; next_rstd = A.rstd[row + step]; }
-    float h[N], g[N], w[N];
-    H::vector(A.weight, A.wvec, 1.f, t, size, A.D, w);
-    if constexpr (H::kAhead) {
-      copies_landed<kStages - 1>();
-      H::take(slots + s * stage, h);
-      H::take(slots + s * stage + part, g);
-    } else {
-      H::load(A.x, A.ldx, live ? row : A.M - 1, t, size, A.D, h);
-      H::load(A.dy, A.lddy, live ? row : A.M - 1, t, size, A.D, g);
-    }
+    if (row + held.step < A.M) { next_mean = A.mean[row + held.step]; next_rstd = A.rstd[row + held.step]; }
+    float h[N], g[N];
+    const unsigned char* from = slot + s * stage;
+    copies_landed<kStages - 1>();
+    H::meet();
     float2 a = make_float2(0.f, 0.f), q = a;
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i) {                      // (behind the row's end dy is 0)
-      const float2 u = mul2(add2(pair(h, i), two(-mean)), two(rstd)), v = pair(g, i), x = mul2(v, pair(w, i));
-      if (live) {
-        set_pair(dw, i, fma2(v, u, pair(dw, i)));
-        set_pair(db, i, add2(pair(db, i), v));
-      }
-      a = add2(a, x);
-      q = fma2(x, u, q);
-      set_pair(h, i, u);
-      set_pair(g, i, x);
-    }
-    float2 sum = team_sum<TEAM>(make_float2(a.x + a.y, q.x + q.y), red, turn);
-    sum.x *= per; sum.y *= per;
+    for (int i = 0; i < H::kAccesses; ++i) {               // (behind the row's end dy is 0)
+      float w[V];
+      held.kept(weights, i, w);
+      held.take(i, from, A.x, A.ldx, row, h + i * V);
+      held.take(i, from + part, A.dy, A.lddy, row, g + i * V);
+      if constexpr (V > 1) {
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i) set_pair(g, i, mul2(sub2(pair(g, i), fma2(pair(h, i), two(sum.y), two(sum.x))), two(rstd)));
+        for (int j = 0; j < V / 2; ++j) {
+          const int k = i * V / 2 + j;
+          const float2 u = mul2(add2(pair(h, k), two(-mean)), two(rstd)), v = pair(g, k), x = mul2(v, pair(w, j));
+          if (live) {
+            set_pair(dw, k, fma2(v, u, pair(dw, k)));
+            set_pair(db, k, add2(pair(db, k), v));
+          }
+          a = add2(a, x);
+          q = fma2(x, u, q);
+          set_pair(h, k, u);
+          set_pair(g, k, x);
+        }
+      } else {
+        const float u = (h[i] - mean) * rstd, v = g[i], x = v * w[0];
+        if (live) { dw[i] = fmaf(v, u, dw[i]); db[i] += v; }
+        a.x += x;
+        q.x = fmaf(x, u, q.x);
+        h[i] = u;
+        g[i] = x;
+      }
+    }
+    const float2 sum = team_sum<TEAM>(make_float2(a.x + a.y, q.x + q.y), red, turn);
+    const float c1 = -sum.x * per * rstd, c2 = -sum.y * per * rstd;
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) set_pair(g, i, fma2(pair(g, i), two(rstd), fma2(pair(h, i), two(c2), two(c1))));
     if (A.add) {
-      if constexpr (H::kAhead) H::take(slots + s * stage + 2 * part, h);
-      else H::load(A.add, A.ldadd, live ? row : A.M - 1, t, size, A.D, h);
+#pragma unroll
+      for (int i = 0; i < H::kAccesses; ++i) held.take(i, from + 2 * part, A.add, A.ldadd, row, h + i * V);
 #pragma unroll
       for (int i = 0; i < N / 2; ++i) set_pair(g, i, add2(pair(g, i), pair(h, i)));
+      if constexpr (V == 1) H::meet();                     // the whole team has its values
     }
-    if (live) H::store(A.out, A.ldout, row, t, size, A.D, g);
-    send(s, row + kStages * step);                         // (its values have been used)
+    if (live) held.store(A.out, A.ldout, row, g);
+    send(s, row + kStages * held.step);
     if (++s == kStages) s = 0;
   }
-  if constexpr (H::kAhead) copies_landed<0>();
+  copies_landed<0>();
   if (!A.part) return;
-  float* part_of = A.part + (TEAM < 0 ? (int64_t)(blockIdx.x / (size / blockDim.x)) : (int64_t)blockIdx.x) * 2 * A.D;
+  float* part_of = A.part + held.group * 2 * A.D;
   if constexpr (TEAM > 0) {
     // the lanes of a warp that hold the same columns, then the warps
-    __syncthreads();                                       // the slots are free
+    __syncthreads();                                       // the stages are free
     float* joined = reinterpret_cast<float*>(raw);         // [warps][2][N][32]
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
@@ -326,7 +399,7 @@ __global__ void __launch_bounds__(Held<T, V, TEAM, N>::kThreads) backward_kernel
     const int warps = blockDim.x >> 5;
     for (int j = threadIdx.x; j < 2 * N * 32; j += blockDim.x) {
       const int l = j & 31, i = (j >> 5) % N, which = (j >> 5) / N;
-      const int c = (i / V * size + l) * V + i % V;
+      const int c = (i / V * TEAM + l) * V + i % V;
       if (l >= TEAM || c >= A.D) continue;
       float v = 0.f;
       for (int k = 0; k < warps; ++k) v += joined[((k * 2 + which) * N + i) * 32 + l];
@@ -335,7 +408,7 @@ __global__ void __launch_bounds__(Held<T, V, TEAM, N>::kThreads) backward_kernel
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int c = (i / V * size + t) * V + i % V;
+      const int c = held.column(i / V) + i % V;
       if (c < A.D) { part_of[c] = dw[i]; part_of[(int64_t)A.D + c] = db[i]; }
     }
   }
@@ -370,7 +443,7 @@ struct Plan {
   int team, values, threads, cluster;
   int64_t groups;            // CTAs, or clusters of them
 };
-Plan plan_of(int64_t M, int D, int backward) {
+Plan plan_of(int64_t M, int D, int dtype, int backward, bool wide) {      // (backward's does not go by `wide`: its workspace is asked for without)
   Plan p = {};
   p.cluster = 1;
   p.threads = 128;
@@ -381,9 +454,13 @@ Plan plan_of(int64_t M, int D, int backward) {
     const int share = (D + p.cluster - 1) / p.cluster;
     p.threads = ((share + 31) / 32 + 31) / 32 * 32;
   }
-  // CTAs on an SM: two in backward with 32 values a thread (its registers), more where a thread holds less
-  const int rows = p.team > 0 ? 128 / p.team : 1, at_once = p.team <= 0 ? (backward ? 256 : 512) / p.threads : p.values == 32 ? (backward ? 2 : 4) : p.values == 16 ? 4 : 6;
-  const int64_t want = (M + rows - 1) / rows, most = 148 * (at_once > 0 ? at_once : 1) / p.cluster;
+  const int bytes = element_size(dtype), values = p.threads * p.values;              // a CTA's of one input
+  const int slots = backward ? kBackwardStages * 3 * values * bytes + 4 * (p.team > 0 ? p.team * p.values : values) : kForwardStages * values * bytes;
+  int at_once = p.team > 0 ? (backward ? backward_ctas(p.values, bytes) : forward_ctas(p.values, wide)) : (backward ? 256 : 512) / p.threads;
+  const int fit = 224 * 1024 / (slots + 2048);
+  at_once = fit < 1 ? 1 : at_once > fit ? fit : at_once;
+  const int rows = p.team > 0 ? 128 / p.team : 1;
+  const int64_t want = (M + rows - 1) / rows, most = 148 * at_once / p.cluster;
   p.groups = want < most ? want : most;
   return p;
 }
@@ -391,15 +468,15 @@ Plan plan_of(int64_t M, int D, int backward) {
 template <typename T, int V, int TEAM, int N>
 int launch(const Args& A, const Plan& p, int backward, cudaStream_t st) {
   const dim3 grid((unsigned)(p.groups * p.cluster));
-  const int input = p.threads * N * (int)sizeof(T);       // a CTA's rows of one input
-  int shared = !Held<T, V, TEAM, N>::kAhead ? 0 : backward ? kBackwardStages<T> * (A.add ? 3 : 2) * input : kForwardStages * input;
+  typedef Held<T, V, TEAM, N> H;
+  int shared = backward ? kBackwardStages * (A.add ? 3 : 2) * H::stage_bytes(p.threads) + 4 * N * (TEAM > 0 ? TEAM : p.threads) : kForwardStages * H::stage_bytes(p.threads);
   if (backward && TEAM > 0 && shared < 4 * 2 * N * 32 * 4) shared = 4 * 2 * N * 32 * 4;        // the warps' sums
   static std::atomic<uint64_t> set[2];                    // devices on which the kernel may use that much
   int device = 0;
   if (!dmxh::cuda_ok(cudaGetDevice(&device))) return DMX_ERR_CUDA;
   const uint64_t bit = (uint64_t)1 << (device & 63);
   if (!(set[backward].load(std::memory_order_relaxed) & bit) || device > 63) {
-    constexpr int kMost = 200 * 1024;
+    constexpr int kMost = 225 * 1024;
     const auto f = backward ? cudaFuncSetAttribute(backward_kernel<T, V, TEAM, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost)
                             : cudaFuncSetAttribute(forward_kernel<T, V, TEAM, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
     if (!dmxh::cuda_ok(f)) return DMX_ERR_CUDA;
@@ -428,7 +505,7 @@ extern "C" {
 
 int64_t dmx_layer_norm_workspace(int64_t M, int D, int dtype) {
   if (!shape_ok(M, D, dtype)) return DMX_ERR_ARG;
-  return M == 0 ? 0 : pad256(plan_of(M, D, 1).groups * 2 * D * (int64_t)sizeof(float));
+  return M == 0 ? 0 : pad256(plan_of(M, D, dtype, 1, true).groups * 2 * D * (int64_t)sizeof(float));
 }
 
 int dmx_layer_norm_forward(int64_t M, int D, int dtype, const void* x, int64_t ldx, const float* weight, const float* bias, float eps, void* y,
@@ -442,7 +519,8 @@ int dmx_layer_norm_forward(int64_t M, int D, int dtype, const void* x, int64_t l
   A.x = x; A.out = y; A.ldx = M > 1 ? ldx : D; A.ldout = M > 1 ? ldy : D; A.M = M; A.D = D;
   A.weight = weight; A.bias = bias; A.mean = mean; A.rstd = rstd; A.eps = eps;
   A.wvec = aligned(weight, 16) && aligned(bias, 16);
-  return launch(A, plan_of(M, D, 0), dtype, wide_rows(x, M, ldx, D, dtype) && wide_rows(y, M, ldy, D, dtype), 0, static_cast<cudaStream_t>(cuda_stream));
+  const bool wide = wide_rows(x, M, ldx, D, dtype) && wide_rows(y, M, ldy, D, dtype);
+  return launch(A, plan_of(M, D, dtype, 0, wide), dtype, wide, 0, static_cast<cudaStream_t>(cuda_stream));
 }
 
 int dmx_layer_norm_backward(int64_t M, int D, int dtype, const void* dy, int64_t lddy, const void* x, int64_t ldx, const float* mean, const float* rstd,
@@ -468,7 +546,7 @@ int dmx_layer_norm_backward(int64_t M, int D, int dtype, const void* dy, int64_t
   A.weight = weight; A.mean = const_cast<float*>(mean); A.rstd = const_cast<float*>(rstd);
   A.part = sums ? static_cast<float*>(workspace) : nullptr;
   A.wvec = aligned(weight, 16);
-  const Plan p = plan_of(M, D, 1);
+  const Plan p = plan_of(M, D, dtype, 1, true);
   const bool wide = wide_rows(x, M, ldx, D, dtype) && wide_rows(dy, M, lddy, D, dtype) && wide_rows(dx, M, lddx, D, dtype) && (!add || wide_rows(add, M, ldadd, D, dtype));
   const int rc = launch(A, p, dtype, wide, 1, st);
   if (rc != DMX_OK || !sums) return rc;
