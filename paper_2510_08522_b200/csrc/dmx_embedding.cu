@@ -3,12 +3,11 @@
 // forward    y[n] = scale T[ids[n]]
 // backward   dT[v] = scale (sum over n with ids[n] = v of dy[n]), added to what dT holds or not
 //
-// Both are bound by HBM. Backward first sorts the tokens by row (stably: by row, then by place): one cluster of eight CTAs sorts,
-// eight bits a pass, counting digits per warp, joining the counts through distributed shared memory; the other CTAs of that
-// launch write the table's zeros meanwhile, which takes longer than the sort of an ordinary batch. Then every warp sums a chunk of the sorted
+// Both are bound by HBM. Backward first sorts the tokens by row (stably: by row, then by place), eight bits a pass in two launches: every
+// CTA counts its keys' digits, then moves its keys. Other CTAs of these launches write the table's zeros meanwhile. Then every warp sums a chunk of the sorted
 // tokens over its columns, row after row in registers: each gradient row is read once, each row of the table written once. A row whose
-// tokens reach over chunks leaves fp32 sums, one per chunk, which a third launch joins. Work is cut by tokens, not by rows: how
-// often a token comes does not matter. Nothing is added atomically; the order of all sums is fixed by the shape and the ids.
+// tokens reach over chunks leaves fp32 sums, one per chunk, which a last launch joins. Work is cut by tokens, not by rows: how
+// often a token comes does not matter. Nothing is added atomically but whole numbers; the order of all sums is fixed by the shape and the ids.
 #include <type_traits>
 
 #include "dmx_rows.cuh"
@@ -17,7 +16,7 @@ namespace {
 
 using namespace dmx_rows;
 
-constexpr int kSortCtas = 8, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kDigits = 256, kKept = 8;
+constexpr int kSortCtas = 128, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kDigits = 256, kKept = 8;      // (CTAs: at most)
 
 // ---------------------------------------------------------------------------------------------- forward
 
@@ -69,21 +68,20 @@ __global__ void __launch_bounds__(256) gather_kernel(const __grid_constant__ Gat
 
 struct SortArgs {
   const void* ids;
-  int wide_ids, passes;
-  int64_t N, V;
-  uint2* pair[2];                  // key and place; passes go from one to the other, the last one ends in 0
+  int wide_ids, shift, ctas;       // shift: of the pass's digit; ctas: that sort
+  int64_t N, V, rounds;            // rounds: of 32 keys, a warp's share
+  const uint2* from;               // key and place, or NULL: the first pass takes the ids
+  uint2* to;
+  unsigned* counts;                // [ctas][digits] of the pass
   unsigned* crossing;              // to be zeroed
-  void* zero;                      // rows to clear, or NULL
-  int64_t zero_ld;                 // in bytes
-  int64_t zero_bytes;              // of a row
+  unsigned char* zero;             // rows to clear meanwhile, by the other CTAs, or NULL
+  int64_t zero_rows, zero_ld, zero_bytes;      // the last two of a row, in bytes
 };
 
-__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory"); }
-
 __device__ void clear_rows(const SortArgs& A, int64_t cta, int64_t ctas) {
-  unsigned char* p = static_cast<unsigned char*>(A.zero);
-  if (A.zero_ld == A.zero_bytes || A.V == 1) {             // one piece
-    const int64_t bytes = A.V * A.zero_bytes;
+  unsigned char* p = A.zero;
+  if (A.zero_ld == A.zero_bytes || A.zero_rows == 1) {     // one piece
+    const int64_t bytes = A.zero_rows * A.zero_bytes;
     int64_t head = (-(int64_t)reinterpret_cast<uintptr_t>(p)) & 15;
     if (head > bytes) head = bytes;
     const int64_t units = (bytes - head) / 16, tail = head + units * 16;
@@ -95,141 +93,128 @@ __device__ void clear_rows(const SortArgs& A, int64_t cta, int64_t ctas) {
     return;
   }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int64_t v = cta * kSortWarps + warp; v < A.V; v += ctas * kSortWarps)
+  for (int64_t v = cta * kSortWarps + warp; v < A.zero_rows; v += ctas * kSortWarps)
     for (int64_t i = lane * 2; i < A.zero_bytes; i += 64) *reinterpret_cast<unsigned short*>(p + v * A.zero_ld + i) = 0;
 }
 
-// One pass takes a digit: every warp counts its keys' digits in order (a key's rank among the warp's own equal digits is what it finds, plus
-// the equal ones in lanes below), the counts become places by prefix sums over warps, CTAs and digits, and keys go there. A warp's keys
-// stay in registers in between if they are no more than eight a lane; else they are ranked a second time.
-__global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads) sort_kernel(const __grid_constant__ SortArgs A) {
-  extern __shared__ unsigned counts[];                    // [warps][digits]: a warp's digits, then where its next one goes
-  __shared__ unsigned totals[kSortCtas][kDigits];         // every CTA's digits
-  __shared__ unsigned quarter[4][kDigits], scan[4][8];
+__device__ __forceinline__ uint2 pair_at(const SortArgs& A, int64_t n) {
+  if (n >= A.N) return make_uint2(0, 0);
+  if (A.from) return A.from[n];
+  const int64_t id = id_at(A.ids, A.wide_ids, n);
+  return make_uint2(id >= 0 && id < A.V ? (unsigned)id : (unsigned)A.V, (unsigned)n);      // what is in no row comes last
+}
+
+// How often each digit comes among a CTA's keys
+__global__ void __launch_bounds__(kSortThreads) count_kernel(const __grid_constant__ SortArgs A) {
+  __shared__ unsigned sh[kDigits];
   start_dependents();
   wait_for_previous();
-  if (blockIdx.x >= kSortCtas) {
-    clear_rows(A, blockIdx.x - kSortCtas, gridDim.x - kSortCtas);
+  if ((int)blockIdx.x >= A.ctas) {
+    clear_rows(A, blockIdx.x - A.ctas, gridDim.x - A.ctas);
     return;
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) *A.crossing = 0;
-  cluster_sync();                                         // all of it is there
+  if (blockIdx.x == 0 && threadIdx.x == 0 && A.crossing) *A.crossing = 0;
+  if (threadIdx.x < kDigits) sh[threadIdx.x] = 0;
+  __syncthreads();
+  const int64_t n0 = (int64_t)blockIdx.x * A.rounds * kSortThreads, n1 = min(n0 + A.rounds * kSortThreads, A.N);
+#pragma unroll 4
+  for (int64_t n = n0 + threadIdx.x; n < n1; n += kSortThreads) atomicAdd(&sh[pair_at(A, n).x >> A.shift & 255], 1u);
+  __syncthreads();
+  if (threadIdx.x < kDigits) A.counts[blockIdx.x * kDigits + threadIdx.x] = sh[threadIdx.x];
+}
+
+// A CTA's keys to where they belong by the digit. Every warp ranks its keys in order (behind its earlier equal digits, and the equal ones in lanes
+// below); the ranks become places by prefix sums over warps, CTAs (whose counts are there) and digits. A warp's keys stay in registers
+// meanwhile if they are no more than eight a lane; else they are ranked a second time.
+__global__ void __launch_bounds__(kSortThreads) scatter_kernel(const __grid_constant__ SortArgs A) {
+  extern __shared__ unsigned counts[];                    // [warps][digits]: a warp's digits, then where its next one goes
+  __shared__ unsigned quarter[4][kDigits], others[4][kDigits], earlier_ctas[4][kDigits], scan[4][8];
+  start_dependents();
+  wait_for_previous();
+  if ((int)blockIdx.x >= A.ctas) {
+    clear_rows(A, blockIdx.x - A.ctas, gridDim.x - A.ctas);
+    return;
+  }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, rank = blockIdx.x;
-  const int digit = threadIdx.x & 255, group = threadIdx.x >> 8;      // of the prefix sums: a digit of eight warps
+  const int digit = threadIdx.x & 255, group = threadIdx.x >> 8;      // of the prefix sums: a digit of eight warps, of every fourth CTA
   const unsigned below = (1u << lane) - 1;
-  // a warp's share: whole rounds of 32
-  const int64_t rounds = (A.N + 32 * kSortWarps * kSortCtas - 1) / (32 * kSortWarps * kSortCtas);
-  const int64_t first = ((int64_t)rank * kSortWarps + warp) * rounds * 32;
-  const bool keep = rounds <= kKept;
+  const int64_t first = ((int64_t)rank * kSortWarps + warp) * A.rounds * 32, end = min(first + A.rounds * 32, A.N);
+  const bool keep = A.rounds <= kKept;
   unsigned* mine = counts + warp * kDigits;
-  for (int pass = 0; pass < A.passes; ++pass) {
-    const int from = (A.passes - pass) & 1, shift = 8 * pass;
-    auto fetch = [&](int64_t n, unsigned& k, unsigned& p) {
-      k = p = 0;
-      if (n >= A.N) return;
-      if (pass > 0) {
-        const uint2 t = __ldcg(A.pair[from] + n);
-        k = t.x;
-        p = t.y;
-      } else {
-        const int64_t id = id_at(A.ids, A.wide_ids, n);
-        k = id >= 0 && id < A.V ? (unsigned)id : (unsigned)A.V;      // what is in no row comes last
-        p = (unsigned)n;
-      }
-    };
-    // the key's rank behind what `mine` holds for its digit, which moves on
-    auto ranked = [&](bool live, unsigned k) {
-      const unsigned d = live ? k >> shift & 255 : 256;
-      const unsigned same = __match_any_sync(0xffffffffu, d);
-      const unsigned before = live ? mine[d] : 0;
-      __syncwarp();
-      if (live && (same & below) == 0) mine[d] = before + __popc(same);
-      __syncwarp();
-      return before + __popc(same & below);
-    };
-    unsigned key[kKept], place[kKept], at[kKept];
-    if (keep) {
-#pragma unroll
-      for (int r = 0; r < kKept; ++r)
-        if (r < rounds) fetch(first + r * 32 + lane, key[r], place[r]);
-    }
-    for (int i = lane; i < kDigits; i += 32) mine[i] = 0;
+  // the key's rank behind what `mine` holds for its digit, which moves on
+  auto ranked = [&](bool live, unsigned k) {
+    const unsigned d = live ? k >> A.shift & 255 : 256;
+    const unsigned same = __match_any_sync(0xffffffffu, d);
+    const unsigned before = live ? mine[d] : 0;
     __syncwarp();
-    if (keep) {
+    if (live && (same & below) == 0) mine[d] = before + __popc(same);
+    __syncwarp();
+    return before + __popc(same & below);
+  };
+  uint2 pair[kKept];
+  unsigned at[kKept];
+  if (keep) {
 #pragma unroll
-      for (int r = 0; r < kKept; ++r)
-        if (r < rounds) at[r] = ranked(first + r * 32 + lane < A.N, key[r]);
-    } else {
-      for (int64_t n = first; n < first + rounds * 32 && n < A.N; n += 32) {
-        unsigned k, p;
-        fetch(n + lane, k, p);
-        ranked(n + lane < A.N, k);
-      }
+    for (int r = 0; r < kKept; ++r)
+      if (r < A.rounds) pair[r] = pair_at(A, first + r * 32 + lane);
+  }
+  unsigned before = 0, total = 0;                         // of the digit, in CTAs before this one, in all
+#pragma unroll 8
+  for (int c = group; c < A.ctas; c += 4) {
+    const unsigned t = A.counts[c * kDigits + digit];
+    before += c < rank ? t : 0;
+    total += t;
+  }
+  earlier_ctas[group][digit] = before;
+  others[group][digit] = total;
+  for (int i = lane; i < kDigits; i += 32) mine[i] = 0;
+  __syncwarp();
+  if (keep) {
+#pragma unroll
+    for (int r = 0; r < kKept; ++r)
+      if (r < A.rounds) at[r] = ranked(first + r * 32 + lane < A.N, pair[r].x);
+  } else {
+    for (int64_t n = first; n < end; n += 32) ranked(n + lane < A.N, pair_at(A, n + lane).x);
+  }
+  __syncthreads();
+  unsigned c[8], sum = 0;                                 // prefix over the warps
+#pragma unroll
+  for (int w = 0; w < 8; ++w) c[w] = counts[(group * 8 + w) * kDigits + digit];
+#pragma unroll
+  for (int w = 0; w < 8; ++w) {
+    const unsigned t = c[w];
+    c[w] = sum;
+    sum += t;
+  }
+  quarter[group][digit] = sum;
+  unsigned start = 0;
+  total = 0;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) { start += earlier_ctas[q][digit]; total += others[q][digit]; }
+  unsigned up = total;                                    // prefix over the digits
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned t = __shfl_up_sync(0xffffffffu, up, o);
+    if (lane >= o) up += t;
+  }
+  if (lane == 31) scan[group][warp & 7] = up;
+  __syncthreads();
+  start += up - total;
+  for (int w = 0; w < (warp & 7); ++w) start += scan[group][w];
+  for (int q = 0; q < group; ++q) start += quarter[q][digit];
+#pragma unroll
+  for (int w = 0; w < 8; ++w) counts[(group * 8 + w) * kDigits + digit] = c[w] + start;
+  __syncthreads();
+  if (keep) {
+#pragma unroll
+    for (int r = 0; r < kKept; ++r)
+      if (r < A.rounds && first + r * 32 + lane < A.N) A.to[at[r] + mine[pair[r].x >> A.shift & 255]] = pair[r];
+  } else {
+    for (int64_t n = first; n < end; n += 32) {
+      const uint2 p = pair_at(A, n + lane);
+      const unsigned to = ranked(n + lane < A.N, p.x);
+      if (n + lane < A.N) A.to[to] = p;
     }
-    __syncthreads();
-    unsigned c[8], sum = 0;                               // prefix over the warps; the CTA's total goes to every CTA
-#pragma unroll
-    for (int w = 0; w < 8; ++w) c[w] = counts[(group * 8 + w) * kDigits + digit];
-#pragma unroll
-    for (int w = 0; w < 8; ++w) {
-      const unsigned t = c[w];
-      c[w] = sum;
-      sum += t;
-    }
-    quarter[group][digit] = sum;
-    __syncthreads();
-    unsigned earlier = 0, total = 0;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const unsigned t = quarter[q][digit];
-      earlier += q < group ? t : 0;
-      total += t;
-    }
-#pragma unroll
-    for (int to = 0; to < kSortCtas / 4; ++to) {
-      unsigned there;
-      asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"((unsigned)__cvta_generic_to_shared(&totals[rank][digit])), "r"(group * (kSortCtas / 4) + to));
-      asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(there), "r"(total) : "memory");
-    }
-    cluster_sync();
-    unsigned all = 0;                                     // where this CTA's first key of a digit goes
-#pragma unroll
-    for (int r = 0; r < kSortCtas; ++r) {
-      const unsigned t = totals[r][digit];
-      earlier += r < rank ? t : 0;
-      all += t;
-    }
-    unsigned up = all;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const unsigned t = __shfl_up_sync(0xffffffffu, up, o);
-      if (lane >= o) up += t;
-    }
-    if (lane == 31) scan[group][warp & 7] = up;
-    asm volatile("bar.sync %0, 256;" ::"r"(1 + group) : "memory");
-    earlier += up - all;
-    for (int w = 0; w < (warp & 7); ++w) earlier += scan[group][w];
-#pragma unroll
-    for (int w = 0; w < 8; ++w) counts[(group * 8 + w) * kDigits + digit] = c[w] + earlier;
-    __syncthreads();
-    if (keep) {
-#pragma unroll
-      for (int r = 0; r < kKept; ++r)
-        if (r < rounds && first + r * 32 + lane < A.N) {
-          const unsigned to = at[r] + mine[key[r] >> shift & 255];
-          A.pair[from ^ 1][to] = make_uint2(key[r], place[r]);
-        }
-    } else {
-      for (int64_t n = first; n < first + rounds * 32 && n < A.N; n += 32) {
-        unsigned k, p;
-        fetch(n + lane, k, p);
-        const unsigned to = ranked(n + lane < A.N, k);
-        if (n + lane < A.N) A.pair[from ^ 1][to] = make_uint2(k, p);
-      }
-    }
-    if (pass + 1 == A.passes) break;
-    __threadfence();
-    cluster_sync();
   }
 }
 
@@ -462,15 +447,15 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ SumAr
 
 // ---------------------------------------------------------------------------------------------- host
 
-// Tokens a chunk: enough chunks for 24 warps on every SM, and 32 tokens at least (a chunk's ends cost it two rows of fp32). W: columns a lane.
+// Tokens a chunk: enough chunks for 24 warps on every SM, and eight tokens at least (a batch of loads). W: columns a lane.
 int chunk_of(int64_t N, int64_t D, int W) {
   const int64_t slices = (D + 32 * W - 1) / (32 * W), chunks = (148 * 24 + slices - 1) / slices;
   const int64_t per = (N + chunks - 1) / chunks;
-  return (int)((per + 31) / 32 * 32);
+  return (int)((per + 7) / 8 * 8);
 }
 
 struct BackPlan {
-  int64_t keys, part, crossing, total;
+  int64_t keys, part, crossing, counts, total;
 };
 BackPlan back_plan(int64_t N, int64_t D) {
   BackPlan p;
@@ -478,7 +463,8 @@ BackPlan back_plan(int64_t N, int64_t D) {
   const int64_t chunk = chunk_of(N, D, 8), chunk4 = chunk_of(N, D, 4), least = chunk < chunk4 ? chunk : chunk4;
   p.part = pad256((N + least - 1) / least * 2 * D * (int64_t)sizeof(float));
   p.crossing = pad256((1 + (N + least - 1) / least) * 4);
-  p.total = 2 * p.keys + p.part + p.crossing;
+  p.counts = kSortCtas * kDigits * 4;
+  p.total = 2 * p.keys + p.part + p.crossing + p.counts;
   return p;
 }
 
@@ -538,18 +524,33 @@ int dmx_embedding_backward(int64_t N, int64_t V, int64_t D, int id_bytes, const 
   if (workspace_bytes < p.total || !workspace) return DMX_ERR_ARG;
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   SortArgs S = {};
+  uint2* pairs[2] = {reinterpret_cast<uint2*>(ws), reinterpret_cast<uint2*>(ws + p.keys)};      // the last pass ends in the first
   S.ids = ids; S.wide_ids = id_bytes == 8; S.N = N; S.V = V;
-  for (S.passes = 1; (uint64_t)V >> (8 * S.passes); ++S.passes) {}
-  for (int i = 0; i < 2; ++i) S.pair[i] = reinterpret_cast<uint2*>(ws + i * p.keys);
+  S.rounds = (N + (int64_t)kSortThreads * kSortCtas - 1) / ((int64_t)kSortThreads * kSortCtas);
+  S.ctas = (int)((N + S.rounds * kSortThreads - 1) / (S.rounds * kSortThreads));
   S.crossing = reinterpret_cast<unsigned*>(ws + 2 * p.keys + p.part);
-  if (!accumulate) { S.zero = dtable; S.zero_ld = (V > 1 ? ldt : D) * eo; S.zero_bytes = D * eo; }
+  S.counts = reinterpret_cast<unsigned*>(ws + 2 * p.keys + p.part + p.crossing);
+  S.zero_ld = (V > 1 ? ldt : D) * eo; S.zero_bytes = D * eo;
+  int passes = 1;
+  while ((uint64_t)V >> (8 * passes)) ++passes;
   constexpr int kShared = kSortWarps * kDigits * 4;       // 32 KB
-  const int rc = start(dim3(accumulate ? kSortCtas : 144), kSortThreads, 1, kShared, st, sort_kernel, S);
+  int rc = DMX_OK;
+  for (int i = 0; i < 2 * passes && rc == DMX_OK; ++i) {  // every launch clears its share of the rows
+    const int64_t v0 = V * i / (2 * passes), v1 = V * (i + 1) / (2 * passes);
+    S.zero = accumulate || v1 == v0 ? nullptr : static_cast<unsigned char*>(dtable) + v0 * S.zero_ld;
+    S.zero_rows = v1 - v0;
+    S.shift = i / 2 * 8;
+    S.from = i < 2 ? nullptr : pairs[(passes - i / 2) & 1];
+    S.to = pairs[(passes - i / 2 - 1) & 1];
+    const dim3 grid((unsigned)(S.ctas + (S.zero ? 148 : 0)));
+    rc = i % 2 == 0 ? start(grid, kSortThreads, 1, 0, st, count_kernel, S) : start(grid, kSortThreads, 1, kShared, st, scatter_kernel, S);
+    S.crossing = nullptr;
+  }
   if (rc != DMX_OK) return rc;
   // 16-byte accesses of dy, and as many elements of the table's rows: 8 to 32 bytes
   const int W = 16 / e;
   const bool wide = wide_rows(dy, N, lddy, D, dtype) && aligned(dtable, W * eo < 16 ? W * eo : 16) && (V <= 1 || ldt % (W * eo < 16 ? W : 16 / (int)eo) == 0);
-  SumArgs A = {S.pair[0], dy, dtable, S.crossing, reinterpret_cast<float*>(ws + 2 * p.keys), N, V, N > 1 ? lddy : D, V > 1 ? ldt : D, (int)D, 0, accumulate != 0, scale};
+  SumArgs A = {pairs[0], dy, dtable, reinterpret_cast<unsigned*>(ws + 2 * p.keys + p.part), reinterpret_cast<float*>(ws + 2 * p.keys), N, V, N > 1 ? lddy : D, V > 1 ? ldt : D, (int)D, 0, accumulate != 0, scale};
   if (dtype == DMX_F32) return out_dtype == DMX_F32 ? sums<float, float>(A, wide, st) : sums<float, bf16>(A, wide, st);
   return out_dtype == DMX_F32 ? sums<bf16, float>(A, wide, st) : sums<bf16, bf16>(A, wide, st);
 }
