@@ -4,7 +4,7 @@
 // backward   dT[v] = scale (sum over n with ids[n] = v of dy[n]), added to what dT holds or not
 //
 // Both are bound by HBM. Backward first sorts the tokens by row (stably: by row, then by place), eight bits a pass in two launches: every
-// CTA counts its keys' digits, then moves its keys. Other CTAs of these launches write the table's zeros meanwhile. Then every warp sums a chunk of the sorted
+// CTA counts its keys' digits, then moves its keys. Other CTAs of the second write the table's zeros meanwhile. Then every warp sums a chunk of the sorted
 // tokens over its columns, row after row in registers: each gradient row is read once, each row of the table written once. A row whose
 // tokens reach over chunks leaves fp32 sums, one per chunk, which a last launch joins. Work is cut by tokens, not by rows: how
 // often a token comes does not matter. Nothing is added atomically but whole numbers; the order of all sums is fixed by the shape and the ids.
@@ -16,7 +16,7 @@ namespace {
 
 using namespace dmx_rows;
 
-constexpr int kSortCtas = 128, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kDigits = 256, kKept = 8;      // (CTAs: at most)
+constexpr int kSortCtas = 128, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kDigits = 256, kKept = 8, kJoinCtas = 148 * 12;      // (CTAs: at most)
 
 // ---------------------------------------------------------------------------------------------- forward
 
@@ -109,10 +109,6 @@ __global__ void __launch_bounds__(kSortThreads) count_kernel(const __grid_consta
   __shared__ unsigned sh[kDigits];
   start_dependents();
   wait_for_previous();
-  if ((int)blockIdx.x >= A.ctas) {
-    clear_rows(A, blockIdx.x - A.ctas, gridDim.x - A.ctas);
-    return;
-  }
   if (blockIdx.x == 0 && threadIdx.x == 0 && A.crossing) *A.crossing = 0;
   if (threadIdx.x < kDigits) sh[threadIdx.x] = 0;
   __syncthreads();
@@ -224,7 +220,7 @@ struct SumArgs {
   const uint2* pair;               // sorted: key and place
   const void* dy;
   void* out;
-  unsigned* crossing;              // how many chunks have a last row that begins there and goes on, then which (in any order)
+  unsigned* crossing;              // how many chunks have a last row that begins there and goes on, then (from the 8th byte) which, and the row, in any order
   float* part;                     // [chunks][2][D]: what a chunk's first and last row got, where they go on
   int64_t N, V, lddy, ldout;
   int D, chunk, accumulate;        // chunk: tokens, a multiple of 32
@@ -394,41 +390,44 @@ __global__ void __launch_bounds__(256, 3) sum_kernel(const __grid_constant__ Sum
   }
   if (!open) return;
   leave(joined ? 0 : 1);
-  if (!joined && slice == 0 && lane == 0) A.crossing[1 + atomicAdd(A.crossing, 1u)] = (unsigned)chunk;
+  if (!joined && slice == 0 && lane == 0) reinterpret_cast<uint2*>(A.crossing)[1 + atomicAdd(A.crossing, 1u)] = make_uint2((unsigned)chunk, __ldg(A.pair + n1).x);
 }
 
-// The rows that reach over chunks, by the chunk in which they begin: a CTA takes 128 columns of one at a time, its eight warps the chunks
-// behind in turn.
+// The rows that reach over chunks, by the chunk in which they begin: a CTA takes 128 columns of one at a time, its four warps the chunks
+// behind in turn. (Most such rows have one chunk behind: small CTAs, many of them.)
 template <typename O>
-__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ SumArgs A) {
-  __shared__ float sh[8][4][32];
+__global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ SumArgs A) {
+  constexpr int kAtOnce = 6;
+  __shared__ float sh[4][4][32];
   start_dependents();
   wait_for_previous();
   const int64_t chunks = (A.N + A.chunk - 1) / A.chunk;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slices = (A.D + 127) / 128;
+  const uint2* list = reinterpret_cast<const uint2*>(A.crossing) + 1;
+  uint2 entry = list[blockIdx.x / slices];                 // (on its way with the count; there is room for every chunk)
   const int64_t units = (int64_t)*A.crossing * slices;
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int64_t chunk = A.crossing[1 + unit / slices];
-    const unsigned k = __ldg(A.pair + (chunk + 1) * A.chunk).x;
+    if (unit != blockIdx.x) entry = list[unit / slices];
+    const int64_t chunk = entry.x;
+    const unsigned k = entry.y;
     const Columns<4, false> at((int)(unit % slices), lane, A.D);
     Row<O, 4, false> old;
     if (warp == 0) old.load(static_cast<const O*>(A.out) + (int64_t)k * A.ldout, at, A.accumulate);
     float s[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t j = chunk + 1 + warp; j < chunks; j += 32) {
-      float x[4][4];
-      bool on[4];
+    for (int64_t j = chunk + 1 + warp; j < chunks; j += 4 * kAtOnce) {
+      unsigned x[kAtOnce][4], key[kAtOnce];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {                        // (what is read of a chunk that is not in the row is left out)
-        const int64_t q = j + 8 * u;
-        on[u] = q < chunks && __ldg(A.pair + q * A.chunk).x == k;
+      for (int u = 0; u < kAtOnce; ++u) {                  // (what is read of a chunk that is not in the row is left out)
+        const int64_t q = j + 4 * u;
+        load_if(key[u], A.pair + q * A.chunk, q < chunks);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[u][i] = q < chunks && at.has(i) ? A.part[q * 2 * A.D + at.at(i)] : 0.f;
+        for (int i = 0; i < 4; ++i) load_if(x[u][i], A.part + q * 2 * A.D + at.at(i), q < chunks && at.has(i));
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u)
+      for (int u = 0; u < kAtOnce; ++u)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] += on[u] ? x[u][i] : 0.f;
-      if (!on[3]) break;
+        for (int i = 0; i < 4; ++i) s[i] += j + 4 * u < chunks && key[u] == k ? __uint_as_float(x[u][i]) : 0.f;
+      if (j + 4 * (kAtOnce - 1) >= chunks || key[kAtOnce - 1] != k) break;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) sh[warp][i][lane] = s[i];
@@ -437,7 +436,7 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ SumAr
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         s[i] = at.has(i) ? A.part[(chunk * 2 + 1) * A.D + at.at(i)] : 0.f;
-        for (int w = 0; w < 8; ++w) s[i] += sh[w][i][lane];
+        for (int w = 0; w < 4; ++w) s[i] += sh[w][i][lane];
       }
       finish_row<O, 4, false>(A, k, at, s, old);
     }
@@ -462,7 +461,7 @@ BackPlan back_plan(int64_t N, int64_t D) {
   p.keys = pad256(N * 8);
   const int64_t chunk = chunk_of(N, D, 8), chunk4 = chunk_of(N, D, 4), least = chunk < chunk4 ? chunk : chunk4;
   p.part = pad256((N + least - 1) / least * 2 * D * (int64_t)sizeof(float));
-  p.crossing = pad256((1 + (N + least - 1) / least) * 4);
+  p.crossing = pad256((1 + (N + least - 1) / least) * 8 + kJoinCtas * 8);      // (the join reads ahead)
   p.counts = kSortCtas * kDigits * 4;
   p.total = 2 * p.keys + p.part + p.crossing + p.counts;
   return p;
@@ -483,7 +482,7 @@ int sums(SumArgs A, bool wide, cudaStream_t st) {
   else rc = wide ? start(grid, 256, 1, 0, st, sum_kernel<T, O, kW, true, false>, A) : start(grid, 256, 1, 0, st, sum_kernel<T, O, 4, false, false>, A);
   if (rc != DMX_OK || chunks == 1) return rc;
   const int64_t most = (chunks - 1) * ((A.D + 127) / 128);
-  return start(dim3((unsigned)(most < 148 * 4 ? most : 148 * 4)), 256, 1, 0, st, join_kernel<O>, A);
+  return start(dim3((unsigned)(most < kJoinCtas ? most : kJoinCtas)), 128, 1, 0, st, join_kernel<O>, A);
 }
 
 }  // namespace
@@ -535,15 +534,18 @@ int dmx_embedding_backward(int64_t N, int64_t V, int64_t D, int id_bytes, const 
   while ((uint64_t)V >> (8 * passes)) ++passes;
   constexpr int kShared = kSortWarps * kDigits * 4;       // 32 KB
   int rc = DMX_OK;
-  for (int i = 0; i < 2 * passes && rc == DMX_OK; ++i) {  // every launch clears its share of the rows
-    const int64_t v0 = V * i / (2 * passes), v1 = V * (i + 1) / (2 * passes);
+  for (int i = 0; i < passes && rc == DMX_OK; ++i) {
+    S.shift = 8 * i;
+    S.from = i == 0 ? nullptr : pairs[(passes - i) & 1];
+    S.to = pairs[(passes - i - 1) & 1];
+    S.zero = nullptr;
+    rc = start(dim3((unsigned)S.ctas), kSortThreads, 1, 0, st, count_kernel, S);
+    if (rc != DMX_OK) break;
+    // the scattering launches, which take longer, clear their share of the rows meanwhile
+    const int64_t v0 = V * i / passes, v1 = V * (i + 1) / passes;
     S.zero = accumulate || v1 == v0 ? nullptr : static_cast<unsigned char*>(dtable) + v0 * S.zero_ld;
     S.zero_rows = v1 - v0;
-    S.shift = i / 2 * 8;
-    S.from = i < 2 ? nullptr : pairs[(passes - i / 2) & 1];
-    S.to = pairs[(passes - i / 2 - 1) & 1];
-    const dim3 grid((unsigned)(S.ctas + (S.zero ? 148 : 0)));
-    rc = i % 2 == 0 ? start(grid, kSortThreads, 1, 0, st, count_kernel, S) : start(grid, kSortThreads, 1, kShared, st, scatter_kernel, S);
+    rc = start(dim3((unsigned)(S.ctas + (S.zero ? 148 : 0))), kSortThreads, 1, kShared, st, scatter_kernel, S);
     S.crossing = nullptr;
   }
   if (rc != DMX_OK) return rc;

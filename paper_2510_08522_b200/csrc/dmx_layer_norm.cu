@@ -22,10 +22,11 @@ using namespace dmx_f32x2;
 
 constexpr int kMaxCluster = 8, kMaxWarps = 8;      // of a CTA that is one team
 // Rows on their way to a team: with the warps there are, more than the 40 KB that an SM has to have on its way
-constexpr int kForwardStages = 4, kBackwardStages = 2;
+constexpr int kForwardStages = 4;
+__host__ __device__ constexpr int backward_stages(int bytes) { return bytes == 2 ? 4 : 2; }
 // CTAs on an SM, for their registers (a thread of backward holds its sums, 2 N, and a row's values, 2 N)
 constexpr int forward_ctas(int values, bool wide) { return values == 32 ? 3 + wide : values == 16 ? 4 + wide : 6; }
-constexpr int backward_ctas(int values, int bytes) { return values == 32 ? (bytes == 2 ? 3 : 2) : values == 16 ? 4 : 6; }
+constexpr int backward_ctas(int values, int bytes) { return values == 32 ? 2 : values == 16 ? 4 : 6; }
 
 struct Args {
   const void *x, *dy, *add;
@@ -100,10 +101,13 @@ struct Held {
       const int count = min(D - first, N * threads), shift = (int)(reinterpret_cast<uintptr_t>(q) & 15);
       const unsigned char* from = reinterpret_cast<const unsigned char*>(q) - shift;
       const int bytes = count > 0 ? shift + count * (int)sizeof(T) : 0;
+      const unsigned char* nothing = reinterpret_cast<const unsigned char*>(reinterpret_cast<uintptr_t>(p) & ~(uintptr_t)15);
 #pragma unroll
       for (int i = 0; i <= N * (int)sizeof(T) / 16; ++i) {
-        const int at = (i * threads + own) * 16;
-        if (at < bytes) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + at), "l"(from + at), "r"(min(16, bytes - at)) : "memory");
+        const int at = (i * threads + own) * 16, left = bytes - at;
+        if (at >= threads * N * (int)sizeof(T) + 32) continue;
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + at), "l"(left > 0 ? from + at : nothing), "r"(left > 16 ? 16 : left > 0 ? left : 0)
+                     : "memory");
       }
     }
   }
@@ -120,8 +124,7 @@ struct Held {
       widen<T>(*reinterpret_cast<const Raw*>(slot + i * blockDim.x * sizeof(Raw)), x);
     } else {
       const int shift = (int)(reinterpret_cast<uintptr_t>(static_cast<const T*>(p) + r * ld + first) & 15);
-      x[0] = 0.f;
-      if (column(i) < D) widen<T>(*reinterpret_cast<const Raw*>(slot + shift + (i * threads + own) * sizeof(T)), x);
+      widen<T>(*reinterpret_cast<const Raw*>(slot + shift + (i * threads + own) * sizeof(T)), x);
     }
   }
   __device__ __forceinline__ void store(void* p, int64_t ld, int64_t r, const float (&x)[N]) const {
@@ -287,7 +290,7 @@ __global__ void __launch_bounds__(Held<T, V, TEAM, N>::kThreads, Held<T, V, TEAM
 
 template <typename T, int V, int TEAM, int N>
 __global__ void __launch_bounds__(Held<T, V, TEAM, N>::kThreads, Held<T, V, TEAM, N>::kBackwardCtas) backward_kernel(const __grid_constant__ Args A) {
-  constexpr int kStages = kBackwardStages;
+  constexpr int kStages = backward_stages(sizeof(T));
   extern __shared__ __align__(16) unsigned char raw[];     // weights, then the stages
   __shared__ float2 red[2][kMaxCluster * kMaxWarps];
   typedef Held<T, V, TEAM, N> H;
@@ -455,7 +458,7 @@ Plan plan_of(int64_t M, int D, int dtype, int backward, bool wide) {      // (ba
     p.threads = ((share + 31) / 32 + 31) / 32 * 32;
   }
   const int bytes = element_size(dtype), values = p.threads * p.values;              // a CTA's of one input
-  const int slots = backward ? kBackwardStages * 3 * values * bytes + 4 * (p.team > 0 ? p.team * p.values : values) : kForwardStages * values * bytes;
+  const int slots = backward ? backward_stages(bytes) * 3 * values * bytes + 4 * (p.team > 0 ? p.team * p.values : values) : kForwardStages * values * bytes;
   int at_once = p.team > 0 ? (backward ? backward_ctas(p.values, bytes) : forward_ctas(p.values, wide)) : (backward ? 256 : 512) / p.threads;
   const int fit = 224 * 1024 / (slots + 2048);
   at_once = fit < 1 ? 1 : at_once > fit ? fit : at_once;
@@ -469,7 +472,7 @@ template <typename T, int V, int TEAM, int N>
 int launch(const Args& A, const Plan& p, int backward, cudaStream_t st) {
   const dim3 grid((unsigned)(p.groups * p.cluster));
   typedef Held<T, V, TEAM, N> H;
-  int shared = backward ? kBackwardStages * (A.add ? 3 : 2) * H::stage_bytes(p.threads) + 4 * N * (TEAM > 0 ? TEAM : p.threads) : kForwardStages * H::stage_bytes(p.threads);
+  int shared = backward ? backward_stages(sizeof(T)) * (A.add ? 3 : 2) * H::stage_bytes(p.threads) + 4 * N * (TEAM > 0 ? TEAM : p.threads) : kForwardStages * H::stage_bytes(p.threads);
   if (backward && TEAM > 0 && shared < 4 * 2 * N * 32 * 4) shared = 4 * 2 * N * 32 * 4;        // the warps' sums
   static std::atomic<uint64_t> set[2];                    // devices on which the kernel may use that much
   int device = 0;
