@@ -60,13 +60,19 @@ __device__ __forceinline__ void add_bias(const bf16* bias, int cols, float (&v)[
 struct SumArgs : GemmShape {
   const bf16* bias;
   const void* target;
-  int wide_target, groups;        // groups: warps that share a row of a tile
+  int wide_target;
   float* hit;                     // the targets' logits
-  float2* part;                   // [tiles across x groups][rows]: maximum in units of log2 e, sum
+  float2* part;                   // [tiles across][rows]: maximum in units of log2 e, sum
 };
+
+__device__ __forceinline__ float2 joined(float2 a, float2 b) {
+  const float most = fmaxf(a.x, b.x), from = most == -INFINITY ? 0.f : most;         // (nothing but -inf so far)
+  return make_float2(most, a.y * ex2(a.x - from) + b.y * ex2(b.x - from));
+}
 
 struct SumEpilogue {
   typedef SumArgs Args;
+  static constexpr int kStaging = 0, kOwnShared = 64 + 2 * 4 * 3 * 32 * 8;
   float top = -INFINITY, sum = 0.f;
   int64_t target = -1;
   __device__ __forceinline__ void begin(const Args& A, int r0, int c0, int lane) {
@@ -97,8 +103,35 @@ struct SumEpilogue {
     top = most;
     sum = s;
   }
-  __device__ __forceinline__ void end(const Args& A, int r0, int tb, int group, int lane) {
-    if (group < A.groups && r0 + lane < A.rowsA) A.part[(int64_t)(tb * A.groups + group) * A.rowsA + r0 + lane] = make_float2(top, sum);
+  // The four warps that share rows meet in shared memory, in two places by turns; the accumulators are handed back afterwards, so that
+  // nobody is so far ahead that it writes where the first still reads.
+  struct Meeting {
+    uint64_t here[2][4];
+    float2 pair[2][4][3][32];
+  };
+  static_assert(sizeof(Meeting) <= kOwnShared, "what the launch leaves room for");
+  static __device__ __forceinline__ Meeting& meeting() {
+    __shared__ Meeting m;
+    return m;
+  }
+  static __device__ __forceinline__ void setup() {
+    for (int i = 0; i < 8; ++i) bar_init(smem_addr(&meeting().here[i / 4][i % 4]), 3);
+  }
+  __device__ __forceinline__ bool end(const Args& A, int r0, int tb, int group, int lane, int turn, unsigned parity) {
+    Meeting& m = meeting();
+    const int quarter = (r0 >> 5) & 3;
+    if (group > 0) {
+      m.pair[turn][quarter][group - 1][lane] = make_float2(top, sum);
+      __syncwarp();
+      if (lane == 0) bar_arrive(smem_addr(&m.here[turn][quarter]));
+      return true;
+    }
+    if (!warp_wait(smem_addr(&m.here[turn][quarter]), parity)) return false;
+    float2 v = make_float2(top, sum);
+#pragma unroll
+    for (int g = 0; g < 3; ++g) v = joined(v, m.pair[turn][quarter][g][lane]);
+    if (r0 + lane < A.rowsA) A.part[(int64_t)tb * A.rowsA + r0 + lane] = v;
+    return true;
   }
 };
 
@@ -108,21 +141,16 @@ __global__ void __launch_bounds__(256) join_kernel(const float2* part, int parts
   start_dependents();
   wait_for_previous();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = blockIdx.x * 32 + lane;
-  float top = -INFINITY, sum = 0.f;
-  auto take = [&](float2 p) {
-    const float most = fmaxf(top, p.x), from = most == -INFINITY ? 0.f : most;
-    sum = sum * ex2(top - from) + p.y * ex2(p.x - from);
-    top = most;
-  };
+  float2 v = make_float2(-INFINITY, 0.f);
   if (n < N) {
 #pragma unroll 8
-    for (int i = warp; i < parts; i += 8) take(part[(int64_t)i * N + n]);
+    for (int i = warp; i < parts; i += 8) v = joined(v, part[(int64_t)i * N + n]);
   }
-  sh[warp][lane] = make_float2(top, sum);
+  sh[warp][lane] = v;
   __syncthreads();
   if (warp > 0 || n >= N) return;
-  for (int w = 1; w < 8; ++w) take(sh[w][lane]);
-  const float l = (top + log2f(sum)) * kLn2;
+  for (int w = 1; w < 8; ++w) v = joined(v, sh[w][lane]);
+  const float l = (v.x + log2f(v.y)) * kLn2;
   const int64_t t = target_at(target, wide_target, n);
   lse[n] = l;
   loss[n] = t >= 0 && t < V ? l - hit[n] : 0.f;
@@ -143,6 +171,7 @@ struct SlopeArgs : GemmShape {
 
 struct SlopeEpilogue {
   typedef SlopeArgs Args;
+  static constexpr int kStaging = 2048, kOwnShared = 0;
   float lse2 = 0.f, scale = 0.f;
   int64_t target = -1;
   __device__ __forceinline__ void begin(const Args& A, int r0, int, int lane) {
@@ -186,7 +215,8 @@ struct SlopeEpilogue {
       if (r0 < A.rowsA && c0 + lane < A.rowsB) A.columns[(int64_t)(r0 >> 5) * A.rowsB + c0 + lane] = v[0];      // (in units)
     }
   }
-  __device__ __forceinline__ void end(const Args&, int, int, int, int) {}
+  static __device__ __forceinline__ void setup() {}
+  __device__ __forceinline__ bool end(const Args&, int, int, int, int, int, unsigned) { return true; }
 };
 
 // dx over several pieces: sums in fp32, in an order of their own (a warp's 32 rows x 32 columns after one another, a column of lanes at a time)
@@ -201,6 +231,7 @@ struct AddArgs : GemmShape {
 template <int BN>
 struct AddEpilogue {
   typedef AddArgs Args;
+  static constexpr int kStaging = 2048, kOwnShared = 0;
   __device__ __forceinline__ void begin(const Args&, int, int, int) {}
   template <int NC>
   __device__ __forceinline__ void chunk(const Args& A, float (&v)[NC], uint4* stage, int r0, int c0, int lane) {
@@ -223,7 +254,8 @@ struct AddEpilogue {
                                          pack2(v[8 * u + 6], v[8 * u + 7]));
     store_tile<32, NC>(A.y, A.ldy, A.vec, stage, r0, A.rowsA, c0, A.rowsB, lane);
   }
-  __device__ __forceinline__ void end(const Args&, int, int, int, int) {}
+  static __device__ __forceinline__ void setup() {}
+  __device__ __forceinline__ bool end(const Args&, int, int, int, int, int, unsigned) { return true; }
 };
 
 // the significand (1 to 2) of the largest finite |dloss|, 1 if that is zero
@@ -278,7 +310,6 @@ int product_rows(const Matrix& a, const Matrix& b, typename E::Args& A, const Ch
   return c.bn == 128 ? launch_gemm<128, false, 1, E>(a, b, A, st) : launch_gemm<64, false, 1, E>(a, b, A, st);
 }
 Choice choose_rows(int64_t N, int64_t V, int64_t D) { return choose(N, V, (int)((D + kBK - 1) / kBK), false, false); }
-int groups_of(const Choice& c) { return c.bn / 32 < kEpiWarps / 4 ? c.bn / 32 : kEpiWarps / 4; }
 
 bool sizes_ok(int64_t N, int64_t V, int64_t D) {
   const int64_t most = DMX_LINEAR_MAX_EXTENT;
@@ -295,7 +326,7 @@ struct ForwardPlan {
 ForwardPlan forward_plan(const Matrix& x, const Matrix& w) {
   ForwardPlan p;
   p.choice = choose_rows(x.rows, w.rows, x.cols);
-  p.parts = (w.rows + p.choice.bn - 1) / p.choice.bn * groups_of(p.choice);
+  p.parts = (w.rows + p.choice.bn - 1) / p.choice.bn;
   p.part = pad256(p.parts * x.rows * 8);
   p.hit = pad256(x.rows * 4);
   p.total = p.part + p.hit + laid_out_bytes(x) + laid_out_bytes(w);
@@ -350,7 +381,7 @@ int dmx_cross_entropy_forward(int64_t N, int64_t V, int64_t D, const void* x, in
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   SumArgs A = {};
   A.rowsA = (int)N; A.rowsB = (int)V; A.kblocks = (int)((D + kBK - 1) / kBK);
-  A.bias = static_cast<const bf16*>(bias); A.target = target; A.wide_target = target_bytes == 8; A.groups = groups_of(p.choice);
+  A.bias = static_cast<const bf16*>(bias); A.target = target; A.wide_target = target_bytes == 8;
   A.part = reinterpret_cast<float2*>(ws);
   A.hit = reinterpret_cast<float*>(ws + p.part);
   ws += p.part + p.hit;

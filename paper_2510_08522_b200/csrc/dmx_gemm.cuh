@@ -202,7 +202,8 @@ __device__ __forceinline__ void load_tile(const bf16* p, int64_t ld, int vec, ui
 // (8192^3: 820 TFLOP/s).
 // SPLIT: that many CTAs (a cluster) share a tile's k; each then completes 1/SPLIT of every 32 columns.
 // E: what becomes of D. A warp calls begin for a tile before it waits for it, chunk for every 32 columns (or its share of them) of its 32 rows,
-// a row per lane, and end.
+// a row per lane, and end (false: a wait in it ran out) before it hands the accumulators back; setup initializes what barriers end has.
+// kStaging: bytes of a warp's staging buffer (2048, or 0 if it uses none), kOwnShared: shared memory that E declares itself.
 template <int BN, bool PAIR, int SPLIT, class E>
 __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                                                                const __grid_constant__ typename E::Args A) {
@@ -216,7 +217,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   constexpr unsigned kCols = 2 * BN < 32 ? 32 : 2 * BN;
   unsigned char* sm = raw + ((1024 - (smem_addr(raw) & 1023)) & 1023);
   uint4* staging = reinterpret_cast<uint4*>(sm + (size_t)A.stages * kStage);                     // 2 KB per epilogue warp
-  float* sums = reinterpret_cast<float*>(sm + (size_t)A.stages * kStage + kEpiWarps * 2048);     // the cluster's partial sums
+  float* sums = reinterpret_cast<float*>(sm + (size_t)A.stages * kStage + kEpiWarps * E::kStaging);     // the cluster's partial sums
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   static_assert(!PAIR || SPLIT == 1, "a pair does not split k");
   constexpr int per = PAIR ? 2 : SPLIT, kOwn = 32 / SPLIT;
@@ -230,6 +231,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
     asm volatile("prefetch.tensormap [%0];" ::"l"(&mapB) : "memory");
     for (int s = 0; s < A.stages; ++s) { bar_init(smem_addr(&full[s]), 1); bar_init(smem_addr(&empty[s]), 1); }
     for (int i = 0; i < 2; ++i) { bar_init(smem_addr(&done[i]), 1); bar_init(smem_addr(&freed[i]), PAIR ? 2 * kEpiWarps : kEpiWarps); }
+    E::setup();
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -357,13 +359,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
           tmem_load32(tmem + buf * BN + c * 32 + ((unsigned)(quarter * 32) << 16), v);
           epilogue.template chunk<32>(A, v, stage, r0, c0, lane);
         }
+        ok = epilogue.end(A, r0, tb, group, lane, buf, aph);
         tmem_fence_before();
         __syncwarp();
         if (lane == 0) {
           if (PAIR) bar_arrive_cluster(in_cta(smem_addr(&freed[buf]), 0));
           else bar_arrive(smem_addr(&freed[buf]));
         }
-        epilogue.end(A, r0, tb, group, lane);
         if (buf) aph ^= 1;
         buf ^= 1;
       } else {
@@ -516,17 +518,17 @@ int launch_gemm(const Matrix& a, const Matrix& b, typename E::Args& A, cudaStrea
   A.tilesA = (A.rowsA + kRows - 1) / kRows;
   A.tilesB = (A.rowsB + BN - 1) / BN;
   const int stage = (kBM + kHalf) * 128, chunks = BN / 32;
-  const int extra = 1024 + kEpiWarps * 2048 + (SPLIT > 1 ? chunks * 32 * kBM * 4 : 0);
+  const int extra = 1024 + E::kOwnShared + kEpiWarps * E::kStaging + (SPLIT > 1 ? chunks * 32 * kBM * 4 : 0);
   A.stages = (kSmemMost - extra) / stage;
   if (A.stages > kMaxStages) A.stages = kMaxStages;
-  const int smem = A.stages * stage + extra;
+  const int smem = A.stages * stage + extra - E::kOwnShared;
   const auto kernel = gemm_kernel<BN, PAIR, SPLIT, E>;
   static std::atomic<uint64_t> set{0};         // devices on which this kernel may use that much shared memory
   int device = 0;
   if (!dmxh::cuda_ok(cudaGetDevice(&device))) return DMX_ERR_CUDA;
   const uint64_t bit = (uint64_t)1 << (device & 63);
   if (!(set.load(std::memory_order_relaxed) & bit) || device > 63) {
-    if (!dmxh::cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost))) return DMX_ERR_CUDA;
+    if (!dmxh::cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - E::kOwnShared))) return DMX_ERR_CUDA;
     set.fetch_or(bit, std::memory_order_relaxed);
   }
   const int64_t tiles = (int64_t)A.tilesA * A.tilesB;

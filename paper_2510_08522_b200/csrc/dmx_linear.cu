@@ -123,6 +123,7 @@ __device__ __forceinline__ void finish_swapped(const GemmArgs& A, float (&v)[NC]
 template <bool SWAP, bool UNIT>
 struct LinearEpilogue {
   typedef GemmArgs Args;
+  static constexpr int kStaging = 2048, kOwnShared = 0;
   float bias = 0.f;
   __device__ __forceinline__ void begin(const Args& A, int r0, int c0, int lane) {
     if (SWAP && A.bias && r0 + lane < A.rowsA) bias = bf_value(__ldg(reinterpret_cast<const unsigned short*>(A.bias) + r0 + lane));
@@ -138,7 +139,8 @@ struct LinearEpilogue {
     if constexpr (SWAP) finish_swapped<NC>(A, v, stage, r0, c0, bias, lane);
     else finish<NC>(A, v, stage, r0, c0, lane);
   }
-  __device__ __forceinline__ void end(const Args&, int, int, int, int) {}
+  static __device__ __forceinline__ void setup() {}
+  __device__ __forceinline__ bool end(const Args&, int, int, int, int, int, unsigned) { return true; }
 };
 
 // ---------------------------------------------------------------------------------------------- elementwise parts
