@@ -333,14 +333,14 @@ ForwardPlan forward_plan(const Matrix& x, const Matrix& w) {
   return p;
 }
 
-// Pieces of the vocabulary: G of a piece takes 256 MB at most (but 256 words at least).
+// Pieces of the vocabulary: G of a piece takes 512 MB at most (but 256 words at least).
 struct BackPlan {
   int64_t pieces, words, g, columns, sums, total;
 };
 BackPlan back_plan(const Matrix& x, const Matrix& w) {
   const int64_t N = x.rows, V = w.rows, D = x.cols;
   BackPlan p;
-  int64_t most = ((int64_t)1 << 28) / (2 * N) / 256 * 256;
+  int64_t most = ((int64_t)1 << 29) / (2 * N) / 256 * 256;
   if (most < 256) most = 256;
   p.pieces = (V + most - 1) / most;
   p.words = ((V + p.pieces - 1) / p.pieces + 255) / 256 * 256;
