@@ -28,6 +28,7 @@ namespace {
 using namespace dmx_gemm;
 using dmx_act::ex2;
 
+constexpr int kFewRows = 2048;          // whose largest dloss every warp finds while the first tile is on its way; a launch of its own takes 2.5 us
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 
 // ---------------------------------------------------------------------------------------------- forward
@@ -63,20 +64,28 @@ struct SumArgs : GemmShape {
   int wide_target;
   float* hit;                     // the targets' logits
   float2* part;                   // [tiles across][rows]: maximum in units of log2 e, sum
+  float *loss, *lse;              // written here where one tile has the whole vocabulary
 };
 
 __device__ __forceinline__ float2 joined(float2 a, float2 b) {
   const float most = fmaxf(a.x, b.x), from = most == -INFINITY ? 0.f : most;         // (nothing but -inf so far)
   return make_float2(most, a.y * ex2(a.x - from) + b.y * ex2(b.x - from));
 }
+__device__ __forceinline__ float lse_of(float2 v) { return (v.x + log2f(v.y)) * kLn2; }
 
 struct SumEpilogue {
   typedef SumArgs Args;
-  static constexpr int kStaging = 0, kOwnShared = 64 + 2 * 4 * 3 * 32 * 8;
-  float top = -INFINITY, sum = 0.f;
-  int64_t target = -1;
+  static constexpr int kStaging = 0, kOwnShared = 64 + 2 * 4 * 3 * 32 * 12;
+  static constexpr bool kRanged = false;
+  float2 all;                     // of the row so far
+  float hit;                      // its target's logit, if that is among them, else -inf
+  int64_t target;
   __device__ __forceinline__ void begin(const Args& A, int r0, int c0, int lane) {
-    if (r0 + lane < A.rowsA) target = target_at(A.target, A.wide_target, r0 + lane);
+    all = make_float2(-INFINITY, 0.f);
+    hit = -INFINITY;
+    target = r0 + lane < A.rowsA ? target_at(A.target, A.wide_target, r0 + lane) : -1;
+    if (target >= A.rowsB) target = -1;
+    if (A.bias && c0 < A.rowsB) asm volatile("prefetch.global.L1 [%0];" ::"l"(A.bias + c0));
   }
   template <int NC>
   __device__ __forceinline__ void chunk(const Args& A, float (&v)[NC], uint4*, int r0, int c0, int lane) {
@@ -86,28 +95,33 @@ struct SumEpilogue {
       for (int i = 0; i < NC; ++i)
         if (c0 + i >= A.rowsB) v[i] = -INFINITY;
     }
-    const bool here = target >= c0 && target < c0 + NC && target < A.rowsB;
+    const bool here = target >= c0 && target < c0 + NC;
     if (__any_sync(0xffffffffu, here)) {
 #pragma unroll
       for (int i = 0; i < NC; ++i)
-        if (here && target == c0 + i) A.hit[r0 + lane] = v[i];
+        if (here && target == c0 + i) hit = v[i];
+      if (here && !A.loss) A.hit[r0 + lane] = hit;
     }
-    float most = v[0];
+    float m[4], e[4];             // four chains each: the epilogue's latency, not its instructions, is what short products wait for
 #pragma unroll
-    for (int i = 1; i < NC; ++i) most = fmaxf(most, v[i]);
-    most = fmaxf(top, most * kLog2e);
+    for (int j = 0; j < 4; ++j) m[j] = v[j];
+#pragma unroll
+    for (int i = 4; i < NC; ++i) m[i & 3] = fmaxf(m[i & 3], v[i]);
+    const float most = fmaxf(all.x, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * kLog2e);
     const float from = most == -INFINITY ? 0.f : most;         // (nothing but -inf so far)
-    float s = sum * ex2(top - from);
+    e[0] = all.y * ex2(all.x - from);
 #pragma unroll
-    for (int i = 0; i < NC; ++i) s += ex2(fmaf(v[i], kLog2e, -from));
-    top = most;
-    sum = s;
+    for (int j = 1; j < 4; ++j) e[j] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) e[i & 3] += ex2(fmaf(v[i], kLog2e, -from));
+    all = make_float2(most, (e[0] + e[1]) + (e[2] + e[3]));
   }
   // The four warps that share rows meet in shared memory, in two places by turns; the accumulators are handed back afterwards, so that
   // nobody is so far ahead that it writes where the first still reads.
   struct Meeting {
     uint64_t here[2][4];
     float2 pair[2][4][3][32];
+    float hit[2][4][3][32];
   };
   static_assert(sizeof(Meeting) <= kOwnShared, "what the launch leaves room for");
   static __device__ __forceinline__ Meeting& meeting() {
@@ -121,16 +135,27 @@ struct SumEpilogue {
     Meeting& m = meeting();
     const int quarter = (r0 >> 5) & 3;
     if (group > 0) {
-      m.pair[turn][quarter][group - 1][lane] = make_float2(top, sum);
+      m.pair[turn][quarter][group - 1][lane] = all;
+      if (A.loss) m.hit[turn][quarter][group - 1][lane] = hit;
       __syncwarp();
       if (lane == 0) bar_arrive(smem_addr(&m.here[turn][quarter]));
       return true;
     }
     if (!warp_wait(smem_addr(&m.here[turn][quarter]), parity)) return false;
-    float2 v = make_float2(top, sum);
 #pragma unroll
-    for (int g = 0; g < 3; ++g) v = joined(v, m.pair[turn][quarter][g][lane]);
-    if (r0 + lane < A.rowsA) A.part[(int64_t)tb * A.rowsA + r0 + lane] = v;
+    for (int g = 0; g < 3; ++g) all = joined(all, m.pair[turn][quarter][g][lane]);
+    if (r0 + lane >= A.rowsA) return true;
+    if (A.loss) {
+      if (target >= 0 && target < A.rowsB) {
+        const int g = (int)target / 32 % 4;                    // which warp had it: chunks go to them in turn
+        if (g > 0) hit = m.hit[turn][quarter][g - 1][lane];
+      }
+      const float l = lse_of(all);
+      A.lse[r0 + lane] = l;
+      A.loss[r0 + lane] = target >= 0 ? l - hit : 0.f;
+    } else {
+      A.part[(int64_t)tb * A.rowsA + r0 + lane] = all;
+    }
     return true;
   }
 };
@@ -150,7 +175,7 @@ __global__ void __launch_bounds__(256) join_kernel(const float2* part, int parts
   __syncthreads();
   if (warp > 0 || n >= N) return;
   for (int w = 1; w < 8; ++w) v = joined(v, sh[w][lane]);
-  const float l = (v.x + log2f(v.y)) * kLn2;
+  const float l = lse_of(v);
   const int64_t t = target_at(target, wide_target, n);
   lse[n] = l;
   loss[n] = t >= 0 && t < V ? l - hit[n] : 0.f;
@@ -162,33 +187,68 @@ struct SlopeArgs : GemmShape {
   const bf16* bias;               // of the piece
   const void* target;
   int wide_target, first, vocabulary, vec;    // first: the piece's first word
-  const float *lse, *dloss, *unit;
+  const float *lse, *dloss;
+  float* unit;                    // there already, or (few rows) found by every warp on its own while the first tile is on its way
+  int find_unit;
   int64_t stride;                 // of dloss: 1 or 0
   bf16* g;
   int64_t ldg;
   float* columns;                 // [rows / 32][piece]: sums over 32 rows, or NULL
 };
 
+__device__ __forceinline__ float finite_size(float d) {
+  d = fabsf(d);
+  return d <= 3.402823466e38f ? d : 0.f;
+}
+__device__ __forceinline__ float unit_of(float most) {
+  int e;
+  return most == 0.f ? 1.f : 2.f * frexpf(most, &e);
+}
+
 struct SlopeEpilogue {
   typedef SlopeArgs Args;
   static constexpr int kStaging = 2048, kOwnShared = 0;
-  float lse2 = 0.f, scale = 0.f;
-  int64_t target = -1;
-  __device__ __forceinline__ void begin(const Args& A, int r0, int, int lane) {
+  static constexpr bool kRanged = false;
+  float lse2, scale, units = 0.f;
+  bool every;                     // all of the warp's rows have a slope
+  int64_t target;
+  __device__ __forceinline__ void begin(const Args& A, int r0, int c0, int lane) {
+    if (units == 0.f) {
+      if (A.find_unit) {
+        float most = 0.f;
+#pragma unroll 8
+        for (int n = lane; n < A.rowsA; n += 32) most = fmaxf(most, finite_size(__ldg(A.dloss + n * A.stride)));
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+        units = unit_of(most);
+        if (r0 == 0 && c0 == 0 && lane == 0) *A.unit = units;
+      } else {
+        units = *A.unit;
+      }
+    }
+    if (A.bias && c0 < A.rowsB) asm volatile("prefetch.global.L1 [%0];" ::"l"(A.bias + c0));
+    lse2 = scale = 0.f;
+    target = -1;
     const int n = r0 + lane;
-    if (n >= A.rowsA) return;
-    const int64_t t = target_at(A.target, A.wide_target, n);
-    const bool live = t >= 0 && t < A.vocabulary;
-    lse2 = __ldg(A.lse + n) * kLog2e;
-    scale = live ? __ldg(A.dloss + n * A.stride) / __ldg(A.unit) : 0.f;
-    target = live ? t - A.first : -1;
+    if (n < A.rowsA) {
+      const int64_t t = target_at(A.target, A.wide_target, n);
+      if (t >= 0 && t < A.vocabulary) {
+        scale = __ldg(A.dloss + n * A.stride) / units;
+        target = t - A.first;
+      }
+      lse2 = __ldg(A.lse + n) * kLog2e;
+    }
+    every = __all_sync(0xffffffffu, scale != 0.f);
   }
   template <int NC>
   __device__ __forceinline__ void chunk(const Args& A, float (&v)[NC], uint4* stage, int r0, int c0, int lane) {
     add_bias(A.bias, A.rowsB, v, c0);
-    // a row without a target has scale 0: its values are zeros whatever its logits are
 #pragma unroll
-    for (int i = 0; i < NC; ++i) v[i] = scale == 0.f ? 0.f : ex2(fmaf(v[i], kLog2e, -lse2)) * scale;
+    for (int i = 0; i < NC; ++i) v[i] = ex2(fmaf(v[i], kLog2e, -lse2)) * scale;
+    if (!every) {                 // a row without a target has scale 0: its values are zeros whatever its logits are
+#pragma unroll
+      for (int i = 0; i < NC; ++i) v[i] = scale == 0.f ? 0.f : v[i];
+    }
     const bool here = target >= c0 && target < c0 + NC;
     if (__any_sync(0xffffffffu, here)) {
 #pragma unroll
@@ -221,7 +281,7 @@ struct SlopeEpilogue {
 
 // dx over several pieces: sums in fp32, in an order of their own (a warp's 32 rows x 32 columns after one another, a column of lanes at a time)
 struct AddArgs : GemmShape {
-  const float* unit;
+  float* unit;
   float* sums;
   bf16* y;
   int64_t ldy;
@@ -232,6 +292,7 @@ template <int BN>
 struct AddEpilogue {
   typedef AddArgs Args;
   static constexpr int kStaging = 2048, kOwnShared = 0;
+  static constexpr bool kRanged = false;
   __device__ __forceinline__ void begin(const Args&, int, int, int) {}
   template <int NC>
   __device__ __forceinline__ void chunk(const Args& A, float (&v)[NC], uint4* stage, int r0, int c0, int lane) {
@@ -258,17 +319,14 @@ struct AddEpilogue {
   __device__ __forceinline__ bool end(const Args&, int, int, int, int, int, unsigned) { return true; }
 };
 
-// the significand (1 to 2) of the largest finite |dloss|, 1 if that is zero
+// the significand (1 to 2) of the largest finite |dloss|, 1 if that is zero: many rows
 __global__ void __launch_bounds__(1024) unit_kernel(const float* dloss, int64_t stride, int N, float* unit) {
   __shared__ float sh[32];
   start_dependents();
   wait_for_previous();
   float most = 0.f;
 #pragma unroll 8
-  for (int n = threadIdx.x; n < N; n += 1024) {
-    const float d = fabsf(dloss[n * stride]);
-    if (d <= 3.402823466e38f) most = fmaxf(most, d);
-  }
+  for (int n = threadIdx.x; n < N; n += 1024) most = fmaxf(most, finite_size(dloss[n * stride]));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = most;
@@ -277,10 +335,55 @@ __global__ void __launch_bounds__(1024) unit_kernel(const float* dloss, int64_t 
   most = sh[threadIdx.x];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-  if (threadIdx.x == 0) {
-    int e;
-    *unit = most == 0.f ? 1.f : 2.f * frexpf(most, &e);
+  if (threadIdx.x == 0) *unit = unit_of(most);
+}
+
+// A product of few tiles over a long k: every range's part in fp32, in the order of AddEpilogue, and a launch that adds them.
+struct PartArgs : GemmShape {
+  float* parts;
+};
+
+template <int BN>
+struct PartEpilogue {
+  typedef PartArgs Args;
+  static constexpr int kStaging = 0, kOwnShared = 0;
+  static constexpr bool kRanged = true;
+  int range;
+  __device__ __forceinline__ void begin(const Args&, int, int, int) {}
+  template <int NC>
+  __device__ __forceinline__ void chunk(const Args& A, float (&v)[NC], uint4*, int r0, int c0, int lane) {
+    const int64_t blocks = (A.rowsA + 31) / 32, across = (A.rowsB + 31) / 32;
+    float* at = A.parts + ((range * blocks + (r0 >> 5)) * across + (c0 >> 5)) * 1024 + lane;
+    if (r0 + lane < A.rowsA) {
+#pragma unroll
+      for (int i = 0; i < NC; ++i) at[i * 32] = v[i];
+    }
+    __syncwarp();
   }
+  static __device__ __forceinline__ void setup() {}
+  __device__ __forceinline__ bool end(const Args&, int, int, int, int, int, unsigned) { return true; }
+};
+
+// a warp: 32 rows (a lane each) x four columns
+__global__ void __launch_bounds__(256) add_parts_kernel(const float* parts, int ranges, int rows, int cols, const float* unit, bf16* y, int64_t ldy) {
+  start_dependents();
+  wait_for_previous();
+  const int lane = threadIdx.x & 31;
+  const int64_t blocks = (rows + 31) / 32, across = (cols + 31) / 32, job = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  if (job >= blocks * across * 8) return;
+  const int64_t block = job / 8;
+  const int r = (int)(block / across) * 32 + lane, c = (int)(block % across) * 32 + (int)(job % 8) * 4;
+  if (r >= rows || c >= cols) return;
+  const float* at = parts + block * 1024 + job % 8 * 128 + lane;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int k = 0; k < ranges; ++k)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] += at[k * blocks * across * 1024 + i * 32];
+  const float times = __ldg(unit);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (c + i < cols) y[(int64_t)r * ldy + c + i] = __float2bfloat16_rn(s[i] * times);
 }
 
 // db from the sums over 32 rows each: 32 columns a CTA
@@ -333,9 +436,43 @@ ForwardPlan forward_plan(const Matrix& x, const Matrix& w) {
   return p;
 }
 
+// A product with few tiles: tiles x ranges of k fill the card once. ranges 0: as plain_product does it, unless ranges take a fifth off its time
+// (a stage's time as `choose` has it, 3.5 us for the launch that adds, the parts' traffic at 4 TB/s). 16000 x 64 into 300 words: dW 21 -> 9 us.
+struct Cut {
+  int bn, ranges;
+  int64_t bytes;
+};
+Cut cut_of(int64_t rows, int64_t cols, int64_t k, int mnA) {
+  const int kblocks = (int)((k + kBK - 1) / kBK);
+  const int64_t area = (rows + 31) / 32 * ((cols + 31) / 32) * 4096;
+  Cut best = {0, 0, 0};
+  float least = 0.8f * plain_product_ns(rows, cols, k, mnA);
+  const struct { int bn; float stage; } forms[2] = {{128, 290.f}, {64, 245.f}};
+  for (const auto& f : forms) {
+    const int64_t tiles = (rows + kBM - 1) / kBM * ((cols + f.bn - 1) / f.bn);
+    int64_t ranges = 148 / tiles < kblocks ? 148 / tiles : kblocks;
+    if (ranges < 2) continue;
+    const float t = (float)((kblocks + ranges - 1) / ranges) * f.stage + 8.f * f.bn + 3500.f + (float)(ranges * area) * 2 / 4000.f;
+    if (t < least) { least = t; best = {f.bn, (int)ranges, pad256(ranges * area)}; }
+  }
+  return best;
+}
+int product_of(const Cut& cut, const Matrix& a, int mnA, const Matrix& b, int mnB, int64_t k, const float* unit, float* parts, bf16* y, int64_t ldy, cudaStream_t st) {
+  if (cut.ranges == 0) return plain_product(a, mnA, b, mnB, k, unit, y, ldy, st);
+  const int64_t rows = mnA ? a.cols : a.rows, cols = mnB ? b.cols : b.rows;
+  PartArgs A = {};
+  A.rowsA = (int)rows; A.rowsB = (int)cols; A.kblocks = (int)((k + kBK - 1) / kBK); A.mnA = mnA; A.mnB = mnB;
+  A.ranges = cut.ranges; A.parts = parts;
+  const int rc = cut.bn == 128 ? launch_gemm<128, false, 1, PartEpilogue<128>>(a, b, A, st) : launch_gemm<64, false, 1, PartEpilogue<64>>(a, b, A, st);
+  if (rc != DMX_OK) return rc;
+  const int64_t jobs = (rows + 31) / 32 * ((cols + 31) / 32) * 8;
+  return start(dim3((unsigned)((jobs + 7) / 8)), st, add_parts_kernel, (const float*)parts, cut.ranges, (int)rows, (int)cols, unit, y, ldy);
+}
+
 // Pieces of the vocabulary: G of a piece takes 512 MB at most (but 256 words at least).
 struct BackPlan {
-  int64_t pieces, words, g, columns, sums, total;
+  int64_t pieces, words, g, columns, sums, total;      // sums: of dx over the pieces, or a cut product's parts
+  Cut dx, dw;                                          // with one piece
 };
 BackPlan back_plan(const Matrix& x, const Matrix& w) {
   const int64_t N = x.rows, V = w.rows, D = x.cols;
@@ -348,7 +485,12 @@ BackPlan back_plan(const Matrix& x, const Matrix& w) {
   const int64_t cols = p.words < V ? p.words : V;
   p.g = pad256(N * pad8(cols) * 2);
   p.columns = pad256((N + 31) / 32 * cols * 4);
-  p.sums = p.pieces > 1 ? ((N + 255) / 256 * 256) * ((D + 255) / 256 * 256) * 4 : 0;
+  p.dx = p.dw = Cut{0, 0, 0};
+  if (p.pieces == 1) {
+    p.dx = cut_of(N, D, V, 0);
+    p.dw = cut_of(V, D, N, 1);
+  }
+  p.sums = p.pieces == 1 ? (p.dx.bytes > p.dw.bytes ? p.dx.bytes : p.dw.bytes) : ((N + 255) / 256 * 256) * ((D + 255) / 256 * 256) * 4;
   p.total = 256 + p.g + p.columns + p.sums + laid_out_bytes(x) + laid_out_bytes(w);
   return p;
 }
@@ -384,6 +526,7 @@ int dmx_cross_entropy_forward(int64_t N, int64_t V, int64_t D, const void* x, in
   A.bias = static_cast<const bf16*>(bias); A.target = target; A.wide_target = target_bytes == 8;
   A.part = reinterpret_cast<float2*>(ws);
   A.hit = reinterpret_cast<float*>(ws + p.part);
+  if (p.parts == 1) { A.loss = loss; A.lse = lse; }
   ws += p.part + p.hit;
   Jobs jobs;
   int n = 0;
@@ -391,7 +534,7 @@ int dmx_cross_entropy_forward(int64_t N, int64_t V, int64_t D, const void* x, in
   lay_out(b, ws, jobs, n);
   int rc = n > 0 ? run_jobs(jobs, n, DMX_ACT_NONE, st) : DMX_OK;
   if (rc == DMX_OK) rc = product_rows<SumEpilogue>(a, b, A, p.choice, st);
-  if (rc != DMX_OK) return rc;
+  if (rc != DMX_OK || p.parts == 1) return rc;
   return start(dim3((unsigned)((N + 31) / 32)), st, join_kernel, (const float2*)A.part, (int)p.parts, (int)N, (int)V, (const float*)A.hit, target, A.wide_target, loss, lse);
 }
 
@@ -430,23 +573,24 @@ int dmx_cross_entropy_backward(int64_t N, int64_t V, int64_t D, const float* dlo
   lay_out(a, ws, jobs, n);
   lay_out(b, ws, jobs, n);
   int rc = n > 0 ? run_jobs(jobs, n, DMX_ACT_NONE, st) : DMX_OK;
-  if (rc == DMX_OK) rc = start(dim3(1), 1024, st, unit_kernel, dloss, N > 1 ? dloss_stride : 0, dloss_stride == 0 ? 1 : (int)N, unit);
+  const bool find_unit = N <= kFewRows;
+  if (rc == DMX_OK && !find_unit) rc = start(dim3(1), 1024, st, unit_kernel, dloss, dloss_stride, dloss_stride == 0 ? 1 : (int)N, unit);
   for (int64_t first = 0; first < V && rc == DMX_OK; first += p.words) {
     const int64_t words = V - first < p.words ? V - first : p.words;
     const Matrix piece = {b.p + first * b.ld, words, D, b.ld};
     SlopeArgs A = {};
     A.rowsA = (int)N; A.rowsB = (int)words; A.kblocks = (int)((D + kBK - 1) / kBK);
     A.bias = bias ? static_cast<const bf16*>(bias) + first : nullptr; A.target = target; A.wide_target = target_bytes == 8;
-    A.first = (int)first; A.vocabulary = (int)V; A.lse = lse; A.dloss = dloss; A.unit = unit; A.stride = N > 1 ? dloss_stride : 0;
+    A.first = (int)first; A.vocabulary = (int)V; A.lse = lse; A.dloss = dloss; A.unit = unit; A.find_unit = find_unit && first == 0; A.stride = N > 1 ? dloss_stride : 0;
     A.g = g; A.ldg = pad8(words); A.vec = 1; A.columns = dbias ? columns : nullptr;
     rc = product_rows<SlopeEpilogue>(a, piece, A, choose_rows(N, words, D), st);
     if (rc == DMX_OK && dbias)
       rc = start(dim3((unsigned)((words + 31) / 32)), 1024, st, columns_kernel, (const float*)columns, (int)((N + 31) / 32), (int)words, (const float*)unit, static_cast<bf16*>(dbias) + first);
     const Matrix G = {g, N, words, A.ldg};
-    if (rc == DMX_OK && dw) rc = plain_product(G, 1, a, 1, N, unit, static_cast<bf16*>(dw) + first * (V > 1 ? lddw : D), V > 1 ? lddw : D, st);
+    if (rc == DMX_OK && dw) rc = product_of(p.dw, G, 1, a, 1, N, unit, sums, static_cast<bf16*>(dw) + first * (V > 1 ? lddw : D), V > 1 ? lddw : D, st);
     if (rc != DMX_OK || !dx) continue;
     if (p.pieces == 1) {
-      rc = plain_product(G, 0, piece, 1, words, unit, static_cast<bf16*>(dx), N > 1 ? lddx : D, st);
+      rc = product_of(p.dx, G, 0, piece, 1, words, unit, sums, static_cast<bf16*>(dx), N > 1 ? lddx : D, st);
       continue;
     }
     AddArgs E = {};

@@ -40,6 +40,7 @@ struct GemmShape {
   int rowsA, rowsB, kblocks;                  // rows of D, columns of D, ceil(k / 64)
   int tilesA, tilesB, stages;
   int mnA, mnB;                               // operand is MN-major
+  int ranges;                                 // of k, if E takes a range's part of D at a time
 };
 
 // ---------------------------------------------------------------------------------------------- PTX
@@ -203,7 +204,7 @@ __device__ __forceinline__ void load_tile(const bf16* p, int64_t ld, int vec, ui
 // SPLIT: that many CTAs (a cluster) share a tile's k; each then completes 1/SPLIT of every 32 columns.
 // E: what becomes of D. A warp calls begin for a tile before it waits for it, chunk for every 32 columns (or its share of them) of its 32 rows,
 // a row per lane, and end (false: a wait in it ran out) before it hands the accumulators back; setup initializes what barriers end has.
-// kStaging: bytes of a warp's staging buffer (2048, or 0 if it uses none), kOwnShared: shared memory that E declares itself.
+// With kRanged k is cut into A.ranges parts, each a D of its own (E's member `range` says which). kStaging: bytes of a warp's staging buffer (2048, or 0 if it uses none), kOwnShared: shared memory that E declares itself.
 template <int BN, bool PAIR, int SPLIT, class E>
 __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_constant__ CUtensorMap mapA, const __grid_constant__ CUtensorMap mapB,
                                                                const __grid_constant__ typename E::Args A) {
@@ -222,8 +223,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   static_assert(!PAIR || SPLIT == 1, "a pair does not split k");
   constexpr int per = PAIR ? 2 : SPLIT, kOwn = 32 / SPLIT;
   const int side = PAIR ? blockIdx.x & 1 : 0, rank = SPLIT > 1 ? blockIdx.x % SPLIT : 0;
-  const int tiles = A.tilesA * A.tilesB, first = blockIdx.x / per, step = gridDim.x / per;
-  const int kb0 = (int)((int64_t)A.kblocks * rank / SPLIT), kb1 = (int)((int64_t)A.kblocks * (rank + 1) / SPLIT);
+  const int every = A.tilesA * A.tilesB, tiles = E::kRanged ? every * A.ranges : every, first = blockIdx.x / per, step = gridDim.x / per;
+  int kb0 = (int)((int64_t)A.kblocks * rank / SPLIT), kb1 = (int)((int64_t)A.kblocks * (rank + 1) / SPLIT);
 
   start_dependents();
   if (threadIdx.x == 0) {
@@ -253,6 +254,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
 
   // tile t: A tiles in bands of 16, B tiles across a band, so that what runs at once shares its operands in L2
   auto tile_at = [&](int t, int& ta, int& tb) {
+    if constexpr (E::kRanged) {
+      const int range = t / every;
+      t -= range * every;
+      kb0 = (int)((int64_t)A.kblocks * range / A.ranges);
+      kb1 = (int)((int64_t)A.kblocks * (range + 1) / A.ranges);
+    }
     const int band = 16 * A.tilesB, b = t / band, in = t - b * band, h = min(16, A.tilesA - 16 * b);
     tb = in / h;
     ta = 16 * b + in - tb * h;
@@ -308,6 +315,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       int s = 0;
       unsigned ph = 0, buf = 0, aph = 0;
       for (int t = first; t < tiles && ok; t += step) {
+        if constexpr (E::kRanged) {
+          int ta, tb;
+          tile_at(t, ta, tb);                  // (for its range of k)
+        }
         ok = warp_wait(smem_addr(&freed[buf]), aph ^ 1);
         if (!ok) break;
         tmem_fence_after();
@@ -342,11 +353,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
     const int e = warp - 2, quarter = warp & 3, group = e >> 2;     // TMEM lanes 32 quarter.. belong to warps of that number mod 4
     uint4* stage = staging + e * 128;
     unsigned buf = 0, aph = 0;
+    E epilogue;
     for (int t = first; t < tiles && ok; t += step) {
       int ta, tb;
       tile_at(t, ta, tb);
       const int r0 = ta * kRows + side * kBM + quarter * 32;
-      E epilogue;
+      if constexpr (E::kRanged) epilogue.range = t / every;
       epilogue.begin(A, r0, tb * BN + group * 32, lane);            // fetches before the wait
       ok = warp_wait(smem_addr(&done[buf]), aph);
       if (!ok) break;
@@ -486,12 +498,13 @@ int start(dim3 grid, cudaStream_t st, void (*kernel)(P...), V... args) { return 
 struct Choice {
   int bn, split;
   bool pair;
+  float ns;
 };
 
 // Tile width, split and pairing, by the time they take: what a stage of 64 k took measured on 8192^3 (ns; the narrow tiles are bound
 // by what the SMs fetch from L2), the last tile's epilogue, a split's cluster barrier and exchange.
 inline Choice choose(int64_t rowsA, int64_t rowsB, int kblocks, bool swap, bool splits = true) {
-  Choice best = {0, 1, false};
+  Choice best = {0, 1, false, 0.f};
   float least = 0.f;
   const struct { int bn; bool pair; float stage; } forms[6] = {{256, true, 405.f}, {256, false, 435.f}, {128, true, 290.f},
                                                                 {128, false, 290.f}, {64, false, 245.f}, {32, false, 200.f}};
@@ -504,7 +517,7 @@ inline Choice choose(int64_t rowsA, int64_t rowsB, int kblocks, bool swap, bool 
       if (split > 1 && (tiles * split > 148 || kblocks / split < 2)) break;
       const int64_t waves = (tiles * split + at_once - 1) / at_once;
       const float t = waves * ((kblocks + split - 1) / split) * f.stage + 8.f * f.bn + (split > 1 ? 1300.f : 0.f);
-      if (best.bn == 0 || t < least) { best.bn = f.bn; best.split = split; best.pair = f.pair; least = t; }
+      if (best.bn == 0 || t < least) { best.bn = f.bn; best.split = split; best.pair = f.pair; best.ns = least = t; }
     }
   }
   return best;
@@ -531,7 +544,7 @@ int launch_gemm(const Matrix& a, const Matrix& b, typename E::Args& A, cudaStrea
     if (!dmxh::cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMost - E::kOwnShared))) return DMX_ERR_CUDA;
     set.fetch_or(bit, std::memory_order_relaxed);
   }
-  const int64_t tiles = (int64_t)A.tilesA * A.tilesB;
+  const int64_t tiles = (int64_t)A.tilesA * A.tilesB * (E::kRanged ? A.ranges : 1);
   constexpr int per = PAIR ? 2 : SPLIT;
   if (tiles * per > 0x7fffffff) return DMX_ERR_ARG;
   cudaLaunchConfig_t cfg = {};
@@ -563,6 +576,8 @@ void lay_out(Matrix& m, unsigned char*& ws, Jobs& jobs, int& n);
 // y = A B^T, times *unit (device memory) if there is one, rounded to bf16. mn: the operand's rows run along D's extent.
 int plain_product(const Matrix& a, int mnA, const Matrix& b, int mnB, int64_t k, const float* unit, bf16* y, int64_t ldy, cudaStream_t st);
 
+// what it takes at the rates that `choose` goes by
+float plain_product_ns(int64_t rowsA, int64_t rowsB, int64_t k, int mnA);
 // the cross entropy's count of warps that gave up
 bool loss_gave_up(unsigned* n);
 

@@ -124,8 +124,10 @@ template <bool SWAP, bool UNIT>
 struct LinearEpilogue {
   typedef GemmArgs Args;
   static constexpr int kStaging = 2048, kOwnShared = 0;
-  float bias = 0.f;
+  static constexpr bool kRanged = false;
+  float bias;
   __device__ __forceinline__ void begin(const Args& A, int r0, int c0, int lane) {
+    bias = 0.f;
     if (SWAP && A.bias && r0 + lane < A.rowsA) bias = bf_value(__ldg(reinterpret_cast<const unsigned short*>(A.bias) + r0 + lane));
     if (!SWAP && A.bias && c0 < A.rowsB) asm volatile("prefetch.global.L1 [%0];" ::"l"(A.bias + c0));
   }
@@ -335,6 +337,8 @@ int plain_product(const Matrix& a, int mnA, const Matrix& b, int mnB, int64_t k,
   E.y = y; E.ldy = ldy; E.unit = unit;
   return unit ? product<true>(a, mnA, b, mnB, k, E, st) : product<false>(a, mnA, b, mnB, k, E, st);
 }
+
+float plain_product_ns(int64_t rowsA, int64_t rowsB, int64_t k, int mnA) { return form_of(rowsA, rowsB, (int)((k + kBK - 1) / kBK), mnA).choice.ns; }
 
 }  // namespace dmx_gemm
 

@@ -299,3 +299,16 @@ def test_refusals():
         with pytest.raises(D.DmxError):
             call()
     torch.cuda.synchronize()
+
+
+# few words or few rows: products of few tiles over a long k, whose ranges are added by a launch of their own
+@pytest.mark.parametrize("N,V,n", [(1, 30522, 264), (5, 20011, 72), (64, 9000, 1024), (130, 30000, 136), (16000, 10, 64), (9999, 300, 40), (5000, 65, 300), (2048, 2000, 24), (2049, 2000, 24)])
+def test_few_tiles_over_a_long_extent(N, V, n):
+    torch, D = _d()
+    x, w, t, b = problem(torch, N, V, n)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    a = compare(torch, D, x, w, t, b, dloss=torch.rand(N, generator=g, device="cuda") / N)
+    wide = (torch.zeros(N, n + 3, device="cuda", dtype=torch.bfloat16)[:, :n], torch.zeros(V, n + 3, device="cuda", dtype=torch.bfloat16)[:, 3:], None)
+    g = torch.Generator(device="cuda").manual_seed(7)
+    again = D.linear_cross_entropy_backward(torch.rand(N, generator=g, device="cuda") / N, x, w, t, a[1], b, need=(True, True, False), out=wide)
+    assert torch.equal(again[0], a[2]) and torch.equal(again[1], a[3])
