@@ -27,6 +27,7 @@ namespace {
 
 using namespace dmx_gemm;
 using dmx_act::ex2;
+using dmx_act::ex2_2;
 
 constexpr int kFewRows = 2048;          // whose largest dloss every warp finds while the first tile is on its way; a launch of its own takes 2.5 us
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
@@ -79,12 +80,13 @@ struct SumEpilogue {
   static constexpr bool kRanged = false;
   float2 all;                     // of the row so far
   float hit;                      // its target's logit, if that is among them, else -inf
-  int64_t target;
-  __device__ __forceinline__ void begin(const Args& A, int r0, int c0, int lane) {
+  int target;                     // -1: none (extents fit an int)
+  int64_t next_target;
+  __device__ __forceinline__ void fetch(const Args& A, int r0, int lane) { next_target = r0 + lane < A.rowsA ? target_at(A.target, A.wide_target, r0 + lane) : -1; }
+  __device__ __forceinline__ void begin(const Args& A, int, int c0, int) {
     all = make_float2(-INFINITY, 0.f);
     hit = -INFINITY;
-    target = r0 + lane < A.rowsA ? target_at(A.target, A.wide_target, r0 + lane) : -1;
-    if (target >= A.rowsB) target = -1;
+    target = next_target >= 0 && next_target < A.rowsB ? (int)next_target : -1;
     if (A.bias && c0 < A.rowsB) asm volatile("prefetch.global.L1 [%0];" ::"l"(A.bias + c0));
   }
   template <int NC>
@@ -95,26 +97,27 @@ struct SumEpilogue {
       for (int i = 0; i < NC; ++i)
         if (c0 + i >= A.rowsB) v[i] = -INFINITY;
     }
-    const bool here = target >= c0 && target < c0 + NC;
-    if (__any_sync(0xffffffffu, here)) {
+    const unsigned place = (unsigned)((int)target - c0);
+    if (__any_sync(0xffffffffu, place < (unsigned)NC)) {
 #pragma unroll
-      for (int i = 0; i < NC; ++i)
-        if (here && target == c0 + i) hit = v[i];
-      if (here && !A.loss) A.hit[r0 + lane] = hit;
+      for (int i = 0; i < NC; ++i) hit = place == (unsigned)i ? v[i] : hit;
+      if (place < (unsigned)NC && !A.loss) A.hit[r0 + lane] = hit;
     }
-    float m[4], e[4];             // four chains each: the epilogue's latency, not its instructions, is what short products wait for
+    float m[4];                   // several chains: the epilogue's latency is what short products wait for
 #pragma unroll
-    for (int j = 0; j < 4; ++j) m[j] = v[j];
+    for (int j = 0; j < 4; ++j) {
+      m[j] = v[j * (NC / 4)];
 #pragma unroll
-    for (int i = 4; i < NC; ++i) m[i & 3] = fmaxf(m[i & 3], v[i]);
+      for (int i = 1; i + 1 < NC / 4; i += 2) m[j] = fmaxf(fmaxf(m[j], v[j * (NC / 4) + i]), v[j * (NC / 4) + i + 1]);
+      m[j] = fmaxf(m[j], v[(j + 1) * (NC / 4) - 1]);
+    }
     const float most = fmaxf(all.x, fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])) * kLog2e);
     const float from = most == -INFINITY ? 0.f : most;         // (nothing but -inf so far)
-    e[0] = all.y * ex2(all.x - from);
+    float2 e[2] = {make_float2(all.y * ex2(all.x - from), 0.f), two(0.f)};
 #pragma unroll
-    for (int j = 1; j < 4; ++j) e[j] = 0.f;
-#pragma unroll
-    for (int i = 0; i < NC; ++i) e[i & 3] += ex2(fmaf(v[i], kLog2e, -from));
-    all = make_float2(most, (e[0] + e[1]) + (e[2] + e[3]));
+    for (int i = 0; i < NC / 2; ++i) e[i & 1] = add2(e[i & 1], ex2_2(fma2(make_float2(v[2 * i], v[2 * i + 1]), two(kLog2e), two(-from))));
+    const float2 s = add2(e[0], e[1]);
+    all = make_float2(most, s.x + s.y);
   }
   // The four warps that share rows meet in shared memory, in two places by turns; the accumulators are handed back afterwards, so that
   // nobody is so far ahead that it writes where the first still reads.
@@ -146,8 +149,8 @@ struct SumEpilogue {
     for (int g = 0; g < 3; ++g) all = joined(all, m.pair[turn][quarter][g][lane]);
     if (r0 + lane >= A.rowsA) return true;
     if (A.loss) {
-      if (target >= 0 && target < A.rowsB) {
-        const int g = (int)target / 32 % 4;                    // which warp had it: chunks go to them in turn
+      if (target >= 0) {
+        const int g = target / 32 % 4;                    // which warp had it: chunks go to them in turn
         if (g > 0) hit = m.hit[turn][quarter][g - 1][lane];
       }
       const float l = lse_of(all);
@@ -211,7 +214,18 @@ struct SlopeEpilogue {
   static constexpr bool kRanged = false;
   float lse2, scale, units = 0.f;
   bool every;                     // all of the warp's rows have a slope
-  int64_t target;
+  int target;                     // in the piece; outside of it where it lies elsewhere, far below where there is none
+  int64_t next_target;
+  float next_lse, next_dloss;
+  __device__ __forceinline__ void fetch(const Args& A, int r0, int lane) {
+    const int n = r0 + lane;
+    next_target = -1;
+    next_lse = next_dloss = 0.f;
+    if (n >= A.rowsA) return;
+    next_target = target_at(A.target, A.wide_target, n);
+    next_lse = __ldg(A.lse + n);
+    next_dloss = __ldg(A.dloss + n * A.stride);
+  }
   __device__ __forceinline__ void begin(const Args& A, int r0, int c0, int lane) {
     if (units == 0.f) {
       if (A.find_unit) {
@@ -227,33 +241,28 @@ struct SlopeEpilogue {
       }
     }
     if (A.bias && c0 < A.rowsB) asm volatile("prefetch.global.L1 [%0];" ::"l"(A.bias + c0));
-    lse2 = scale = 0.f;
-    target = -1;
-    const int n = r0 + lane;
-    if (n < A.rowsA) {
-      const int64_t t = target_at(A.target, A.wide_target, n);
-      if (t >= 0 && t < A.vocabulary) {
-        scale = __ldg(A.dloss + n * A.stride) / units;
-        target = t - A.first;
-      }
-      lse2 = __ldg(A.lse + n) * kLog2e;
-    }
+    const bool live = next_target >= 0 && next_target < A.vocabulary;
+    lse2 = next_lse * kLog2e;
+    scale = live ? next_dloss / units : 0.f;
+    target = live ? (int)next_target - A.first : -0x40000000;
     every = __all_sync(0xffffffffu, scale != 0.f);
   }
   template <int NC>
   __device__ __forceinline__ void chunk(const Args& A, float (&v)[NC], uint4* stage, int r0, int c0, int lane) {
     add_bias(A.bias, A.rowsB, v, c0);
 #pragma unroll
-    for (int i = 0; i < NC; ++i) v[i] = ex2(fmaf(v[i], kLog2e, -lse2)) * scale;
+    for (int i = 0; i < NC / 2; ++i) {
+      const float2 p = mul2(ex2_2(fma2(make_float2(v[2 * i], v[2 * i + 1]), two(kLog2e), two(-lse2))), two(scale));
+      v[2 * i] = p.x; v[2 * i + 1] = p.y;
+    }
     if (!every) {                 // a row without a target has scale 0: its values are zeros whatever its logits are
 #pragma unroll
       for (int i = 0; i < NC; ++i) v[i] = scale == 0.f ? 0.f : v[i];
     }
-    const bool here = target >= c0 && target < c0 + NC;
-    if (__any_sync(0xffffffffu, here)) {
+    const unsigned place = (unsigned)((int)target - c0);
+    if (__any_sync(0xffffffffu, place < (unsigned)NC)) {
 #pragma unroll
-      for (int i = 0; i < NC; ++i)
-        if (here && target == c0 + i) v[i] -= scale;
+      for (int i = 0; i < NC; ++i) v[i] -= place == (unsigned)i ? scale : 0.f;
     }
 #pragma unroll
     for (int u = 0; u < NC / 8; ++u)
@@ -293,6 +302,7 @@ struct AddEpilogue {
   typedef AddArgs Args;
   static constexpr int kStaging = 2048, kOwnShared = 0;
   static constexpr bool kRanged = false;
+  __device__ __forceinline__ void fetch(const Args&, int, int) {}
   __device__ __forceinline__ void begin(const Args&, int, int, int) {}
   template <int NC>
   __device__ __forceinline__ void chunk(const Args& A, float (&v)[NC], uint4* stage, int r0, int c0, int lane) {
@@ -349,6 +359,7 @@ struct PartEpilogue {
   static constexpr int kStaging = 0, kOwnShared = 0;
   static constexpr bool kRanged = true;
   int range;
+  __device__ __forceinline__ void fetch(const Args&, int, int) {}
   __device__ __forceinline__ void begin(const Args&, int, int, int) {}
   template <int NC>
   __device__ __forceinline__ void chunk(const Args& A, float (&v)[NC], uint4*, int r0, int c0, int lane) {

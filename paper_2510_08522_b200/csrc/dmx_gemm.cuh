@@ -202,7 +202,7 @@ __device__ __forceinline__ void load_tile(const bf16* p, int64_t ld, int vec, ui
 // That halves what an SM has to fetch per product: 128 x 256 tiles by single CTAs are bound by the traffic out of L2
 // (8192^3: 820 TFLOP/s).
 // SPLIT: that many CTAs (a cluster) share a tile's k; each then completes 1/SPLIT of every 32 columns.
-// E: what becomes of D. A warp calls begin for a tile before it waits for it, chunk for every 32 columns (or its share of them) of its 32 rows,
+// E: what becomes of D. A warp calls fetch for a tile's rows a tile ahead, begin for a tile before it waits for it, chunk for every 32 columns (or its share of them) of its 32 rows,
 // a row per lane, and end (false: a wait in it ran out) before it hands the accumulators back; setup initializes what barriers end has.
 // With kRanged k is cut into A.ranges parts, each a D of its own (E's member `range` says which). kStaging: bytes of a warp's staging buffer (2048, or 0 if it uses none), kOwnShared: shared memory that E declares itself.
 template <int BN, bool PAIR, int SPLIT, class E>
@@ -354,24 +354,32 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
     uint4* stage = staging + e * 128;
     unsigned buf = 0, aph = 0;
     E epilogue;
+    int ta = 0, tb = 0;
+    if (first < tiles) {
+      tile_at(first, ta, tb);
+      epilogue.fetch(A, ta * kRows + side * kBM + quarter * 32, lane);
+    }
     for (int t = first; t < tiles && ok; t += step) {
-      int ta, tb;
-      tile_at(t, ta, tb);
       const int r0 = ta * kRows + side * kBM + quarter * 32;
       if constexpr (E::kRanged) epilogue.range = t / every;
       epilogue.begin(A, r0, tb * BN + group * 32, lane);            // fetches before the wait
+      const int tb_now = tb;
+      if (t + step < tiles) {                                       // what the next tile's rows need is on its way meanwhile
+        tile_at(t + step, ta, tb);
+        epilogue.fetch(A, ta * kRows + side * kBM + quarter * 32, lane);
+      }
       ok = warp_wait(smem_addr(&done[buf]), aph);
       if (!ok) break;
       tmem_fence_after();
       if constexpr (SPLIT == 1) {
         for (int c = group; c < kChunks; c += kEpiWarps / 4) {
-          const int c0 = tb * BN + c * 32;
+          const int c0 = tb_now * BN + c * 32;
           if (c0 >= A.rowsB) break;
           float v[32];
           tmem_load32(tmem + buf * BN + c * 32 + ((unsigned)(quarter * 32) << 16), v);
           epilogue.template chunk<32>(A, v, stage, r0, c0, lane);
         }
-        ok = epilogue.end(A, r0, tb, group, lane, buf, aph);
+        ok = epilogue.end(A, r0, tb_now, group, lane, buf, aph);
         tmem_fence_before();
         __syncwarp();
         if (lane == 0) {
@@ -383,7 +391,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       } else {
         // one tile per cluster, at most one chunk per warp: what others complete goes to them, the rest stays
         static_assert(SPLIT == 1 || kChunks <= kEpiWarps / 4, "a warp keeps its chunk in registers");
-        const int c0 = tb * BN + group * 32;
+        const int c0 = tb_now * BN + group * 32;
         const bool mine = group < kChunks && c0 < A.rowsB;
         float v[32], own[kOwn];
         float* slots = sums + (size_t)group * SPLIT * kOwn * kBM + quarter * 32 + lane;       // [SPLIT sources][kOwn][128]

@@ -126,6 +126,7 @@ struct LinearEpilogue {
   static constexpr int kStaging = 2048, kOwnShared = 0;
   static constexpr bool kRanged = false;
   float bias;
+  __device__ __forceinline__ void fetch(const Args&, int, int) {}
   __device__ __forceinline__ void begin(const Args& A, int r0, int c0, int lane) {
     bias = 0.f;
     if (SWAP && A.bias && r0 + lane < A.rowsA) bias = bf_value(__ldg(reinterpret_cast<const unsigned short*>(A.bias) + r0 + lane));
