@@ -636,7 +636,8 @@ int dmx_embedding_backward(int64_t N, int64_t V, int64_t D, int id_bytes, const 
  * A row whose target lies outside 0..V-1 (an ignored place) has loss 0 and no gradient; its lse is computed all the same. backward
  * computes the logits again and goes through the vocabulary in pieces: the workspace holds a piece of G (512 MB at most, or 256 words), and,
  * where there are several, dx in fp32. Everything up to a store is fp32, with one exception: G is rounded to bf16 before the two
- * products (the tensor cores take 16-bit operands), in units of the largest finite |dloss|'s significand; dbias is summed from the unrounded G. Exponentials are good to 2 ulp. Logits
+ * products (the tensor cores take 16-bit operands), in units of the largest finite |dloss|'s significand; dbias is summed from the unrounded G. Exponentials are good to 2 ulp and 0 below 2^-126; the tensor cores'
+ * sums of D products may truncate at every step (lse of D = 4000 is good to 5e-6 of the logits' size). Logits
  * of -inf (a bias of -inf) are words that do not occur; a logit of +inf or NaN makes its row's loss and gradient NaN, as does a row without
  * any finite logit.
  *   x, w, bias, dx, dw, dbias   bf16, row-major, ld* = elements from row to row (>= 0; of outputs >= D unless there is one row; inputs may
@@ -646,8 +647,11 @@ int dmx_embedding_backward(int64_t N, int64_t V, int64_t D, int id_bytes, const 
  *   target     N integers of target_bytes (4 or 8) bytes, aligned to their size
  *   loss, lse, dloss   fp32, N entries; dloss with a stride in elements (0: one value for all rows)
  *   dx, dw, dbias   each may be NULL and is then not computed
- *   workspace  at least dmx_cross_entropy_workspace(...) / dmx_cross_entropy_backward_workspace(...) bytes for the same arguments, 256-byte
- *              aligned, contents undefined
+ *   workspace  at least dmx_cross_entropy_workspace(...) (8 bytes for each row and 64 to 256 words) / dmx_cross_entropy_backward_workspace(...) bytes for
+ *              the same arguments, 256-byte aligned, contents undefined
+ *   dmx_cross_entropy_plan   for inspection and tests (no device needed): how a problem is cut. plan (HOST, 11 entries) receives forward's tile width, pairing
+ *              of CTAs (0/1) and tiles across the vocabulary; the pieces and a piece's words; the gradient's first product's tile width and pairing; of
+ *              dx and of dW the tile width and ranges of k that are added afterwards (0: none)
  * N = 0 gives dW = 0 and dbias = 0. Results are bitwise reproducible. Waits inside the kernels are bounded; dmx_linear_status counts these too.
  * Errors: DMX_ERR_ARG (extents < 1 of V or D, or > DMX_LINEAR_MAX_EXTENT, strides, null pointers, workspace too small), DMX_ERR_ALIGN,
  * DMX_ERR_CUDA.
@@ -661,6 +665,7 @@ int dmx_cross_entropy_backward(int64_t N, int64_t V, int64_t D, const float* dlo
                                const void* w, int64_t ldw, const void* bias, int target_bytes, const void* target,
                                const float* lse, void* dx, int64_t lddx, void* dw, int64_t lddw, void* dbias, void* workspace,
                                int64_t workspace_bytes, void* cuda_stream);
+int dmx_cross_entropy_plan(int64_t N, int64_t V, int64_t D, int64_t* plan);
 
 /* Frees the tables and the scratch. NULL is accepted; a handle that is not live (destroyed
  * already) gives DMX_ERR_HANDLE. The caller makes sure no step of this handle is still running. */

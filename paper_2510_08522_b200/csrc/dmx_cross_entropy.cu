@@ -613,4 +613,15 @@ int dmx_cross_entropy_backward(int64_t N, int64_t V, int64_t D, const float* dlo
   return rc;
 }
 
+int dmx_cross_entropy_plan(int64_t N, int64_t V, int64_t D, int64_t* plan) {
+  if (!sizes_ok(N, V, D) || N < 1 || !plan) return DMX_ERR_ARG;
+  const Matrix x = {nullptr, N, D, D}, w = {nullptr, V, D, D};
+  const ForwardPlan f = forward_plan(x, w);
+  const BackPlan b = back_plan(x, w);
+  const Choice s = choose_rows(N, b.words < V ? b.words : V, D);
+  const int64_t values[11] = {f.choice.bn, f.choice.pair, f.parts, b.pieces, b.words, s.bn, s.pair, b.dx.bn, b.dx.ranges, b.dw.bn, b.dw.ranges};
+  for (int i = 0; i < 11; ++i) plan[i] = values[i];
+  return DMX_OK;
+}
+
 }  // extern "C"

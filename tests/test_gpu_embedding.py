@@ -239,3 +239,16 @@ def test_refusals():
         with pytest.raises(D.DmxError):
             call()
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("N", [1, 1023, 1024, 1025, 4095, 4096, 4097, 131072, 1048576, 1048577])
+def test_borders_between_the_sorts(N):
+    """One CTA's tokens and one more; a warp's rounds of 32 in all of 128 CTAs, and what no longer stays in registers."""
+    torch, D = _d()
+    g = torch.Generator(device="cuda").manual_seed(N)
+    for V in (200, 256, 65536, 70000):
+        ids = words(torch, g, N, V)
+        ids[torch.rand(N, generator=g, device="cuda") < 0.1] = -5
+        dy = torch.randn(N, 8, generator=g, device="cuda")
+        a = check(torch, D, dy, ids, V)
+        assert torch.equal(a, D.embedding_backward(dy, ids, V))
