@@ -12,7 +12,11 @@
 // target's entry is 1 - p times a power of two. (Units with the exponent would let rows of far smaller dloss underflow.)
 // With dloss inside, the entries near -dloss of all rows were rounded the same way: dx and dW were off by 0.33 % in the mean square, with
 // the unit 0.17 to 0.20 %, where one rounding of the result alone gives 0.17 %.
-// Bound: the tensor cores, 2 N V D operations forward and 6 N V D backward (the logits are computed again).
+// Bound: the tensor cores, 2 N V D operations forward and 6 N V D backward (the logits are computed again). With D up to some hundred the epilogues: a
+// tile's 65536 logits take about 2.8 us whatever D is (taking them out of TMEM alone 1.5).
+// Measured on B200, 8192 x 30522 x 1024 with bias: forward 320 us in bursts at full clock (1.6 PFLOP/s; floor 299 at the measured 1715), 385 us back to back under
+// the power limit; backward 1120 / 1340 us (896 / 1062 at the measured 1715 / 1447; storing G takes 58 us, db 46, dx's last wave of tiles 40). 128 x 10 x 64 forward 3.5 us,
+// 777 x 1000 x 513 backward 25 us.
 #include "dmx.h"
 
 #include <cuda_bf16.h>

@@ -10,6 +10,10 @@
 // small second launch adds the CTAs' in a fixed order.
 // Variance: deviations from the rounded mean are summed beside their squares, and what that mean was off is taken out again:
 // a mean a million deviations away costs the variance nothing.
+// Measured on B200 (replayed in graphs, data mostly in L2): 16384 x 1024 bf16 forward 12 us (10.4 at the measured copy rate; 14 us a call among others),
+// gradient 23 us (15.6), with a residual 29 us (20.9): about 550 instructions a row and warp at eight warps per SM, of which two fifths issue.
+// 2999 x 771 fp32, a slice of wider rows, gradient 13 us (4.3): three rows a warp, and 4.5 us for the second launch. A third CTA per SM in backward spilled (37 us),
+// weights loaded anew for every row cost 8 us, halves kept packed over the row's loop saved no instruction.
 #include <atomic>
 
 #include "dmx_f32x2.cuh"
@@ -20,13 +24,13 @@ namespace {
 using namespace dmx_rows;
 using namespace dmx_f32x2;
 
-constexpr int kMaxCluster = 8, kMaxWarps = 8;      // of a CTA that is one team
+constexpr int kMaxCluster = 8, kMaxWarps = 16;      // of a CTA that is one team
 // Rows on their way to a team: with the warps there are, more than the 40 KB that an SM has to have on its way
 constexpr int kForwardStages = 4;
-__host__ __device__ constexpr int backward_stages(int bytes) { return bytes == 2 ? 4 : 2; }
+__host__ __device__ constexpr int backward_stages(int bytes, bool wide_team) { return bytes == 2 ? (wide_team ? 3 : 4) : 2; }
 // CTAs on an SM, for their registers (a thread of backward holds its sums, 2 N, and a row's values, 2 N)
 constexpr int forward_ctas(int values, bool wide) { return values == 32 ? 3 + wide : values == 16 ? 4 + wide : 6; }
-constexpr int backward_ctas(int values, int bytes) { return values == 32 ? 2 : values == 16 ? 4 : 6; }
+constexpr int backward_ctas(int values) { return values == 32 ? 2 : values == 16 ? 4 : 6; }
 
 struct Args {
   const void *x, *dy, *add;
@@ -44,8 +48,7 @@ struct Args {
 // team's threads copy what covers the row from one 16-byte border to the next (the bytes before its start lie in the same 16, and are not used).
 template <typename T, int V, int TEAM, int N>
 struct Held {
-  static constexpr int kAccesses = N / V, kThreads = TEAM > 0 ? 128 : 256;
-  static constexpr int kForwardCtas = TEAM > 0 ? forward_ctas(N, V > 1) : 2, kBackwardCtas = TEAM > 0 ? backward_ctas(N, sizeof(T)) : 1;
+  static constexpr int kAccesses = N / V, kThreads = TEAM > 0 ? 128 : 8192 / N;
   typedef typename Vec<T, V>::type Raw;
 
   int t, size;          // access i has the columns from (i * size + t) * V on
@@ -234,7 +237,7 @@ __device__ __forceinline__ float team_sum(float v, float2 (*red)[kMaxCluster * k
 
 // (A warp's lanes stay together: those of a team without a row left take part in its sums and store nothing.)
 template <typename T, int V, int TEAM, int N>
-__global__ void __launch_bounds__(Held<T, V, TEAM, N>::kThreads, Held<T, V, TEAM, N>::kForwardCtas) forward_kernel(const __grid_constant__ Args A) {
+__global__ void __launch_bounds__(Held<T, V, TEAM, N>::kThreads, (TEAM > 0 ? forward_ctas(N, V > 1) : 2)) forward_kernel(const __grid_constant__ Args A) {
   extern __shared__ __align__(16) unsigned char raw[];
   __shared__ float2 red[2][kMaxCluster * kMaxWarps];
   typedef Held<T, V, TEAM, N> H;
@@ -289,8 +292,8 @@ __global__ void __launch_bounds__(Held<T, V, TEAM, N>::kThreads, Held<T, V, TEAM
 }
 
 template <typename T, int V, int TEAM, int N>
-__global__ void __launch_bounds__(Held<T, V, TEAM, N>::kThreads, Held<T, V, TEAM, N>::kBackwardCtas) backward_kernel(const __grid_constant__ Args A) {
-  constexpr int kStages = backward_stages(sizeof(T));
+__global__ void __launch_bounds__(Held<T, V, TEAM, N>::kThreads, (TEAM > 0 ? backward_ctas(N) : 1)) backward_kernel(const __grid_constant__ Args A) {
+  constexpr int kStages = backward_stages(sizeof(T), TEAM <= 0);
   extern __shared__ __align__(16) unsigned char raw[];     // weights, then the stages
   __shared__ float2 red[2][kMaxCluster * kMaxWarps];
   typedef Held<T, V, TEAM, N> H;
@@ -440,6 +443,8 @@ __global__ void __launch_bounds__(1024) columns_kernel(const float* part, int64_
 
 // ---------------------------------------------------------------------------------------------- host
 
+constexpr int kMostShared = 225 * 1024;
+
 // A row's team by its width: 8 lanes to 64 values, a warp to 1024, a CTA to 8192, a cluster above. (Wider teams leave fewer
 // values to a thread and add a barrier to every sum.)
 struct Plan {
@@ -451,15 +456,17 @@ Plan plan_of(int64_t M, int D, int dtype, int backward, bool wide) {      // (ba
   p.cluster = 1;
   p.threads = 128;
   p.team = D <= 64 ? 8 : D <= 1024 ? 32 : D <= 8192 ? 0 : -1;
-  p.values = D <= 256 ? 8 : D <= 512 ? 16 : 32;
+  // (backward's teams of several warps hold 16 values a thread: with 32 the two CTAs on an SM, a barrier a row, were too few warps: 4000 x 4096 bf16
+  // 44 us, with 16 33 us)
+  p.values = D <= 256 ? 8 : D <= 512 || (backward && D > 1024) ? 16 : 32;
   if (D > 1024) {
     while (p.cluster * 8192 < D) p.cluster *= 2;
     const int share = (D + p.cluster - 1) / p.cluster;
-    p.threads = ((share + 31) / 32 + 31) / 32 * 32;
+    p.threads = ((share + p.values - 1) / p.values + 31) / 32 * 32;
   }
   const int bytes = element_size(dtype), values = p.threads * p.values;              // a CTA's of one input
-  const int slots = backward ? backward_stages(bytes) * 3 * values * bytes + 4 * (p.team > 0 ? p.team * p.values : values) : kForwardStages * values * bytes;
-  int at_once = p.team > 0 ? (backward ? backward_ctas(p.values, bytes) : forward_ctas(p.values, wide)) : (backward ? 256 : 512) / p.threads;
+  const int slots = backward ? backward_stages(bytes, p.team <= 0) * 3 * values * bytes + 4 * (p.team > 0 ? p.team * p.values : values) : kForwardStages * values * bytes;
+  int at_once = p.team > 0 ? (backward ? backward_ctas(p.values) : forward_ctas(p.values, wide)) : 512 / p.threads;
   const int fit = 224 * 1024 / (slots + 2048);
   at_once = fit < 1 ? 1 : at_once > fit ? fit : at_once;
   const int rows = p.team > 0 ? 128 / p.team : 1;
@@ -468,33 +475,40 @@ Plan plan_of(int64_t M, int D, int dtype, int backward, bool wide) {      // (ba
   return p;
 }
 
-template <typename T, int V, int TEAM, int N>
-int launch(const Args& A, const Plan& p, int backward, cudaStream_t st) {
-  const dim3 grid((unsigned)(p.groups * p.cluster));
+template <typename T, int V, int TEAM, int N, bool BACK>
+int launch(const Args& A, const Plan& p, cudaStream_t st) {
   typedef Held<T, V, TEAM, N> H;
-  int shared = backward ? backward_stages(sizeof(T)) * (A.add ? 3 : 2) * H::stage_bytes(p.threads) + 4 * N * (TEAM > 0 ? TEAM : p.threads) : kForwardStages * H::stage_bytes(p.threads);
-  if (backward && TEAM > 0 && shared < 4 * 2 * N * 32 * 4) shared = 4 * 2 * N * 32 * 4;        // the warps' sums
-  static std::atomic<uint64_t> set[2];                    // devices on which the kernel may use that much
+  const dim3 grid((unsigned)(p.groups * p.cluster));
+  int shared = kForwardStages * H::stage_bytes(p.threads);
+  void (*kernel)(const Args);
+  if constexpr (BACK) {
+    kernel = backward_kernel<T, V, TEAM, N>;
+    shared = backward_stages(sizeof(T), TEAM <= 0) * (A.add ? 3 : 2) * H::stage_bytes(p.threads) + 4 * N * (TEAM > 0 ? TEAM : p.threads);
+    if (TEAM > 0 && shared < 4 * 2 * N * 32 * 4) shared = 4 * 2 * N * 32 * 4;        // the warps' sums
+  } else {
+    kernel = forward_kernel<T, V, TEAM, N>;
+  }
+  static std::atomic<uint64_t> set{0};                    // devices on which the kernel may use that much
   int device = 0;
   if (!dmxh::cuda_ok(cudaGetDevice(&device))) return DMX_ERR_CUDA;
   const uint64_t bit = (uint64_t)1 << (device & 63);
-  if (!(set[backward].load(std::memory_order_relaxed) & bit) || device > 63) {
-    constexpr int kMost = 225 * 1024;
-    const auto f = backward ? cudaFuncSetAttribute(backward_kernel<T, V, TEAM, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost)
-                            : cudaFuncSetAttribute(forward_kernel<T, V, TEAM, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMost);
-    if (!dmxh::cuda_ok(f)) return DMX_ERR_CUDA;
-    set[backward].fetch_or(bit, std::memory_order_relaxed);
+  if (!(set.load(std::memory_order_relaxed) & bit) || device > 63) {
+    if (!dmxh::cuda_ok(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared))) return DMX_ERR_CUDA;
+    set.fetch_or(bit, std::memory_order_relaxed);
   }
-  return backward ? start(grid, p.threads, p.cluster, shared, st, backward_kernel<T, V, TEAM, N>, A) : start(grid, p.threads, p.cluster, shared, st, forward_kernel<T, V, TEAM, N>, A);
+  return start(grid, p.threads, p.cluster, shared, st, kernel, A);
+}
+template <typename T, int V, bool BACK>
+int launch(const Args& A, const Plan& p, cudaStream_t st) {
+  constexpr int kTeamValues = BACK ? 16 : 32;
+  if (p.team == 8) return launch<T, V, 8, 8, BACK>(A, p, st);
+  if (p.team < 0) return launch<T, V, -1, kTeamValues, BACK>(A, p, st);
+  if (p.team == 0) return launch<T, V, 0, kTeamValues, BACK>(A, p, st);
+  if (p.values == 8) return launch<T, V, 32, 8, BACK>(A, p, st);
+  return p.values == 16 ? launch<T, V, 32, 16, BACK>(A, p, st) : launch<T, V, 32, 32, BACK>(A, p, st);
 }
 template <typename T, int V>
-int launch(const Args& A, const Plan& p, int backward, cudaStream_t st) {
-  if (p.team == 8) return launch<T, V, 8, 8>(A, p, backward, st);
-  if (p.team < 0) return launch<T, V, -1, 32>(A, p, backward, st);
-  if (p.team == 0) return launch<T, V, 0, 32>(A, p, backward, st);
-  if (p.values == 8) return launch<T, V, 32, 8>(A, p, backward, st);
-  return p.values == 16 ? launch<T, V, 32, 16>(A, p, backward, st) : launch<T, V, 32, 32>(A, p, backward, st);
-}
+int launch(const Args& A, const Plan& p, int backward, cudaStream_t st) { return backward ? launch<T, V, true>(A, p, st) : launch<T, V, false>(A, p, st); }
 int launch(const Args& A, const Plan& p, int dtype, bool wide, int backward, cudaStream_t st) {
   if (dtype == DMX_F32) return wide ? launch<float, 4>(A, p, backward, st) : launch<float, 1>(A, p, backward, st);
   return wide ? launch<bf16, 8>(A, p, backward, st) : launch<bf16, 1>(A, p, backward, st);
