@@ -47,8 +47,7 @@ __device__ __forceinline__ typename Vec<T, V>::type narrow(const float* x) {
   else return make_uint4(pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7]));
 }
 
-// A load where `live`, else zeros. Loads written this way are issued where they stand, however far behind their first use is (the
-// compiler moves plain conditional ones to it, one latency after another).
+// A load where `live`, else zeros, issued where it stands (a plain conditional load may move towards its use).
 __device__ __forceinline__ void load_if(uint4& r, const void* p, bool live) {
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\tmov.u32 %0, 0;\n\tmov.u32 %1, 0;\n\tmov.u32 %2, 0;\n\tmov.u32 %3, 0;\n\t@p ld.global.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
                : "=&r"(r.x), "=&r"(r.y), "=&r"(r.z), "=&r"(r.w) : "l"(p), "r"((unsigned)live) : "memory");

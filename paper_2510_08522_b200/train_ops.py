@@ -1,5 +1,6 @@
 """The training operators of include/dmx.h for torch callers: AdamW over many tensors, group norm with an
-activation on channels-last data, and the matrix product with bias, activation and residual in its epilogue.
+activation on channels-last data, layer norm, the embedding lookup, and the matrix product with bias, activation and residual in its
+epilogue or with the cross entropy of its rows.
 
 Tensors in, raw pointers through the C ABI; every call runs on the current stream of its tensors' device, takes its
 workspace from torch's allocator there, and raises DmxError with the library's code for arguments it refuses.
