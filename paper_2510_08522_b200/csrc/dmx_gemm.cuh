@@ -252,16 +252,29 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
   const unsigned tmem = tmem_base;
   bool ok = true;
 
-  // tile t: A tiles in bands of 16, B tiles across a band, so that what runs at once shares its operands in L2
-  auto tile_at = [&](int t, int& ta, int& tb) {
+  // Tiles in turn, from the CTA's first by steps: A tiles in bands of 16, B tiles across a band, so that what runs at once shares its
+  // operands in L2. (A band and a place in it are kept: divisions by the problem's extents cost an epilogue over a short k a tenth of its time.)
+  const int band = 16 * A.tilesB;
+  struct Walk {
+    int t, b, in;
+  };
+  auto from = [&](int t) { return Walk{t, E::kRanged ? 0 : t / band, E::kRanged ? 0 : t % band}; };
+  auto next = [&](Walk& w) {
+    w.t += step;
+    w.in += step;
+    while (w.in >= band) { w.in -= band; ++w.b; }
+  };
+  auto place = [&](const Walk& w, int& ta, int& tb) {
+    int b = w.b, in = w.in;
     if constexpr (E::kRanged) {
-      const int range = t / every;
-      t -= range * every;
+      const int range = w.t / every, t = w.t - range * every;
       kb0 = (int)((int64_t)A.kblocks * range / A.ranges);
       kb1 = (int)((int64_t)A.kblocks * (range + 1) / A.ranges);
+      b = t / band;
+      in = t - b * band;
     }
-    const int band = 16 * A.tilesB, b = t / band, in = t - b * band, h = min(16, A.tilesA - 16 * b);
-    tb = in / h;
+    const int h = min(16, A.tilesA - 16 * b);
+    tb = h == 16 ? in >> 4 : in / h;
     ta = 16 * b + in - tb * h;
   };
 
@@ -270,9 +283,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
     {
       int s = 0, issued = 0;
       unsigned ph = 0;
-      for (int t = first; t < tiles && ok; t += step) {
+      for (Walk w = from(first); w.t < tiles && ok; next(w)) {
         int ta, tb;
-        tile_at(t, ta, tb);
+        place(w, ta, tb);
         for (int kb = kb0; kb < kb1; ++kb) {
           ok = warp_wait(smem_addr(&empty[s]), ph ^ 1);
           if (!ok) break;
@@ -314,10 +327,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
       const unsigned stepA = A.mnA ? 2048 >> 4 : 32 >> 4, stepB = A.mnB ? 2048 >> 4 : 32 >> 4;
       int s = 0;
       unsigned ph = 0, buf = 0, aph = 0;
-      for (int t = first; t < tiles && ok; t += step) {
+      for (Walk w = from(first); w.t < tiles && ok; next(w)) {
         if constexpr (E::kRanged) {
           int ta, tb;
-          tile_at(t, ta, tb);                  // (for its range of k)
+          place(w, ta, tb);                    // (for its range of k)
         }
         ok = warp_wait(smem_addr(&freed[buf]), aph ^ 1);
         if (!ok) break;
@@ -355,17 +368,19 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
     unsigned buf = 0, aph = 0;
     E epilogue;
     int ta = 0, tb = 0;
-    if (first < tiles) {
-      tile_at(first, ta, tb);
+    Walk w = from(first);
+    if (w.t < tiles) {
+      place(w, ta, tb);
       epilogue.fetch(A, ta * kRows + side * kBM + quarter * 32, lane);
     }
-    for (int t = first; t < tiles && ok; t += step) {
+    while (w.t < tiles && ok) {
       const int r0 = ta * kRows + side * kBM + quarter * 32;
-      if constexpr (E::kRanged) epilogue.range = t / every;
+      if constexpr (E::kRanged) epilogue.range = w.t / every;
       epilogue.begin(A, r0, tb * BN + group * 32, lane);            // fetches before the wait
       const int tb_now = tb;
-      if (t + step < tiles) {                                       // what the next tile's rows need is on its way meanwhile
-        tile_at(t + step, ta, tb);
+      next(w);
+      if (w.t < tiles) {                                            // what the next tile's rows need is on its way meanwhile
+        place(w, ta, tb);
         epilogue.fetch(A, ta * kRows + side * kBM + quarter * 32, lane);
       }
       ok = warp_wait(smem_addr(&done[buf]), aph);

@@ -252,3 +252,22 @@ def test_borders_between_the_sorts(N):
         dy = torch.randn(N, 8, generator=g, device="cuda")
         a = check(torch, D, dy, ids, V)
         assert torch.equal(a, D.embedding_backward(dy, ids, V))
+
+
+def test_a_table_of_more_than_2_to_24_rows():
+    """Four passes of the sort, in one CTA and in several."""
+    torch, D = _d()
+    g = torch.Generator(device="cuda").manual_seed(1)
+    V = 20_000_003
+    for N in (3000, 9000):
+        ids = torch.randint(0, V, (N,), generator=g, device="cuda")
+        ids[::3] = ids[0]
+        ids[1::7] = V - 1
+        dy = torch.randn(N, 4, generator=g, device="cuda")
+        got = D.embedding_backward(dy, ids, V)
+        rows, back = ids.unique(return_inverse=True)
+        want, size, _ = definition(torch, dy, back, len(rows), 1.0)
+        assert ((got[rows].double() - want).abs() <= size + U * want.abs()).all()
+        got[rows] = 0
+        assert not got.any()
+        assert torch.equal(D.embedding(ids, got), torch.zeros(N, 4, device="cuda"))
