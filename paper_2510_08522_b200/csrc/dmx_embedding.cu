@@ -9,8 +9,8 @@
 // tokens reach over chunks leaves fp32 sums, one per chunk, which a last launch joins. Work is cut by tokens, not by rows: how
 // often a token comes does not matter. Nothing is added atomically but whole numbers; the order of all sums is fixed by the shape and the ids.
 // Measured on B200 (replayed in graphs, data mostly in L2): forward of 32768 x 1024 bf16 17 us (20.2 at the measured copy rate), unaligned 29 us. Gradient of 16384
-// tokens in 30522 x 1024 bf16 38 us (14.9): six launches in a row, sort and zeros 20 us, sums 10, joins 6; 64 tokens 8 us; 65536 tokens added to 50257 x 771
-// fp32 82 us (46).
+// tokens in 30522 x 1024 bf16 36 us (14.9): six launches in a row, sort 14 us and 5 more for zeros meanwhile, sums 11, joins 6; 64 tokens 8 us; 65536 tokens
+// added to 50257 x 771 fp32 80 us (46).
 #include <atomic>
 #include <type_traits>
 
@@ -417,8 +417,8 @@ __device__ __forceinline__ void finish_row(const SumArgs& A, unsigned v, const C
 // T: type of dy, O: of the table's gradient. A warp: a chunk of the sorted tokens, 32 x W columns, `kAhead` rows of dy on their way at a time,
 // with ADD also what the table holds where a row ends.
 template <typename T, typename O, int W, bool WIDE, bool ADD>
-__global__ void __launch_bounds__(256, 3) sum_kernel(const __grid_constant__ SumArgs A) {
-  constexpr int kAhead = ADD ? 4 : 8;
+__global__ void __launch_bounds__(256, 2) sum_kernel(const __grid_constant__ SumArgs A) {
+  constexpr int kAhead = ADD ? 8 : 16;
   start_dependents();
   wait_for_previous();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -538,9 +538,10 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ SumAr
 
 // ---------------------------------------------------------------------------------------------- host
 
-// Tokens a chunk: enough chunks for 24 warps on every SM, and eight tokens at least (a batch of loads). W: columns a lane.
+// Tokens a chunk: enough chunks for 16 warps on every SM, as many as there is room for, and eight tokens at least. W: columns a lane. (Sixteen rows on
+// their way in each of 16 warps beat eight in each of 24: 131072 tokens of 1024 bf16 92 and 94 us, added to a table 88 and 93.)
 int chunk_of(int64_t N, int64_t D, int W) {
-  const int64_t slices = (D + 32 * W - 1) / (32 * W), chunks = (148 * 24 + slices - 1) / slices;
+  const int64_t slices = (D + 32 * W - 1) / (32 * W), chunks = (148 * 16 + slices - 1) / slices;
   const int64_t per = (N + chunks - 1) / chunks;
   return (int)((per + 7) / 8 * 8);
 }
@@ -641,7 +642,7 @@ int dmx_embedding_backward(int64_t N, int64_t V, int64_t D, int id_bytes, const 
       if (!dmxh::cuda_ok(cudaFuncSetAttribute(sort_few_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared + kFewTokens * 8))) return DMX_ERR_CUDA;
       set.fetch_or(bit, std::memory_order_relaxed);
     }
-    rc = start(dim3(S.zero ? 148 : 1), kSortThreads, 1, shared, st, sort_few_kernel, S);
+    rc = start(dim3(S.zero ? 296 : 1), kSortThreads, 1, shared, st, sort_few_kernel, S);
   }
   for (int i = 0; i < passes && N > kFewTokens && rc == DMX_OK; ++i) {
     S.shift = 8 * i;
@@ -654,7 +655,7 @@ int dmx_embedding_backward(int64_t N, int64_t V, int64_t D, int id_bytes, const 
     const int64_t v0 = V * i / passes, v1 = V * (i + 1) / passes;
     S.zero = accumulate || v1 == v0 ? nullptr : static_cast<unsigned char*>(dtable) + v0 * S.zero_ld;
     S.zero_rows = v1 - v0;
-    rc = start(dim3((unsigned)(S.ctas + (S.zero ? 148 : 0))), kSortThreads, 1, kShared, st, scatter_kernel, S);
+    rc = start(dim3((unsigned)(S.ctas + (S.zero ? 296 : 0))), kSortThreads, 1, kShared, st, scatter_kernel, S);
     S.crossing = nullptr;
   }
   if (rc != DMX_OK) return rc;
