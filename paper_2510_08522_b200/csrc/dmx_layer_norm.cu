@@ -12,7 +12,7 @@
 // a mean a million deviations away costs the variance nothing.
 // Measured on B200 (replayed in graphs, data mostly in L2): 16384 x 1024 bf16 forward 12 us (10.4 at the measured copy rate; 14 us a call among others),
 // gradient 23 us (15.6), with a residual 29 us (20.9): about 550 instructions a row and warp at eight warps per SM, of which two fifths issue.
-// 2999 x 771 fp32, a slice of wider rows, gradient 13 us (4.3): three rows a warp, and 4.5 us for the second launch. A third CTA per SM in backward spilled (37 us),
+// 2999 x 771 fp32, a slice of wider rows, gradient 13 us (4.3): three rows a warp, and 4.5 us for the second launch. A third CTA per SM in backward spilled (37 us), five warps a CTA too (40 us),
 // weights loaded anew for every row cost 8 us, halves kept packed over the row's loop saved no instruction.
 #include <atomic>
 
@@ -27,7 +27,7 @@ using namespace dmx_f32x2;
 constexpr int kMaxCluster = 8, kMaxWarps = 16;      // of a CTA that is one team
 // Rows on their way to a team: with the warps there are, more than the 40 KB that an SM has to have on its way
 constexpr int kForwardStages = 4;
-__host__ __device__ constexpr int backward_stages(int bytes, bool wide_team) { return bytes == 2 ? (wide_team ? 3 : 4) : 2; }
+__host__ __device__ constexpr int backward_stages(int bytes) { return bytes == 2 ? 3 : 2; }
 // CTAs on an SM, for their registers (a thread of backward holds its sums, 2 N, and a row's values, 2 N)
 constexpr int forward_ctas(int values, bool wide) { return values == 32 ? 3 + wide : values == 16 ? 4 + wide : 6; }
 constexpr int backward_ctas(int values) { return values == 32 ? 2 : values == 16 ? 4 : 6; }
@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(Held<T, V, TEAM, N>::kThreads, (TEAM > 0 ? for
 
 template <typename T, int V, int TEAM, int N>
 __global__ void __launch_bounds__(Held<T, V, TEAM, N>::kThreads, (TEAM > 0 ? backward_ctas(N) : 1)) backward_kernel(const __grid_constant__ Args A) {
-  constexpr int kStages = backward_stages(sizeof(T), TEAM <= 0);
+  constexpr int kStages = backward_stages(sizeof(T));
   extern __shared__ __align__(16) unsigned char raw[];     // weights, then the stages
   __shared__ float2 red[2][kMaxCluster * kMaxWarps];
   typedef Held<T, V, TEAM, N> H;
@@ -465,7 +465,7 @@ Plan plan_of(int64_t M, int D, int dtype, int backward, bool wide) {      // (ba
     p.threads = ((share + p.values - 1) / p.values + 31) / 32 * 32;
   }
   const int bytes = element_size(dtype), values = p.threads * p.values;              // a CTA's of one input
-  const int slots = backward ? backward_stages(bytes, p.team <= 0) * 3 * values * bytes + 4 * (p.team > 0 ? p.team * p.values : values) : kForwardStages * values * bytes;
+  const int slots = backward ? backward_stages(bytes) * 3 * values * bytes + 4 * (p.team > 0 ? p.team * p.values : values) : kForwardStages * values * bytes;
   int at_once = p.team > 0 ? (backward ? backward_ctas(p.values) : forward_ctas(p.values, wide)) : 512 / p.threads;
   const int fit = 224 * 1024 / (slots + 2048);
   at_once = fit < 1 ? 1 : at_once > fit ? fit : at_once;
@@ -483,7 +483,7 @@ int launch(const Args& A, const Plan& p, cudaStream_t st) {
   void (*kernel)(const Args);
   if constexpr (BACK) {
     kernel = backward_kernel<T, V, TEAM, N>;
-    shared = backward_stages(sizeof(T), TEAM <= 0) * (A.add ? 3 : 2) * H::stage_bytes(p.threads) + 4 * N * (TEAM > 0 ? TEAM : p.threads);
+    shared = backward_stages(sizeof(T)) * (A.add ? 3 : 2) * H::stage_bytes(p.threads) + 4 * N * (TEAM > 0 ? TEAM : p.threads);
     if (TEAM > 0 && shared < 4 * 2 * N * 32 * 4) shared = 4 * 2 * N * 32 * 4;        // the warps' sums
   } else {
     kernel = forward_kernel<T, V, TEAM, N>;
