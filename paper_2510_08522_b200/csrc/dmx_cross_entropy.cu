@@ -13,10 +13,10 @@
 // With dloss inside, the entries near -dloss of all rows were rounded the same way: dx and dW were off by 0.33 % in the mean square, with
 // the unit 0.17 to 0.20 %, where one rounding of the result alone gives 0.17 %.
 // Bound: the tensor cores, 2 N V D operations forward and 6 N V D backward (the logits are computed again). With D up to some hundred the epilogues: a
-// tile's 65536 logits take about 2.8 us whatever D is (taking them out of TMEM alone 1.5).
+// pair's tile of 65536 logits takes about 2.5 us whatever D is (taking them out of TMEM alone 1.5), one CTA's of 32768 2.1 us, two at a time.
 // Measured on B200, 8192 x 30522 x 1024 with bias: forward 320 us in bursts at full clock (1.6 PFLOP/s; floor 299 at the measured 1715), 385 us back to back under
 // the power limit; backward 1120 / 1340 us (896 / 1062 at the measured 1715 / 1447; storing G takes 58 us, db 46, dx's last wave of tiles 40). 128 x 10 x 64 forward 3.5 us,
-// 777 x 1000 x 513 backward 25 us.
+// 777 x 1000 x 513 backward 25 us, 8192 x 30522 x 256 forward 113, backward 414 us.
 #include "dmx.h"
 
 #include <cuda_bf16.h>
@@ -427,7 +427,8 @@ int product_rows(const Matrix& a, const Matrix& b, typename E::Args& A, const Ch
   if (c.bn == 256) return launch_gemm<256, false, 1, E>(a, b, A, st);
   return c.bn == 128 ? launch_gemm<128, false, 1, E>(a, b, A, st) : launch_gemm<64, false, 1, E>(a, b, A, st);
 }
-Choice choose_rows(int64_t N, int64_t V, int64_t D) { return choose(N, V, (int)((D + kBK - 1) / kBK), false, false); }
+Choice choose_rows(int64_t N, int64_t V, int64_t D, float weight) { return choose_by_tiles(N, V, (int)((D + kBK - 1) / kBK), false, false, weight); }
+constexpr float kSumWeight = 1.f, kSlopeWeight = 1.3f;        // of their epilogues (1.5 leaves 8192 x 30522 x 512 to single CTAs: slopes 290 us, in pairs 272)
 
 bool sizes_ok(int64_t N, int64_t V, int64_t D) {
   const int64_t most = DMX_LINEAR_MAX_EXTENT;
@@ -443,7 +444,7 @@ struct ForwardPlan {
 };
 ForwardPlan forward_plan(const Matrix& x, const Matrix& w) {
   ForwardPlan p;
-  p.choice = choose_rows(x.rows, w.rows, x.cols);
+  p.choice = choose_rows(x.rows, w.rows, x.cols, kSumWeight);
   p.parts = (w.rows + p.choice.bn - 1) / p.choice.bn;
   p.part = pad256(p.parts * x.rows * 8);
   p.hit = pad256(x.rows * 4);
@@ -452,7 +453,7 @@ ForwardPlan forward_plan(const Matrix& x, const Matrix& w) {
 }
 
 // A product with few tiles: tiles x ranges of k fill the card once. ranges 0: as plain_product does it, unless ranges take a fifth off its time
-// (a stage's time as `choose` has it, 3.5 us for the launch that adds, the parts' traffic at 4 TB/s). 16000 x 64 into 300 words: dW 21 -> 9 us.
+// (a stage's time as `choose_by_tiles` has it, 3.5 us for the launch that adds, the parts' traffic at 4 TB/s). 16000 x 64 into 300 words: dW 21 -> 9 us.
 struct Cut {
   int bn, ranges;
   int64_t bytes;
@@ -598,7 +599,7 @@ int dmx_cross_entropy_backward(int64_t N, int64_t V, int64_t D, const float* dlo
     A.bias = bias ? static_cast<const bf16*>(bias) + first : nullptr; A.target = target; A.wide_target = target_bytes == 8;
     A.first = (int)first; A.vocabulary = (int)V; A.lse = lse; A.dloss = dloss; A.unit = unit; A.find_unit = find_unit && first == 0; A.stride = N > 1 ? dloss_stride : 0;
     A.g = g; A.ldg = pad8(words); A.vec = 1; A.columns = dbias ? columns : nullptr;
-    rc = product_rows<SlopeEpilogue>(a, piece, A, choose_rows(N, words, D), st);
+    rc = product_rows<SlopeEpilogue>(a, piece, A, choose_rows(N, words, D, kSlopeWeight), st);
     if (rc == DMX_OK && dbias)
       rc = start(dim3((unsigned)((words + 31) / 32)), 1024, st, columns_kernel, (const float*)columns, (int)((N + 31) / 32), (int)words, (const float*)unit, static_cast<bf16*>(dbias) + first);
     const Matrix G = {g, N, words, A.ldg};
@@ -622,7 +623,7 @@ int dmx_cross_entropy_plan(int64_t N, int64_t V, int64_t D, int64_t* plan) {
   const Matrix x = {nullptr, N, D, D}, w = {nullptr, V, D, D};
   const ForwardPlan f = forward_plan(x, w);
   const BackPlan b = back_plan(x, w);
-  const Choice s = choose_rows(N, b.words < V ? b.words : V, D);
+  const Choice s = choose_rows(N, b.words < V ? b.words : V, D, kSlopeWeight);
   const int64_t values[11] = {f.choice.bn, f.choice.pair, f.parts, b.pieces, b.words, s.bn, s.pair, b.dx.bn, b.dx.ranges, b.dw.bn, b.dw.ranges};
   for (int i = 0; i < 11; ++i) plan[i] = values[i];
   return DMX_OK;

@@ -526,7 +526,7 @@ struct Choice {
 
 // Tile width, split and pairing, by the time they take: what a stage of 64 k took measured on 8192^3 (ns; the narrow tiles are bound
 // by what the SMs fetch from L2), the last tile's epilogue, a split's cluster barrier and exchange.
-inline Choice choose(int64_t rowsA, int64_t rowsB, int kblocks, bool swap, bool splits = true) {
+inline Choice choose(int64_t rowsA, int64_t rowsB, int kblocks, bool swap) {
   Choice best = {0, 1, false, 0.f};
   float least = 0.f;
   const struct { int bn; bool pair; float stage; } forms[6] = {{256, true, 405.f}, {256, false, 435.f}, {128, true, 290.f},
@@ -535,12 +535,36 @@ inline Choice choose(int64_t rowsA, int64_t rowsB, int kblocks, bool swap, bool 
     if (swap ? f.pair || f.bn != (rowsB <= 32 ? 32 : 64) : f.bn == 32) continue;
     const int rows = f.pair ? 2 * kBM : kBM, at_once = f.pair ? 74 : 148;
     const int64_t tiles = ((rowsA + rows - 1) / rows) * ((rowsB + f.bn - 1) / f.bn);
-    const int most = !splits ? 1 : swap ? 4 : f.pair || f.bn == 256 ? 1 : 2;
+    const int most = swap ? 4 : f.pair || f.bn == 256 ? 1 : 2;
     for (int split = 1; split <= most; split *= 2) {
       if (split > 1 && (tiles * split > 148 || kblocks / split < 2)) break;
       const int64_t waves = (tiles * split + at_once - 1) / at_once;
       const float t = waves * ((kblocks + split - 1) / split) * f.stage + 8.f * f.bn + (split > 1 ? 1300.f : 0.f);
       if (best.bn == 0 || t < least) { best.bn = f.bn; best.split = split; best.pair = f.pair; best.ns = least = t; }
+    }
+  }
+  return best;
+}
+
+// The same for products whose tiles may have little k: a tile takes the longer of its stages and its epilogue and a quarter of the other. What
+// an epilogue takes per tile (ns) was measured on the cross entropy's sums at k = 64; slopes and plain stores take `weight` times it. A single CTA's tile of
+// 256 columns then beats a pair's, whose accumulators go back and forth between two SMs: 8192 x 30522 x 256 forward 114 us against 141, at k = 1024 338 against 317.
+// A pair's of 128 columns is for one wave over a long k: dx of 2048 x 30522 x 1024 takes 3 us less than single CTAs' of 128 columns.
+inline Choice choose_by_tiles(int64_t rowsA, int64_t rowsB, int kblocks, bool swap, bool splits, float weight) {
+  Choice best = {0, 1, false, 0.f};
+  const struct { int bn; bool pair; float stage, epilogue; } forms[6] = {{256, true, 405.f, 2450.f}, {256, false, 435.f, 2000.f}, {128, true, 282.f, 1850.f},
+                                                                          {128, false, 290.f, 1400.f}, {64, false, 245.f, 1050.f}, {32, false, 200.f, 800.f}};
+  for (const auto& f : forms) {
+    if (swap ? f.pair || f.bn != (rowsB <= 32 ? 32 : 64) : f.bn == 32) continue;
+    const int rows = f.pair ? 2 * kBM : kBM, at_once = f.pair ? 74 : 148;
+    const int64_t tiles = ((rowsA + rows - 1) / rows) * ((rowsB + f.bn - 1) / f.bn);
+    const int most = !splits ? 1 : swap ? 4 : f.pair || f.bn == 256 ? 1 : 2;
+    for (int split = 1; split <= most; split *= 2) {
+      if (split > 1 && (tiles * split > 148 || kblocks / split < 2)) break;
+      const int64_t waves = (tiles * split + at_once - 1) / at_once;
+      const float k = (float)((kblocks + split - 1) / split) * f.stage, e = f.epilogue * weight;
+      const float t = waves * (k > e ? k + 0.25f * e : e + 0.25f * k) + (split > 1 ? 1300.f : 0.f);
+      if (best.bn == 0 || t < best.ns) best = {f.bn, split, f.pair, t};
     }
   }
   return best;
@@ -599,7 +623,7 @@ void lay_out(Matrix& m, unsigned char*& ws, Jobs& jobs, int& n);
 // y = A B^T, times *unit (device memory) if there is one, rounded to bf16. mn: the operand's rows run along D's extent.
 int plain_product(const Matrix& a, int mnA, const Matrix& b, int mnB, int64_t k, const float* unit, bf16* y, int64_t ldy, cudaStream_t st);
 
-// what it takes at the rates that `choose` goes by
+// what it takes with a unit, by choose_by_tiles
 float plain_product_ns(int64_t rowsA, int64_t rowsB, int64_t k, int mnA);
 // the cross entropy's count of warps that gave up
 bool loss_gave_up(unsigned* n);

@@ -263,8 +263,9 @@ struct Form {
   bool exchanged;
   Choice choice;
 };
-Form form_of(int64_t rowsA, int64_t rowsB, int kblocks, int mnA) {
+Form form_of(int64_t rowsA, int64_t rowsB, int kblocks, int mnA, bool unit = false) {
   const bool exchanged = rowsA <= 64 && !mnA;
+  if (unit) return {exchanged, exchanged ? choose_by_tiles(rowsB, rowsA, kblocks, true, true, 1.2f) : choose_by_tiles(rowsA, rowsB, kblocks, false, true, 1.2f)};
   return {exchanged, exchanged ? choose(rowsB, rowsA, kblocks, true) : choose(rowsA, rowsB, kblocks, false)};
 }
 
@@ -277,7 +278,7 @@ int product(const Matrix& a, int mnA, const Matrix& b, int mnB, int64_t k, const
   A.vecy = aligned(A.y, 16) && (rowsA <= 1 || A.ldy % 8 == 0);
   A.vecz = A.z && aligned(A.z, 16) && (rowsA <= 1 || A.ldz % 8 == 0);
   A.vecr = A.residual && aligned(A.residual, 16) && (rowsA <= 1 || A.ldr % 8 == 0);
-  const Form f = form_of(rowsA, rowsB, A.kblocks, mnA);
+  const Form f = form_of(rowsA, rowsB, A.kblocks, mnA, UNIT);
   const Choice& c = f.choice;
   if (f.exchanged) {
     A.rowsA = (int)rowsB; A.rowsB = (int)rowsA;
@@ -339,7 +340,7 @@ int plain_product(const Matrix& a, int mnA, const Matrix& b, int mnB, int64_t k,
   return unit ? product<true>(a, mnA, b, mnB, k, E, st) : product<false>(a, mnA, b, mnB, k, E, st);
 }
 
-float plain_product_ns(int64_t rowsA, int64_t rowsB, int64_t k, int mnA) { return form_of(rowsA, rowsB, (int)((k + kBK - 1) / kBK), mnA).choice.ns; }
+float plain_product_ns(int64_t rowsA, int64_t rowsB, int64_t k, int mnA) { return form_of(rowsA, rowsB, (int)((k + kBK - 1) / kBK), mnA, true).choice.ns; }
 
 }  // namespace dmx_gemm
 
