@@ -39,7 +39,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
 // ---------------------------------------------------------------------------------------------- forward
 
 __device__ __forceinline__ int64_t target_at(const void* targets, int wide, int n) {
-  return wide ? __ldg(static_cast<const long long*>(targets) + n) : (int64_t)__ldg(static_cast<const int*>(targets) + n);
+  return wide ? static_cast<const long long*>(targets)[n] : (int64_t)static_cast<const int*>(targets)[n];
 }
 
 template <int NC>
@@ -48,7 +48,7 @@ __device__ __forceinline__ void add_bias(const bf16* bias, int cols, float (&v)[
   if (c0 + NC <= cols && (reinterpret_cast<uintptr_t>(bias + c0) & 15) == 0) {
 #pragma unroll
     for (int u = 0; u < NC / 8; ++u) {
-      const uint4 b = __ldg(reinterpret_cast<const uint4*>(bias + c0) + u);
+      const uint4 b = reinterpret_cast<const uint4*>(bias + c0)[u];
       const unsigned w[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -59,7 +59,7 @@ __device__ __forceinline__ void add_bias(const bf16* bias, int cols, float (&v)[
   } else {
 #pragma unroll
     for (int i = 0; i < NC; ++i)
-      if (c0 + i < cols) v[i] += bf_value(__ldg(reinterpret_cast<const unsigned short*>(bias) + c0 + i));
+      if (c0 + i < cols) v[i] += bf_value(reinterpret_cast<const unsigned short*>(bias)[c0 + i]);
   }
 }
 
@@ -227,15 +227,15 @@ struct SlopeEpilogue {
     next_lse = next_dloss = 0.f;
     if (n >= A.rowsA) return;
     next_target = target_at(A.target, A.wide_target, n);
-    next_lse = __ldg(A.lse + n);
-    next_dloss = __ldg(A.dloss + n * A.stride);
+    next_lse = A.lse[n];
+    next_dloss = A.dloss[n * A.stride];
   }
   __device__ __forceinline__ void begin(const Args& A, int r0, int c0, int lane) {
     if (units == 0.f) {
       if (A.find_unit) {
         float most = 0.f;
 #pragma unroll 8
-        for (int n = lane; n < A.rowsA; n += 32) most = fmaxf(most, finite_size(__ldg(A.dloss + n * A.stride)));
+        for (int n = lane; n < A.rowsA; n += 32) most = fmaxf(most, finite_size(A.dloss[n * A.stride]));
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
         units = unit_of(most);
@@ -320,7 +320,7 @@ struct AddEpilogue {
       for (int i = 0; i < NC; ++i) __stcs(at + i * 32, v[i]);
       return;
     }
-    const float times = __ldg(A.unit);
+    const float times = *A.unit;
 #pragma unroll
     for (int i = 0; i < NC; ++i) v[i] *= times;
 #pragma unroll
@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(256) add_parts_kernel(const float* parts, int 
   for (int k = 0; k < ranges; ++k)
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[i] += at[k * blocks * across * 1024 + i * 32];
-  const float times = __ldg(unit);
+  const float times = *unit;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (c + i < cols) y[(int64_t)r * ldy + c + i] = __float2bfloat16_rn(s[i] * times);
@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(1024) columns_kernel(const float* sums, int ro
   __syncthreads();
   if (warp > 0 || c >= cols) return;
   for (int w = 1; w < 32; ++w) s += sh[w][lane];
-  out[c] = __float2bfloat16_rn(s * __ldg(unit));
+  out[c] = __float2bfloat16_rn(s * *unit);
 }
 
 // ---------------------------------------------------------------------------------------------- host

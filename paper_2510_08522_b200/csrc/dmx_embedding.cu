@@ -33,7 +33,7 @@ struct GatherArgs {
 };
 
 __device__ __forceinline__ int64_t id_at(const void* ids, int wide, int64_t n) {
-  return wide ? __ldg(static_cast<const long long*>(ids) + n) : (int64_t)__ldg(static_cast<const int*>(ids) + n);
+  return wide ? static_cast<const long long*>(ids)[n] : (int64_t)static_cast<const int*>(ids)[n];
 }
 
 // How a lane holds its share of 32 x W columns: W neighbours in one access (of dy's type; 16 bytes), or, where alignment allows no
@@ -429,8 +429,8 @@ __global__ void __launch_bounds__(256, 2) sum_kernel(const __grid_constant__ Sum
   const int64_t n0 = chunk * A.chunk, n1 = min(n0 + A.chunk, A.N);
   if (n0 >= A.N) return;
   const unsigned none = (unsigned)A.V;
-  const unsigned front = __ldg(A.pair + n0).x;
-  bool joined = n0 > 0 && __ldg(A.pair + n0 - 1).x == front;             // the row began in an earlier chunk
+  const unsigned front = A.pair[n0].x;
+  bool joined = n0 > 0 && A.pair[n0 - 1].x == front;             // the row began in an earlier chunk
   if (front == none) return;
   float acc[W];
 #pragma unroll
@@ -443,8 +443,8 @@ __global__ void __launch_bounds__(256, 2) sum_kernel(const __grid_constant__ Sum
   };
   bool open = false;                                                     // the last row goes on in the next chunk
   for (int64_t n = n0; n < n1; n += 32) {
-    const uint2 pair = n + lane < n1 ? __ldg(A.pair + n + lane) : make_uint2(none, 0);
-    const unsigned key = pair.x, place = pair.y, after = n + lane + 1 < A.N ? __ldg(A.pair + n + lane + 1).x : none;
+    const uint2 pair = n + lane < n1 ? A.pair[n + lane] : make_uint2(none, 0);
+    const unsigned key = pair.x, place = pair.y, after = n + lane + 1 < A.N ? A.pair[n + lane + 1].x : none;
     const unsigned some = __ballot_sync(0xffffffffu, key != none), ends = __ballot_sync(0xffffffffu, key != after) & some;
     const int count = __popc(some);                                      // (what is in no row comes last)
     for (int i = 0; i < count; i += kAhead) {
@@ -482,7 +482,7 @@ __global__ void __launch_bounds__(256, 2) sum_kernel(const __grid_constant__ Sum
   }
   if (!open) return;
   leave(joined ? 0 : 1);
-  if (!joined && slice == 0 && lane == 0) reinterpret_cast<uint2*>(A.crossing)[1 + atomicAdd(A.crossing, 1u)] = make_uint2((unsigned)chunk, __ldg(A.pair + n1).x);
+  if (!joined && slice == 0 && lane == 0) reinterpret_cast<uint2*>(A.crossing)[1 + atomicAdd(A.crossing, 1u)] = make_uint2((unsigned)chunk, A.pair[n1].x);
 }
 
 // The rows that reach over chunks, by the chunk in which they begin: a CTA takes 128 columns of one at a time, its four warps the chunks

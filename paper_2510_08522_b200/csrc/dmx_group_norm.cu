@@ -723,7 +723,7 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, ACT>) backward
     if constexpr (M == APPLY) {      // the image's sums
       for (int c = tid; c < 2 * W; c += threads) {
         const int k = c < W ? c : c - W;
-        if (k < now.Wl) mine[(c < W ? 0 : pW) + k] = __ldg(A.part + 2 * plane + ((c < W ? 0 : (int64_t)A.N) + now.n) * A.C + now.c0 + k);
+        if (k < now.Wl) mine[(c < W ? 0 : pW) + k] = A.part[2 * plane + ((c < W ? 0 : (int64_t)A.N) + now.n) * A.C + now.c0 + k];
       }
       __syncthreads();
     }
@@ -791,8 +791,8 @@ __global__ void __launch_bounds__(kMostThreads<V, M>, kCtas<V, M, ACT>) backward
 }
 
 // The chunks' sums of an image, joined between the two launches that read it. Forward: a warp per image and group.
-__global__ void __launch_bounds__(256) join_groups_kernel(const float* __restrict__ part, int64_t groups, int parts, int rows, int L, int G, int cpg,
-                                                          float eps, float* __restrict__ mean, float* __restrict__ rstd) {
+__global__ void __launch_bounds__(256) join_groups_kernel(const float* part, int64_t groups, int parts, int rows, int L, int G, int cpg,
+                                                          float eps, float* mean, float* rstd) {
   asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
   const int64_t i = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);       // image * G + group
   const int lane = threadIdx.x & 31;
@@ -802,16 +802,16 @@ __global__ void __launch_bounds__(256) join_groups_kernel(const float* __restric
   // 32nd parts by lane: each lane joins its own first
   float sum = 0.f, have = 0.f;
   for (int k = lane; k < parts; k += 32) {
-    sum = fmaf(__ldg(src + (int64_t)k * 3 * G), positions(k), sum);
+    sum = fmaf(src[(int64_t)k * 3 * G], positions(k), sum);
     have += positions(k);
   }
   const float mu = have > 0.f ? sum / have : 0.f;
   float c = 0.f, m2 = 0.f;
   for (int k = lane; k < parts; k += 32) {
     const float* p = src + (int64_t)k * 3 * G;
-    const float n = positions(k), d = (__ldg(p) - mu) + __ldg(p + 1);
+    const float n = positions(k), d = (p[0] - mu) + p[1];
     c = fmaf(n, d, c);
-    m2 += fmaf(n * (float)cpg * d, d, __ldg(p + 2));
+    m2 += fmaf(n * (float)cpg * d, d, p[2]);
   }
   const float by = have > 0.f ? c / have : 0.f;
   const float2 t = join(corrected(mu, by), squares(m2, c * (float)cpg, by), have, (float)cpg, (float)L, 32);
@@ -821,7 +821,7 @@ __global__ void __launch_bounds__(256) join_groups_kernel(const float* __restric
   }
 }
 // Backward: the rows of an image's chunks to one row, for A and for B. 32 channels and eight row lanes per CTA.
-__global__ void __launch_bounds__(256) join_rows_kernel(const float* __restrict__ part, float* __restrict__ out, int N, int parts, int C) {
+__global__ void __launch_bounds__(256) join_rows_kernel(const float* part, float* out, int N, int parts, int C) {
   __shared__ float sh[8][33];
   asm volatile("griddepcontrol.launch_dependents;\n\tgriddepcontrol.wait;" ::: "memory");
   const int lane = threadIdx.x & 31, r = threadIdx.x >> 5, blocks = (C + 31) / 32;
@@ -831,7 +831,7 @@ __global__ void __launch_bounds__(256) join_rows_kernel(const float* __restrict_
   if (c < C) {
     const float* p = part + row * parts * C + c;
 #pragma unroll 8
-    for (int i = r; i < parts; i += 8) s += __ldg(p + (int64_t)i * C);
+    for (int i = r; i < parts; i += 8) s += p[(int64_t)i * C];
   }
   sh[r][lane] = s;
   __syncthreads();
@@ -842,8 +842,8 @@ __global__ void __launch_bounds__(256) join_rows_kernel(const float* __restrict_
 }
 
 // dweight and dbias: sums of the images' rows, those of A times their group's rstd. 32 channels and 32 row lanes per CTA.
-__global__ void __launch_bounds__(1024) columns_kernel(const float* __restrict__ part, int64_t rows, int C, int G, int cpg,
-                                                      const float* __restrict__ rstd, float* __restrict__ dw, float* __restrict__ db) {
+__global__ void __launch_bounds__(1024) columns_kernel(const float* part, int64_t rows, int C, int G, int cpg,
+                                                      const float* rstd, float* dw, float* db) {
   __shared__ float sh[32][33];
   const int lane = threadIdx.x & 31, r = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
   const float* p = part + (int64_t)blockIdx.y * rows * C;
@@ -855,10 +855,10 @@ __global__ void __launch_bounds__(1024) columns_kernel(const float* __restrict__
     const float* q = rstd + c / cpg;
     if (blockIdx.y) {
 #pragma unroll 8
-      for (int64_t i = r; i < rows; i += 32) s += __ldg(p + i * C + c);
+      for (int64_t i = r; i < rows; i += 32) s += p[i * C + c];
     } else {
 #pragma unroll 8
-      for (int64_t i = r; i < rows; i += 32) s = fmaf(__ldg(p + i * C + c), __ldg(q + i * G), s);
+      for (int64_t i = r; i < rows; i += 32) s = fmaf(p[i * C + c], q[i * G], s);
     }
   }
   sh[r][lane] = s;

@@ -144,12 +144,12 @@ struct Held {
       if (V > 1 && w && wvec) {
 #pragma unroll
         for (int k = 0; k < V; k += 4) {
-          const float4 v = c < D ? __ldg(reinterpret_cast<const float4*>(w + c + k)) : make_float4(0.f, 0.f, 0.f, 0.f);
+          const float4 v = c < D ? *reinterpret_cast<const float4*>(w + c + k) : make_float4(0.f, 0.f, 0.f, 0.f);
           x[i * V + k] = v.x; x[(i * V + k + 1) % N] = v.y; x[(i * V + k + 2) % N] = v.z; x[(i * V + k + 3) % N] = v.w;
         }
       } else {
 #pragma unroll
-        for (int k = 0; k < V; ++k) x[i * V + k] = w ? (c < D ? __ldg(w + c + k) : 0.f) : otherwise;
+        for (int k = 0; k < V; ++k) x[i * V + k] = w ? (c < D ? w[c + k] : 0.f) : otherwise;
       }
     }
   }

@@ -70,11 +70,11 @@ __device__ __forceinline__ void finish(const GemmArgs& A, float (&v)[NC], uint4*
   if (A.bias) {
     if (c0 + NC <= A.rowsB && (reinterpret_cast<uintptr_t>(A.bias) & 15) == 0) {
 #pragma unroll
-      for (int u = 0; u < NC / 8; ++u) add8(u, __ldg(reinterpret_cast<const uint4*>(A.bias + c0) + u));
+      for (int u = 0; u < NC / 8; ++u) add8(u, reinterpret_cast<const uint4*>(A.bias + c0)[u]);
     } else {
 #pragma unroll
       for (int i = 0; i < NC; ++i)
-        if (c0 + i < A.rowsB) v[i] += bf_value(__ldg(reinterpret_cast<const unsigned short*>(A.bias) + c0 + i));
+        if (c0 + i < A.rowsB) v[i] += bf_value(reinterpret_cast<const unsigned short*>(A.bias)[c0 + i]);
     }
   }
   if (A.z) {
@@ -129,13 +129,13 @@ struct LinearEpilogue {
   __device__ __forceinline__ void fetch(const Args&, int, int) {}
   __device__ __forceinline__ void begin(const Args& A, int r0, int c0, int lane) {
     bias = 0.f;
-    if (SWAP && A.bias && r0 + lane < A.rowsA) bias = bf_value(__ldg(reinterpret_cast<const unsigned short*>(A.bias) + r0 + lane));
+    if (SWAP && A.bias && r0 + lane < A.rowsA) bias = bf_value(reinterpret_cast<const unsigned short*>(A.bias)[r0 + lane]);
     if (!SWAP && A.bias && c0 < A.rowsB) asm volatile("prefetch.global.L1 [%0];" ::"l"(A.bias + c0));
   }
   template <int NC>
   __device__ __forceinline__ void chunk(const Args& A, float (&v)[NC], uint4* stage, int r0, int c0, int lane) {
     if constexpr (UNIT) {
-      const float unit = __ldg(A.unit);
+      const float unit = *A.unit;
 #pragma unroll
       for (int i = 0; i < NC; ++i) v[i] *= unit;
     }
@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(256, 6) rows_kernel(const __grid_constant__ Jo
 }
 
 // dbias from the chunks' sums: 32 columns and eight lanes of chunks per CTA
-__global__ void __launch_bounds__(256) columns_kernel(const float* __restrict__ sums, int64_t chunks, int cols, bf16* __restrict__ out) {
+__global__ void __launch_bounds__(256) columns_kernel(const float* sums, int64_t chunks, int cols, bf16* out) {
   __shared__ float sh[8][33];
   start_dependents();
   wait_for_previous();
@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(256) columns_kernel(const float* __restrict__ 
   float s = 0.f;
   if (c < cols) {
 #pragma unroll 8
-    for (int64_t i = r; i < chunks; i += 8) s += __ldg(sums + i * cols + c);
+    for (int64_t i = r; i < chunks; i += 8) s += sums[i * cols + c];
   }
   sh[r][lane] = s;
   __syncthreads();

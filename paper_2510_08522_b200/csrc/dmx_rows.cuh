@@ -65,6 +65,8 @@ __device__ __forceinline__ void load_if(unsigned short& r, const void* p, bool l
 
 // Launched as programmatic dependents: what needs no data is set up while the kernel before still runs; then all of its
 // (and earlier) writes are waited for. The kernel after may begin likewise.
+// Inputs are read behind the wait and with ordinary loads: a read-only one promises that its data do not change while the kernel is resident, which is
+// while the one before still writes them.
 __device__ __forceinline__ void start_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
