@@ -633,7 +633,8 @@ int dmx_embedding_backward(int64_t N, int64_t V, int64_t D, int id_bytes, const 
  * accumulation on the tensor cores).
  *   forward    z = x W^T + bias,  lse[n] = log(sum over v of exp(z[n, v])),  loss[n] = lse[n] - z[n, target[n]]     x: N x D, W: V x D
  *   backward   G[n, v] = (exp(z[n, v] - lse[n]) - [v = target[n]]) * dloss[n],  dx = G W,  dW = G^T x,  dbias = column sums of G
- * A row whose target lies outside 0..V-1 (an ignored place) has loss 0 and no gradient; its lse is computed all the same. backward
+ * A row whose target lies outside 0..V-1 (an ignored place) has loss 0 and no gradient; its lse is computed all the same. No loss is
+ * negative: it is log(sum of exponentials of the distances from the largest logit), at least log 1, and the largest logit's lead over the target's. backward
  * computes the logits again and goes through the vocabulary in pieces: the workspace holds a piece of G (512 MB at most, or 256 words), and,
  * where there are several, dx in fp32. Everything up to a store is fp32, with one exception: G is rounded to bf16 before the two
  * products (the tensor cores take 16-bit operands), in units of the largest finite |dloss|'s significand; dbias is summed from the unrounded G. Exponentials are good to 2 ulp and 0 below 2^-126; the tensor cores'
