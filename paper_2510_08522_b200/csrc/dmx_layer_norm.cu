@@ -426,6 +426,8 @@ __global__ void __launch_bounds__(1024) columns_kernel(const float* part, int64_
   start_dependents();
   wait_for_previous();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane, which = blockIdx.y;
+  float* out = which ? dbias : dweight;
+  if (!out) return;
   float s = 0.f;
   if (c < D) {
 #pragma unroll 8
@@ -436,8 +438,7 @@ __global__ void __launch_bounds__(1024) columns_kernel(const float* part, int64_
   if (warp == 0 && c < D) {
     s = 0.f;
     for (int k = 0; k < 32; ++k) s += sh[k][lane];
-    float* out = which ? dbias : dweight;
-    if (out) out[c] = s;
+    out[c] = s;
   }
 }
 

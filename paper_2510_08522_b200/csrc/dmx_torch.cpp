@@ -362,25 +362,28 @@ PyObject* layer_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// dy, x, mean, rstd, weight, add, out -> (dx, dweight, dbias)
+// dy, x, mean, rstd, weight, add, out, need (bits: dweight, dbias) -> (dx, dweight, dbias)
 PyObject* layer_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded([&]() -> PyObject* {
-    need(n == 7);
+    need(n == 8);
     const at::Tensor &dy = tensor(a[0]), &x = tensor(a[1]), &mean = tensor(a[2]), &rstd = tensor(a[3]);
     const at::Tensor *w = maybe(a[4]), *add = maybe(a[5]), *given = maybe(a[6]);
+    const long want = whole(a[7]);
     const int type = type_of(x);
     const Flat X = flat(x), G = same_rows(dy, x), E = add ? same_rows(*add, x) : X;
     const int D = layer_width(X);
     const float *wp = vector(w, x, D), *mp = vector(&mean, x, X.M), *rp = vector(&rstd, x, X.M);
-    const int64_t bytes = layer_workspace(X.M, D, type);
+    const int64_t bytes = want ? layer_workspace(X.M, D, type) : 0;
     if (bytes < 0) refuse(bytes);
     Call call(x);
     at::Tensor dx = given ? *given : at::empty(x.sizes(), x.options());
     const Flat O = same_rows(dx, x);
-    at::Tensor dw = at::empty({D}, x.options().dtype(at::kFloat)), db = at::empty({D}, x.options().dtype(at::kFloat));
+    at::Tensor dw, db;
+    if (want & 1) dw = at::empty({D}, x.options().dtype(at::kFloat));
+    if (want & 2) db = at::empty({D}, x.options().dtype(at::kFloat));
     at::Tensor ws = workspace(bytes, x);
-    const int rc = layer_backward(X.M, D, type, in(&dy), G.ld, in(&x), X.ld, mp, rp, wp, in(add), E.ld, out(&dx), O.ld, static_cast<float*>(out(&dw)),
-                                  static_cast<float*>(out(&db)), start_of(ws), bytes, call.stream);
+    const int rc = layer_backward(X.M, D, type, in(&dy), G.ld, in(&x), X.ld, mp, rp, wp, in(add), E.ld, out(&dx), O.ld,
+                                  dw.defined() ? static_cast<float*>(out(&dw)) : nullptr, db.defined() ? static_cast<float*>(out(&db)) : nullptr, start_of(ws), bytes, call.stream);
     if (rc != DMX_OK) refuse(rc);
     written(given);
     return tuple(&dx, &dw, &db);

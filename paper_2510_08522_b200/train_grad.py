@@ -63,7 +63,7 @@ class LayerNorm(torch.autograd.Function):
     def backward(ctx, dy, *_):
         x, mean, rstd, weight = ctx.saved_tensors
         need_x, need_w, need_b, _ = ctx.needs_input_grad
-        dx, dw, db = T.layer_norm_backward(dy.contiguous(), x, mean, rstd, weight)
+        dx, dw, db = T.layer_norm_backward(dy.contiguous(), x, mean, rstd, weight, need=(need_w, need_b))
         return dx if need_x else None, dw.view(weight.shape) if need_w else None, db.view(ctx.bias_shape) if need_b else None, None
 
 

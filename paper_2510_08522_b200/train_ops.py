@@ -267,10 +267,11 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None):
     return LayerNorm.apply(x, weight, bias, eps)
 
 
-def layer_norm_backward(dy, x, mean, rstd, weight=None, add=None, out=None):
+def layer_norm_backward(dy, x, mean, rstd, weight=None, add=None, out=None, need=(True, True)):
     """Gradient of layer_norm from its saved statistics -> (dx, dweight, dbias). add: a tensor that is added to dx before it
-    is rounded (the gradient that reaches x past the norm). out may be dy, x or add."""
-    r = (_fast or _module()).layer_norm_backward(dy, x, mean, rstd, weight, add, out)
+    is rounded (the gradient that reaches x past the norm). out may be dy, x or add. need: whether dweight and dbias are wanted; one that is
+    not is None (without either there are no sums over rows: no workspace and one launch less)."""
+    r = (_fast or _module()).layer_norm_backward(dy, x, mean, rstd, weight, add, out, (1 if need[0] else 0) + (2 if need[1] else 0))
     return r if r.__class__ is tuple else _refuse("layer_norm_backward", r)
 
 
