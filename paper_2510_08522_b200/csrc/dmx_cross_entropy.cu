@@ -307,8 +307,9 @@ struct AddEpilogue {
   typedef AddArgs Args;
   static constexpr int kStaging = 2048, kOwnShared = 0;
   static constexpr bool kRanged = false;
+  float times;
   __device__ __forceinline__ void fetch(const Args&, int, int) {}
-  __device__ __forceinline__ void begin(const Args&, int, int, int) {}
+  __device__ __forceinline__ void begin(const Args& A, int, int, int) { times = A.last ? *A.unit : 1.f; }
   template <int NC>
   __device__ __forceinline__ void chunk(const Args& A, float (&v)[NC], uint4* stage, int r0, int c0, int lane) {
     float* at = A.sums + ((int64_t)(r0 >> 5) * (A.tilesB * (BN / 32)) + (c0 >> 5)) * 1024 + lane;
@@ -321,7 +322,6 @@ struct AddEpilogue {
       for (int i = 0; i < NC; ++i) __stcs(at + i * 32, v[i]);
       return;
     }
-    const float times = *A.unit;
 #pragma unroll
     for (int i = 0; i < NC; ++i) v[i] *= times;
 #pragma unroll

@@ -125,17 +125,17 @@ struct LinearEpilogue {
   typedef GemmArgs Args;
   static constexpr int kStaging = 2048, kOwnShared = 0;
   static constexpr bool kRanged = false;
-  float bias;
+  float bias, unit;
   __device__ __forceinline__ void fetch(const Args&, int, int) {}
   __device__ __forceinline__ void begin(const Args& A, int r0, int c0, int lane) {
     bias = 0.f;
+    if (UNIT) unit = *A.unit;                  // (here: read for each chunk it would be waited for, 64 x 30522 x 1024's dW 8 us)
     if (SWAP && A.bias && r0 + lane < A.rowsA) bias = bf_value(reinterpret_cast<const unsigned short*>(A.bias)[r0 + lane]);
     if (!SWAP && A.bias && c0 < A.rowsB) asm volatile("prefetch.global.L1 [%0];" ::"l"(A.bias + c0));
   }
   template <int NC>
   __device__ __forceinline__ void chunk(const Args& A, float (&v)[NC], uint4* stage, int r0, int c0, int lane) {
     if constexpr (UNIT) {
-      const float unit = *A.unit;
 #pragma unroll
       for (int i = 0; i < NC; ++i) v[i] *= unit;
     }
