@@ -635,8 +635,7 @@ int dmx_embedding_backward(int64_t N, int64_t V, int64_t D, int id_bytes, const 
  *   backward   G[n, v] = (exp(z[n, v] - lse[n]) - [v = target[n]]) * dloss[n],  dx = G W,  dW = G^T x,  dbias = column sums of G
  * A row whose target lies outside 0..V-1 (an ignored place) has loss 0 and no gradient; its lse is computed all the same. No loss is
  * negative: it is log(sum of exponentials of the distances from the largest logit), at least log 1, and the largest logit's lead over the target's. backward
- * computes the logits again and goes through the vocabulary in pieces: the workspace holds a piece of G (512 MB at most, or 256 words), and,
- * where there are several, dx in fp32. Everything up to a store is fp32, with one exception: G is rounded to bf16 before the two
+ * computes the logits again and goes through the vocabulary in pieces. Everything up to a store is fp32, with one exception: G is rounded to bf16 before the two
  * products (the tensor cores take 16-bit operands), in units of the largest finite |dloss|'s significand; dbias is summed from the unrounded G. Exponentials are good to 2 ulp and 0 below 2^-126; the tensor cores'
  * sums of D products may truncate at every step (lse of D = 4000 is good to 5e-6 of the logits' size). Logits
  * of -inf (a bias of -inf) are words that do not occur; a logit of +inf or NaN makes its row's loss and gradient NaN, as does a row without
@@ -648,8 +647,11 @@ int dmx_embedding_backward(int64_t N, int64_t V, int64_t D, int id_bytes, const 
  *   target     N integers of target_bytes (4 or 8) bytes, aligned to their size
  *   loss, lse, dloss   fp32, N entries; dloss with a stride in elements (0: one value for all rows)
  *   dx, dw, dbias   each may be NULL and is then not computed
- *   workspace  at least dmx_cross_entropy_workspace(...) (8 bytes for each row and 64 to 256 words) / dmx_cross_entropy_backward_workspace(...) bytes for
- *              the same arguments, 256-byte aligned, contents undefined
+ *   workspace  at least dmx_cross_entropy_workspace(...) / dmx_cross_entropy_backward_workspace(...) bytes for the same arguments, 256-byte aligned,
+ *              contents undefined. Forward: 8 bytes for each row and 64 to 256 words, 4 for each row. Backward: for dx or dw a piece of G (bf16, 512 MB at
+ *              most, or 256 words), for dbias fp32 sums over 32 rows each of that piece, for dx fp32 sums (N x D, both rounded up to 256) where there are several pieces, and
+ *              with one the parts of products that are cut into ranges. Both: the operands that are laid out. dmx_cross_entropy_backward_workspace counts
+ *              all outputs, ..._for those of `outputs` (1 for dx, 2 for dw, 4 for dbias, added): enough for a call that gives the others as NULL.
  *   dmx_cross_entropy_plan   for inspection and tests (no device needed): how a problem is cut. plan (HOST, 11 entries) receives forward's tile width, pairing
  *              of CTAs (0/1) and tiles across the vocabulary; the pieces and a piece's words; the gradient's first product's tile width and pairing; of
  *              dx and of dW the tile width and ranges of k that are added afterwards (0: none)
@@ -662,6 +664,7 @@ int dmx_cross_entropy_forward(int64_t N, int64_t V, int64_t D, const void* x, in
                               const void* bias, int target_bytes, const void* target, float* loss, float* lse, void* workspace,
                               int64_t workspace_bytes, void* cuda_stream);
 int64_t dmx_cross_entropy_backward_workspace(int64_t N, int64_t V, int64_t D, const void* x, int64_t ldx, const void* w, int64_t ldw);
+int64_t dmx_cross_entropy_backward_workspace_for(int64_t N, int64_t V, int64_t D, const void* x, int64_t ldx, const void* w, int64_t ldw, int outputs);
 int dmx_cross_entropy_backward(int64_t N, int64_t V, int64_t D, const float* dloss, int64_t dloss_stride, const void* x, int64_t ldx,
                                const void* w, int64_t ldw, const void* bias, int target_bytes, const void* target,
                                const float* lse, void* dx, int64_t lddx, void* dw, int64_t lddw, void* dbias, void* workspace,

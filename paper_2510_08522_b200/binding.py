@@ -30,7 +30,7 @@ EXPORTS = ("dmx_create", "dmx_state_len", "dmx_step", "dmx_step_adam", "dmx_step
            "dmx_group_norm_plan", "dmx_linear_plan",
            "dmx_layer_norm_workspace", "dmx_layer_norm_forward", "dmx_layer_norm_backward",
            "dmx_embedding_forward", "dmx_embedding_backward_workspace", "dmx_embedding_backward",
-           "dmx_cross_entropy_workspace", "dmx_cross_entropy_forward", "dmx_cross_entropy_backward_workspace", "dmx_cross_entropy_backward",
+           "dmx_cross_entropy_workspace", "dmx_cross_entropy_forward", "dmx_cross_entropy_backward_workspace", "dmx_cross_entropy_backward_workspace_for", "dmx_cross_entropy_backward",
            "dmx_cross_entropy_plan")
 CTL_ACTIONS = (-100, -25, 0, 25, 100)
 
@@ -157,6 +157,8 @@ def lib():
         for f in (L.dmx_cross_entropy_workspace, L.dmx_cross_entropy_backward_workspace):
             f.argtypes = [i64, i64, i64, vp, i64, vp, i64]
             f.restype = i64
+        L.dmx_cross_entropy_backward_workspace_for.argtypes = [i64, i64, i64, vp, i64, vp, i64, i32]
+        L.dmx_cross_entropy_backward_workspace_for.restype = i64
         L.dmx_cross_entropy_plan.argtypes = [i64, i64, i64, ctypes.POINTER(i64)]
         L.dmx_cross_entropy_plan.restype = i32
         L.dmx_cross_entropy_forward.argtypes = [i64, i64, i64, vp, i64, vp, i64, vp, i32, vp, vp, vp, vp, i64, vp]

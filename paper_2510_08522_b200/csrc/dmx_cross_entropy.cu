@@ -199,7 +199,7 @@ struct SlopeArgs : GemmShape {
   float* unit;                    // there already, or (few rows) found by every warp on its own while the first tile is on its way
   int find_unit;
   int64_t stride;                 // of dloss: 1 or 0
-  bf16* g;
+  bf16* g;                        // or NULL: the columns' sums alone
   int64_t ldg;
   float* columns;                 // [rows / 32][piece]: sums over 32 rows, or NULL
 };
@@ -269,11 +269,13 @@ struct SlopeEpilogue {
 #pragma unroll
       for (int i = 0; i < NC; ++i) v[i] -= place == (unsigned)i ? scale : 0.f;
     }
+    if (A.g) {
 #pragma unroll
-    for (int u = 0; u < NC / 8; ++u)
-      *unit(stage, lane, u) = make_uint4(pack2(v[8 * u], v[8 * u + 1]), pack2(v[8 * u + 2], v[8 * u + 3]), pack2(v[8 * u + 4], v[8 * u + 5]),
-                                         pack2(v[8 * u + 6], v[8 * u + 7]));
-    store_tile<32, NC>(A.g, A.ldg, A.vec, stage, r0, A.rowsA, c0, A.rowsB, lane);
+      for (int u = 0; u < NC / 8; ++u)
+        *unit(stage, lane, u) = make_uint4(pack2(v[8 * u], v[8 * u + 1]), pack2(v[8 * u + 2], v[8 * u + 3]), pack2(v[8 * u + 4], v[8 * u + 5]),
+                                           pack2(v[8 * u + 6], v[8 * u + 7]));
+      store_tile<32, NC>(A.g, A.ldg, A.vec, stage, r0, A.rowsA, c0, A.rowsB, lane);
+    }
     if (A.columns) {
       // lane i ends with column i's sum: in every step half of the columns go to the lane across
       static_assert(NC == 32, "a column per lane");
@@ -491,7 +493,8 @@ struct BackPlan {
   int64_t pieces, words, g, columns, sums, total;      // sums: of dx over the pieces, or a cut product's parts
   Cut dx, dw;                                          // with one piece
 };
-BackPlan back_plan(const Matrix& x, const Matrix& w) {
+enum { kDx = 1, kDw = 2, kDbias = 4 };                 // outputs
+BackPlan back_plan(const Matrix& x, const Matrix& w, int outputs) {
   const int64_t N = x.rows, V = w.rows, D = x.cols;
   BackPlan p;
   int64_t most = ((int64_t)1 << 29) / (2 * N) / 256 * 256;
@@ -500,14 +503,14 @@ BackPlan back_plan(const Matrix& x, const Matrix& w) {
   p.words = ((V + p.pieces - 1) / p.pieces + 255) / 256 * 256;
   p.pieces = (V + p.words - 1) / p.words;
   const int64_t cols = p.words < V ? p.words : V;
-  p.g = pad256(N * pad8(cols) * 2);
-  p.columns = pad256((N + 31) / 32 * cols * 4);
+  p.g = outputs & (kDx | kDw) ? pad256(N * pad8(cols) * 2) : 0;
+  p.columns = outputs & kDbias ? pad256((N + 31) / 32 * cols * 4) : 0;
   p.dx = p.dw = Cut{0, 0, 0};
   if (p.pieces == 1) {
-    p.dx = cut_of(N, D, V, 0);
-    p.dw = cut_of(V, D, N, 1);
+    if (outputs & kDx) p.dx = cut_of(N, D, V, 0);
+    if (outputs & kDw) p.dw = cut_of(V, D, N, 1);
   }
-  p.sums = p.pieces == 1 ? (p.dx.bytes > p.dw.bytes ? p.dx.bytes : p.dw.bytes) : ((N + 255) / 256 * 256) * ((D + 255) / 256 * 256) * 4;
+  p.sums = p.pieces == 1 ? (p.dx.bytes > p.dw.bytes ? p.dx.bytes : p.dw.bytes) : outputs & kDx ? ((N + 255) / 256 * 256) * ((D + 255) / 256 * 256) * 4 : 0;
   p.total = 256 + p.g + p.columns + p.sums + laid_out_bytes(x) + laid_out_bytes(w);
   return p;
 }
@@ -555,9 +558,13 @@ int dmx_cross_entropy_forward(int64_t N, int64_t V, int64_t D, const void* x, in
   return start(dim3((unsigned)((N + 31) / 32)), st, join_kernel, (const float2*)A.part, (int)p.parts, (int)N, (int)V, (const float*)A.hit, target, A.wide_target, loss, lse);
 }
 
+int64_t dmx_cross_entropy_backward_workspace_for(int64_t N, int64_t V, int64_t D, const void* x, int64_t ldx, const void* w, int64_t ldw, int outputs) {
+  if (!sizes_ok(N, V, D) || outputs < 0 || outputs > (kDx | kDw | kDbias)) return DMX_ERR_ARG;
+  return N == 0 || outputs == 0 ? 0 : back_plan(matrix(x, N, D, ldx), matrix(w, V, D, ldw), outputs).total;
+}
+
 int64_t dmx_cross_entropy_backward_workspace(int64_t N, int64_t V, int64_t D, const void* x, int64_t ldx, const void* w, int64_t ldw) {
-  if (!sizes_ok(N, V, D)) return DMX_ERR_ARG;
-  return N == 0 ? 0 : back_plan(matrix(x, N, D, ldx), matrix(w, V, D, ldw)).total;
+  return dmx_cross_entropy_backward_workspace_for(N, V, D, x, ldx, w, ldw, kDx | kDw | kDbias);
 }
 
 int dmx_cross_entropy_backward(int64_t N, int64_t V, int64_t D, const float* dloss, int64_t dloss_stride, const void* x, int64_t ldx, const void* w, int64_t ldw,
@@ -576,7 +583,7 @@ int dmx_cross_entropy_backward(int64_t N, int64_t V, int64_t D, const float* dlo
   if (!dx && !dw && !dbias) return DMX_OK;
   if (!x || !w || !target || !lse || !dloss) return DMX_ERR_ARG;
   Matrix a = matrix(x, N, D, ldx), b = matrix(w, V, D, ldw);
-  const BackPlan p = back_plan(a, b);
+  const BackPlan p = back_plan(a, b, (dx ? kDx : 0) | (dw ? kDw : 0) | (dbias ? kDbias : 0));
   if (workspace_bytes < p.total || !workspace) return DMX_ERR_ARG;
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   float* unit = reinterpret_cast<float*>(ws);
@@ -599,7 +606,7 @@ int dmx_cross_entropy_backward(int64_t N, int64_t V, int64_t D, const float* dlo
     A.rowsA = (int)N; A.rowsB = (int)words; A.kblocks = (int)((D + kBK - 1) / kBK);
     A.bias = bias ? static_cast<const bf16*>(bias) + first : nullptr; A.target = target; A.wide_target = target_bytes == 8;
     A.first = (int)first; A.vocabulary = (int)V; A.lse = lse; A.dloss = dloss; A.unit = unit; A.find_unit = find_unit && first == 0; A.stride = N > 1 ? dloss_stride : 0;
-    A.g = g; A.ldg = pad8(words); A.vec = 1; A.columns = dbias ? columns : nullptr;
+    A.g = dx || dw ? g : nullptr; A.ldg = pad8(words); A.vec = 1; A.columns = dbias ? columns : nullptr;
     rc = product_rows<SlopeEpilogue>(a, piece, A, choose_rows(N, words, D, kSlopeWeight), st);
     if (rc == DMX_OK && dbias)
       rc = start(dim3((unsigned)((words + 31) / 32)), 1024, st, columns_kernel, (const float*)columns, (int)((N + 31) / 32), (int)words, (const float*)unit, static_cast<bf16*>(dbias) + first);
@@ -623,7 +630,7 @@ int dmx_cross_entropy_plan(int64_t N, int64_t V, int64_t D, int64_t* plan) {
   if (!sizes_ok(N, V, D) || N < 1 || !plan) return DMX_ERR_ARG;
   const Matrix x = {nullptr, N, D, D}, w = {nullptr, V, D, D};
   const ForwardPlan f = forward_plan(x, w);
-  const BackPlan b = back_plan(x, w);
+  const BackPlan b = back_plan(x, w, kDx | kDw | kDbias);
   const Choice s = choose_rows(N, b.words < V ? b.words : V, D, kSlopeWeight);
   const int64_t values[11] = {f.choice.bn, f.choice.pair, f.parts, b.pieces, b.words, s.bn, s.pair, b.dx.bn, b.dx.ranges, b.dw.bn, b.dw.ranges};
   for (int i = 0; i < 11; ++i) plan[i] = values[i];

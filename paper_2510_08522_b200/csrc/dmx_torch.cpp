@@ -39,7 +39,7 @@ decltype(&dmx_embedding_backward_workspace) lookup_workspace;
 decltype(&dmx_embedding_backward) lookup_backward;
 decltype(&dmx_cross_entropy_workspace) loss_workspace;
 decltype(&dmx_cross_entropy_forward) loss_forward;
-decltype(&dmx_cross_entropy_backward_workspace) loss_backward_workspace;
+decltype(&dmx_cross_entropy_backward_workspace_for) loss_backward_workspace;
 decltype(&dmx_cross_entropy_backward) loss_backward;
 
 struct Refused {
@@ -504,7 +504,7 @@ PyObject* cross_entropy_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
     bf16_vector(b, x, V);
     const float* lp = vector(&lse, x, N);
     const int tb = id_bytes(target, x);
-    const int64_t bytes = loss_backward_workspace(N, V, D, in(&x), X.ld, in(&w), W.ld);
+    const int64_t bytes = loss_backward_workspace(N, V, D, in(&x), X.ld, in(&w), W.ld, (int)(want & 7));
     if (bytes < 0) refuse(bytes);
     Call call(x);
     const at::Tensor dense = target.contiguous();

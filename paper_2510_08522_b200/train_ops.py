@@ -230,7 +230,7 @@ def _module():
             L.dmx_linear_backward_workspace, L.dmx_linear_backward, L.dmx_adamw_grad_norm, L.dmx_adamw_step,
             L.dmx_layer_norm_workspace, L.dmx_layer_norm_forward, L.dmx_layer_norm_backward, L.dmx_embedding_forward,
             L.dmx_embedding_backward_workspace, L.dmx_embedding_backward, L.dmx_cross_entropy_workspace, L.dmx_cross_entropy_forward,
-            L.dmx_cross_entropy_backward_workspace, L.dmx_cross_entropy_backward)])
+            L.dmx_cross_entropy_backward_workspace_for, L.dmx_cross_entropy_backward)])
         _fast = m
     return _fast
 
