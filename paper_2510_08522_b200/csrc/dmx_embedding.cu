@@ -7,7 +7,8 @@
 // CTA counts its keys' digits, then moves its keys. Other CTAs of the second write the table's zeros meanwhile. Then every warp sums a chunk of the sorted
 // tokens over its columns, row after row in registers: each gradient row is read once, each row of the table written once. A row whose
 // tokens reach over chunks leaves fp32 sums, one per chunk, which a last launch joins. Work is cut by tokens, not by rows: how
-// often a token comes does not matter. Nothing is added atomically but whole numbers; the order of all sums is fixed by the shape and the ids.
+// often a token comes does not matter. Nothing is added atomically but whole numbers; the order of all sums is fixed by the ids, the sizes and types, and by
+// whether rows are 16-byte aligned (which says how many columns a lane takes, and so where chunks begin).
 // Measured on B200 (replayed in graphs, data mostly in L2): forward of 32768 x 1024 bf16 17 us (20.2 at the measured copy rate), unaligned 29 us. Gradient of 16384
 // tokens in 30522 x 1024 bf16 36 us (14.9): six launches in a row, sort 14 us and 5 more for zeros meanwhile, sums 11, joins 6; 64 tokens 8 us; 65536 tokens
 // added to 50257 x 771 fp32 80 us (46).
@@ -20,7 +21,10 @@ namespace {
 
 using namespace dmx_rows;
 
-constexpr int kSortCtas = 128, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kDigits = 256, kKept = 8, kFew = 4, kFewTokens = kFew * kSortThreads, kJoinCtas = 148 * 12;      // (CTAs: at most)
+constexpr int kSortCtas = 128, kSortThreads = 1024, kSortWarps = kSortThreads / 32, kDigits = 256;      // (CTAs: at most)
+constexpr int kKept = 8;                                   // keys a lane that scatter_kernel keeps
+constexpr int kFew = 4, kFewTokens = kFew * kSortThreads;  // keys a thread that sort_few_kernel keeps
+constexpr int kJoinCtas = 148 * 12;                        // at most
 
 // ---------------------------------------------------------------------------------------------- forward
 
@@ -344,7 +348,7 @@ struct SumArgs {
   unsigned* crossing;              // how many chunks have a last row that begins there and goes on, then (from the 8th byte) which, and the row, in any order
   float* part;                     // [chunks][2][D]: what a chunk's first and last row got, where they go on
   int64_t N, V, lddy, ldout;
-  int D, chunk, accumulate;        // chunk: tokens, a multiple of 32
+  int D, chunk, accumulate;        // chunk: tokens, a multiple of 8
   float scale;
 };
 
@@ -496,7 +500,7 @@ __global__ void __launch_bounds__(128) join_kernel(const __grid_constant__ SumAr
   const int64_t chunks = (A.N + A.chunk - 1) / A.chunk;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slices = (A.D + 127) / 128;
   const uint2* list = reinterpret_cast<const uint2*>(A.crossing) + 1;
-  uint2 entry = list[blockIdx.x / slices];                 // (on its way with the count; there is room for every chunk)
+  uint2 entry = list[blockIdx.x / slices];                 // (on its way with the count; there is room for every chunk, and no more CTAs than those take)
   const int64_t units = (int64_t)*A.crossing * slices;
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
     if (unit != blockIdx.x) entry = list[unit / slices];
@@ -554,7 +558,7 @@ BackPlan back_plan(int64_t N, int64_t D) {
   p.keys = pad256(N * 8);
   const int64_t chunk = chunk_of(N, D, 8), chunk4 = chunk_of(N, D, 4), least = chunk < chunk4 ? chunk : chunk4;
   p.part = pad256((N + least - 1) / least * 2 * D * (int64_t)sizeof(float));
-  p.crossing = pad256((1 + (N + least - 1) / least) * 8 + kJoinCtas * 8);      // (the join reads ahead)
+  p.crossing = pad256((1 + (N + least - 1) / least) * 8);
   p.counts = kSortCtas * kDigits * 4;
   p.total = 2 * p.keys + p.part + p.crossing + p.counts;
   return p;
