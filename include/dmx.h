@@ -590,7 +590,7 @@ int dmx_linear_status(int* errors);
  *   dweight, dbias     fp32, D entries, or NULL
  *   workspace          backward, if dweight or dbias is wanted: at least dmx_layer_norm_workspace(...) bytes, 16-byte aligned,
  *                      contents undefined
- * Results are bitwise reproducible. y may be x, and dx may be dy, x or add, with the same strides (unless rows repeat). M = 0 gives dweight = 0 and
+ * Results are bitwise reproducible (for rows that are 16-byte aligned and for others: sums have another order there). y may be x, and dx may be dy, x or add, with the same strides (unless rows repeat). M = 0 gives dweight = 0 and
  * dbias = 0.
  * Errors: DMX_ERR_ARG (D < 1, D > DMX_LN_MAX_WIDTH, M >= 2^40, strides, eps < 0, null pointers, workspace too small), DMX_ERR_ALIGN,
  * DMX_ERR_CUDA.
@@ -609,7 +609,8 @@ int dmx_layer_norm_backward(int64_t M, int D, int dtype, const void* dy, int64_t
  *   forward    y[n] = scale * table[ids[n]]                       table: V x D, y: N x D (DMX_F32 or DMX_BF16, both of dtype)
  *   backward   dtable[v] = scale * (sum over n with ids[n] = v of dy[n])   (+ dtable[v] if accumulate)
  * An id outside 0..V-1 (padding, an ignored place) gives a row of zeros and takes no gradient. Sums are fp32, in the order of n within
- * chunks of neighbouring places in the sorted order; results are rounded once and are bitwise reproducible.
+ * chunks of neighbouring places in the sorted order (where they begin goes by the sizes, the types and whether rows are 16-byte aligned); results are
+ * rounded once and are bitwise reproducible.
  *   ids          N integers of id_bytes (4 or 8) bytes, aligned to their size
  *   dtable       V x D of out_dtype. Without accumulate every row is written, zeros where no token is. With it rows without
  *                a token are neither read nor written (a table tied to a head whose gradient is there already).
@@ -633,7 +634,8 @@ int dmx_embedding_backward(int64_t N, int64_t V, int64_t D, int id_bytes, const 
  * accumulation on the tensor cores).
  *   forward    z = x W^T + bias,  lse[n] = log(sum over v of exp(z[n, v])),  loss[n] = lse[n] - z[n, target[n]]     x: N x D, W: V x D
  *   backward   G[n, v] = (exp(z[n, v] - lse[n]) - [v = target[n]]) * dloss[n],  dx = G W,  dW = G^T x,  dbias = column sums of G
- * A row whose target lies outside 0..V-1 (an ignored place) has loss 0 and no gradient; its lse is computed all the same. No loss is
+ * A row whose target lies outside 0..V-1 (an ignored place) has loss 0 and no gradient; its lse is computed all the same. (dW
+ * multiplies its x by zeros: that x has to be finite, or dW is NaN where it is not.) No loss is
  * negative: it is log(sum of exponentials of the distances from the largest logit), at least log 1, and the largest logit's lead over the target's. backward
  * computes the logits again and goes through the vocabulary in pieces. Everything up to a store is fp32, with one exception: G is rounded to bf16 before the two
  * products (the tensor cores take 16-bit operands), in units of the largest finite |dloss|'s significand; dbias is summed from the unrounded G. Exponentials are good to 2 ulp and 0 below 2^-126; the tensor cores'

@@ -12,12 +12,12 @@
 // the significand of the largest |dloss|, by which the products' epilogues multiply: where all rows that count have one dloss (a mean), a
 // target's entry is 1 - p times a power of two. (Units with the exponent would let rows of far smaller dloss underflow.)
 // With dloss inside, the entries near -dloss of all rows were rounded the same way: dx and dW were off by 0.33 % in the mean square, with
-// the unit 0.17 to 0.20 %, where one rounding of the result alone gives 0.17 %.
+// the unit 0.17 to 0.20 %, where one rounding of the result alone gives 0.17 %. (Few rows or words: a result may be off by two roundings, 0.2 to 0.3 % in the mean square.)
 // Bound: the tensor cores, 2 N V D operations forward and 6 N V D backward (the logits are computed again). With D up to some hundred the epilogues: a
 // pair's tile of 65536 logits takes about 2.5 us whatever D is (taking them out of TMEM alone 1.5), one CTA's of 32768 2.1 us, two at a time.
-// Measured on B200, 8192 x 30522 x 1024 with bias: forward 320 us in bursts at full clock (1.6 PFLOP/s; floor 299 at the measured 1715), 385 us back to back under
-// the power limit; backward 1120 / 1340 us (896 / 1062 at the measured 1715 / 1447; storing G takes 58 us, db 46, dx's last wave of tiles 40). 128 x 10 x 64 forward 3.5 us,
-// 777 x 1000 x 513 backward 25 us, 8192 x 30522 x 256 forward 113, backward 414 us.
+// Measured on B200, 8192 x 30522 x 1024 with bias: forward 315 us in bursts at full clock (1.6 PFLOP/s; floor 299 at the measured 1715), 374 us back to back under
+// the power limit; backward 1120 / 1316 us (896 / 1062 at the measured 1715 / 1447; storing G takes 58 us, db 46, dx's last wave of tiles 40). 128 x 10 x 64 forward 3.5 us,
+// 777 x 1000 x 513 backward 25 us, 8192 x 30522 x 256 without bias forward 115, backward 428 us (with bias and dbias 131 to 150, 490 to 520).
 #include "dmx.h"
 
 #include <cuda_bf16.h>

@@ -9,9 +9,9 @@
 // tokens reach over chunks leaves fp32 sums, one per chunk, which a last launch joins. Work is cut by tokens, not by rows: how
 // often a token comes does not matter. Nothing is added atomically but whole numbers; the order of all sums is fixed by the ids, the sizes and types, and by
 // whether rows are 16-byte aligned (which says how many columns a lane takes, and so where chunks begin).
-// Measured on B200 (replayed in graphs, data mostly in L2): forward of 32768 x 1024 bf16 17 us (20.2 at the measured copy rate), unaligned 29 us. Gradient of 16384
-// tokens in 30522 x 1024 bf16 36 us (14.9): six launches in a row, sort 14 us and 5 more for zeros meanwhile, sums 11, joins 6; 64 tokens 8 us; 65536 tokens
-// added to 50257 x 771 fp32 80 us (46).
+// Measured on B200 (replayed in graphs, data mostly in L2): forward of 32768 tokens (8400 distinct) x 1024 bf16 13 us, a call among others 17
+// (13.1 at the measured copy rate), fp32 29 (26.4), unaligned 23, scaled 25. Gradient of 16384 tokens in 30522 x 1024 bf16 36 us (14.9), fp32 53 (29.9): six launches in a row, sort 14 us
+// and 5 more for zeros meanwhile, sums 11, joins 6; 64 tokens 17 us (9.7), added 10; 65536 tokens (12400 distinct) added to 50257 x 771 fp32 74 us (34).
 #include <atomic>
 #include <type_traits>
 
@@ -69,7 +69,7 @@ struct Share {
   }
 };
 
-// A warp takes 32 x W columns of four rows. Unaligned rows with four elements a lane: with one, 32768 x 1023 bf16 took 59 us, now 29.
+// A warp takes 32 x W columns of four rows. Unaligned rows with four elements a lane: with one, 32768 x 1023 bf16 took 59 us, so 29 (any ids, scaled).
 template <typename T, int W, bool WIDE>
 __global__ void __launch_bounds__(256) gather_kernel(const __grid_constant__ GatherArgs A) {
   constexpr int kRows = 4;

@@ -550,7 +550,7 @@ inline Choice choose(int64_t rowsA, int64_t rowsB, int kblocks, bool swap) {
 
 // The same for products whose tiles may have little k: a tile takes the longer of its stages and its epilogue and a quarter of the other. What
 // an epilogue takes per tile (ns) was measured on the cross entropy's sums at k = 64; slopes and plain stores take `weight` times it. A single CTA's tile of
-// 256 columns then beats a pair's: 8192 x 30522 x 256 forward 114 us against 141, at k = 1024 338 against 317.
+// 256 columns then beats a pair's: 8192 x 30522 x 256 forward without bias 114 us against 141, at k = 1024 338 against 317.
 // A pair's of 128 columns is for one wave over a long k: dx of 2048 x 30522 x 1024 takes 3 us less than single CTAs' of 128 columns.
 inline Choice choose_by_tiles(int64_t rowsA, int64_t rowsB, int kblocks, bool swap, bool splits, float weight) {
   Choice best = {0, 1, false, 0.f};

@@ -10,8 +10,8 @@
 // small second launch adds the CTAs' in a fixed order.
 // Variance: deviations from the rounded mean are summed beside their squares, and what that mean was off is taken out again:
 // a mean a million deviations away costs the variance nothing.
-// Measured on B200 (replayed in graphs, data mostly in L2): 16384 x 1024 bf16 forward 12 us (10.4 at the measured copy rate; 14 us a call among others),
-// gradient 23 us (15.6), with a residual 29 us (20.9): about 550 instructions a row and warp at eight warps per SM, of which two fifths issue.
+// Measured on B200 (replayed in graphs, data mostly in L2): 16384 x 1024 bf16 forward 12 us (10.4 at the measured copy rate; 14 us a call among others), fp32 24 us (20.9),
+// gradient 22 us (15.6), fp32 36 (31.3), without dw and db 17 and 31, with a residual 28 us (20.9): about 550 instructions a row and warp at eight warps per SM, of which two fifths issue.
 // 2999 x 771 fp32, a slice of wider rows, gradient 13 us (4.3): three rows a warp, and 4.5 us for the second launch. A third CTA per SM in backward spilled (37 us), five warps a CTA too (40 us),
 // weights loaded anew for every row cost 8 us, halves kept packed over the row's loop saved no instruction.
 #include <atomic>

@@ -318,7 +318,8 @@ def linear_backward(dy, x, weight, z=None, act="none", need=(True, True, True), 
 def linear_cross_entropy(x, weight, target, bias=None):
     """Softmax cross entropy of x @ weight.T + bias (bf16 matrices (N, D) and (V, D)) without keeping the logits -> (loss, lse), fp32 (N,):
     every row's loss, 0 where its target (int32 or int64) lies outside 0..V-1, and the logarithm of its sum of exponentials. Where an
-    input requires a gradient torch records the call (loss's gradient; lse carries none)."""
+    input requires a gradient torch records the call (loss's gradient; lse carries none). An ignored row has no gradient, but its x is multiplied by zeros
+    in the weight's: it has to be finite."""
     r = (_fast or _module()).cross_entropy(x, weight, target, bias)
     if r.__class__ is tuple:
         return r
@@ -330,7 +331,8 @@ def linear_cross_entropy(x, weight, target, bias=None):
 
 def linear_cross_entropy_backward(dloss, x, weight, target, lse, bias=None, need=(True, True, True), out=(None, None, None)):
     """Gradient of linear_cross_entropy -> (dx, dweight, dbias), those not in `need` None. dloss: fp32 (N,), also one value expanded.
-    `out`: tensors to write them to, e.g. views of a flat gradient vector."""
+    `out`: tensors to write them to, e.g. views of a flat gradient vector. exp(z - lse) - onehot is rounded to bf16 before the two products: a single
+    row's dx and dweight are off by up to two roundings to bf16, sums over many by 0.17 to 0.2 % in the mean square (0.17 % is one rounding)."""
     r = (_fast or _module()).cross_entropy_backward(dloss, x, weight, target, lse, bias, (1 if need[0] else 0) + (2 if need[1] else 0) + (4 if need[2] else 0), *out)
     return r if r.__class__ is tuple else _refuse("linear_cross_entropy_backward", r)
 
